@@ -1,7 +1,7 @@
 """The operators of an attention layer that keeps its keys and values in pages, and what each is measured on.
 
   rope      attn_rope_append:   rotary positions of q and k, and the append of k and v to the pages
-  attend    attn_paged_prefill: causal attention of a chunk of new tokens over the pages, and each row's log-sum-exp
+  attend    attn_paged_prefill: causal attention of a chunk of new tokens over the pages, and each row's log-sum-exp on request
   weights   attn_key_weights:   the attention weight every cached row gathers from the chunk
   evict     attn_evict:         the rows with the most weight, copied to fresh pages
 
@@ -29,9 +29,10 @@ def _rope(n_req, heads_q, heads_kv, d, rot, layout, lo, hi, pos, page=64, dtype=
                 prefix_lo=0, prefix_hi=200, pos=pos, page=page, dtype=dtype, scaled=scaled, shared=0, lengths=lengths)
 
 
-def _over_cache(kind, n_req, heads_q, heads_kv, d, lo, hi, prefix_lo, prefix_hi, page=64, shared=0, gate=False, lengths=0):
+def _over_cache(kind, n_req, heads_q, heads_kv, d, lo, hi, prefix_lo, prefix_hi, page=64, shared=0, gate=False,
+                lse=False, lengths=0):
     return dict(kind=kind, n_req=n_req, heads_q=heads_q, heads_kv=heads_kv, d=d, lo=lo, hi=hi, prefix_lo=prefix_lo,
-                prefix_hi=prefix_hi, page=page, shared=shared, gate=gate, lengths=lengths)
+                prefix_hi=prefix_hi, page=page, shared=shared, gate=gate, lse=lse, lengths=lengths)
 
 
 def _evict(n_req, heads_kv, d, lo, hi, keep, page=64, lengths=0):
@@ -50,11 +51,11 @@ def listed():
         # decoding of a full batch: one token per request behind 4 to 10 thousand rows
         dict(name="attend_decode", **_over_cache("attend", 64, 16, 2, 128, 1, 1, 4000, 10000, 64, lengths=22)),
         # one user deep in a long document: a single row over 150 thousand
-        dict(name="attend_long", **_over_cache("attend", 1, 16, 2, 128, 1, 1, 150001, 150001, 128)),
+        dict(name="attend_long", **_over_cache("attend", 1, 16, 2, 128, 1, 1, 150001, 150001, 128, lse=True)),
         # chunks of sixteen requests behind a few thousand rows, of which 2048 are a prefix that they share; gated outputs
-        dict(name="attend_chunks", **_over_cache("attend", 16, 16, 2, 128, 200, 1000, 3000, 5000, 16, 2048, True, 23)),
-        # the prompt: 8192 tokens over themselves
-        dict(name="attend_prompt", **_over_cache("attend", 1, 16, 2, 128, 8192, 8192, 0, 0)),
+        dict(name="attend_chunks", **_over_cache("attend", 16, 16, 2, 128, 200, 1000, 3000, 5000, 16, 2048, gate=True, lengths=23)),
+        # the prompt: 8192 tokens over themselves; the weights that its rows gather are asked for next
+        dict(name="attend_prompt", **_over_cache("attend", 1, 16, 2, 128, 8192, 8192, 0, 0, lse=True)),
         # the weights of a decoding batch
         dict(name="weights_decode", **_over_cache("weights", 64, 16, 2, 128, 1, 1, 4000, 10000, 64, lengths=22)),
         # the last chunk of a document: 500 tokens behind 7700 rows, one key/value head for every 4 query heads
@@ -108,7 +109,7 @@ def _draw_any(rng):
         hi, n_req = min(2 * lo, 8192), _log_int(rng, 1, 32)
     shared = 256 * rng.randrange(1, 9) if kind == "attend" and prefix > 2560 and rng.random() < 0.3 else 0
     return _over_cache(kind, n_req, *heads, d, lo, hi, prefix, 2 * prefix if prefix <= 20000 else prefix, page, shared,
-                       kind == "attend" and rng.random() < 0.3, lengths)
+                       kind == "attend" and rng.random() < 0.3, kind == "attend" and rng.random() < 0.5, lengths)
 
 
 def _lengths(case):
@@ -136,7 +137,7 @@ def work(case):
         return {"bytes": T * d * (H + 2 * K) * (size + 2), "flops": T * (H + K) * (case["rot"] // 2) * 6}
     if case["kind"] == "attend":
         distinct = rows - (case["n_req"] - 1) * min(case["shared"], min(prefix))
-        return {"bytes": T * H * d * (4 + 2 * case["gate"]) + 4 * T * H + distinct * K * d * 4, "flops": pairs * H * d * 4}
+        return {"bytes": T * H * d * (4 + 2 * case["gate"]) + 4 * T * H * case["lse"] + distinct * K * d * 4, "flops": pairs * H * d * 4}
     if case["kind"] == "weights":
         return {"bytes": T * H * (2 * d + 4) + rows * K * (2 * d + 8), "flops": pairs * H * d * 2}
     kept = sum(_kept(case)[2])
@@ -219,7 +220,7 @@ def prepare(case, seed):
         if case["kind"] == "attend":
             s["gate"] = normal(T, H, d).bfloat16() if case["gate"] else None
             s["o"] = torch.zeros(T, H, d, dtype=torch.bfloat16, device=dev)
-            s["lse"] = torch.zeros(T, H, device=dev)
+            s["lse"] = torch.zeros(T, H, device=dev) if case["lse"] else None
         else:
             s["lse"] = _plain_logits(s)[1]
             s["w_in"] = torch.exp(normal(ids.size, K, P))
@@ -303,7 +304,8 @@ def _plain_attend(s):
     if s["gate"] is not None:
         o = o / (1.0 + (-s["gate"].float()).exp())
     s["o"].copy_(o.bfloat16())
-    s["lse"].copy_(lse)
+    if s["lse"] is not None:
+        s["lse"].copy_(lse)
     return {"o": s["o"], "lse": s["lse"]}
 
 
@@ -437,4 +439,4 @@ def exact(case, seed):
         return {"w": w_out}
     if s["gate"] is not None:
         o = o * torch.sigmoid(s["gate"].double())
-    return {"o": o, "lse": lse}
+    return {"o": o, "lse": lse if case["lse"] else None}
