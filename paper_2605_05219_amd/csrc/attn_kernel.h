@@ -35,12 +35,20 @@
 // piece into parts of whole tiles: each part is a workgroup that leaves its unnormalised O, running
 // maximum and normaliser in a workspace slot, and a second kernel merges the parts of a piece.
 //
+// The same kernels read a cache kept in pages (PagedArgs, see include/attn_paged.h): a page holds [H_kv][page_rows][D], page_rows a power
+// of two of 16 at least, so that the rows that one wave brings of a tile (16, or 8) lie in one page.  Each lane of a wave holds the page of
+// one of the wave's next 64 tiles, a tile takes its page by a lane read and makes its buffer descriptor of it: one vector load of page ids for every 64
+// tiles, no wait on a dependent load in between.  The descriptor ends with the request's last row in the page, so that rows behind it (which
+// another request may have left, whatever they hold) come as zeros.
+//
 // LDS rows are unpadded (a load to LDS writes a wave's 64 x 16 bytes contiguously); bank
 // conflicts are avoided by storing 16-byte chunk c of row r at chunk position c ^ f(r), with f
 // chosen per tile for its read pattern (16 rows x same chunk for keys, 4 rows x 4 chunks for values).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 namespace attn {
 
@@ -93,6 +101,15 @@ struct AttnArgs {
     float scale_log2e;        // scale * log2(e)
 };
 
+// The cache in pages: k_cache, v_cache are pools of pages of [H_kv][page_rows][D], slot_stride the elements from one page to the
+// next, slot[r] (and the slot of a few-rows record) where request r's pages begin in page_ids.
+struct PagedArgs : AttnArgs {
+    const int32_t* page_ids;  // device
+    float* lse;               // [T][H_q]: natural logarithm of the sum of the exponentials of a row's scaled logits, or nullptr
+    float* part_le;           // [row]: sum of the unrounded weights of a partial result (behind lse only)
+    int32_t page_shift;       // log2 of page_rows
+};
+
 struct AppendArgs {
     const uint16_t* k_new;    // [T][H_kv][D]
     const uint16_t* v_new;
@@ -105,6 +122,11 @@ struct AppendArgs {
     int64_t n_chunks;         // T * row_chunks
     int32_t n_req;
     int32_t row_chunks;       // 16-byte chunks per token row: H_kv * D / 8
+};
+
+// Arguments of the few-rows kernel on a cache of slots, to which it appends itself.
+struct SlotNarrowArgs : AttnArgs {
+    AppendArgs ap;
 };
 
 // s_waitcnt vmcnt(N) (gfx9 encoding: vmcnt in bits 3:0 and 15:14; other counters left alone)
@@ -121,6 +143,9 @@ __device__ __forceinline__ void load_to_lds(const void* base, int bytes, char* l
     const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00020000);
     __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)lds, 16, voff, soff, 0, CPOL);
 }
+
+// log-sum-exp of a row from its maximal raw logit m and the sum l of 2^((logit - m) c), c = scale * log2(e)
+__device__ __forceinline__ float row_lse(float m, float l, float c) { return (__builtin_fmaf(m, c, __builtin_amdgcn_logf(l))) * 0.6931471805599453f; }
 
 // max / sum of a value with the lane 32 up or down (one swap instruction, no LDS)
 __device__ __forceinline__ float max_with_other_half(float x) {
@@ -167,25 +192,34 @@ __device__ __forceinline__ void store_out(void* o, const uint16_t* gate, int64_t
     }
 }
 
-// Appends the suffix's key and value rows to the cache rows start .. start+n-1 of each request's
-// slot: one 16-byte chunk of k and of v per thread, the values widened from bf16 to fp16.
-__global__ void __launch_bounds__(APPEND_THREADS) attn_append_kernel(AppendArgs a) {
-    const int64_t id = (int64_t)blockIdx.x * APPEND_THREADS + threadIdx.x;
-    if (id >= a.n_chunks) return;
-    const int32_t t = (int32_t)(id / a.row_chunks);
-    const int32_t c = (int32_t)(id - (int64_t)t * a.row_chunks);
-    int lo = 0, hi = a.n_req;                       // request with cu[r] <= t < cu[r+1]
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a.cu[mid] <= t) lo = mid; else hi = mid;
+__device__ __forceinline__ int page_shift(const AttnArgs&) { return 0; }
+__device__ __forceinline__ int page_shift(const PagedArgs& a) { return a.page_shift; }
+
+// Where consecutive rows of one page lie: `base` elements into the pool, the first of them row `at` of the page, of whose rows the
+// request's own are the first `rows` (0: all of the rows asked for are behind its last one).
+struct PageRows {
+    int64_t base;
+    int at, rows;
+};
+
+// A wave's next 64 page ids, one in each lane: step t's in lane t - (end - 64).
+struct PageIds {
+    int v = 0, end = INT32_MIN;
+
+    // ids of the steps t .. t + 63, step t + l beginning at row row_of(l); rows behind the request's last one name its last page
+    template <typename F>
+    __device__ __forceinline__ void fill(const PagedArgs& a, int first, int t, int lane, F row_of, int kv_len) {
+        const int page = min(row_of(lane), kv_len - 1) >> a.page_shift;
+        v = a.page_ids[first + page];
+        asm volatile("" : "+v"(v));            // the wait for the ids belongs here, not in front of every use
+        end = t + 64;
     }
-    const int r = lo;
-    if (a.start[r] < 0) return;
-    const int64_t row = (int64_t)a.start[r] + (t - a.cu[r]);
-    const int64_t dst = (int64_t)a.slot[r] * a.slot_stride + (row * a.row_chunks + c) * 8;
-    const int64_t src = ((int64_t)t * a.row_chunks + c) * 8;
-    append_chunk(a.k_new + src, a.v_new + src, a.k_cache + dst, a.v_cache + dst);
-}
+    __device__ __forceinline__ PageRows rows(const PagedArgs& a, int t, int row0, int kv_len) const {
+        const int P = 1 << a.page_shift;
+        const int at = row0 & (P - 1);
+        return {(int64_t)__builtin_amdgcn_readlane(v, t - (end - 64)) * a.slot_stride, at, max(0, min(P, kv_len - (row0 - at)))};
+    }
+};
 
 template <int D>
 struct AttnSmem {
@@ -203,9 +237,12 @@ struct AttnSmem {
     static __device__ __forceinline__ int fv(int row) { return CPR >= 16 ? ((row & 3) << 2) : (((row >> 1) & 1) << 2); }
 };
 
-// NH: head blocks per workgroup, four waves each
-template <int D, typename OT, int NH>
-__global__ void __launch_bounds__(ATT_THREADS * NH, 2) attn_suffix_kernel(AttnArgs a) {
+// NH: head blocks per workgroup, four waves each.  Args: AttnArgs (slots) or PagedArgs.  LSE: the rows' log-sum-exp too, from a sum of the
+// weights as they are before their rounding.
+template <int D, typename OT, int NH, typename Args, bool LSE>
+__global__ void __launch_bounds__(ATT_THREADS * NH, 2) attn_suffix_kernel(Args a) {
+    constexpr bool PAGED = std::is_same<Args, PagedArgs>::value;
+    static_assert(PAGED || !LSE, "the log-sum-exp is an output of the paged form");
     typedef AttnSmem<D> SM;
     constexpr int CPR = SM::CPR;
     constexpr int KB = D / 16;      // contraction steps of S^T
@@ -270,20 +307,37 @@ __global__ void __launch_bounds__(ATT_THREADS * NH, 2) attn_suffix_kernel(AttnAr
     // however the hardware compares the sum.
     constexpr int PPW = SM::PIECES / (4 * NH);                    // pieces per wave and tensor
     constexpr int RPP = 64 / CPR;                          // rows per piece
-    const int row_bytes = a.H_kv * D * 2;
-    const uint16_t* const kslot = a.k_cache + (int64_t)a.slot[r] * a.slot_stride;
-    const uint16_t* const vslot = a.v_cache + (int64_t)a.slot[r] * a.slot_stride;
-    const int slot_bytes = kv_len * row_bytes;
+    const int row_bytes = PAGED ? D * 2 : a.H_kv * D * 2;
+    const int head_off = PAGED ? 0 : kvh * D * 2;
+    const int64_t slot_at = PAGED ? (int64_t)kvh * D << page_shift(a) : (int64_t)a.slot[r] * a.slot_stride;
+    const uint16_t* const kslot = a.k_cache + slot_at;
+    const uint16_t* const vslot = a.v_cache + slot_at;
+    const int slot_bytes = PAGED ? 0 : kv_len * row_bytes;
     int koff[PPW], voff[PPW];
 #pragma unroll
     for (int i = 0; i < PPW; ++i) {
         const int s = (wg_wave * PPW + i) * 64 + lane;        // 16-byte slot inside the tile
         const int row = s / CPR, pos = s % CPR;
-        const int in_piece = (row - (wg_wave * PPW + i) * RPP) * row_bytes + kvh * D * 2;
+        const int in_piece = (row - (wg_wave * PPW + i) * RPP) * row_bytes + head_off;
         koff[i] = in_piece + ((pos ^ SM::fk(row)) << 4);
         voff[i] = in_piece + ((pos ^ SM::fv(row)) << 4);
     }
+    PageIds ids;
     auto issue = [&](int t, char* sb) {
+        if constexpr (PAGED) {
+            const int row0 = t * ATT_KT + wg_wave * PPW * RPP;
+            if (t >= ids.end) ids.fill(a, a.slot[r], t, lane, [&](int l) { return (t + l) * ATT_KT + wg_wave * PPW * RPP; }, kv_len);
+            const PageRows pr = ids.rows(a, t, row0, kv_len);
+            const int bytes = pr.rows * row_bytes;
+#pragma unroll
+            for (int i = 0; i < PPW; ++i) {
+                const int p = wg_wave * PPW + i;
+                const int soff = min((pr.at + i * RPP) * row_bytes, bytes);
+                load_to_lds(kslot + pr.base, bytes, sb + SM::K_OFF + p * 1024, koff[i], soff);
+                load_to_lds(vslot + pr.base, bytes, sb + SM::V_OFF + p * 1024, voff[i], soff);
+            }
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < PPW; ++i) {
             const int p = wg_wave * PPW + i;
@@ -309,6 +363,7 @@ __global__ void __launch_bounds__(ATT_THREADS * NH, 2) attn_suffix_kernel(AttnAr
         for (int i = 0; i < 16; ++i) O[rb][i] = 0.f;
     float m = -INFINITY;     // running maximum of the raw logits of this lane's query (both half-waves agree)
     float l = 0.f;           // this half-wave's share of the normaliser
+    float le = 0.f;          // LSE: the same of the unrounded weights
     const float c = a.scale_log2e;
 
     // per-lane LDS byte offsets inside a stage
@@ -384,7 +439,7 @@ __global__ void __launch_bounds__(ATT_THREADS * NH, 2) attn_suffix_kernel(AttnAr
         const float mc = m_ref * c;
         m = m_new;
         half8 pf[2 * ATT_KVB];                 // B operands of the 16-row steps
-        float lsum = 0.f;
+        float lsum = 0.f, esum = 0.f;
 #pragma unroll
         for (int s = 0; s < 2 * ATT_KVB; ++s) {
             f32x2 e[4];
@@ -393,6 +448,7 @@ __global__ void __launch_bounds__(ATT_THREADS * NH, 2) attn_suffix_kernel(AttnAr
                 e[j][0] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[s >> 1][8 * (s & 1) + 2 * j], c, -mc));
                 e[j][1] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[s >> 1][8 * (s & 1) + 2 * j + 1], c, -mc));
             }
+            if constexpr (LSE) esum += ((e[0][0] + e[0][1]) + (e[1][0] + e[1][1])) + ((e[2][0] + e[2][1]) + (e[3][0] + e[3][1]));
             half2 h[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -404,6 +460,7 @@ __global__ void __launch_bounds__(ATT_THREADS * NH, 2) attn_suffix_kernel(AttnAr
                                             __builtin_shufflevector(h[2], h[3], 0, 1, 2, 3), 0, 1, 2, 3, 4, 5, 6, 7);
         }
         l = l * alpha + lsum;
+        if constexpr (LSE) le = le * alpha + esum;
         if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0) {
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb)
@@ -443,6 +500,10 @@ __global__ void __launch_bounds__(ATT_THREADS * NH, 2) attn_suffix_kernel(AttnAr
                                            : a.few_row0 + ((int64_t)(-2 - part) * (a.H_q / R) + hb) * NAR_ROWS + wrow;
             const float lt = sum_with_other_half(l);
             if (g == 0) *reinterpret_cast<f32x2*>(a.part_ml + prow * 2) = f32x2{m, lt};
+            if constexpr (LSE) {
+                const float let = sum_with_other_half(le);
+                if (g == 0) a.part_le[prow] = let;
+            }
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
@@ -456,6 +517,10 @@ __global__ void __launch_bounds__(ATT_THREADS * NH, 2) attn_suffix_kernel(AttnAr
     if (valid) {
         const float inv = 1.f / sum_with_other_half(l);
         const int64_t base = ((int64_t)(tok0 + q0 + tl) * a.H_q + hq) * D;
+        if constexpr (LSE) {
+            const float lse = row_lse(m, sum_with_other_half(le), c);
+            if (g == 0) a.lse[(int64_t)(tok0 + q0 + tl) * a.H_q + hq] = lse;
+        }
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
@@ -504,8 +569,11 @@ __device__ __forceinline__ float sum_over_groups(float x) {
     return sum_with_other_half(__builtin_bit_cast(float, (unsigned)p[0]) + __builtin_bit_cast(float, (unsigned)p[1]));
 }
 
-template <int D, typename OT, bool NT>
-__global__ void __launch_bounds__(ATT_THREADS, narrow_wgs_per_cu(D)) attn_narrow_kernel(AttnArgs a, AppendArgs ap) {
+// Args: SlotNarrowArgs or PagedArgs (whose rows are in the pages already: nothing is appended).
+template <int D, typename OT, bool NT, typename Args, bool LSE>
+__global__ void __launch_bounds__(ATT_THREADS, narrow_wgs_per_cu(D)) attn_narrow_kernel(Args a) {
+    constexpr bool PAGED = std::is_same<Args, PagedArgs>::value;
+    static_assert(PAGED || !LSE, "the log-sum-exp is an output of the paged form");
     typedef NarrowSmem<D> SM;
     constexpr int KS = D / 32;      // contraction steps of S^T
     constexpr int DB = D / 16;      // 16-column tiles of O^T
@@ -514,7 +582,7 @@ __global__ void __launch_bounds__(ATT_THREADS, narrow_wgs_per_cu(D)) attn_narrow
     // the two halves of the rings are variables of their own: the compiler then sees that the transposing reads of one half
     // do not depend on the loads to LDS in flight to the other, for which it would wait otherwise
     __shared__ __attribute__((aligned(1024))) char ring0[4][SM::BLOCK_BYTES], ring1[4][SM::BLOCK_BYTES];
-    __shared__ float ml[4][NAR_ROWS][2];
+    __shared__ float ml[4][NAR_ROWS][LSE ? 3 : 2];
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -526,9 +594,11 @@ __global__ void __launch_bounds__(ATT_THREADS, narrow_wgs_per_cu(D)) attn_narrow
     const int tok0 = rec[0], n = rec[1], c0 = rec[2], slot = rec[3], k0 = rec[4], k1 = rec[5], part = rec[6];
     const int kv_len = c0 + n;
     const int rows = n * G;
-    const int row_bytes = a.H_kv * D * 2;
-    uint16_t* const kslot = ap.k_cache + (int64_t)slot * a.slot_stride;
-    uint16_t* const vslot = ap.v_cache + (int64_t)slot * a.slot_stride;
+    const int row_bytes = PAGED ? D * 2 : a.H_kv * D * 2;
+    const int head_off = PAGED ? 0 : kvh * D * 2;
+    const int64_t slot_at = PAGED ? (int64_t)kvh * D << page_shift(a) : (int64_t)slot * a.slot_stride;
+    const uint16_t* const kslot = a.k_cache + slot_at;
+    const uint16_t* const vslot = a.v_cache + slot_at;
 
     // ---- loads of one block: values to LDS (a wave's 1 KiB per load, the chunk swizzle on the global side), keys to registers
     const int nb = (k1 - k0 + NAR_KEYS - 1) / NAR_KEYS;
@@ -538,18 +608,51 @@ __global__ void __launch_bounds__(ATT_THREADS, narrow_wgs_per_cu(D)) attn_narrow
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int s = i * 64 + lane, row = s / SM::CPR, pos = s % SM::CPR;
-        voff[i] = row * row_bytes + kvh * D * 2 + ((pos ^ SM::f(row)) << 4);
+        voff[i] = (PAGED ? row & 15 : row) * row_bytes + head_off + ((pos ^ SM::f(row)) << 4);
     }
-    const int koff = i16 * row_bytes + kvh * D * 2 + 16 * g;
+    const int koff = i16 * row_bytes + head_off + 16 * g;
+    // pages: half a block (16 rows) lies in one page; half h of block j is step 2 j + h
+    PageIds ids;
+    auto half_row = [&](int step) { return k0 + (wave + 4 * (step >> 1)) * NAR_KEYS + 16 * (step & 1); };
+    auto paged_half = [&](int j, int h, int64_t& base, int& bytes, int& soff) {
+        if constexpr (PAGED) {
+            const PageRows pr = ids.rows(a, 2 * j + h, half_row(2 * j + h), kv_len);
+            base = pr.base;
+            bytes = j < my ? pr.rows * row_bytes : 0;
+            soff = min(pr.at * row_bytes, bytes);
+        }
+    };
     auto load_values = [&](int j, char* st) {                // block j of this wave; past the last one the descriptor is empty
+        if constexpr (PAGED) {
+            if (2 * j >= ids.end) ids.fill(a, slot, 2 * j, lane, [&](int l) { return half_row(2 * j + l); }, kv_len);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                int64_t base; int bytes, soff;
+                paged_half(j, h, base, bytes, soff);
+#pragma unroll
+                for (int i = h * NV / 2; i < (h + 1) * NV / 2; ++i) load_to_lds<NT ? 2 : 0>(vslot + base, bytes, st + i * 1024, voff[i], soff);
+            }
+            return;
+        }
         const int soff = __builtin_amdgcn_readfirstlane(j < my ? (k0 + (wave + 4 * j) * NAR_KEYS) * row_bytes : 0);
         const int bytes = j < my ? slot_bytes : 0;
 #pragma unroll
         for (int i = 0; i < NV; ++i) load_to_lds<NT ? 2 : 0>(vslot, bytes, st + i * 1024, voff[i], soff);
     };
-    auto load_keys = [&](int j, u32x4* kf) {
+    auto load_keys = [&](int j, u32x4* kf) {                 // (behind the same block's load_values, which sees to the page ids)
+        if constexpr (PAGED) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                int64_t base; int bytes, soff;
+                paged_half(j, h, base, bytes, soff);
+                const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(kslot + base), 0, bytes, 0x00020000);
+#pragma unroll
+                for (int s = 0; s < KS; ++s) kf[KS * h + s] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, koff + 64 * s, soff, NT ? 2 : 0);
+            }
+            return;
+        }
         const int soff = __builtin_amdgcn_readfirstlane(j < my ? (k0 + (wave + 4 * j) * NAR_KEYS) * row_bytes : 0);
-        const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(kslot, 0, j < my ? slot_bytes : 0, 0x00020000);
+        const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(kslot), 0, j < my ? slot_bytes : 0, 0x00020000);
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -559,12 +662,14 @@ __global__ void __launch_bounds__(ATT_THREADS, narrow_wgs_per_cu(D)) attn_narrow
 
     // ---- the suffix rows inside [k0, k1) go to the cache (usually none, or those of the request's last unit)
     const int new0 = max(c0, k0);
-    if (new0 < k1) {                 // uniform over the workgroup
+    if constexpr (!PAGED) if (new0 < k1) {                 // uniform over the workgroup
+        uint16_t* const kdst = a.ap.k_cache + slot_at;
+        uint16_t* const vdst = a.ap.v_cache + slot_at;
         for (int i = threadIdx.x; i < (k1 - new0) * SM::CPR; i += ATT_THREADS) {
             const int row = new0 + i / SM::CPR, c = i % SM::CPR;
             const int64_t dst = (int64_t)row * (a.H_kv * D) + kvh * D + 8 * c;
             const int64_t src = (int64_t)(tok0 + row - c0) * (a.H_kv * D) + kvh * D + 8 * c;
-            append_chunk(ap.k_new + src, ap.v_new + src, kslot + dst, vslot + dst);
+            append_chunk(a.ap.k_new + src, a.ap.v_new + src, kdst + dst, vdst + dst);
         }
         __syncthreads();             // (waits for the stores: the walk below reads these rows)
     }
@@ -587,6 +692,7 @@ __global__ void __launch_bounds__(ATT_THREADS, narrow_wgs_per_cu(D)) attn_narrow
 #pragma unroll
     for (int i = 0; i < DB; ++i) O[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;    // m: of this lane's row; l: this lane's share of the row's normaliser
+    float le = 0.f;                  // LSE: the same of the unrounded weights
     const float c = a.scale_log2e;
     const int vrow = 4 * g + (i16 >> 2);                     // + 16: row of the transposing reads
     const int vbase = vrow * SM::ROW_BYTES + 8 * (i16 & 1);
@@ -618,12 +724,13 @@ __global__ void __launch_bounds__(ATT_THREADS, narrow_wgs_per_cu(D)) attn_narrow
         const float mc = m_ref * c;
         m = m_new;
         half2 h[4];
-        float lsum = 0.f;
+        float lsum = 0.f, esum = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             f32x2 e;
             e[0] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[i >> 1][2 * (i & 1)], c, -mc));
             e[1] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[i >> 1][2 * (i & 1) + 1], c, -mc));
+            if constexpr (LSE) esum += e[0] + e[1];
             h[i] = __builtin_convertvector(e, half2);
             const half2 one = {(_Float16)1.0f, (_Float16)1.0f};
             lsum = __builtin_amdgcn_fdot2(h[i], one, lsum, false);   // the sum of the ROUNDED weights
@@ -631,6 +738,7 @@ __global__ void __launch_bounds__(ATT_THREADS, narrow_wgs_per_cu(D)) attn_narrow
         const half8 pf = __builtin_shufflevector(__builtin_shufflevector(h[0], h[1], 0, 1, 2, 3),
                                                  __builtin_shufflevector(h[2], h[3], 0, 1, 2, 3), 0, 1, 2, 3, 4, 5, 6, 7);
         l = l * alpha + lsum;
+        if constexpr (LSE) le = le * alpha + esum;
         if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0) {
 #pragma unroll
             for (int i = 0; i < DB; ++i) O[i] *= alpha;
@@ -681,6 +789,10 @@ __global__ void __launch_bounds__(ATT_THREADS, narrow_wgs_per_cu(D)) attn_narrow
     {
         const float lt = sum_over_groups(l);
         if (g == 0) { ml[wave][i16][0] = m; ml[wave][i16][1] = lt; }
+        if constexpr (LSE) {
+            const float let = sum_over_groups(le);
+            if (g == 0) ml[wave][i16][2] = let;
+        }
 #pragma unroll
         for (int db = 0; db < DB; ++db)
             *reinterpret_cast<f32x4*>(om(wave, i16) + 16 * db + 4 * g) = O[db];
@@ -691,19 +803,22 @@ __global__ void __launch_bounds__(ATT_THREADS, narrow_wgs_per_cu(D)) attn_narrow
         const float M = fmaxf(fmaxf(ml[0][row][0], ml[1][row][0]), fmaxf(ml[2][row][0], ml[3][row][0]));
         const float ref = M == -INFINITY ? 0.f : M;           // no key of this part is visible to this row
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-        float L = 0.f;
+        float L = 0.f, Le = 0.f;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             const float wt = __builtin_amdgcn_exp2f((ml[w][row][0] - ref) * c);
             acc += wt * *reinterpret_cast<const f32x4*>(om(w, row) + dv);
             L += wt * ml[w][row][1];
+            if constexpr (LSE) Le += wt * ml[w][row][2];
         }
         if (part >= 0) {
             const int64_t prow = a.few_row0 + ((int64_t)part * a.H_kv + kvh) * NAR_ROWS + row;
             if (dv == 0) *reinterpret_cast<f32x2*>(a.part_ml + prow * 2) = f32x2{M, L};
+            if constexpr (LSE) if (dv == 0) a.part_le[prow] = Le;
             *reinterpret_cast<f32x4*>(a.part_o + prow * D + dv) = acc;
         } else {
             const int t = row / G;
+            if constexpr (LSE) if (dv == 0) a.lse[(int64_t)(tok0 + t) * a.H_q + kvh * G + row - t * G] = row_lse(M, Le, c);
             store_out<OT>(a.o, a.gate, ((int64_t)(tok0 + t) * a.H_q + kvh * G + row - t * G) * D + dv, acc * (1.f / L));
         }
     }
@@ -728,6 +843,8 @@ struct CombineArgs {
     const uint16_t* gate;     // or nullptr
     void* o;
     const int32_t* cu;
+    float* lse;               // LSE: [T][H_q]
+    const float* part_le;
     CombineSet set[2];        // the other requests' pieces, the few-rows requests'
     int32_t H_q;
     float scale_log2e;
@@ -737,7 +854,7 @@ struct CombineArgs {
 // w_p = 2^((m_p - max_p m_p) * scale * log2 e); a part that saw no key has m_p = -inf, weight 0 and O_p = 0.
 // One thread per (row, four value columns), `subs` workgroups per (piece, head block); the loads of all
 // parts are independent of each other, so the pass costs a few memory round trips, not one per part.
-template <int D, typename OT>
+template <int D, typename OT, bool LSE>
 __global__ void __launch_bounds__(ATT_THREADS) attn_combine_kernel(CombineArgs a) {
     constexpr int CH = D / 4;                  // threads per row
     const bool second = (int)blockIdx.x >= a.set[0].blocks;
@@ -771,6 +888,12 @@ __global__ void __launch_bounds__(ATT_THREADS) attn_combine_kernel(CombineArgs a
             const float w = __builtin_amdgcn_exp2f((ml[0] - M) * a.scale_log2e);
             acc[0] += w * op[0]; acc[1] += w * op[1]; acc[2] += w * op[2]; acc[3] += w * op[3];
             L += w * ml[1];
+        }
+        if (LSE && ch == 0) {
+            float Le = 0.f;
+            for (int p = 0; p < P; ++p)
+                Le += __builtin_amdgcn_exp2f((a.part_ml[(prow0 + p * pstep) * 2] - M) * a.scale_log2e) * a.part_le[prow0 + p * pstep];
+            a.lse[(int64_t)(tok0 + q0 + tl) * a.H_q + hq] = row_lse(M, Le, a.scale_log2e);
         }
         const float inv = 1.f / L;
         store_out<OT>(a.o, a.gate, ((int64_t)(tok0 + q0 + tl) * a.H_q + hq) * D + 4 * ch,

@@ -1,0 +1,526 @@
+// attn_paged: host side of the paged key/value cache (see include/attn_paged.h).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <stdexcept>
+#include <vector>
+
+#include "attn_launch.h"
+#include "attn_paged.h"
+#include "attn_paged_kernel.h"
+
+namespace attn {
+namespace {
+
+// Rows are numbered with 32 bits in the kernels, which look up to 64 tiles ahead.
+constexpr int64_t MAX_ROWS = INT32_MAX - 8192;
+
+int32_t check_pages(const attn_shape* s, const attn_pages* p) {
+    if (!p) return GDN_ERR_NULL;
+    if (p->n_pages < 0) return GDN_ERR_COUNT;
+    if (p->page_rows < 16 || p->page_rows > 4096 || (p->page_rows & (p->page_rows - 1)) != 0) return GDN_ERR_SHAPE;
+    if (p->page_stride < 0 || p->page_stride % 8 != 0) return GDN_ERR_ALIGN;
+    const int64_t elems = (int64_t)s->H_kv * p->page_rows * s->d;
+    if (elems * 2 > INT32_MAX || p->page_stride < elems) return GDN_ERR_SHAPE;
+    return GDN_OK;
+}
+
+inline int shift_of(const attn_pages* p) { return __builtin_ctz((unsigned)p->page_rows); }
+
+// The new tokens of every request.
+int32_t check_lengths(int32_t n_req, const int32_t* cu, const int32_t* start, std::vector<int32_t>& len) {
+    if (!cu || !start) return GDN_ERR_NULL;
+    if (cu[0] != 0) return GDN_ERR_SEQLENS;
+    len.resize(n_req);
+    for (int32_t r = 0; r < n_req; ++r) {
+        if (cu[r + 1] < cu[r]) return GDN_ERR_SEQLENS;
+        len[r] = cu[r + 1] - cu[r];
+        if (start[r] < 0 || (int64_t)start[r] + len[r] > MAX_ROWS) return GDN_ERR_START;
+    }
+    return GDN_OK;
+}
+
+// A page table: every listed id inside the pool, and enough of them for rows(r) rows of request r.
+template <typename F>
+int32_t check_table(const attn_pages* p, int32_t n_req, const int32_t* page_cu, const int32_t* page_ids, F rows) {
+    if (!page_cu) return GDN_ERR_NULL;
+    if (page_cu[0] != 0) return GDN_ERR_SEQLENS;
+    for (int32_t r = 0; r < n_req; ++r) {
+        if (page_cu[r + 1] < page_cu[r]) return GDN_ERR_SEQLENS;
+        if ((int64_t)(page_cu[r + 1] - page_cu[r]) * p->page_rows < rows(r)) return GDN_ERR_START;
+    }
+    const int32_t n = page_cu[n_req];
+    if (n > 0 && !page_ids) return GDN_ERR_NULL;
+    bool bad = false;
+    for (int32_t i = 0; i < n; ++i) bad |= (uint32_t)page_ids[i] >= (uint32_t)p->n_pages;
+    return bad ? GDN_ERR_SLOT_RANGE : GDN_OK;
+}
+
+// A set of page ids.
+class PageSet {
+  public:
+    explicit PageSet(int32_t n_pages) : bits_((size_t)n_pages / 64 + 1, 0) {}
+    bool has(int32_t id) const { return bits_[(size_t)id / 64] >> (id % 64) & 1; }
+    bool add(int32_t id) {       // false: it was there
+        const bool was = has(id);
+        bits_[(size_t)id / 64] |= 1ull << (id % 64);
+        return !was;
+    }
+
+  private:
+    std::vector<uint64_t> bits_;
+};
+
+// The region of the partial results behind the uploaded image: maxima and normalisers, outputs, sums of the unrounded weights.
+// attn_key_weights leaves its parts there instead.
+inline int64_t part_le_bytes() { return (int64_t)SPLIT_MAX_WGS * ATT_BQ * sizeof(float); }
+inline int64_t parts_bytes(int d) {
+    return std::max<int64_t>(part_ml_bytes() + part_o_bytes(d) + part_le_bytes(), (int64_t)WGT_PARTS * WGT_KEYS * sizeof(float));
+}
+// ints of an image: the attention's are the most (plan_ints) but for calls of very few tokens and many requests
+inline int64_t image_bytes(const attn_shape* s, int32_t n_req, int64_t T, int64_t n_ids) {
+    const int64_t ints = std::max<int64_t>(plan_ints(n_req, T, s->H_q / s->H_kv), 8 * ((int64_t)n_req + 1)) + n_ids;
+    return (ints * (int64_t)sizeof(int32_t) + 255) / 256 * 256;
+}
+
+int32_t check_workspace(const attn_shape* s, int32_t n_req, int64_t T, int64_t n_ids, const void* ws, int64_t bytes) {
+    if (!ws || !aligned16(ws) || bytes < image_bytes(s, n_req, T, n_ids) + parts_bytes(s->d)) return GDN_ERR_WORKSPACE;
+    return GDN_OK;
+}
+
+// What every call with new tokens checks of its index arrays, in this order.
+int32_t check_call(const attn_shape* s, int32_t n_req, const int32_t* cu, const int32_t* start, const attn_pages* pages,
+                   const int32_t* page_cu, const int32_t* page_ids, std::vector<int32_t>& len) {
+    int32_t rc = check_lengths(n_req, cu, start, len);
+    if (rc != GDN_OK) return rc;
+    return check_table(pages, n_req, page_cu, page_ids, [&](int32_t r) { return (int64_t)start[r] + len[r]; });
+}
+
+int32_t check_front(const attn_shape* s, int32_t n_req, const attn_pages* pages) {
+    const int32_t rc = check_shape(s);
+    if (rc != GDN_OK) return rc;
+    if (n_req < 0) return GDN_ERR_COUNT;
+    return check_pages(s, pages);
+}
+
+int32_t rope_append(const attn_shape* s, const attn_rope* rope, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v,
+                    int64_t ldv, int32_t n_req, const int32_t* cu, const int32_t* pos, const int32_t* start, const attn_pages* pages,
+                    void* k_pool, void* v_pool, const int32_t* page_cu, const int32_t* page_ids, void* q_out, void* workspace,
+                    int64_t workspace_bytes, hipStream_t stream) {
+    int32_t rc = check_front(s, n_req, pages);
+    if (rc != GDN_OK) return rc;
+    if (!rope) return GDN_ERR_NULL;
+    if (rope->rot < 0 || rope->rot > s->d || rope->rot % 16 != 0 || (rope->layout != 0 && rope->layout != 1)) return GDN_ERR_SHAPE;
+    if (rope->in_dtype != GDN_F32 && rope->in_dtype != GDN_BF16) return GDN_ERR_SHAPE;
+    if (!std::isfinite(rope->amplitude)) return GDN_ERR_SHAPE;
+    if (rope->rot > 0 && !rope->freq) return GDN_ERR_NULL;
+    const int per16 = rope->in_dtype == GDN_F32 ? 4 : 8;
+    const int64_t wq = (int64_t)s->H_q * s->d, wkv = (int64_t)s->H_kv * s->d;
+    if (ldq % per16 != 0 || ldk % per16 != 0 || ldv % per16 != 0) return GDN_ERR_ALIGN;
+    if (ldq < wq || ldk < wkv || ldv < wkv) return GDN_ERR_SHAPE;
+    RopeArgs a;
+    for (int p = 0; p < rope->rot / 2; ++p) {
+        if (!std::isfinite(rope->freq[p])) return GDN_ERR_SHAPE;
+        long double t = (long double)rope->freq[p] / 6.283185307179586476925286766559005768L;
+        t = (t - floorl(t)) * 18446744073709551616.0L;
+        a.turn[p] = t >= 18446744073709551615.0L ? 0 : (uint64_t)(t + 0.5L);
+    }
+    if (n_req == 0) return GDN_OK;
+    std::vector<int32_t> len;
+    rc = check_call(s, n_req, cu, start, pages, page_cu, page_ids, len);
+    if (rc != GDN_OK) return rc;
+    if (!pos) pos = start;
+    for (int32_t r = 0; r < n_req; ++r)
+        if (pos[r] < 0 || (int64_t)pos[r] + len[r] > INT32_MAX) return GDN_ERR_START;
+    const int64_t T = cu[n_req];
+    if (T == 0) return GDN_OK;
+    // ---- the pages that get rows, and that nobody else in the call has them
+    const int shift = shift_of(pages);
+    std::vector<int32_t> img((size_t)(4 * (int64_t)n_req + 1));
+    PageSet written(pages->n_pages);
+    for (int32_t r = 0; r < n_req; ++r) {
+        const int32_t p0 = start[r] >> shift;
+        img[1 + n_req + r] = start[r];
+        img[1 + 2 * n_req + r] = pos[r];
+        img[1 + 3 * n_req + r] = (int32_t)(img.size() - (4 * (size_t)n_req + 1)) - p0;
+        if (len[r] == 0) continue;
+        const int32_t p1 = (start[r] + len[r] - 1) >> shift;
+        for (int32_t p = p0; p <= p1; ++p) {
+            if (!written.add(page_ids[page_cu[r] + p])) return GDN_ERR_SLOT_DUP;
+            img.push_back(page_ids[page_cu[r] + p]);
+        }
+    }
+    for (int32_t r = 0; r < n_req; ++r) {
+        const int32_t held = (start[r] + (1 << shift) - 1) >> shift, p0 = len[r] > 0 ? start[r] >> shift : held;
+        for (int32_t p = 0; p < p0; ++p)
+            if (written.has(page_ids[page_cu[r] + p])) return GDN_ERR_SLOT_DUP;
+    }
+    for (int32_t r = 0; r <= n_req; ++r) img[r] = cu[r];
+    if (!q || !k || !v || !k_pool || !v_pool || !q_out) return GDN_ERR_NULL;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(k_pool) || !aligned16(v_pool) || !aligned16(q_out)) return GDN_ERR_ALIGN;
+    rc = check_workspace(s, n_req, T, page_cu[n_req], workspace, workspace_bytes);
+    if (rc != GDN_OK) return rc;
+    rc = gdn::upload_plan(img.data(), img.size() * sizeof(int32_t), workspace, stream);
+    if (rc != GDN_OK) return rc;
+    const int32_t* const d = static_cast<const int32_t*>(workspace);
+    a.q = q; a.k = k; a.v = v;
+    a.q_out = static_cast<uint16_t*>(q_out);
+    a.k_pool = static_cast<uint16_t*>(k_pool);
+    a.v_pool = static_cast<uint16_t*>(v_pool);
+    a.cu = d;
+    a.start = d + n_req + 1;
+    a.pos = a.start + n_req;
+    a.place = a.pos + n_req;
+    a.page_ids = a.place + n_req;
+    a.ldq = ldq; a.ldk = ldk; a.ldv = ldv;
+    a.page_stride = pages->page_stride;
+    a.n_req = n_req;
+    a.T = (int32_t)T;
+    a.tokens = T >= 8 * 1024 ? ROPE_TOKENS : T >= 1024 ? 4 : 1;
+    a.H_q = s->H_q; a.H_kv = s->H_kv;
+    a.units = s->d / 16;
+    a.page_shift = shift;
+    a.rot = rope->rot;
+    a.layout = rope->layout;
+    a.amplitude = rope->amplitude;
+    const dim3 grid((unsigned)((T + a.tokens - 1) / a.tokens)), block(ROPE_THREADS);
+    if (rope->in_dtype == GDN_F32) hipLaunchKernelGGL((attn_rope_kernel<true>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((attn_rope_kernel<false>), grid, block, 0, stream, a);
+    return hip_err(hipGetLastError());
+}
+
+template <bool LSE>
+int32_t launch_paged(const attn_shape* s, const UnitPlan& plan, const CallImage& im, const int32_t* d, bool nt, PagedArgs& a, hipStream_t stream) {
+    int32_t rc;
+    if (im.n_narrow > 0 && (rc = launch_narrow_units<LSE>(s, nt, im, a, stream)) != GDN_OK) return rc;
+    if (im.n_wide > 0 && (rc = launch_wide_units<LSE>(s, plan, im, a, stream)) != GDN_OK) return rc;
+    return launch_merge<LSE>(s, plan, im, d, a, a.lse, a.part_le, stream);
+}
+
+int32_t paged_prefill(const attn_shape* s, const void* q, const void* gate, int32_t n_req, const int32_t* cu, const int32_t* start,
+                      const attn_pages* pages, const void* k_pool, const void* v_pool, const int32_t* page_cu, const int32_t* page_ids,
+                      void* o, float* lse, void* workspace, int64_t workspace_bytes, hipStream_t stream) {
+    int32_t rc = check_front(s, n_req, pages);
+    if (rc != GDN_OK) return rc;
+    if (n_req == 0) return GDN_OK;
+    std::vector<int32_t> len;
+    rc = check_call(s, n_req, cu, start, pages, page_cu, page_ids, len);
+    if (rc != GDN_OK) return rc;
+    const int64_t T = cu[n_req];
+    if (T == 0) return GDN_OK;
+    if (!q || !k_pool || !v_pool || !o) return GDN_ERR_NULL;
+    if (!aligned16(q) || !aligned16(gate) || !aligned16(k_pool) || !aligned16(v_pool) || !aligned16(o)) return GDN_ERR_ALIGN;
+    if (reinterpret_cast<uintptr_t>(lse) % 4 != 0) return GDN_ERR_ALIGN;
+    const int32_t n_ids = page_cu[n_req];
+    rc = check_workspace(s, n_req, T, n_ids, workspace, workspace_bytes);
+    if (rc != GDN_OK) return rc;
+
+    UnitPlan plan;
+    build_units(*s, n_req, len.data(), start, plan);
+    CallImage im;
+    rc = make_image(s, plan, n_req, cu, start, len.data(), page_cu, page_ids, n_ids, im);
+    if (rc != GDN_OK) return rc;
+    rc = gdn::upload_plan(im.img.data(), im.img.size() * sizeof(int32_t), workspace, stream);
+    if (rc != GDN_OK) return rc;
+    const int32_t* const d = static_cast<const int32_t*>(workspace);
+    char* const parts = static_cast<char*>(workspace) + image_bytes(s, n_req, T, n_ids);
+    PagedArgs a;
+    a.q = static_cast<const uint16_t*>(q);
+    a.gate = static_cast<const uint16_t*>(gate);
+    a.k_cache = static_cast<const uint16_t*>(k_pool);
+    a.v_cache = static_cast<const uint16_t*>(v_pool);
+    a.o = o;
+    a.slot_stride = pages->page_stride;
+    image_args(s, plan, n_req, im, d, parts, a);
+    a.page_ids = d + im.ids_at;
+    a.page_shift = shift_of(pages);
+    a.lse = lse;
+    a.part_le = reinterpret_cast<float*>(parts + part_ml_bytes() + part_o_bytes(s->d));
+    const bool nt = narrow_nt(s, plan, n_req, start, len.data());
+    return lse ? launch_paged<true>(s, plan, im, d, nt, a, stream) : launch_paged<false>(s, plan, im, d, nt, a, stream);
+}
+
+template <int D>
+void launch_weights(const WeightArgs& a, unsigned blocks, hipStream_t stream) {
+    hipLaunchKernelGGL((attn_weights_kernel<D>), dim3(blocks), dim3(WGT_THREADS), 0, stream, a);
+}
+
+int32_t key_weights(const attn_shape* s, const void* q, const float* lse, int32_t n_req, const int32_t* cu, const int32_t* start,
+                    const attn_pages* pages, const void* k_pool, const int32_t* page_cu, const int32_t* page_ids, float decay,
+                    const float* w_in, float* w_out, int64_t w_stride, void* workspace, int64_t workspace_bytes, hipStream_t stream) {
+    int32_t rc = check_front(s, n_req, pages);
+    if (rc != GDN_OK) return rc;
+    if (!std::isfinite(decay) || w_stride < (int64_t)s->H_kv * pages->page_rows) return GDN_ERR_SHAPE;
+    if (n_req == 0) return GDN_OK;
+    std::vector<int32_t> len;
+    rc = check_call(s, n_req, cu, start, pages, page_cu, page_ids, len);
+    if (rc != GDN_OK) return rc;
+    const int shift = shift_of(pages);
+    PageSet written(pages->n_pages);
+    int64_t rows = 0;
+    for (int32_t r = 0; r < n_req; ++r) {
+        const int32_t total = start[r] + len[r];
+        rows += total;
+        for (int32_t p = 0; (int64_t)p << shift < total; ++p)
+            if (!written.add(page_ids[page_cu[r] + p])) return GDN_ERR_SLOT_DUP;
+    }
+    if (rows == 0) return GDN_OK;
+    const int64_t T = cu[n_req];
+    if ((T > 0 && (!q || !lse)) || !k_pool || !w_out) return GDN_ERR_NULL;
+    if (!aligned16(q) || !aligned16(k_pool)) return GDN_ERR_ALIGN;
+    if (reinterpret_cast<uintptr_t>(lse) % 4 != 0 || reinterpret_cast<uintptr_t>(w_in) % 4 != 0 || reinterpret_cast<uintptr_t>(w_out) % 4 != 0) return GDN_ERR_ALIGN;
+    const int32_t n_ids = page_cu[n_req];
+    rc = check_workspace(s, n_req, T, n_ids, workspace, workspace_bytes);
+    if (rc != GDN_OK) return rc;
+
+    // ---- key tiles, and the cut of their query rows into parts where there are too few tiles for the chip
+    const int G = s->H_q / s->H_kv;
+    int64_t tiles = 0, longest = 0;
+    for (int32_t r = 0; r < n_req; ++r) {
+        tiles += ((int64_t)start[r] + len[r] + WGT_KEYS - 1) / WGT_KEYS;
+        longest = std::max<int64_t>(longest, (int64_t)len[r] * G);
+    }
+    if (longest > INT32_MAX - 2 * WGT_ROWS || ((int64_t)s->H_q * 32 + G) * s->d * 2 > INT32_MAX) return GDN_ERR_SHAPE;
+    int64_t part_rows = (longest + WGT_ROWS - 1) / WGT_ROWS * WGT_ROWS;
+    auto pairs_of = [&](int64_t pr) {
+        int64_t n = 0;
+        for (int32_t r = 0; r < n_req; ++r)
+            n += ((int64_t)start[r] + len[r] + WGT_KEYS - 1) / WGT_KEYS * std::max<int64_t>(1, ((int64_t)len[r] * G + pr - 1) / pr);
+        return n;
+    };
+    constexpr int64_t WANT = 1024, MIN_ROWS = 256;
+    if (tiles * s->H_kv < WANT && part_rows > MIN_ROWS) {
+        part_rows = MIN_ROWS;
+        while (pairs_of(part_rows) * s->H_kv > WGT_PARTS) part_rows *= 2;
+    }
+    part_rows = std::max<int64_t>(part_rows, WGT_ROWS);
+    const int64_t pairs = pairs_of(part_rows);
+    if (pairs * s->H_kv > INT32_MAX) return GDN_ERR_COUNT;
+    std::vector<int32_t> img((size_t)(5 * (int64_t)n_req + 3 + n_ids));
+    int32_t* const p_start = img.data() + n_req + 1;
+    int32_t* const p_place = p_start + n_req;
+    int32_t* const p_block = p_place + n_req;
+    int32_t* const p_cut = p_block + n_req + 1;
+    std::copy(cu, cu + n_req + 1, img.data());
+    std::copy(start, start + n_req, p_start);
+    std::copy(page_cu, page_cu + n_req, p_place);
+    std::copy(page_ids, page_ids + n_ids, p_cut + n_req + 1);
+    p_block[0] = p_cut[0] = 0;
+    for (int32_t r = 0; r < n_req; ++r) {
+        const int32_t t = (int32_t)(((int64_t)start[r] + len[r] + WGT_KEYS - 1) / WGT_KEYS);
+        const int32_t parts = (int32_t)std::max<int64_t>(1, ((int64_t)len[r] * G + part_rows - 1) / part_rows);
+        p_block[r + 1] = p_block[r] + t * parts;
+        p_cut[r + 1] = p_cut[r] + (parts > 1 ? t : 0);
+    }
+    const int32_t cut_tiles = p_cut[n_req];
+    rc = gdn::upload_plan(img.data(), img.size() * sizeof(int32_t), workspace, stream);
+    if (rc != GDN_OK) return rc;
+    const int32_t* const d = static_cast<const int32_t*>(workspace);
+    WeightArgs a;
+    a.q = static_cast<const uint16_t*>(q);
+    a.lse = lse;
+    a.k_pool = static_cast<const uint16_t*>(k_pool);
+    a.w_in = w_in;
+    a.w_out = w_out;
+    a.cu = d;
+    a.start = d + n_req + 1;
+    a.place = a.start + n_req;
+    a.block_cu = a.place + n_req;
+    a.page_ids = a.block_cu + 2 * ((int64_t)n_req + 1);
+    a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + image_bytes(s, n_req, T, n_ids));
+    a.page_stride = pages->page_stride;
+    a.w_stride = w_stride;
+    a.n_req = n_req;
+    a.H_q = s->H_q; a.H_kv = s->H_kv; a.G = G;
+    a.page_shift = shift;
+    a.part_rows = (int32_t)part_rows;
+    a.scale_log2e = s->scale * 1.4426950408889634f;
+    a.decay = decay;
+    const unsigned blocks = (unsigned)(pairs * s->H_kv);
+    switch (s->d) {
+        case 64: launch_weights<64>(a, blocks, stream); break;
+        case 128: launch_weights<128>(a, blocks, stream); break;
+        default: launch_weights<256>(a, blocks, stream); break;
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || cut_tiles == 0) return hip_err(e);
+    hipLaunchKernelGGL(attn_weights_merge_kernel, dim3((unsigned)(cut_tiles * s->H_kv)), dim3(WGT_KEYS), 0, stream, a, a.block_cu + n_req + 1);
+    return hip_err(hipGetLastError());
+}
+
+int32_t evict(const attn_shape* s, int32_t n_req, const int32_t* rows, const int32_t* keep, const int32_t* first, const int32_t* recent,
+              const attn_pages* pages, void* k_pool, void* v_pool, float* w_pool, int64_t w_stride, const int32_t* page_cu,
+              const int32_t* page_ids, const int32_t* new_page_cu, const int32_t* new_page_ids, int32_t* index, void* workspace,
+              int64_t workspace_bytes, hipStream_t stream) {
+    int32_t rc = check_front(s, n_req, pages);
+    if (rc != GDN_OK) return rc;
+    if (w_stride < (int64_t)s->H_kv * pages->page_rows) return GDN_ERR_SHAPE;
+    if (n_req == 0) return GDN_OK;
+    if (!rows || !keep || !first || !recent) return GDN_ERR_NULL;
+    std::vector<int32_t> kept(n_req);
+    int64_t total = 0;
+    for (int32_t r = 0; r < n_req; ++r) {
+        if (rows[r] < 0 || keep[r] < 0 || first[r] < 0 || recent[r] < 0 || rows[r] > MAX_ROWS) return GDN_ERR_START;
+        kept[r] = std::min(keep[r], rows[r]);
+        if ((int64_t)first[r] + recent[r] > kept[r]) return GDN_ERR_START;
+        total += kept[r];
+    }
+    if (total * s->H_kv > INT32_MAX) return GDN_ERR_COUNT;
+    rc = check_table(pages, n_req, page_cu, page_ids, [&](int32_t r) { return (int64_t)rows[r]; });
+    if (rc != GDN_OK) return rc;
+    rc = check_table(pages, n_req, new_page_cu, new_page_ids, [&](int32_t r) { return (int64_t)kept[r]; });
+    if (rc != GDN_OK) return rc;
+    const int32_t n_old = page_cu[n_req], n_new = new_page_cu[n_req];
+    PageSet fresh(pages->n_pages);
+    for (int32_t i = 0; i < n_new; ++i)
+        if (!fresh.add(new_page_ids[i])) return GDN_ERR_SLOT_DUP;
+    for (int32_t i = 0; i < n_old; ++i)
+        if (fresh.has(page_ids[i])) return GDN_ERR_SLOT_HAZARD;
+    if (total == 0) return GDN_OK;
+    if (!k_pool || !v_pool || !w_pool || !index) return GDN_ERR_NULL;
+    if (!aligned16(k_pool) || !aligned16(v_pool)) return GDN_ERR_ALIGN;
+    if (reinterpret_cast<uintptr_t>(w_pool) % 4 != 0 || reinterpret_cast<uintptr_t>(index) % 4 != 0) return GDN_ERR_ALIGN;
+    rc = check_workspace(s, n_req, 0, (int64_t)n_old + n_new, workspace, workspace_bytes);
+    if (rc != GDN_OK) return rc;
+
+    std::vector<int32_t> img((size_t)(7 * (int64_t)n_req + 1 + n_old + n_new));
+    int32_t* p = img.data();
+    p = std::copy(rows, rows + n_req, p);
+    p = std::copy(kept.begin(), kept.end(), p);
+    p = std::copy(first, first + n_req, p);
+    p = std::copy(recent, recent + n_req, p);
+    p = std::copy(page_cu, page_cu + n_req, p);
+    for (int32_t r = 0; r < n_req; ++r) *p++ = n_old + new_page_cu[r];
+    *p++ = 0;
+    for (int32_t r = 0; r < n_req; ++r, ++p) *p = p[-1] + kept[r];
+    p = std::copy(page_ids, page_ids + n_old, p);
+    p = std::copy(new_page_ids, new_page_ids + n_new, p);
+    rc = gdn::upload_plan(img.data(), img.size() * sizeof(int32_t), workspace, stream);
+    if (rc != GDN_OK) return rc;
+    const int32_t* const d = static_cast<const int32_t*>(workspace);
+    EvictArgs a;
+    a.k_pool = static_cast<uint16_t*>(k_pool);
+    a.v_pool = static_cast<uint16_t*>(v_pool);
+    a.w_pool = w_pool;
+    a.index = index;
+    a.rows = d;
+    a.keep = d + n_req;
+    a.first = d + 2 * (int64_t)n_req;
+    a.recent = d + 3 * (int64_t)n_req;
+    a.place = d + 4 * (int64_t)n_req;
+    a.new_place = d + 5 * (int64_t)n_req;
+    a.keep_cu = d + 6 * (int64_t)n_req;
+    a.page_ids = d + 7 * (int64_t)n_req + 1;
+    a.page_stride = pages->page_stride;
+    a.w_stride = w_stride;
+    a.n_req = n_req;
+    a.H_kv = s->H_kv;
+    a.page_shift = shift_of(pages);
+    a.chunks = s->d / 8;
+    const int64_t n = total * s->H_kv * a.chunks, blocks = (n + GATHER_THREADS - 1) / GATHER_THREADS;
+    if (blocks > INT32_MAX || (int64_t)n_req * s->H_kv > INT32_MAX) return GDN_ERR_COUNT;
+    hipLaunchKernelGGL(attn_select_kernel, dim3((unsigned)(n_req * s->H_kv)), dim3(SEL_THREADS), 0, stream, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return hip_err(e);
+    hipLaunchKernelGGL(attn_gather_rows_kernel, dim3((unsigned)blocks), dim3(GATHER_THREADS), 0, stream, a, n);
+    return hip_err(hipGetLastError());
+}
+
+// No exception leaves a C entry: host memory that runs out is a count too large.
+template <typename F>
+int32_t guarded(F f) {
+    try {
+        return f();
+    } catch (const std::bad_alloc&) {
+        return GDN_ERR_COUNT;
+    } catch (const std::length_error&) {
+        return GDN_ERR_COUNT;
+    }
+}
+
+}  // namespace
+}  // namespace attn
+
+using namespace attn;
+
+extern "C" {
+
+int32_t attn_rope_freqs(int32_t rot, double base, int32_t kind, double factor, double context, double fast, double slow, double* freq,
+                        double* amplitude) {
+    if (!amplitude || (rot > 0 && !freq)) return GDN_ERR_NULL;
+    if (rot < 0 || rot % 2 != 0 || !(base > 1.0) || !std::isfinite(base)) return GDN_ERR_SHAPE;
+    if (kind < ATTN_ROPE_PLAIN || kind > ATTN_ROPE_RAMP) return GDN_ERR_SHAPE;
+    if (kind != ATTN_ROPE_PLAIN && !(factor >= 1.0 && std::isfinite(factor))) return GDN_ERR_SHAPE;
+    if (kind == ATTN_ROPE_BASE && rot == 2) return GDN_ERR_SHAPE;
+    *amplitude = 1.0;
+    double lo = 0.0, hi = 0.0;
+    if (kind == ATTN_ROPE_RAMP) {
+        if (!(context > 0.0 && std::isfinite(context) && slow > 0.0 && fast > slow && std::isfinite(fast))) return GDN_ERR_SHAPE;
+        *amplitude = 0.1 * std::log(factor) + 1.0;
+        // the pair (a real number) that makes `turns` turns over the context
+        auto at = [&](double turns) { return rot * std::log(context / (turns * 6.283185307179586)) / (2.0 * std::log(base)); };
+        lo = std::max(std::floor(at(fast)), 0.0);
+        hi = std::min(std::ceil(at(slow)), (double)rot - 1.0);
+    }
+    if (kind == ATTN_ROPE_BASE && rot > 2) base *= std::pow(factor, (double)rot / (rot - 2));
+    for (int32_t p = 0; p < rot / 2; ++p) {
+        double f = std::pow(base, -2.0 * p / rot);
+        if (kind == ATTN_ROPE_LINEAR) f /= factor;
+        if (kind == ATTN_ROPE_RAMP) {
+            const double w = std::min(std::max((p - lo) / std::max(hi - lo, 0.001), 0.0), 1.0);
+            f = f * (1.0 - w) + f / factor * w;
+        }
+        freq[p] = f;
+    }
+    return GDN_OK;
+}
+
+int64_t attn_paged_workspace_bytes(const attn_shape* s, int32_t n_req, int64_t total_tokens, int64_t n_page_ids) {
+    const int32_t rc = check_shape(s);
+    if (rc != GDN_OK) return rc;
+    if (n_req < 0 || total_tokens < 0 || total_tokens > INT32_MAX || n_page_ids < 0 || n_page_ids > 2 * (int64_t)INT32_MAX) return GDN_ERR_COUNT;
+    return image_bytes(s, n_req, total_tokens, n_page_ids) + parts_bytes(s->d);
+}
+
+int32_t attn_rope_append(const attn_shape* s, const attn_rope* rope, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v,
+                         int64_t ldv, int32_t n_req, const int32_t* cu_seqlens, const int32_t* pos, const int32_t* start,
+                         const attn_pages* pages, void* k_pool, void* v_pool, const int32_t* page_cu, const int32_t* page_ids, void* q_out,
+                         void* workspace, int64_t workspace_bytes, void* stream) {
+    return guarded([&] {
+        return rope_append(s, rope, q, ldq, k, ldk, v, ldv, n_req, cu_seqlens, pos, start, pages, k_pool, v_pool, page_cu, page_ids, q_out,
+                           workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+    });
+}
+
+int32_t attn_paged_prefill(const attn_shape* s, const void* q, const void* out_gate, int32_t n_req, const int32_t* cu_seqlens,
+                           const int32_t* start, const attn_pages* pages, const void* k_pool, const void* v_pool, const int32_t* page_cu,
+                           const int32_t* page_ids, void* o, float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
+    return guarded([&] {
+        return paged_prefill(s, q, out_gate, n_req, cu_seqlens, start, pages, k_pool, v_pool, page_cu, page_ids, o, lse, workspace,
+                             workspace_bytes, static_cast<hipStream_t>(stream));
+    });
+}
+
+int32_t attn_key_weights(const attn_shape* s, const void* q, const float* lse, int32_t n_req, const int32_t* cu_seqlens,
+                         const int32_t* start, const attn_pages* pages, const void* k_pool, const int32_t* page_cu, const int32_t* page_ids,
+                         float decay, const float* w_in, float* w_out, int64_t w_stride, void* workspace, int64_t workspace_bytes,
+                         void* stream) {
+    return guarded([&] {
+        return key_weights(s, q, lse, n_req, cu_seqlens, start, pages, k_pool, page_cu, page_ids, decay, w_in, w_out, w_stride, workspace,
+                           workspace_bytes, static_cast<hipStream_t>(stream));
+    });
+}
+
+int32_t attn_evict(const attn_shape* s, int32_t n_req, const int32_t* rows, const int32_t* keep, const int32_t* first,
+                   const int32_t* recent, const attn_pages* pages, void* k_pool, void* v_pool, float* w_pool, int64_t w_stride,
+                   const int32_t* page_cu, const int32_t* page_ids, const int32_t* new_page_cu, const int32_t* new_page_ids, int32_t* index,
+                   void* workspace, int64_t workspace_bytes, void* stream) {
+    return guarded([&] {
+        return evict(s, n_req, rows, keep, first, recent, pages, k_pool, v_pool, w_pool, w_stride, page_cu, page_ids, new_page_cu,
+                     new_page_ids, index, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+    });
+}
+
+}  // extern "C"

@@ -1,0 +1,583 @@
+"""The paged key/value cache (include/attn_paged.h) against its oracle.
+
+CPU part: exports, the frequencies, the refusals.  GPU part (marked gpu), through the C ABI, on pools whose unused rows and
+pages hold NaN.  The tolerances, from the roundings (half a step: bf16 2^-8, fp16 2^-11, fp32 2^-24 relative):
+
+  rotated q, k  2^-8 |ref| for the store, and 2^-20 amplitude (|x| + |y|) for the angle (2^-25 of a turn from its fp32 value),
+                cosine, sine and three fp32 roundings; values are numpy's own float16 conversion, bit for bit
+  o             every weight is off by 2^-11 at most and they are normalised by their own sum: 2 * 2^-11 max |v - o| <= 2^-9 max |v|,
+                twice the step for what the fp32 sums add (2^-8 max |v|), and 2^-8 |ref| for a bf16 store
+  lse           a logit is a sum of d products in fp32, (d + 16) 2^-24 scale sum |q_i k_i|, and so is their log-sum-exp; 2^-20 (1 + |lse|) for
+                the exponentials, the logarithm and the scaling
+  weights       each term off by e^x - 1 with x the error of a logit and of lse in fp32 (2^-22 |lse|), and rows 2^-24 for the sum
+  eviction      copies: bit for bit
+"""
+import ctypes
+import os
+import re
+
+import numpy as np
+import pytest
+
+from oracle import attn_oracle as ao, paged_oracle as po
+from paper_2605_05219_amd import attention as AT, binding as B, paged as PG, workloads as wl
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+# ----------------------------------------------------------------------------- host
+def test_library_exports_every_symbol_the_paged_header_declares():
+    header = open(os.path.join(ROOT, "include", "attn_paged.h")).read()
+    header = re.sub(r"/\*.*?\*/", "", header, flags=re.S)
+    declared = set(re.findall(r"\b(attn_\w+)\s*\(", header))
+    assert declared == set(PG.EXPORTS)
+    L = ctypes.CDLL(B.LIB_PATH)
+    for name in declared:
+        assert getattr(L, name) is not None
+
+
+@pytest.mark.parametrize("rot", [2, 16, 64, 128, 256])
+@pytest.mark.parametrize("kw", [dict(), dict(kind="linear", factor=8.0), dict(kind="base", factor=4.0), dict(kind="ramp", factor=16.0, context=4096.0),
+                                dict(kind="ramp", factor=2.0, context=100.0, fast=8.0, slow=0.5), dict(kind="ramp", factor=1.0, context=10.0)])
+def test_frequencies_are_the_formulas(rot, kw):
+    if rot == 2 and kw.get("kind") == "base":
+        with pytest.raises(B.GdnError):
+            PG.attn_rope_freqs(rot, **kw)
+        return
+    f, a = PG.attn_rope_freqs(rot, 10000.0, **kw)
+    rf, ra = po.rope_freqs(rot, 10000.0, **kw)
+    np.testing.assert_allclose(f, rf, rtol=1e-13)
+    assert a == pytest.approx(ra, rel=1e-15)
+    assert PG.attn_rope_freqs(0)[0].size == 0
+
+
+@pytest.mark.parametrize("args,kw", [((15,), {}), ((-2,), {}), ((16, 1.0), {}), ((16, float("nan")), {}), ((16, 1e4), dict(kind="linear", factor=0.5)),
+                                     ((16, 1e4), dict(kind="ramp", factor=2.0, context=0.0)), ((16, 1e4), dict(kind="base", factor=float("inf"))),
+                                     ((16, 1e4), dict(kind="ramp", factor=2.0, context=100.0, fast=1.0, slow=1.0))])
+def test_frequencies_refuse(args, kw):
+    with pytest.raises(B.GdnError) as ei:
+        PG.attn_rope_freqs(*args, **kw)
+    assert ei.value.code == -3
+
+
+class FakePool:
+    """Stands in for a device tensor: the checks under test return before any pointer is used."""
+
+    def __init__(self, ptr=0x10000, shape=(40, 2, 16, 64), stride0=None, nbytes=1 << 30):
+        self._ptr, self.shape, self._n = ptr, shape, nbytes
+        self._s0 = int(np.prod(shape[1:])) if stride0 is None else stride0
+
+    def data_ptr(self): return self._ptr
+    def stride(self, i): return self._s0
+    def numel(self): return self._n
+    def element_size(self): return 1
+
+
+K_POOL, V_POOL, W_POOL = FakePool(0x200000), FakePool(0x300000), FakePool(0x400000, (40, 2, 16))
+X = FakePool(0x10000, (9, 4, 64))
+WS = FakePool(0x100000)
+CALL = dict(shape=AT.make_attn_shape(4, 2, 64), cu_seqlens=[0, 5, 9], start=[0, 20], k_pool=K_POOL, v_pool=V_POOL, page_cu=[0, 1, 3],
+            page_ids=[7, 3, 39], workspace=WS)
+FRONT = [                                                                     # what every call refuses
+    (dict(shape=AT.make_attn_shape(4, 2, 96)), -3),
+    (dict(shape=AT.make_attn_shape(4, 3, 64)), -3),
+    (dict(k_pool=FakePool(0x200000, (40, 2, 24, 64)), v_pool=FakePool(0x300000, (40, 2, 24, 64))), -3),   # rows per page
+    (dict(k_pool=FakePool(0x200000, (40, 2, 8, 64)), v_pool=FakePool(0x300000, (40, 2, 8, 64))), -3),
+    (dict(k_pool=FakePool(0x200000, stride0=2044), v_pool=FakePool(0x300000, stride0=2044)), -2),
+    (dict(k_pool=FakePool(0x200000, stride0=1024), v_pool=FakePool(0x300000, stride0=1024)), -3),         # pages would overlap
+    (dict(page_ids=[7, 3, 40]), -5),
+    (dict(page_ids=[-1, 3, 39]), -5),
+    (dict(k_pool=FakePool(0)), -1),
+    (dict(k_pool=FakePool(0x200008)), -2),
+    (dict(workspace=None), -9),
+    (dict(workspace=FakePool(0x100000, nbytes=64)), -9),
+    (dict(workspace=FakePool(0x100004)), -9),
+]
+TOKENS = FRONT + [
+    (dict(cu_seqlens=[1, 5, 9]), -4),
+    (dict(cu_seqlens=[0, 5, 4]), -4),
+    (dict(page_cu=[1, 1, 3]), -4),
+    (dict(page_cu=[0, 3, 1]), -4),
+    (dict(start=[-1, 20]), -10),
+    (dict(start=[0, 29]), -10),                                               # 33 rows, two pages
+    (dict(start=[0, 2 ** 31 - 5]), -10),
+    (dict(page_cu=[0, 0, 3]), -10),
+]
+
+
+def refused(fn, code, *args):
+    with pytest.raises(B.GdnError) as ei:
+        fn(*args)
+    assert ei.value.code == code
+
+
+@pytest.fixture
+def no_stream(monkeypatch):
+    monkeypatch.setattr(PG, "_stream_ptr", lambda s=None: ctypes.c_void_p(0))
+
+
+@pytest.mark.parametrize("over,code", TOKENS + [
+    (dict(page_ids=[7, 3, 3]), -6), (dict(page_ids=[39, 3, 39]), -6),         # a page that gets rows, listed twice
+    (dict(page_ids=[3, 3, 39]), -6),                                          # ... among the rows another request holds
+    (dict(pos=[0, -1]), -10), (dict(pos=[0, 2 ** 31 - 3]), -10),
+    (dict(rope=PG.make_attn_rope(np.ones(36))), -3), (dict(rope=PG.make_attn_rope(np.ones(4))), -3),
+    (dict(rope=PG.make_attn_rope(np.full(8, np.inf))), -3), (dict(rope=PG.make_attn_rope(np.ones(8), amplitude=float("nan"))), -3),
+    (dict(q=FakePool(0, (9, 4, 64))), -1), (dict(k=FakePool(0x10002, (9, 2, 64))), -2), (dict(q_out=FakePool(0x10008, (9, 4, 64))), -2),
+    (dict(v=FakePool(0x10000, (9, 2, 64), 132)), -2), (dict(q=FakePool(0x10000, (9, 4, 64), 128)), -3),
+])
+def test_rope_append_refuses(no_stream, over, code):
+    a = dict(CALL, rope=PG.make_attn_rope(np.ones(32)), q=X, k=FakePool(0x10000, (9, 2, 64)), v=FakePool(0x10000, (9, 2, 64)), pos=[0, 100], q_out=X)
+    a.update(over)
+    refused(PG.attn_rope_append, code, a["shape"], a["rope"], a["q"], a["k"], a["v"], a["cu_seqlens"], a["pos"], a["start"], a["k_pool"], a["v_pool"],
+            a["page_cu"], a["page_ids"], a["q_out"], a["workspace"])
+
+
+@pytest.mark.parametrize("over,code", TOKENS + [
+    (dict(q=FakePool(0, (9, 4, 64))), -1), (dict(o=FakePool(0)), -1), (dict(o=FakePool(0x10004)), -2), (dict(gate=FakePool(0x10002)), -2),
+    (dict(lse=FakePool(0x10002)), -2), (dict(shape=AT.make_attn_shape(4, 2, 64, scale=0.0)), -3),
+])
+def test_paged_prefill_refuses(no_stream, over, code):
+    a = dict(CALL, q=X, gate=None, o=X, lse=None)
+    a.update(over)
+    refused(PG.attn_paged_prefill, code, a["shape"], a["q"], a["gate"], a["cu_seqlens"], a["start"], a["k_pool"], a["v_pool"], a["page_cu"],
+            a["page_ids"], a["o"], a["lse"], a["workspace"])
+
+
+@pytest.mark.parametrize("over,code", TOKENS + [
+    (dict(page_ids=[7, 7, 39]), -6), (dict(q=FakePool(0, (9, 4, 64))), -1), (dict(lse=FakePool(0)), -1), (dict(w_out=FakePool(0, (40, 2, 16))), -1),
+    (dict(w_out=FakePool(0x400002, (40, 2, 16))), -2), (dict(w_in=FakePool(0x400001, (40, 2, 16))), -2), (dict(decay=float("nan")), -3),
+    (dict(w_in=None, w_out=FakePool(0x400000, (40, 2, 16), 31)), -3), (dict(w_in=FakePool(0x400000, (40, 2, 16), 64)), -3),
+])
+def test_key_weights_refuses(no_stream, over, code):
+    a = dict(CALL, q=X, lse=FakePool(0x10000), decay=1.0, w_in=W_POOL, w_out=W_POOL)
+    a.update(over)
+    refused(PG.attn_key_weights, code, a["shape"], a["q"], a["lse"], a["cu_seqlens"], a["start"], a["k_pool"], a["page_cu"], a["page_ids"], a["decay"],
+            a["w_in"], a["w_out"], a["workspace"])
+
+
+@pytest.mark.parametrize("over,code", FRONT + [
+    (dict(rows=[17, 24]), -10), (dict(rows=[-1, 24]), -10), (dict(keep=[5, -1]), -10), (dict(first=[3, 2]), -10), (dict(recent=[2, 30]), -10),
+    (dict(keep=[5, 17]), -10), (dict(page_cu=[0, 3, 1]), -4), (dict(new_page_cu=[1, 1, 2]), -4),
+    (dict(new_page_ids=[1, 1]), -6), (dict(new_page_ids=[1, 40]), -5), (dict(new_page_ids=[1, 39]), -7), (dict(index=FakePool(0)), -1),
+    (dict(index=FakePool(0x10001)), -2), (dict(v_pool=FakePool(0)), -1), (dict(w_pool=FakePool(0x400000, (40, 2, 16), 31)), -3),
+])
+def test_evict_refuses(no_stream, over, code):
+    a = dict(CALL, rows=[5, 24], keep=[4, 10], first=[2, 2], recent=[2, 3], w_pool=W_POOL, new_page_cu=[0, 1, 2], new_page_ids=[1, 2], index=FakePool())
+    a.update(over)
+    refused(PG.attn_evict, code, a["shape"], a["rows"], a["keep"], a["first"], a["recent"], a["k_pool"], a["v_pool"], a["w_pool"], a["page_cu"],
+            a["page_ids"], a["new_page_cu"], a["new_page_ids"], a["index"], a["workspace"])
+
+
+def test_calls_with_nothing_to_do_touch_nothing(no_stream):
+    sh, rope = AT.make_attn_shape(4, 2, 64), PG.make_attn_rope(np.ones(32))
+    z = FakePool(0, (0, 4, 64))
+    for cu, st, tcu, ids in [([0], [], [0], []), ([0, 0, 0], [0, 3], [0, 0, 1], [7])]:
+        PG.attn_rope_append(sh, rope, z, z, z, cu, None, st, K_POOL, V_POOL, tcu, ids, z, None)
+        PG.attn_paged_prefill(sh, z, None, cu, st, K_POOL, V_POOL, tcu, ids, z, None, None)
+    PG.attn_key_weights(sh, z, z, [0, 0], [0], K_POOL, [0, 0], [], 1.0, None, W_POOL, None)
+    PG.attn_evict(sh, [0, 5], [3, 0], [0, 0], [0, 0], K_POOL, V_POOL, W_POOL, [0, 0, 1], [7], [0, 0, 0], [], z, None)
+    with pytest.raises(B.GdnError):
+        PG.attn_paged_workspace_bytes(sh, -1, 0, 0)
+    assert PG.attn_paged_workspace_bytes(sh, 3, 100, 500) > PG.attn_paged_workspace_bytes(sh, 3, 100, 0) > 0
+
+
+# ----------------------------------------------------------------------------- GPU
+def f64(bits):
+    return wl.to_f32(bits).astype(np.float64)
+
+
+class Paged:
+    """A call's pools on the device: every request's pages in no order, whatever no request holds NaN."""
+
+    def __init__(self, seed, H_q, H_kv, d, P, lens, starts, shared=0, extra=0, stride_pad=0):
+        import torch
+        rng = self.rng = np.random.default_rng(seed)
+        self.H_q, self.H_kv, self.d, self.P = H_q, H_kv, d, P
+        self.lens, self.starts = list(lens), list(starts)
+        self.total = [s + n for s, n in zip(starts, lens)]
+        self.T, R = sum(lens), len(lens)
+        self.cu = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+        sp = shared // P
+        pages = [-(-t // P) for t in self.total]
+        assert all(s >= sp * P for s in starts)
+        n_pages = sp + sum(p - sp for p in pages) + extra + 2
+        ids = rng.permutation(n_pages).astype(np.int32)
+        common, rest = ids[:sp], list(ids[sp:])
+        self.table = [np.concatenate([common, [rest.pop() for _ in range(p - sp)]]).astype(np.int32) for p in pages]
+        self.spare = np.array(rest, np.int32)
+        self.page_cu = np.concatenate([[0], np.cumsum(pages)]).astype(np.int32)
+        self.page_ids = np.concatenate(self.table + [np.zeros(0, np.int32)]).astype(np.int32)
+        size = H_kv * P * d
+        self.k_np = np.full((n_pages, size + stride_pad), 0x7fc0, np.uint16)
+        self.v_np = np.full((n_pages, size + stride_pad), np.nan, np.float16)
+        self.k_rows, self.v_rows = [], []
+        for r, t in enumerate(self.total):
+            k = wl.f32_to_bf16_bits(rng.standard_normal((t, H_kv, d), dtype=np.float32))
+            v = rng.standard_normal((t, H_kv, d)).astype(np.float16)
+            if r > 0:
+                k[:sp * P], v[:sp * P] = self.k_rows[0][:sp * P], self.v_rows[0][:sp * P]
+            self.k_rows.append(k)
+            self.v_rows.append(v)
+        self.shape = AT.make_attn_shape(H_q, H_kv, d, "bf16")
+        self.torch = torch
+
+    def place(self, r, count, table=None):
+        j = np.arange(count)
+        return (table if table is not None else self.table[r])[j // self.P], j % self.P
+
+    def view(self, a, d=None):
+        return a[:, :self.H_kv * self.P * (d or self.d)].reshape(a.shape[0], self.H_kv, self.P, -1)
+
+    def fill(self, held_only=False):
+        """Rows into the pools (those held before the call only, or all) and the pools to the device."""
+        for r in range(len(self.lens)):
+            n = self.starts[r] if held_only else self.total[r]
+            page, row = self.place(r, n)
+            self.view(self.k_np)[page, :, row] = self.k_rows[r][:n]
+            self.view(self.v_np)[page, :, row] = self.v_rows[r][:n]
+        t = self.torch
+        self.k_dev = t.from_numpy(self.k_np.view(np.int16)).cuda().view(t.bfloat16)
+        self.v_dev = t.from_numpy(self.v_np).cuda()
+        size = self.H_kv * self.P * self.d
+        self.k_pool, self.v_pool = (x[:, :size].unflatten(1, (self.H_kv, self.P, self.d)) for x in (self.k_dev, self.v_dev))
+        return self
+
+    def workspace(self, tokens=None, ids=None):
+        t = self.torch
+        n = PG.attn_paged_workspace_bytes(self.shape, len(self.lens), self.T if tokens is None else tokens, self.page_ids.size if ids is None else ids)
+        return t.full((n,), 0xA5, dtype=t.uint8, device="cuda")
+
+    def bf16(self, *shape, s=1.0):
+        return wl.f32_to_bf16_bits((self.rng.standard_normal(shape, dtype=np.float32) * np.float32(s)).astype(np.float32))
+
+    def dev(self, bits):
+        return self.torch.from_numpy(np.ascontiguousarray(bits).view(np.int16)).cuda().view(self.torch.bfloat16)
+
+
+def bits_of(t):
+    import torch
+    return t.contiguous().view(torch.int16).cpu().numpy().view(np.uint16)
+
+
+def logit_error(c, q):
+    """A bound of the error of a scaled logit in fp32."""
+    worst = max([np.sqrt((f64(k) ** 2).sum(-1)).max() for k in c.k_rows if k.size] + [0.0]) * np.sqrt((f64(q) ** 2).sum(-1)).max()
+    return (c.d + 16) * 2.0 ** -24 * c.d ** -0.5 * worst
+
+
+ROPE = [  # H_q, H_kv, d, P, rot, layout, dtype, lens, starts, pos
+    (4, 2, 64, 16, 64, "half", "bf16", [1], [0], [0]),
+    (4, 2, 64, 16, 64, "interleaved", "bf16", [5, 0, 37], [15, 3, 16], [7, 0, 2000000000]),
+    (6, 2, 128, 32, 32, "half", "f32", [33, 1], [31, 0], None),
+    (8, 1, 256, 64, 48, "interleaved", "f32", [3, 70], [1, 62], [123456789, 1]),
+    (3, 3, 128, 16, 0, "half", "bf16", [17], [8], [3]),
+    (16, 2, 128, 128, 128, "half", "bf16", [1] * 70, list(range(100, 170)), None),
+    (4, 4, 64, 16, 16, "half", "bf16", [1100], [5], [900000]),
+    (2, 1, 256, 32, 256, "half", "bf16", [9001], [0], [0]),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H_q,H_kv,d,P,rot,layout,dtype,lens,starts,pos", ROPE)
+@pytest.mark.parametrize("packed", [True, False])
+def test_rope_append(H_q, H_kv, d, P, rot, layout, dtype, lens, starts, pos, packed):
+    import torch
+    c = Paged(5, H_q, H_kv, d, P, lens, starts, stride_pad=0 if packed else 24).fill(held_only=True)
+    freqs, amp = PG.attn_rope_freqs(rot, 10000.0, "ramp", 8.0, 4096.0) if rot else (np.zeros(0), 1.0)
+    rope = PG.make_attn_rope(freqs, layout, amp, dtype)
+    heads = [H_q, H_kv, H_kv]
+    x = torch.randn(c.T, sum(heads) * d + (0 if packed else 8), generator=torch.Generator().manual_seed(1))
+    x = x if dtype == "f32" else x.bfloat16()
+    ref = x.double().numpy()
+    if packed:                       # tensors of their own, or column ranges of one projection's output
+        parts = [y.contiguous().cuda().unflatten(1, (-1, d)) for y in x.split([h * d for h in heads], 1)]
+    else:
+        parts = [y.unflatten(1, (-1, d)) for y in x.cuda()[:, 8:].split([h * d for h in heads], 1)]
+        ref = ref[:, 8:]
+    q, k, v = (y.reshape(c.T, -1, d) for y in np.split(ref, np.cumsum([h * d for h in heads])[:2], 1))
+    q_out = parts[0] if packed and dtype == "bf16" else torch.zeros(c.T, H_q, d, dtype=torch.bfloat16, device="cuda")   # in place where it may be
+    before_k, before_v = c.k_dev.clone(), c.v_dev.clone()
+    PG.attn_rope_append(c.shape, rope, *parts, c.cu, pos, starts, c.k_pool, c.v_pool, c.page_cu, c.page_ids, q_out, c.workspace())
+    got_q = q_out.double().cpu().numpy()
+    k_after, v_after = c.k_pool.double().cpu().numpy(), bits_of(c.v_pool)
+    m = rot // 2
+    for r, n in enumerate(lens):
+        if n == 0:
+            continue
+        s, p0 = slice(c.cu[r], c.cu[r + 1]), starts[r] if pos is None else pos[r]
+        page, row = c.place(r, c.total[r])
+        page, row = page[starts[r]:], row[starts[r]:]
+        few = np.unique(np.r_[0:min(n, 20), max(0, n - 20):n, n // 2])     # of long calls some tokens
+        for got, src in ((got_q[s], q[s]), (k_after[page, :, row], k[s])):
+            for i in few:
+                want = po.rotate(src[i:i + 1], p0 + i, freqs, layout, amp)
+                pair = np.abs(src[i:i + 1]).copy()
+                if m:
+                    a, b = (slice(0, m), slice(m, rot)) if layout == "half" else (slice(0, rot, 2), slice(1, rot, 2))
+                    both = pair[..., a] + pair[..., b]
+                    pair[..., a], pair[..., b] = both, both
+                assert (np.abs(got[i:i + 1] - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -20 * amp * pair).all(), (r, i)
+        assert np.array_equal(v_after[page, :, row], v[s].astype(np.float32).astype(np.float16).view(np.uint16)), r
+    # nothing else was written
+    mask = torch.ones_like(c.k_dev, dtype=torch.bool)
+    mv = mask[:, :H_kv * P * d].unflatten(1, (H_kv, P, d))
+    for r in range(len(lens)):
+        page, row = c.place(r, c.total[r])
+        mv[torch.from_numpy(page[starts[r]:].astype(np.int64)).cuda(), :, torch.from_numpy(row[starts[r]:]).cuda()] = False
+    for a, b in ((before_k, c.k_dev), (before_v, c.v_dev)):
+        assert torch.equal(a.view(torch.int16)[mask], b.view(torch.int16)[mask])
+
+
+ATTEND = [  # H_q, H_kv, d, P, lens, starts, shared, gate, dtype
+    (4, 2, 64, 16, [1], [0], 0, False, "bf16"),                              # one token, one row
+    (4, 2, 128, 16, [1, 0, 2, 17, 64, 65], [0, 7, 1, 15, 33, 200], 0, True, "f32"),
+    (8, 1, 256, 32, [3, 130], [31, 40], 0, False, "bf16"),
+    (6, 2, 64, 64, [5, 200], [100, 63], 0, False, "bf16"),                   # a group of three: not packed
+    (1, 1, 128, 128, [129], [0], 0, False, "f32"),
+    (16, 2, 128, 256, [300, 40], [700, 0], 0, True, "bf16"),
+    (16, 2, 128, 16, [1, 1, 1], [1500, 1023, 2047], 0, False, "bf16"),       # decoding: the few-rows kernel, walks cut
+    (8, 8, 64, 32, [2, 1], [1100, 5000], 0, True, "f32"),
+    (8, 1, 256, 16, [1, 2], [1300, 1022], 0, False, "bf16"),
+    (4, 1, 128, 64, [1] * 40, [1000 + 37 * i for i in range(40)], 0, False, "bf16"),
+    (16, 2, 128, 64, [1, 1, 100], [4000, 1200, 900], 0, False, "bf16"),      # both kinds in one call
+    (16, 2, 128, 16, [1, 30, 200], [600, 512, 700], 512, False, "bf16"),     # a shared prefix
+    (32, 4, 128, 128, [700], [2000], 0, False, "bf16"),                      # walks cut, two heads to a workgroup
+    (2, 2, 256, 128, [50], [9000], 0, False, "f32"),
+    (16, 2, 64, 16, [1], [20000], 0, False, "f32"),                          # more steps than page ids are held at once
+    (4, 2, 128, 16, [600], [8000], 0, False, "bf16"),
+]
+
+
+def run_attend(c, q, gate, dtype, lse=True, stream=None):
+    t = c.torch
+    sh = AT.make_attn_shape(c.H_q, c.H_kv, c.d, dtype)
+    o = t.full((c.T, c.H_q, c.d), float("nan"), dtype=t.float32 if dtype == "f32" else t.bfloat16, device="cuda")
+    z = t.full((c.T, c.H_q), float("nan"), device="cuda") if lse else None
+    PG.attn_paged_prefill(sh, c.dev(q), c.dev(gate) if gate is not None else None, c.cu, c.starts, c.k_pool, c.v_pool, c.page_cu, c.page_ids, o, z,
+                          c.workspace(), stream)
+    return o, z
+
+
+def check_attend(c, q, gate, dtype, o, z):
+    scale = c.d ** -0.5
+    o, z = o.double().cpu().numpy(), z.cpu().numpy().astype(np.float64) if z is not None else None
+    le = logit_error(c, q) if c.T else 0.0
+    for r in range(len(c.lens)):
+        if c.lens[r] == 0:
+            continue
+        s = slice(c.cu[r], c.cu[r + 1])
+        k, v = f64(c.k_rows[r]), c.v_rows[r].astype(np.float64)
+        ref = ao.attention_suffix(f64(q[s]), k, v, c.starts[r], scale)
+        if gate is not None:
+            ref = ao.output_gate(ref, f64(gate[s]))
+        tol = 2.0 ** -8 * np.abs(v).max() + (2.0 ** -8 * np.abs(ref) if dtype == "bf16" else 0.0)
+        assert (np.abs(o[s] - ref) <= tol).all(), (r, np.nanmax(np.abs(o[s] - ref)), np.isnan(o[s]).sum())
+        if z is not None:
+            zr = po.row_lse(f64(q[s]), k, c.starts[r], scale)
+            assert (np.abs(z[s] - zr) <= le + 2.0 ** -20 * (1 + np.abs(zr))).all(), (r, np.nanmax(np.abs(z[s] - zr)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H_q,H_kv,d,P,lens,starts,shared,gate,dtype", ATTEND)
+def test_paged_prefill(H_q, H_kv, d, P, lens, starts, shared, gate, dtype):
+    c = Paged(11, H_q, H_kv, d, P, lens, starts, shared, stride_pad=8).fill()
+    q, g = c.bf16(c.T, H_q, d, s=2.0), c.bf16(c.T, H_q, d) if gate else None
+    o, z = run_attend(c, q, g, dtype)
+    check_attend(c, q, g, dtype, o, z)
+    o2, _ = run_attend(c, q, g, dtype, lse=False)
+    assert np.array_equal(bits_of(o2), bits_of(o))                          # asking for lse changes no bit of o
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("seed", range(6))
+def test_paged_prefill_equals_the_slot_form_bit_for_bit(seed):
+    """The same rows in slots and in pages: the same kernels walk them in the same order."""
+    import torch
+    rng = np.random.default_rng(100 + seed)
+    H_q, H_kv = [(16, 2), (4, 4), (8, 1), (32, 4), (6, 2), (16, 2)][seed]
+    d, P = int(rng.choice([64, 128, 256])), int(rng.choice([16, 64, 128]))
+    R = int(rng.integers(1, 6))
+    lens, starts = [int(x) for x in rng.integers(1, 300, R)], [int(x) for x in rng.integers(0, 2500, R)]
+    if seed % 2:
+        lens = [1] * R
+    c = Paged(200 + seed, H_q, H_kv, d, P, lens, starts).fill()
+    q = c.bf16(c.T, H_q, d)
+    cap = max(c.total)
+    kc, vc = np.zeros((R, cap, H_kv, d), np.uint16), np.zeros((R, cap, H_kv, d), np.float16)
+    # the slot form appends itself: its new values come in bf16, so the pages get what that widens to
+    v_new = [wl.f32_to_bf16_bits(v[s:].astype(np.float32)) for v, s in zip(c.v_rows, starts)]
+    for r in range(R):
+        c.v_rows[r][starts[r]:] = wl.to_f32(v_new[r]).astype(np.float16)
+        kc[r, :starts[r]], vc[r, :starts[r]] = c.k_rows[r][:starts[r]], c.v_rows[r][:starts[r]]
+    c.fill()
+    o, _ = run_attend(c, q, None, "f32", lse=False)
+    sh = AT.make_attn_shape(H_q, H_kv, d, "f32")
+    os_ = torch.zeros_like(o)
+    ws = torch.empty(AT.attn_workspace_bytes(sh, R, c.T), dtype=torch.uint8, device="cuda")
+    AT.attn_suffix_prefill(sh, c.dev(q), c.dev(np.concatenate([k[s:] for k, s in zip(c.k_rows, starts)])), c.dev(np.concatenate(v_new)), None, c.cu, starts,
+                           c.dev(kc), torch.from_numpy(vc).cuda(), list(range(R)), os_, ws)
+    assert torch.equal(o, os_)
+
+
+WEIGHTS = [  # H_q, H_kv, d, P, lens, starts, w_in: None, "in", "same"
+    (4, 2, 64, 16, [1], [0], None),
+    (4, 2, 128, 16, [1, 0, 0, 2, 33], [0, 70, 0, 300, 15], "in"),
+    (8, 1, 256, 32, [3, 130], [31, 400], "same"),
+    (6, 2, 64, 64, [5, 200], [100, 63], "in"),
+    (16, 2, 128, 256, [300, 40], [700, 0], "in"),
+    (32, 1, 128, 16, [1, 1, 1], [1500, 1023, 255], "in"),
+    (48, 1, 64, 128, [2], [600], None),
+    (16, 2, 128, 64, [1200], [0], "same"),                                  # rows cut into parts
+    (3, 3, 256, 16, [900, 7], [33, 500], "in"),
+    (16, 4, 128, 32, [1] * 70, [10 * i for i in range(70)], "in"),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H_q,H_kv,d,P,lens,starts,w_in", WEIGHTS)
+def test_key_weights(H_q, H_kv, d, P, lens, starts, w_in):
+    import torch
+    c = Paged(21, H_q, H_kv, d, P, lens, starts).fill()
+    q = c.bf16(c.T, H_q, d, s=2.0)
+    scale, decay = d ** -0.5, 0.75
+    lse = np.zeros((c.T, H_q), np.float32)
+    for r in range(len(lens)):
+        if lens[r]:
+            lse[c.cu[r]:c.cu[r + 1]] = po.row_lse(f64(q[c.cu[r]:c.cu[r + 1]]), f64(c.k_rows[r]), starts[r], scale)
+    n_pages = c.k_np.shape[0]
+    w_np = np.full((n_pages, H_kv, P), np.nan, np.float32)
+    held = [c.rng.exponential(size=(s, H_kv)).astype(np.float32) for s in starts]
+    for r, s in enumerate(starts):
+        page, row = c.place(r, s)
+        w_np[page, :, row] = held[r]
+    w0 = torch.from_numpy(w_np).cuda()
+    w_out = w0 if w_in == "same" else torch.full_like(w0, float("nan"))
+    PG.attn_key_weights(c.shape, c.dev(q), torch.from_numpy(lse).cuda(), c.cu, starts, c.k_pool, c.page_cu, c.page_ids, decay,
+                        None if w_in is None else w0, w_out, c.workspace())
+    got = w_out.cpu().numpy().astype(np.float64)
+    untouched = np.ones(got.shape, bool)
+    rtol = np.expm1(logit_error(c, q) + 2.0 ** -22 * (1 + np.abs(lse).max())) + (max(lens) * (H_q // H_kv) + 8) * 2.0 ** -24
+    for r in range(len(lens)):
+        page, row = c.place(r, c.total[r])
+        s = slice(c.cu[r], c.cu[r + 1])
+        ref = po.key_weights(f64(q[s]), lse[s], f64(c.k_rows[r]), starts[r], scale, decay, held[r] if w_in else None) if lens[r] else \
+            (decay * held[r].astype(np.float64) if w_in else np.zeros((starts[r], H_kv)))
+        x = got[page, :, row]
+        assert (np.abs(x - ref) <= rtol * ref).all(), (r, np.nanmax(np.abs(x - ref) / ref))
+        untouched[page, :, row] = False
+    assert np.isnan(got[untouched]).all()
+
+
+EVICT = [  # H_kv, d, P, rows, keep, first, recent, weights
+    (2, 64, 16, [40], [10], [2], [3], "normal"),
+    (1, 128, 16, [1, 0, 33, 16], [1, 5, 16, 16], [0, 0, 4, 0], [0, 0, 4, 16], "normal"),
+    (2, 64, 32, [100, 70], [100, 90], [0, 5], [0, 5], "normal"),              # everything is kept
+    (4, 256, 64, [1000, 31], [500, 31], [4, 0], [64, 0], "ties"),
+    (2, 64, 16, [300], [100], [0], [0], "equal"),
+    (2, 128, 128, [5000], [1234], [4], [64], "odd"),                          # NaN, infinities, zeros of both signs, negative ones
+    (1, 64, 16, [50], [30], [10], [20], "normal"),                            # first and last rows alone
+    (3, 64, 256, [20000, 9, 4097], [2000, 3, 4096], [4, 1, 0], [128, 1, 0], "ties"),
+    (2, 64, 16, [64], [0], [0], [0], "normal"),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H_kv,d,P,rows,keep,first,recent,kind", EVICT)
+def test_evict(H_kv, d, P, rows, keep, first, recent, kind):
+    import torch
+    kept = [min(a, b) for a, b in zip(keep, rows)]
+    new_n = [-(-m // P) for m in kept]
+    c = Paged(31, H_kv, H_kv, d, P, [0] * len(rows), rows, extra=sum(new_n)).fill()
+    w_np = np.full(c.k_np.shape[:1] + (H_kv, P), np.nan, np.float32)
+    w_rows = []
+    for r, n in enumerate(rows):
+        w = c.rng.standard_normal((n, H_kv)).astype(np.float32)
+        if kind == "ties":
+            w = np.round(w)
+        if kind == "equal":
+            w[:] = 0.25
+        if kind == "odd":
+            w = np.maximum(w, 0)                                             # the lowest row of many equal ones
+            for x in (np.nan, np.inf, -np.inf, -0.0, 0.0, -1.0, 1e-45):
+                w[c.rng.integers(0, n, 300), :] = x
+        w_rows.append(w)
+        page, row = c.place(r, n)
+        w_np[page, :, row] = w
+    spare = list(c.spare)
+    new_table = [np.array([spare.pop() for _ in range(m)], np.int32) for m in new_n]
+    new_cu = np.concatenate([[0], np.cumsum(new_n)]).astype(np.int32)
+    w_pool = torch.from_numpy(w_np).cuda()
+    index = torch.full((max(1, sum(kept) * H_kv),), -7, dtype=torch.int32, device="cuda")
+    PG.attn_evict(c.shape, rows, keep, first, recent, c.k_pool, c.v_pool, w_pool, c.page_cu, c.page_ids, new_cu,
+                  np.concatenate(new_table + [np.zeros(0, np.int32)]), index, c.workspace(0, c.page_ids.size + sum(new_n)))
+    k_got, v_got, w_got, idx = bits_of(c.k_pool), bits_of(c.v_pool), w_pool.cpu().numpy(), index.cpu().numpy()
+    k_ref, v_ref, w_ref = c.view(c.k_np).copy(), c.view(c.v_np).copy(), w_np.copy()
+    at = 0
+    for r in range(len(rows)):
+        page, row = c.place(r, kept[r], new_table[r])
+        for g in range(H_kv):
+            want = po.rows_kept(w_rows[r][:, g], keep[r], first[r], recent[r])
+            assert len(want) == kept[r]
+            assert np.array_equal(idx[at:at + kept[r]], want), (r, g)
+            at += kept[r]
+            k_ref[page, g, row] = c.k_rows[r][want, g]
+            v_ref[page, g, row] = c.v_rows[r][want, g]
+            w_ref[page, g, row] = w_rows[r][want, g]
+    assert np.array_equal(k_got, k_ref) and np.array_equal(v_got, v_ref.view(np.uint16))
+    assert np.array_equal(w_got.view(np.uint32), w_ref.view(np.uint32))
+
+
+@pytest.mark.gpu
+def test_pages_behind_32_bit_offsets():
+    """Pages whose offsets pass 2^31 elements (2^32 bytes and more): every operator reads and writes the right ones."""
+    import torch
+    H_q, H_kv, d, P, stride = 4, 2, 64, 16, 1 << 31
+    c = Paged(41, H_q, H_kv, d, P, [9], [30], extra=1)
+    base_k, base_v = (torch.empty(3 * stride + H_kv * P * d, dtype=x, device="cuda") for x in (torch.bfloat16, torch.float16))
+    shape, strides = (4, H_kv, P, d), (stride, P * d, d, 1)
+    c.k_pool, c.v_pool = base_k.as_strided(shape, strides), base_v.as_strided(shape, strides)
+    w_pool = torch.empty(3 * stride + H_kv * P, device="cuda").as_strided((4, H_kv, P), (stride, P, 1))
+    c.table, c.page_ids = [np.array([3, 1, 2], np.int32)], np.array([3, 1, 2], np.int32)
+    for x in (c.k_pool, c.v_pool, w_pool):
+        x.fill_(float("nan"))
+    page, row = (torch.from_numpy(x.astype(np.int64)).cuda() for x in c.place(0, 39))
+    k, v = c.dev(c.k_rows[0]), torch.from_numpy(c.v_rows[0]).cuda()
+    c.k_pool[page[:30], :, row[:30]], c.v_pool[page[:30], :, row[:30]] = k[:30], v[:30]
+    q = c.bf16(9, H_q, d)
+    c.v_rows[0][30:] = c.v_rows[0][30:].astype(np.float32).astype(np.float16)
+    v_new = c.dev(wl.f32_to_bf16_bits(c.v_rows[0][30:].astype(np.float32)))
+    c.v_rows[0][30:] = v_new.float().cpu().numpy().astype(np.float16)
+    q_out = torch.zeros(9, H_q, d, dtype=torch.bfloat16, device="cuda")
+    PG.attn_rope_append(c.shape, PG.make_attn_rope([]), c.dev(q), k[30:].contiguous(), v_new, c.cu, None, c.starts, c.k_pool, c.v_pool, c.page_cu, c.page_ids,
+                        q_out, c.workspace())
+    assert np.array_equal(bits_of(q_out), q) and torch.equal(c.k_pool[page, :, row], k)
+    o, z = run_attend(c, q, None, "f32")
+    check_attend(c, q, None, "f32", o, z)
+    PG.attn_key_weights(c.shape, q_out, z, c.cu, c.starts, c.k_pool, c.page_cu, c.page_ids, 1.0, None, w_pool, c.workspace())
+    w = w_pool[page, :, row].cpu().numpy()
+    assert abs(w.sum() - 9 * H_q) <= 1e-4 * 9 * H_q
+    index = torch.zeros(16 * H_kv, dtype=torch.int32, device="cuda")
+    PG.attn_evict(c.shape, [39], [16], [1], [4], c.k_pool, c.v_pool, w_pool, c.page_cu, c.page_ids, [0, 1], [0], index, c.workspace(0, 4))
+    idx = index.cpu().numpy().reshape(H_kv, 16)
+    for g in range(H_kv):
+        assert list(idx[g]) == po.rows_kept(w[:, g], 16, 1, 4)
+        assert torch.equal(c.k_pool[0, g], k[torch.from_numpy(idx[g].astype(np.int64)).cuda(), g])
+
+
+@pytest.mark.gpu
+def test_calls_on_another_stream_and_again_give_the_same_bits():
+    import torch
+    c = Paged(51, 16, 2, 128, 64, [1, 40, 1], [3000, 800, 5000]).fill()
+    q = c.bf16(c.T, 16, 128)
+    o, z = run_attend(c, q, None, "bf16")
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        o2, z2 = run_attend(c, q, None, "bf16")
+        w = torch.zeros(c.k_np.shape[0], 2, 64, device="cuda")
+        PG.attn_key_weights(c.shape, c.dev(q), z2, c.cu, c.starts, c.k_pool, c.page_cu, c.page_ids, 1.0, None, w, c.workspace())
+    side.synchronize()
+    assert torch.equal(o, o2) and torch.equal(z, z2)
+    w2 = torch.zeros_like(w)
+    PG.attn_key_weights(c.shape, c.dev(q), z, c.cu, c.starts, c.k_pool, c.page_cu, c.page_ids, 1.0, None, w2, c.workspace())
+    assert torch.equal(w, w2)
