@@ -901,4 +901,61 @@ __global__ void __launch_bounds__(ATT_THREADS) attn_combine_kernel(CombineArgs a
     }
 }
 
+// The same for pieces of many parts (a decode row behind a long cache: 256 parts of 2 workgroups' rows, 92 us by the kernel above): one workgroup per
+// row, the parts dealt to its CL_THREADS / (D / 4) groups of threads, the groups' sums joined through LDS.
+constexpr int CL_THREADS = 1024;
+
+template <int D, typename OT, bool LSE>
+__global__ void __launch_bounds__(CL_THREADS) attn_combine_long_kernel(CombineArgs a) {
+    constexpr int CH = D / 4, GROUPS = CL_THREADS / CH, WAVES = CL_THREADS / 64;
+    __shared__ __attribute__((aligned(16))) float sums[GROUPS][D + 4];      // a group's outputs, normaliser, unrounded normaliser
+    __shared__ float top[WAVES];
+    const bool second = (int)blockIdx.x >= a.set[0].blocks;
+    const CombineSet s = second ? a.set[1] : a.set[0];
+    const int block = second ? (int)blockIdx.x - a.set[0].blocks : (int)blockIdx.x;
+    const int ph = block / s.subs, row = block % s.subs;
+    const int R = s.pack, HB = a.H_q / R, TPW = ATT_BQ / R;
+    const int piece = ph / HB, hb = ph % HB;
+    const int r = s.piece_req[piece];
+    const int q0 = s.piece_tile[piece] * TPW;
+    const int tok0 = a.cu[r];
+    if (row >= min(TPW, a.cu[r + 1] - tok0 - q0) * R) return;       // the whole workgroup
+    const int P = s.piece_parts[piece];
+    const int64_t prow0 = s.row0 + ((int64_t)s.piece_base[piece] * HB + hb) * s.slot_rows + row;
+    const int64_t pstep = (int64_t)HB * s.slot_rows;
+    const int tl = row / R, hq = hb * R + (row - tl * R);
+    float M = -INFINITY;
+    for (int p = threadIdx.x; p < P; p += CL_THREADS) M = fmaxf(M, a.part_ml[(prow0 + p * pstep) * 2]);
+    for (int d = 32; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor(M, d));
+    if ((threadIdx.x & 63) == 0) top[threadIdx.x >> 6] = M;
+    __syncthreads();
+    for (int w = 0; w < WAVES; ++w) M = fmaxf(M, top[w]);           // finite: part 0 sees key row 0
+    const int ch = threadIdx.x % CH, group = threadIdx.x / CH;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    float L = 0.f, Le = 0.f;
+#pragma unroll 4
+    for (int p = group; p < P; p += GROUPS) {
+        const int64_t prow = prow0 + p * pstep;
+        const f32x2 ml = *reinterpret_cast<const f32x2*>(a.part_ml + prow * 2);
+        const f32x4 op = *reinterpret_cast<const f32x4*>(a.part_o + prow * D + 4 * ch);
+        const float w = __builtin_amdgcn_exp2f((ml[0] - M) * a.scale_log2e);
+        acc[0] += w * op[0]; acc[1] += w * op[1]; acc[2] += w * op[2]; acc[3] += w * op[3];
+        L += w * ml[1];
+        if constexpr (LSE) Le += w * a.part_le[prow];
+    }
+    *reinterpret_cast<f32x4*>(&sums[group][4 * ch]) = acc;
+    if (ch == 0) { sums[group][D] = L; sums[group][D + 1] = Le; }
+    __syncthreads();
+    if (threadIdx.x >= CH) return;
+    for (int k = 1; k < GROUPS; ++k) {
+        const f32x4 op = *reinterpret_cast<const f32x4*>(&sums[k][4 * ch]);
+        acc[0] += op[0]; acc[1] += op[1]; acc[2] += op[2]; acc[3] += op[3];
+    }
+    L = Le = 0.f;
+    for (int k = 0; k < GROUPS; ++k) { L += sums[k][D]; Le += sums[k][D + 1]; }
+    if (LSE && ch == 0) a.lse[(int64_t)(tok0 + q0 + tl) * a.H_q + hq] = row_lse(M, Le, a.scale_log2e);
+    const float inv = 1.f / L;
+    store_out<OT>(a.o, a.gate, ((int64_t)(tok0 + q0 + tl) * a.H_q + hq) * D + 4 * ch, f32x4{acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv});
+}
+
 }  // namespace attn

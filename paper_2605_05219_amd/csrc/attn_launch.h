@@ -90,15 +90,25 @@ hipError_t launch_narrow_d(int d, bool nt, const Args& a, unsigned blocks, hipSt
     }
 }
 
-template <typename OT, bool LSE>
-hipError_t launch_combine_d(int d, const CombineArgs& a, hipStream_t stream) {
-    const dim3 grid((unsigned)(a.set[0].blocks + a.set[1].blocks)), block(ATT_THREADS);
-    switch (d) {
-        case 64: hipLaunchKernelGGL((attn_combine_kernel<64, OT, LSE>), grid, block, 0, stream, a); break;
-        case 128: hipLaunchKernelGGL((attn_combine_kernel<128, OT, LSE>), grid, block, 0, stream, a); break;
-        default: hipLaunchKernelGGL((attn_combine_kernel<256, OT, LSE>), grid, block, 0, stream, a); break;
-    }
+template <int D, typename OT, bool LSE, bool LONG>
+hipError_t launch_combine(bool by_row, const CombineArgs& a, hipStream_t stream) {
+    const dim3 grid((unsigned)(a.set[0].blocks + a.set[1].blocks));
+    if constexpr (LONG)
+        if (by_row) {
+            hipLaunchKernelGGL((attn_combine_long_kernel<D, OT, LSE>), grid, dim3(CL_THREADS), 0, stream, a);
+            return hipGetLastError();
+        }
+    hipLaunchKernelGGL((attn_combine_kernel<D, OT, LSE>), grid, dim3(ATT_THREADS), 0, stream, a);
     return hipGetLastError();
+}
+
+template <typename OT, bool LSE, bool LONG>
+hipError_t launch_combine_d(int d, bool by_row, const CombineArgs& a, hipStream_t stream) {
+    switch (d) {
+        case 64: return launch_combine<64, OT, LSE, LONG>(by_row, a, stream);
+        case 128: return launch_combine<128, OT, LSE, LONG>(by_row, a, stream);
+        default: return launch_combine<256, OT, LSE, LONG>(by_row, a, stream);
+    }
 }
 
 // The work of one attention call (host, integer): how the rows of a workgroup are made up, the pieces
@@ -426,10 +436,11 @@ int32_t launch_wide_units(const attn_shape* s, const UnitPlan& plan, const CallI
                                          : launch_attn_d<uint16_t, LSE>(s->d, im.NH, a, (unsigned)im.blocks, stream));
 }
 
-// The merge pass over the split pieces, if there are any.
-template <bool LSE>
+// The merge pass over the split pieces, if there are any.  LONG: calls with pieces of more than LONG_PARTS parts are merged a row to a workgroup.
+constexpr int LONG_PARTS = 16;
+template <bool LSE, bool LONG>
 int32_t launch_merge(const attn_shape* s, const UnitPlan& plan, const CallImage& im, const int32_t* d, const AttnArgs& a, float* lse,
-                            const float* part_le, hipStream_t stream) {
+                     const float* part_le, hipStream_t stream) {
     CombineArgs ca;
     ca.part_o = a.part_o;
     ca.part_ml = a.part_ml;
@@ -438,6 +449,10 @@ int32_t launch_merge(const attn_shape* s, const UnitPlan& plan, const CallImage&
     ca.cu = a.cu;
     ca.lse = lse;
     ca.part_le = part_le;
+    bool by_row = false;
+    if (LONG)
+        for (int k = 0; k < 2; ++k)
+            for (const Piece& p : plan.split[k]) by_row |= p.parts > LONG_PARTS;
     for (int k = 0; k < 2; ++k) {
         CombineSet& c = ca.set[k];
         const int64_t n = (int64_t)plan.split[k].size();
@@ -448,13 +463,14 @@ int32_t launch_merge(const attn_shape* s, const UnitPlan& plan, const CallImage&
         c.row0 = k ? a.few_row0 : 0;
         c.slot_rows = k ? NAR_ROWS : ATT_BQ;
         c.pack = k && plan.apart ? s->H_q / s->H_kv : plan.pack;
-        c.subs = (std::min(plan.longest[k], ATT_BQ / c.pack) * c.pack * (s->d / 4) + ATT_THREADS - 1) / ATT_THREADS;
+        const int rows = std::min(plan.longest[k], ATT_BQ / c.pack) * c.pack;    // of the fullest piece
+        c.subs = by_row ? rows : (rows * (s->d / 4) + ATT_THREADS - 1) / ATT_THREADS;
         c.blocks = (int32_t)(n * (s->H_q / c.pack) * c.subs);
     }
     if (ca.set[0].blocks + ca.set[1].blocks == 0) return GDN_OK;
     ca.H_q = s->H_q;
     ca.scale_log2e = a.scale_log2e;
-    return hip_err(s->o_dtype == GDN_F32 ? launch_combine_d<float, LSE>(s->d, ca, stream) : launch_combine_d<uint16_t, LSE>(s->d, ca, stream));
+    return hip_err(s->o_dtype == GDN_F32 ? launch_combine_d<float, LSE, LONG>(s->d, by_row, ca, stream) : launch_combine_d<uint16_t, LSE, LONG>(s->d, by_row, ca, stream));
 }
 
 }  // namespace attn

@@ -196,7 +196,7 @@ int32_t launch_paged(const attn_shape* s, const UnitPlan& plan, const CallImage&
     int32_t rc;
     if (im.n_narrow > 0 && (rc = launch_narrow_units<LSE>(s, nt, im, a, stream)) != GDN_OK) return rc;
     if (im.n_wide > 0 && (rc = launch_wide_units<LSE>(s, plan, im, a, stream)) != GDN_OK) return rc;
-    return launch_merge<LSE>(s, plan, im, d, a, a.lse, a.part_le, stream);
+    return launch_merge<LSE, true>(s, plan, im, d, a, a.lse, a.part_le, stream);
 }
 
 int32_t paged_prefill(const attn_shape* s, const void* q, const void* gate, int32_t n_req, const int32_t* cu, const int32_t* start,
