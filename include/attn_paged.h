@@ -33,7 +33,7 @@ extern "C" {
 typedef struct attn_pages {
     int64_t page_stride;  /* elements from one page to the next: a multiple of 8, at least H_kv * page_rows * d */
     int32_t n_pages;
-    int32_t page_rows;    /* rows per page: a power of two, 16 .. 4096 (and H_kv * page_rows * d * 2 < 2^31) */
+    int32_t page_rows;    /* rows per page: a power of two, 16 .. 256 (and H_kv * page_rows * d * 2 < 2^31) */
 } attn_pages;
 
 /* Rotary positions: the first `rot` elements of a head turn in pairs, the others stay as they are. */

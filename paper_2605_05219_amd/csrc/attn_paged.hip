@@ -20,7 +20,7 @@ constexpr int64_t MAX_ROWS = INT32_MAX - 8192;
 int32_t check_pages(const attn_shape* s, const attn_pages* p) {
     if (!p) return GDN_ERR_NULL;
     if (p->n_pages < 0) return GDN_ERR_COUNT;
-    if (p->page_rows < 16 || p->page_rows > 4096 || (p->page_rows & (p->page_rows - 1)) != 0) return GDN_ERR_SHAPE;
+    if (p->page_rows < 16 || p->page_rows > 256 || (p->page_rows & (p->page_rows - 1)) != 0) return GDN_ERR_SHAPE;
     if (p->page_stride < 0 || p->page_stride % 8 != 0) return GDN_ERR_ALIGN;
     const int64_t elems = (int64_t)s->H_kv * p->page_rows * s->d;
     if (elems * 2 > INT32_MAX || p->page_stride < elems) return GDN_ERR_SHAPE;
@@ -77,11 +77,14 @@ class PageSet {
 // attn_key_weights leaves its parts there instead.
 inline int64_t part_le_bytes() { return (int64_t)SPLIT_MAX_WGS * ATT_BQ * sizeof(float); }
 inline int64_t parts_bytes(int d) {
-    return std::max<int64_t>(part_ml_bytes() + part_o_bytes(d) + part_le_bytes(), (int64_t)WGT_PARTS * WGT_KEYS * sizeof(float));
+    return std::max<int64_t>(part_ml_bytes() + part_o_bytes(d) + part_le_bytes(), (int64_t)WGT_PARTS * wgt_keys(d) * sizeof(float));
 }
-// ints of an image: the attention's are the most (plan_ints) but for calls of very few tokens and many requests
+// ints of an image: the page ids, and the attention's plan, or the units of attn_key_weights (at most two tiles of keys to a page of 256 rows, and the
+// cut ones), or the arrays of one entry per request of the others
 inline int64_t image_bytes(const attn_shape* s, int32_t n_req, int64_t T, int64_t n_ids) {
-    const int64_t ints = std::max<int64_t>(plan_ints(n_req, T, s->H_q / s->H_kv), 8 * ((int64_t)n_req + 1)) + n_ids;
+    const int64_t attend = plan_ints(n_req, T, s->H_q / s->H_kv);
+    const int64_t weights = WGT_REC * (2 * n_ids + n_req + WGT_PARTS) + WGT_MERGE * ((int64_t)WGT_PARTS + 1);
+    const int64_t ints = std::max<int64_t>(std::max(attend, weights), 8 * ((int64_t)n_req + 1)) + n_ids;
     return (ints * (int64_t)sizeof(int32_t) + 255) / 256 * 256;
 }
 
@@ -243,8 +246,127 @@ int32_t paged_prefill(const attn_shape* s, const void* q, const void* gate, int3
 }
 
 template <int D>
-void launch_weights(const WeightArgs& a, unsigned blocks, hipStream_t stream) {
-    hipLaunchKernelGGL((attn_weights_kernel<D>), dim3(blocks), dim3(WGT_THREADS), 0, stream, a);
+void launch_weights_d(bool few, const WeightArgs& a, unsigned blocks, hipStream_t stream) {
+    if (few) hipLaunchKernelGGL((attn_weights_few_kernel<D>), dim3(blocks), dim3(WGT_THREADS), 0, stream, a);
+    else hipLaunchKernelGGL((attn_weights_kernel<D>), dim3(blocks), dim3(WGT_THREADS), 0, stream, a);
+}
+void launch_weights(int d, bool few, const WeightArgs& a, unsigned blocks, hipStream_t stream) {
+    switch (d) {
+        case 64: launch_weights_d<64>(few, a, blocks, stream); break;
+        case 128: launch_weights_d<128>(few, a, blocks, stream); break;
+        default: launch_weights_d<256>(few, a, blocks, stream); break;
+    }
+}
+
+// The work of one attn_key_weights call: units (a tile of keys and a run of the request's query rows) of either kernel, and the tiles whose rows are cut.
+struct WeightPlan {
+    std::vector<int32_t> wide, few, merge;       // WGT_REC, WGT_REC, WGT_MERGE ints each
+};
+
+// The rows of a tile are cut on a grid of `run` row tiles of 64, so that the chip is full and its last round short: a workgroup takes as long as its row
+// tiles and about WGT_START more for its keys, and WGT_SLOTS of them run at once (two to a compute unit).
+constexpr int WGT_SLOTS = 512, WGT_START = 2;
+
+void plan_weights(const attn_shape* s, int32_t n_req, const int32_t* cu, const int32_t* start, const int32_t* len, const int32_t* place, WeightPlan& out) {
+    const int G = s->H_q / s->H_kv, keys = wgt_keys(s->d);
+    auto is_few = [&](int32_t r) { return len[r] > 0 && (int64_t)len[r] * G <= WGT_FEW; };
+    auto tiles_of = [&](int32_t r) { return (int32_t)(((int64_t)start[r] + len[r] + keys - 1) / keys); };
+    auto row_tiles = [&](int32_t r) { return (int32_t)(((int64_t)len[r] * G + WGT_ROWS - 1) / WGT_ROWS); };
+    auto first_seen = [&](int32_t r, int32_t tile) {       // the first row tile that sees a key of the tile
+        return (int32_t)(std::max<int64_t>(0, (int64_t)tile * keys - start[r]) * G / WGT_ROWS);
+    };
+    // ---- units and row tiles in all if rows are cut every `run` row tiles
+    int64_t work = 0, most = 0;
+    auto units_of = [&](int64_t run, int64_t& cut) {
+        int64_t units = 0;
+        cut = work = 0;
+        for (int32_t r = 0; r < n_req; ++r) {
+            if (is_few(r)) continue;
+            const int64_t m = row_tiles(r);
+            most = std::max(most, m);
+            const int64_t whole = std::min<int64_t>(tiles_of(r), start[r] / keys + 1), parts = std::max<int64_t>(1, (m + run - 1) / run);   // tiles that every row sees a key of
+            units += whole * parts;
+            work += whole * m;
+            if (parts > 1) cut += whole * parts;
+            for (int32_t t = (int32_t)whole; t < tiles_of(r); ++t) {
+                const int64_t f = first_seen(r, t), p = (m - 1) / run - f / run + 1;
+                units += p;
+                work += m - f;
+                if (p > 1) cut += p;
+            }
+        }
+        return units;
+    };
+    int64_t cut = 0, units = units_of(INT32_MAX, cut), run = std::max<int64_t>(most, 1);
+    if (most > 1) {
+        auto cost = [&](int64_t c, int64_t n) {            // half way between whole rounds of equal units and units that fill every gap
+            const double per = (double)(n * s->H_kv) / WGT_SLOTS;
+            const double even = ((double)work * s->H_kv + (double)WGT_START * n * s->H_kv) / WGT_SLOTS + 0.5 * (c + WGT_START);
+            return 0.5 * (std::ceil(per) * (c + WGT_START) + std::max(even, (double)(c + WGT_START)));
+        };
+        double best = cost(most, units);
+        for (int64_t c = most; c > 1;) {
+            c = c > 8 ? c * 3 / 4 : c - 1;
+            const int64_t n = units_of(c, cut);
+            if (cut * s->H_kv > WGT_PARTS) break;
+            if (cost(c, n) < 0.97 * best) {
+                best = cost(c, n);
+                run = c;
+                units = n;
+            }
+        }
+    }
+    // ---- the units, those of the same rows together (they read the same queries), the longest first
+    struct Unit { int32_t r, kv0, lo, hi, part; };
+    std::vector<Unit> list;
+    list.reserve((size_t)units);
+    std::vector<int32_t> base;
+    int32_t slot = 0;
+    for (int32_t r = 0; r < n_req; ++r) {
+        const int32_t tiles = tiles_of(r);
+        if (is_few(r)) {
+            for (int32_t t = 0; t < tiles; ++t)
+                out.few.insert(out.few.end(), {cu[r], len[r], start[r], place[r], t * keys, 0, len[r] * G, -1});
+            continue;
+        }
+        const int32_t m = row_tiles(r), rows = len[r] * G;
+        if (m == 0) {
+            for (int32_t t = 0; t < tiles; ++t) list.push_back({r, t * keys, 0, 0, -1});
+            continue;
+        }
+        base.resize(tiles);
+        const int32_t runs = (int32_t)((m + run - 1) / run);
+        for (int32_t t = 0; t < tiles; ++t) {
+            const int32_t parts = runs - (int32_t)(first_seen(r, t) / run);
+            base[t] = parts > 1 ? slot - (int32_t)(first_seen(r, t) / run) : -1;     // + the run's number: its partial sum
+            if (parts <= 1) continue;
+            out.merge.insert(out.merge.end(), {start[r] + len[r], start[r], place[r], t * keys, slot});
+            slot += parts;
+        }
+        for (int32_t c = runs - 1; c >= 0; --c) {
+            const int32_t lo = (int32_t)(c * run), hi = (int32_t)std::min<int64_t>((c + 1) * run, m);
+            for (int32_t t = 0; t < tiles; ++t) {
+                const int32_t f = std::max(lo, first_seen(r, t));
+                if (f >= hi) break;
+                const bool whole = runs - (int32_t)(first_seen(r, t) / run) <= 1;
+                list.push_back({r, t * keys, f * WGT_ROWS, std::min(hi * WGT_ROWS, rows), whole ? -1 : base[t] + c});
+            }
+        }
+    }
+    if (!out.merge.empty()) out.merge.insert(out.merge.end(), {0, 0, 0, 0, slot});
+    // by length, in classes: a counting sort that keeps their order
+    constexpr int CLASSES = 64;
+    const int64_t top = std::max<int64_t>(1, std::min<int64_t>(run, most)) * WGT_ROWS;
+    std::vector<int32_t> at(CLASSES + 1, 0);
+    auto class_of = [&](const Unit& u) { return (int)(CLASSES - 1 - (int64_t)(u.hi - u.lo) * (CLASSES - 1) / top); };
+    for (const Unit& u : list) ++at[class_of(u) + 1];
+    for (int i = 0; i < CLASSES; ++i) at[i + 1] += at[i];
+    out.wide.resize(list.size() * WGT_REC);
+    for (const Unit& u : list) {
+        int32_t* const rec = out.wide.data() + (size_t)at[class_of(u)]++ * WGT_REC;
+        const int32_t x[WGT_REC] = {cu[u.r], len[u.r], start[u.r], place[u.r], u.kv0, u.lo, u.hi, u.part};
+        std::copy(x, x + WGT_REC, rec);
+    }
 }
 
 int32_t key_weights(const attn_shape* s, const void* q, const float* lse, int32_t n_req, const int32_t* cu, const int32_t* start,
@@ -275,46 +397,21 @@ int32_t key_weights(const attn_shape* s, const void* q, const float* lse, int32_
     rc = check_workspace(s, n_req, T, n_ids, workspace, workspace_bytes);
     if (rc != GDN_OK) return rc;
 
-    // ---- key tiles, and the cut of their query rows into parts where there are too few tiles for the chip
     const int G = s->H_q / s->H_kv;
-    int64_t tiles = 0, longest = 0;
-    for (int32_t r = 0; r < n_req; ++r) {
-        tiles += ((int64_t)start[r] + len[r] + WGT_KEYS - 1) / WGT_KEYS;
-        longest = std::max<int64_t>(longest, (int64_t)len[r] * G);
-    }
-    if (longest > INT32_MAX - 2 * WGT_ROWS || ((int64_t)s->H_q * 32 + G) * s->d * 2 > INT32_MAX) return GDN_ERR_SHAPE;
-    int64_t part_rows = (longest + WGT_ROWS - 1) / WGT_ROWS * WGT_ROWS;
-    auto pairs_of = [&](int64_t pr) {
-        int64_t n = 0;
-        for (int32_t r = 0; r < n_req; ++r)
-            n += ((int64_t)start[r] + len[r] + WGT_KEYS - 1) / WGT_KEYS * std::max<int64_t>(1, ((int64_t)len[r] * G + pr - 1) / pr);
-        return n;
-    };
-    constexpr int64_t WANT = 1024, MIN_ROWS = 256;
-    if (tiles * s->H_kv < WANT && part_rows > MIN_ROWS) {
-        part_rows = MIN_ROWS;
-        while (pairs_of(part_rows) * s->H_kv > WGT_PARTS) part_rows *= 2;
-    }
-    part_rows = std::max<int64_t>(part_rows, WGT_ROWS);
-    const int64_t pairs = pairs_of(part_rows);
-    if (pairs * s->H_kv > INT32_MAX) return GDN_ERR_COUNT;
-    std::vector<int32_t> img((size_t)(5 * (int64_t)n_req + 3 + n_ids));
-    int32_t* const p_start = img.data() + n_req + 1;
-    int32_t* const p_place = p_start + n_req;
-    int32_t* const p_block = p_place + n_req;
-    int32_t* const p_cut = p_block + n_req + 1;
-    std::copy(cu, cu + n_req + 1, img.data());
-    std::copy(start, start + n_req, p_start);
-    std::copy(page_cu, page_cu + n_req, p_place);
-    std::copy(page_ids, page_ids + n_ids, p_cut + n_req + 1);
-    p_block[0] = p_cut[0] = 0;
-    for (int32_t r = 0; r < n_req; ++r) {
-        const int32_t t = (int32_t)(((int64_t)start[r] + len[r] + WGT_KEYS - 1) / WGT_KEYS);
-        const int32_t parts = (int32_t)std::max<int64_t>(1, ((int64_t)len[r] * G + part_rows - 1) / part_rows);
-        p_block[r + 1] = p_block[r] + t * parts;
-        p_cut[r + 1] = p_cut[r] + (parts > 1 ? t : 0);
-    }
-    const int32_t cut_tiles = p_cut[n_req];
+    for (int32_t r = 0; r < n_req; ++r)
+        if (((int64_t)len[r] + 512) * G > INT32_MAX) return GDN_ERR_SHAPE;
+    if (((int64_t)s->H_q * (WGT_ROWS + 1) + G) * s->d * 2 > INT32_MAX) return GDN_ERR_SHAPE;
+    WeightPlan plan;
+    plan_weights(s, n_req, cu, start, len.data(), page_cu, plan);
+    const int64_t n_wide = (int64_t)plan.wide.size() / WGT_REC, n_few = (int64_t)plan.few.size() / WGT_REC;
+    const int64_t n_cut = plan.merge.empty() ? 0 : (int64_t)plan.merge.size() / WGT_MERGE - 1;
+    if (std::max(n_wide, n_few) * s->H_kv > INT32_MAX) return GDN_ERR_COUNT;
+    std::vector<int32_t> img(plan.wide.size() + plan.few.size() + plan.merge.size() + (size_t)n_ids);
+    const int64_t few_at = (int64_t)plan.wide.size(), merge_at = few_at + (int64_t)plan.few.size(), ids_at = merge_at + (int64_t)plan.merge.size();
+    std::copy(plan.wide.begin(), plan.wide.end(), img.begin());
+    std::copy(plan.few.begin(), plan.few.end(), img.begin() + few_at);
+    std::copy(plan.merge.begin(), plan.merge.end(), img.begin() + merge_at);
+    std::copy(page_ids, page_ids + n_ids, img.begin() + ids_at);
     rc = gdn::upload_plan(img.data(), img.size() * sizeof(int32_t), workspace, stream);
     if (rc != GDN_OK) return rc;
     const int32_t* const d = static_cast<const int32_t*>(workspace);
@@ -324,29 +421,32 @@ int32_t key_weights(const attn_shape* s, const void* q, const float* lse, int32_
     a.k_pool = static_cast<const uint16_t*>(k_pool);
     a.w_in = w_in;
     a.w_out = w_out;
-    a.cu = d;
-    a.start = d + n_req + 1;
-    a.place = a.start + n_req;
-    a.block_cu = a.place + n_req;
-    a.page_ids = a.block_cu + 2 * ((int64_t)n_req + 1);
+    a.page_ids = d + ids_at;
+    a.merge_rec = d + merge_at;
     a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + image_bytes(s, n_req, T, n_ids));
     a.page_stride = pages->page_stride;
     a.w_stride = w_stride;
-    a.n_req = n_req;
     a.H_q = s->H_q; a.H_kv = s->H_kv; a.G = G;
     a.page_shift = shift;
-    a.part_rows = (int32_t)part_rows;
+    a.inv_G = 1.f / (float)G;
     a.scale_log2e = s->scale * 1.4426950408889634f;
     a.decay = decay;
-    const unsigned blocks = (unsigned)(pairs * s->H_kv);
-    switch (s->d) {
-        case 64: launch_weights<64>(a, blocks, stream); break;
-        case 128: launch_weights<128>(a, blocks, stream); break;
-        default: launch_weights<256>(a, blocks, stream); break;
+    if (n_few > 0) {
+        a.unit_rec = d + few_at;
+        launch_weights(s->d, true, a, (unsigned)(n_few * s->H_kv), stream);
+        rc = hip_err(hipGetLastError());
+        if (rc != GDN_OK) return rc;
     }
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || cut_tiles == 0) return hip_err(e);
-    hipLaunchKernelGGL(attn_weights_merge_kernel, dim3((unsigned)(cut_tiles * s->H_kv)), dim3(WGT_KEYS), 0, stream, a, a.block_cu + n_req + 1);
+    if (n_wide > 0) {
+        a.unit_rec = d;
+        launch_weights(s->d, false, a, (unsigned)(n_wide * s->H_kv), stream);
+        rc = hip_err(hipGetLastError());
+        if (rc != GDN_OK) return rc;
+    }
+    if (n_cut == 0) return GDN_OK;
+    const dim3 grid((unsigned)(n_cut * s->H_kv)), block((unsigned)wgt_keys(s->d));
+    if (s->d == 256) hipLaunchKernelGGL((attn_weights_merge_kernel<wgt_keys(256)>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((attn_weights_merge_kernel<wgt_keys(128)>), grid, block, 0, stream, a);
     return hip_err(hipGetLastError());
 }
 

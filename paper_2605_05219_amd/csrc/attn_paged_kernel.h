@@ -149,14 +149,19 @@ __global__ void __launch_bounds__(ROPE_THREADS) attn_rope_kernel(RopeArgs a) {
 }
 
 // ---------------------------------------------------------------- the weight that cached rows gather
-// A key's sum runs over query rows, so keys stay and queries pass: each of the four waves of a workgroup holds 64 keys in registers as
-// matrix operands, tiles of 32 query rows (tokens x heads of the group, row = token * G + head) go through two LDS stages, brought by loads to LDS a
-// tile ahead.  S[row][key] puts a key into a lane's column and 16 of the rows into its registers: the sum over rows needs no
+// A key's sum runs over query rows, so keys stay and queries pass: each of the four waves of a workgroup holds 64 keys (32 at d = 256) in registers as
+// matrix operands, tiles of 64 query rows (tokens x heads of the group, row = token * G + head) go through two LDS stages, brought by loads to LDS a
+// tile ahead.  S[row][key] puts a key into a lane's column and 16 of 32 rows into its registers: the sum over rows needs no
 // exchange between lanes but one with the other half at the end, and no atomics.  A row's log-sum-exp comes by LDS in units of log2.
+// Bound: matrix and vector units alike (8192 tokens of 16 heads, d = 128: 55 us of products and 55 us of multiply-adds, exponentials and
+// sums at 2.4 GHz), so a wave computes the products of the next 32 rows in between the exponentials of the last.
 constexpr int WGT_THREADS = 256;
-constexpr int WGT_KEYS = 256;         // keys per workgroup
-constexpr int WGT_ROWS = 32;          // query rows per tile
-constexpr int WGT_PARTS = 2048;       // (tile, part, head) triples of calls that cut the rows of a tile into parts, at most
+__host__ __device__ constexpr int wgt_keys(int d) { return d == 256 ? 128 : 256; }   // keys per workgroup
+constexpr int WGT_ROWS = 64;          // query rows per tile
+constexpr int WGT_PARTS = 16384;      // partial sums (of a tile of keys, a part of its rows, a head) of a call, at most
+constexpr int WGT_FEW = 16;           // rows of a request of the few-rows kernel, at most
+constexpr int WGT_REC = 8;            // a unit's record: first token, tokens, start, place, first key, first row, one past the last, partial sum or -1
+constexpr int WGT_MERGE = 5;          // a cut tile's record: tokens + start, start, place, first key, first partial sum; one past the last is the next one's
 
 struct WeightArgs {
     const uint16_t* q;
@@ -164,13 +169,14 @@ struct WeightArgs {
     const uint16_t* k_pool;
     const float* w_in;        // or nullptr
     float* w_out;
-    const int32_t *cu, *start, *place, *page_ids;
-    const int32_t* block_cu;  // n_req + 1: (key tile, part) pairs before each request
-    float* part;              // [pair][head][WGT_KEYS], where a request's rows are cut
+    const int32_t* page_ids;
+    const int32_t* unit_rec;  // WGT_REC ints per unit
+    const int32_t* merge_rec; // WGT_MERGE ints per tile whose rows are cut, and the first partial sum behind the last one
+    float* part;              // [partial sum][head][keys of a tile]
     int64_t page_stride, w_stride;
-    int32_t n_req, H_q, H_kv, G;
+    int32_t H_q, H_kv, G;
     int32_t page_shift;
-    int32_t part_rows;        // query rows per part, a multiple of WGT_ROWS
+    float inv_G;              // 1 / G: x / G = (int)((x + 1/2) inv_G) for the small x that it is used for
     float scale_log2e, decay;
 };
 
@@ -187,31 +193,26 @@ __device__ __forceinline__ void store_weight(const WeightArgs& a, int place, int
 }
 
 template <int D>
-__global__ void __launch_bounds__(WGT_THREADS) attn_weights_kernel(WeightArgs a) {
+__global__ void __launch_bounds__(WGT_THREADS, 2) attn_weights_kernel(WeightArgs a) {
     typedef WeightSmem<D> SM;
-    constexpr int KB = D / 16;
+    constexpr int KB = D / 16, KEYS = wgt_keys(D), NB = KEYS / 128;      // NB: blocks of 32 keys per wave
     __shared__ __attribute__((aligned(1024))) char stage0[SM::TILE_BYTES], stage1[SM::TILE_BYTES];
-    __shared__ __attribute__((aligned(16))) float neg_lse[2][WGT_ROWS];   // -lse log2(e); rows past the end -inf
-    __shared__ __attribute__((aligned(16))) int limit[2][WGT_ROWS];       // last key a row sees
+    __shared__ __attribute__((aligned(16))) float neg_lse[4][WGT_ROWS];   // -lse log2(e); rows past the end -inf
+    __shared__ __attribute__((aligned(16))) int limit[4][WGT_ROWS];       // last key a row sees
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, g = lane >> 5;
-    const int kvh = (int)blockIdx.x % a.H_kv, pair = (int)blockIdx.x / a.H_kv;
-    const int r = request_of(a.block_cu, a.n_req, pair);
-    const int tok0 = a.cu[r], n = a.cu[r + 1] - tok0, c0 = a.start[r], place = a.place[r];
-    const int kv_len = c0 + n, rows = n * a.G;
-    const int parts = max(1, (rows + a.part_rows - 1) / a.part_rows);
-    const int in_req = pair - a.block_cu[r];
-    const int kv0 = in_req / parts * WGT_KEYS, part = in_req % parts;
-    const int seen_from = max(0, kv0 - c0) * a.G / WGT_ROWS * WGT_ROWS;   // the first rows that see a key of this tile
-    const int row_lo = max(part * a.part_rows, seen_from), row_hi = min((part + 1) * a.part_rows, rows);
+    const int kvh = (int)blockIdx.x % a.H_kv;
+    const int32_t* const rec = a.unit_rec + (int64_t)((int)blockIdx.x / a.H_kv) * WGT_REC;
+    const int tok0 = rec[0], n = rec[1], c0 = rec[2], place = rec[3], kv0 = rec[4], row_lo = rec[5], row_hi = rec[6], part = rec[7];
+    const int kv_len = c0 + n;
 
     // ---- this wave's keys: operand B, column = key, d = 16 kb + 8 g + {0..7}
-    const int key0 = kv0 + 64 * wave;
-    bf16x8 kf[2][KB];
+    const int key0 = kv0 + 32 * NB * wave;
+    bf16x8 kf[NB][KB];
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < NB; ++b) {
         const int key = min(key0 + 32 * b + col, kv_len - 1);
         const uint16_t* const kp = a.k_pool + (int64_t)a.page_ids[place + (key >> a.page_shift)] * a.page_stride + ((int64_t)kvh * D << a.page_shift) +
                                    (int64_t)(key & ((1 << a.page_shift) - 1)) * D + 8 * g;
@@ -219,86 +220,246 @@ __global__ void __launch_bounds__(WGT_THREADS) attn_weights_kernel(WeightArgs a)
         for (int kb = 0; kb < KB; ++kb) kf[b][kb] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(kp + 16 * kb));
     }
 
-    // ---- a tile of query rows from `row`: to LDS, 16-byte chunk c of a row at c ^ f(row)
-    auto issue = [&](int row, char* sb) {
-        const int t_lo = min(row, rows - 1) / a.G, t_hi = min(row + WGT_ROWS - 1, rows - 1) / a.G;
-        const uint16_t* const base = a.q + ((int64_t)(tok0 + t_lo) * a.H_q + kvh * a.G) * D;
-        const int bytes = ((t_hi - t_lo) * a.H_q + a.G) * D * 2;
+    // ---- the next tile to bring: its first row, that row's token and head (uniform; a tile is step_t tokens and step_h heads on)
+    const int step_t = WGT_ROWS / a.G, step_h = WGT_ROWS - step_t * a.G;
+    int row_n = row_lo, t_n = row_lo / a.G, h_n = row_lo - t_n * a.G;
+    const int64_t tok_bytes = (int64_t)a.H_q * D * 2;
+    float lse_n = 0.f;           // of row row_n + thread (the first 64 threads)
+    int lim_n = 0;
+    // to LDS, 16-byte chunk c of a row at c ^ f(row); rows past the request's last one come as zeros
+    auto issue = [&](char* sb) {
+        const uint16_t* const base = a.q + ((int64_t)(tok0 + t_n) * a.H_q + kvh * a.G) * D;
+        const int bytes = (int)min((int64_t)INT32_MAX, (int64_t)(n - 1 - t_n) * tok_bytes + a.G * D * 2);
 #pragma unroll
         for (int i = 0; i < SM::PPW; ++i) {
             const int s = (wave * SM::PPW + i) * 64 + lane, rr = s / SM::CPR, pos = s % SM::CPR;
-            const int rho = min(row + rr, rows - 1), t = rho / a.G;
-            load_to_lds(base, bytes, sb + (wave * SM::PPW + i) * 1024, ((t - t_lo) * a.H_q + rho - t * a.G) * D * 2 + ((pos ^ SM::f(rr)) << 4), 0);
+            const int x = h_n + rr, t = (int)(((float)x + 0.5f) * a.inv_G);
+            load_to_lds(base, bytes, sb + (wave * SM::PPW + i) * 1024, (t * a.H_q + x - t * a.G) * D * 2 + ((pos ^ SM::f(rr)) << 4), 0);
+        }
+        if (threadIdx.x < WGT_ROWS) {
+            const int x = h_n + (int)threadIdx.x, t = (int)(((float)x + 0.5f) * a.inv_G);
+            lim_n = c0 + t_n + t;
+            if (row_n + (int)threadIdx.x < row_hi) lse_n = a.lse[(int64_t)(tok0 + t_n + t) * a.H_q + kvh * a.G + x - t * a.G];
+            else lse_n = INFINITY;
         }
     };
-    auto stage_rows = [&](int row, int st) {             // by 32 threads
-        const int rho = min(row + (int)threadIdx.x, rows - 1), t = rho / a.G;
-        const float x = a.lse[(int64_t)(tok0 + t) * a.H_q + kvh * a.G + rho - t * a.G];
-        neg_lse[st][threadIdx.x] = row + (int)threadIdx.x < row_hi ? -x * 1.4426950408889634f : -INFINITY;
-        limit[st][threadIdx.x] = c0 + t;
+    auto stage_rows = [&](int st) {             // what issue() fetched of the rows' sums goes to LDS
+        if (threadIdx.x < WGT_ROWS) {
+            neg_lse[st][threadIdx.x] = -lse_n * 1.4426950408889634f;
+            limit[st][threadIdx.x] = lim_n;
+        }
+        row_n += WGT_ROWS;
+        t_n += step_t;
+        h_n += step_h;
+        if (h_n >= a.G) { h_n -= a.G; ++t_n; }
     };
-    float acc[2] = {0.f, 0.f};
-    auto tile = [&](int row, int st, const char* sb, char* other) {
-        wait_vmcnt<0>();
-        __syncthreads();
-        if (row + WGT_ROWS < row_hi) issue(row + WGT_ROWS, other);
-        f32x16 S[2];
+    float acc[NB];
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+    for (int b = 0; b < NB; ++b) acc[b] = 0.f;
+    // the logits of 32 rows of a stage
+    auto products = [&](f32x16 (&S)[NB], const char* sb, int sub) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) S[b][i] = 0.f;
+        const char* const qrow = sb + (32 * sub + col) * SM::ROW_BYTES;
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
-            const bf16x8 qf = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(sb + col * SM::ROW_BYTES + (((2 * kb + g) ^ SM::f(col)) << 4)));
+            const bf16x8 qf = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qrow + (((2 * kb + g) ^ SM::f(col)) << 4)));
 #pragma unroll
-            for (int b = 0; b < 2; ++b) S[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, kf[b][kb], S[b], 0, 0, 0);
+            for (int b = 0; b < NB; ++b) S[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, kf[b][kb], S[b], 0, 0, 0);
         }
-        const bool cut = c0 + row / a.G < key0 + 63;      // some row does not see some key of this wave
+    };
+    // their weights, summed; CUT: some row does not see some key of this wave
+    auto sums = [&](const f32x16 (&S)[NB], int st, int sub, auto cut) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const f32x4 nl = *reinterpret_cast<const f32x4*>(&neg_lse[st][8 * q + 4 * g]);
+            const f32x4 nl = *reinterpret_cast<const f32x4*>(&neg_lse[st][32 * sub + 8 * q + 4 * g]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int lim = cut ? limit[st][8 * q + 4 * g + e] : INT32_MAX;
+            for (int b = 0; b < NB; ++b) {
+                float p[4];
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(S[b][4 * q + e], a.scale_log2e, nl[e]));
-                    acc[b] += key0 + 32 * b + col <= lim ? p : 0.f;
+                for (int e = 0; e < 4; ++e) {
+                    p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[b][4 * q + e], a.scale_log2e, nl[e]));
+                    if constexpr (decltype(cut)::value)
+                        if (key0 + 32 * b + col > limit[st][32 * sub + 8 * q + 4 * g + e]) p[e] = 0.f;
                 }
+                acc[b] += (p[0] + p[1]) + (p[2] + p[3]);
             }
         }
-        if (row + WGT_ROWS < row_hi && threadIdx.x < WGT_ROWS) stage_rows(row + WGT_ROWS, st ^ 1);
     };
+    // both, of different rows, in turn: the products of a step of the contraction, then the vector work of four weights or more, which the
+    // products in flight cover; nothing moves from step to step
+    auto both = [&](f32x16 (&Sn)[NB], const char* sb, int sub_n, const f32x16 (&Sp)[NB], int st, int sub_p) {
+        constexpr int AHEAD = 3;                         // operand fragments read ahead
+        const char* const qrow = sb + (32 * sub_n + col) * SM::ROW_BYTES;
+        auto fragment = [&](int kb) { return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qrow + (((2 * kb + g) ^ SM::f(col)) << 4))); };
+        bf16x8 qf[KB];
+        f32x4 nl[4];
+#pragma unroll
+        for (int kb = 0; kb < AHEAD; ++kb) qf[kb] = fragment(kb);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) nl[q] = *reinterpret_cast<const f32x4*>(&neg_lse[st][32 * sub_p + 8 * q + 4 * g]);
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) Sn[b][i] = 0.f;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (kb + AHEAD < KB) qf[kb + AHEAD] = fragment(kb + AHEAD);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) Sn[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[kb], kf[b][kb], Sn[b], 0, 0, 0);
+#pragma unroll
+            for (int x = 4 * NB * kb / KB; x < 4 * NB * (kb + 1) / KB; ++x) {      // four weights: registers 4 q .. 4 q + 3 of block b
+                const int q = x / NB, b = x % NB;
+                float p[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(Sp[b][4 * q + e], a.scale_log2e, nl[q][e]));
+                acc[b] += (p[0] + p[1]) + (p[2] + p[3]);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    f32x16 A[NB], B[NB];
     if (row_lo < row_hi) {
-        issue(row_lo, stage0);
-        if (threadIdx.x < WGT_ROWS) stage_rows(row_lo, 0);
-        for (int row = row_lo; row < row_hi; row += 2 * WGT_ROWS) {
-            tile(row, 0, stage0, stage1);
-            if (row + WGT_ROWS < row_hi) tile(row + WGT_ROWS, 1, stage1, stage0);
+        int row = row_lo;
+        issue(stage0);
+        stage_rows(0);
+        // ---- rows that do not see all of the workgroup's keys, an even number of tiles
+        auto plain = [&](int st, const char* sb, char* other) {
+            wait_vmcnt<0>();
+            __syncthreads();
+            if (row + WGT_ROWS < row_hi) issue(other);
+#pragma unroll 1
+            for (int sub = 0; sub < 2; ++sub) {
+                products(A, sb, sub);
+                sums(A, st, sub, std::true_type{});
+            }
+            if (row + WGT_ROWS < row_hi) stage_rows(st ^ 1);
+            row += WGT_ROWS;
+        };
+        while (row < row_hi && row < (kv0 + KEYS - 1 - c0) * a.G) {
+            plain(0, stage0, stage1);
+            if (row < row_hi) plain(1, stage1, stage0);
+        }
+        // ---- the others.  Tile i lies in stage i & 1 and has its rows' sums in slot i & 3 (a wave may still be at the last rows of tile i - 1 when
+        // another stages those of tile i + 1).
+        if (row < row_hi) {
+            wait_vmcnt<0>();
+            __syncthreads();
+            if (row + WGT_ROWS < row_hi) issue(stage1);
+            products(A, stage0, 0);
+            int i = 0;
+            auto next = [&](char* free_stage, const char* sb) {     // on to the next tile, in sb
+                stage_rows((i + 1) & 3);
+                wait_vmcnt<0>();
+                __syncthreads();
+                row += WGT_ROWS;
+                if (row + WGT_ROWS < row_hi) issue(free_stage);
+                both(A, sb, 0, B, i & 3, 1);
+                ++i;
+            };
+            for (;;) {
+                both(B, stage0, 1, A, i & 3, 0);
+                if (row + WGT_ROWS >= row_hi) break;
+                next(stage0, stage1);
+                both(B, stage1, 1, A, i & 3, 0);
+                if (row + WGT_ROWS >= row_hi) break;
+                next(stage1, stage0);
+            }
+            sums(B, i & 3, 1, std::false_type{});
         }
     }
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < NB; ++b) {
         const float sum = sum_with_other_half(acc[b]);
         const int key = key0 + 32 * b + col;
         if (g != 0 || key >= kv_len) continue;
-        if (parts == 1) store_weight(a, place, kvh, c0, key, sum);
-        else a.part[((int64_t)pair * a.H_kv + kvh) * WGT_KEYS + key - kv0] = sum;
+        if (part < 0) store_weight(a, place, kvh, c0, key, sum);
+        else a.part[((int64_t)part * a.H_kv + kvh) * KEYS + key - kv0] = sum;
     }
 }
 
-// The parts of a tile's rows, summed in order; one workgroup per (tile, head) and one thread per key.  tile_cu: tiles of cut requests
-// before each request.
-__global__ void __launch_bounds__(WGT_KEYS) attn_weights_merge_kernel(WeightArgs a, const int32_t* tile_cu) {
-    const int kvh = (int)blockIdx.x % a.H_kv, tile = (int)blockIdx.x / a.H_kv;
-    const int r = request_of(tile_cu, a.n_req, tile);
-    const int tok0 = a.cu[r], n = a.cu[r + 1] - tok0, c0 = a.start[r];
-    const int parts = (n * a.G + a.part_rows - 1) / a.part_rows;
-    const int in_req = tile - tile_cu[r], key = in_req * WGT_KEYS + (int)threadIdx.x;
-    if (key >= c0 + n) return;
+// The same for requests of at most 16 rows (decoding): bound by the keys' bytes, so that nothing is shared between waves and none waits for
+// another.  A wave holds 64 keys as four blocks of columns of 16x16x32 products, 64 contiguous bytes of a key per load and lane group, all of them in
+// flight at once, four workgroups to a compute unit; the query rows come straight from memory.
+template <int D>
+__global__ void __launch_bounds__(WGT_THREADS, D == 256 ? 2 : 4) attn_weights_few_kernel(WeightArgs a) {
+    constexpr int KS = D / 32, NB = wgt_keys(D) / 64;       // NB: blocks of 16 keys per wave
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int i16 = lane & 15, g = lane >> 4;
+    const int kvh = (int)blockIdx.x % a.H_kv;
+    const int32_t* const rec = a.unit_rec + (int64_t)((int)blockIdx.x / a.H_kv) * WGT_REC;
+    const int tok0 = rec[0], n = rec[1], c0 = rec[2], place = rec[3], rows = rec[6];
+    const int kv_len = c0 + n, key0 = rec[4] + 16 * NB * wave;
+    if (key0 >= kv_len) return;
+    const int mask = (1 << a.page_shift) - 1;
+    u32x4 kf[NB][KS];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const int key = min(key0 + 16 * b + i16, kv_len - 1);
+        const uint16_t* const kp = a.k_pool + (int64_t)a.page_ids[place + (key >> a.page_shift)] * a.page_stride + ((int64_t)kvh * D << a.page_shift) +
+                                   (int64_t)(key & mask) * D + 8 * g;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) kf[b][s] = *reinterpret_cast<const u32x4*>(kp + 32 * s);
+    }
+    // the key whose sum this lane stores
+    const int mine = key0 + lane;
+    const bool stores = lane < 16 * NB && mine < kv_len;
+    int64_t at = 0;
+    float held = 0.f;
+    if (stores) {
+        at = (int64_t)a.page_ids[place + (mine >> a.page_shift)] * a.w_stride + ((int64_t)kvh << a.page_shift) + (mine & mask);
+        if (a.w_in && mine < c0) held = a.w_in[at];
+    }
+    // query rows: operand A, row i16, d = 32 s + 8 g + {0..7};  the sums: rows 4 g + e
+    bf16x8 qf[KS];
+    float nl[4];
+    int lim[4];
+    {
+        const int row = min(i16, rows - 1), t = row / a.G;
+        const uint16_t* const qp = a.q + ((int64_t)(tok0 + t) * a.H_q + kvh * a.G + row - t * a.G) * D + 8 * g;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) qf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qp + 32 * s));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int x = 4 * g + e, te = min(x, rows - 1) / a.G;
+            lim[e] = x < rows ? c0 + te : -1;
+            nl[e] = -a.lse[(int64_t)(tok0 + te) * a.H_q + kvh * a.G + min(x, rows - 1) - te * a.G] * 1.4426950408889634f;
+        }
+    }
     float sum = 0.f;
-    for (int p = 0; p < parts; ++p) sum += a.part[(((int64_t)a.block_cu[r] + (int64_t)in_req * parts + p) * a.H_kv + kvh) * WGT_KEYS + threadIdx.x];
-    store_weight(a, a.place[r], kvh, c0, key, sum);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        f32x4 S = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < KS; ++s) S = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[s], __builtin_bit_cast(bf16x8, kf[b][s]), S, 0, 0, 0);
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[e], a.scale_log2e, nl[e]));
+            if (key0 + 16 * b + i16 > lim[e]) p[e] = 0.f;
+        }
+        const float all = sum_over_groups((p[0] + p[1]) + (p[2] + p[3]));
+        if (g == b) sum = all;
+    }
+    if (stores) a.w_out[at] = (a.w_in && mine < c0 ? a.decay * held : 0.f) + sum;
+}
+
+// The parts of a tile's rows, summed in order; one workgroup per (tile, head) and one thread per key.
+template <int KEYS>
+__global__ void __launch_bounds__(KEYS) attn_weights_merge_kernel(WeightArgs a) {
+    const int kvh = (int)blockIdx.x % a.H_kv;
+    const int32_t* const rec = a.merge_rec + (int64_t)((int)blockIdx.x / a.H_kv) * WGT_MERGE;
+    const int kv_len = rec[0], c0 = rec[1], place = rec[2], kv0 = rec[3], p0 = rec[4], p1 = rec[WGT_MERGE + 4];
+    const int key = kv0 + (int)threadIdx.x;
+    if (key >= kv_len) return;
+    float sum = 0.f;
+#pragma unroll 8
+    for (int p = p0; p < p1; ++p) sum += a.part[((int64_t)p * a.H_kv + kvh) * KEYS + threadIdx.x];
+    store_weight(a, place, kvh, c0, key, sum);
 }
 
 // ---------------------------------------------------------------- eviction

@@ -83,6 +83,7 @@ FRONT = [                                                                     # 
     (dict(shape=AT.make_attn_shape(4, 3, 64)), -3),
     (dict(k_pool=FakePool(0x200000, (40, 2, 24, 64)), v_pool=FakePool(0x300000, (40, 2, 24, 64))), -3),   # rows per page
     (dict(k_pool=FakePool(0x200000, (40, 2, 8, 64)), v_pool=FakePool(0x300000, (40, 2, 8, 64))), -3),
+    (dict(k_pool=FakePool(0x200000, (40, 2, 512, 64)), v_pool=FakePool(0x300000, (40, 2, 512, 64))), -3),
     (dict(k_pool=FakePool(0x200000, stride0=2044), v_pool=FakePool(0x300000, stride0=2044)), -2),
     (dict(k_pool=FakePool(0x200000, stride0=1024), v_pool=FakePool(0x300000, stride0=1024)), -3),         # pages would overlap
     (dict(page_ids=[7, 3, 40]), -5),
