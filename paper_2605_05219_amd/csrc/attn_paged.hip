@@ -263,9 +263,16 @@ struct WeightPlan {
     std::vector<int32_t> wide, few, merge;       // WGT_REC, WGT_REC, WGT_MERGE ints each
 };
 
-// The rows of a tile are cut on a grid of `run` row tiles of 64, so that the chip is full and its last round short: a workgroup takes as long as its row
-// tiles and about WGT_START more for its keys, and WGT_SLOTS of them run at once (two to a compute unit).
+// The rows of a tile are cut on a grid of `run` row tiles of 64, the first quarter of them four times finer, so that the chip is full and the short units,
+// which go last, fill its end: a workgroup takes as long as its row tiles and about WGT_START more for its keys, and WGT_SLOTS of them run at
+// once (two to a compute unit).
 constexpr int WGT_SLOTS = 512, WGT_START = 2;
+struct RowGrid {
+    int64_t run, fine, edge;             // row tiles per cut behind `edge` and before it (a multiple of `fine`)
+    RowGrid(int64_t run, int64_t m) : run(run), fine(std::max<int64_t>(1, run / 4)), edge(run >= m ? 0 : m / 4 / fine * fine) {}
+    int64_t index(int64_t tile) const { return tile < edge ? tile / fine : edge / fine + (tile - edge) / run; }
+    int64_t begin(int64_t i) const { return i < edge / fine ? i * fine : edge + (i - edge / fine) * run; }
+};
 
 void plan_weights(const attn_shape* s, int32_t n_req, const int32_t* cu, const int32_t* start, const int32_t* len, const int32_t* place, WeightPlan& out) {
     const int G = s->H_q / s->H_kv, keys = wgt_keys(s->d);
@@ -284,12 +291,13 @@ void plan_weights(const attn_shape* s, int32_t n_req, const int32_t* cu, const i
             if (is_few(r)) continue;
             const int64_t m = row_tiles(r);
             most = std::max(most, m);
-            const int64_t whole = std::min<int64_t>(tiles_of(r), start[r] / keys + 1), parts = std::max<int64_t>(1, (m + run - 1) / run);   // tiles that every row sees a key of
+            const RowGrid grid(run, m);
+            const int64_t whole = std::min<int64_t>(tiles_of(r), start[r] / keys + 1), parts = m > 0 ? grid.index(m - 1) + 1 : 1;   // tiles that every row sees a key of
             units += whole * parts;
             work += whole * m;
             if (parts > 1) cut += whole * parts;
             for (int32_t t = (int32_t)whole; t < tiles_of(r); ++t) {
-                const int64_t f = first_seen(r, t), p = (m - 1) / run - f / run + 1;
+                const int64_t f = first_seen(r, t), p = grid.index(m - 1) - grid.index(f) + 1;
                 units += p;
                 work += m - f;
                 if (p > 1) cut += p;
@@ -299,10 +307,10 @@ void plan_weights(const attn_shape* s, int32_t n_req, const int32_t* cu, const i
     };
     int64_t cut = 0, units = units_of(INT32_MAX, cut), run = std::max<int64_t>(most, 1);
     if (most > 1) {
-        auto cost = [&](int64_t c, int64_t n) {            // half way between whole rounds of equal units and units that fill every gap
-            const double per = (double)(n * s->H_kv) / WGT_SLOTS;
-            const double even = ((double)work * s->H_kv + (double)WGT_START * n * s->H_kv) / WGT_SLOTS + 0.5 * (c + WGT_START);
-            return 0.5 * (std::ceil(per) * (c + WGT_START) + std::max(even, (double)(c + WGT_START)));
+        auto cost = [&](int64_t c, int64_t n) {            // units that fill every gap but half of the last short one, and no less than one unit
+            const int64_t last = c < most ? std::max<int64_t>(1, c / 4) : c;
+            const double even = (double)((work + WGT_START * n) * s->H_kv) / WGT_SLOTS + 0.5 * (double)(last + WGT_START);
+            return std::max(even, (double)(c + WGT_START));
         };
         double best = cost(most, units);
         for (int64_t c = most; c > 1;) {
@@ -335,21 +343,22 @@ void plan_weights(const attn_shape* s, int32_t n_req, const int32_t* cu, const i
             continue;
         }
         base.resize(tiles);
-        const int32_t runs = (int32_t)((m + run - 1) / run);
+        const RowGrid grid(run, m);
+        auto cut_of = [&](int32_t t) { return (int32_t)grid.index(first_seen(r, t)); };      // the first cut of rows that sees a key of tile t
+        const int32_t cuts = (int32_t)grid.index(m - 1) + 1;
         for (int32_t t = 0; t < tiles; ++t) {
-            const int32_t parts = runs - (int32_t)(first_seen(r, t) / run);
-            base[t] = parts > 1 ? slot - (int32_t)(first_seen(r, t) / run) : -1;     // + the run's number: its partial sum
+            const int32_t parts = cuts - cut_of(t);
+            base[t] = slot - cut_of(t);                  // + the cut's number: its partial sum
             if (parts <= 1) continue;
             out.merge.insert(out.merge.end(), {start[r] + len[r], start[r], place[r], t * keys, slot});
             slot += parts;
         }
-        for (int32_t c = runs - 1; c >= 0; --c) {
-            const int32_t lo = (int32_t)(c * run), hi = (int32_t)std::min<int64_t>((c + 1) * run, m);
+        for (int32_t c = cuts - 1; c >= 0; --c) {
+            const int32_t lo = (int32_t)grid.begin(c), hi = (int32_t)std::min<int64_t>(grid.begin(c + 1), m);
             for (int32_t t = 0; t < tiles; ++t) {
                 const int32_t f = std::max(lo, first_seen(r, t));
                 if (f >= hi) break;
-                const bool whole = runs - (int32_t)(first_seen(r, t) / run) <= 1;
-                list.push_back({r, t * keys, f * WGT_ROWS, std::min(hi * WGT_ROWS, rows), whole ? -1 : base[t] + c});
+                list.push_back({r, t * keys, f * WGT_ROWS, std::min(hi * WGT_ROWS, rows), cuts - cut_of(t) <= 1 ? -1 : base[t] + c});
             }
         }
     }

@@ -196,7 +196,8 @@ template <int D>
 __global__ void __launch_bounds__(WGT_THREADS, 2) attn_weights_kernel(WeightArgs a) {
     typedef WeightSmem<D> SM;
     constexpr int KB = D / 16, KEYS = wgt_keys(D), NB = KEYS / 128;      // NB: blocks of 32 keys per wave
-    __shared__ __attribute__((aligned(1024))) char stage0[SM::TILE_BYTES], stage1[SM::TILE_BYTES];
+    constexpr int AHEAD_TILES = D == 256 ? 1 : 2;    // a tile is asked for this many tiles ahead (three stages at d = 256 would leave one workgroup to a compute unit)
+    __shared__ __attribute__((aligned(1024))) char stage0[SM::TILE_BYTES], stage1[SM::TILE_BYTES], stage2[AHEAD_TILES == 2 ? SM::TILE_BYTES : 16];
     __shared__ __attribute__((aligned(16))) float neg_lse[4][WGT_ROWS];   // -lse log2(e); rows past the end -inf
     __shared__ __attribute__((aligned(16))) int limit[4][WGT_ROWS];       // last key a row sees
 
@@ -210,54 +211,79 @@ __global__ void __launch_bounds__(WGT_THREADS, 2) attn_weights_kernel(WeightArgs
 
     // ---- this wave's keys: operand B, column = key, d = 16 kb + 8 g + {0..7}
     const int key0 = kv0 + 32 * NB * wave;
-    bf16x8 kf[NB][KB];
+    int page[NB];
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-        const int key = min(key0 + 32 * b + col, kv_len - 1);
-        const uint16_t* const kp = a.k_pool + (int64_t)a.page_ids[place + (key >> a.page_shift)] * a.page_stride + ((int64_t)kvh * D << a.page_shift) +
-                                   (int64_t)(key & ((1 << a.page_shift) - 1)) * D + 8 * g;
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb) kf[b][kb] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(kp + 16 * kb));
-    }
+    for (int b = 0; b < NB; ++b) page[b] = a.page_ids[place + (min(key0 + 32 * b + col, kv_len - 1) >> a.page_shift)];
 
     // ---- the next tile to bring: its first row, that row's token and head (uniform; a tile is step_t tokens and step_h heads on)
     const int step_t = WGT_ROWS / a.G, step_h = WGT_ROWS - step_t * a.G;
     int row_n = row_lo, t_n = row_lo / a.G, h_n = row_lo - t_n * a.G;
     const int64_t tok_bytes = (int64_t)a.H_q * D * 2;
-    float lse_n = 0.f;           // of row row_n + thread (the first 64 threads)
-    int lim_n = 0;
-    // to LDS, 16-byte chunk c of a row at c ^ f(row); rows past the request's last one come as zeros
-    auto issue = [&](char* sb) {
-        const uint16_t* const base = a.q + ((int64_t)(tok0 + t_n) * a.H_q + kvh * a.G) * D;
-        const int bytes = (int)min((int64_t)INT32_MAX, (int64_t)(n - 1 - t_n) * tok_bytes + a.G * D * 2);
+    const float* const lse_base = a.lse + (int64_t)tok0 * a.H_q + kvh * a.G;
+    const uint16_t* const q_base = a.q + ((int64_t)tok0 * a.H_q + kvh * a.G) * D;
+    // where a lane's 16-byte chunks of a tile and its row's sum lie from the tile's first token: the same for every tile where tiles begin with a token's
+    // first head (64 a multiple of G)
+    int voff[SM::PPW], lse_t = 0, lse_off = 0;
+    auto places = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < SM::PPW; ++i) {
             const int s = (wave * SM::PPW + i) * 64 + lane, rr = s / SM::CPR, pos = s % SM::CPR;
             const int x = h_n + rr, t = (int)(((float)x + 0.5f) * a.inv_G);
-            load_to_lds(base, bytes, sb + (wave * SM::PPW + i) * 1024, (t * a.H_q + x - t * a.G) * D * 2 + ((pos ^ SM::f(rr)) << 4), 0);
+            voff[i] = (t * a.H_q + x - t * a.G) * D * 2 + ((pos ^ SM::f(rr)) << 4);
         }
-        if (threadIdx.x < WGT_ROWS) {
-            const int x = h_n + (int)threadIdx.x, t = (int)(((float)x + 0.5f) * a.inv_G);
-            lim_n = c0 + t_n + t;
-            if (row_n + (int)threadIdx.x < row_hi) lse_n = a.lse[(int64_t)(tok0 + t_n + t) * a.H_q + kvh * a.G + x - t * a.G];
-            else lse_n = INFINITY;
-        }
+        const int x = h_n + ((int)threadIdx.x & (WGT_ROWS - 1));
+        lse_t = (int)(((float)x + 0.5f) * a.inv_G);
+        lse_off = lse_t * a.H_q + x - lse_t * a.G;
     };
-    auto stage_rows = [&](int st) {             // what issue() fetched of the rows' sums goes to LDS
+    places();
+    float lse_n = 0.f;           // of row row_n + thread (the first 64 threads)
+    int lim_n = 0;
+    // to LDS, 16-byte chunk c of a row at c ^ f(row); rows past the request's last one come as zeros
+    auto issue = [&](char* sb) __attribute__((always_inline)) {
+        if (step_h != 0) places();
         if (threadIdx.x < WGT_ROWS) {
-            neg_lse[st][threadIdx.x] = -lse_n * 1.4426950408889634f;
-            limit[st][threadIdx.x] = lim_n;
+            lim_n = c0 + t_n + lse_t;
+            lse_n = row_n + (int)threadIdx.x < row_hi ? lse_base[(int64_t)t_n * a.H_q + lse_off] : INFINITY;
         }
+        const uint16_t* const base = q_base + (int64_t)t_n * (a.H_q * D);
+        const int bytes = (int)min((int64_t)INT32_MAX, (int64_t)(n - 1 - t_n) * tok_bytes + a.G * D * 2);
+#pragma unroll
+        for (int i = 0; i < SM::PPW; ++i) load_to_lds(base, bytes, sb + (wave * SM::PPW + i) * 1024, voff[i], 0);
         row_n += WGT_ROWS;
         t_n += step_t;
         h_n += step_h;
         if (h_n >= a.G) { h_n -= a.G; ++t_n; }
     };
+    auto stage_rows = [&](int st, float lse, int lim) __attribute__((always_inline)) {    // what issue() fetched of the rows' sums goes to LDS
+        if (threadIdx.x < WGT_ROWS) {
+            neg_lse[st][threadIdx.x] = -lse * 1.4426950408889634f;
+            limit[st][threadIdx.x] = lim;
+        }
+    };
+    // the first tiles are on their way while the page ids come, behind which the keys can be asked for
+    const bool any = row_lo < row_hi, second = AHEAD_TILES == 2 && row_lo + WGT_ROWS < row_hi;
+    float lse0 = 0.f;
+    int lim0 = 0;
+    if (any) {
+        issue(stage0);
+        lse0 = lse_n;
+        lim0 = lim_n;
+        if (second) issue(stage1);
+    }
+    bf16x8 kf[NB][KB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const int key = min(key0 + 32 * b + col, kv_len - 1);
+        const uint16_t* const kp = a.k_pool + (int64_t)page[b] * a.page_stride + ((int64_t)kvh * D << a.page_shift) +
+                                   (int64_t)(key & ((1 << a.page_shift) - 1)) * D + 8 * g;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) kf[b][kb] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(kp + 16 * kb));
+    }
     float acc[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) acc[b] = 0.f;
     // the logits of 32 rows of a stage
-    auto products = [&](f32x16 (&S)[NB], const char* sb, int sub) {
+    auto products = [&](f32x16 (&S)[NB], const char* sb, int sub) __attribute__((always_inline)) {
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -270,30 +296,32 @@ __global__ void __launch_bounds__(WGT_THREADS, 2) attn_weights_kernel(WeightArgs
             for (int b = 0; b < NB; ++b) S[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, kf[b][kb], S[b], 0, 0, 0);
         }
     };
-    // their weights, summed; CUT: some row does not see some key of this wave
-    auto sums = [&](const f32x16 (&S)[NB], int st, int sub, auto cut) {
+    // the weights of 32 rows, summed, four of a block (registers 4 q .. 4 q + 3) at a time; CUT: some row does not see some key of this wave
+    auto sum4 = [&](const f32x16& S, int b, int q, f32x4 nl, const int* lim, auto cut) __attribute__((always_inline)) {
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[4 * q + e], a.scale_log2e, nl[e]));
+            if constexpr (decltype(cut)::value)
+                if (key0 + 32 * b + col > lim[e]) p[e] = 0.f;
+        }
+        acc[b] += (p[0] + p[1]) + (p[2] + p[3]);
+    };
+    auto sums = [&](const f32x16 (&S)[NB], int st, int sub) __attribute__((always_inline)) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const f32x4 nl = *reinterpret_cast<const f32x4*>(&neg_lse[st][32 * sub + 8 * q + 4 * g]);
+            const int at = 32 * sub + 8 * q + 4 * g;
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                float p[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[b][4 * q + e], a.scale_log2e, nl[e]));
-                    if constexpr (decltype(cut)::value)
-                        if (key0 + 32 * b + col > limit[st][32 * sub + 8 * q + 4 * g + e]) p[e] = 0.f;
-                }
-                acc[b] += (p[0] + p[1]) + (p[2] + p[3]);
-            }
+            for (int b = 0; b < NB; ++b) sum4(S[b], b, q, *reinterpret_cast<const f32x4*>(&neg_lse[st][at]), &limit[st][at], std::true_type{});
         }
     };
     // both, of different rows, in turn: the products of a step of the contraction, then the vector work of four weights or more, which the
     // products in flight cover; nothing moves from step to step
-    auto both = [&](f32x16 (&Sn)[NB], const char* sb, int sub_n, const f32x16 (&Sp)[NB], int st, int sub_p) {
+    auto both_cut = [&](f32x16 (&Sn)[NB], const char* sb, int sub_n, const f32x16 (&Sp)[NB], int st, int sub_p, auto cut) __attribute__((always_inline)) {
         constexpr int AHEAD = 3;                         // operand fragments read ahead
+        constexpr int LATE = KB >= 8 ? KB / 4 : 1;       // steps before the first weights: the last products of these and their rows' sums are on their way
         const char* const qrow = sb + (32 * sub_n + col) * SM::ROW_BYTES;
-        auto fragment = [&](int kb) { return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qrow + (((2 * kb + g) ^ SM::f(col)) << 4))); };
+        auto fragment = [&](int kb) __attribute__((always_inline)) { return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qrow + (((2 * kb + g) ^ SM::f(col)) << 4))); };
         bf16x8 qf[KB];
         f32x4 nl[4];
 #pragma unroll
@@ -311,65 +339,51 @@ __global__ void __launch_bounds__(WGT_THREADS, 2) attn_weights_kernel(WeightArgs
 #pragma unroll
             for (int b = 0; b < NB; ++b) Sn[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[kb], kf[b][kb], Sn[b], 0, 0, 0);
 #pragma unroll
-            for (int x = 4 * NB * kb / KB; x < 4 * NB * (kb + 1) / KB; ++x) {      // four weights: registers 4 q .. 4 q + 3 of block b
-                const int q = x / NB, b = x % NB;
-                float p[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(Sp[b][4 * q + e], a.scale_log2e, nl[q][e]));
-                acc[b] += (p[0] + p[1]) + (p[2] + p[3]);
-            }
+            for (int x = 4 * NB * max(kb - LATE, 0) / (KB - LATE); x < 4 * NB * max(kb + 1 - LATE, 0) / (KB - LATE); ++x)
+                sum4(Sp[x % NB], x % NB, x / NB, nl[x / NB], &limit[st][32 * sub_p + 8 * (x / NB) + 4 * g], cut);
         }
         __builtin_amdgcn_sched_barrier(0);
     };
+    auto both = [&](f32x16 (&Sn)[NB], const char* sb, int sub_n, const f32x16 (&Sp)[NB], int st, int sub_p, bool cut) __attribute__((always_inline)) {
+        if (cut) both_cut(Sn, sb, sub_n, Sp, st, sub_p, std::true_type{});
+        else both_cut(Sn, sb, sub_n, Sp, st, sub_p, std::false_type{});
+    };
+    // Tile i has its rows' sums in slot i & 3 (a wave may still be at the last rows of tile i - 1 when another stages those of the tile ahead).
     f32x16 A[NB], B[NB];
-    if (row_lo < row_hi) {
-        int row = row_lo;
-        issue(stage0);
-        stage_rows(0);
-        // ---- rows that do not see all of the workgroup's keys, an even number of tiles
-        auto plain = [&](int st, const char* sb, char* other) {
-            wait_vmcnt<0>();
-            __syncthreads();
-            if (row + WGT_ROWS < row_hi) issue(other);
-#pragma unroll 1
-            for (int sub = 0; sub < 2; ++sub) {
-                products(A, sb, sub);
-                sums(A, st, sub, std::true_type{});
-            }
-            if (row + WGT_ROWS < row_hi) stage_rows(st ^ 1);
-            row += WGT_ROWS;
-        };
-        while (row < row_hi && row < (kv0 + KEYS - 1 - c0) * a.G) {
-            plain(0, stage0, stage1);
-            if (row < row_hi) plain(1, stage1, stage0);
-        }
-        // ---- the others.  Tile i lies in stage i & 1 and has its rows' sums in slot i & 3 (a wave may still be at the last rows of tile i - 1 when
-        // another stages those of tile i + 1).
-        if (row < row_hi) {
-            wait_vmcnt<0>();
-            __syncthreads();
-            if (row + WGT_ROWS < row_hi) issue(stage1);
-            products(A, stage0, 0);
-            int i = 0;
-            auto next = [&](char* free_stage, const char* sb) {     // on to the next tile, in sb
-                stage_rows((i + 1) & 3);
+    if (any) {
+        int row = row_lo, i = 0;
+        const int cut_end = (key0 + 32 * NB - 1 - c0) * a.G;      // rows before it do not see all of this wave's keys
+        stage_rows(0, lse0, lim0);
+        if (second) stage_rows(1, lse_n, lim_n);
+        wait_vmcnt<0>();
+        __syncthreads();
+        products(A, stage0, 0);
+        // a tile from its second half to the first half of the next; `ahead`: the stage that the tile before left.  False: it was the last one.
+        auto step = [&](const char* sb, const char* next, char* ahead) __attribute__((always_inline)) {
+            const bool more = row + AHEAD_TILES * WGT_ROWS < row_hi;
+            if (more) issue(ahead);
+            both(B, sb, 1, A, i & 3, 0, row < cut_end);
+            if (row + WGT_ROWS >= row_hi) return false;
+            if (more) {
+                stage_rows((i + AHEAD_TILES) & 3, lse_n, lim_n);
+                wait_vmcnt<AHEAD_TILES == 2 ? SM::PPW : 0>();
+            } else {
                 wait_vmcnt<0>();
-                __syncthreads();
-                row += WGT_ROWS;
-                if (row + WGT_ROWS < row_hi) issue(free_stage);
-                both(A, sb, 0, B, i & 3, 1);
-                ++i;
-            };
-            for (;;) {
-                both(B, stage0, 1, A, i & 3, 0);
-                if (row + WGT_ROWS >= row_hi) break;
-                next(stage0, stage1);
-                both(B, stage1, 1, A, i & 3, 0);
-                if (row + WGT_ROWS >= row_hi) break;
-                next(stage1, stage0);
             }
-            sums(B, i & 3, 1, std::false_type{});
+            __syncthreads();
+            both(A, next, 0, B, i & 3, 1, row < cut_end);
+            row += WGT_ROWS;
+            ++i;
+            return true;
+        };
+        for (;;) {
+            if constexpr (AHEAD_TILES == 2) {
+                if (!step(stage0, stage1, stage2) || !step(stage1, stage2, stage0) || !step(stage2, stage0, stage1)) break;
+            } else {
+                if (!step(stage0, stage1, stage1) || !step(stage1, stage0, stage0)) break;
+            }
         }
+        sums(B, i & 3, 1);
     }
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
