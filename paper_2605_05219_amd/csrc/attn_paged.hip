@@ -3,8 +3,10 @@
 
 #include <algorithm>
 #include <cmath>
+#include <mutex>
 #include <new>
 #include <stdexcept>
+#include <thread>
 #include <vector>
 
 #include "attn_launch.h"
@@ -108,6 +110,68 @@ int32_t check_front(const attn_shape* s, int32_t n_req, const attn_pages* pages)
     return check_pages(s, pages);
 }
 
+// ---- a call's image to the device.  Small ones go by value (gdn::upload_plan); page tables are larger, and a copy of more than 16 KiB takes the
+// stream 20 us between two kernels: these a launch of ours reads out of pinned memory (4 us for 90 KB).  The buffers form a ring; a workgroup that has
+// read its piece says so in a word of the buffer, and a call that comes round to a buffer waits (on the host) for all of them.
+constexpr int FETCH_RING = 8, FETCH_THREADS = 256, FETCH_PIECE = 16 * FETCH_THREADS;   // bytes per workgroup
+constexpr size_t FETCH_ABOVE = 7168;
+
+__global__ void __launch_bounds__(FETCH_THREADS) attn_fetch_kernel(const u32x4* src, u32x4* dst, int64_t n, uint32_t* read, uint32_t mark) {
+    const int64_t i = (int64_t)blockIdx.x * FETCH_THREADS + threadIdx.x;
+    if (i < n) dst[i] = src[i];
+    __syncthreads();                      // (waits for every load of the workgroup, whose values have been stored)
+    if (threadIdx.x == 0) __hip_atomic_store(read + blockIdx.x, mark, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+}
+
+struct FetchRing {
+    std::mutex mu;
+    struct Slot {
+        char* host = nullptr;             // words of the workgroups that have read, then the image
+        size_t bytes = 0;                 // room for the image
+        uint32_t mark = 0, blocks = 0;    // of the last upload
+    } slot[FETCH_RING];
+    int next = 0;
+};
+FetchRing g_fetch;
+
+int32_t send_image(const std::vector<int32_t>& img, void* dst, hipStream_t stream) {
+    const size_t bytes = img.size() * sizeof(int32_t);
+    if (bytes <= FETCH_ABOVE) return gdn::upload_plan(img.data(), bytes, dst, stream);
+    std::lock_guard<std::mutex> lock(g_fetch.mu);
+    FetchRing::Slot& s = g_fetch.slot[g_fetch.next];
+    g_fetch.next = (g_fetch.next + 1) % FETCH_RING;
+    const auto words = [](size_t room) { return (room + FETCH_PIECE - 1) / FETCH_PIECE; };
+    if (s.host) {
+        uint32_t* const read = reinterpret_cast<uint32_t*>(s.host);
+        for (uint32_t b = 0; b < s.blocks; ++b)
+            while (__atomic_load_n(read + b, __ATOMIC_ACQUIRE) != s.mark) std::this_thread::yield();
+    }
+    if (s.bytes < bytes) {
+        if (s.host) (void)hipHostFree(s.host);
+        s.host = nullptr;
+        s.bytes = s.blocks = 0;
+        const size_t room = (std::max<size_t>(2 * bytes, 1 << 17) + FETCH_PIECE - 1) / FETCH_PIECE * FETCH_PIECE;
+        void* p = nullptr;
+        const hipError_t e = hipHostMalloc(&p, room + (words(room) * sizeof(uint32_t) + 255) / 256 * 256, hipHostMallocCoherent);
+        if (e != hipSuccess) return hip_err(e);
+        s.host = static_cast<char*>(p);
+        s.bytes = room;
+        std::memset(s.host, 0, words(room) * sizeof(uint32_t));
+        s.mark = 0;
+    }
+    uint32_t* const read = reinterpret_cast<uint32_t*>(s.host);
+    char* const image = s.host + (words(s.bytes) * sizeof(uint32_t) + 255) / 256 * 256;
+    std::memcpy(image, img.data(), bytes);
+    const uint32_t blocks = (uint32_t)words(bytes), mark = s.mark + 1 == 0 ? 1 : s.mark + 1;
+    hipLaunchKernelGGL(attn_fetch_kernel, dim3(blocks), dim3(FETCH_THREADS), 0, stream, reinterpret_cast<const u32x4*>(image), static_cast<u32x4*>(dst),
+                       (int64_t)((bytes + 15) / 16), read, mark);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return hip_err(e);
+    s.mark = mark;
+    s.blocks = blocks;
+    return GDN_OK;
+}
+
 int32_t rope_append(const attn_shape* s, const attn_rope* rope, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v,
                     int64_t ldv, int32_t n_req, const int32_t* cu, const int32_t* pos, const int32_t* start, const attn_pages* pages,
                     void* k_pool, void* v_pool, const int32_t* page_cu, const int32_t* page_ids, void* q_out, void* workspace,
@@ -165,7 +229,7 @@ int32_t rope_append(const attn_shape* s, const attn_rope* rope, const void* q, i
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(k_pool) || !aligned16(v_pool) || !aligned16(q_out)) return GDN_ERR_ALIGN;
     rc = check_workspace(s, n_req, T, page_cu[n_req], workspace, workspace_bytes);
     if (rc != GDN_OK) return rc;
-    rc = gdn::upload_plan(img.data(), img.size() * sizeof(int32_t), workspace, stream);
+    rc = send_image(img, workspace, stream);
     if (rc != GDN_OK) return rc;
     const int32_t* const d = static_cast<const int32_t*>(workspace);
     a.q = q; a.k = k; a.v = v;
@@ -225,7 +289,7 @@ int32_t paged_prefill(const attn_shape* s, const void* q, const void* gate, int3
     CallImage im;
     rc = make_image(s, plan, n_req, cu, start, len.data(), page_cu, page_ids, n_ids, im);
     if (rc != GDN_OK) return rc;
-    rc = gdn::upload_plan(im.img.data(), im.img.size() * sizeof(int32_t), workspace, stream);
+    rc = send_image(im.img, workspace, stream);
     if (rc != GDN_OK) return rc;
     const int32_t* const d = static_cast<const int32_t*>(workspace);
     char* const parts = static_cast<char*>(workspace) + image_bytes(s, n_req, T, n_ids);
@@ -421,7 +485,7 @@ int32_t key_weights(const attn_shape* s, const void* q, const float* lse, int32_
     std::copy(plan.few.begin(), plan.few.end(), img.begin() + few_at);
     std::copy(plan.merge.begin(), plan.merge.end(), img.begin() + merge_at);
     std::copy(page_ids, page_ids + n_ids, img.begin() + ids_at);
-    rc = gdn::upload_plan(img.data(), img.size() * sizeof(int32_t), workspace, stream);
+    rc = send_image(img, workspace, stream);
     if (rc != GDN_OK) return rc;
     const int32_t* const d = static_cast<const int32_t*>(workspace);
     WeightArgs a;
@@ -506,7 +570,7 @@ int32_t evict(const attn_shape* s, int32_t n_req, const int32_t* rows, const int
     for (int32_t r = 0; r < n_req; ++r, ++p) *p = p[-1] + kept[r];
     p = std::copy(page_ids, page_ids + n_old, p);
     p = std::copy(new_page_ids, new_page_ids + n_new, p);
-    rc = gdn::upload_plan(img.data(), img.size() * sizeof(int32_t), workspace, stream);
+    rc = send_image(img, workspace, stream);
     if (rc != GDN_OK) return rc;
     const int32_t* const d = static_cast<const int32_t*>(workspace);
     EvictArgs a;
