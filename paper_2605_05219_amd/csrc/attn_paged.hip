@@ -86,7 +86,7 @@ inline int64_t parts_bytes(int d) {
 inline int64_t image_bytes(const attn_shape* s, int32_t n_req, int64_t T, int64_t n_ids) {
     const int64_t attend = plan_ints(n_req, T, s->H_q / s->H_kv);
     const int64_t weights = WGT_REC * (2 * n_ids + n_req + WGT_PARTS) + WGT_MERGE * ((int64_t)WGT_PARTS + 1);
-    const int64_t ints = std::max<int64_t>(std::max(attend, weights), 8 * ((int64_t)n_req + 1)) + n_ids;
+    const int64_t ints = std::max<int64_t>(std::max(attend, weights), 8 * (int64_t)n_req + 2) + n_ids;
     return (ints * (int64_t)sizeof(int32_t) + 255) / 256 * 256;
 }
 
@@ -558,7 +558,8 @@ int32_t evict(const attn_shape* s, int32_t n_req, const int32_t* rows, const int
     rc = check_workspace(s, n_req, 0, (int64_t)n_old + n_new, workspace, workspace_bytes);
     if (rc != GDN_OK) return rc;
 
-    std::vector<int32_t> img((size_t)(7 * (int64_t)n_req + 1 + n_old + n_new));
+    const int copied = gather_rows(s->d);              // rows per workgroup of the copy
+    std::vector<int32_t> img((size_t)(8 * (int64_t)n_req + 2 + n_old + n_new));
     int32_t* p = img.data();
     p = std::copy(rows, rows + n_req, p);
     p = std::copy(kept.begin(), kept.end(), p);
@@ -568,6 +569,9 @@ int32_t evict(const attn_shape* s, int32_t n_req, const int32_t* rows, const int
     for (int32_t r = 0; r < n_req; ++r) *p++ = n_old + new_page_cu[r];
     *p++ = 0;
     for (int32_t r = 0; r < n_req; ++r, ++p) *p = p[-1] + kept[r];
+    *p++ = 0;
+    for (int32_t r = 0; r < n_req; ++r, ++p) *p = p[-1] + (kept[r] + copied - 1) / copied;
+    const int64_t blocks = (int64_t)p[-1] * s->H_kv;
     p = std::copy(page_ids, page_ids + n_old, p);
     p = std::copy(new_page_ids, new_page_ids + n_new, p);
     rc = send_image(img, workspace, stream);
@@ -585,19 +589,23 @@ int32_t evict(const attn_shape* s, int32_t n_req, const int32_t* rows, const int
     a.place = d + 4 * (int64_t)n_req;
     a.new_place = d + 5 * (int64_t)n_req;
     a.keep_cu = d + 6 * (int64_t)n_req;
-    a.page_ids = d + 7 * (int64_t)n_req + 1;
+    a.block_cu = d + 7 * (int64_t)n_req + 1;
+    a.page_ids = d + 8 * (int64_t)n_req + 2;
     a.page_stride = pages->page_stride;
     a.w_stride = w_stride;
     a.n_req = n_req;
     a.H_kv = s->H_kv;
     a.page_shift = shift_of(pages);
-    a.chunks = s->d / 8;
-    const int64_t n = total * s->H_kv * a.chunks, blocks = (n + GATHER_THREADS - 1) / GATHER_THREADS;
     if (blocks > INT32_MAX || (int64_t)n_req * s->H_kv > INT32_MAX) return GDN_ERR_COUNT;
     hipLaunchKernelGGL(attn_select_kernel, dim3((unsigned)(n_req * s->H_kv)), dim3(SEL_THREADS), 0, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return hip_err(e);
-    hipLaunchKernelGGL(attn_gather_rows_kernel, dim3((unsigned)blocks), dim3(GATHER_THREADS), 0, stream, a, n);
+    const dim3 grid((unsigned)blocks), block(GATHER_THREADS);
+    switch (s->d) {
+        case 64: hipLaunchKernelGGL((attn_gather_rows_kernel<64>), grid, block, 0, stream, a); break;
+        case 128: hipLaunchKernelGGL((attn_gather_rows_kernel<128>), grid, block, 0, stream, a); break;
+        default: hipLaunchKernelGGL((attn_gather_rows_kernel<256>), grid, block, 0, stream, a); break;
+    }
     return hip_err(hipGetLastError());
 }
 

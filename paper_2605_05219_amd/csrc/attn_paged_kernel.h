@@ -483,12 +483,10 @@ struct EvictArgs {
     int32_t* index;
     const int32_t *rows, *keep, *first, *recent;          // keep: at most rows
     const int32_t *place, *new_place, *keep_cu, *page_ids;   // page_ids: old and new ones; keep_cu: kept rows before each request
+    const int32_t* block_cu;                              // n_req + 1: workgroups of the copy, for one head, before each request
     int64_t page_stride, w_stride;
     int32_t n_req, H_kv, page_shift;
-    int32_t chunks;                                       // 16-byte chunks per row, d / 8
 };
-constexpr int SEL_THREADS = 1024;
-constexpr int GATHER_THREADS = 256;
 
 // A weight's rank as an unsigned number: larger weights larger, -0 as +0, what is not a number 0.
 __device__ __forceinline__ uint32_t weight_rank(float w) {
@@ -497,114 +495,180 @@ __device__ __forceinline__ uint32_t weight_rank(float w) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// The rows that one (request, head) keeps.  Four rounds over 8 bits each of the rank find the smallest rank kept and how many rows of
-// just that rank are; a last pass over the rows in order writes the row numbers kept.
+// The rows that one (request, head) keeps, by one workgroup.  The ranks come to LDS in one pass over the weights (those of rows behind SEL_HELD are read
+// again where they are needed) and give their least and greatest; rounds over 11 bits at a time, from the highest bit in which those differ, find
+// the smallest rank kept and how many rows of just that rank are.  Each wave then counts a run of rows of its own and writes the
+// numbers of those kept behind the waves before it.
+// Bound: latencies (a chain of dependent steps, one compute unit per head); digits of 11 bits from the highest differing one spread the weights over many
+// counters, where a byte of the exponent would put most of them on a few.  30000 rows 91 us with four rounds of 8 bits over memory.
+constexpr int SEL_THREADS = 1024;
+constexpr int SEL_HELD = 32768;
+constexpr int SEL_BITS = 11;
+
 __global__ void __launch_bounds__(SEL_THREADS) attn_select_kernel(EvictArgs a) {
-    constexpr int WAVES = SEL_THREADS / 64;
-    __shared__ int hist[256];
-    __shared__ uint32_t found[2];        // prefix of the smallest rank kept, rows of it still to take
-    __shared__ int wave_sum[2][WAVES];
+    constexpr int WAVES = SEL_THREADS / 64, BINS = 1 << SEL_BITS, LOADS = 8;
+    __shared__ uint32_t held[SEL_HELD];
+    __shared__ int hist[BINS];
+    __shared__ uint32_t wave_least[WAVES], wave_most[WAVES];
+    __shared__ int wave_a[WAVES], wave_b[WAVES], found[2];
     const int r = (int)blockIdx.x / a.H_kv, kvh = (int)blockIdx.x % a.H_kv;
     const int rows = a.rows[r], keep = a.keep[r], first = a.first[r], last = rows - a.recent[r];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int32_t* const out = a.index + (int64_t)a.H_kv * a.keep_cu[r] + (int64_t)kvh * keep;
+    if (keep == rows) {
+        for (int j = tid; j < rows; j += SEL_THREADS) out[j] = j;
+        return;
+    }
     const int32_t* const ids = a.page_ids + a.place[r];
-    auto rank_of = [&](int j) {
-        return weight_rank(a.w_pool[(int64_t)ids[j >> a.page_shift] * a.w_stride + ((int64_t)kvh << a.page_shift) + (j & ((1 << a.page_shift) - 1))]);
-    };
-    const int want = keep - first - a.recent[r];          // rows to take from [first, last)
-    uint32_t prefix = 0;
-    int left = want;
-    if (keep < rows && want > 0) {
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            if (tid < 256) hist[tid] = 0;
+    const float* const w = a.w_pool + ((int64_t)kvh << a.page_shift);
+    const int mask = (1 << a.page_shift) - 1;
+    auto rank_of = [&](int j) { return weight_rank(w[(int64_t)ids[j >> a.page_shift] * a.w_stride + (j & mask)]); };
+    auto rank = [&](int j) { return j < SEL_HELD ? held[j] : rank_of(j); };
+    const int want = keep - first - a.recent[r];          // rows to take from [first, last), fewer than there are
+    uint32_t edge = 0xffffffffu;                          // the smallest rank kept
+    int left = 0;                                         // how many rows of it
+    if (want > 0) {
+        uint32_t least = 0xffffffffu, most = 0u;
+        for (int j0 = first + tid; j0 < last; j0 += LOADS * SEL_THREADS) {
+            uint32_t x[LOADS];
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) x[i] = rank_of(min(j0 + i * SEL_THREADS, last - 1));
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int j = j0 + i * SEL_THREADS;
+                if (j < last && j < SEL_HELD) held[j] = x[i];
+                least = min(least, x[i]);
+                most = max(most, x[i]);
+            }
+        }
+        for (int d = 32; d > 0; d >>= 1) {
+            least = min(least, (uint32_t)__shfl_xor((int)least, d));
+            most = max(most, (uint32_t)__shfl_xor((int)most, d));
+        }
+        if (lane == 0) { wave_least[wave] = least; wave_most[wave] = most; }
+        __syncthreads();
+        for (int i = 0; i < WAVES; ++i) { least = min(least, wave_least[i]); most = max(most, wave_most[i]); }
+        edge = most;
+        left = want;
+        int bits = 32 - __clz((int)(least ^ most));       // __clz(0) is 32: all ranks are one
+        edge = bits < 32 ? edge >> bits << bits : 0u;     // the bits that all have
+        while (bits > 0) {
+            const int shift = max(0, bits - SEL_BITS), digits = 1 << (bits - shift);
+            for (int i = tid; i < digits; i += SEL_THREADS) hist[i] = 0;
             __syncthreads();
+#pragma unroll 4
             for (int j = first + tid; j < last; j += SEL_THREADS) {
-                const uint32_t x = rank_of(j);
-                if (shift == 24 || x >> (shift + 8) == prefix >> (shift + 8)) atomicAdd(&hist[(x >> shift) & 255], 1);
+                const uint32_t x = rank(j);
+                if (bits == 32 || x >> bits == edge >> bits) atomicAdd(&hist[(x >> shift) & (digits - 1)], 1);
             }
             __syncthreads();
-            if (wave == 0) {                              // from the largest digit down: lane l has digits 255 - 4 l .. 252 - 4 l
-                int c[4], sum = 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) sum += c[i] = hist[255 - 4 * lane - i];
-                int before = sum;
-                for (int d = 1; d < 64; d <<= 1) {
-                    const int up = __shfl_up(before, d);
-                    if (lane >= d) before += up;
-                }
-                before -= sum;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (before < left && before + c[i] >= left) {
-                        found[0] = prefix | (uint32_t)(255 - 4 * lane - i) << shift;
-                        found[1] = (uint32_t)(left - before);
-                    }
-                    before += c[i];
-                }
+            // from the largest digit down: thread t has digits digits - 1 - 2 t and the one below
+            const int d0 = digits - 1 - 2 * tid, n0 = d0 >= 0 ? hist[d0] : 0, n1 = d0 >= 1 ? hist[d0 - 1] : 0;
+            int upto = n0 + n1;
+            for (int d = 1; d < 64; d <<= 1) {
+                const int up = __shfl_up(upto, d);
+                if (lane >= d) upto += up;
             }
+            if (lane == 63) wave_a[wave] = upto;
             __syncthreads();
-            prefix = found[0];
-            left = (int)found[1];
+            int before = upto - n0 - n1;
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i) {
+                const int n = wave_a[i];                  // (all of them, whichever wave: the reads do not wait for each other)
+                before += i < wave ? n : 0;
+            }
+            if (before < left && before + n0 >= left) { found[0] = d0; found[1] = left - before; }
+            else if (before + n0 < left && before + n0 + n1 >= left) { found[0] = d0 - 1; found[1] = left - before - n0; }
             __syncthreads();
+            edge |= (uint32_t)found[0] << shift;
+            left = found[1];
+            bits = shift;
         }
     }
-    // ---- the rows kept, in order
-    int32_t* const out = a.index + (int64_t)a.H_kv * a.keep_cu[r] + (int64_t)kvh * keep;
-    int kept = 0, ties = 0;
-    for (int j0 = 0; j0 < rows; j0 += SEL_THREADS) {
-        const int j = j0 + tid;
-        const bool always = j < rows && (keep == rows || j < first || j >= last);
-        const bool middle = j < rows && !always && want > 0;
-        const uint32_t x = middle ? rank_of(j) : 0u;
-        const bool tie = middle && x == prefix;
-        const uint64_t tie_mask = __ballot(tie);
-        const uint64_t below = (1ull << lane) - 1;
-        if (lane == 0) wave_sum[0][wave] = __popcll(tie_mask);
-        __syncthreads();
-        int tie_at = ties, tie_all = 0;
-        for (int w = 0; w < WAVES; ++w) {
-            if (w < wave) tie_at += wave_sum[0][w];
-            tie_all += wave_sum[0][w];
-        }
-        tie_at += __popcll(tie_mask & below);
-        const bool take = always || (middle && (x > prefix || (tie && tie_at < left)));
-        const uint64_t mask = __ballot(take);
-        if (lane == 0) wave_sum[1][wave] = __popcll(mask);
-        __syncthreads();
-        int at = kept, all = 0;
-        for (int w = 0; w < WAVES; ++w) {
-            if (w < wave) at += wave_sum[1][w];
-            all += wave_sum[1][w];
-        }
-        if (take) out[at + __popcll(mask & below)] = j;
-        kept += all;
-        ties += tie_all;
-        __syncthreads();
+    // ---- the rows kept, in order: wave i has the rows [i run, (i + 1) run), 64 at a time
+    const int run = ((rows + WAVES - 1) / WAVES + 63) / 64 * 64;
+    const int j_lo = wave * run, j_hi = min(rows, j_lo + run);
+    auto look = [&](int j, bool& take, bool& tie) {
+        const bool always = j < j_hi && (j < first || j >= last), middle = j < j_hi && !always && want > 0;
+        const uint32_t x = middle ? rank(j) : 0u;
+        take = always || (middle && x > edge);
+        tie = middle && x == edge;
+    };
+    int taken = 0, ties = 0;
+#pragma unroll 4
+    for (int j = j_lo; j < j_hi; j += 64) {
+        bool take, tie;
+        look(j + lane, take, tie);
+        taken += __popcll(__ballot(take));
+        ties += __popcll(__ballot(tie));
+    }
+    __syncthreads();                                      // (wave_a was read above)
+    if (lane == 0) { wave_a[wave] = taken; wave_b[wave] = ties; }
+    __syncthreads();
+    int at = 0, tie_at = 0;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) {
+        const int n = wave_a[i], m = wave_b[i];
+        at += i < wave ? n : 0;
+        tie_at += i < wave ? m : 0;
+    }
+    at += min(tie_at, left);
+#pragma unroll 4
+    for (int j = j_lo; j < j_hi; j += 64) {
+        bool take, tie;
+        look(j + lane, take, tie);
+        const uint64_t below = (1ull << lane) - 1, tie_mask = __ballot(tie);
+        take = take || (tie && tie_at + __popcll(tie_mask & below) < left);
+        const uint64_t take_mask = __ballot(take);
+        if (take) out[at + __popcll(take_mask & below)] = j + lane;
+        at += __popcll(take_mask);
+        tie_at += __popcll(tie_mask);
     }
 }
 
-// The kept rows go to the new pages: one thread per 16-byte chunk of k and of v, a row's first one its weight too.
-__global__ void __launch_bounds__(GATHER_THREADS) attn_gather_rows_kernel(EvictArgs a, int64_t n) {
-    const int64_t id = (int64_t)blockIdx.x * GATHER_THREADS + threadIdx.x;
-    if (id >= n) return;
-    const int64_t item = id / a.chunks;                   // index entry
-    const int c = (int)(id - item * a.chunks);
-    int lo = 0, hi = a.n_req;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if ((int64_t)a.keep_cu[mid] * a.H_kv <= item) lo = mid; else hi = mid;
-    }
-    const int r = lo, keep = a.keep[r];
-    const int64_t in = item - (int64_t)a.keep_cu[r] * a.H_kv;
-    const int kvh = (int)(in / keep), to = (int)(in - (int64_t)kvh * keep), from = a.index[item];
-    const int mask = (1 << a.page_shift) - 1;
-    const int64_t p0 = a.page_ids[a.place[r] + (from >> a.page_shift)], p1 = a.page_ids[a.new_place[r] + (to >> a.page_shift)];
+// The kept rows go to the new pages: a workgroup copies ROWS consecutive ones of a head, a 16-byte chunk of k and of v of PASSES rows per thread, all
+// loads ahead of the stores.
+constexpr int GATHER_THREADS = 256, GATHER_PASSES = 4;
+__host__ __device__ constexpr int gather_rows(int d) { return GATHER_THREADS / (d / 8) * GATHER_PASSES; }
+
+template <int D>
+__global__ void __launch_bounds__(GATHER_THREADS) attn_gather_rows_kernel(EvictArgs a) {
+    constexpr int CPR = D / 8, STEP = GATHER_THREADS / CPR;
+    const int kvh = (int)blockIdx.x % a.H_kv, block = (int)blockIdx.x / a.H_kv;
+    const int r = __builtin_amdgcn_readfirstlane(request_of(a.block_cu, a.n_req, block));
+    const int keep = a.keep[r], mask = (1 << a.page_shift) - 1;
+    const int32_t* const index = a.index + (int64_t)a.H_kv * a.keep_cu[r] + (int64_t)kvh * keep;
+    const int32_t *const ids = a.page_ids + a.place[r], *const new_ids = a.page_ids + a.new_place[r];
+    const int to0 = (block - a.block_cu[r]) * gather_rows(D) + (int)threadIdx.x / CPR, c = (int)threadIdx.x % CPR;
     const int64_t head = (int64_t)kvh << a.page_shift;
-    const int64_t src = p0 * a.page_stride + ((head + (from & mask)) * a.chunks + c) * 8;
-    const int64_t dst = p1 * a.page_stride + ((head + (to & mask)) * a.chunks + c) * 8;
-    *reinterpret_cast<u32x4*>(a.k_pool + dst) = *reinterpret_cast<const u32x4*>(a.k_pool + src);
-    *reinterpret_cast<u32x4*>(a.v_pool + dst) = *reinterpret_cast<const u32x4*>(a.v_pool + src);
-    if (c == 0) a.w_pool[p1 * a.w_stride + head + (to & mask)] = a.w_pool[p0 * a.w_stride + head + (from & mask)];
+    int from[GATHER_PASSES];
+    int64_t old_page[GATHER_PASSES], new_page[GATHER_PASSES];
+#pragma unroll
+    for (int i = 0; i < GATHER_PASSES; ++i) {
+        const int to = min(to0 + i * STEP, keep - 1);
+        from[i] = index[to];
+        new_page[i] = new_ids[to >> a.page_shift];
+    }
+#pragma unroll
+    for (int i = 0; i < GATHER_PASSES; ++i) old_page[i] = ids[from[i] >> a.page_shift];
+    u32x4 k[GATHER_PASSES], v[GATHER_PASSES];
+    float w[GATHER_PASSES];
+#pragma unroll
+    for (int i = 0; i < GATHER_PASSES; ++i) {
+        const int64_t src = old_page[i] * a.page_stride + (head + (from[i] & mask)) * D + 8 * c;
+        k[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.k_pool + src));
+        v[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.v_pool + src));
+        if (c == 0) w[i] = a.w_pool[old_page[i] * a.w_stride + head + (from[i] & mask)];
+    }
+#pragma unroll
+    for (int i = 0; i < GATHER_PASSES; ++i) {
+        const int to = to0 + i * STEP;
+        if (to >= keep) break;
+        const int64_t dst = new_page[i] * a.page_stride + (head + (to & mask)) * D + 8 * c;
+        __builtin_nontemporal_store(k[i], reinterpret_cast<u32x4*>(a.k_pool + dst));
+        __builtin_nontemporal_store(v[i], reinterpret_cast<u32x4*>(a.v_pool + dst));
+        if (c == 0) a.w_pool[new_page[i] * a.w_stride + head + (to & mask)] = w[i];
+    }
 }
 
 }  // namespace attn

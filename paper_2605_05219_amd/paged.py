@@ -34,6 +34,15 @@ def make_attn_rope(freqs, layout="half", amplitude=1.0, in_dtype="bf16") -> attn
     return rope
 
 
+_ints = ctypes.c_int32 * 0
+
+
+def _ip(x):
+    """A host sequence as an int32 array that the call may read in place (a fifth of what `_hp` of `_h32` takes)."""
+    a = _h32(x)
+    return _ints.from_buffer(a if a.flags.writeable else a.copy())
+
+
 _ready = False
 
 
@@ -56,22 +65,18 @@ def _lib():
     return L
 
 
-def _pages(*pools) -> attn_pages:
+def _pages(*pools):
     """The common geometry of the given key and value pools."""
     p = pools[0]
-    geo = (int(p.stride(0)), int(p.shape[0]), int(p.shape[2]))
+    stride, shape = p.stride(0), p.shape
     for x in pools[1:]:
-        if (int(x.stride(0)), int(x.shape[0]), int(x.shape[2])) != geo:
+        if x.stride(0) != stride or x.shape[0] != shape[0] or x.shape[2] != shape[2]:
             raise GdnError(-3, "pools of one geometry")
-    return attn_pages(*geo)
-
-
-def _table(page_cu, page_ids):
-    return _h32(page_cu), _h32(page_ids)
+    return ctypes.byref(attn_pages(stride, shape[0], shape[2]))
 
 
 def _ws(workspace):
-    return _dp(workspace), int(workspace.numel() * workspace.element_size()) if workspace is not None else 0
+    return _dp(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0
 
 
 KINDS = {"plain": 0, "linear": 1, "base": 2, "ramp": 3}
@@ -95,46 +100,33 @@ def attn_rope_append(shape: attn_shape, rope: attn_rope, q, k, v, cu_seqlens, po
                      workspace, stream=None) -> None:
     """See include/attn_paged.h.  q, k, v are [T][heads][d] tensors whose token stride is passed on (heads and elements packed);
     pos may be None."""
-    cu, st = _h32(cu_seqlens), _h32(start)
-    ps = _h32(pos) if pos is not None else None
-    tcu, ids = _table(page_cu, page_ids)
-    pages = _pages(k_pool, v_pool)
-    _check(_lib().attn_rope_append(ctypes.byref(shape), ctypes.byref(rope), _dp(q), int(q.stride(0)), _dp(k), int(k.stride(0)), _dp(v),
-                                   int(v.stride(0)), int(st.size), _hp(cu), _hp(ps), _hp(st), ctypes.byref(pages), _dp(k_pool),
-                                   _dp(v_pool), _hp(tcu), _hp(ids), _dp(q_out), *_ws(workspace), _stream_ptr(stream)), "attn_rope_append")
+    _check(_lib().attn_rope_append(ctypes.byref(shape), ctypes.byref(rope), _dp(q), q.stride(0), _dp(k), k.stride(0), _dp(v), v.stride(0),
+                                   len(start), _ip(cu_seqlens), None if pos is None else _ip(pos), _ip(start), _pages(k_pool, v_pool),
+                                   _dp(k_pool), _dp(v_pool), _ip(page_cu), _ip(page_ids), _dp(q_out), *_ws(workspace), _stream_ptr(stream)),
+           "attn_rope_append")
 
 
 def attn_paged_prefill(shape: attn_shape, q, out_gate, cu_seqlens, start, k_pool, v_pool, page_cu, page_ids, o, lse, workspace,
                        stream=None) -> None:
     """See include/attn_paged.h.  out_gate and lse may be None."""
-    cu, st = _h32(cu_seqlens), _h32(start)
-    tcu, ids = _table(page_cu, page_ids)
-    pages = _pages(k_pool, v_pool)
-    _check(_lib().attn_paged_prefill(ctypes.byref(shape), _dp(q), _dp(out_gate), int(st.size), _hp(cu), _hp(st), ctypes.byref(pages),
-                                     _dp(k_pool), _dp(v_pool), _hp(tcu), _hp(ids), _dp(o), _dp(lse), *_ws(workspace),
+    _check(_lib().attn_paged_prefill(ctypes.byref(shape), _dp(q), _dp(out_gate), len(start), _ip(cu_seqlens), _ip(start), _pages(k_pool, v_pool),
+                                     _dp(k_pool), _dp(v_pool), _ip(page_cu), _ip(page_ids), _dp(o), _dp(lse), *_ws(workspace),
                                      _stream_ptr(stream)), "attn_paged_prefill")
 
 
 def attn_key_weights(shape: attn_shape, q, lse, cu_seqlens, start, k_pool, page_cu, page_ids, decay, w_in, w_out, workspace,
                      stream=None) -> None:
     """See include/attn_paged.h.  w_in may be None or w_out; the two have one page stride."""
-    cu, st = _h32(cu_seqlens), _h32(start)
-    tcu, ids = _table(page_cu, page_ids)
-    pages = _pages(k_pool)
-    if w_in is not None and int(w_in.stride(0)) != int(w_out.stride(0)):
+    if w_in is not None and w_in.stride(0) != w_out.stride(0):
         raise GdnError(-3, "attn_key_weights: w_in and w_out of one geometry")
-    _check(_lib().attn_key_weights(ctypes.byref(shape), _dp(q), _dp(lse), int(st.size), _hp(cu), _hp(st), ctypes.byref(pages),
-                                   _dp(k_pool), _hp(tcu), _hp(ids), float(decay), _dp(w_in), _dp(w_out), int(w_out.stride(0)),
-                                   *_ws(workspace), _stream_ptr(stream)), "attn_key_weights")
+    _check(_lib().attn_key_weights(ctypes.byref(shape), _dp(q), _dp(lse), len(start), _ip(cu_seqlens), _ip(start), _pages(k_pool), _dp(k_pool),
+                                   _ip(page_cu), _ip(page_ids), float(decay), _dp(w_in), _dp(w_out), w_out.stride(0), *_ws(workspace),
+                                   _stream_ptr(stream)), "attn_key_weights")
 
 
 def attn_evict(shape: attn_shape, rows, keep, first, recent, k_pool, v_pool, w_pool, page_cu, page_ids, new_page_cu, new_page_ids, index,
                workspace, stream=None) -> None:
     """See include/attn_paged.h.  index: int32, H_kv entries per kept row."""
-    rw, kp, fi, rc = _h32(rows), _h32(keep), _h32(first), _h32(recent)
-    tcu, ids = _table(page_cu, page_ids)
-    ncu, nids = _table(new_page_cu, new_page_ids)
-    pages = _pages(k_pool, v_pool)
-    _check(_lib().attn_evict(ctypes.byref(shape), int(rw.size), _hp(rw), _hp(kp), _hp(fi), _hp(rc), ctypes.byref(pages), _dp(k_pool),
-                             _dp(v_pool), _dp(w_pool), int(w_pool.stride(0)), _hp(tcu), _hp(ids), _hp(ncu), _hp(nids), _dp(index),
-                             *_ws(workspace), _stream_ptr(stream)), "attn_evict")
+    _check(_lib().attn_evict(ctypes.byref(shape), len(rows), _ip(rows), _ip(keep), _ip(first), _ip(recent), _pages(k_pool, v_pool), _dp(k_pool),
+                             _dp(v_pool), _dp(w_pool), w_pool.stride(0), _ip(page_cu), _ip(page_ids), _ip(new_page_cu), _ip(new_page_ids),
+                             _dp(index), *_ws(workspace), _stream_ptr(stream)), "attn_evict")
