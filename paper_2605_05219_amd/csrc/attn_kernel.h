@@ -947,11 +947,13 @@ __global__ void __launch_bounds__(CL_THREADS) attn_combine_long_kernel(CombineAr
     if (ch == 0) { sums[group][D] = L; sums[group][D + 1] = Le; }
     __syncthreads();
     if (threadIdx.x >= CH) return;
+#pragma unroll 8
     for (int k = 1; k < GROUPS; ++k) {
         const f32x4 op = *reinterpret_cast<const f32x4*>(&sums[k][4 * ch]);
         acc[0] += op[0]; acc[1] += op[1]; acc[2] += op[2]; acc[3] += op[3];
     }
     L = Le = 0.f;
+#pragma unroll 8
     for (int k = 0; k < GROUPS; ++k) { L += sums[k][D]; Le += sums[k][D + 1]; }
     if (LSE && ch == 0) a.lse[(int64_t)(tok0 + q0 + tl) * a.H_q + hq] = row_lse(M, Le, a.scale_log2e);
     const float inv = 1.f / L;

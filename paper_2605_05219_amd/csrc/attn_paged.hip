@@ -172,6 +172,14 @@ int32_t send_image(const std::vector<int32_t>& img, void* dst, hipStream_t strea
     return GDN_OK;
 }
 
+// A plan that fits goes by value, with `words` set from it; any other to the workspace.
+inline int32_t place_plan(const std::vector<int32_t>& img, PlanWords<true>& words, bool& by_value, void* workspace, hipStream_t stream) {
+    by_value = img.size() <= PLAN_WORDS;
+    if (!by_value) return send_image(img, workspace, stream);
+    std::copy(img.begin(), img.end(), words.w);
+    return GDN_OK;
+}
+
 int32_t rope_append(const attn_shape* s, const attn_rope* rope, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v,
                     int64_t ldv, int32_t n_req, const int32_t* cu, const int32_t* pos, const int32_t* start, const attn_pages* pages,
                     void* k_pool, void* v_pool, const int32_t* page_cu, const int32_t* page_ids, void* q_out, void* workspace,
@@ -190,9 +198,10 @@ int32_t rope_append(const attn_shape* s, const attn_rope* rope, const void* q, i
     RopeArgs a;
     for (int p = 0; p < rope->rot / 2; ++p) {
         if (!std::isfinite(rope->freq[p])) return GDN_ERR_SHAPE;
-        long double t = (long double)rope->freq[p] / 6.283185307179586476925286766559005768L;
-        t = (t - floorl(t)) * 18446744073709551616.0L;
-        a.turn[p] = t >= 18446744073709551615.0L ? 0 : (uint64_t)(t + 0.5L);
+        long double t = (long double)rope->freq[p] * 0.159154943091895335768883763372514362L;      // turns: over 2 pi
+        if (!(t >= 0.0L && t < 1.0L)) t -= floorl(t);
+        t = t * 18446744073709551616.0L + 0.5L;
+        a.turn[p] = t >= 18446744073709551616.0L ? 0 : (uint64_t)t;
     }
     if (n_req == 0) return GDN_OK;
     std::vector<int32_t> len;
@@ -229,18 +238,15 @@ int32_t rope_append(const attn_shape* s, const attn_rope* rope, const void* q, i
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(k_pool) || !aligned16(v_pool) || !aligned16(q_out)) return GDN_ERR_ALIGN;
     rc = check_workspace(s, n_req, T, page_cu[n_req], workspace, workspace_bytes);
     if (rc != GDN_OK) return rc;
-    rc = send_image(img, workspace, stream);
+    PlanWords<true> words;
+    bool by_value;
+    rc = place_plan(img, words, by_value, workspace, stream);
     if (rc != GDN_OK) return rc;
-    const int32_t* const d = static_cast<const int32_t*>(workspace);
     a.q = q; a.k = k; a.v = v;
     a.q_out = static_cast<uint16_t*>(q_out);
     a.k_pool = static_cast<uint16_t*>(k_pool);
     a.v_pool = static_cast<uint16_t*>(v_pool);
-    a.cu = d;
-    a.start = d + n_req + 1;
-    a.pos = a.start + n_req;
-    a.place = a.pos + n_req;
-    a.page_ids = a.place + n_req;
+    a.plan = static_cast<const int32_t*>(workspace);
     a.ldq = ldq; a.ldk = ldk; a.ldv = ldv;
     a.page_stride = pages->page_stride;
     a.n_req = n_req;
@@ -253,8 +259,11 @@ int32_t rope_append(const attn_shape* s, const attn_rope* rope, const void* q, i
     a.layout = rope->layout;
     a.amplitude = rope->amplitude;
     const dim3 grid((unsigned)((T + a.tokens - 1) / a.tokens)), block(ROPE_THREADS);
-    if (rope->in_dtype == GDN_F32) hipLaunchKernelGGL((attn_rope_kernel<true>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((attn_rope_kernel<false>), grid, block, 0, stream, a);
+    const bool f32 = rope->in_dtype == GDN_F32;
+    if (by_value && f32) hipLaunchKernelGGL((attn_rope_kernel<true, true>), grid, block, 0, stream, a, words);
+    else if (by_value) hipLaunchKernelGGL((attn_rope_kernel<false, true>), grid, block, 0, stream, a, words);
+    else if (f32) hipLaunchKernelGGL((attn_rope_kernel<true, false>), grid, block, 0, stream, a, PlanWords<false>());
+    else hipLaunchKernelGGL((attn_rope_kernel<false, false>), grid, block, 0, stream, a, PlanWords<false>());
     return hip_err(hipGetLastError());
 }
 
@@ -309,17 +318,24 @@ int32_t paged_prefill(const attn_shape* s, const void* q, const void* gate, int3
     return lse ? launch_paged<true>(s, plan, im, d, nt, a, stream) : launch_paged<false>(s, plan, im, d, nt, a, stream);
 }
 
-template <int D>
-void launch_weights_d(bool few, const WeightArgs& a, unsigned blocks, hipStream_t stream) {
-    if (few) hipLaunchKernelGGL((attn_weights_few_kernel<D>), dim3(blocks), dim3(WGT_THREADS), 0, stream, a);
-    else hipLaunchKernelGGL((attn_weights_kernel<D>), dim3(blocks), dim3(WGT_THREADS), 0, stream, a);
+template <int D, bool BY_VALUE>
+void launch_weights_d(bool few, const WeightArgs& a, const PlanWords<BY_VALUE>& words, unsigned blocks, hipStream_t stream) {
+    if (few) hipLaunchKernelGGL((attn_weights_few_kernel<D, BY_VALUE>), dim3(blocks), dim3(WGT_THREADS), 0, stream, a, words);
+    else hipLaunchKernelGGL((attn_weights_kernel<D, BY_VALUE>), dim3(blocks), dim3(WGT_THREADS), 0, stream, a, words);
 }
-void launch_weights(int d, bool few, const WeightArgs& a, unsigned blocks, hipStream_t stream) {
+template <bool BY_VALUE>
+void launch_weights(int d, bool few, const WeightArgs& a, const PlanWords<BY_VALUE>& words, unsigned blocks, hipStream_t stream) {
     switch (d) {
-        case 64: launch_weights_d<64>(few, a, blocks, stream); break;
-        case 128: launch_weights_d<128>(few, a, blocks, stream); break;
-        default: launch_weights_d<256>(few, a, blocks, stream); break;
+        case 64: launch_weights_d<64>(few, a, words, blocks, stream); break;
+        case 128: launch_weights_d<128>(few, a, words, blocks, stream); break;
+        default: launch_weights_d<256>(few, a, words, blocks, stream); break;
     }
+}
+template <bool BY_VALUE>
+void launch_weights_merge(int d, const WeightArgs& a, const PlanWords<BY_VALUE>& words, unsigned blocks, hipStream_t stream) {
+    const dim3 block((unsigned)wgt_keys(d));
+    if (d == 256) hipLaunchKernelGGL((attn_weights_merge_kernel<wgt_keys(256), BY_VALUE>), dim3(blocks), block, 0, stream, a, words);
+    else hipLaunchKernelGGL((attn_weights_merge_kernel<wgt_keys(128), BY_VALUE>), dim3(blocks), block, 0, stream, a, words);
 }
 
 // The work of one attn_key_weights call: units (a tile of keys and a run of the request's query rows) of either kernel, and the tiles whose rows are cut.
@@ -485,17 +501,19 @@ int32_t key_weights(const attn_shape* s, const void* q, const float* lse, int32_
     std::copy(plan.few.begin(), plan.few.end(), img.begin() + few_at);
     std::copy(plan.merge.begin(), plan.merge.end(), img.begin() + merge_at);
     std::copy(page_ids, page_ids + n_ids, img.begin() + ids_at);
-    rc = send_image(img, workspace, stream);
+    PlanWords<true> words;
+    bool by_value;
+    rc = place_plan(img, words, by_value, workspace, stream);
     if (rc != GDN_OK) return rc;
-    const int32_t* const d = static_cast<const int32_t*>(workspace);
     WeightArgs a;
     a.q = static_cast<const uint16_t*>(q);
     a.lse = lse;
     a.k_pool = static_cast<const uint16_t*>(k_pool);
     a.w_in = w_in;
     a.w_out = w_out;
-    a.page_ids = d + ids_at;
-    a.merge_rec = d + merge_at;
+    a.plan = static_cast<const int32_t*>(workspace);
+    a.merges = (int32_t)merge_at;
+    a.ids = (int32_t)ids_at;
     a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + image_bytes(s, n_req, T, n_ids));
     a.page_stride = pages->page_stride;
     a.w_stride = w_stride;
@@ -504,23 +522,30 @@ int32_t key_weights(const attn_shape* s, const void* q, const float* lse, int32_
     a.inv_G = 1.f / (float)G;
     a.scale_log2e = s->scale * 1.4426950408889634f;
     a.decay = decay;
-    if (n_few > 0) {
-        a.unit_rec = d + few_at;
-        launch_weights(s->d, true, a, (unsigned)(n_few * s->H_kv), stream);
-        rc = hip_err(hipGetLastError());
-        if (rc != GDN_OK) return rc;
-    }
-    if (n_wide > 0) {
-        a.unit_rec = d;
-        launch_weights(s->d, false, a, (unsigned)(n_wide * s->H_kv), stream);
-        rc = hip_err(hipGetLastError());
-        if (rc != GDN_OK) return rc;
-    }
-    if (n_cut == 0) return GDN_OK;
-    const dim3 grid((unsigned)(n_cut * s->H_kv)), block((unsigned)wgt_keys(s->d));
-    if (s->d == 256) hipLaunchKernelGGL((attn_weights_merge_kernel<wgt_keys(256)>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((attn_weights_merge_kernel<wgt_keys(128)>), grid, block, 0, stream, a);
-    return hip_err(hipGetLastError());
+    auto launch = [&](const auto& words) {
+        hipError_t e = hipSuccess;
+        if (n_few > 0) {
+            a.units = (int32_t)few_at;
+            launch_weights(s->d, true, a, words, (unsigned)(n_few * s->H_kv), stream);
+            e = hipGetLastError();
+        }
+        if (e == hipSuccess && n_wide > 0) {
+            a.units = 0;
+            launch_weights(s->d, false, a, words, (unsigned)(n_wide * s->H_kv), stream);
+            e = hipGetLastError();
+        }
+        if (e == hipSuccess && n_cut > 0) {
+            launch_weights_merge(s->d, a, words, (unsigned)(n_cut * s->H_kv), stream);
+            e = hipGetLastError();
+        }
+        return hip_err(e);
+    };
+    return by_value ? launch(words) : launch(PlanWords<false>());
+}
+
+template <int D, bool BY_VALUE>
+void launch_gather(const EvictArgs& a, const PlanWords<BY_VALUE>& words, unsigned blocks, hipStream_t stream) {
+    hipLaunchKernelGGL((attn_gather_rows_kernel<D, BY_VALUE>), dim3(blocks), dim3(GATHER_THREADS), 0, stream, a, words);
 }
 
 int32_t evict(const attn_shape* s, int32_t n_req, const int32_t* rows, const int32_t* keep, const int32_t* first, const int32_t* recent,
@@ -574,39 +599,35 @@ int32_t evict(const attn_shape* s, int32_t n_req, const int32_t* rows, const int
     const int64_t blocks = (int64_t)p[-1] * s->H_kv;
     p = std::copy(page_ids, page_ids + n_old, p);
     p = std::copy(new_page_ids, new_page_ids + n_new, p);
-    rc = send_image(img, workspace, stream);
+    if (blocks > INT32_MAX || (int64_t)n_req * s->H_kv > INT32_MAX) return GDN_ERR_COUNT;
+    PlanWords<true> words;
+    bool by_value;
+    rc = place_plan(img, words, by_value, workspace, stream);
     if (rc != GDN_OK) return rc;
-    const int32_t* const d = static_cast<const int32_t*>(workspace);
     EvictArgs a;
     a.k_pool = static_cast<uint16_t*>(k_pool);
     a.v_pool = static_cast<uint16_t*>(v_pool);
     a.w_pool = w_pool;
     a.index = index;
-    a.rows = d;
-    a.keep = d + n_req;
-    a.first = d + 2 * (int64_t)n_req;
-    a.recent = d + 3 * (int64_t)n_req;
-    a.place = d + 4 * (int64_t)n_req;
-    a.new_place = d + 5 * (int64_t)n_req;
-    a.keep_cu = d + 6 * (int64_t)n_req;
-    a.block_cu = d + 7 * (int64_t)n_req + 1;
-    a.page_ids = d + 8 * (int64_t)n_req + 2;
+    a.plan = static_cast<const int32_t*>(workspace);
     a.page_stride = pages->page_stride;
     a.w_stride = w_stride;
     a.n_req = n_req;
     a.H_kv = s->H_kv;
     a.page_shift = shift_of(pages);
-    if (blocks > INT32_MAX || (int64_t)n_req * s->H_kv > INT32_MAX) return GDN_ERR_COUNT;
-    hipLaunchKernelGGL(attn_select_kernel, dim3((unsigned)(n_req * s->H_kv)), dim3(SEL_THREADS), 0, stream, a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return hip_err(e);
-    const dim3 grid((unsigned)blocks), block(GATHER_THREADS);
-    switch (s->d) {
-        case 64: hipLaunchKernelGGL((attn_gather_rows_kernel<64>), grid, block, 0, stream, a); break;
-        case 128: hipLaunchKernelGGL((attn_gather_rows_kernel<128>), grid, block, 0, stream, a); break;
-        default: hipLaunchKernelGGL((attn_gather_rows_kernel<256>), grid, block, 0, stream, a); break;
-    }
-    return hip_err(hipGetLastError());
+    auto launch = [&](const auto& words) {
+        constexpr bool BY_VALUE = std::is_same<std::decay_t<decltype(words)>, PlanWords<true>>::value;
+        hipLaunchKernelGGL((attn_select_kernel<BY_VALUE>), dim3((unsigned)(n_req * s->H_kv)), dim3(SEL_THREADS), 0, stream, a, words);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return hip_err(e);
+        switch (s->d) {
+            case 64: launch_gather<64>(a, words, (unsigned)blocks, stream); break;
+            case 128: launch_gather<128>(a, words, (unsigned)blocks, stream); break;
+            default: launch_gather<256>(a, words, (unsigned)blocks, stream); break;
+        }
+        return hip_err(hipGetLastError());
+    };
+    return by_value ? launch(words) : launch(PlanWords<false>());
 }
 
 // No exception leaves a C entry: host memory that runs out is a count too large.

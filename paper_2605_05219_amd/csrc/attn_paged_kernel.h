@@ -8,6 +8,14 @@
 
 namespace attn {
 
+// A call's index arrays ("plan"): in device memory, or by value in the arguments of its launches where they are few words, which spares the
+// launch that would write them there.
+constexpr int PLAN_WORDS = 640;
+template <bool BY_VALUE>
+struct PlanWords {
+    int32_t w[BY_VALUE ? PLAN_WORDS : 1];
+};
+
 // The request with cu[r] <= t < cu[r + 1], for a wave: 64 of the ends at a time, one in each lane.
 __device__ __forceinline__ int request_of(const int32_t* cu, int n_req, int t) {
     const int lane = threadIdx.x & 63;
@@ -30,7 +38,7 @@ struct RopeArgs {
     const void *q, *k, *v;
     uint16_t* q_out;
     uint16_t *k_pool, *v_pool;
-    const int32_t *cu, *start, *pos, *place, *page_ids;   // place: where the page of row 0 would be listed
+    const int32_t* plan;              // cu (n_req + 1), start, pos, place (n_req each: where the page of row 0 would be listed), page ids
     int64_t ldq, ldk, ldv, page_stride;
     int32_t n_req, T, tokens;         // tokens: per workgroup
     int32_t H_q, H_kv, units;         // units: pieces of 16 elements per head, d / 16
@@ -70,8 +78,8 @@ __device__ __forceinline__ void store8_fp16(uint16_t* p, const float* x) {
 
 // One workgroup takes `tokens` tokens: their cosines and sines once, to LDS, for all heads; then one thread per 16 elements of a
 // head (two runs of 8 where a pair's halves lie apart).
-template <bool F32>
-__global__ void __launch_bounds__(ROPE_THREADS) attn_rope_kernel(RopeArgs a) {
+template <bool F32, bool BY_VALUE>
+__global__ void __launch_bounds__(ROPE_THREADS) attn_rope_kernel(RopeArgs a, PlanWords<BY_VALUE> words) {
     __shared__ float cs[ROPE_TOKENS][2][128];
     __shared__ int64_t row_at[ROPE_TOKENS];      // the token's row in the pools, head 0
     __shared__ int32_t position[ROPE_TOKENS];
@@ -79,12 +87,14 @@ __global__ void __launch_bounds__(ROPE_THREADS) attn_rope_kernel(RopeArgs a) {
     const int n_tok = min(a.tokens, a.T - tok0);
     const int wave = threadIdx.x >> 6;
     const int D = 16 * a.units;
+    const int32_t* const cu = BY_VALUE ? words.w : a.plan;
+    const int32_t *const start = cu + a.n_req + 1, *const pos = start + a.n_req, *const place = pos + a.n_req, *const page_ids = place + a.n_req;
     for (int i = wave; i < n_tok; i += ROPE_THREADS / 64) {
-        const int t = tok0 + i, r = request_of(a.cu, a.n_req, t);
+        const int t = tok0 + i, r = request_of(cu, a.n_req, t);
         if ((threadIdx.x & 63) == 0) {
-            const int in = t - a.cu[r], row = a.start[r] + in;
-            position[i] = a.pos[r] + in;
-            row_at[i] = (int64_t)a.page_ids[a.place[r] + (row >> a.page_shift)] * a.page_stride + (int64_t)(row & ((1 << a.page_shift) - 1)) * D;
+            const int in = t - cu[r], row = start[r] + in;
+            position[i] = pos[r] + in;
+            row_at[i] = (int64_t)page_ids[place[r] + (row >> a.page_shift)] * a.page_stride + (int64_t)(row & ((1 << a.page_shift) - 1)) * D;
         }
     }
     __syncthreads();
@@ -169,9 +179,8 @@ struct WeightArgs {
     const uint16_t* k_pool;
     const float* w_in;        // or nullptr
     float* w_out;
-    const int32_t* page_ids;
-    const int32_t* unit_rec;  // WGT_REC ints per unit
-    const int32_t* merge_rec; // WGT_MERGE ints per tile whose rows are cut, and the first partial sum behind the last one
+    const int32_t* plan;      // WGT_REC ints per unit of either kernel, WGT_MERGE per tile whose rows are cut (and the first partial sum behind the last one), page ids
+    int32_t units, merges, ids;   // where each begins (units: of the kernel launched)
     float* part;              // [partial sum][head][keys of a tile]
     int64_t page_stride, w_stride;
     int32_t H_q, H_kv, G;
@@ -187,13 +196,13 @@ struct WeightSmem {
     static __device__ __forceinline__ int f(int row) { return CPR >= 16 ? (row & 15) : ((row >> 1) & 7); }
 };
 
-__device__ __forceinline__ void store_weight(const WeightArgs& a, int place, int kvh, int c0, int key, float sum) {
-    const int64_t at = (int64_t)a.page_ids[place + (key >> a.page_shift)] * a.w_stride + ((int64_t)kvh << a.page_shift) + (key & ((1 << a.page_shift) - 1));
+__device__ __forceinline__ void store_weight(const WeightArgs& a, const int32_t* page_ids, int place, int kvh, int c0, int key, float sum) {
+    const int64_t at = (int64_t)page_ids[place + (key >> a.page_shift)] * a.w_stride + ((int64_t)kvh << a.page_shift) + (key & ((1 << a.page_shift) - 1));
     a.w_out[at] = (a.w_in && key < c0 ? a.decay * a.w_in[at] : 0.f) + sum;
 }
 
-template <int D>
-__global__ void __launch_bounds__(WGT_THREADS, 2) attn_weights_kernel(WeightArgs a) {
+template <int D, bool BY_VALUE>
+__global__ void __launch_bounds__(WGT_THREADS, 2) attn_weights_kernel(WeightArgs a, PlanWords<BY_VALUE> words) {
     typedef WeightSmem<D> SM;
     constexpr int KB = D / 16, KEYS = wgt_keys(D), NB = KEYS / 128;      // NB: blocks of 32 keys per wave
     constexpr int AHEAD_TILES = D == 256 ? 1 : 2;    // a tile is asked for this many tiles ahead (three stages at d = 256 would leave one workgroup to a compute unit)
@@ -205,7 +214,8 @@ __global__ void __launch_bounds__(WGT_THREADS, 2) attn_weights_kernel(WeightArgs
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, g = lane >> 5;
     const int kvh = (int)blockIdx.x % a.H_kv;
-    const int32_t* const rec = a.unit_rec + (int64_t)((int)blockIdx.x / a.H_kv) * WGT_REC;
+    const int32_t *const plan = BY_VALUE ? words.w : a.plan, *const page_ids = plan + a.ids;
+    const int32_t* const rec = plan + a.units + (int64_t)((int)blockIdx.x / a.H_kv) * WGT_REC;
     const int tok0 = rec[0], n = rec[1], c0 = rec[2], place = rec[3], kv0 = rec[4], row_lo = rec[5], row_hi = rec[6], part = rec[7];
     const int kv_len = c0 + n;
 
@@ -213,7 +223,7 @@ __global__ void __launch_bounds__(WGT_THREADS, 2) attn_weights_kernel(WeightArgs
     const int key0 = kv0 + 32 * NB * wave;
     int page[NB];
 #pragma unroll
-    for (int b = 0; b < NB; ++b) page[b] = a.page_ids[place + (min(key0 + 32 * b + col, kv_len - 1) >> a.page_shift)];
+    for (int b = 0; b < NB; ++b) page[b] = page_ids[place + (min(key0 + 32 * b + col, kv_len - 1) >> a.page_shift)];
 
     // ---- the next tile to bring: its first row, that row's token and head (uniform; a tile is step_t tokens and step_h heads on)
     const int step_t = WGT_ROWS / a.G, step_h = WGT_ROWS - step_t * a.G;
@@ -390,7 +400,7 @@ __global__ void __launch_bounds__(WGT_THREADS, 2) attn_weights_kernel(WeightArgs
         const float sum = sum_with_other_half(acc[b]);
         const int key = key0 + 32 * b + col;
         if (g != 0 || key >= kv_len) continue;
-        if (part < 0) store_weight(a, place, kvh, c0, key, sum);
+        if (part < 0) store_weight(a, page_ids, place, kvh, c0, key, sum);
         else a.part[((int64_t)part * a.H_kv + kvh) * KEYS + key - kv0] = sum;
     }
 }
@@ -398,14 +408,15 @@ __global__ void __launch_bounds__(WGT_THREADS, 2) attn_weights_kernel(WeightArgs
 // The same for requests of at most 16 rows (decoding): bound by the keys' bytes, so that nothing is shared between waves and none waits for
 // another.  A wave holds 64 keys as four blocks of columns of 16x16x32 products, 64 contiguous bytes of a key per load and lane group, all of them in
 // flight at once, four workgroups to a compute unit; the query rows come straight from memory.
-template <int D>
-__global__ void __launch_bounds__(WGT_THREADS, D == 256 ? 2 : 4) attn_weights_few_kernel(WeightArgs a) {
+template <int D, bool BY_VALUE>
+__global__ void __launch_bounds__(WGT_THREADS, D == 256 ? 2 : 4) attn_weights_few_kernel(WeightArgs a, PlanWords<BY_VALUE> words) {
     constexpr int KS = D / 32, NB = wgt_keys(D) / 64;       // NB: blocks of 16 keys per wave
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i16 = lane & 15, g = lane >> 4;
     const int kvh = (int)blockIdx.x % a.H_kv;
-    const int32_t* const rec = a.unit_rec + (int64_t)((int)blockIdx.x / a.H_kv) * WGT_REC;
+    const int32_t *const plan = BY_VALUE ? words.w : a.plan, *const page_ids = plan + a.ids;
+    const int32_t* const rec = plan + a.units + (int64_t)((int)blockIdx.x / a.H_kv) * WGT_REC;
     const int tok0 = rec[0], n = rec[1], c0 = rec[2], place = rec[3], rows = rec[6];
     const int kv_len = c0 + n, key0 = rec[4] + 16 * NB * wave;
     if (key0 >= kv_len) return;
@@ -414,7 +425,7 @@ __global__ void __launch_bounds__(WGT_THREADS, D == 256 ? 2 : 4) attn_weights_fe
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
         const int key = min(key0 + 16 * b + i16, kv_len - 1);
-        const uint16_t* const kp = a.k_pool + (int64_t)a.page_ids[place + (key >> a.page_shift)] * a.page_stride + ((int64_t)kvh * D << a.page_shift) +
+        const uint16_t* const kp = a.k_pool + (int64_t)page_ids[place + (key >> a.page_shift)] * a.page_stride + ((int64_t)kvh * D << a.page_shift) +
                                    (int64_t)(key & mask) * D + 8 * g;
 #pragma unroll
         for (int s = 0; s < KS; ++s) kf[b][s] = *reinterpret_cast<const u32x4*>(kp + 32 * s);
@@ -425,7 +436,7 @@ __global__ void __launch_bounds__(WGT_THREADS, D == 256 ? 2 : 4) attn_weights_fe
     int64_t at = 0;
     float held = 0.f;
     if (stores) {
-        at = (int64_t)a.page_ids[place + (mine >> a.page_shift)] * a.w_stride + ((int64_t)kvh << a.page_shift) + (mine & mask);
+        at = (int64_t)page_ids[place + (mine >> a.page_shift)] * a.w_stride + ((int64_t)kvh << a.page_shift) + (mine & mask);
         if (a.w_in && mine < c0) held = a.w_in[at];
     }
     // query rows: operand A, row i16, d = 32 s + 8 g + {0..7};  the sums: rows 4 g + e
@@ -463,17 +474,18 @@ __global__ void __launch_bounds__(WGT_THREADS, D == 256 ? 2 : 4) attn_weights_fe
 }
 
 // The parts of a tile's rows, summed in order; one workgroup per (tile, head) and one thread per key.
-template <int KEYS>
-__global__ void __launch_bounds__(KEYS) attn_weights_merge_kernel(WeightArgs a) {
+template <int KEYS, bool BY_VALUE>
+__global__ void __launch_bounds__(KEYS) attn_weights_merge_kernel(WeightArgs a, PlanWords<BY_VALUE> words) {
     const int kvh = (int)blockIdx.x % a.H_kv;
-    const int32_t* const rec = a.merge_rec + (int64_t)((int)blockIdx.x / a.H_kv) * WGT_MERGE;
+    const int32_t *const plan = BY_VALUE ? words.w : a.plan, *const page_ids = plan + a.ids;
+    const int32_t* const rec = plan + a.merges + (int64_t)((int)blockIdx.x / a.H_kv) * WGT_MERGE;
     const int kv_len = rec[0], c0 = rec[1], place = rec[2], kv0 = rec[3], p0 = rec[4], p1 = rec[WGT_MERGE + 4];
     const int key = kv0 + (int)threadIdx.x;
     if (key >= kv_len) return;
     float sum = 0.f;
 #pragma unroll 8
     for (int p = p0; p < p1; ++p) sum += a.part[((int64_t)p * a.H_kv + kvh) * KEYS + threadIdx.x];
-    store_weight(a, place, kvh, c0, key, sum);
+    store_weight(a, page_ids, place, kvh, c0, key, sum);
 }
 
 // ---------------------------------------------------------------- eviction
@@ -481,11 +493,20 @@ struct EvictArgs {
     uint16_t *k_pool, *v_pool;
     float* w_pool;
     int32_t* index;
-    const int32_t *rows, *keep, *first, *recent;          // keep: at most rows
-    const int32_t *place, *new_place, *keep_cu, *page_ids;   // page_ids: old and new ones; keep_cu: kept rows before each request
-    const int32_t* block_cu;                              // n_req + 1: workgroups of the copy, for one head, before each request
+    const int32_t* plan;
     int64_t page_stride, w_stride;
     int32_t n_req, H_kv, page_shift;
+};
+
+// The arrays of an eviction's plan.
+struct EvictPlan {
+    const int32_t *rows, *keep, *first, *recent;          // keep: at most rows
+    const int32_t *place, *new_place;                     // where a request's old and new pages begin in page_ids
+    const int32_t *keep_cu, *block_cu;                    // n_req + 1: kept rows, and workgroups of the copy for one head, before each request
+    const int32_t* page_ids;
+    __host__ __device__ EvictPlan(const int32_t* p, int64_t n)
+        : rows(p), keep(p + n), first(p + 2 * n), recent(p + 3 * n), place(p + 4 * n), new_place(p + 5 * n), keep_cu(p + 6 * n),
+          block_cu(p + 7 * n + 1), page_ids(p + 8 * n + 2) {}
 };
 
 // A weight's rank as an unsigned number: larger weights larger, -0 as +0, what is not a number 0.
@@ -505,26 +526,28 @@ constexpr int SEL_THREADS = 1024;
 constexpr int SEL_HELD = 32768;
 constexpr int SEL_BITS = 11;
 
-__global__ void __launch_bounds__(SEL_THREADS) attn_select_kernel(EvictArgs a) {
+template <bool BY_VALUE>
+__global__ void __launch_bounds__(SEL_THREADS) attn_select_kernel(EvictArgs a, PlanWords<BY_VALUE> words) {
     constexpr int WAVES = SEL_THREADS / 64, BINS = 1 << SEL_BITS, LOADS = 8;
     __shared__ uint32_t held[SEL_HELD];
     __shared__ int hist[BINS];
     __shared__ uint32_t wave_least[WAVES], wave_most[WAVES];
     __shared__ int wave_a[WAVES], wave_b[WAVES], found[2];
+    const EvictPlan e(BY_VALUE ? words.w : a.plan, a.n_req);
     const int r = (int)blockIdx.x / a.H_kv, kvh = (int)blockIdx.x % a.H_kv;
-    const int rows = a.rows[r], keep = a.keep[r], first = a.first[r], last = rows - a.recent[r];
+    const int rows = e.rows[r], keep = e.keep[r], first = e.first[r], last = rows - e.recent[r];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    int32_t* const out = a.index + (int64_t)a.H_kv * a.keep_cu[r] + (int64_t)kvh * keep;
+    int32_t* const out = a.index + (int64_t)a.H_kv * e.keep_cu[r] + (int64_t)kvh * keep;
     if (keep == rows) {
         for (int j = tid; j < rows; j += SEL_THREADS) out[j] = j;
         return;
     }
-    const int32_t* const ids = a.page_ids + a.place[r];
+    const int32_t* const ids = e.page_ids + e.place[r];
     const float* const w = a.w_pool + ((int64_t)kvh << a.page_shift);
     const int mask = (1 << a.page_shift) - 1;
     auto rank_of = [&](int j) { return weight_rank(w[(int64_t)ids[j >> a.page_shift] * a.w_stride + (j & mask)]); };
     auto rank = [&](int j) { return j < SEL_HELD ? held[j] : rank_of(j); };
-    const int want = keep - first - a.recent[r];          // rows to take from [first, last), fewer than there are
+    const int want = keep - first - e.recent[r];          // rows to take from [first, last), fewer than there are
     uint32_t edge = 0xffffffffu;                          // the smallest rank kept
     int left = 0;                                         // how many rows of it
     if (want > 0) {
@@ -595,7 +618,6 @@ __global__ void __launch_bounds__(SEL_THREADS) attn_select_kernel(EvictArgs a) {
         tie = middle && x == edge;
     };
     int taken = 0, ties = 0;
-#pragma unroll 4
     for (int j = j_lo; j < j_hi; j += 64) {
         bool take, tie;
         look(j + lane, take, tie);
@@ -613,7 +635,6 @@ __global__ void __launch_bounds__(SEL_THREADS) attn_select_kernel(EvictArgs a) {
         tie_at += i < wave ? m : 0;
     }
     at += min(tie_at, left);
-#pragma unroll 4
     for (int j = j_lo; j < j_hi; j += 64) {
         bool take, tie;
         look(j + lane, take, tie);
@@ -631,15 +652,16 @@ __global__ void __launch_bounds__(SEL_THREADS) attn_select_kernel(EvictArgs a) {
 constexpr int GATHER_THREADS = 256, GATHER_PASSES = 4;
 __host__ __device__ constexpr int gather_rows(int d) { return GATHER_THREADS / (d / 8) * GATHER_PASSES; }
 
-template <int D>
-__global__ void __launch_bounds__(GATHER_THREADS) attn_gather_rows_kernel(EvictArgs a) {
+template <int D, bool BY_VALUE>
+__global__ void __launch_bounds__(GATHER_THREADS) attn_gather_rows_kernel(EvictArgs a, PlanWords<BY_VALUE> words) {
     constexpr int CPR = D / 8, STEP = GATHER_THREADS / CPR;
+    const EvictPlan e(BY_VALUE ? words.w : a.plan, a.n_req);
     const int kvh = (int)blockIdx.x % a.H_kv, block = (int)blockIdx.x / a.H_kv;
-    const int r = __builtin_amdgcn_readfirstlane(request_of(a.block_cu, a.n_req, block));
-    const int keep = a.keep[r], mask = (1 << a.page_shift) - 1;
-    const int32_t* const index = a.index + (int64_t)a.H_kv * a.keep_cu[r] + (int64_t)kvh * keep;
-    const int32_t *const ids = a.page_ids + a.place[r], *const new_ids = a.page_ids + a.new_place[r];
-    const int to0 = (block - a.block_cu[r]) * gather_rows(D) + (int)threadIdx.x / CPR, c = (int)threadIdx.x % CPR;
+    const int r = __builtin_amdgcn_readfirstlane(request_of(e.block_cu, a.n_req, block));
+    const int keep = e.keep[r], mask = (1 << a.page_shift) - 1;
+    const int32_t* const index = a.index + (int64_t)a.H_kv * e.keep_cu[r] + (int64_t)kvh * keep;
+    const int32_t *const ids = e.page_ids + e.place[r], *const new_ids = e.page_ids + e.new_place[r];
+    const int to0 = (block - e.block_cu[r]) * gather_rows(D) + (int)threadIdx.x / CPR, c = (int)threadIdx.x % CPR;
     const int64_t head = (int64_t)kvh << a.page_shift;
     int from[GATHER_PASSES];
     int64_t old_page[GATHER_PASSES], new_page[GATHER_PASSES];

@@ -9,7 +9,8 @@ import ctypes
 import numpy as np
 
 from .attention import attn_shape
-from .binding import GDN_BF16, GDN_F32, GdnError, _check, _dp, _h32, _hp, _stream_ptr, lib
+from .binding import GDN_BF16, GDN_F32, GdnError, _check, _dp, _h32, _hp, lib
+from .binding import _stream_ptr as _stream_object_ptr
 
 _i32, _i64, _vp, _f32, _f64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_float, ctypes.c_double
 
@@ -32,6 +33,13 @@ def make_attn_rope(freqs, layout="half", amplitude=1.0, in_dtype="bf16") -> attn
     rope = attn_rope(2 * f.size, {"half": 0, "interleaved": 1}[layout], code[in_dtype], float(amplitude), f.ctypes.data if f.size else None)
     rope._freqs = f
     return rope
+
+
+def _stream_ptr(stream=None):
+    """The given stream's handle, or the current one's without an object made for it (3 us a call)."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return _vp(raw(torch.cuda.current_device())) if stream is None and raw is not None else _stream_object_ptr(stream)
 
 
 _ints = ctypes.c_int32 * 0
