@@ -516,23 +516,37 @@ __device__ __forceinline__ uint32_t weight_rank(float w) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// The rows that one (request, head) keeps, by one workgroup.  The ranks come to LDS in one pass over the weights (those of rows behind SEL_HELD are read
-// again where they are needed) and give their least and greatest; rounds over 11 bits at a time, from the highest bit in which those differ, find
-// the smallest rank kept and how many rows of just that rank are.  Each wave then counts a run of rows of its own and writes the
-// numbers of those kept behind the waves before it.
-// Bound: latencies (a chain of dependent steps, one compute unit per head); digits of 11 bits from the highest differing one spread the weights over many
-// counters, where a byte of the exponent would put most of them on a few.  30000 rows 91 us with four rounds of 8 bits over memory.
+// Sum over this lane and those before it, by lane exchanges inside the vector unit (within rows of 16, then a row's last lane to the next rows).
+__device__ __forceinline__ int wave_sum_upto(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);    // 1, 2, 4, 8 lanes down the row
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // last lane of rows 0, 2 to rows 1, 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // last lane of row 1 to rows 2, 3
+    return x;
+}
+
+// The rows that one (request, head) keeps, by one workgroup.  Of every 8192 rows a thread has eight, 1024 apart; the ranks of the first SEL_HELD blocks of
+// 8192 stay in registers, those behind them are read again where they are needed.  One pass counts the ranks' highest 11 bits; the digit in
+// which the smallest rank kept lies leaves few rows as a rule, one to a thread from there on; the next 11 bits are counted until one row or all bits are
+// left.  The counts of every 64 rows, summed, then say where each one's rows go.
+// Bound: latencies, and the instructions of one compute unit per head (four copies of the counters, because neighbouring weights share their
+// highest bits).
 constexpr int SEL_THREADS = 1024;
-constexpr int SEL_HELD = 32768;
+constexpr int SEL_OWN = 8;             // rows of a thread in a block
+constexpr int SEL_HELD = 4;
 constexpr int SEL_BITS = 11;
+constexpr int SEL_COPIES = 4;
 
 template <bool BY_VALUE>
 __global__ void __launch_bounds__(SEL_THREADS) attn_select_kernel(EvictArgs a, PlanWords<BY_VALUE> words) {
-    constexpr int WAVES = SEL_THREADS / 64, BINS = 1 << SEL_BITS, LOADS = 8;
-    __shared__ uint32_t held[SEL_HELD];
-    __shared__ int hist[BINS];
-    __shared__ uint32_t wave_least[WAVES], wave_most[WAVES];
-    __shared__ int wave_a[WAVES], wave_b[WAVES], found[2];
+    constexpr int WAVES = SEL_THREADS / 64, BINS = 1 << SEL_BITS, BLOCK = SEL_THREADS * SEL_OWN;
+    static_assert(BINS == 2 * SEL_THREADS && SEL_COPIES == 4, "a thread sums two digits, four copies in one read each");
+    __shared__ __attribute__((aligned(16))) int hist[BINS * SEL_COPIES];
+    __shared__ uint32_t few[SEL_THREADS];
+    __shared__ __attribute__((aligned(16))) int part[2][SEL_OWN * WAVES];
+    __shared__ int wave_a[WAVES], found[3], n_few;
     const EvictPlan e(BY_VALUE ? words.w : a.plan, a.n_req);
     const int r = (int)blockIdx.x / a.H_kv, kvh = (int)blockIdx.x % a.H_kv;
     const int rows = e.rows[r], keep = e.keep[r], first = e.first[r], last = rows - e.recent[r];
@@ -545,53 +559,73 @@ __global__ void __launch_bounds__(SEL_THREADS) attn_select_kernel(EvictArgs a, P
     const int32_t* const ids = e.page_ids + e.place[r];
     const float* const w = a.w_pool + ((int64_t)kvh << a.page_shift);
     const int mask = (1 << a.page_shift) - 1;
-    auto rank_of = [&](int j) { return weight_rank(w[(int64_t)ids[j >> a.page_shift] * a.w_stride + (j & mask)]); };
-    auto rank = [&](int j) { return j < SEL_HELD ? held[j] : rank_of(j); };
     const int want = keep - first - e.recent[r];          // rows to take from [first, last), fewer than there are
+    auto load = [&](int base, uint32_t (&x)[SEL_OWN]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < SEL_OWN; ++i) {
+            const int j = min(base + SEL_THREADS * i + tid, rows - 1);
+            x[i] = weight_rank(w[(int64_t)ids[j >> a.page_shift] * a.w_stride + (j & mask)]);
+        }
+    };
+    uint32_t held[SEL_HELD][SEL_OWN] = {};
+    // f(number, ranks) of every block of rows
+    auto each_block = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int b = 0; b < SEL_HELD; ++b)
+            if (b * BLOCK < rows) f(b, held[b]);
+#pragma unroll 1
+        for (int b = SEL_HELD; b < (rows - 1) / BLOCK + 1; ++b) {
+            uint32_t x[SEL_OWN];
+            load(b * BLOCK, x);
+            f(b, x);
+        }
+    };
+    // f(rank) of this thread's rows in [first, last)
+    auto each_row = [&](auto f) __attribute__((always_inline)) {
+        each_block([&](int b, const uint32_t (&x)[SEL_OWN]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < SEL_OWN; ++i) {
+                const int j = b * BLOCK + SEL_THREADS * i + tid;
+                if (j >= first && j < last) f(x[i]);
+            }
+        });
+    };
     uint32_t edge = 0xffffffffu;                          // the smallest rank kept
     int left = 0;                                         // how many rows of it
     if (want > 0) {
-        uint32_t least = 0xffffffffu, most = 0u;
-        for (int j0 = first + tid; j0 < last; j0 += LOADS * SEL_THREADS) {
-            uint32_t x[LOADS];
+        auto clear = [&](int digits) __attribute__((always_inline)) {
+            for (int i = tid; i < digits; i += SEL_THREADS) *reinterpret_cast<u32x4*>(&hist[SEL_COPIES * i]) = u32x4{0u, 0u, 0u, 0u};
+        };
+        clear(BINS);
+        if (tid == 0) n_few = 0;
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) x[i] = rank_of(min(j0 + i * SEL_THREADS, last - 1));
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int j = j0 + i * SEL_THREADS;
-                if (j < last && j < SEL_HELD) held[j] = x[i];
-                least = min(least, x[i]);
-                most = max(most, x[i]);
-            }
-        }
-        for (int d = 32; d > 0; d >>= 1) {
-            least = min(least, (uint32_t)__shfl_xor((int)least, d));
-            most = max(most, (uint32_t)__shfl_xor((int)most, d));
-        }
-        if (lane == 0) { wave_least[wave] = least; wave_most[wave] = most; }
+        for (int b = 0; b < SEL_HELD; ++b)
+            if (b * BLOCK < rows) load(b * BLOCK, held[b]);
         __syncthreads();
-        for (int i = 0; i < WAVES; ++i) { least = min(least, wave_least[i]); most = max(most, wave_most[i]); }
-        edge = most;
+        int bits = 32;                                    // bits of the edge that are not known yet
+        bool one_each = false;                            // the rows that agree in the others are few: thread t has one, if t < count
+        uint32_t mine = 0;
+        int count = 0;
         left = want;
-        int bits = 32 - __clz((int)(least ^ most));       // __clz(0) is 32: all ranks are one
-        edge = bits < 32 ? edge >> bits << bits : 0u;     // the bits that all have
+        edge = 0u;
         while (bits > 0) {
-            const int shift = max(0, bits - SEL_BITS), digits = 1 << (bits - shift);
-            for (int i = tid; i < digits; i += SEL_THREADS) hist[i] = 0;
-            __syncthreads();
-#pragma unroll 4
-            for (int j = first + tid; j < last; j += SEL_THREADS) {
-                const uint32_t x = rank(j);
-                if (bits == 32 || x >> bits == edge >> bits) atomicAdd(&hist[(x >> shift) & (digits - 1)], 1);
+            const int shift = max(0, bits - SEL_BITS), digits = bits == 32 ? BINS : 1 << (bits - shift);
+            auto add = [&](uint32_t x) __attribute__((always_inline)) {
+                atomicAdd(&hist[SEL_COPIES * ((x >> shift) & (digits - 1)) + (lane & (SEL_COPIES - 1))], 1);
+            };
+            if (one_each) {
+                if (tid < count) add(mine);
+            } else {
+                each_row([&](uint32_t x) __attribute__((always_inline)) {
+                    if (bits == 32 || x >> bits == edge >> bits) add(x);
+                });
             }
+            bits = shift;
             __syncthreads();
-            // from the largest digit down: thread t has digits digits - 1 - 2 t and the one below
-            const int d0 = digits - 1 - 2 * tid, n0 = d0 >= 0 ? hist[d0] : 0, n1 = d0 >= 1 ? hist[d0 - 1] : 0;
-            int upto = n0 + n1;
-            for (int d = 1; d < 64; d <<= 1) {
-                const int up = __shfl_up(upto, d);
-                if (lane >= d) upto += up;
-            }
+            // from the largest digit down: thread t has digits - 1 - 2 t and the one below
+            auto count_of = [&](int d) { const u32x4 n = *reinterpret_cast<const u32x4*>(&hist[SEL_COPIES * d]); return (int)((n[0] + n[1]) + (n[2] + n[3])); };
+            const int d0 = digits - 1 - 2 * tid, n0 = d0 >= 0 ? count_of(d0) : 0, n1 = d0 >= 1 ? count_of(d0 - 1) : 0;
+            const int upto = wave_sum_upto(n0 + n1);
             if (lane == 63) wave_a[wave] = upto;
             __syncthreads();
             int before = upto - n0 - n1;
@@ -600,51 +634,66 @@ __global__ void __launch_bounds__(SEL_THREADS) attn_select_kernel(EvictArgs a, P
                 const int n = wave_a[i];                  // (all of them, whichever wave: the reads do not wait for each other)
                 before += i < wave ? n : 0;
             }
-            if (before < left && before + n0 >= left) { found[0] = d0; found[1] = left - before; }
-            else if (before + n0 < left && before + n0 + n1 >= left) { found[0] = d0 - 1; found[1] = left - before - n0; }
+            if (before < left && before + n0 >= left) { found[0] = d0; found[1] = left - before; found[2] = n0; }
+            else if (before + n0 < left && before + n0 + n1 >= left) { found[0] = d0 - 1; found[1] = left - before - n0; found[2] = n1; }
+            if (bits > 0) clear(1 << (bits - max(0, bits - SEL_BITS)));      // (everybody's digits have been read)
             __syncthreads();
-            edge |= (uint32_t)found[0] << shift;
+            edge |= (uint32_t)found[0] << bits;
             left = found[1];
-            bits = shift;
+            if (bits == 0) break;
+            const bool was = one_each;
+            one_each = found[2] <= SEL_THREADS;
+            if (one_each && !was) {                       // a row to a thread from here on
+                count = found[2];
+                each_row([&](uint32_t x) __attribute__((always_inline)) {
+                    if (x >> bits == edge >> bits) few[atomicAdd(&n_few, 1)] = x;
+                });
+                __syncthreads();
+                mine = tid < count ? few[tid] : 0u;
+            } else if (one_each && found[2] == 1) {       // one is left: it is the edge
+                __syncthreads();                          // (found has been read)
+                if (tid < count && mine >> bits == edge >> bits) found[0] = (int)mine;
+                __syncthreads();
+                edge = (uint32_t)found[0];
+                break;
+            } else if (one_each && mine >> bits != edge >> bits) {
+                count = 0;                                // this thread's row is out
+            }
         }
     }
-    // ---- the rows kept, in order: wave i has the rows [i run, (i + 1) run), 64 at a time
-    const int run = ((rows + WAVES - 1) / WAVES + 63) / 64 * 64;
-    const int j_lo = wave * run, j_hi = min(rows, j_lo + run);
-    auto look = [&](int j, bool& take, bool& tie) {
-        const bool always = j < j_hi && (j < first || j >= last), middle = j < j_hi && !always && want > 0;
-        const uint32_t x = middle ? rank(j) : 0u;
-        take = always || (middle && x > edge);
-        tie = middle && x == edge;
-    };
-    int taken = 0, ties = 0;
-    for (int j = j_lo; j < j_hi; j += 64) {
-        bool take, tie;
-        look(j + lane, take, tie);
-        taken += __popcll(__ballot(take));
-        ties += __popcll(__ballot(tie));
-    }
-    __syncthreads();                                      // (wave_a was read above)
-    if (lane == 0) { wave_a[wave] = taken; wave_b[wave] = ties; }
-    __syncthreads();
-    int at = 0, tie_at = 0;
+    // ---- the rows kept, in order
+    int taken = 0, ties = 0;                              // rows above the edge or always kept, rows at the edge, of the blocks before
+    each_block([&](int b, const uint32_t (&x)[SEL_OWN]) __attribute__((always_inline)) {
+        const int j0 = b * BLOCK + tid;
+        int* const sums = part[b & 1];                    // of row sixty-fours, in order: (i, wave)
+        uint64_t take[SEL_OWN], tie[SEL_OWN];
 #pragma unroll
-    for (int i = 0; i < WAVES; ++i) {
-        const int n = wave_a[i], m = wave_b[i];
-        at += i < wave ? n : 0;
-        tie_at += i < wave ? m : 0;
-    }
-    at += min(tie_at, left);
-    for (int j = j_lo; j < j_hi; j += 64) {
-        bool take, tie;
-        look(j + lane, take, tie);
-        const uint64_t below = (1ull << lane) - 1, tie_mask = __ballot(tie);
-        take = take || (tie && tie_at + __popcll(tie_mask & below) < left);
-        const uint64_t take_mask = __ballot(take);
-        if (take) out[at + __popcll(take_mask & below)] = j + lane;
-        at += __popcll(take_mask);
-        tie_at += __popcll(tie_mask);
-    }
+        for (int i = 0; i < SEL_OWN; ++i) {
+            const int j = j0 + SEL_THREADS * i;
+            take[i] = tie[i] = 0;
+            if (b * BLOCK + SEL_THREADS * i + 64 * wave < rows) {
+                const bool mid = j >= first && j < last;
+                take[i] = __ballot(j < rows && (!mid || x[i] > edge));
+                tie[i] = __ballot(mid && x[i] == edge);
+            }
+            if (lane == 0) sums[WAVES * i + wave] = __popcll(take[i]) | __popcll(tie[i]) << 16;    // (both sums of a block are below 2^16)
+        }
+        __syncthreads();
+        const int s0 = sums[2 * lane], s1 = sums[2 * lane + 1];
+        const int upto = wave_sum_upto(s0 + s1), before = upto - s0 - s1;
+        const uint64_t below = (1ull << lane) - 1;
+#pragma unroll
+        for (int i = 0; i < SEL_OWN; ++i) {
+            const int q = WAVES * i + wave;
+            const int ahead = __builtin_amdgcn_readlane(before, q / 2) + (q & 1 ? __builtin_amdgcn_readlane(s0, q / 2) : 0);
+            const int tie_at = ties + (ahead >> 16), at = taken + (ahead & 0xffff) + min(tie_at, left);
+            const int n_tie = max(0, left - tie_at), my_tie = __popcll(tie[i] & below);      // ties kept are the first
+            if ((take[i] >> lane & 1) || ((tie[i] >> lane & 1) && my_tie < n_tie)) out[at + __popcll(take[i] & below) + min(my_tie, n_tie)] = j0 + SEL_THREADS * i;
+        }
+        const int all = __builtin_amdgcn_readlane(upto, 63);
+        taken += all & 0xffff;
+        ties += all >> 16;
+    });
 }
 
 // The kept rows go to the new pages: a workgroup copies ROWS consecutive ones of a head, a 16-byte chunk of k and of v of PASSES rows per thread, all
