@@ -251,9 +251,12 @@ int32_t rope_append(const attn_shape* s, const attn_rope* rope, const void* q, i
     a.page_stride = pages->page_stride;
     a.n_req = n_req;
     a.T = (int32_t)T;
-    a.tokens = T >= 8 * 1024 ? ROPE_TOKENS : T >= 1024 ? 4 : 1;
+    // as many tokens to a workgroup as its threads have on their way at once, but one while there are fewer tokens than compute units
+    const int64_t units = ((int64_t)s->H_q + 2 * s->H_kv) * (s->d / 16);
+    a.tokens = (int32_t)std::max<int64_t>(1, std::min<int64_t>({(int64_t)ROPE_TOKENS, ROPE_UNITS * ROPE_THREADS / units, (T + 255) / 256}));
+    if (units * ROPE_TOKENS > INT32_MAX) return GDN_ERR_SHAPE;
     a.H_q = s->H_q; a.H_kv = s->H_kv;
-    a.units = s->d / 16;
+    a.unit_shift = __builtin_ctz((unsigned)s->d / 16);
     a.page_shift = shift;
     a.rot = rope->rot;
     a.layout = rope->layout;

@@ -33,6 +33,7 @@ __device__ __forceinline__ int request_of(const int32_t* cu, int n_req, int t) {
 // exactly, so that far positions keep 2^-32 of a turn.
 constexpr int ROPE_THREADS = 256;
 constexpr int ROPE_TOKENS = 8;        // tokens per workgroup, at most
+constexpr int ROPE_UNITS = 4;         // pieces of 16 elements that a thread has on their way at once
 
 struct RopeArgs {
     const void *q, *k, *v;
@@ -41,28 +42,41 @@ struct RopeArgs {
     const int32_t* plan;              // cu (n_req + 1), start, pos, place (n_req each: where the page of row 0 would be listed), page ids
     int64_t ldq, ldk, ldv, page_stride;
     int32_t n_req, T, tokens;         // tokens: per workgroup
-    int32_t H_q, H_kv, units;         // units: pieces of 16 elements per head, d / 16
+    int32_t H_q, H_kv, unit_shift;    // log2 of the pieces of 16 elements per head, d / 16
     int32_t page_shift, rot, layout;
     float amplitude;
     uint64_t turn[128];               // turns per position, 2^-64
 };
 
+// Eight elements as they come (two or one 16-byte loads), and as floats.
 template <bool F32>
-__device__ __forceinline__ void load8(const void* p, int64_t at, float* x) {
-    if constexpr (F32) {
-        const f32x4* const s = reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + at);
-        const f32x4 a = s[0], b = s[1];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
-    } else {
-        const u32x4 a = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p) + at);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[2 * i] = __builtin_bit_cast(float, a[i] << 16);
-            x[2 * i + 1] = __builtin_bit_cast(float, a[i] & 0xffff0000u);
+struct Raw8 {
+    u32x4 r[F32 ? 2 : 1];
+    __device__ __forceinline__ void load(const void* p, int64_t at) {
+        if constexpr (F32) {
+            const u32x4* const s = reinterpret_cast<const u32x4*>(static_cast<const float*>(p) + at);
+            r[0] = s[0];
+            r[1] = s[1];
+        } else {
+            r[0] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p) + at);
         }
     }
-}
+    __device__ __forceinline__ void floats(float* x) const {
+        if constexpr (F32) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t u = r[i / 4][i % 4];           // (a value: a cast of the vector's element itself takes the first)
+                x[i] = __builtin_bit_cast(float, u);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                x[2 * i] = __builtin_bit_cast(float, r[0][i] << 16);
+                x[2 * i + 1] = __builtin_bit_cast(float, r[0][i] & 0xffff0000u);
+            }
+        }
+    }
+};
 __device__ __forceinline__ void store8_bf16(uint16_t* p, const float* x) {
     bf16x8 y;
 #pragma unroll
@@ -76,8 +90,9 @@ __device__ __forceinline__ void store8_fp16(uint16_t* p, const float* x) {
     *reinterpret_cast<u32x4*>(p) = __builtin_bit_cast(u32x4, y);
 }
 
-// One workgroup takes `tokens` tokens: their cosines and sines once, to LDS, for all heads; then one thread per 16 elements of a
-// head (two runs of 8 where a pair's halves lie apart).
+// One workgroup takes `tokens` tokens: one thread per 16 elements of a head (two runs of 8), ROPE_UNITS of them on
+// their way while the tokens' places in the pages are looked up and their cosines and sines made, once for all heads, in LDS.
+// Bound: memory, read and written once.
 template <bool F32, bool BY_VALUE>
 __global__ void __launch_bounds__(ROPE_THREADS) attn_rope_kernel(RopeArgs a, PlanWords<BY_VALUE> words) {
     __shared__ float cs[ROPE_TOKENS][2][128];
@@ -85,76 +100,111 @@ __global__ void __launch_bounds__(ROPE_THREADS) attn_rope_kernel(RopeArgs a, Pla
     __shared__ int32_t position[ROPE_TOKENS];
     const int tok0 = (int)blockIdx.x * a.tokens;
     const int n_tok = min(a.tokens, a.T - tok0);
-    const int wave = threadIdx.x >> 6;
-    const int D = 16 * a.units;
+    const int tid = threadIdx.x, wave = tid >> 6;
+    const int D = 16 << a.unit_shift, half = a.rot >> 1;
+    const int per = (a.H_q + 2 * a.H_kv) << a.unit_shift, total = n_tok * per;
+    const int step_t = ROPE_THREADS / per, step_j = ROPE_THREADS - step_t * per;
+
+    Raw8<F32> raw[ROPE_UNITS][2];
+    int next_t = tid / per, next_j = tid - next_t * per;      // the unit to be loaded: its token, its number among the token's
+    // a unit's places: elements lo .. lo + 7 and hi .. hi + 7 of its head, of the first and the second half of the part that turns, of the part that
+    // does not, or of a value (so that neighbouring threads load and store neighbouring 16 bytes)
+    auto runs_of = [&](int j, int& head, int& lo, int& hi, bool& turned) __attribute__((always_inline)) {
+        head = j >> a.unit_shift;
+        const int u = j & ((1 << a.unit_shift) - 1), rot = head < a.H_q + a.H_kv ? a.rot : 0;
+        turned = 16 * u < rot;
+        lo = turned ? 8 * u : rot + 8 * u - (rot >> 1);
+        hi = lo + (turned ? half : (D - rot) >> 1);
+    };
+    auto on = [&](int& t, int& j) __attribute__((always_inline)) {
+        t += step_t;
+        j += step_j;
+        if (j >= per) { j -= per; ++t; }
+    };
+    auto load_units = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < ROPE_UNITS; ++i) {
+            if (next_t < n_tok) {
+                int head, lo, hi;
+                bool turned;
+                runs_of(next_j, head, lo, hi, turned);
+                const int64_t tok = tok0 + next_t;
+                const bool is_q = head < a.H_q, is_k = head < a.H_q + a.H_kv;
+                const void* const from = is_q ? a.q : is_k ? a.k : a.v;
+                const int64_t at = tok * (is_q ? a.ldq : is_k ? a.ldk : a.ldv) + (head - (is_q ? 0 : is_k ? a.H_q : a.H_q + a.H_kv)) * D;
+                raw[i][0].load(from, at + lo);
+                raw[i][1].load(from, at + hi);
+            }
+            on(next_t, next_j);
+        }
+    };
+    int t = next_t, j = next_j;                               // the unit to be stored
+    load_units();
+
     const int32_t* const cu = BY_VALUE ? words.w : a.plan;
     const int32_t *const start = cu + a.n_req + 1, *const pos = start + a.n_req, *const place = pos + a.n_req, *const page_ids = place + a.n_req;
     for (int i = wave; i < n_tok; i += ROPE_THREADS / 64) {
-        const int t = tok0 + i, r = request_of(cu, a.n_req, t);
-        if ((threadIdx.x & 63) == 0) {
-            const int in = t - cu[r], row = start[r] + in;
+        const int r = request_of(cu, a.n_req, tok0 + i);
+        if ((tid & 63) == 0) {
+            const int in = tok0 + i - cu[r], row = start[r] + in;
             position[i] = pos[r] + in;
             row_at[i] = (int64_t)page_ids[place[r] + (row >> a.page_shift)] * a.page_stride + (int64_t)(row & ((1 << a.page_shift) - 1)) * D;
         }
     }
     __syncthreads();
-    const int half = a.rot >> 1;
-    for (int i = threadIdx.x; i < n_tok * half; i += ROPE_THREADS) {
-        const int t = i / half, p = i - t * half;
-        const uint64_t turns = (uint64_t)(uint32_t)position[t] * a.turn[p];
+    for (int i = tid; i < n_tok * half; i += ROPE_THREADS) {
+        const int tk = i / half, p = i - tk * half;
+        const uint64_t turns = (uint64_t)(uint32_t)position[tk] * a.turn[p];
         float sn, cn;
         sincospif((float)(int32_t)(turns >> 32) * 0x1p-31f, &sn, &cn);
-        cs[t][0][p] = cn * a.amplitude;
-        cs[t][1][p] = sn * a.amplitude;
+        cs[tk][0][p] = cn * a.amplitude;
+        cs[tk][1][p] = sn * a.amplitude;
     }
     __syncthreads();
-    const int heads = a.H_q + 2 * a.H_kv, per = heads * a.units;
-    for (int i = threadIdx.x; i < n_tok * per; i += ROPE_THREADS) {
-        const int t = i / per, j = i - t * per;
-        const int head = j / a.units, u = j - head * a.units;
-        const int64_t tok = tok0 + t;
-        float x[16];
-        if (head >= a.H_q + a.H_kv) {            // a value: widened
-            const int h = head - a.H_q - a.H_kv;
-            const int64_t src = tok * a.ldv + h * D + 16 * u;
-            load8<F32>(a.v, src, x);
-            load8<F32>(a.v, src + 8, x + 8);
-            uint16_t* const dst = a.v_pool + row_at[t] + ((int64_t)h * D << a.page_shift) + 16 * u;
-            store8_fp16(dst, x);
-            store8_fp16(dst + 8, x + 8);
-            continue;
-        }
-        const bool key = head >= a.H_q;
-        const int h = key ? head - a.H_q : head;
-        const bool turned = 16 * u < a.rot, apart = turned && a.layout == 0;
-        const int lo = apart ? 8 * u : 16 * u, hi = apart ? half + 8 * u : 16 * u + 8;
-        const int64_t src = (key ? tok * a.ldk : tok * a.ldq) + h * D;
-        const void* const from = key ? a.k : a.q;
-        load8<F32>(from, src + lo, x);
-        load8<F32>(from, src + hi, x + 8);
-        if (turned) {
-            float y[16];
-            if (apart) {
+    for (int done = 0; done < total; done += ROPE_THREADS * ROPE_UNITS) {
+        if (done > 0) load_units();
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float cn = cs[t][0][8 * u + e], sn = cs[t][1][8 * u + e];
-                    y[e] = x[e] * cn - x[8 + e] * sn;
-                    y[8 + e] = x[8 + e] * cn + x[e] * sn;
-                }
-            } else {
+        for (int i = 0; i < ROPE_UNITS; ++i) {
+            if (t < n_tok) {
+                int head, lo, hi;
+                bool turned;
+                runs_of(j, head, lo, hi, turned);
+                float x[16];
+                raw[i][0].floats(x);
+                raw[i][1].floats(x + 8);
+                if (head >= a.H_q + a.H_kv) {                 // a value: widened
+                    uint16_t* const dst = a.v_pool + row_at[t] + ((int64_t)(head - a.H_q - a.H_kv) * D << a.page_shift) + lo;
+                    store8_fp16(dst, x);
+                    store8_fp16(dst + hi - lo, x + 8);
+                } else {
+                    if (turned) {
+                        const float *const c = cs[t][0], *const s = cs[t][1];
+                        float y[16];
+                        if (a.layout == 0) {                  // pair lo + e: its halves are e of the two runs
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float cn = cs[t][0][8 * u + e], sn = cs[t][1][8 * u + e];
-                    y[2 * e] = x[2 * e] * cn - x[2 * e + 1] * sn;
-                    y[2 * e + 1] = x[2 * e + 1] * cn + x[2 * e] * sn;
+                            for (int e = 0; e < 8; ++e) {
+                                y[e] = x[e] * c[lo + e] - x[8 + e] * s[lo + e];
+                                y[8 + e] = x[8 + e] * c[lo + e] + x[e] * s[lo + e];
+                            }
+                        } else {                              // four pairs in each run
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                const int p = (e < 4 ? lo : hi) / 2 + (e & 3);
+                                y[2 * e] = x[2 * e] * c[p] - x[2 * e + 1] * s[p];
+                                y[2 * e + 1] = x[2 * e + 1] * c[p] + x[2 * e] * s[p];
+                            }
+                        }
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) x[e] = y[e];
+                    }
+                    uint16_t* const dst = head < a.H_q ? a.q_out + ((int64_t)(tok0 + t) * a.H_q + head) * D
+                                                       : a.k_pool + row_at[t] + ((int64_t)(head - a.H_q) * D << a.page_shift);
+                    store8_bf16(dst + lo, x);
+                    store8_bf16(dst + hi, x + 8);
                 }
             }
-#pragma unroll
-            for (int e = 0; e < 16; ++e) x[e] = y[e];
+            on(t, j);
         }
-        uint16_t* const dst = key ? a.k_pool + row_at[t] + ((int64_t)h * D << a.page_shift) : a.q_out + (tok * a.H_q + h) * D;
-        store8_bf16(dst + lo, x);
-        store8_bf16(dst + hi, x + 8);
     }
 }
 
