@@ -221,6 +221,91 @@ struct PageIds {
     }
 };
 
+// One query row over the keys [k_lo, k_hi), by a wave, without matrix instructions: what is left for rows that these gave something that is not a
+// number.  A weight of 0 times an infinite value is not a number, and the last tile that a row sees may hold values of later tokens; the row's own
+// result is the sum over what it sees.  Lane i gets D / 64 columns from i * D / 64 of the unnormalised output.
+template <int D>
+__device__ void walk_row(const PagedArgs& a, int first, int kvh, const uint16_t* q, int k_lo, int k_hi, float& m, float& l, float& le, float (&o)[D / 64]) {
+    constexpr int COLS = D / 64;
+    const int lane = threadIdx.x & 63, mask = (1 << a.page_shift) - 1;
+    const float c = a.scale_log2e;
+    m = -INFINITY;
+    l = le = 0.f;
+#pragma unroll
+    for (int i = 0; i < COLS; ++i) o[i] = 0.f;
+#pragma unroll 1
+    for (int base = k_lo; base < k_hi; base += 64) {
+        const int key = min(base + lane, k_hi - 1);
+        const int64_t at = (int64_t)a.page_ids[first + (key >> a.page_shift)] * a.slot_stride + (((int64_t)kvh << a.page_shift) + (key & mask)) * D;
+        float s = 0.f;
+#pragma unroll 1
+        for (int x = 0; x < D; x += 8) {
+            const u32x4 qv = *reinterpret_cast<const u32x4*>(q + x), kv = *reinterpret_cast<const u32x4*>(a.k_cache + at + x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t qw = qv[i], kw = kv[i];
+                s = __builtin_fmaf(__builtin_bit_cast(float, qw << 16), __builtin_bit_cast(float, kw << 16), s);
+                s = __builtin_fmaf(__builtin_bit_cast(float, qw & 0xffff0000u), __builtin_bit_cast(float, kw & 0xffff0000u), s);
+            }
+        }
+        if (base + lane >= k_hi) s = -INFINITY;
+        float top = s;
+        for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+        const float m_new = fmaxf(m, top), m_ref = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = __builtin_amdgcn_exp2f((m - m_ref) * c);
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s, c, -m_ref * c)), ph = (float)(_Float16)p;
+        float sum = ph, esum = p;
+        for (int d = 32; d > 0; d >>= 1) {
+            sum += __shfl_xor(sum, d);
+            esum += __shfl_xor(esum, d);
+        }
+        l = l * alpha + sum;
+        le = le * alpha + esum;
+        m = m_new;
+#pragma unroll
+        for (int i = 0; i < COLS; ++i) o[i] *= alpha;
+        const int n = min(64, k_hi - base);
+#pragma unroll 1
+        for (int k = 0; k < n; ++k) {
+            const float w = __shfl(ph, k);
+            const int64_t row = (int64_t)__shfl((long long)at, k);
+#pragma unroll
+            for (int i = 0; i < COLS; ++i) o[i] += w * (float)__builtin_bit_cast(_Float16, a.v_cache[row + lane * COLS + i]);
+        }
+    }
+}
+
+// Output column `col` of row (token, head): normalised, gated, stored.
+template <int D, typename OT>
+__device__ __forceinline__ void store_column(const AttnArgs& a, int64_t token, int head, int col, float y) {
+    const int64_t at = (token * a.H_q + head) * D + col;
+    if (a.gate) y *= 1.f / (1.f + __expf(-__builtin_bit_cast(float, (uint32_t)a.gate[at] << 16)));
+    if constexpr (sizeof(OT) == 4) static_cast<float*>(a.o)[at] = y;
+    else static_cast<uint16_t*>(a.o)[at] = __builtin_bit_cast(uint16_t, (__bf16)y);
+}
+
+// walk_row's result to its place: a workspace row, or the output.
+template <int D, typename OT, bool LSE>
+__device__ void redo_row(const PagedArgs& a, int first, int kvh, int64_t token, int head, int k_lo, int k_hi, int64_t part_row) {
+    constexpr int COLS = D / 64;
+    const int lane = threadIdx.x & 63;
+    float m, l, le, o[COLS];
+    walk_row<D>(a, first, kvh, a.q + (token * a.H_q + head) * D, k_lo, k_hi, m, l, le, o);
+    if (part_row >= 0) {
+        if (lane == 0) {
+            *reinterpret_cast<f32x2*>(a.part_ml + part_row * 2) = f32x2{m, l};
+            if constexpr (LSE) a.part_le[part_row] = le;
+        }
+#pragma unroll
+        for (int i = 0; i < COLS; ++i) a.part_o[part_row * D + lane * COLS + i] = o[i];
+        return;
+    }
+    if constexpr (LSE)
+        if (lane == 0) a.lse[token * a.H_q + head] = row_lse(m, le, a.scale_log2e);
+#pragma unroll
+    for (int i = 0; i < COLS; ++i) store_column<D, OT>(a, token, head, lane * COLS + i, o[i] / l);
+}
+
 template <int D>
 struct AttnSmem {
     static constexpr int CPR = D / 8;                     // 16-byte chunks per row
@@ -295,7 +380,7 @@ __global__ void __launch_bounds__(ATT_THREADS * NH, 2) attn_suffix_kernel(Args a
     const int wq0 = q0 + (32 * wave) / R;                  // first token of this wave
     const int wq1 = min(q0 + (32 * wave + 31) / R + 1, q_end);   // one past its last
     const int n_tiles_w = wq0 < q_end ? (c0 + wq1 + ATT_KT - 1) / ATT_KT : 0;   // tiles this wave can see
-    const bool valid = q0 + tl < q_end;                    // this lane's row is a token of the request
+    bool valid = q0 + tl < q_end;                          // this lane's row is a token of the request
     const int qrow = min(q0 + tl, q_end - 1);              // clamped: lanes past the end repeat the last token
     const int lim = c0 + qrow;                             // last visible key row (0-based) of this lane's query
 
@@ -493,11 +578,27 @@ __global__ void __launch_bounds__(ATT_THREADS * NH, 2) attn_suffix_kernel(Args a
     }
 
     wait_vmcnt<0>();                           // no load to LDS may be in flight when the workgroup's LDS is given back
+    auto part_row = [&](int row) {
+        return part >= 0 ? ((int64_t)part * (a.H_q / R) + hb) * ATT_BQ + row : a.few_row0 + ((int64_t)(-2 - part) * (a.H_q / R) + hb) * NAR_ROWS + row;
+    };
+    if constexpr (PAGED) {                     // rows with something that is not a number are walked again (see walk_row)
+        bool bad = false;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) bad |= O[rb][i] != O[rb][i];
+        const uint64_t lanes = __builtin_amdgcn_ballot_w64(bad && valid);
+        for (uint32_t cols = (uint32_t)lanes | (uint32_t)(lanes >> 32); cols != 0; cols &= cols - 1) {
+            const int x = __builtin_ctz(cols);
+            const int row = 32 * wave + x, tok = q0 + row / R, head = hb * R + row % R;
+            redo_row<D, OT, LSE>(a, a.slot[r], kvh, tok0 + tok, head, t0 * ATT_KT, min(t1 * ATT_KT, c0 + tok + 1), part == -1 ? -1 : part_row(row));
+            if (col == x) valid = false;
+        }
+    }
     // ---- a part of a split walk leaves its unnormalised result in its workspace slot
     if (part != -1) {
         if (valid) {
-            const int64_t prow = part >= 0 ? ((int64_t)part * (a.H_q / R) + hb) * ATT_BQ + wrow
-                                           : a.few_row0 + ((int64_t)(-2 - part) * (a.H_q / R) + hb) * NAR_ROWS + wrow;
+            const int64_t prow = part_row(wrow);
             const float lt = sum_with_other_half(l);
             if (g == 0) *reinterpret_cast<f32x2*>(a.part_ml + prow * 2) = f32x2{m, lt};
             if constexpr (LSE) {
@@ -583,6 +684,7 @@ __global__ void __launch_bounds__(ATT_THREADS, narrow_wgs_per_cu(D)) attn_narrow
     // do not depend on the loads to LDS in flight to the other, for which it would wait otherwise
     __shared__ __attribute__((aligned(1024))) char ring0[4][SM::BLOCK_BYTES], ring1[4][SM::BLOCK_BYTES];
     __shared__ float ml[4][NAR_ROWS][LSE ? 3 : 2];
+    __shared__ int bad[PAGED ? NAR_ROWS : 1];                // pages: rows with something that is not a number
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -783,6 +885,7 @@ __global__ void __launch_bounds__(ATT_THREADS, narrow_wgs_per_cu(D)) attn_narrow
     // ---- merge of the four waves: each leaves its result in LDS, in the place of the value blocks
     wait_vmcnt<0>();
     __syncthreads();
+    if (PAGED && threadIdx.x < NAR_ROWS) bad[threadIdx.x] = 0;
     auto om = [&](int w, int row) {                          // a row of wave w's result: waves 0, 1 in one half, 2, 3 in the other
         return reinterpret_cast<float*>(w < 2 ? &ring0[0][0] : &ring1[0][0]) + ((w & 1) * NAR_ROWS + row) * SM::OROW;
     };
@@ -811,6 +914,8 @@ __global__ void __launch_bounds__(ATT_THREADS, narrow_wgs_per_cu(D)) attn_narrow
             L += wt * ml[w][row][1];
             if constexpr (LSE) Le += wt * ml[w][row][2];
         }
+        if constexpr (PAGED)
+            if (n > 1 && (acc[0] != acc[0] || acc[1] != acc[1] || acc[2] != acc[2] || acc[3] != acc[3])) bad[row] = 1;
         if (part >= 0) {
             const int64_t prow = a.few_row0 + ((int64_t)part * a.H_kv + kvh) * NAR_ROWS + row;
             if (dv == 0) *reinterpret_cast<f32x2*>(a.part_ml + prow * 2) = f32x2{M, L};
@@ -821,6 +926,14 @@ __global__ void __launch_bounds__(ATT_THREADS, narrow_wgs_per_cu(D)) attn_narrow
             if constexpr (LSE) if (dv == 0) a.lse[(int64_t)(tok0 + t) * a.H_q + kvh * G + row - t * G] = row_lse(M, Le, c);
             store_out<OT>(a.o, a.gate, ((int64_t)(tok0 + t) * a.H_q + kvh * G + row - t * G) * D + dv, acc * (1.f / L));
         }
+    }
+    if constexpr (PAGED) {                                   // a single token sees every row there is
+        if (n == 1) return;
+        __syncthreads();
+        for (int row = wave; row < rows; row += 4)
+            if (bad[row])
+                redo_row<D, OT, LSE>(a, slot, kvh, tok0 + row / G, kvh * G + row % G, k0, min(k1, c0 + row / G + 1),
+                                     part >= 0 ? a.few_row0 + ((int64_t)part * a.H_kv + kvh) * NAR_ROWS + row : -1);
     }
 }
 

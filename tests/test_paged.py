@@ -582,3 +582,56 @@ def test_calls_on_another_stream_and_again_give_the_same_bits():
     w2 = torch.zeros_like(w)
     PG.attn_key_weights(c.shape, c.dev(q), z, c.cu, c.starts, c.k_pool, c.page_cu, c.page_ids, 1.0, None, w2, c.workspace())
     assert torch.equal(w, w2)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H_q,H_kv,d,P,lens,starts,at", [
+    (4, 2, 64, 16, [40], [3], 20),                    # inside one tile
+    (16, 2, 128, 32, [24, 5], [100, 60], 2),          # packed rows
+    (4, 1, 128, 16, [3], [1300], 1),                  # the few-rows kernel, walks cut
+    (8, 8, 256, 64, [70], [2500], 33),                # walks cut, parts that see nothing
+    (16, 2, 128, 64, [400], [600], 250),              # two heads to a workgroup or one
+    (1, 1, 64, 16, [9], [1100], 4),
+])
+@pytest.mark.parametrize("what", [np.inf, np.nan])
+def test_what_a_later_token_holds_does_not_reach_earlier_rows(H_q, H_kv, d, P, lens, starts, at, what):
+    """Token `at` of every request has a value row that is not finite and a key of NaN: the rows before it are those of a request that
+    ends there, the rows from it on are not finite."""
+    c = Paged(61, H_q, H_kv, d, P, lens, starts)
+    for r in range(len(lens)):
+        c.v_rows[r][starts[r] + at] = what
+        c.k_rows[r][starts[r] + at] = 0x7fc0
+    c.fill()
+    q = c.bf16(c.T, H_q, d)
+    o, z = run_attend(c, q, None, "f32")
+    o, z = o.double().cpu().numpy(), z.double().cpu().numpy()
+    for r in range(len(lens)):
+        cut, s0 = starts[r] + at, c.cu[r]
+        k, v = f64(c.k_rows[r][:cut]), c.v_rows[r][:cut].astype(np.float64)
+        ref = ao.attention_suffix(f64(q[s0:s0 + at]), k, v, starts[r], d ** -0.5)
+        assert (np.abs(o[s0:s0 + at] - ref) <= 2.0 ** -8 * np.abs(v).max()).all(), r
+        zr = po.row_lse(f64(q[s0:s0 + at]), k, starts[r], d ** -0.5)
+        bound = (d + 16) * 2.0 ** -24 * d ** -0.5 * np.sqrt((k ** 2).sum(-1)).max() * np.sqrt((f64(q) ** 2).sum(-1)).max()
+        assert (np.abs(z[s0:s0 + at] - zr) <= bound + 2.0 ** -20 * (1 + np.abs(zr))).all()
+        assert not np.isfinite(o[s0 + at:s0 + lens[r]]).any()
+
+
+@pytest.mark.gpu
+def test_key_weights_of_rows_and_keys_that_are_not_numbers_stay_theirs():
+    """A key of NaN has a weight of NaN and no other has; a query row of NaN reaches the keys that it sees and no others."""
+    import torch
+    c = Paged(62, 4, 2, 128, 16, [40, 1], [300, 20])
+    c.k_rows[0][310, 1] = 0x7fc0
+    c.fill()
+    q = c.bf16(41, 4, 128)
+    q[10, 1] = 0x7fc0                                  # token 10 of the first request, head group 0
+    lse = torch.zeros(41, 4, device="cuda") + 8.0
+    w = torch.full((c.k_np.shape[0], 2, 16), 7.0, device="cuda")
+    PG.attn_key_weights(c.shape, c.dev(q), lse, c.cu, c.starts, c.k_pool, c.page_cu, c.page_ids, 1.0, None, w, c.workspace())
+    w = w.cpu().numpy()
+    page, row = c.place(0, 340)
+    got = w[page, :, row]
+    assert np.isnan(got[:311, 0]).all() and np.isfinite(got[311:, 0]).all()
+    assert np.isnan(got[310, 1]) and np.isfinite(np.delete(got[:, 1], 310)).all()
+    page, row = c.place(1, 21)
+    assert np.isfinite(w[page, :, row]).all()
