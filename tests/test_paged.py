@@ -635,3 +635,50 @@ def test_key_weights_of_rows_and_keys_that_are_not_numbers_stay_theirs():
     assert np.isnan(got[310, 1]) and np.isfinite(np.delete(got[:, 1], 310)).all()
     page, row = c.place(1, 21)
     assert np.isfinite(w[page, :, row]).all()
+
+
+@pytest.mark.gpu
+def test_a_session_of_prompts_decoding_and_eviction_matches_the_oracle():
+    """The operators in turn, as a serving program runs them: after an eviction the requests go on with fewer rows and the same positions."""
+    import torch
+    from paper_2605_05219_amd.paged_session import PagedLayer
+    H_q, H_kv, d, R = 4, 2, 64, 2
+    layer = PagedLayer(H_q, H_kv, d, R, 40, page_rows=16, decay=0.9)
+    freqs = po.rope_freqs(d)[0]
+    gen = torch.Generator().manual_seed(3)
+    held = [dict(k=np.zeros((0, H_kv, d)), v=np.zeros((0, H_kv, d)), w=np.zeros((0, H_kv))) for _ in range(R)]
+    pos = [0, 0]
+    for lens in ([70, 33], [1, 1], [5, 0], [1, 1]):
+        q, k, v = (torch.randn(sum(lens), h, d, generator=gen).bfloat16() for h in (H_q, H_kv, H_kv))
+        o = layer.step(q.cuda(), k.cuda(), v.cuda(), lens).double().cpu().numpy()
+        at = 0
+        for r, n in enumerate(lens):
+            if n == 0:
+                held[r]["w"] = held[r]["w"] * 0.9
+                continue
+            s = slice(at, at + n)
+            at += n
+            bf = lambda x: torch.from_numpy(x).bfloat16().double().numpy()  # noqa: E731
+            qr, kr = (bf(po.rotate(x[s].double().numpy(), pos[r], freqs, "half", 1.0)) for x in (q, k))
+            h, c = held[r], held[r]["k"].shape[0]
+            h["k"], h["v"] = np.concatenate([h["k"], kr]), np.concatenate([h["v"], v[s].double().numpy()])
+            ref = ao.attention_suffix(qr, h["k"], h["v"], c, d ** -0.5)
+            # a rotated value may round the other way: 2^-7 of q and of k moves a logit by 2^-6 |q||k| scale at the very most, where it is far less
+            assert np.abs(o[s] - ref).max() <= 2.0 ** -5 * np.abs(h["v"]).max()
+            h["w"] = po.key_weights(qr, po.row_lse(qr, h["k"], c, d ** -0.5), h["k"], c, d ** -0.5, 0.9, h["w"])
+            pos[r] += n
+        if layer.rows.max() > 60:
+            before, w_pool = [list(p) for p in layer.pages], layer.w_pool.cpu().numpy()
+            rows = layer.rows.copy()
+            layer.evict(60, 40, first=2, recent=8)
+            for r in range(R):
+                if rows[r] <= 60:
+                    continue
+                j = np.arange(rows[r])
+                w = w_pool[np.asarray(before[r])[j // 16], :, j % 16]
+                assert np.allclose(w, held[r]["w"], rtol=2e-2, atol=1e-3)
+                idx = [po.rows_kept(w[:, g], 40, 2, 8) for g in range(H_kv)]
+                for x in held[r]:
+                    held[r][x] = np.stack([held[r][x][idx[g], g] for g in range(H_kv)], axis=1)
+                assert layer.rows[r] == 40 and len(layer.pages[r]) == 3 and layer.pos[r] == pos[r]
+    assert len(layer.free) + sum(len(p) for p in layer.pages) == 40
