@@ -322,15 +322,14 @@ inline int heads_per_workgroup(const attn_shape& s, const UnitPlan& plan) {
 // request's page ids begin), the records of the few-rows kernel's units, the five arrays of the 128-row kernel's units, the four of the split pieces of
 // either kind of request, and the page ids.
 struct CallImage {
-    std::vector<int32_t> img;
+    int64_t ints = 0;                 // in all
     int64_t n_narrow = 0, n_wide = 0, rec_at = 0, unit_at = 0, piece_at[2] = {0, 0}, ids_at = 0;
     int64_t blocks = 0;               // workgroups of the 128-row kernel
     int NH = 1;                       // head blocks per workgroup of it
     bool xcd_split = false;
 };
 
-inline int32_t make_image(const attn_shape* s, const UnitPlan& plan, int32_t n_req, const int32_t* cu_seqlens, const int32_t* start_pos,
-                          const int32_t* len, const int32_t* place, const int32_t* page_ids, int64_t n_ids, CallImage& im) {
+inline int32_t lay_out_image(const attn_shape* s, const UnitPlan& plan, int32_t n_req, int64_t n_ids, CallImage& im) {
     const int G = s->H_q / s->H_kv;
     const int pack = plan.pack, HB = s->H_q / pack;
     const int NH = im.NH = heads_per_workgroup(*s, plan);
@@ -352,8 +351,13 @@ inline int32_t make_image(const attn_shape* s, const UnitPlan& plan, int32_t n_r
     im.piece_at[0] = im.unit_at + WIDE_INTS * n_wide;
     im.piece_at[1] = im.piece_at[0] + 4 * (int64_t)plan.split[0].size();
     im.ids_at = im.piece_at[1] + 4 * (int64_t)plan.split[1].size();
-    im.img.assign((size_t)(im.ids_at + n_ids), 0);
-    int32_t* p_cu = im.img.data();
+    im.ints = im.ids_at + n_ids;
+    return GDN_OK;
+}
+
+inline void fill_image(const attn_shape* s, const UnitPlan& plan, int32_t n_req, const int32_t* cu_seqlens, const int32_t* start_pos, const int32_t* len,
+                       const int32_t* place, const int32_t* page_ids, int64_t n_ids, const CallImage& im, int32_t* p_cu) {
+    const int64_t n_wide = im.n_wide;
     int32_t* p_start = p_cu + n_req + 1;
     int32_t* p_slot = p_start + n_req;
     int32_t* p_rec = p_cu + im.rec_at;         // records of the few-rows kernel's units
@@ -388,7 +392,6 @@ inline int32_t make_image(const attn_shape* s, const UnitPlan& plan, int32_t n_r
             p_piece[3 * n + i] = plan.split[k][i].parts;
         }
     }
-    return GDN_OK;
 }
 
 // The fields of a call's arguments that follow from its image, whose device copy begins at d, and from the region of the partial

@@ -44,7 +44,7 @@ int32_t check_lengths(int32_t n_req, const int32_t* cu, const int32_t* start, st
     return GDN_OK;
 }
 
-// A page table: every listed id inside the pool, and enough of them for rows(r) rows of request r.
+// The lengths of a page table: enough pages listed for rows(r) rows of request r.
 template <typename F>
 int32_t check_table(const attn_pages* p, int32_t n_req, const int32_t* page_cu, const int32_t* page_ids, F rows) {
     if (!page_cu) return GDN_ERR_NULL;
@@ -53,26 +53,40 @@ int32_t check_table(const attn_pages* p, int32_t n_req, const int32_t* page_cu, 
         if (page_cu[r + 1] < page_cu[r]) return GDN_ERR_SEQLENS;
         if ((int64_t)(page_cu[r + 1] - page_cu[r]) * p->page_rows < rows(r)) return GDN_ERR_START;
     }
-    const int32_t n = page_cu[n_req];
-    if (n > 0 && !page_ids) return GDN_ERR_NULL;
-    bool bad = false;
-    for (int32_t i = 0; i < n; ++i) bad |= (uint32_t)page_ids[i] >= (uint32_t)p->n_pages;
+    return page_cu[n_req] > 0 && !page_ids ? GDN_ERR_NULL : GDN_OK;
+}
+
+// Its ids, all inside the pool.
+int32_t check_ids(const attn_pages* p, const int32_t* ids, int64_t n) {
+    uint32_t bad = 0;
+    for (int64_t i = 0; i < n; ++i) bad |= (uint32_t)ids[i] >= (uint32_t)p->n_pages;
     return bad ? GDN_ERR_SLOT_RANGE : GDN_OK;
 }
 
-// A set of page ids.
+// A set of page ids.  The bits are the thread's own between calls (a long table would cost the calls fresh memory each time).
 class PageSet {
   public:
-    explicit PageSet(int32_t n_pages) : bits_((size_t)n_pages / 64 + 1, 0) {}
-    bool has(int32_t id) const { return bits_[(size_t)id / 64] >> (id % 64) & 1; }
-    bool add(int32_t id) {       // false: it was there
-        const bool was = has(id);
-        bits_[(size_t)id / 64] |= 1ull << (id % 64);
-        return !was;
+    explicit PageSet(int32_t n_pages) {
+        thread_local std::vector<uint64_t> store;
+        bits_ = &store;
+        store.assign((size_t)n_pages / 64 + 1, 0);
+    }
+    bool has(int32_t id) const { return (*bits_)[(size_t)id / 64] >> (id % 64) & 1; }
+    // ids inside the pool; false: one of them was there
+    bool add(const int32_t* ids, int64_t n) {
+        uint64_t* const b = bits_->data();
+        uint64_t twice = 0;
+        for (int64_t i = 0; i < n; ++i) {
+            uint64_t& word = b[(uint32_t)ids[i] / 64];
+            const uint64_t bit = 1ull << ((uint32_t)ids[i] % 64);
+            twice |= word & bit;
+            word |= bit;
+        }
+        return twice == 0;
     }
 
   private:
-    std::vector<uint64_t> bits_;
+    std::vector<uint64_t>* bits_;
 };
 
 // The region of the partial results behind the uploaded image: maxima and normalisers, outputs, sums of the unrounded weights.
@@ -100,7 +114,8 @@ int32_t check_call(const attn_shape* s, int32_t n_req, const int32_t* cu, const 
                    const int32_t* page_cu, const int32_t* page_ids, std::vector<int32_t>& len) {
     int32_t rc = check_lengths(n_req, cu, start, len);
     if (rc != GDN_OK) return rc;
-    return check_table(pages, n_req, page_cu, page_ids, [&](int32_t r) { return (int64_t)start[r] + len[r]; });
+    rc = check_table(pages, n_req, page_cu, page_ids, [&](int32_t r) { return (int64_t)start[r] + len[r]; });
+    return rc != GDN_OK ? rc : check_ids(pages, page_ids, page_cu[n_req]);
 }
 
 int32_t check_front(const attn_shape* s, int32_t n_req, const attn_pages* pages) {
@@ -110,11 +125,12 @@ int32_t check_front(const attn_shape* s, int32_t n_req, const attn_pages* pages)
     return check_pages(s, pages);
 }
 
-// ---- a call's image to the device.  Small ones go by value (gdn::upload_plan); page tables are larger, and a copy of more than 16 KiB takes the
-// stream 20 us between two kernels: these a launch of ours reads out of pinned memory (4 us for 90 KB).  The buffers form a ring; a workgroup that has
-// read its piece says so in a word of the buffer, and a call that comes round to a buffer waits (on the host) for all of them.
+// ---- a call's plan (its index arrays) to the device.  What fits goes by value, in the arguments of the call's launches where those take it, or of a
+// small launch (gdn::upload_plan).  Page tables are larger, and a copy of more than 16 KiB takes the stream 20 us between two kernels: these are
+// written into pinned memory, out of which a launch of ours reads them (4 us for 90 KB).  The buffers form a ring; a workgroup that has read its
+// piece says so in a word of the buffer, and a call that comes round to a buffer waits (on the host) for all of them.
 constexpr int FETCH_RING = 8, FETCH_THREADS = 256, FETCH_PIECE = 16 * FETCH_THREADS;   // bytes per workgroup
-constexpr size_t FETCH_ABOVE = 7168;
+constexpr int SMALL_WORDS = 1792;
 
 __global__ void __launch_bounds__(FETCH_THREADS) attn_fetch_kernel(const u32x4* src, u32x4* dst, int64_t n, uint32_t* read, uint32_t mark) {
     const int64_t i = (int64_t)blockIdx.x * FETCH_THREADS + threadIdx.x;
@@ -126,59 +142,82 @@ __global__ void __launch_bounds__(FETCH_THREADS) attn_fetch_kernel(const u32x4* 
 struct FetchRing {
     std::mutex mu;
     struct Slot {
-        char* host = nullptr;             // words of the workgroups that have read, then the image
-        size_t bytes = 0;                 // room for the image
+        char* host = nullptr;             // words of the workgroups that have read, then the plan
+        size_t bytes = 0;                 // room for the plan
         uint32_t mark = 0, blocks = 0;    // of the last upload
+        size_t words_bytes() const { return (bytes / FETCH_PIECE * sizeof(uint32_t) + 255) / 256 * 256; }
     } slot[FETCH_RING];
     int next = 0;
 };
 FetchRing g_fetch;
 
-int32_t send_image(const std::vector<int32_t>& img, void* dst, hipStream_t stream) {
-    const size_t bytes = img.size() * sizeof(int32_t);
-    if (bytes <= FETCH_ABOVE) return gdn::upload_plan(img.data(), bytes, dst, stream);
-    std::lock_guard<std::mutex> lock(g_fetch.mu);
-    FetchRing::Slot& s = g_fetch.slot[g_fetch.next];
-    g_fetch.next = (g_fetch.next + 1) % FETCH_RING;
-    const auto words = [](size_t room) { return (room + FETCH_PIECE - 1) / FETCH_PIECE; };
-    if (s.host) {
-        uint32_t* const read = reinterpret_cast<uint32_t*>(s.host);
-        for (uint32_t b = 0; b < s.blocks; ++b)
-            while (__atomic_load_n(read + b, __ATOMIC_ACQUIRE) != s.mark) std::this_thread::yield();
+class Plan {
+  public:
+    // Room for `ints` words at data(); `in_arguments`: the call's launches take up to PLAN_WORDS of them by value.
+    int32_t open(int64_t ints, bool in_arguments) {
+        ints_ = ints;
+        by_value_ = in_arguments && ints <= PLAN_WORDS;
+        if (ints <= SMALL_WORDS) {
+            data_ = small_.w;
+            return GDN_OK;
+        }
+        lock_ = std::unique_lock<std::mutex>(g_fetch.mu);
+        slot_ = &g_fetch.slot[g_fetch.next];
+        FetchRing::Slot& s = *slot_;
+        if (s.host) {
+            uint32_t* const read = reinterpret_cast<uint32_t*>(s.host);
+            for (uint32_t b = 0; b < s.blocks; ++b)
+                while (__atomic_load_n(read + b, __ATOMIC_ACQUIRE) != s.mark) std::this_thread::yield();
+        }
+        const size_t bytes = (size_t)ints * sizeof(int32_t);
+        if (s.bytes < bytes) {
+            if (s.host) (void)hipHostFree(s.host);
+            s = FetchRing::Slot();
+            FetchRing::Slot fresh;
+            fresh.bytes = (std::max<size_t>(2 * bytes, 1 << 17) + FETCH_PIECE - 1) / FETCH_PIECE * FETCH_PIECE;
+            void* p = nullptr;
+            const hipError_t e = hipHostMalloc(&p, fresh.bytes + fresh.words_bytes(), hipHostMallocCoherent);
+            if (e != hipSuccess) return hip_err(e);
+            fresh.host = static_cast<char*>(p);
+            std::memset(p, 0, fresh.words_bytes());
+            s = fresh;
+        }
+        data_ = reinterpret_cast<int32_t*>(s.host + s.words_bytes());
+        return GDN_OK;
     }
-    if (s.bytes < bytes) {
-        if (s.host) (void)hipHostFree(s.host);
-        s.host = nullptr;
-        s.bytes = s.blocks = 0;
-        const size_t room = (std::max<size_t>(2 * bytes, 1 << 17) + FETCH_PIECE - 1) / FETCH_PIECE * FETCH_PIECE;
-        void* p = nullptr;
-        const hipError_t e = hipHostMalloc(&p, room + (words(room) * sizeof(uint32_t) + 255) / 256 * 256, hipHostMallocCoherent);
+    int32_t* data() { return data_; }
+    bool by_value() const { return by_value_; }
+    const PlanWords<true>& words() const { return arguments_; }
+    // What data() holds to the workspace, or, by value, to words().
+    int32_t send(void* workspace, hipStream_t stream) {
+        if (by_value_) {
+            std::memcpy(arguments_.w, small_.w, sizeof(int32_t) * (size_t)ints_);
+            return GDN_OK;
+        }
+        if (!slot_) return gdn::upload_plan(small_.w, sizeof(int32_t) * (size_t)ints_, workspace, stream);
+        FetchRing::Slot& s = *slot_;
+        const size_t bytes = (size_t)ints_ * sizeof(int32_t);
+        const uint32_t blocks = (uint32_t)((bytes + FETCH_PIECE - 1) / FETCH_PIECE), mark = s.mark + 1 == 0 ? 1 : s.mark + 1;
+        hipLaunchKernelGGL(attn_fetch_kernel, dim3(blocks), dim3(FETCH_THREADS), 0, stream, reinterpret_cast<const u32x4*>(data_),
+                           static_cast<u32x4*>(workspace), (int64_t)((bytes + 15) / 16), reinterpret_cast<uint32_t*>(s.host), mark);
+        const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return hip_err(e);
-        s.host = static_cast<char*>(p);
-        s.bytes = room;
-        std::memset(s.host, 0, words(room) * sizeof(uint32_t));
-        s.mark = 0;
+        s.mark = mark;
+        s.blocks = blocks;
+        g_fetch.next = (g_fetch.next + 1) % FETCH_RING;
+        lock_.unlock();
+        return GDN_OK;
     }
-    uint32_t* const read = reinterpret_cast<uint32_t*>(s.host);
-    char* const image = s.host + (words(s.bytes) * sizeof(uint32_t) + 255) / 256 * 256;
-    std::memcpy(image, img.data(), bytes);
-    const uint32_t blocks = (uint32_t)words(bytes), mark = s.mark + 1 == 0 ? 1 : s.mark + 1;
-    hipLaunchKernelGGL(attn_fetch_kernel, dim3(blocks), dim3(FETCH_THREADS), 0, stream, reinterpret_cast<const u32x4*>(image), static_cast<u32x4*>(dst),
-                       (int64_t)((bytes + 15) / 16), read, mark);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return hip_err(e);
-    s.mark = mark;
-    s.blocks = blocks;
-    return GDN_OK;
-}
 
-// A plan that fits goes by value, with `words` set from it; any other to the workspace.
-inline int32_t place_plan(const std::vector<int32_t>& img, PlanWords<true>& words, bool& by_value, void* workspace, hipStream_t stream) {
-    by_value = img.size() <= PLAN_WORDS;
-    if (!by_value) return send_image(img, workspace, stream);
-    std::copy(img.begin(), img.end(), words.w);
-    return GDN_OK;
-}
+  private:
+    struct Small { int32_t w[SMALL_WORDS]; } small_;
+    PlanWords<true> arguments_;
+    int32_t* data_ = nullptr;
+    int64_t ints_ = 0;
+    bool by_value_ = false;
+    FetchRing::Slot* slot_ = nullptr;
+    std::unique_lock<std::mutex> lock_;
+};
 
 int32_t rope_append(const attn_shape* s, const attn_rope* rope, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v,
                     int64_t ldv, int32_t n_req, const int32_t* cu, const int32_t* pos, const int32_t* start, const attn_pages* pages,
@@ -214,33 +253,41 @@ int32_t rope_append(const attn_shape* s, const attn_rope* rope, const void* q, i
     if (T == 0) return GDN_OK;
     // ---- the pages that get rows, and that nobody else in the call has them
     const int shift = shift_of(pages);
-    std::vector<int32_t> img((size_t)(4 * (int64_t)n_req + 1));
     PageSet written(pages->n_pages);
+    int64_t n_written = 0;
+    auto first_page = [&](int32_t r) { return start[r] >> shift; };
+    auto last_page = [&](int32_t r) { return (start[r] + len[r] - 1) >> shift; };
     for (int32_t r = 0; r < n_req; ++r) {
-        const int32_t p0 = start[r] >> shift;
-        img[1 + n_req + r] = start[r];
-        img[1 + 2 * n_req + r] = pos[r];
-        img[1 + 3 * n_req + r] = (int32_t)(img.size() - (4 * (size_t)n_req + 1)) - p0;
         if (len[r] == 0) continue;
-        const int32_t p1 = (start[r] + len[r] - 1) >> shift;
-        for (int32_t p = p0; p <= p1; ++p) {
-            if (!written.add(page_ids[page_cu[r] + p])) return GDN_ERR_SLOT_DUP;
-            img.push_back(page_ids[page_cu[r] + p]);
-        }
+        const int32_t n = last_page(r) - first_page(r) + 1;
+        if (!written.add(page_ids + page_cu[r] + first_page(r), n)) return GDN_ERR_SLOT_DUP;
+        n_written += n;
     }
+    bool shared = false;
     for (int32_t r = 0; r < n_req; ++r) {
-        const int32_t held = (start[r] + (1 << shift) - 1) >> shift, p0 = len[r] > 0 ? start[r] >> shift : held;
-        for (int32_t p = 0; p < p0; ++p)
-            if (written.has(page_ids[page_cu[r] + p])) return GDN_ERR_SLOT_DUP;
+        const int32_t held = (start[r] + (1 << shift) - 1) >> shift, p0 = len[r] > 0 ? first_page(r) : held;
+        for (int32_t p = 0; p < p0; ++p) shared |= written.has(page_ids[page_cu[r] + p]);
     }
-    for (int32_t r = 0; r <= n_req; ++r) img[r] = cu[r];
+    if (shared) return GDN_ERR_SLOT_DUP;
     if (!q || !k || !v || !k_pool || !v_pool || !q_out) return GDN_ERR_NULL;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(k_pool) || !aligned16(v_pool) || !aligned16(q_out)) return GDN_ERR_ALIGN;
     rc = check_workspace(s, n_req, T, page_cu[n_req], workspace, workspace_bytes);
     if (rc != GDN_OK) return rc;
-    PlanWords<true> words;
-    bool by_value;
-    rc = place_plan(img, words, by_value, workspace, stream);
+    Plan plan;
+    rc = plan.open(4 * (int64_t)n_req + 1 + n_written, true);
+    if (rc != GDN_OK) return rc;
+    int32_t* p = std::copy(cu, cu + n_req + 1, plan.data());
+    p = std::copy(start, start + n_req, p);
+    p = std::copy(pos, pos + n_req, p);
+    int32_t *ids = p + n_req, at = 0;
+    for (int32_t r = 0; r < n_req; ++r) {
+        p[r] = at - first_page(r);
+        if (len[r] == 0) continue;
+        const int32_t n = last_page(r) - first_page(r) + 1;
+        ids = std::copy_n(page_ids + page_cu[r] + first_page(r), n, ids);
+        at += n;
+    }
+    rc = plan.send(workspace, stream);
     if (rc != GDN_OK) return rc;
     a.q = q; a.k = k; a.v = v;
     a.q_out = static_cast<uint16_t*>(q_out);
@@ -263,8 +310,8 @@ int32_t rope_append(const attn_shape* s, const attn_rope* rope, const void* q, i
     a.amplitude = rope->amplitude;
     const dim3 grid((unsigned)((T + a.tokens - 1) / a.tokens)), block(ROPE_THREADS);
     const bool f32 = rope->in_dtype == GDN_F32;
-    if (by_value && f32) hipLaunchKernelGGL((attn_rope_kernel<true, true>), grid, block, 0, stream, a, words);
-    else if (by_value) hipLaunchKernelGGL((attn_rope_kernel<false, true>), grid, block, 0, stream, a, words);
+    if (plan.by_value() && f32) hipLaunchKernelGGL((attn_rope_kernel<true, true>), grid, block, 0, stream, a, plan.words());
+    else if (plan.by_value()) hipLaunchKernelGGL((attn_rope_kernel<false, true>), grid, block, 0, stream, a, plan.words());
     else if (f32) hipLaunchKernelGGL((attn_rope_kernel<true, false>), grid, block, 0, stream, a, PlanWords<false>());
     else hipLaunchKernelGGL((attn_rope_kernel<false, false>), grid, block, 0, stream, a, PlanWords<false>());
     return hip_err(hipGetLastError());
@@ -299,9 +346,13 @@ int32_t paged_prefill(const attn_shape* s, const void* q, const void* gate, int3
     UnitPlan plan;
     build_units(*s, n_req, len.data(), start, plan);
     CallImage im;
-    rc = make_image(s, plan, n_req, cu, start, len.data(), page_cu, page_ids, n_ids, im);
+    rc = lay_out_image(s, plan, n_req, n_ids, im);
     if (rc != GDN_OK) return rc;
-    rc = send_image(im.img, workspace, stream);
+    Plan image;
+    rc = image.open(im.ints, false);
+    if (rc != GDN_OK) return rc;
+    fill_image(s, plan, n_req, cu, start, len.data(), page_cu, page_ids, n_ids, im, image.data());
+    rc = image.send(workspace, stream);
     if (rc != GDN_OK) return rc;
     const int32_t* const d = static_cast<const int32_t*>(workspace);
     char* const parts = static_cast<char*>(workspace) + image_bytes(s, n_req, T, n_ids);
@@ -341,11 +392,6 @@ void launch_weights_merge(int d, const WeightArgs& a, const PlanWords<BY_VALUE>&
     else hipLaunchKernelGGL((attn_weights_merge_kernel<wgt_keys(128), BY_VALUE>), dim3(blocks), block, 0, stream, a, words);
 }
 
-// The work of one attn_key_weights call: units (a tile of keys and a run of the request's query rows) of either kernel, and the tiles whose rows are cut.
-struct WeightPlan {
-    std::vector<int32_t> wide, few, merge;       // WGT_REC, WGT_REC, WGT_MERGE ints each
-};
-
 // The rows of a tile are cut on a grid of `run` row tiles of 64, the first quarter of them four times finer, so that the chip is full and the short units,
 // which go last, fill its end: a workgroup takes as long as its row tiles and about WGT_START more for its keys, and WGT_SLOTS of them run at
 // once (two to a compute unit).
@@ -357,107 +403,138 @@ struct RowGrid {
     int64_t begin(int64_t i) const { return i < edge / fine ? i * fine : edge + (i - edge / fine) * run; }
 };
 
-void plan_weights(const attn_shape* s, int32_t n_req, const int32_t* cu, const int32_t* start, const int32_t* len, const int32_t* place, WeightPlan& out) {
-    const int G = s->H_q / s->H_kv, keys = wgt_keys(s->d);
-    auto is_few = [&](int32_t r) { return len[r] > 0 && (int64_t)len[r] * G <= WGT_FEW; };
-    auto tiles_of = [&](int32_t r) { return (int32_t)(((int64_t)start[r] + len[r] + keys - 1) / keys); };
-    auto row_tiles = [&](int32_t r) { return (int32_t)(((int64_t)len[r] * G + WGT_ROWS - 1) / WGT_ROWS); };
-    auto first_seen = [&](int32_t r, int32_t tile) {       // the first row tile that sees a key of the tile
-        return (int32_t)(std::max<int64_t>(0, (int64_t)tile * keys - start[r]) * G / WGT_ROWS);
-    };
-    // ---- units and row tiles in all if rows are cut every `run` row tiles
-    int64_t work = 0, most = 0;
-    auto units_of = [&](int64_t run, int64_t& cut) {
-        int64_t units = 0;
-        cut = work = 0;
+// The work of one attn_key_weights call: units (a tile of keys and a run of the request's query rows) of either kernel, and the tiles whose rows are cut.
+struct WeightPlan {
+    int64_t run = 1, most = 0;                     // row tiles per cut, and of the longest request
+    int64_t n_wide = 0, n_few = 0, n_cut = 0;      // units of either kernel, cut tiles
+};
+// A request's tiles.
+struct WeightRequest {
+    bool few;
+    int32_t G, start, tiles, rows, keys;
+    int64_t row_tiles;
+    WeightRequest(const attn_shape* s, int32_t start, int32_t len)
+        : G(s->H_q / s->H_kv), start(start), keys(wgt_keys(s->d)) {
+        few = len > 0 && (int64_t)len * G <= WGT_FEW;
+        tiles = (int32_t)(((int64_t)start + len + keys - 1) / keys);
+        rows = len * G;
+        row_tiles = (rows + WGT_ROWS - 1) / WGT_ROWS;
+    }
+    // the first row tile that sees a key of the tile
+    int64_t first_seen(int32_t tile) const { return std::max<int64_t>(0, (int64_t)tile * keys - start) * G / WGT_ROWS; }
+    // tiles that every row sees a key of
+    int32_t seen_by_all() const { return std::min<int32_t>(tiles, start / keys + 1); }
+};
+
+void plan_weights(const attn_shape* s, int32_t n_req, const int32_t* start, const int32_t* len, WeightPlan& out) {
+    // ---- units, parts of cut tiles, cut tiles and row tiles in all if rows are cut every `run` row tiles
+    int64_t work = 0;
+    auto count = [&](int64_t run, int64_t& units, int64_t& parts, int64_t& cut) {
+        units = parts = cut = work = 0;
         for (int32_t r = 0; r < n_req; ++r) {
-            if (is_few(r)) continue;
-            const int64_t m = row_tiles(r);
-            most = std::max(most, m);
+            const WeightRequest q(s, start[r], len[r]);
+            if (q.few) continue;
+            const int64_t m = q.row_tiles;
+            out.most = std::max(out.most, m);
             const RowGrid grid(run, m);
-            const int64_t whole = std::min<int64_t>(tiles_of(r), start[r] / keys + 1), parts = m > 0 ? grid.index(m - 1) + 1 : 1;   // tiles that every row sees a key of
-            units += whole * parts;
+            const int64_t whole = q.seen_by_all(), cuts = m > 0 ? grid.index(m - 1) + 1 : 1;
+            units += whole * cuts;
             work += whole * m;
-            if (parts > 1) cut += whole * parts;
-            for (int32_t t = (int32_t)whole; t < tiles_of(r); ++t) {
-                const int64_t f = first_seen(r, t), p = grid.index(m - 1) - grid.index(f) + 1;
+            if (cuts > 1) { parts += whole * cuts; cut += whole; }
+            for (int32_t t = (int32_t)whole; t < q.tiles; ++t) {
+                const int64_t f = q.first_seen(t), p = grid.index(m - 1) - grid.index(f) + 1;
                 units += p;
                 work += m - f;
-                if (p > 1) cut += p;
+                if (p > 1) { parts += p; ++cut; }
             }
         }
-        return units;
     };
-    int64_t cut = 0, units = units_of(INT32_MAX, cut), run = std::max<int64_t>(most, 1);
-    if (most > 1) {
-        auto cost = [&](int64_t c, int64_t n) {            // units that fill every gap but half of the last short one, and no less than one unit
-            const int64_t last = c < most ? std::max<int64_t>(1, c / 4) : c;
-            const double even = (double)((work + WGT_START * n) * s->H_kv) / WGT_SLOTS + 0.5 * (double)(last + WGT_START);
-            return std::max(even, (double)(c + WGT_START));
-        };
-        double best = cost(most, units);
-        for (int64_t c = most; c > 1;) {
-            c = c > 8 ? c * 3 / 4 : c - 1;
-            const int64_t n = units_of(c, cut);
-            if (cut * s->H_kv > WGT_PARTS) break;
-            if (cost(c, n) < 0.97 * best) {
-                best = cost(c, n);
-                run = c;
-                units = n;
-            }
+    for (int32_t r = 0; r < n_req; ++r) {
+        const WeightRequest q(s, start[r], len[r]);
+        if (q.few) out.n_few += q.tiles;
+    }
+    int64_t parts = 0;
+    count(INT32_MAX, out.n_wide, parts, out.n_cut);
+    out.run = std::max<int64_t>(out.most, 1);
+    if (out.most <= 1) return;
+    auto cost = [&](int64_t c, int64_t n) {                // units that fill every gap but half of the last short one, and no less than one unit
+        const int64_t last = c < out.most ? std::max<int64_t>(1, c / 4) : c;
+        const double even = (double)((work + WGT_START * n) * s->H_kv) / WGT_SLOTS + 0.5 * (double)(last + WGT_START);
+        return std::max(even, (double)(c + WGT_START));
+    };
+    double best = cost(out.most, out.n_wide);
+    for (int64_t c = out.most; c > 1;) {
+        c = c > 8 ? c * 3 / 4 : c - 1;
+        int64_t n, cut;
+        count(c, n, parts, cut);
+        if (parts * s->H_kv > WGT_PARTS) break;
+        if (cost(c, n) < 0.97 * best) {
+            best = cost(c, n);
+            out.run = c;
+            out.n_wide = n;
+            out.n_cut = cut;
         }
     }
-    // ---- the units, those of the same rows together (they read the same queries), the longest first
+}
+
+// The units, those of the same rows together (they read the same queries), the longest first, and the cut tiles.
+void list_weights(const attn_shape* s, int32_t n_req, const int32_t* cu, const int32_t* start, const int32_t* len, const int32_t* place,
+                  const WeightPlan& plan, int32_t* wide, int32_t* few, int32_t* merge) {
     struct Unit { int32_t r, kv0, lo, hi, part; };
     std::vector<Unit> list;
-    list.reserve((size_t)units);
+    list.reserve((size_t)plan.n_wide);
     std::vector<int32_t> base;
     int32_t slot = 0;
     for (int32_t r = 0; r < n_req; ++r) {
-        const int32_t tiles = tiles_of(r);
-        if (is_few(r)) {
-            for (int32_t t = 0; t < tiles; ++t)
-                out.few.insert(out.few.end(), {cu[r], len[r], start[r], place[r], t * keys, 0, len[r] * G, -1});
+        const WeightRequest q(s, start[r], len[r]);
+        if (q.few) {
+            for (int32_t t = 0; t < q.tiles; ++t, few += WGT_REC) {
+                const int32_t rec[WGT_REC] = {cu[r], len[r], start[r], place[r], t * q.keys, 0, q.rows, -1};
+                std::memcpy(few, rec, sizeof rec);
+            }
             continue;
         }
-        const int32_t m = row_tiles(r), rows = len[r] * G;
+        const int64_t m = q.row_tiles;
         if (m == 0) {
-            for (int32_t t = 0; t < tiles; ++t) list.push_back({r, t * keys, 0, 0, -1});
+            for (int32_t t = 0; t < q.tiles; ++t) list.push_back({r, t * q.keys, 0, 0, -1});
             continue;
         }
-        base.resize(tiles);
-        const RowGrid grid(run, m);
-        auto cut_of = [&](int32_t t) { return (int32_t)grid.index(first_seen(r, t)); };      // the first cut of rows that sees a key of tile t
+        const RowGrid grid(plan.run, m);
+        auto cut_of = [&](int32_t t) { return (int32_t)grid.index(q.first_seen(t)); };      // the first cut of rows that sees a key of tile t
         const int32_t cuts = (int32_t)grid.index(m - 1) + 1;
-        for (int32_t t = 0; t < tiles; ++t) {
+        base.resize(q.tiles);
+        for (int32_t t = 0; t < q.tiles; ++t) {
             const int32_t parts = cuts - cut_of(t);
             base[t] = slot - cut_of(t);                  // + the cut's number: its partial sum
             if (parts <= 1) continue;
-            out.merge.insert(out.merge.end(), {start[r] + len[r], start[r], place[r], t * keys, slot});
+            const int32_t rec[WGT_MERGE] = {start[r] + len[r], start[r], place[r], t * q.keys, slot};
+            std::memcpy(merge, rec, sizeof rec);
+            merge += WGT_MERGE;
             slot += parts;
         }
         for (int32_t c = cuts - 1; c >= 0; --c) {
             const int32_t lo = (int32_t)grid.begin(c), hi = (int32_t)std::min<int64_t>(grid.begin(c + 1), m);
-            for (int32_t t = 0; t < tiles; ++t) {
-                const int32_t f = std::max(lo, first_seen(r, t));
+            for (int32_t t = 0; t < q.tiles; ++t) {
+                const int32_t f = std::max(lo, (int32_t)q.first_seen(t));
                 if (f >= hi) break;
-                list.push_back({r, t * keys, f * WGT_ROWS, std::min(hi * WGT_ROWS, rows), cuts - cut_of(t) <= 1 ? -1 : base[t] + c});
+                list.push_back({r, t * q.keys, f * WGT_ROWS, std::min(hi * WGT_ROWS, q.rows), cuts - cut_of(t) <= 1 ? -1 : base[t] + c});
             }
         }
     }
-    if (!out.merge.empty()) out.merge.insert(out.merge.end(), {0, 0, 0, 0, slot});
+    if (plan.n_cut > 0) {                                 // one past the last partial sum
+        const int32_t rec[WGT_MERGE] = {0, 0, 0, 0, slot};
+        std::memcpy(merge, rec, sizeof rec);
+    }
     // by length, in classes: a counting sort that keeps their order
     constexpr int CLASSES = 64;
-    const int64_t top = std::max<int64_t>(1, std::min<int64_t>(run, most)) * WGT_ROWS;
-    std::vector<int32_t> at(CLASSES + 1, 0);
+    const int64_t top = std::max<int64_t>(1, std::min(plan.run, plan.most)) * WGT_ROWS;
+    int32_t at[CLASSES + 1] = {0};
     auto class_of = [&](const Unit& u) { return (int)(CLASSES - 1 - (int64_t)(u.hi - u.lo) * (CLASSES - 1) / top); };
     for (const Unit& u : list) ++at[class_of(u) + 1];
     for (int i = 0; i < CLASSES; ++i) at[i + 1] += at[i];
-    out.wide.resize(list.size() * WGT_REC);
     for (const Unit& u : list) {
-        int32_t* const rec = out.wide.data() + (size_t)at[class_of(u)]++ * WGT_REC;
-        const int32_t x[WGT_REC] = {cu[u.r], len[u.r], start[u.r], place[u.r], u.kv0, u.lo, u.hi, u.part};
-        std::copy(x, x + WGT_REC, rec);
+        const int32_t rec[WGT_REC] = {cu[u.r], len[u.r], start[u.r], place[u.r], u.kv0, u.lo, u.hi, u.part};
+        std::memcpy(wide + (size_t)at[class_of(u)]++ * WGT_REC, rec, sizeof rec);
     }
 }
 
@@ -477,8 +554,7 @@ int32_t key_weights(const attn_shape* s, const void* q, const float* lse, int32_
     for (int32_t r = 0; r < n_req; ++r) {
         const int32_t total = start[r] + len[r];
         rows += total;
-        for (int32_t p = 0; (int64_t)p << shift < total; ++p)
-            if (!written.add(page_ids[page_cu[r] + p])) return GDN_ERR_SLOT_DUP;
+        if (!written.add(page_ids + page_cu[r], ((int64_t)total + (1 << shift) - 1) >> shift)) return GDN_ERR_SLOT_DUP;
     }
     if (rows == 0) return GDN_OK;
     const int64_t T = cu[n_req];
@@ -493,20 +569,17 @@ int32_t key_weights(const attn_shape* s, const void* q, const float* lse, int32_
     for (int32_t r = 0; r < n_req; ++r)
         if (((int64_t)len[r] + 512) * G > INT32_MAX) return GDN_ERR_SHAPE;
     if (((int64_t)s->H_q * (WGT_ROWS + 1) + G) * s->d * 2 > INT32_MAX) return GDN_ERR_SHAPE;
-    WeightPlan plan;
-    plan_weights(s, n_req, cu, start, len.data(), page_cu, plan);
-    const int64_t n_wide = (int64_t)plan.wide.size() / WGT_REC, n_few = (int64_t)plan.few.size() / WGT_REC;
-    const int64_t n_cut = plan.merge.empty() ? 0 : (int64_t)plan.merge.size() / WGT_MERGE - 1;
+    WeightPlan units;
+    plan_weights(s, n_req, start, len.data(), units);
+    const int64_t n_wide = units.n_wide, n_few = units.n_few, n_cut = units.n_cut;
     if (std::max(n_wide, n_few) * s->H_kv > INT32_MAX) return GDN_ERR_COUNT;
-    std::vector<int32_t> img(plan.wide.size() + plan.few.size() + plan.merge.size() + (size_t)n_ids);
-    const int64_t few_at = (int64_t)plan.wide.size(), merge_at = few_at + (int64_t)plan.few.size(), ids_at = merge_at + (int64_t)plan.merge.size();
-    std::copy(plan.wide.begin(), plan.wide.end(), img.begin());
-    std::copy(plan.few.begin(), plan.few.end(), img.begin() + few_at);
-    std::copy(plan.merge.begin(), plan.merge.end(), img.begin() + merge_at);
-    std::copy(page_ids, page_ids + n_ids, img.begin() + ids_at);
-    PlanWords<true> words;
-    bool by_value;
-    rc = place_plan(img, words, by_value, workspace, stream);
+    const int64_t few_at = WGT_REC * n_wide, merge_at = few_at + WGT_REC * n_few, ids_at = merge_at + (n_cut > 0 ? WGT_MERGE * (n_cut + 1) : 0);
+    Plan plan;
+    rc = plan.open(ids_at + n_ids, true);
+    if (rc != GDN_OK) return rc;
+    list_weights(s, n_req, cu, start, len.data(), page_cu, units, plan.data(), plan.data() + few_at, plan.data() + merge_at);
+    std::copy(page_ids, page_ids + n_ids, plan.data() + ids_at);
+    rc = plan.send(workspace, stream);
     if (rc != GDN_OK) return rc;
     WeightArgs a;
     a.q = static_cast<const uint16_t*>(q);
@@ -543,7 +616,7 @@ int32_t key_weights(const attn_shape* s, const void* q, const float* lse, int32_
         }
         return hip_err(e);
     };
-    return by_value ? launch(words) : launch(PlanWords<false>());
+    return plan.by_value() ? launch(plan.words()) : launch(PlanWords<false>());
 }
 
 template <int D, bool BY_VALUE>
@@ -574,11 +647,15 @@ int32_t evict(const attn_shape* s, int32_t n_req, const int32_t* rows, const int
     rc = check_table(pages, n_req, new_page_cu, new_page_ids, [&](int32_t r) { return (int64_t)kept[r]; });
     if (rc != GDN_OK) return rc;
     const int32_t n_old = page_cu[n_req], n_new = new_page_cu[n_req];
+    rc = check_ids(pages, page_ids, n_old);
+    if (rc != GDN_OK) return rc;
+    rc = check_ids(pages, new_page_ids, n_new);
+    if (rc != GDN_OK) return rc;
     PageSet fresh(pages->n_pages);
-    for (int32_t i = 0; i < n_new; ++i)
-        if (!fresh.add(new_page_ids[i])) return GDN_ERR_SLOT_DUP;
-    for (int32_t i = 0; i < n_old; ++i)
-        if (fresh.has(page_ids[i])) return GDN_ERR_SLOT_HAZARD;
+    if (!fresh.add(new_page_ids, n_new)) return GDN_ERR_SLOT_DUP;
+    bool hazard = false;
+    for (int32_t i = 0; i < n_old; ++i) hazard |= fresh.has(page_ids[i]);
+    if (hazard) return GDN_ERR_SLOT_HAZARD;
     if (total == 0) return GDN_OK;
     if (!k_pool || !v_pool || !w_pool || !index) return GDN_ERR_NULL;
     if (!aligned16(k_pool) || !aligned16(v_pool)) return GDN_ERR_ALIGN;
@@ -587,8 +664,10 @@ int32_t evict(const attn_shape* s, int32_t n_req, const int32_t* rows, const int
     if (rc != GDN_OK) return rc;
 
     const int copied = gather_rows(s->d);              // rows per workgroup of the copy
-    std::vector<int32_t> img((size_t)(8 * (int64_t)n_req + 2 + n_old + n_new));
-    int32_t* p = img.data();
+    Plan plan;
+    rc = plan.open(8 * (int64_t)n_req + 2 + n_old + n_new, true);
+    if (rc != GDN_OK) return rc;
+    int32_t* p = plan.data();
     p = std::copy(rows, rows + n_req, p);
     p = std::copy(kept.begin(), kept.end(), p);
     p = std::copy(first, first + n_req, p);
@@ -603,9 +682,7 @@ int32_t evict(const attn_shape* s, int32_t n_req, const int32_t* rows, const int
     p = std::copy(page_ids, page_ids + n_old, p);
     p = std::copy(new_page_ids, new_page_ids + n_new, p);
     if (blocks > INT32_MAX || (int64_t)n_req * s->H_kv > INT32_MAX) return GDN_ERR_COUNT;
-    PlanWords<true> words;
-    bool by_value;
-    rc = place_plan(img, words, by_value, workspace, stream);
+    rc = plan.send(workspace, stream);
     if (rc != GDN_OK) return rc;
     EvictArgs a;
     a.k_pool = static_cast<uint16_t*>(k_pool);
@@ -630,7 +707,7 @@ int32_t evict(const attn_shape* s, int32_t n_req, const int32_t* rows, const int
         }
         return hip_err(hipGetLastError());
     };
-    return by_value ? launch(words) : launch(PlanWords<false>());
+    return plan.by_value() ? launch(plan.words()) : launch(PlanWords<false>());
 }
 
 // No exception leaves a C entry: host memory that runs out is a count too large.

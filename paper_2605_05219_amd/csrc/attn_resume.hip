@@ -217,9 +217,11 @@ int32_t attn_suffix_prefill(const attn_shape* s, const void* q, const void* k_ne
     UnitPlan plan;
     build_units(*s, n_req, len.data(), start_pos, plan);
     CallImage im;
-    rc = make_image(s, plan, n_req, cu_seqlens, start_pos, len.data(), seq_slot, nullptr, 0, im);
+    rc = lay_out_image(s, plan, n_req, 0, im);
     if (rc != GDN_OK) return rc;
-    rc = gdn::upload_plan(im.img.data(), im.img.size() * sizeof(int32_t), workspace, stream);
+    std::vector<int32_t> img((size_t)im.ints, 0);
+    fill_image(s, plan, n_req, cu_seqlens, start_pos, len.data(), seq_slot, nullptr, 0, im, img.data());
+    rc = gdn::upload_plan(img.data(), img.size() * sizeof(int32_t), workspace, stream);
     if (rc != GDN_OK) return rc;
     const int32_t* d = static_cast<const int32_t*>(workspace);
 
