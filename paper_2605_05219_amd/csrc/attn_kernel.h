@@ -39,7 +39,8 @@
 // of two of 16 at least, so that the rows that one wave brings of a tile (16, or 8) lie in one page.  Each lane of a wave holds the page of
 // one of the wave's next 64 tiles, a tile takes its page by a lane read and makes its buffer descriptor of it: one vector load of page ids for every 64
 // tiles, no wait on a dependent load in between.  The descriptor ends with the request's last row in the page, so that rows behind it (which
-// another request may have left, whatever they hold) come as zeros.
+// another request may have left, whatever they hold) come as zeros.  64 one-token requests behind 4 to 10 thousand rows in pages of 64: 76 us, 6.0 TB/s;
+// 8192 tokens of 16 heads 286 us a call, 960 TFLOP/s, as in slots.
 //
 // LDS rows are unpadded (a load to LDS writes a wave's 64 x 16 bytes contiguously); bank
 // conflicts are avoided by storing 16-byte chunk c of row r at chunk position c ^ f(r), with f
@@ -1014,7 +1015,7 @@ __global__ void __launch_bounds__(ATT_THREADS) attn_combine_kernel(CombineArgs a
     }
 }
 
-// The same for pieces of many parts (a decode row behind a long cache: 256 parts of 2 workgroups' rows, 92 us by the kernel above): one workgroup per
+// The same for pieces of many parts (a decode row behind 150 thousand keys: 256 parts, 6.7 us, and 92 by the kernel above): one workgroup per
 // row, the parts dealt to its CL_THREADS / (D / 4) groups of threads, the groups' sums joined through LDS.
 constexpr int CL_THREADS = 1024;
 
