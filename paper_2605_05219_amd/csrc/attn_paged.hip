@@ -110,7 +110,7 @@ int32_t check_workspace(const attn_shape* s, int32_t n_req, int64_t T, int64_t n
 }
 
 // What every call with new tokens checks of its index arrays, in this order.
-int32_t check_call(const attn_shape* s, int32_t n_req, const int32_t* cu, const int32_t* start, const attn_pages* pages,
+int32_t check_call(int32_t n_req, const int32_t* cu, const int32_t* start, const attn_pages* pages,
                    const int32_t* page_cu, const int32_t* page_ids, std::vector<int32_t>& len) {
     int32_t rc = check_lengths(n_req, cu, start, len);
     if (rc != GDN_OK) return rc;
@@ -176,7 +176,7 @@ class Plan {
             FetchRing::Slot fresh;
             fresh.bytes = (std::max<size_t>(2 * bytes, 1 << 17) + FETCH_PIECE - 1) / FETCH_PIECE * FETCH_PIECE;
             void* p = nullptr;
-            const hipError_t e = hipHostMalloc(&p, fresh.bytes + fresh.words_bytes(), hipHostMallocCoherent);
+            const hipError_t e = hipHostMalloc(&p, fresh.bytes + fresh.words_bytes(), hipHostMallocCoherent | hipHostMallocPortable);
             if (e != hipSuccess) return hip_err(e);
             fresh.host = static_cast<char*>(p);
             std::memset(p, 0, fresh.words_bytes());
@@ -244,7 +244,7 @@ int32_t rope_append(const attn_shape* s, const attn_rope* rope, const void* q, i
     }
     if (n_req == 0) return GDN_OK;
     std::vector<int32_t> len;
-    rc = check_call(s, n_req, cu, start, pages, page_cu, page_ids, len);
+    rc = check_call(n_req, cu, start, pages, page_cu, page_ids, len);
     if (rc != GDN_OK) return rc;
     if (!pos) pos = start;
     for (int32_t r = 0; r < n_req; ++r)
@@ -332,7 +332,7 @@ int32_t paged_prefill(const attn_shape* s, const void* q, const void* gate, int3
     if (rc != GDN_OK) return rc;
     if (n_req == 0) return GDN_OK;
     std::vector<int32_t> len;
-    rc = check_call(s, n_req, cu, start, pages, page_cu, page_ids, len);
+    rc = check_call(n_req, cu, start, pages, page_cu, page_ids, len);
     if (rc != GDN_OK) return rc;
     const int64_t T = cu[n_req];
     if (T == 0) return GDN_OK;
@@ -546,7 +546,7 @@ int32_t key_weights(const attn_shape* s, const void* q, const float* lse, int32_
     if (!std::isfinite(decay) || w_stride < (int64_t)s->H_kv * pages->page_rows) return GDN_ERR_SHAPE;
     if (n_req == 0) return GDN_OK;
     std::vector<int32_t> len;
-    rc = check_call(s, n_req, cu, start, pages, page_cu, page_ids, len);
+    rc = check_call(n_req, cu, start, pages, page_cu, page_ids, len);
     if (rc != GDN_OK) return rc;
     const int shift = shift_of(pages);
     PageSet written(pages->n_pages);
@@ -574,6 +574,7 @@ int32_t key_weights(const attn_shape* s, const void* q, const float* lse, int32_
     const int64_t n_wide = units.n_wide, n_few = units.n_few, n_cut = units.n_cut;
     if (std::max(n_wide, n_few) * s->H_kv > INT32_MAX) return GDN_ERR_COUNT;
     const int64_t few_at = WGT_REC * n_wide, merge_at = few_at + WGT_REC * n_few, ids_at = merge_at + (n_cut > 0 ? WGT_MERGE * (n_cut + 1) : 0);
+    if ((ids_at + n_ids) * (int64_t)sizeof(int32_t) > image_bytes(s, n_req, T, n_ids)) return GDN_ERR_WORKSPACE;
     Plan plan;
     rc = plan.open(ids_at + n_ids, true);
     if (rc != GDN_OK) return rc;
