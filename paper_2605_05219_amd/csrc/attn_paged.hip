@@ -5,7 +5,6 @@
 #include <cmath>
 #include <mutex>
 #include <new>
-#include <stdexcept>
 #include <thread>
 #include <vector>
 
@@ -375,7 +374,7 @@ int32_t paged_prefill(const attn_shape* s, const void* q, const void* gate, int3
 template <int D, bool BY_VALUE>
 void launch_weights_d(bool few, const WeightArgs& a, const PlanWords<BY_VALUE>& words, unsigned blocks, hipStream_t stream) {
     if (few) hipLaunchKernelGGL((attn_weights_few_kernel<D, BY_VALUE>), dim3(blocks), dim3(WGT_THREADS), 0, stream, a, words);
-    else hipLaunchKernelGGL((attn_weights_kernel<D, BY_VALUE>), dim3(blocks), dim3(WGT_THREADS), 0, stream, a, words);
+    else hipLaunchKernelGGL((attn_weights_kernel<D, BY_VALUE>), dim3(blocks), dim3(64 * wgt_waves(D)), 0, stream, a, words);
 }
 template <bool BY_VALUE>
 void launch_weights(int d, bool few, const WeightArgs& a, const PlanWords<BY_VALUE>& words, unsigned blocks, hipStream_t stream) {
@@ -711,14 +710,12 @@ int32_t evict(const attn_shape* s, int32_t n_req, const int32_t* rows, const int
     return plan.by_value() ? launch(plan.words()) : launch(PlanWords<false>());
 }
 
-// No exception leaves a C entry: host memory that runs out is a count too large.
+// No exception leaves a C entry: what is thrown here is host memory that runs out, for a call of too many entries.
 template <typename F>
 int32_t guarded(F f) {
     try {
         return f();
-    } catch (const std::bad_alloc&) {
-        return GDN_ERR_COUNT;
-    } catch (const std::length_error&) {
+    } catch (...) {
         return GDN_ERR_COUNT;
     }
 }

@@ -210,15 +210,16 @@ __global__ void __launch_bounds__(ROPE_THREADS) attn_rope_kernel(RopeArgs a, Pla
 }
 
 // ---------------------------------------------------------------- the weight that cached rows gather
-// A key's sum runs over query rows, so keys stay and queries pass: each of the four waves of a workgroup holds 64 keys (32 at d = 256) in registers as
-// matrix operands, tiles of 64 query rows (tokens x heads of the group, row = token * G + head) go through two LDS stages, brought by loads to LDS a
+// A key's sum runs over query rows, so keys stay and queries pass: each of the four waves of a workgroup holds 64 keys (32 at d = 256; at d = 64 there are eight
+// waves with 32 each, 8192 tokens of 16 heads 126 -> 117 us, which at d = 128 gains 2 % or loses 3) in registers as matrix operands, tiles of 64 query rows (tokens x heads of the group, row = token * G + head) go through two LDS stages, brought by loads to LDS a
 // tile ahead.  S[row][key] puts a key into a lane's column and 16 of 32 rows into its registers: the sum over rows needs no
 // exchange between lanes but one with the other half at the end, and no atomics.  A row's log-sum-exp comes by LDS in units of log2.
 // Bound: matrix and vector units alike (8192 tokens of 16 heads, d = 128: 55 us of products and 70 us of multiply-adds, exponentials and
 // sums at 2.4 GHz), so a wave computes the products of the next 32 rows in between the exponentials of the last (in turn they took 40 % more).  The call takes
 // 157 us (875 TFLOP/s): matrix units busy 0.40, vector units 0.50 of 341 k clocks at a power-limited 2.1 GHz, two waves to a SIMD (registers); a unit's
 // start (4 us, three rounds) and the last round cost 25 of them.  500 tokens behind 7700 rows, d = 64: 25 us.
-constexpr int WGT_THREADS = 256;
+constexpr int WGT_THREADS = 256;      // of the few-rows kernel
+__host__ __device__ constexpr int wgt_waves(int d) { return d == 64 ? 8 : 4; }
 __host__ __device__ constexpr int wgt_keys(int d) { return d == 256 ? 128 : 256; }   // keys per workgroup
 constexpr int WGT_ROWS = 64;          // query rows per tile
 constexpr int WGT_PARTS = 16384;      // partial sums (of a tile of keys, a part of its rows, a head) of a call, at most
@@ -245,7 +246,7 @@ struct WeightArgs {
 template <int D>
 struct WeightSmem {
     static constexpr int CPR = D / 8, ROW_BYTES = D * 2, TILE_BYTES = WGT_ROWS * ROW_BYTES;
-    static constexpr int PPW = TILE_BYTES / 4096;       // 1 KiB loads per wave and tile
+    static constexpr int PPW = TILE_BYTES / (1024 * wgt_waves(D));       // 1 KiB loads per wave and tile
     static __device__ __forceinline__ int f(int row) { return CPR >= 16 ? (row & 15) : ((row >> 1) & 7); }
 };
 
@@ -255,9 +256,9 @@ __device__ __forceinline__ void store_weight(const WeightArgs& a, const int32_t*
 }
 
 template <int D, bool BY_VALUE>
-__global__ void __launch_bounds__(WGT_THREADS, 2) attn_weights_kernel(WeightArgs a, PlanWords<BY_VALUE> words) {
+__global__ void __launch_bounds__(64 * wgt_waves(D), wgt_waves(D) / 2) attn_weights_kernel(WeightArgs a, PlanWords<BY_VALUE> words) {
     typedef WeightSmem<D> SM;
-    constexpr int KB = D / 16, KEYS = wgt_keys(D), NB = KEYS / 128;      // NB: blocks of 32 keys per wave
+    constexpr int KB = D / 16, KEYS = wgt_keys(D), NB = KEYS / (32 * wgt_waves(D));      // NB: blocks of 32 keys per wave
     constexpr int AHEAD_TILES = D == 256 ? 1 : 2;    // a tile is asked for this many tiles ahead (three stages at d = 256 would leave one workgroup to a compute unit)
     __shared__ __attribute__((aligned(1024))) char stage0[SM::TILE_BYTES], stage1[SM::TILE_BYTES], stage2[AHEAD_TILES == 2 ? SM::TILE_BYTES : 16];
     __shared__ __attribute__((aligned(16))) float neg_lse[4][WGT_ROWS];   // -lse log2(e); rows past the end -inf
