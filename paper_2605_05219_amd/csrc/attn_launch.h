@@ -76,8 +76,12 @@ hipError_t launch_attn_d(int d, int NH, const Args& a, unsigned blocks, hipStrea
 
 template <int D, typename OT, bool LSE, typename Args>
 hipError_t launch_narrow(bool nt, const Args& a, unsigned blocks, hipStream_t stream) {
-    if (nt) hipLaunchKernelGGL((attn_narrow_kernel<D, OT, true, Args, LSE>), dim3(blocks), dim3(ATT_THREADS), 0, stream, a);
-    else hipLaunchKernelGGL((attn_narrow_kernel<D, OT, false, Args, LSE>), dim3(blocks), dim3(ATT_THREADS), 0, stream, a);
+    if constexpr (!std::is_same<Args, PagedValueArgs>::value)      // (page tables that fit the arguments are of small calls)
+        if (nt) {
+            hipLaunchKernelGGL((attn_narrow_kernel<D, OT, true, Args, LSE>), dim3(blocks), dim3(ATT_THREADS), 0, stream, a);
+            return hipGetLastError();
+        }
+    hipLaunchKernelGGL((attn_narrow_kernel<D, OT, false, Args, LSE>), dim3(blocks), dim3(ATT_THREADS), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -90,20 +94,20 @@ hipError_t launch_narrow_d(int d, bool nt, const Args& a, unsigned blocks, hipSt
     }
 }
 
-template <int D, typename OT, bool LSE, bool LONG>
-hipError_t launch_combine(bool by_row, const CombineArgs& a, hipStream_t stream) {
+template <int D, typename OT, bool LSE, bool LONG, typename Args>
+hipError_t launch_combine(bool by_row, const Args& a, hipStream_t stream) {
     const dim3 grid((unsigned)(a.set[0].blocks + a.set[1].blocks));
     if constexpr (LONG)
         if (by_row) {
-            hipLaunchKernelGGL((attn_combine_long_kernel<D, OT, LSE>), grid, dim3(CL_THREADS), 0, stream, a);
+            hipLaunchKernelGGL((attn_combine_long_kernel<D, OT, LSE, Args>), grid, dim3(CL_THREADS), 0, stream, a);
             return hipGetLastError();
         }
-    hipLaunchKernelGGL((attn_combine_kernel<D, OT, LSE>), grid, dim3(ATT_THREADS), 0, stream, a);
+    hipLaunchKernelGGL((attn_combine_kernel<D, OT, LSE, Args>), grid, dim3(ATT_THREADS), 0, stream, a);
     return hipGetLastError();
 }
 
-template <typename OT, bool LSE, bool LONG>
-hipError_t launch_combine_d(int d, bool by_row, const CombineArgs& a, hipStream_t stream) {
+template <typename OT, bool LSE, bool LONG, typename Args>
+hipError_t launch_combine_d(int d, bool by_row, const Args& a, hipStream_t stream) {
     switch (d) {
         case 64: return launch_combine<64, OT, LSE, LONG>(by_row, a, stream);
         case 128: return launch_combine<128, OT, LSE, LONG>(by_row, a, stream);
@@ -443,10 +447,10 @@ int32_t launch_wide_units(const attn_shape* s, const UnitPlan& plan, const CallI
 // (one-token requests behind 9000 keys, by such rows / by threads of four columns: 4 requests, 21 parts, 19.5 / 21.4 us; 12 requests 32.4 / 35.0; 16 of 16
 // parts 37.0 / 37.3; 32 of 8 parts 60.4 / 58.7, 48 88 / 84).
 constexpr int LONG_PARTS = 16;
-template <bool LSE, bool LONG>
+// Args: CombineArgs, or CombineValueArgs with its words set.
+template <bool LSE, bool LONG, typename Args>
 int32_t launch_merge(const attn_shape* s, const UnitPlan& plan, const CallImage& im, const int32_t* d, const AttnArgs& a, float* lse,
-                     const float* part_le, hipStream_t stream) {
-    CombineArgs ca;
+                     const float* part_le, Args& ca, hipStream_t stream) {
     ca.part_o = a.part_o;
     ca.part_ml = a.part_ml;
     ca.gate = a.gate;

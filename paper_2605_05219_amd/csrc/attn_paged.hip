@@ -152,10 +152,10 @@ FetchRing g_fetch;
 
 class Plan {
   public:
-    // Room for `ints` words at data(); `in_arguments`: the call's launches take up to PLAN_WORDS of them by value.
-    int32_t open(int64_t ints, bool in_arguments) {
+    // Room for `ints` words at data(); up to PLAN_WORDS of them go by value.
+    int32_t open(int64_t ints) {
         ints_ = ints;
-        by_value_ = in_arguments && ints <= PLAN_WORDS;
+        by_value_ = ints <= PLAN_WORDS;
         if (ints <= SMALL_WORDS) {
             data_ = small_.w;
             return GDN_OK;
@@ -273,7 +273,7 @@ int32_t rope_append(const attn_shape* s, const attn_rope* rope, const void* q, i
     rc = check_workspace(s, n_req, T, page_cu[n_req], workspace, workspace_bytes);
     if (rc != GDN_OK) return rc;
     Plan plan;
-    rc = plan.open(4 * (int64_t)n_req + 1 + n_written, true);
+    rc = plan.open(4 * (int64_t)n_req + 1 + n_written);
     if (rc != GDN_OK) return rc;
     int32_t* p = std::copy(cu, cu + n_req + 1, plan.data());
     p = std::copy(start, start + n_req, p);
@@ -316,12 +316,12 @@ int32_t rope_append(const attn_shape* s, const attn_rope* rope, const void* q, i
     return hip_err(hipGetLastError());
 }
 
-template <bool LSE>
-int32_t launch_paged(const attn_shape* s, const UnitPlan& plan, const CallImage& im, const int32_t* d, bool nt, PagedArgs& a, hipStream_t stream) {
+template <bool LSE, typename Args, typename Merge>
+int32_t launch_paged(const attn_shape* s, const UnitPlan& plan, const CallImage& im, const int32_t* d, bool nt, Args& a, Merge& merge, hipStream_t stream) {
     int32_t rc;
     if (im.n_narrow > 0 && (rc = launch_narrow_units<LSE>(s, nt, im, a, stream)) != GDN_OK) return rc;
     if (im.n_wide > 0 && (rc = launch_wide_units<LSE>(s, plan, im, a, stream)) != GDN_OK) return rc;
-    return launch_merge<LSE, true>(s, plan, im, d, a, a.lse, a.part_le, stream);
+    return launch_merge<LSE, true>(s, plan, im, d, a, a.lse, a.part_le, merge, stream);
 }
 
 int32_t paged_prefill(const attn_shape* s, const void* q, const void* gate, int32_t n_req, const int32_t* cu, const int32_t* start,
@@ -348,14 +348,15 @@ int32_t paged_prefill(const attn_shape* s, const void* q, const void* gate, int3
     rc = lay_out_image(s, plan, n_req, n_ids, im);
     if (rc != GDN_OK) return rc;
     Plan image;
-    rc = image.open(im.ints, false);
+    rc = image.open(im.ints);
     if (rc != GDN_OK) return rc;
     fill_image(s, plan, n_req, cu, start, len.data(), page_cu, page_ids, n_ids, im, image.data());
     rc = image.send(workspace, stream);
     if (rc != GDN_OK) return rc;
-    const int32_t* const d = static_cast<const int32_t*>(workspace);
+    // by value, the arrays begin at offset 0 of the words
+    const int32_t* const d = image.by_value() ? nullptr : static_cast<const int32_t*>(workspace);
     char* const parts = static_cast<char*>(workspace) + image_bytes(s, n_req, T, n_ids);
-    PagedArgs a;
+    PagedValueArgs a;
     a.q = static_cast<const uint16_t*>(q);
     a.gate = static_cast<const uint16_t*>(gate);
     a.k_cache = static_cast<const uint16_t*>(k_pool);
@@ -367,8 +368,16 @@ int32_t paged_prefill(const attn_shape* s, const void* q, const void* gate, int3
     a.page_shift = shift_of(pages);
     a.lse = lse;
     a.part_le = reinterpret_cast<float*>(parts + part_ml_bytes() + part_o_bytes(s->d));
+    if (image.by_value()) {
+        CombineValueArgs merge;
+        std::memcpy(a.words, image.data(), sizeof(int32_t) * (size_t)im.ints);
+        std::memcpy(merge.words, image.data(), sizeof(int32_t) * (size_t)im.ints);
+        return lse ? launch_paged<true>(s, plan, im, d, false, a, merge, stream) : launch_paged<false>(s, plan, im, d, false, a, merge, stream);
+    }
     const bool nt = narrow_nt(s, plan, n_req, start, len.data());
-    return lse ? launch_paged<true>(s, plan, im, d, nt, a, stream) : launch_paged<false>(s, plan, im, d, nt, a, stream);
+    CombineArgs merge;
+    PagedArgs& in_memory = a;
+    return lse ? launch_paged<true>(s, plan, im, d, nt, in_memory, merge, stream) : launch_paged<false>(s, plan, im, d, nt, in_memory, merge, stream);
 }
 
 template <int D, bool BY_VALUE>
@@ -575,7 +584,7 @@ int32_t key_weights(const attn_shape* s, const void* q, const float* lse, int32_
     const int64_t few_at = WGT_REC * n_wide, merge_at = few_at + WGT_REC * n_few, ids_at = merge_at + (n_cut > 0 ? WGT_MERGE * (n_cut + 1) : 0);
     if ((ids_at + n_ids) * (int64_t)sizeof(int32_t) > image_bytes(s, n_req, T, n_ids)) return GDN_ERR_WORKSPACE;
     Plan plan;
-    rc = plan.open(ids_at + n_ids, true);
+    rc = plan.open(ids_at + n_ids);
     if (rc != GDN_OK) return rc;
     list_weights(s, n_req, cu, start, len.data(), page_cu, units, plan.data(), plan.data() + few_at, plan.data() + merge_at);
     std::copy(page_ids, page_ids + n_ids, plan.data() + ids_at);
@@ -665,7 +674,7 @@ int32_t evict(const attn_shape* s, int32_t n_req, const int32_t* rows, const int
 
     const int copied = gather_rows(s->d);              // rows per workgroup of the copy
     Plan plan;
-    rc = plan.open(8 * (int64_t)n_req + 2 + n_old + n_new, true);
+    rc = plan.open(8 * (int64_t)n_req + 2 + n_old + n_new);
     if (rc != GDN_OK) return rc;
     int32_t* p = plan.data();
     p = std::copy(rows, rows + n_req, p);

@@ -10,7 +10,6 @@ namespace attn {
 
 // A call's index arrays ("plan"): in device memory, or by value in the arguments of its launches where they are few words, which spares the
 // launch that would write them there (one token 10.4 against 12.7 us, an eviction of 8200 rows 20.3 against 22.4).
-constexpr int PLAN_WORDS = 640;
 template <bool BY_VALUE>
 struct PlanWords {
     int32_t w[BY_VALUE ? PLAN_WORDS : 1];
@@ -217,7 +216,7 @@ __global__ void __launch_bounds__(ROPE_THREADS) attn_rope_kernel(RopeArgs a, Pla
 // Bound: matrix and vector units alike (8192 tokens of 16 heads, d = 128: 55 us of products and 70 us of multiply-adds, exponentials and
 // sums at 2.4 GHz), so a wave computes the products of the next 32 rows in between the exponentials of the last (in turn they took 40 % more).  The call takes
 // 157 us (875 TFLOP/s): matrix units busy 0.40, vector units 0.50 of 341 k clocks at a power-limited 2.1 GHz, two waves to a SIMD (registers); a unit's
-// start (4 us, three rounds) and the last round cost 25 of them.  500 tokens behind 7700 rows, d = 64: 25 us.
+// start (4 us, three rounds) and the last round cost 25 of them.  500 tokens behind 7700 rows, d = 64: 24 us.
 constexpr int WGT_THREADS = 256;      // of the few-rows kernel
 __host__ __device__ constexpr int wgt_waves(int d) { return d == 64 ? 8 : 4; }
 __host__ __device__ constexpr int wgt_keys(int d) { return d == 256 ? 128 : 256; }   // keys per workgroup

@@ -260,7 +260,8 @@ int32_t attn_suffix_prefill(const attn_shape* s, const void* q, const void* k_ne
         rc = launch_wide_units<false>(s, plan, im, static_cast<AttnArgs&>(a), stream);
         if (rc != GDN_OK) return rc;
     }
-    return launch_merge<false, false>(s, plan, im, d, a, nullptr, nullptr, stream);
+    CombineArgs ca;
+    return launch_merge<false, false>(s, plan, im, d, a, nullptr, nullptr, ca, stream);
 }
 
 int32_t attn_tune_split(int32_t allow) { return g_allow_split.exchange(allow != 0); }
