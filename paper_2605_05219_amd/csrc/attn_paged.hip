@@ -4,7 +4,6 @@
 #include <algorithm>
 #include <cmath>
 #include <mutex>
-#include <new>
 #include <thread>
 #include <vector>
 
@@ -124,10 +123,10 @@ int32_t check_front(const attn_shape* s, int32_t n_req, const attn_pages* pages)
     return check_pages(s, pages);
 }
 
-// ---- a call's plan (its index arrays) to the device.  What fits goes by value, in the arguments of the call's launches where those take it, or of a
-// small launch (gdn::upload_plan).  Page tables are larger, and a copy of more than 16 KiB takes the stream 20 us between two kernels: these are
-// written into pinned memory, out of which a launch of ours reads them (4 us for 90 KB).  The buffers form a ring; a workgroup that has read its
-// piece says so in a word of the buffer, and a call that comes round to a buffer waits (on the host) for all of them.
+// ---- a call's plan (its index arrays) to the device.  Up to PLAN_WORDS go by value, in the arguments of the call's launches, and up to SMALL_WORDS in those
+// of a small launch (gdn::upload_plan).  Longer page tables cost more: a copy of more than 16 KiB takes the stream 20 us between two kernels.  These
+// are written into pinned memory, out of which a launch of ours reads them (4 us for 90 KB).  The buffers form a ring; a workgroup that has read
+// its piece says so in a word of the buffer, and a call that comes round to a buffer waits (on the host) for all of them.
 constexpr int FETCH_RING = 8, FETCH_THREADS = 256, FETCH_PIECE = 16 * FETCH_THREADS;   // bytes per workgroup
 constexpr int SMALL_WORDS = 1792;
 

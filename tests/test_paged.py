@@ -682,3 +682,82 @@ def test_a_session_of_prompts_decoding_and_eviction_matches_the_oracle():
                     held[r][x] = np.stack([held[r][x][idx[g], g] for g in range(H_kv)], axis=1)
                 assert layer.rows[r] == 40 and len(layer.pages[r]) == 3 and layer.pos[r] == pos[r]
     assert len(layer.free) + sum(len(p) for p in layer.pages) == 40
+
+
+@pytest.mark.gpu
+def test_many_calls_with_long_page_tables_in_a_row_keep_their_own_plans():
+    """More calls than there are staging buffers, none waited for, each with page tables of its own (and all too long for the arguments)."""
+    import torch
+    rng = np.random.default_rng(7)
+    c = Paged(71, 4, 2, 64, 16, [1] * 24, [int(x) for x in rng.integers(1200, 2400, 24)]).fill()
+    assert c.page_ids.size > 1792
+    q = c.bf16(c.T, 4, 64)
+    want, wz = run_attend(c, q, None, "f32")
+    torch.cuda.synchronize()
+    qd, ws = c.dev(q), c.workspace()
+    sh = AT.make_attn_shape(4, 2, 64, "f32")
+    outs = []
+    for i in range(30):                     # the requests in another order every time
+        order = rng.permutation(24)
+        cu = np.arange(25, dtype=np.int32)
+        tables = [c.table[r] for r in order]
+        tcu = np.concatenate([[0], np.cumsum([t.size for t in tables])]).astype(np.int32)
+        o, z = torch.zeros(24, 4, 64, device="cuda"), torch.zeros(24, 4, device="cuda")
+        at = torch.from_numpy(order).cuda()
+        w = torch.zeros(c.k_np.shape[0], 2, 16, device="cuda") if i % 3 == 0 else None
+        PG.attn_paged_prefill(sh, qd[at].contiguous(), None, cu, np.asarray(c.starts)[order], c.k_pool, c.v_pool, tcu, np.concatenate(tables), o, z, ws)
+        if w is not None:
+            PG.attn_key_weights(sh, qd[at].contiguous(), z, cu, np.asarray(c.starts)[order], c.k_pool, tcu, np.concatenate(tables), 1.0, None, w, ws)
+        outs.append((at, o, z, w))
+    torch.cuda.synchronize()
+    for at, o, z, w in outs:
+        assert torch.equal(o, want[at]) and torch.equal(z, wz[at])
+        if w is not None:                   # every row of queries spreads a weight of one over its request's rows
+            page, row = c.place(3, c.total[3])
+            assert abs(float(w[torch.from_numpy(page.astype(np.int64)).cuda(), :, torch.from_numpy(row).cuda()].sum()) - 4) <= 1e-3
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("seed", range(8))
+def test_random_calls_of_the_weights_and_the_eviction_that_follows(seed):
+    """Ragged batches of both kinds of requests, against the oracle, and an eviction by the weights that came out."""
+    import torch
+    rng = np.random.default_rng(900 + seed)
+    H_q, H_kv = [(16, 2), (8, 8), (6, 2), (32, 4), (8, 1), (4, 4), (20, 4), (16, 4)][seed]
+    d, P, R = int(rng.choice([64, 128, 256])), int(rng.choice([16, 32, 128, 256])), int(rng.integers(2, 7))
+    lens = [int(x) for x in rng.choice([0, 1, 2, 63, 64, 65, 300, 700], R)]
+    starts = [int(x) for x in rng.integers(0, 2000, R)]
+    lens[0] = max(lens[0], 1)
+    kept = [min(s + n, int(rng.integers(1, 600))) for s, n in zip(starts, lens)]
+    new_n = [-(-m // P) for m in kept]
+    c = Paged(950 + seed, H_q, H_kv, d, P, lens, starts, extra=sum(new_n)).fill()
+    q = c.bf16(c.T, H_q, d, s=1.5)
+    lse = np.zeros((c.T, H_q), np.float32)
+    for r in range(R):
+        if lens[r]:
+            lse[c.cu[r]:c.cu[r + 1]] = po.row_lse(f64(q[c.cu[r]:c.cu[r + 1]]), f64(c.k_rows[r]), starts[r], d ** -0.5)
+    w = torch.full((c.k_np.shape[0], H_kv, P), float("nan"), device="cuda")
+    ws = c.workspace(ids=c.page_ids.size + sum(new_n))
+    PG.attn_key_weights(c.shape, c.dev(q), torch.from_numpy(lse).cuda(), c.cu, starts, c.k_pool, c.page_cu, c.page_ids, 1.0, None, w, ws)
+    got = w.cpu().numpy()
+    rtol = np.expm1(logit_error(c, q) + 2.0 ** -22 * (1 + np.abs(lse).max())) + (max(lens) * (H_q // H_kv) + 8) * 2.0 ** -24
+    spare = list(c.spare)
+    new_table = [np.array([spare.pop() for _ in range(m)], np.int32) for m in new_n]
+    new_cu = np.concatenate([[0], np.cumsum(new_n)]).astype(np.int32)
+    index = torch.zeros(max(1, sum(kept) * H_kv), dtype=torch.int32, device="cuda")
+    first, recent = [min(2, m) for m in kept], [min(5, max(0, m - 2)) for m in kept]
+    PG.attn_evict(c.shape, c.total, kept, first, recent, c.k_pool, c.v_pool, w, c.page_cu, c.page_ids, new_cu,
+                  np.concatenate(new_table + [np.zeros(0, np.int32)]), index, ws)
+    idx, k_got, at = index.cpu().numpy(), bits_of(c.k_pool), 0
+    for r in range(R):
+        page, row = c.place(r, c.total[r])
+        x = got[page, :, row].astype(np.float64)
+        s = slice(c.cu[r], c.cu[r + 1])
+        ref = po.key_weights(f64(q[s]), lse[s], f64(c.k_rows[r]), starts[r], d ** -0.5, 1.0, None) if lens[r] else np.zeros((starts[r], H_kv))
+        assert (np.abs(x - ref) <= rtol * ref).all(), r
+        to_page, to_row = c.place(r, kept[r], new_table[r])
+        for g in range(H_kv):
+            want = po.rows_kept(x[:, g], kept[r], first[r], recent[r])
+            assert np.array_equal(idx[at:at + kept[r]], want), (r, g)
+            assert np.array_equal(k_got[to_page, g, to_row], c.k_rows[r][want, g])
+            at += kept[r]
