@@ -3,7 +3,8 @@
  * append, attention of a chunk of new tokens, the attention weight every cached row gathers, and eviction by that
  * weight.  Same library and conventions as attn_resume.h (host / device pointers named per argument, validation
  * before anything is enqueued, negative error codes, no device allocation, no stream synchronisation except the wait for an
- * earlier call's plan upload to leave its pinned staging buffer).
+ * earlier call's plan upload to leave its pinned staging buffer).  Under graph capture, a call whose index arrays need that
+ * buffer (more than 1792 words of page ids and plan) is refused with the capture's error; a replay of a smaller one repeats its arrays.
  *
  * The cache.  A pool of n_pages pages per tensor; page p is at pool + p * page_stride (elements) and holds
  * page_rows rows of every key/value head, [H_kv][page_rows][d]: keys in bf16, values in fp16 (as in attn_resume.h: the

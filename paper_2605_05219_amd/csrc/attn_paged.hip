@@ -126,7 +126,8 @@ int32_t check_front(const attn_shape* s, int32_t n_req, const attn_pages* pages)
 // ---- a call's plan (its index arrays) to the device.  Up to PLAN_WORDS go by value, in the arguments of the call's launches, and up to SMALL_WORDS in those
 // of a small launch (gdn::upload_plan).  Longer page tables cost more: a copy of more than 16 KiB takes the stream 20 us between two kernels.  These
 // are written into pinned memory, out of which a launch of ours reads them (4 us for 90 KB).  The buffers form a ring; a workgroup that has read
-// its piece says so in a word of the buffer, and a call that comes round to a buffer waits (on the host) for all of them.
+// its piece says so in a word of the buffer, and a call that comes round to a buffer waits (on the host) for all of them.  A graph's replay would read
+// what a later call wrote there, and its capture reads nothing that the wait could see: such a call under capture is refused.
 constexpr int FETCH_RING = 8, FETCH_THREADS = 256, FETCH_PIECE = 16 * FETCH_THREADS;   // bytes per workgroup
 constexpr int SMALL_WORDS = 1792;
 
@@ -152,13 +153,17 @@ FetchRing g_fetch;
 class Plan {
   public:
     // Room for `ints` words at data(); up to PLAN_WORDS of them go by value.
-    int32_t open(int64_t ints) {
+    int32_t open(int64_t ints, hipStream_t stream) {
         ints_ = ints;
         by_value_ = ints <= PLAN_WORDS;
         if (ints <= SMALL_WORDS) {
             data_ = small_.w;
             return GDN_OK;
         }
+        hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+        const hipError_t asked = hipStreamIsCapturing(stream, &capture);
+        if (asked != hipSuccess) return hip_err(asked);
+        if (capture != hipStreamCaptureStatusNone) return hip_err(hipErrorStreamCaptureUnsupported);
         lock_ = std::unique_lock<std::mutex>(g_fetch.mu);
         slot_ = &g_fetch.slot[g_fetch.next];
         FetchRing::Slot& s = *slot_;
@@ -272,7 +277,7 @@ int32_t rope_append(const attn_shape* s, const attn_rope* rope, const void* q, i
     rc = check_workspace(s, n_req, T, page_cu[n_req], workspace, workspace_bytes);
     if (rc != GDN_OK) return rc;
     Plan plan;
-    rc = plan.open(4 * (int64_t)n_req + 1 + n_written);
+    rc = plan.open(4 * (int64_t)n_req + 1 + n_written, stream);
     if (rc != GDN_OK) return rc;
     int32_t* p = std::copy(cu, cu + n_req + 1, plan.data());
     p = std::copy(start, start + n_req, p);
@@ -347,7 +352,7 @@ int32_t paged_prefill(const attn_shape* s, const void* q, const void* gate, int3
     rc = lay_out_image(s, plan, n_req, n_ids, im);
     if (rc != GDN_OK) return rc;
     Plan image;
-    rc = image.open(im.ints);
+    rc = image.open(im.ints, stream);
     if (rc != GDN_OK) return rc;
     fill_image(s, plan, n_req, cu, start, len.data(), page_cu, page_ids, n_ids, im, image.data());
     rc = image.send(workspace, stream);
@@ -583,7 +588,7 @@ int32_t key_weights(const attn_shape* s, const void* q, const float* lse, int32_
     const int64_t few_at = WGT_REC * n_wide, merge_at = few_at + WGT_REC * n_few, ids_at = merge_at + (n_cut > 0 ? WGT_MERGE * (n_cut + 1) : 0);
     if ((ids_at + n_ids) * (int64_t)sizeof(int32_t) > image_bytes(s, n_req, T, n_ids)) return GDN_ERR_WORKSPACE;
     Plan plan;
-    rc = plan.open(ids_at + n_ids);
+    rc = plan.open(ids_at + n_ids, stream);
     if (rc != GDN_OK) return rc;
     list_weights(s, n_req, cu, start, len.data(), page_cu, units, plan.data(), plan.data() + few_at, plan.data() + merge_at);
     std::copy(page_ids, page_ids + n_ids, plan.data() + ids_at);
@@ -673,7 +678,7 @@ int32_t evict(const attn_shape* s, int32_t n_req, const int32_t* rows, const int
 
     const int copied = gather_rows(s->d);              // rows per workgroup of the copy
     Plan plan;
-    rc = plan.open(8 * (int64_t)n_req + 2 + n_old + n_new);
+    rc = plan.open(8 * (int64_t)n_req + 2 + n_old + n_new, stream);
     if (rc != GDN_OK) return rc;
     int32_t* p = plan.data();
     p = std::copy(rows, rows + n_req, p);

@@ -1,7 +1,7 @@
 """ctypes binding of the paged key/value cache (include/attn_paged.h): argument marshalling only.
 
-Pools are device tensors [n_pages][H_kv][page_rows][d] (k bf16, v fp16) and [n_pages][H_kv][page_rows] (w fp32), unit
-stride inside a page; the stride of the first dimension is passed on.  Index arrays and page tables are host sequences."""
+Pools are device tensors [n_pages][H_kv][page_rows][d] (k bf16, v fp16) and [n_pages][H_kv][page_rows] (w fp32), packed
+inside a page; the stride of the first dimension is passed on.  Index arrays and page tables are host sequences."""
 from __future__ import annotations
 
 import ctypes
@@ -73,14 +73,47 @@ def _lib():
     return L
 
 
-def _pages(*pools):
+def _packed(*tensors):
+    for x in tensors:
+        if x is not None and not x.is_contiguous():
+            raise GdnError(-3, "a tensor without gaps and in order is needed")
+
+
+def _ld(x):
+    """The token stride of [T][heads][d] (or [T][heads * d]) whose tokens are packed; that of a single token is nobody's."""
+    stride, size = x.stride(), x.shape
+    if stride[-1] != 1 or (len(size) == 3 and stride[1] != size[2] and size[1] > 1):
+        raise GdnError(-3, "a token's heads and elements are packed")
+    return stride[0] if size[0] > 1 else size[-1] * (size[1] if len(size) == 3 else 1)
+
+
+def _inside(stride, size):
+    """Whether a pool's pages are packed inside."""
+    rest = 1
+    for i in range(len(size) - 1, 0, -1):
+        if stride[i] != rest and size[i] > 1:
+            return False
+        rest *= size[i]
+    return True
+
+
+def _pages(shape, *pools):
     """The common geometry of the given key and value pools."""
     p = pools[0]
-    stride, shape = p.stride(0), p.shape
+    stride, size = p.stride(), p.shape
     for x in pools[1:]:
-        if x.stride(0) != stride or x.shape[0] != shape[0] or x.shape[2] != shape[2]:
+        if x.stride() != stride or x.shape != size:
             raise GdnError(-3, "pools of one geometry")
-    return ctypes.byref(attn_pages(stride, shape[0], shape[2]))
+    if not _inside(stride, size) or size[1] != shape.H_kv or size[3] != shape.d:
+        raise GdnError(-3, "a page is packed: [H_kv][page_rows][d]")
+    return ctypes.byref(attn_pages(stride[0], size[0], size[2]))
+
+
+def _weights_stride(w, k_pool):
+    stride = w.stride()
+    if w.shape != k_pool.shape[:3] or not _inside(stride, w.shape):
+        raise GdnError(-3, "a page of weights is packed, and there is one for every page of keys: [H_kv][page_rows]")
+    return stride[0]
 
 
 def _ws(workspace):
@@ -108,8 +141,9 @@ def attn_rope_append(shape: attn_shape, rope: attn_rope, q, k, v, cu_seqlens, po
                      workspace, stream=None) -> None:
     """See include/attn_paged.h.  q, k, v are [T][heads][d] tensors whose token stride is passed on (heads and elements packed);
     pos may be None."""
-    _check(_lib().attn_rope_append(ctypes.byref(shape), ctypes.byref(rope), _dp(q), q.stride(0), _dp(k), k.stride(0), _dp(v), v.stride(0),
-                                   len(start), _ip(cu_seqlens), None if pos is None else _ip(pos), _ip(start), _pages(k_pool, v_pool),
+    _packed(q_out)
+    _check(_lib().attn_rope_append(ctypes.byref(shape), ctypes.byref(rope), _dp(q), _ld(q), _dp(k), _ld(k), _dp(v), _ld(v),
+                                   len(start), _ip(cu_seqlens), None if pos is None else _ip(pos), _ip(start), _pages(shape, k_pool, v_pool),
                                    _dp(k_pool), _dp(v_pool), _ip(page_cu), _ip(page_ids), _dp(q_out), *_ws(workspace), _stream_ptr(stream)),
            "attn_rope_append")
 
@@ -117,7 +151,8 @@ def attn_rope_append(shape: attn_shape, rope: attn_rope, q, k, v, cu_seqlens, po
 def attn_paged_prefill(shape: attn_shape, q, out_gate, cu_seqlens, start, k_pool, v_pool, page_cu, page_ids, o, lse, workspace,
                        stream=None) -> None:
     """See include/attn_paged.h.  out_gate and lse may be None."""
-    _check(_lib().attn_paged_prefill(ctypes.byref(shape), _dp(q), _dp(out_gate), len(start), _ip(cu_seqlens), _ip(start), _pages(k_pool, v_pool),
+    _packed(q, out_gate, o, lse)
+    _check(_lib().attn_paged_prefill(ctypes.byref(shape), _dp(q), _dp(out_gate), len(start), _ip(cu_seqlens), _ip(start), _pages(shape, k_pool, v_pool),
                                      _dp(k_pool), _dp(v_pool), _ip(page_cu), _ip(page_ids), _dp(o), _dp(lse), *_ws(workspace),
                                      _stream_ptr(stream)), "attn_paged_prefill")
 
@@ -125,16 +160,19 @@ def attn_paged_prefill(shape: attn_shape, q, out_gate, cu_seqlens, start, k_pool
 def attn_key_weights(shape: attn_shape, q, lse, cu_seqlens, start, k_pool, page_cu, page_ids, decay, w_in, w_out, workspace,
                      stream=None) -> None:
     """See include/attn_paged.h.  w_in may be None or w_out; the two have one page stride."""
-    if w_in is not None and w_in.stride(0) != w_out.stride(0):
+    _packed(q, lse)
+    w_stride = _weights_stride(w_out, k_pool)
+    if w_in is not None and w_in is not w_out and _weights_stride(w_in, k_pool) != w_stride:
         raise GdnError(-3, "attn_key_weights: w_in and w_out of one geometry")
-    _check(_lib().attn_key_weights(ctypes.byref(shape), _dp(q), _dp(lse), len(start), _ip(cu_seqlens), _ip(start), _pages(k_pool), _dp(k_pool),
-                                   _ip(page_cu), _ip(page_ids), float(decay), _dp(w_in), _dp(w_out), w_out.stride(0), *_ws(workspace),
+    _check(_lib().attn_key_weights(ctypes.byref(shape), _dp(q), _dp(lse), len(start), _ip(cu_seqlens), _ip(start), _pages(shape, k_pool), _dp(k_pool),
+                                   _ip(page_cu), _ip(page_ids), float(decay), _dp(w_in), _dp(w_out), w_stride, *_ws(workspace),
                                    _stream_ptr(stream)), "attn_key_weights")
 
 
 def attn_evict(shape: attn_shape, rows, keep, first, recent, k_pool, v_pool, w_pool, page_cu, page_ids, new_page_cu, new_page_ids, index,
                workspace, stream=None) -> None:
     """See include/attn_paged.h.  index: int32, H_kv entries per kept row."""
-    _check(_lib().attn_evict(ctypes.byref(shape), len(rows), _ip(rows), _ip(keep), _ip(first), _ip(recent), _pages(k_pool, v_pool), _dp(k_pool),
-                             _dp(v_pool), _dp(w_pool), w_pool.stride(0), _ip(page_cu), _ip(page_ids), _ip(new_page_cu), _ip(new_page_ids),
+    _packed(index)
+    _check(_lib().attn_evict(ctypes.byref(shape), len(rows), _ip(rows), _ip(keep), _ip(first), _ip(recent), _pages(shape, k_pool, v_pool), _dp(k_pool),
+                             _dp(v_pool), _dp(w_pool), _weights_stride(w_pool, k_pool), _ip(page_cu), _ip(page_ids), _ip(new_page_cu), _ip(new_page_ids),
                              _dp(index), *_ws(workspace), _stream_ptr(stream)), "attn_evict")

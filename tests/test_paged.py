@@ -68,7 +68,11 @@ class FakePool:
         self._s0 = int(np.prod(shape[1:])) if stride0 is None else stride0
 
     def data_ptr(self): return self._ptr
-    def stride(self, i): return self._s0
+    def is_contiguous(self): return True
+
+    def stride(self, i=None):
+        inside = [int(np.prod(self.shape[j + 1:])) for j in range(1, len(self.shape))]
+        return (self._s0, *inside) if i is None else (self._s0, *inside)[i]
     def numel(self): return self._n
     def element_size(self): return 1
 
@@ -180,6 +184,49 @@ def test_calls_with_nothing_to_do_touch_nothing(no_stream):
     with pytest.raises(B.GdnError):
         PG.attn_paged_workspace_bytes(sh, -1, 0, 0)
     assert PG.attn_paged_workspace_bytes(sh, 3, 100, 500) > PG.attn_paged_workspace_bytes(sh, 3, 100, 0) > 0
+
+
+def test_tensors_that_the_call_would_read_wrongly_are_refused(no_stream):
+    """Orders and gaps that no argument of the C call says."""
+    import torch
+    sh, rope = AT.make_attn_shape(4, 2, 64), PG.make_attn_rope(np.ones(32))
+    k, v = torch.zeros(40, 2, 16, 64, dtype=torch.bfloat16), torch.zeros(40, 2, 16, 64, dtype=torch.float16)
+    w, ws = torch.zeros(40, 2, 16), torch.zeros(1 << 10, dtype=torch.uint8)
+    q, kv, lse = torch.zeros(9, 4, 64, dtype=torch.bfloat16), torch.zeros(9, 2, 64, dtype=torch.bfloat16), torch.zeros(9, 4)
+    cu, st, tcu, ids = [0, 5, 9], [0, 20], [0, 1, 3], [7, 3, 39]
+    turned = lambda x: x.transpose(1, 2).contiguous().transpose(1, 2)  # noqa: E731
+    wide = lambda x: torch.zeros(*x.shape[:-1], 2 * x.shape[-1], dtype=x.dtype)[..., :x.shape[-1]]  # noqa: E731
+    append = lambda q=q, k_=kv, v_=kv, kp=k, vp=v, out=q: PG.attn_rope_append(sh, rope, q, k_, v_, cu, None, st, kp, vp, tcu, ids, out, ws)  # noqa: E731
+    attend = lambda q=q, gate=None, kp=k, vp=v, o=q, z=lse: PG.attn_paged_prefill(sh, q, gate, cu, st, kp, vp, tcu, ids, o, z, ws)  # noqa: E731
+    weigh = lambda q=q, z=lse, kp=k, wi=w, wo=w: PG.attn_key_weights(sh, q, z, cu, st, kp, tcu, ids, 1.0, wi, wo, ws)  # noqa: E731
+    evict = lambda kp=k, vp=v, w=w, i=torch.zeros(99, dtype=torch.int32): PG.attn_evict(sh, [5, 24], [4, 9], [1, 1], [1, 1], kp, vp, w, tcu, ids, [0, 1, 2], [1, 2], i, ws)  # noqa: E731
+    for call in (append, attend, weigh, evict):
+        refused(call, -9)                                                     # nothing else is wrong: the workspace is too small
+    for bad in (turned, wide):
+        for name in ("q", "k_", "v_", "out"):
+            refused(append, -3, *[bad(x) if n == name else x for n, x in (("q", q), ("k_", kv), ("v_", kv))], k, v, bad(q) if name == "out" else q)
+        for pools in ((bad(k), v), (k, bad(v)), (bad(k), bad(v))):
+            refused(lambda: append(kp=pools[0], vp=pools[1]), -3)
+            refused(lambda: attend(kp=pools[0], vp=pools[1]), -3)
+            refused(lambda: evict(kp=pools[0], vp=pools[1]), -3)
+        refused(lambda: weigh(kp=bad(k)), -3)
+        for kw in (dict(q=bad(q)), dict(gate=bad(q)), dict(o=bad(q)), dict(z=wide(lse))):
+            refused(lambda: attend(**kw), -3)
+        for kw in (dict(q=bad(q)), dict(z=wide(lse)), dict(wi=bad(w)), dict(wo=bad(w), wi=None)):
+            refused(lambda: weigh(**kw), -3)
+        refused(lambda: evict(w=bad(w)), -3)
+    refused(lambda: evict(i=torch.zeros(198, dtype=torch.int32)[::2]), -3)
+    for w_ in (w[:39], w[:, :1], torch.zeros(40, 2, 32)):                     # fewer weights than the keys' pages have rows
+        refused(lambda: weigh(wi=None, wo=w_), -3)
+        refused(lambda: evict(w=w_), -3)
+    refused(lambda: attend(kp=torch.zeros(40, 3, 16, 64)[:, :, :, :], vp=torch.zeros(40, 3, 16, 64)), -3)
+
+
+def test_the_token_stride_of_one_token_is_nobodys(no_stream):
+    import torch
+    a = torch.zeros(4, 1, 64).transpose(0, 1)                                 # [1][4][64] with a token stride of 64
+    assert a.stride(0) == 64 and PG._ld(a) == 256 and PG._ld(a[:, :2]) == 128
+    assert PG._ld(torch.zeros(9, 12, 64)[:, 4:8]) == 768 and PG._ld(torch.zeros(1, 256)) == 256 and PG._ld(torch.zeros(0, 4, 64)) == 256
 
 
 # ----------------------------------------------------------------------------- GPU
@@ -761,3 +808,68 @@ def test_random_calls_of_the_weights_and_the_eviction_that_follows(seed):
             assert np.array_equal(idx[at:at + kept[r]], want), (r, g)
             assert np.array_equal(k_got[to_page, g, to_row], c.k_rows[r][want, g])
             at += kept[r]
+
+
+@pytest.mark.gpu
+def test_a_captured_call_of_few_pages_replays_and_one_of_many_is_refused():
+    import torch
+    c = Paged(81, 8, 2, 128, 32, [1, 1, 6], [700, 31, 95]).fill()
+    sh = AT.make_attn_shape(8, 2, 128, "f32")
+    q, ws = c.dev(c.bf16(c.T, 8, 128)), c.workspace()
+    o, z = torch.zeros(c.T, 8, 128, device="cuda"), torch.zeros(c.T, 8, device="cuda")
+    w = torch.zeros(c.k_np.shape[0], 2, 32, device="cuda")
+
+    def step():
+        PG.attn_paged_prefill(sh, q, None, c.cu, c.starts, c.k_pool, c.v_pool, c.page_cu, c.page_ids, o, z, ws)
+        PG.attn_key_weights(sh, q, z, c.cu, c.starts, c.k_pool, c.page_cu, c.page_ids, 1.0, None, w, ws)
+
+    big = Paged(82, 4, 2, 64, 16, [1] * 4, [9000] * 4).fill()
+    assert big.page_ids.size > 1792
+    qb, big_ws = big.dev(big.bf16(big.T, 4, 64)), big.workspace()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        step()
+        for _ in range(10):                                                   # more than there are buffers
+            with pytest.raises(B.GdnError) as e:
+                PG.attn_paged_prefill(big.shape, qb, None, big.cu, big.starts, big.k_pool, big.v_pool, big.page_cu, big.page_ids, qb, None, big_ws)
+            assert e.value.code < -1000                                        # the capture's own error
+    torch.cuda.synchronize()
+    for i in range(4):
+        q.copy_(c.dev(c.bf16(c.T, 8, 128)))
+        step()
+        torch.cuda.synchronize()
+        want = [x.clone() for x in (o, z, w)]
+        for x in (o, z, w):
+            x.fill_(float("nan"))
+        if i == 2:                                                            # other work of the same kind between two replays
+            ob, zb = run_attend(big, big.bf16(big.T, 4, 64), None, "f32")
+            assert bool(torch.isfinite(ob).all()) and bool(torch.isfinite(zb).all())
+        g.replay()
+        torch.cuda.synchronize()
+        for r in range(3):
+            page, row = c.place(r, c.total[r])
+            page, row = torch.from_numpy(page.astype(np.int64)).cuda(), torch.from_numpy(row).cuda()
+            assert torch.equal(w[page, :, row], want[2][page, :, row])
+        assert torch.equal(o, want[0]) and torch.equal(z, want[1])
+
+
+@pytest.mark.gpu
+def test_one_token_given_by_heads_first():
+    """A token whose heads were the first dimension of a tensor of one token: its token stride says nothing."""
+    import torch
+    c = Paged(83, 8, 2, 64, 16, [1], [40]).fill()
+    rope, ws = PG.make_attn_rope(PG.attn_rope_freqs(64)[0]), c.workspace()
+    x = [c.dev(c.bf16(1, h, 64)) for h in (8, 2, 2)]
+    got = []
+    for turn in (False, True):
+        k, v, out = c.k_pool.clone(), c.v_pool.clone(), torch.zeros(1, 8, 64, dtype=torch.bfloat16, device="cuda")
+        q_, k_, v_ = [t.reshape(-1, 1, 64).clone().transpose(0, 1) if turn else t for t in x]
+        PG.attn_rope_append(c.shape, rope, q_, k_, v_, c.cu, None, c.starts, k, v, c.page_cu, c.page_ids, out, ws)
+        got.append((bits_of(out), bits_of(k), v.cpu().numpy().view(np.int16)))
+    for a, b in zip(*got):
+        assert np.array_equal(a, b)
