@@ -660,6 +660,7 @@ int32_t evict(const attn_shape* s, int32_t n_req, const int32_t* rows, const int
     rc = check_table(pages, n_req, new_page_cu, new_page_ids, [&](int32_t r) { return (int64_t)kept[r]; });
     if (rc != GDN_OK) return rc;
     const int32_t n_old = page_cu[n_req], n_new = new_page_cu[n_req];
+    if ((int64_t)n_old + n_new > INT32_MAX) return GDN_ERR_COUNT;
     rc = check_ids(pages, page_ids, n_old);
     if (rc != GDN_OK) return rc;
     rc = check_ids(pages, new_page_ids, n_new);

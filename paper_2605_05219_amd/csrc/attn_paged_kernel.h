@@ -415,7 +415,7 @@ __global__ void __launch_bounds__(64 * wgt_waves(D), wgt_waves(D) / 2) attn_weig
     f32x16 A[NB], B[NB];
     if (any) {
         int row = row_lo, i = 0;
-        const int cut_end = (key0 + 32 * NB - 1 - c0) * a.G;      // rows before it do not see all of this wave's keys
+        const int cut_end = max(key0 + 32 * NB - 1 - c0, 0) * a.G;      // rows before it do not see all of this wave's keys
         stage_rows(0, lse0, lim0);
         if (second) stage_rows(1, lse_n, lim_n);
         wait_vmcnt<0>();
