@@ -93,8 +93,9 @@ int32_t attn_rope_append(const attn_shape *shape, const attn_rope *rope, const v
  * already, by attn_rope_append):
  *   o_t[h] = sum_{j <= c+t} softmax_j(scale * q_t[h] . k_j[g]) v_j[g],  g = h / (H_q / H_kv);  times sigmoid(gate_t[h])
  *   lse_t[h] = ln sum_{j <= c+t} exp(scale * q_t[h] . k_j[g])
- * Precision, launches, and how walks are cut and packed are those of attn_suffix_prefill, the tuning knobs too; lse comes
- * from a sum of the weights before their rounding.  What a later token's key and value rows hold, infinities and NaN
+ * Precision, launches, and how walks are packed are those of attn_suffix_prefill, the tuning knobs too; small calls cut their
+ * walks from 512 keys on (256 at d = 256), and what is not cut has that call's bits.  lse comes from a sum of the weights before
+ * their rounding.  What a later token's key and value rows hold, infinities and NaN
  * included, does not reach the rows before it.
  *   q            device, bf16, [T][H_q][d];  out_gate: device, bf16, [T][H_q][d] or NULL
  *   o            device, o_dtype, [T][H_q][d];  lse: device, fp32, [T][H_q] or NULL

@@ -35,6 +35,12 @@ inline int32_t check_shape(const attn_shape* s) {
 constexpr int SPLIT_BELOW = 512;       // two workgroups per compute unit
 constexpr int SPLIT_MIN_KEYS = 512;
 constexpr int SPLIT_MAX_WGS = 768;
+// The paged form cuts finer, into parts of fine_keys keys or more, where that leaves at most one workgroup per compute unit and the longest walk ends sooner: a
+// part takes as long as its key tiles, the merge as long as 4 to 8 of them (32 to 128 workgroups) and 0.4 for each part of 128 rows.  (The slot form does not: there a row's bits do not
+// depend on the call around it below 1024 keys.)  Of 120 drawn calls of fewer than 400 workgroups without the cut 27 change by 3 % or more, one of them for the worse: one
+// token of 4 requests behind 469 to 938 rows, 6 heads on 2, d = 256, 35.2 -> 15.9 us; 7 to 14 tokens of two behind 499 to 998, 8 heads, d = 128, 23.0 -> 15.4; one of 4
+// behind 515 to 1030, d = 64, 19.5 -> 14.7; one to 4 tokens of three behind 294 to 588, 16 heads on 4, 16.1 -> 17.6.
+inline int fine_keys(int d) { return d == 256 ? 128 : 256; }
 // The few-rows kernel's walks are cut into at most NARROW_WGS workgroups in all: two per compute unit, one round, at d = 64 and
 // 128 (64 one-token requests behind 4 to 10 thousand keys, d = 128: at most 256 / 384 / 512 / 640 / 768 / 1024 workgroups 104 / 109 /
 // 91 / 98 / 90 / 107 us; four such requests 24 / 24 / 20 / 20 / 20 / 20 us).  At d = 256 one workgroup fills a compute unit's LDS and
@@ -204,7 +210,9 @@ inline void pick_kernels(const attn_shape& s, int32_t n_req, const int32_t* len,
     if (out.apart) out.pack = pick_pack(s, n_req, len, start_pos, out.few);
 }
 
-inline void build_units(const attn_shape& sh, int32_t n_req, const int32_t* len, const int32_t* start_pos, UnitPlan& out) {
+// FINE: see fine_keys.
+template <bool FINE>
+void build_units(const attn_shape& sh, int32_t n_req, const int32_t* len, const int32_t* start_pos, UnitPlan& out) {
     const attn_shape* s = &sh;
     const int KT = att_kt(s->d);
     pick_kernels(sh, n_req, len, start_pos, out);
@@ -250,6 +258,34 @@ inline void build_units(const attn_shape& sh, int32_t n_req, const int32_t* len,
     }
     if (wide_items * HB[0] < SPLIT_BELOW && g_allow_split.load() != 0) {
         int64_t tp = std::max<int64_t>(SPLIT_MIN_KEYS / KT, (wide_tiles * HB[0] + SPLIT_BELOW - 1) / SPLIT_BELOW);
+        if (FINE && !pieces[0].empty()) {
+            constexpr int64_t CUS = SPLIT_BELOW / 2;
+            const Piece* longest = &pieces[0][0];
+            for (const Piece& p : pieces[0])
+                if (p.n_tiles > longest->n_tiles) longest = &p;
+            const int32_t rows = std::min(ATT_BQ / pack, len[longest->req] - longest->tile * (ATT_BQ / pack)) * pack;
+            auto parts_of = [](int64_t n, int64_t t) { return n >= 2 * t ? (n + t - 1) / t : 1; };
+            auto units_of = [&](int64_t t) {
+                int64_t n = 0;
+                for (const Piece& p : pieces[0]) n += parts_of(p.n_tiles, t);
+                if (!out.apart)
+                    for (const Piece& p : pieces[1]) n += std::max<int64_t>(2, parts_of(p.n_tiles, t));
+                return n * HB[0];
+            };
+            auto cost = [&](int64_t t, int64_t units) {
+                const int64_t n = parts_of(longest->n_tiles, t);
+                const double merge = (4.0 + (double)units / 32.0) * (s->d == 64 ? 1.6 : 1.0) + 0.4 * (double)(n * rows) / ATT_BQ;
+                return n > 1 ? (double)t + merge : (double)longest->n_tiles;
+            };
+            double best = cost(tp, units_of(tp));
+            const int64_t coarse = tp;
+            for (int64_t t = std::max<int64_t>(fine_keys(s->d) / KT, (wide_tiles * HB[0] + CUS - 1) / CUS); t < coarse; t *= 2) {
+                const int64_t units = units_of(t);
+                if (units > CUS || cost(t, units) >= best) continue;
+                best = cost(t, units);
+                tp = t;
+            }
+        }
         for (;; tp *= 2) {
             cut(0, [&](int64_t n) { return n >= 2 * tp ? (n + tp - 1) / tp : 1; });
             if (!out.apart) cut(1, [&](int64_t n) { return n >= 2 * tp ? (n + tp - 1) / tp : 2; });

@@ -347,7 +347,7 @@ int32_t paged_prefill(const attn_shape* s, const void* q, const void* gate, int3
     if (rc != GDN_OK) return rc;
 
     UnitPlan plan;
-    build_units(*s, n_req, len.data(), start, plan);
+    build_units<true>(*s, n_req, len.data(), start, plan);
     CallImage im;
     rc = lay_out_image(s, plan, n_req, n_ids, im);
     if (rc != GDN_OK) return rc;

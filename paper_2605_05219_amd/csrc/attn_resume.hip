@@ -157,7 +157,7 @@ int32_t attn_plan(const attn_shape* s, int32_t n_req, const int32_t* cu_seqlens,
     rc = plan_lengths(n_req, cu_seqlens, start_pos, len);
     if (rc != GDN_OK) return rc;
     UnitPlan plan;
-    build_units(*s, n_req, len.data(), start_pos, plan);
+    build_units<false>(*s, n_req, len.data(), start_pos, plan);
     *n_units = (int32_t)plan.units.size();
     *heads_per_row_group = plan.apart && plan.n_units[0] == 0 ? s->H_q / s->H_kv : plan.pack;
     if ((int64_t)plan.units.size() > capacity) return GDN_ERR_COUNT;
@@ -181,7 +181,7 @@ int32_t attn_plan_heads(const attn_shape* s, int32_t n_req, const int32_t* cu_se
     rc = plan_lengths(n_req, cu_seqlens, start_pos, len);
     if (rc != GDN_OK) return rc;
     UnitPlan plan;
-    build_units(*s, n_req, len.data(), start_pos, plan);
+    build_units<false>(*s, n_req, len.data(), start_pos, plan);
     return heads_per_workgroup(*s, plan);
 }
 
@@ -215,7 +215,7 @@ int32_t attn_suffix_prefill(const attn_shape* s, const void* q, const void* k_ne
     if (!workspace || !aligned16(workspace) || workspace_bytes < attn_workspace_bytes(s, n_req, T)) return GDN_ERR_WORKSPACE;
 
     UnitPlan plan;
-    build_units(*s, n_req, len.data(), start_pos, plan);
+    build_units<false>(*s, n_req, len.data(), start_pos, plan);
     CallImage im;
     rc = lay_out_image(s, plan, n_req, 0, im);
     if (rc != GDN_OK) return rc;

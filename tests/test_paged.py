@@ -283,6 +283,10 @@ class Paged:
             page, row = self.place(r, n)
             self.view(self.k_np)[page, :, row] = self.k_rows[r][:n]
             self.view(self.v_np)[page, :, row] = self.v_rows[r][:n]
+        return self.fill_values()
+
+    def fill_values(self):
+        """The pools as they are to the device."""
         t = self.torch
         self.k_dev = t.from_numpy(self.k_np.view(np.int16)).cuda().view(t.bfloat16)
         self.v_dev = t.from_numpy(self.v_np).cuda()
@@ -458,12 +462,18 @@ def test_paged_prefill_equals_the_slot_form_bit_for_bit(seed):
         c.v_rows[r][starts[r]:] = wl.to_f32(v_new[r]).astype(np.float16)
         kc[r, :starts[r]], vc[r, :starts[r]] = c.k_rows[r][:starts[r]], c.v_rows[r][:starts[r]]
     c.fill()
-    o, _ = run_attend(c, q, None, "f32", lse=False)
+    o, z = run_attend(c, q, None, "f32")
+    check_attend(c, q, None, "f32", o, z)
     sh = AT.make_attn_shape(H_q, H_kv, d, "f32")
     os_ = torch.zeros_like(o)
     ws = torch.empty(AT.attn_workspace_bytes(sh, R, c.T), dtype=torch.uint8, device="cuda")
-    AT.attn_suffix_prefill(sh, c.dev(q), c.dev(np.concatenate([k[s:] for k, s in zip(c.k_rows, starts)])), c.dev(np.concatenate(v_new)), None, c.cu, starts,
-                           c.dev(kc), torch.from_numpy(vc).cuda(), list(range(R)), os_, ws)
+    AT.attn_tune_split(False)                                               # whole walks (the paged form's small calls cut more of them)
+    try:
+        o, _ = run_attend(c, q, None, "f32", lse=False)
+        AT.attn_suffix_prefill(sh, c.dev(q), c.dev(np.concatenate([k[s:] for k, s in zip(c.k_rows, starts)])), c.dev(np.concatenate(v_new)), None, c.cu, starts,
+                               c.dev(kc), torch.from_numpy(vc).cuda(), list(range(R)), os_, ws)
+    finally:
+        AT.attn_tune_split(True)
     assert torch.equal(o, os_)
 
 
@@ -873,3 +883,28 @@ def test_one_token_given_by_heads_first():
         got.append((bits_of(out), bits_of(k), v.cpu().numpy().view(np.int16)))
     for a, b in zip(*got):
         assert np.array_equal(a, b)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H_q,H_kv,d,P,lens,starts", [
+    (16, 2, 128, 64, [1], [900]), (6, 2, 64, 16, [1, 0, 1, 1], [975, 12, 512, 640]), (4, 2, 256, 32, [1, 5], [300, 470]),
+    (8, 8, 128, 256, [14, 13], [668, 705]), (8, 1, 256, 16, [30], [1700]), (32, 4, 64, 32, [3, 1], [767, 1100]),   # (the last beside a few-rows request)
+    (2, 1, 128, 16, [1, 200], [5000, 600]), (1, 1, 256, 128, [300], [0]),
+])
+def test_short_walks_cut_in_small_calls(H_q, H_kv, d, P, lens, starts):
+    """Cut or whole, the same values; where a later token's rows are not numbers, the earlier ones' are."""
+    import torch
+    c = Paged(91, H_q, H_kv, d, P, lens, starts, stride_pad=8).fill()
+    q, g = c.bf16(c.T, H_q, d, s=2.0), c.bf16(c.T, H_q, d)
+    o, z = run_attend(c, q, g, "f32")
+    check_attend(c, q, g, "f32", o, z)
+    r = int(np.argmax(lens))
+    page, row = c.place(r, c.total[r])
+    c.view(c.v_np)[page[-1], :, row[-1]] = np.inf                            # what the longest request's last token brings
+    c.view(c.k_np)[page[-1], :, row[-1]] = 0x7fc0
+    c.fill_values()
+    o2, z2 = run_attend(c, q, g, "f32")
+    last = int(c.cu[r + 1]) - 1
+    assert bool(torch.isnan(o2[last]).all()) and bool(torch.isnan(z2[last]).all())
+    o2[last], z2[last] = o[last], z[last]
+    check_attend(c, q, g, "f32", o2, z2)
