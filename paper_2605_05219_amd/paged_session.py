@@ -69,9 +69,10 @@ class PagedLayer:
         return o
 
     def evict(self, budget, keep, first=4, recent=64):
-        """Requests of more than `budget` rows go back to `keep`; returns the rows dropped (per head)."""
+        """Requests of more than `budget` rows go back to `keep` (those that hold no more than `keep` stay as they are); returns the rows
+        dropped (per head)."""
         import torch
-        over = [r for r in range(self.n_req) if self.rows[r] > budget]
+        over = [r for r in range(self.n_req) if self.rows[r] > max(budget, keep)]
         if not over:
             return 0
         new = [self._take(-(-keep // self.P)) for _ in over]

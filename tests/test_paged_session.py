@@ -1,0 +1,47 @@
+"""PagedLayer's own bookkeeping (pages, rows, positions), on the CPU with the library's calls stubbed."""
+import numpy as np
+import pytest
+
+from paper_2605_05219_amd import paged as PG
+from paper_2605_05219_amd.paged_session import PagedLayer
+
+
+@pytest.fixture
+def made(monkeypatch):
+    """made(rows, n_pages): a layer of pages of 16 rows whose requests hold `rows`; layer.calls gets the arguments of its evictions."""
+    import torch
+    empty = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *size, device=None, **kw: empty(*size, **kw))
+
+    def make(rows, n_pages):
+        layer = PagedLayer(4, 2, 64, len(rows), n_pages, page_rows=16)
+        layer.calls = []
+        monkeypatch.setattr(PG, "attn_evict", lambda *args: layer.calls.append(args))
+        for r, n in enumerate(rows):
+            layer.pages[r] = layer._take(-(-n // 16))
+            layer.rows[r] = layer.pos[r] = n
+        return layer
+    return make
+
+
+def whole(layer, n_pages):
+    """Every page is free or one request's."""
+    held = [p for pages in layer.pages for p in pages]
+    assert sorted(layer.free + held) == list(range(n_pages))
+    assert all(len(p) * layer.P >= n for p, n in zip(layer.pages, layer.rows))
+
+
+@pytest.mark.parametrize("rows,budget,keep,after", [
+    ([150], 100, 200, [150]), ([150, 300, 90], 100, 200, [150, 200, 90]), ([150], 100, 150, [150]), ([150, 20], 100, 80, [80, 20]),
+    ([100], 100, 80, [100]),
+])
+def test_an_eviction_leaves_no_request_with_more_rows_than_it_held(made, rows, budget, keep, after):
+    layer = made(rows, 80)
+    dropped = layer.evict(budget, keep, first=2, recent=8)
+    assert list(layer.rows) == after and dropped == sum(rows) - sum(after)
+    assert list(layer.pos) == rows
+    assert len(layer.calls) == (after != rows)
+    for call in layer.calls:                    # rows, keep, first, recent; the index has room for what is kept
+        assert [min(a, b) for a, b in zip(call[1], call[2])] == [x for x, n in zip(after, rows) if x != n]
+        assert call[-2].numel() == layer.H_kv * sum(min(a, b) for a, b in zip(call[1], call[2]))
+    whole(layer, 80)
