@@ -75,19 +75,23 @@ class PagedLayer:
         over = [r for r in range(self.n_req) if self.rows[r] > max(budget, keep)]
         if not over:
             return 0
-        new = [self._take(-(-keep // self.P)) for _ in over]
+        n, per = len(over), -(-keep // self.P)
         cu = np.concatenate([[0], np.cumsum([len(self.pages[r]) for r in over])]).astype(np.int32)
         ids = np.asarray([i for r in over for i in self.pages[r]], np.int32)
-        new_cu = np.concatenate([[0], np.cumsum([len(p) for p in new])]).astype(np.int32)
-        new_ids = np.asarray([i for p in new for i in p], np.int32)
-        n = len(over)
-        index = torch.empty(n * keep * self.H_kv, dtype=torch.int32, device="cuda")
-        paged.attn_evict(self.shape, self.rows[over], np.full(n, keep), np.full(n, first), np.full(n, recent), self.k_pool, self.v_pool, self.w_pool,
-                         cu, ids, new_cu, new_ids, index, self._room(0, ids.size + new_ids.size))
+        new_cu = np.arange(n + 1, dtype=np.int32) * per
+        new = self._take(n * per)
+        try:
+            new_ids = np.asarray(new, np.int32)
+            index = torch.empty(n * keep * self.H_kv, dtype=torch.int32, device="cuda")
+            paged.attn_evict(self.shape, self.rows[over], np.full(n, keep), np.full(n, first), np.full(n, recent), self.k_pool, self.v_pool, self.w_pool,
+                             cu, ids, new_cu, new_ids, index, self._room(0, ids.size + new_ids.size))
+        except Exception:
+            self.free += reversed(new)
+            raise
         dropped = int((self.rows[over] - keep).sum())
-        for r, p in zip(over, new):          # later calls of this stream see the copies; the old pages may be written by them
+        for i, r in enumerate(over):         # later calls of this stream see the copies; the old pages may be written by them
             self.free += self.pages[r]
-            self.pages[r] = p
+            self.pages[r] = new[i * per:(i + 1) * per]
         self.rows[over] = keep
         return dropped
 

@@ -2,7 +2,7 @@
 import numpy as np
 import pytest
 
-from paper_2605_05219_amd import paged as PG
+from paper_2605_05219_amd import binding as B, paged as PG
 from paper_2605_05219_amd.paged_session import PagedLayer
 
 
@@ -45,3 +45,21 @@ def test_an_eviction_leaves_no_request_with_more_rows_than_it_held(made, rows, b
         assert [min(a, b) for a, b in zip(call[1], call[2])] == [x for x, n in zip(after, rows) if x != n]
         assert call[-2].numel() == layer.H_kv * sum(min(a, b) for a, b in zip(call[1], call[2]))
     whole(layer, 80)
+
+
+def test_pages_of_an_eviction_that_fails_are_free_again(made, monkeypatch):
+    layer = made([150, 150], 24)                # 20 pages held, 4 free: enough for one request's copy, not for both
+    free, pages = sorted(layer.free), [list(p) for p in layer.pages]
+    with pytest.raises(RuntimeError, match="out of pages"):
+        layer.evict(100, 48, first=2, recent=8)
+    whole(layer, 24)
+    assert sorted(layer.free) == free and layer.pages == pages and list(layer.rows) == [150, 150] and not layer.calls
+
+    def refuse(*args):
+        raise B.GdnError(-10, "attn_evict")
+    monkeypatch.setattr(PG, "attn_evict", refuse)
+    layer.rows[1] = 90
+    with pytest.raises(B.GdnError):
+        layer.evict(100, 48, first=2, recent=8)
+    whole(layer, 24)
+    assert sorted(layer.free) == free and layer.pages == pages and list(layer.rows) == [150, 90]
