@@ -69,9 +69,11 @@ class PagedLayer:
         return o
 
     def evict(self, budget, keep, first=4, recent=64):
-        """Requests of more than `budget` rows go back to `keep` (those that hold no more than `keep` stay as they are); returns the rows
-        dropped (per head)."""
+        """Requests of more than `budget` rows go back to `keep` (those that hold no more than `keep` stay as they are), among them the
+        first `first` and the last `recent` as far as `keep` has room for them, the first before the last; returns the rows dropped (per head)."""
         import torch
+        first = min(first, keep)
+        recent = min(recent, keep - first)
         over = [r for r in range(self.n_req) if self.rows[r] > max(budget, keep)]
         if not over:
             return 0

@@ -63,3 +63,13 @@ def test_pages_of_an_eviction_that_fails_are_free_again(made, monkeypatch):
         layer.evict(100, 48, first=2, recent=8)
     whole(layer, 24)
     assert sorted(layer.free) == free and layer.pages == pages and list(layer.rows) == [150, 90]
+
+
+@pytest.mark.parametrize("keep,first,recent,want", [(60, 4, 64, (4, 56)), (3, 4, 64, (3, 0)), (0, 4, 64, (0, 0)), (68, 4, 64, (4, 64)), (100, 4, 64, (4, 64))])
+def test_an_eviction_to_few_rows_keeps_of_the_first_and_the_last_what_there_is_room_for(made, keep, first, recent, want):
+    layer = made([150, 200], 80)
+    layer.evict(100, keep, first=first, recent=recent)
+    (call,) = layer.calls
+    assert list(call[2]) == [keep] * 2 and list(call[3]) == [want[0]] * 2 and list(call[4]) == [want[1]] * 2
+    assert list(layer.rows) == [keep] * 2
+    whole(layer, 80)
