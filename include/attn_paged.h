@@ -77,11 +77,13 @@ int64_t attn_paged_workspace_bytes(const attn_shape *shape, int32_t n_req, int64
  *   q, k, v      device, in_dtype, [T][H_q][d] and [T][H_kv][d], tokens ldq, ldk, ldv elements apart (16-byte multiples:
  *                they may be column ranges of one projection's output)
  *   pos          host, n_req: the position of each request's first new token, >= 0; NULL: start
- *   q_out        device, bf16, [T][H_q][d]; may be q itself where q is bf16 and ldq = H_q * d
+ *   q_out        device, bf16, [T][H_q][d]; may be q itself where q is bf16 and ldq = H_q * d (or T is 1), and lies over no other
+ *                part of q, k or v
  *   k_pool, v_pool  device; the pages that get rows belong to one request alone and are listed once in the call
  *   shape        H_q, H_kv and d are used
  * Errors: GDN_ERR_NULL, _ALIGN, _SHAPE, _SEQLENS, _START (a negative start or position, positions beyond 2^31 - 1, or
- * too few pages for the rows), _COUNT, _SLOT_RANGE (a page id outside the pool), _SLOT_DUP, _WORKSPACE.
+ * too few pages for the rows), _COUNT, _SLOT_RANGE (a page id outside the pool), _SLOT_DUP, _SLOT_HAZARD (q_out over what is read),
+ * _WORKSPACE.
  */
 int32_t attn_rope_append(const attn_shape *shape, const attn_rope *rope, const void *q, int64_t ldq, const void *k, int64_t ldk,
                          const void *v, int64_t ldv, int32_t n_req, const int32_t *cu_seqlens, const int32_t *pos,

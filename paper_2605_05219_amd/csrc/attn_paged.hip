@@ -276,6 +276,14 @@ int32_t rope_append(const attn_shape* s, const attn_rope* rope, const void* q, i
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(k_pool) || !aligned16(v_pool) || !aligned16(q_out)) return GDN_ERR_ALIGN;
     rc = check_workspace(s, n_req, T, page_cu[n_req], workspace, workspace_bytes);
     if (rc != GDN_OK) return rc;
+    // ---- a workgroup stores its queries while others have yet to load theirs: q_out lies on q token by token, or on nothing that is read
+    const int64_t size = rope->in_dtype == GDN_F32 ? 4 : 2;
+    auto out_over = [&](const void* x, int64_t ld, int64_t width) {
+        const uintptr_t lo = reinterpret_cast<uintptr_t>(x), out = reinterpret_cast<uintptr_t>(q_out);
+        return out < lo + (uintptr_t)(((T - 1) * ld + width) * size) && lo < out + (uintptr_t)(T * wq * 2);
+    };
+    const bool in_place = q_out == q && size == 2 && (ldq == wq || T == 1);
+    if ((!in_place && out_over(q, ldq, wq)) || out_over(k, ldk, wkv) || out_over(v, ldv, wkv)) return GDN_ERR_SLOT_HAZARD;
     Plan plan;
     rc = plan.open(4 * (int64_t)n_req + 1 + n_written, stream);
     if (rc != GDN_OK) return rc;

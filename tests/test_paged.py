@@ -908,3 +908,21 @@ def test_short_walks_cut_in_small_calls(H_q, H_kv, d, P, lens, starts):
     assert bool(torch.isnan(o2[last]).all()) and bool(torch.isnan(z2[last]).all())
     o2[last], z2[last] = o[last], z[last]
     check_attend(c, q, g, "f32", o2, z2)
+
+
+# ----------------------------------------------------------------------------- what else is refused
+@pytest.mark.parametrize("over", [
+    dict(q=FakePool(0x10000, (9, 4, 64), 512), q_out=FakePool(0x10000, (9, 4, 64))),          # in place, but the queries lie apart
+    dict(rope=PG.make_attn_rope(np.ones(32), in_dtype="f32"), q_out=FakePool(0x10000, (9, 4, 64))),   # ... or are twice as wide
+    dict(q_out=FakePool(0x10010, (9, 4, 64))),                                                # ... or begin elsewhere
+    dict(q_out=FakePool(0x10000 + 4608 - 16, (9, 4, 64))),                                    # over the last query
+    dict(q_out=FakePool(0x20000 - 4608 + 16, (9, 4, 64))), dict(q_out=FakePool(0x20000 + 2304 - 16, (9, 4, 64))),   # over the first and the last key
+    dict(v=FakePool(0x30000, (9, 2, 64), 1024), q_out=FakePool(0x30000 + 8 * 2048, (9, 4, 64))),                    # over a value
+])
+def test_rope_append_refuses_an_output_over_its_inputs(no_stream, over):
+    """q_out over q that is not q itself, packed and bf16, or over k or v: workgroups would write what others have yet to read."""
+    a = dict(CALL, rope=PG.make_attn_rope(np.ones(32)), q=X, k=FakePool(0x20000, (9, 2, 64)), v=FakePool(0x30000, (9, 2, 64)), pos=[0, 100],
+             q_out=FakePool(0x40000, (9, 4, 64)))
+    a.update(over)
+    refused(PG.attn_rope_append, -7, a["shape"], a["rope"], a["q"], a["k"], a["v"], a["cu_seqlens"], a["pos"], a["start"], a["k_pool"], a["v_pool"],
+            a["page_cu"], a["page_ids"], a["q_out"], a["workspace"])
