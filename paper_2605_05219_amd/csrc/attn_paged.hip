@@ -237,6 +237,8 @@ int32_t rope_append(const attn_shape* s, const attn_rope* rope, const void* q, i
     const int64_t wq = (int64_t)s->H_q * s->d, wkv = (int64_t)s->H_kv * s->d;
     if (ldq % per16 != 0 || ldk % per16 != 0 || ldv % per16 != 0) return GDN_ERR_ALIGN;
     if (ldq < wq || ldk < wkv || ldv < wkv) return GDN_ERR_SHAPE;
+    const int64_t units = ((int64_t)s->H_q + 2 * (int64_t)s->H_kv) * (s->d / 16);       // pieces of 16 elements per token
+    if (units * ROPE_TOKENS > INT32_MAX) return GDN_ERR_SHAPE;
     RopeArgs a;
     for (int p = 0; p < rope->rot / 2; ++p) {
         if (!std::isfinite(rope->freq[p])) return GDN_ERR_SHAPE;
@@ -310,9 +312,7 @@ int32_t rope_append(const attn_shape* s, const attn_rope* rope, const void* q, i
     a.n_req = n_req;
     a.T = (int32_t)T;
     // as many tokens to a workgroup as its threads have on their way at once, but one while there are fewer tokens than compute units
-    const int64_t units = ((int64_t)s->H_q + 2 * s->H_kv) * (s->d / 16);
     a.tokens = (int32_t)std::max<int64_t>(1, std::min<int64_t>({(int64_t)ROPE_TOKENS, ROPE_UNITS * ROPE_THREADS / units, (T + 255) / 256}));
-    if (units * ROPE_TOKENS > INT32_MAX) return GDN_ERR_SHAPE;
     a.H_q = s->H_q; a.H_kv = s->H_kv;
     a.unit_shift = __builtin_ctz((unsigned)s->d / 16);
     a.page_shift = shift;

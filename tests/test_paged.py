@@ -926,3 +926,13 @@ def test_rope_append_refuses_an_output_over_its_inputs(no_stream, over):
     a.update(over)
     refused(PG.attn_rope_append, -7, a["shape"], a["rope"], a["q"], a["k"], a["v"], a["cu_seqlens"], a["pos"], a["start"], a["k_pool"], a["v_pool"],
             a["page_cu"], a["page_ids"], a["q_out"], a["workspace"])
+
+
+def test_rope_append_refuses_too_many_heads_before_anything_is_enqueued(no_stream):
+    """More pieces to a token than its kernel numbers, in a call whose plan is long enough for a launch of its own."""
+    n, heads = 200, 1 << 26
+    q = FakePool(0x1000000, (n, heads, 64))
+    kv = FakePool(0x10000, (n, 1, 64))
+    pool = FakePool(0x200000, (n, 1, 16, 64))
+    refused(PG.attn_rope_append, -3, AT.make_attn_shape(heads, 1, 64), PG.make_attn_rope(np.ones(32)), q, kv, kv, np.arange(n + 1), None, np.zeros(n, np.int32),
+            pool, pool, np.arange(n + 1), np.arange(n), FakePool(1 << 50, (n, heads, 64)), FakePool(0x100000, nbytes=1 << 45))
