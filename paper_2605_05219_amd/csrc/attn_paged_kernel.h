@@ -261,7 +261,7 @@ __global__ void __launch_bounds__(64 * wgt_waves(D), wgt_waves(D) / 2) attn_weig
     constexpr int AHEAD_TILES = D == 256 ? 1 : 2;    // a tile is asked for this many tiles ahead (three stages at d = 256 would leave one workgroup to a compute unit)
     __shared__ __attribute__((aligned(1024))) char stage0[SM::TILE_BYTES], stage1[SM::TILE_BYTES], stage2[AHEAD_TILES == 2 ? SM::TILE_BYTES : 16];
     __shared__ __attribute__((aligned(16))) float neg_lse[4][WGT_ROWS];   // -lse log2(e); rows past the end -inf
-    __shared__ __attribute__((aligned(16))) int limit[4][WGT_ROWS];       // last key a row sees
+    __shared__ __attribute__((aligned(16))) int limit[4][WGT_ROWS];       // last key a row sees; rows past the end -1
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -305,8 +305,9 @@ __global__ void __launch_bounds__(64 * wgt_waves(D), wgt_waves(D) / 2) attn_weig
     auto issue = [&](char* sb) __attribute__((always_inline)) {
         if (step_h != 0) places();
         if (threadIdx.x < WGT_ROWS) {
-            lim_n = c0 + t_n + lse_t;
-            lse_n = row_n + (int)threadIdx.x < row_hi ? lse_base[(int64_t)t_n * a.H_q + lse_off] : INFINITY;
+            const bool row = row_n + (int)threadIdx.x < row_hi;
+            lim_n = row ? c0 + t_n + lse_t : -1;
+            lse_n = row ? lse_base[(int64_t)t_n * a.H_q + lse_off] : INFINITY;
         }
         const uint16_t* const base = q_base + (int64_t)t_n * (a.H_q * D);
         const int bytes = (int)min((int64_t)INT32_MAX, (int64_t)(n - 1 - t_n) * tok_bytes + a.G * D * 2);
@@ -359,7 +360,8 @@ __global__ void __launch_bounds__(64 * wgt_waves(D), wgt_waves(D) / 2) attn_weig
             for (int b = 0; b < NB; ++b) S[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, kf[b][kb], S[b], 0, 0, 0);
         }
     };
-    // the weights of 32 rows, summed, four of a block (registers 4 q .. 4 q + 3) at a time; CUT: some row does not see some key of this wave
+    // the weights of 32 rows, summed, four of a block (registers 4 q .. 4 q + 3) at a time; CUT: some row does not see some key of this wave, or is past
+    // the last one (whose zeros an infinite key turns into what is not a number)
     auto sum4 = [&](const f32x16& S, int b, int q, f32x4 nl, const int* lim, auto cut) __attribute__((always_inline)) {
         float p[4];
 #pragma unroll
@@ -423,9 +425,9 @@ __global__ void __launch_bounds__(64 * wgt_waves(D), wgt_waves(D) / 2) attn_weig
         products(A, stage0, 0);
         // a tile from its second half to the first half of the next; `ahead`: the stage that the tile before left.  False: it was the last one.
         auto step = [&](const char* sb, const char* next, char* ahead) __attribute__((always_inline)) {
-            const bool more = row + AHEAD_TILES * WGT_ROWS < row_hi;
+            const bool more = row + AHEAD_TILES * WGT_ROWS < row_hi, cut = row < cut_end || row + WGT_ROWS > row_hi;
             if (more) issue(ahead);
-            both(B, sb, 1, A, i & 3, 0, row < cut_end);
+            both(B, sb, 1, A, i & 3, 0, cut);
             if (row + WGT_ROWS >= row_hi) return false;
             if (more) {
                 stage_rows((i + AHEAD_TILES) & 3, lse_n, lim_n);
@@ -434,7 +436,7 @@ __global__ void __launch_bounds__(64 * wgt_waves(D), wgt_waves(D) / 2) attn_weig
                 wait_vmcnt<0>();
             }
             __syncthreads();
-            both(A, next, 0, B, i & 3, 1, row < cut_end);
+            both(A, next, 0, B, i & 3, 1, cut);
             row += WGT_ROWS;
             ++i;
             return true;

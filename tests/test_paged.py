@@ -936,3 +936,37 @@ def test_rope_append_refuses_too_many_heads_before_anything_is_enqueued(no_strea
     pool = FakePool(0x200000, (n, 1, 16, 64))
     refused(PG.attn_rope_append, -3, AT.make_attn_shape(heads, 1, 64), PG.make_attn_rope(np.ones(32)), q, kv, kv, np.arange(n + 1), None, np.zeros(n, np.int32),
             pool, pool, np.arange(n + 1), np.arange(n), FakePool(1 << 50, (n, heads, 64)), FakePool(0x100000, nbytes=1 << 45))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H_q,H_kv,d,P,lens,starts", [
+    (4, 2, 128, 16, [40], [300]), (8, 1, 64, 32, [5, 70], [500, 10]), (6, 2, 256, 64, [9, 21], [20, 700]), (16, 2, 128, 64, [1100], [40]),   # (cut rows)
+    (16, 2, 128, 16, [1, 2], [90, 33]),                                       # the few-rows kernel
+])
+def test_key_weights_of_a_key_that_every_row_gives_minus_infinity(H_q, H_kv, d, P, lens, starts):
+    """An element of a cached key is -infinity and positive in every query: its weight is 0, also beside rows that fill a tile's end."""
+    import torch
+    c = Paged(63, H_q, H_kv, d, P, lens, starts)
+    at = [s // 2 for s in starts]
+    for k, j in zip(c.k_rows, at):
+        k[j, :, 5] = 0xff80
+    c.fill()
+    q = c.bf16(c.T, H_q, d)
+    q[..., 5] = 0x3f80                                 # 1
+    lse = np.zeros((c.T, H_q), np.float32)
+    finite = [k.copy() for k in c.k_rows]
+    for r in range(len(lens)):
+        s = slice(c.cu[r], c.cu[r + 1])
+        lse[s] = po.row_lse(f64(q[s]), f64(c.k_rows[r]), starts[r], d ** -0.5)
+        finite[r][at[r], :, 5] = 0
+    assert np.isfinite(lse).all()
+    w = torch.full((c.k_np.shape[0], H_kv, P), float("nan"), device="cuda")
+    PG.attn_key_weights(c.shape, c.dev(q), torch.from_numpy(lse).cuda(), c.cu, starts, c.k_pool, c.page_cu, c.page_ids, 1.0, None, w, c.workspace())
+    w = w.cpu().numpy().astype(np.float64)
+    held, c.k_rows = c.k_rows, finite
+    rtol = np.expm1(logit_error(c, q) + 2.0 ** -22 * (1 + np.abs(lse).max())) + (max(lens) * (H_q // H_kv) + 8) * 2.0 ** -24
+    for r in range(len(lens)):
+        s = slice(c.cu[r], c.cu[r + 1])
+        page, row = c.place(r, c.total[r])
+        ref = po.key_weights(f64(q[s]), lse[s], f64(held[r]), starts[r], d ** -0.5, 1.0, None)
+        assert (ref[at[r]] == 0).all() and (np.abs(w[page, :, row] - ref) <= rtol * ref).all(), r
