@@ -17,6 +17,16 @@
 namespace attn {
 
 inline int32_t hip_err(hipError_t e) { return e == hipSuccess ? GDN_OK : GDN_ERR_HIP - (int32_t)e; }
+// A launch whose arguments are read where they lie.  (hipLaunchKernelGGL passes them by value, which copies a plan's 2.5 KB twice; where the two
+// copies' addresses fall badly, as the size of a caller's frame decides, that is 5 us of a call of 10.)
+template <typename... P, typename... A>
+inline hipError_t launch_in_place(void (*kernel)(P...), dim3 grid, dim3 block, hipStream_t stream, const A&... args) {
+    static_assert((std::is_same<P, A>::value && ...), "a kernel's parameters and its arguments have the same types");
+    void* at[] = {const_cast<void*>(static_cast<const void*>(&args))...};
+    const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, at, 0, stream);
+    if (e != hipSuccess) (void)hipGetLastError();        // (it is this call's, not the next one's)
+    return e;
+}
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 inline int32_t check_shape(const attn_shape* s) {
@@ -65,8 +75,7 @@ inline int64_t part_o_bytes(int d) { return (int64_t)SPLIT_MAX_WGS * ATT_BQ * d 
 
 template <int D, typename OT, int NH, typename Args, bool LSE>
 hipError_t launch_attn(const Args& a, unsigned blocks, hipStream_t stream) {
-    hipLaunchKernelGGL((attn_suffix_kernel<D, OT, NH, Args, LSE>), dim3(blocks), dim3(ATT_THREADS * NH), 0, stream, a);
-    return hipGetLastError();
+    return launch_in_place(attn_suffix_kernel<D, OT, NH, Args, LSE>, dim3(blocks), dim3(ATT_THREADS * NH), stream, a);
 }
 
 // NH: head blocks per workgroup; 2 is built for d = 128 only
@@ -83,12 +92,8 @@ hipError_t launch_attn_d(int d, int NH, const Args& a, unsigned blocks, hipStrea
 template <int D, typename OT, bool LSE, typename Args>
 hipError_t launch_narrow(bool nt, const Args& a, unsigned blocks, hipStream_t stream) {
     if constexpr (!std::is_same<Args, PagedValueArgs>::value)      // (page tables that fit the arguments are of small calls)
-        if (nt) {
-            hipLaunchKernelGGL((attn_narrow_kernel<D, OT, true, Args, LSE>), dim3(blocks), dim3(ATT_THREADS), 0, stream, a);
-            return hipGetLastError();
-        }
-    hipLaunchKernelGGL((attn_narrow_kernel<D, OT, false, Args, LSE>), dim3(blocks), dim3(ATT_THREADS), 0, stream, a);
-    return hipGetLastError();
+        if (nt) return launch_in_place(attn_narrow_kernel<D, OT, true, Args, LSE>, dim3(blocks), dim3(ATT_THREADS), stream, a);
+    return launch_in_place(attn_narrow_kernel<D, OT, false, Args, LSE>, dim3(blocks), dim3(ATT_THREADS), stream, a);
 }
 
 template <typename OT, bool LSE, typename Args>
@@ -104,12 +109,8 @@ template <int D, typename OT, bool LSE, bool LONG, typename Args>
 hipError_t launch_combine(bool by_row, const Args& a, hipStream_t stream) {
     const dim3 grid((unsigned)(a.set[0].blocks + a.set[1].blocks));
     if constexpr (LONG)
-        if (by_row) {
-            hipLaunchKernelGGL((attn_combine_long_kernel<D, OT, LSE, Args>), grid, dim3(CL_THREADS), 0, stream, a);
-            return hipGetLastError();
-        }
-    hipLaunchKernelGGL((attn_combine_kernel<D, OT, LSE, Args>), grid, dim3(ATT_THREADS), 0, stream, a);
-    return hipGetLastError();
+        if (by_row) return launch_in_place(attn_combine_long_kernel<D, OT, LSE, Args>, grid, dim3(CL_THREADS), stream, a);
+    return launch_in_place(attn_combine_kernel<D, OT, LSE, Args>, grid, dim3(ATT_THREADS), stream, a);
 }
 
 template <typename OT, bool LSE, bool LONG, typename Args>

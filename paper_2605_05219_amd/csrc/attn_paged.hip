@@ -321,11 +321,8 @@ int32_t rope_append(const attn_shape* s, const attn_rope* rope, const void* q, i
     a.amplitude = rope->amplitude;
     const dim3 grid((unsigned)((T + a.tokens - 1) / a.tokens)), block(ROPE_THREADS);
     const bool f32 = rope->in_dtype == GDN_F32;
-    if (plan.by_value() && f32) hipLaunchKernelGGL((attn_rope_kernel<true, true>), grid, block, 0, stream, a, plan.words());
-    else if (plan.by_value()) hipLaunchKernelGGL((attn_rope_kernel<false, true>), grid, block, 0, stream, a, plan.words());
-    else if (f32) hipLaunchKernelGGL((attn_rope_kernel<true, false>), grid, block, 0, stream, a, PlanWords<false>());
-    else hipLaunchKernelGGL((attn_rope_kernel<false, false>), grid, block, 0, stream, a, PlanWords<false>());
-    return hip_err(hipGetLastError());
+    if (plan.by_value()) return hip_err(launch_in_place(f32 ? attn_rope_kernel<true, true> : attn_rope_kernel<false, true>, grid, block, stream, a, plan.words()));
+    return hip_err(launch_in_place(f32 ? attn_rope_kernel<true, false> : attn_rope_kernel<false, false>, grid, block, stream, a, PlanWords<false>()));
 }
 
 template <bool LSE, typename Args, typename Merge>
@@ -393,23 +390,23 @@ int32_t paged_prefill(const attn_shape* s, const void* q, const void* gate, int3
 }
 
 template <int D, bool BY_VALUE>
-void launch_weights_d(bool few, const WeightArgs& a, const PlanWords<BY_VALUE>& words, unsigned blocks, hipStream_t stream) {
-    if (few) hipLaunchKernelGGL((attn_weights_few_kernel<D, BY_VALUE>), dim3(blocks), dim3(WGT_THREADS), 0, stream, a, words);
-    else hipLaunchKernelGGL((attn_weights_kernel<D, BY_VALUE>), dim3(blocks), dim3(64 * wgt_waves(D)), 0, stream, a, words);
+hipError_t launch_weights_d(bool few, const WeightArgs& a, const PlanWords<BY_VALUE>& words, unsigned blocks, hipStream_t stream) {
+    if (few) return launch_in_place(attn_weights_few_kernel<D, BY_VALUE>, dim3(blocks), dim3(WGT_THREADS), stream, a, words);
+    return launch_in_place(attn_weights_kernel<D, BY_VALUE>, dim3(blocks), dim3(64 * wgt_waves(D)), stream, a, words);
 }
 template <bool BY_VALUE>
-void launch_weights(int d, bool few, const WeightArgs& a, const PlanWords<BY_VALUE>& words, unsigned blocks, hipStream_t stream) {
+hipError_t launch_weights(int d, bool few, const WeightArgs& a, const PlanWords<BY_VALUE>& words, unsigned blocks, hipStream_t stream) {
     switch (d) {
-        case 64: launch_weights_d<64>(few, a, words, blocks, stream); break;
-        case 128: launch_weights_d<128>(few, a, words, blocks, stream); break;
-        default: launch_weights_d<256>(few, a, words, blocks, stream); break;
+        case 64: return launch_weights_d<64>(few, a, words, blocks, stream);
+        case 128: return launch_weights_d<128>(few, a, words, blocks, stream);
+        default: return launch_weights_d<256>(few, a, words, blocks, stream);
     }
 }
 template <bool BY_VALUE>
-void launch_weights_merge(int d, const WeightArgs& a, const PlanWords<BY_VALUE>& words, unsigned blocks, hipStream_t stream) {
+hipError_t launch_weights_merge(int d, const WeightArgs& a, const PlanWords<BY_VALUE>& words, unsigned blocks, hipStream_t stream) {
     const dim3 block((unsigned)wgt_keys(d));
-    if (d == 256) hipLaunchKernelGGL((attn_weights_merge_kernel<wgt_keys(256), BY_VALUE>), dim3(blocks), block, 0, stream, a, words);
-    else hipLaunchKernelGGL((attn_weights_merge_kernel<wgt_keys(128), BY_VALUE>), dim3(blocks), block, 0, stream, a, words);
+    return launch_in_place(d == 256 ? attn_weights_merge_kernel<wgt_keys(256), BY_VALUE> : attn_weights_merge_kernel<wgt_keys(128), BY_VALUE>, dim3(blocks), block,
+                           stream, a, words);
 }
 
 // The rows of a tile are cut on a grid of `run` row tiles of 64, the first quarter of them four times finer, so that the chip is full and the short units,
@@ -623,26 +620,21 @@ int32_t key_weights(const attn_shape* s, const void* q, const float* lse, int32_
         hipError_t e = hipSuccess;
         if (n_few > 0) {
             a.units = (int32_t)few_at;
-            launch_weights(s->d, true, a, words, (unsigned)(n_few * s->H_kv), stream);
-            e = hipGetLastError();
+            e = launch_weights(s->d, true, a, words, (unsigned)(n_few * s->H_kv), stream);
         }
         if (e == hipSuccess && n_wide > 0) {
             a.units = 0;
-            launch_weights(s->d, false, a, words, (unsigned)(n_wide * s->H_kv), stream);
-            e = hipGetLastError();
+            e = launch_weights(s->d, false, a, words, (unsigned)(n_wide * s->H_kv), stream);
         }
-        if (e == hipSuccess && n_cut > 0) {
-            launch_weights_merge(s->d, a, words, (unsigned)(n_cut * s->H_kv), stream);
-            e = hipGetLastError();
-        }
+        if (e == hipSuccess && n_cut > 0) e = launch_weights_merge(s->d, a, words, (unsigned)(n_cut * s->H_kv), stream);
         return hip_err(e);
     };
     return plan.by_value() ? launch(plan.words()) : launch(PlanWords<false>());
 }
 
 template <int D, bool BY_VALUE>
-void launch_gather(const EvictArgs& a, const PlanWords<BY_VALUE>& words, unsigned blocks, hipStream_t stream) {
-    hipLaunchKernelGGL((attn_gather_rows_kernel<D, BY_VALUE>), dim3(blocks), dim3(GATHER_THREADS), 0, stream, a, words);
+hipError_t launch_gather(const EvictArgs& a, const PlanWords<BY_VALUE>& words, unsigned blocks, hipStream_t stream) {
+    return launch_in_place(attn_gather_rows_kernel<D, BY_VALUE>, dim3(blocks), dim3(GATHER_THREADS), stream, a, words);
 }
 
 int32_t evict(const attn_shape* s, int32_t n_req, const int32_t* rows, const int32_t* keep, const int32_t* first, const int32_t* recent,
@@ -719,15 +711,13 @@ int32_t evict(const attn_shape* s, int32_t n_req, const int32_t* rows, const int
     a.page_shift = shift_of(pages);
     auto launch = [&](const auto& words) {
         constexpr bool BY_VALUE = std::is_same<std::decay_t<decltype(words)>, PlanWords<true>>::value;
-        hipLaunchKernelGGL((attn_select_kernel<BY_VALUE>), dim3((unsigned)(n_req * s->H_kv)), dim3(SEL_THREADS), 0, stream, a, words);
-        const hipError_t e = hipGetLastError();
+        const hipError_t e = launch_in_place(attn_select_kernel<BY_VALUE>, dim3((unsigned)(n_req * s->H_kv)), dim3(SEL_THREADS), stream, a, words);
         if (e != hipSuccess) return hip_err(e);
         switch (s->d) {
-            case 64: launch_gather<64>(a, words, (unsigned)blocks, stream); break;
-            case 128: launch_gather<128>(a, words, (unsigned)blocks, stream); break;
-            default: launch_gather<256>(a, words, (unsigned)blocks, stream); break;
+            case 64: return hip_err(launch_gather<64>(a, words, (unsigned)blocks, stream));
+            case 128: return hip_err(launch_gather<128>(a, words, (unsigned)blocks, stream));
+            default: return hip_err(launch_gather<256>(a, words, (unsigned)blocks, stream));
         }
-        return hip_err(hipGetLastError());
     };
     return plan.by_value() ? launch(plan.words()) : launch(PlanWords<false>());
 }
