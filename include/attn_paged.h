@@ -2,9 +2,9 @@
  * attn_paged — an attention layer's keys and values in pages, for one MI355X (gfx950): rotary positions with the
  * append, attention of a chunk of new tokens, the attention weight every cached row gathers, and eviction by that
  * weight.  Same library and conventions as attn_resume.h (host / device pointers named per argument, validation
- * before anything is enqueued, negative error codes, no device allocation, no stream synchronisation except the wait for an
- * earlier call's plan upload to leave its pinned staging buffer).  Under graph capture, a call whose index arrays need that
- * buffer (more than 1792 words of page ids and plan) is refused with the capture's error; a replay of a smaller one repeats its arrays.
+ * before anything is enqueued, negative error codes, no device allocation, no stream synchronisation: a call whose index arrays need a
+ * pinned staging buffer, more than 1792 words of page ids and plan, waits for one of eight for 2 ms at most).  Under graph capture such
+ * a call is refused with the capture's error; a replay of a smaller one repeats its arrays.
  *
  * The cache.  A pool of n_pages pages per tensor; page p is at pool + p * page_stride (elements) and holds
  * page_rows rows of every key/value head, [H_kv][page_rows][d]: keys in bf16, values in fp16 (as in attn_resume.h: the

@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <chrono>
 #include <cmath>
 #include <mutex>
 #include <thread>
@@ -124,11 +125,14 @@ int32_t check_front(const attn_shape* s, int32_t n_req, const attn_pages* pages)
 }
 
 // ---- a call's plan (its index arrays) to the device.  Up to PLAN_WORDS go by value, in the arguments of the call's launches, and up to SMALL_WORDS in those
-// of a small launch (gdn::upload_plan).  Longer page tables cost more: a copy of more than 16 KiB takes the stream 20 us between two kernels.  These
-// are written into pinned memory, out of which a launch of ours reads them (4 us for 90 KB).  The buffers form a ring; a workgroup that has read
-// its piece says so in a word of the buffer, and a call that comes round to a buffer waits (on the host) for all of them.  A graph's replay would read
-// what a later call wrote there, and its capture reads nothing that the wait could see: such a call under capture is refused.
+// of a small launch (gdn::write_plan).  Longer page tables cost more: a copy of more than 16 KiB takes the stream 20 us between two kernels.  These
+// are written into pinned memory, out of which a launch of ours reads them (4 us for 90 KB).  The buffers are the process's; a workgroup that has read
+// its piece says so in a word of the buffer, and a buffer is free when all of them have.  Where none is, a call waits (on the host, with no lock held)
+// for FETCH_PATIENCE at most: calls in a row on a busy stream stay that close to the device.  Behind that its plan goes by value, in small launches (26 for
+// 90 KB), so that a stream that stands still, or a device that has failed, holds up no call on another one.  A graph's replay would read
+// what a later call wrote to a buffer, and its capture reads nothing that the wait could see: such a call under capture is refused.
 constexpr int FETCH_RING = 8, FETCH_THREADS = 256, FETCH_PIECE = 16 * FETCH_THREADS;   // bytes per workgroup
+constexpr std::chrono::microseconds FETCH_PATIENCE(2000);
 constexpr int SMALL_WORDS = 1792;
 
 __global__ void __launch_bounds__(FETCH_THREADS) attn_fetch_kernel(const u32x4* src, u32x4* dst, int64_t n, uint32_t* read, uint32_t mark) {
@@ -138,45 +142,80 @@ __global__ void __launch_bounds__(FETCH_THREADS) attn_fetch_kernel(const u32x4* 
     if (threadIdx.x == 0) __hip_atomic_store(read + blockIdx.x, mark, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
 }
 
-struct FetchRing {
-    std::mutex mu;
+class FetchRing {
+  public:
     struct Slot {
         char* host = nullptr;             // words of the workgroups that have read, then the plan
         size_t bytes = 0;                 // room for the plan
         uint32_t mark = 0, blocks = 0;    // of the last upload
+        bool taken = false;               // a call is writing it
         size_t words_bytes() const { return (bytes / FETCH_PIECE * sizeof(uint32_t) + 255) / 256 * 256; }
-    } slot[FETCH_RING];
-    int next = 0;
+        bool read() const {
+            const uint32_t* const words = reinterpret_cast<const uint32_t*>(host);
+            for (uint32_t b = 0; b < blocks; ++b)
+                if (__atomic_load_n(words + b, __ATOMIC_ACQUIRE) != mark) return false;
+            return true;
+        }
+    };
+    // A free buffer, the caller's until it is given back, or nullptr.
+    Slot* take() {
+        std::lock_guard<std::mutex> lock(mu_);
+        for (int i = 0; i < FETCH_RING; ++i) {
+            Slot& s = slot_[(next_ + i) % FETCH_RING];
+            if (s.taken || !s.read()) continue;
+            s.taken = true;
+            next_ = (next_ + i + 1) % FETCH_RING;
+            return &s;
+        }
+        return nullptr;
+    }
+    void give_back(Slot* s) {
+        std::lock_guard<std::mutex> lock(mu_);
+        s->taken = false;
+    }
+
+  private:
+    std::mutex mu_;                       // held to look at the slots, not to wait or to write them
+    Slot slot_[FETCH_RING];
+    int next_ = 0;
 };
 FetchRing g_fetch;
 
 class Plan {
   public:
+    Plan() = default;
+    Plan(const Plan&) = delete;
+    Plan& operator=(const Plan&) = delete;
+    ~Plan() {
+        if (slot_) g_fetch.give_back(slot_);
+    }
     // Room for `ints` words at data(); up to PLAN_WORDS of them go by value.
     int32_t open(int64_t ints, hipStream_t stream) {
         ints_ = ints;
         by_value_ = ints <= PLAN_WORDS;
         if (ints <= SMALL_WORDS) {
-            data_ = small_.w;
+            data_ = by_value_ ? arguments_.w : small_.w;
             return GDN_OK;
         }
         hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
         const hipError_t asked = hipStreamIsCapturing(stream, &capture);
         if (asked != hipSuccess) return hip_err(asked);
         if (capture != hipStreamCaptureStatusNone) return hip_err(hipErrorStreamCaptureUnsupported);
-        lock_ = std::unique_lock<std::mutex>(g_fetch.mu);
-        slot_ = &g_fetch.slot[g_fetch.next];
-        FetchRing::Slot& s = *slot_;
-        if (s.host) {
-            uint32_t* const read = reinterpret_cast<uint32_t*>(s.host);
-            for (uint32_t b = 0; b < s.blocks; ++b)
-                while (__atomic_load_n(read + b, __ATOMIC_ACQUIRE) != s.mark) std::this_thread::yield();
+        slot_ = g_fetch.take();
+        if (!slot_) {
+            const auto until = std::chrono::steady_clock::now() + FETCH_PATIENCE;
+            while (!(slot_ = g_fetch.take()) && std::chrono::steady_clock::now() < until) std::this_thread::yield();
         }
+        if (!slot_) {
+            long_.resize((size_t)ints);
+            data_ = long_.data();
+            return GDN_OK;
+        }
+        FetchRing::Slot& s = *slot_;
         const size_t bytes = (size_t)ints * sizeof(int32_t);
-        if (s.bytes < bytes) {
-            if (s.host) (void)hipHostFree(s.host);
-            s = FetchRing::Slot();
+        if (s.bytes < bytes) {            // (a buffer outgrown is not freed, which would wait for the device: the next one is more than twice as long)
             FetchRing::Slot fresh;
+            fresh.taken = true;
             fresh.bytes = (std::max<size_t>(2 * bytes, 1 << 17) + FETCH_PIECE - 1) / FETCH_PIECE * FETCH_PIECE;
             void* p = nullptr;
             const hipError_t e = hipHostMalloc(&p, fresh.bytes + fresh.words_bytes(), hipHostMallocCoherent | hipHostMallocPortable);
@@ -191,15 +230,12 @@ class Plan {
     int32_t* data() { return data_; }
     bool by_value() const { return by_value_; }
     const PlanWords<true>& words() const { return arguments_; }
-    // What data() holds to the workspace, or, by value, to words().
+    // What data() holds to the workspace (by value it is words()).
     int32_t send(void* workspace, hipStream_t stream) {
-        if (by_value_) {
-            std::memcpy(arguments_.w, small_.w, sizeof(int32_t) * (size_t)ints_);
-            return GDN_OK;
-        }
-        if (!slot_) return gdn::upload_plan(small_.w, sizeof(int32_t) * (size_t)ints_, workspace, stream);
-        FetchRing::Slot& s = *slot_;
+        if (by_value_) return GDN_OK;
         const size_t bytes = (size_t)ints_ * sizeof(int32_t);
+        if (!slot_) return gdn::write_plan(data_, bytes, workspace, stream);
+        FetchRing::Slot& s = *slot_;
         const uint32_t blocks = (uint32_t)((bytes + FETCH_PIECE - 1) / FETCH_PIECE), mark = s.mark + 1 == 0 ? 1 : s.mark + 1;
         hipLaunchKernelGGL(attn_fetch_kernel, dim3(blocks), dim3(FETCH_THREADS), 0, stream, reinterpret_cast<const u32x4*>(data_),
                            static_cast<u32x4*>(workspace), (int64_t)((bytes + 15) / 16), reinterpret_cast<uint32_t*>(s.host), mark);
@@ -207,19 +243,20 @@ class Plan {
         if (e != hipSuccess) return hip_err(e);
         s.mark = mark;
         s.blocks = blocks;
-        g_fetch.next = (g_fetch.next + 1) % FETCH_RING;
-        lock_.unlock();
+        g_fetch.give_back(slot_);
+        slot_ = nullptr;
         return GDN_OK;
     }
 
   private:
-    struct Small { int32_t w[SMALL_WORDS]; } small_;
-    PlanWords<true> arguments_;
+    struct Small { int32_t w[SMALL_WORDS]; };
+    alignas(64) Small small_;
+    alignas(64) PlanWords<true> arguments_;
+    std::vector<int32_t> long_;
     int32_t* data_ = nullptr;
     int64_t ints_ = 0;
     bool by_value_ = false;
-    FetchRing::Slot* slot_ = nullptr;
-    std::unique_lock<std::mutex> lock_;
+    FetchRing::Slot* slot_ = nullptr;     // this call's buffer, if it has one
 };
 
 int32_t rope_append(const attn_shape* s, const attn_rope* rope, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v,

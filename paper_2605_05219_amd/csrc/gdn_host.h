@@ -13,4 +13,7 @@ namespace gdn {
 // buffer.  Returns GDN_OK or a GDN_ERR_HIP code.
 int32_t upload_plan(const void* src, size_t bytes, void* dst, hipStream_t stream);
 
+// The same by value whatever the length, 3.5 KiB to a launch: nothing is waited for or kept.
+int32_t write_plan(const void* src, size_t bytes, void* dst, hipStream_t stream);
+
 }  // namespace gdn

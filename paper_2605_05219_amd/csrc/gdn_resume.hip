@@ -108,7 +108,10 @@ __global__ void __launch_bounds__(256) plan_write_kernel(PlanPiece piece, int32_
     for (int i = threadIdx.x; i < n; i += 256) dst[i] = piece.w[i];
 }
 
-// The words of a plan image, by value in the arguments of small launches: no staging buffer, nothing for a replay to find changed.
+}  // namespace
+
+// The words of a plan image, by value in the arguments of small launches: no staging buffer, nothing for a replay to find changed
+// (declared in gdn_host.h).
 int32_t write_plan(const void* src, size_t bytes, void* dst, hipStream_t stream) {
     const size_t words = bytes / sizeof(int32_t);
     for (size_t at = 0; at < words; at += PLAN_PIECE_WORDS) {
@@ -121,6 +124,8 @@ int32_t write_plan(const void* src, size_t bytes, void* dst, hipStream_t stream)
     }
     return GDN_OK;
 }
+
+namespace {
 
 // The device address of `scratch` on the current device, looked up once per device (the array's name is only a
 // host-side handle, never a device address: host code uses the pointer returned here).

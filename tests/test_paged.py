@@ -970,3 +970,89 @@ def test_key_weights_of_a_key_that_every_row_gives_minus_infinity(H_q, H_kv, d, 
         page, row = c.place(r, c.total[r])
         ref = po.key_weights(f64(q[s]), lse[s], f64(held[r]), starts[r], d ** -0.5, 1.0, None)
         assert (ref[at[r]] == 0).all() and (np.abs(w[page, :, row] - ref) <= rtol * ref).all(), r
+
+
+@pytest.mark.gpu
+def test_a_stream_that_stands_still_holds_up_no_call_on_another():
+    """More calls with long page tables behind half a second of other work than there are staging buffers, and one on another stream: each returns in
+    milliseconds, and all come out right."""
+    import time
+    import torch
+    c = Paged(72, 4, 2, 64, 16, [1] * 20, [1500 + 20 * i for i in range(20)]).fill()
+    assert c.page_ids.size > 1792
+    q = c.bf16(c.T, 4, 64)
+    want, wz = run_attend(c, q, None, "f32")
+    qd, sh = c.dev(q), AT.make_attn_shape(4, 2, 64, "f32")
+    outs = [(torch.zeros(c.T, 4, 64, device="cuda"), torch.zeros(c.T, 4, device="cuda"), c.workspace()) for _ in range(13)]
+
+    def call(i, stream=None):
+        o, z, ws = outs[i]
+        PG.attn_paged_prefill(sh, qd, None, c.cu, c.starts, c.k_pool, c.v_pool, c.page_cu, c.page_ids, o, z, ws, stream)
+
+    for i in range(13):                     # every buffer there is has been made
+        call(i)
+    for o, z, _ in outs:
+        o.fill_(float("nan"))
+        z.fill_(float("nan"))
+    a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    torch.cuda._sleep(1 << 20)
+    a.record()
+    torch.cuda._sleep(1 << 22)
+    b.record()
+    torch.cuda.synchronize()
+    cycles = int((1 << 22) * 500 / a.elapsed_time(b))                          # of half a second
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(cycles)
+    t0 = time.perf_counter()
+    for i in range(12):
+        call(i, side)
+    call(12)
+    host = time.perf_counter() - t0
+    torch.cuda.synchronize()
+    for o, z, _ in outs:
+        assert torch.equal(o, want) and torch.equal(z, wz)
+    assert host < 0.2, host
+
+
+@pytest.mark.gpu
+def test_threads_with_streams_of_their_own_keep_their_own_plans():
+    import threading
+    import torch
+    c = Paged(73, 4, 2, 64, 16, [1] * 24, [1200 + 30 * i for i in range(24)]).fill()
+    assert c.page_ids.size > 1792
+    q = c.bf16(c.T, 4, 64)
+    want, wz = run_attend(c, q, None, "f32")
+    torch.cuda.synchronize()
+    qd, sh = c.dev(q), AT.make_attn_shape(4, 2, 64, "f32")
+    work = []
+    for t in range(4):
+        rng, stream, ws = np.random.default_rng(t), torch.cuda.Stream(), c.workspace()
+        stream.wait_stream(torch.cuda.current_stream())
+        calls = []
+        for i in range(20):
+            order = rng.permutation(24)
+            at = torch.from_numpy(order).cuda()
+            tables = [c.table[r] for r in order]
+            calls.append((at, qd[at].contiguous(), np.asarray(c.starts)[order], np.concatenate([[0], np.cumsum([x.size for x in tables])]), np.concatenate(tables),
+                          torch.zeros(24, 4, 64, device="cuda"), torch.zeros(24, 4, device="cuda")))
+        work.append((stream, ws, calls))
+    torch.cuda.synchronize()
+    failed = []
+
+    def run(stream, ws, calls):
+        try:
+            for at, qt, st, tcu, ids, o, z in calls:
+                PG.attn_paged_prefill(sh, qt, None, np.arange(25), st, c.k_pool, c.v_pool, tcu, ids, o, z, ws, stream)
+        except Exception as e:              # noqa: BLE001
+            failed.append(e)
+    threads = [threading.Thread(target=run, args=w) for w in work]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not failed
+    for _, _, calls in work:
+        for at, _, _, _, _, o, z in calls:
+            assert torch.equal(o, want[at]) and torch.equal(z, wz[at])
