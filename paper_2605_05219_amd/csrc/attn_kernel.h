@@ -250,89 +250,40 @@ struct PageIds {
     }
 };
 
-// One query row over the keys [k_lo, k_hi), by a wave, without matrix instructions: what is left for rows that these gave something that is not a
-// number.  A weight of 0 times an infinite value is not a number, and the last tile that a row sees may hold values of later tokens; the row's own
-// result is the sum over what it sees.  Lane i gets D / 64 columns from i * D / 64 of the unnormalised output.
-template <int D>
-__device__ void walk_row(const PagedArgs& a, int first, int kvh, const uint16_t* q, int k_lo, int k_hi, float& m, float& l, float& le, float (&o)[D / 64]) {
-    constexpr int COLS = D / 64;
-    const int lane = threadIdx.x & 63, mask = (1 << a.page_shift) - 1;
-    const float c = a.scale_log2e;
-    m = -INFINITY;
-    l = le = 0.f;
+// A value that is not finite, times the weight 0 of a row that does not see it, is not a number.  In tiles that hold keys which some of a wave's rows do not
+// see, such values are taken out of the products (a matrix operand's eight go to 0, `kind` gets what they were), and those that a row sees are added to its
+// output afterwards, as the matrix product of their kinds with ones where the row sees the key: each kind is counted in bits of its own, 128 keys at most.
+__device__ __forceinline__ bool take_out_not_finite(half8& v, half8& kind) {
+    u32x4 x = __builtin_bit_cast(u32x4, v), k = {0u, 0u, 0u, 0u};
+    bool any = false;
 #pragma unroll
-    for (int i = 0; i < COLS; ++i) o[i] = 0.f;
-#pragma unroll 1
-    for (int base = k_lo; base < k_hi; base += 64) {
-        const int key = min(base + lane, k_hi - 1);
-        const int64_t at = (int64_t)a.page_ids[first + (key >> a.page_shift)] * a.slot_stride + (((int64_t)kvh << a.page_shift) + (key & mask)) * D;
-        float s = 0.f;
-#pragma unroll 1
-        for (int x = 0; x < D; x += 8) {
-            const u32x4 qv = *reinterpret_cast<const u32x4*>(q + x), kv = *reinterpret_cast<const u32x4*>(a.k_cache + at + x);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t qw = qv[i], kw = kv[i];
-                s = __builtin_fmaf(__builtin_bit_cast(float, qw << 16), __builtin_bit_cast(float, kw << 16), s);
-                s = __builtin_fmaf(__builtin_bit_cast(float, qw & 0xffff0000u), __builtin_bit_cast(float, kw & 0xffff0000u), s);
-            }
-        }
-        if (base + lane >= k_hi) s = -INFINITY;
-        float top = s;
-        for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-        const float m_new = fmaxf(m, top), m_ref = m_new == -INFINITY ? 0.f : m_new;
-        const float alpha = __builtin_amdgcn_exp2f((m - m_ref) * c);
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s, c, -m_ref * c)), ph = (float)(_Float16)p;
-        float sum = ph, esum = p;
-        for (int d = 32; d > 0; d >>= 1) {
-            sum += __shfl_xor(sum, d);
-            esum += __shfl_xor(esum, d);
-        }
-        l = l * alpha + sum;
-        le = le * alpha + esum;
-        m = m_new;
-#pragma unroll
-        for (int i = 0; i < COLS; ++i) o[i] *= alpha;
-        const int n = min(64, k_hi - base);
-#pragma unroll 1
-        for (int k = 0; k < n; ++k) {
-            const float w = __shfl(ph, k);
-            const int64_t row = (int64_t)__shfl((long long)at, k);
-#pragma unroll
-            for (int i = 0; i < COLS; ++i) o[i] += w * (float)__builtin_bit_cast(_Float16, a.v_cache[row + lane * COLS + i]);
-        }
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t w = x[i >> 1], h = (i & 1 ? w >> 16 : w) & 0xffffu;
+        const bool out = (h & 0x7c00u) == 0x7c00u;
+        const uint32_t count = h & 0x3ffu ? 0x7800u : h & 0x8000u ? 0x5c00u : 0x3c00u;      // 2^15, 2^8, 1 in fp16
+        k[i >> 1] |= out ? count << 16 * (i & 1) : 0u;
+        x[i >> 1] = out ? w & (i & 1 ? 0xffffu : 0xffff0000u) : w;
+        any |= out;
     }
+    v = __builtin_bit_cast(half8, x);
+    kind = __builtin_bit_cast(half8, k);
+    return any;
 }
-
-// Output column `col` of row (token, head): normalised, gated, stored.
-template <int D, typename OT>
-__device__ __forceinline__ void store_column(const AttnArgs& a, int64_t token, int head, int col, float y) {
-    const int64_t at = (token * a.H_q + head) * D + col;
-    if (a.gate) y *= 1.f / (1.f + __expf(-__builtin_bit_cast(float, (uint32_t)a.gate[at] << 16)));
-    if constexpr (sizeof(OT) == 4) static_cast<float*>(a.o)[at] = y;
-    else static_cast<uint16_t*>(a.o)[at] = __builtin_bit_cast(uint16_t, (__bf16)y);
+// Operand of ones where the row that sees the keys up to `last` sees `key`, `key` + 1, + 2, + 3, `key` + step, ...
+__device__ __forceinline__ half8 seen_of(int key, int step, int last) {
+    u32x4 k = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) k[i >> 1] |= key + (i >> 2) * step + (i & 3) <= last ? 0x3c00u << 16 * (i & 1) : 0u;
+    return __builtin_bit_cast(half8, k);
 }
-
-// walk_row's result to its place: a workspace row, or the output.
-template <int D, typename OT, bool LSE>
-__device__ void redo_row(const PagedArgs& a, int first, int kvh, int64_t token, int head, int k_lo, int k_hi, int64_t part_row) {
-    constexpr int COLS = D / 64;
-    const int lane = threadIdx.x & 63;
-    float m, l, le, o[COLS];
-    walk_row<D>(a, first, kvh, a.q + (token * a.H_q + head) * D, k_lo, k_hi, m, l, le, o);
-    if (part_row >= 0) {
-        if (lane == 0) {
-            *reinterpret_cast<f32x2*>(a.part_ml + part_row * 2) = f32x2{m, l};
-            if constexpr (LSE) a.part_le[part_row] = le;
-        }
-#pragma unroll
-        for (int i = 0; i < COLS; ++i) a.part_o[part_row * D + lane * COLS + i] = o[i];
-        return;
-    }
-    if constexpr (LSE)
-        if (lane == 0) a.lse[token * a.H_q + head] = row_lse(m, le, a.scale_log2e);
-#pragma unroll
-    for (int i = 0; i < COLS; ++i) store_column<D, OT>(a, token, head, lane * COLS + i, o[i] / l);
+// What `kinds`, a sum of such counts, adds to an output: 0, an infinity, or not a number.
+__device__ __forceinline__ float sum_not_finite(float kinds) {
+    const int n = (int)kinds;
+    float x = 0.f;
+    if (n & 0xff) x += INFINITY;
+    if (n >> 8 & 0x7f) x -= INFINITY;
+    if (n >> 15) x = __builtin_nanf("");
+    return x;
 }
 
 template <int D>
@@ -490,6 +441,58 @@ __global__ void __launch_bounds__(ATT_THREADS * NH, 2) attn_suffix_kernel(Args a
     const int vrow_off = SM::V_OFF + vrow * SM::ROW_BYTES + 8 * (i16 & 1);
     const int vchunk = 2 * b4 + ((i16 & 3) >> 1);                   // + 4*rb
 
+    // a tile's weights for this lane's query, from its logits: the operands of the products with the values; returns what the output so far is scaled by
+    auto weigh = [&](int kv0, f32x16 (&S)[ATT_KVB], half8 (&pf)[2 * ATT_KVB]) __attribute__((always_inline)) {
+        // ---- causal mask on the tiles that reach past the first row's limit
+        if (kv0 + ATT_KT - 1 > c0 + wq0) {
+#pragma unroll
+            for (int kvb = 0; kvb < ATT_KVB; ++kvb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int kv = kv0 + 32 * kvb + 8 * (i >> 2) + 4 * g + (i & 3);
+                    if (kv > lim) S[kvb][i] = -INFINITY;
+                }
+        }
+        // ---- online softmax for this lane's query
+        float mx = S[0][0];
+#pragma unroll
+        for (int kvb = 0; kvb < ATT_KVB; ++kvb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, S[kvb][i]);
+        mx = max_with_other_half(mx);
+        // The weights' reference is the running maximum itself, so that a row's heaviest weight is exactly 1 and carries no
+        // rounding.  (A reference that follows the maximum only when that has grown by 2^8 spares most passes over O, 4 % of a
+        // large call at d = 128, 7 % at 256, but rounds the weight that counts most to fp16 like the others: errors 1.6 to 1.7 times as large on peaked rows.)
+        const float m_new = fmaxf(m, mx);
+        // -inf only in a part of a split walk whose first tiles lie past this query's limit: nothing to weigh yet
+        const float m_ref = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = __builtin_amdgcn_exp2f((m - m_ref) * c);
+        const float mc = m_ref * c;
+        m = m_new;
+        float lsum = 0.f, esum = 0.f;
+#pragma unroll
+        for (int s = 0; s < 2 * ATT_KVB; ++s) {
+            f32x2 e[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                e[j][0] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[s >> 1][8 * (s & 1) + 2 * j], c, -mc));
+                e[j][1] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[s >> 1][8 * (s & 1) + 2 * j + 1], c, -mc));
+            }
+            if constexpr (LSE) esum += ((e[0][0] + e[0][1]) + (e[1][0] + e[1][1])) + ((e[2][0] + e[2][1]) + (e[3][0] + e[3][1]));
+            half2 h[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                h[j] = __builtin_convertvector(e[j], half2);
+                const half2 one = {(_Float16)1.0f, (_Float16)1.0f};
+                lsum = __builtin_amdgcn_fdot2(h[j], one, lsum, false);   // the sum of the ROUNDED weights
+            }
+            pf[s] = __builtin_shufflevector(__builtin_shufflevector(h[0], h[1], 0, 1, 2, 3),
+                                            __builtin_shufflevector(h[2], h[3], 0, 1, 2, 3), 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+        l = l * alpha + lsum;
+        if constexpr (LSE) le = le * alpha + esum;
+        return alpha;
+    };
     // one key tile: this wave's part of tile t in stage sb, the loads of tile t + 1 to the other stage
     auto tile = [&](int t, const char* sb, char* other) {
         wait_vmcnt<0>();
@@ -527,55 +530,8 @@ __global__ void __launch_bounds__(ATT_THREADS * NH, 2) attn_suffix_kernel(Args a
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);        // one key fragment read
             if (i < 2 * PPW) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);   // one load to LDS
         }
-        // ---- causal mask on the tiles that reach past the first row's limit
-        if (kv0 + ATT_KT - 1 > c0 + wq0) {
-#pragma unroll
-            for (int kvb = 0; kvb < ATT_KVB; ++kvb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int kv = kv0 + 32 * kvb + 8 * (i >> 2) + 4 * g + (i & 3);
-                    if (kv > lim) S[kvb][i] = -INFINITY;
-                }
-        }
-        // ---- online softmax for this lane's query
-        float mx = S[0][0];
-#pragma unroll
-        for (int kvb = 0; kvb < ATT_KVB; ++kvb)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, S[kvb][i]);
-        mx = max_with_other_half(mx);
-        // The weights' reference is the running maximum itself, so that a row's heaviest weight is exactly 1 and carries no
-        // rounding.  (A reference that follows the maximum only when that has grown by 2^8 spares most passes over O, 4 % of a
-        // large call at d = 128, 7 % at 256, but rounds the weight that counts most to fp16 like the others: errors 1.6 to 1.7 times as large on peaked rows.)
-        const float m_new = fmaxf(m, mx);
-        // -inf only in a part of a split walk whose first tiles lie past this query's limit: nothing to weigh yet
-        const float m_ref = m_new == -INFINITY ? 0.f : m_new;
-        const float alpha = __builtin_amdgcn_exp2f((m - m_ref) * c);
-        const float mc = m_ref * c;
-        m = m_new;
         half8 pf[2 * ATT_KVB];                 // B operands of the 16-row steps
-        float lsum = 0.f, esum = 0.f;
-#pragma unroll
-        for (int s = 0; s < 2 * ATT_KVB; ++s) {
-            f32x2 e[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                e[j][0] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[s >> 1][8 * (s & 1) + 2 * j], c, -mc));
-                e[j][1] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[s >> 1][8 * (s & 1) + 2 * j + 1], c, -mc));
-            }
-            if constexpr (LSE) esum += ((e[0][0] + e[0][1]) + (e[1][0] + e[1][1])) + ((e[2][0] + e[2][1]) + (e[3][0] + e[3][1]));
-            half2 h[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                h[j] = __builtin_convertvector(e[j], half2);
-                const half2 one = {(_Float16)1.0f, (_Float16)1.0f};
-                lsum = __builtin_amdgcn_fdot2(h[j], one, lsum, false);   // the sum of the ROUNDED weights
-            }
-            pf[s] = __builtin_shufflevector(__builtin_shufflevector(h[0], h[1], 0, 1, 2, 3),
-                                            __builtin_shufflevector(h[2], h[3], 0, 1, 2, 3), 0, 1, 2, 3, 4, 5, 6, 7);
-        }
-        l = l * alpha + lsum;
-        if constexpr (LSE) le = le * alpha + esum;
+        const float alpha = weigh(kv0, S, pf);
         if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0) {
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb)
@@ -608,57 +564,132 @@ __global__ void __launch_bounds__(ATT_THREADS * NH, 2) attn_suffix_kernel(Args a
     }
 
     wait_vmcnt<0>();                           // no load to LDS may be in flight when the workgroup's LDS is given back
-    auto part_row = [&](int row) {
-        return part >= 0 ? ((int64_t)part * (a.H_q / R) + hb) * ATT_BQ + row : a.few_row0 + ((int64_t)(-2 - part) * (a.H_q / R) + hb) * NAR_ROWS + row;
+    // ---- Rows that came out as not a number because of a value that they do not see (of a later token, in their last tiles: 0 times infinity) are walked
+    // once more, further down.  A row whose own normaliser is not a number, or in front of which no unseen value is infinite or not a number, is
+    // what it should be.
+    bool again = false;
+    const int t_end = min(t1, n_tiles_w);
+    // (pages) where row `row` of the request lies; behind its last one: some row of its last page, which nothing sees
+    auto row_at = [&](int row) -> int64_t {
+        if constexpr (PAGED)
+            return slot_at + (int64_t)a.page_ids[a.slot[r] + (min(row, kv_len - 1) >> a.page_shift)] * a.slot_stride + (int64_t)(row & ((1 << a.page_shift) - 1)) * D;
+        else return 0;
     };
-    if constexpr (PAGED) {                     // rows with something that is not a number are walked again (see walk_row)
+    if constexpr (PAGED) {
+        const int unseen = max(c0 + wq0 + 1, t0 * ATT_KT), seen_end = min(t_end * ATT_KT, kv_len);
         bool bad = false;
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
             for (int i = 0; i < 16; ++i) bad |= O[rb][i] != O[rb][i];
-        const uint64_t lanes = __builtin_amdgcn_ballot_w64(bad && valid);
-        for (uint32_t cols = (uint32_t)lanes | (uint32_t)(lanes >> 32); cols != 0; cols &= cols - 1) {
-            const int x = __builtin_ctz(cols);
-            const int row = 32 * wave + x, tok = q0 + row / R, head = hb * R + row % R;
-            redo_row<D, OT, LSE>(a, a.slot[r], kvh, tok0 + tok, head, t0 * ATT_KT, min(t1 * ATT_KT, c0 + tok + 1), part == -1 ? -1 : part_row(row));
-            if (col == x) valid = false;
-        }
-    }
-    // ---- a part of a split walk leaves its unnormalised result in its workspace slot
-    if (part != -1) {
-        if (valid) {
-            const int64_t prow = part_row(wrow);
-            const float lt = sum_with_other_half(l);
-            if (g == 0) *reinterpret_cast<f32x2*>(a.part_ml + prow * 2) = f32x2{m, lt};
-            if constexpr (LSE) {
-                const float let = sum_with_other_half(le);
-                if (g == 0) a.part_le[prow] = let;
+        const float lt = sum_with_other_half(l);
+        if (seen_end > unseen && __builtin_amdgcn_ballot_w64(bad && valid && lt == lt) != 0) {
+            int last_bad = -1;                                     // the last of the unseen rows with such a value
+#pragma unroll 1
+            for (int i = lane; i < (seen_end - unseen) * CPR; i += 64) {
+                const int row = unseen + i / CPR;
+                const u32x4 v = *reinterpret_cast<const u32x4*>(a.v_cache + row_at(row) + 8 * (i % CPR));
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                    if ((v[x] & 0x7c00u) == 0x7c00u || (v[x] & 0x7c000000u) == 0x7c000000u) last_bad = row;
             }
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-                for (int b = 0; b < 4; ++b)
-                    *reinterpret_cast<f32x4*>(a.part_o + prow * D + 32 * rb + 8 * b + 4 * g) =
-                        f32x4{O[rb][4 * b], O[rb][4 * b + 1], O[rb][4 * b + 2], O[rb][4 * b + 3]};
+            for (int d = 32; d > 0; d >>= 1) last_bad = max(last_bad, __shfl_xor(last_bad, d));
+            const uint64_t lanes = __builtin_amdgcn_ballot_w64(bad && valid && lt == lt && lim < last_bad);
+            again = ((uint32_t)lanes | (uint32_t)(lanes >> 32)) >> col & 1;
         }
-        return;
     }
-    // ---- normalise, gate, store: register 4b+e of tile rb is value column 32*rb + 8*b + 4*g + e
-    if (valid) {
-        const float inv = 1.f / sum_with_other_half(l);
-        const int64_t base = ((int64_t)(tok0 + q0 + tl) * a.H_q + hq) * D;
+    // a row's statistics, and the 32 columns from 32 * rb of its output: a part of a split walk leaves its unnormalised result in its workspace slot, the
+    // others are normalised, gated and stored; register 4b+e is value column 32*rb + 8*b + 4*g + e
+    const int64_t prow = part >= 0 ? ((int64_t)part * (a.H_q / R) + hb) * ATT_BQ + wrow : a.few_row0 + ((int64_t)(-2 - part) * (a.H_q / R) + hb) * NAR_ROWS + wrow;
+    const int64_t orow = (int64_t)(tok0 + q0 + tl) * a.H_q + hq;
+    auto store_sums = [&]() __attribute__((always_inline)) {
+        const float lt = sum_with_other_half(l);
+        if (part != -1 && g == 0) *reinterpret_cast<f32x2*>(a.part_ml + prow * 2) = f32x2{m, lt};
         if constexpr (LSE) {
-            const float lse = row_lse(m, sum_with_other_half(le), c);
-            if (g == 0) a.lse[(int64_t)(tok0 + q0 + tl) * a.H_q + hq] = lse;
-        }
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                const int dv = 32 * rb + 8 * b + 4 * g;
-                store_out<OT>(a.o, a.gate, base + dv, f32x4{O[rb][4 * b] * inv, O[rb][4 * b + 1] * inv, O[rb][4 * b + 2] * inv, O[rb][4 * b + 3] * inv});
+            const float let = sum_with_other_half(le);
+            if (g == 0) {
+                if (part != -1) a.part_le[prow] = let;
+                else a.lse[orow] = row_lse(m, let, c);
             }
+        }
+        return 1.f / lt;
+    };
+    auto store_columns = [&](int rb, const f32x16& x, float inv) __attribute__((always_inline)) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const int dv = 32 * rb + 8 * b + 4 * g;
+            const f32x4 y = {x[4 * b], x[4 * b + 1], x[4 * b + 2], x[4 * b + 3]};
+            if (part != -1) *reinterpret_cast<f32x4*>(a.part_o + prow * D + dv) = y;
+            else store_out<OT>(a.o, a.gate, orow * D + dv, y * inv);
+        }
+    };
+    if (valid && !again) {
+        const float inv = store_sums();
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) store_columns(rb, O[rb], inv);
+    }
+    // ---- The second walk, by the wave alone and out of memory, 32 columns of the output at a time (so that it asks for no more registers than the first): in
+    // tiles with unseen keys, values that are not finite go apart.  Nothing else pays for it.  16 heads on 2, d = 128: the last of 400 tokens behind 6000
+    // brings an infinity 63 -> 277 us, a column of infinities in every row 270; 8192 tokens with such a column 290 -> 4400; a cached value in front of the
+    // chunk that is not a number 63.
+    if constexpr (PAGED) {
+        if (__builtin_amdgcn_ballot_w64(again) == 0) return;
+        int first = __builtin_amdgcn_readfirstlane(q0);
+        asm volatile("" : "+s"(first));            // (the queries' addresses are made anew, not kept through the first walk)
+        const uint16_t* const qp = a.q + ((int64_t)(tok0 + min(first + tl, q_end - 1)) * a.H_q + hq) * D + 8 * g;
+#pragma unroll 1
+        for (int rb = 0; rb < RB; ++rb) {
+            m = -INFINITY;
+            l = le = 0.f;
+            f32x16 Y;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) Y[i] = 0.f;
+#pragma unroll 1
+            for (int t = t0; t < t_end; ++t) {
+                const int kv0 = t * ATT_KT;
+                f32x16 S[ATT_KVB];
+#pragma unroll
+                for (int kvb = 0; kvb < ATT_KVB; ++kvb) {
+                    const uint16_t* const kp = a.k_cache + row_at(kv0 + 32 * kvb + col) + 8 * g;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) S[kvb][i] = 0.f;
+#pragma unroll
+                    for (int kb = 0; kb < KB; ++kb) {
+                        const u32x4 kf = *reinterpret_cast<const u32x4*>(kp + 16 * kb), q = *reinterpret_cast<const u32x4*>(qp + 16 * kb);
+                        S[kvb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, q), S[kvb], 0, 0, 0);
+                        if (kb % 4 == 3) __builtin_amdgcn_sched_barrier(0);      // (no more registers than the first walk's)
+                    }
+                }
+                half8 pf[2 * ATT_KVB];
+                const float alpha = weigh(kv0, S, pf);
+                const bool apart = kv0 + ATT_KT - 1 > c0 + wq0;
+                f32x16 kinds;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) { Y[i] *= alpha; kinds[i] = 0.f; }
+                bool any = false;
+#pragma unroll
+                for (int s = 0; s < 2 * ATT_KVB; ++s) {
+                    const uint16_t* const vp = a.v_cache + row_at(kv0 + 16 * s) + 4 * g * D + 32 * rb + col;     // (16 rows lie in one page)
+                    u32x4 w;
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const int key = 8 * (x >> 1) + 2 * (x & 1);
+                        w[x] = (uint32_t)vp[key * D] | (uint32_t)vp[(key + 1) * D] << 16;
+                    }
+                    half8 vf = __builtin_bit_cast(half8, w), kind;
+                    if (apart && __builtin_amdgcn_ballot_w64(take_out_not_finite(vf, kind)) != 0) {
+                        kinds = __builtin_amdgcn_mfma_f32_32x32x16_f16(kind, seen_of(kv0 + 16 * s + 4 * g, 8, lim), kinds, 0, 0, 0);
+                        any = true;
+                    }
+                    Y = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, pf[s], Y, 0, 0, 0);
+                }
+                if (any)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) Y[i] += sum_not_finite(kinds[i]);
+            }
+            if (again) store_columns(rb, Y, store_sums());
+        }
     }
 }
 
@@ -715,7 +746,6 @@ __global__ void __launch_bounds__(ATT_THREADS, narrow_wgs_per_cu(D)) attn_narrow
     // do not depend on the loads to LDS in flight to the other, for which it would wait otherwise
     __shared__ __attribute__((aligned(1024))) char ring0[4][SM::BLOCK_BYTES], ring1[4][SM::BLOCK_BYTES];
     __shared__ float ml[4][NAR_ROWS][LSE ? 3 : 2];
-    __shared__ int bad[PAGED ? NAR_ROWS : 1];                // pages: rows with something that is not a number
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -877,15 +907,31 @@ __global__ void __launch_bounds__(ATT_THREADS, narrow_wgs_per_cu(D)) attn_narrow
             for (int i = 0; i < DB; ++i) O[i] *= alpha;
         }
         // ---- O^T += V^T P^T
-#pragma unroll
-        for (int db = 0; db < DB; ++db) {
+        auto values = [&](int db) __attribute__((always_inline)) {
             const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(
                 st + vbase + (((2 * db + vch) ^ SM::f(vrow)) << 4)));
             const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(
                 st + vbase + 16 * SM::ROW_BYTES + (((2 * db + vch) ^ SM::f(vrow + 16)) << 4)));
-            O[db] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)), pf,
-                                                           O[db], 0, 0, 0);
-        }
+            return __builtin_bit_cast(half8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        };
+        if constexpr (PAGED)
+            if (kv0 + NAR_KEYS - 1 > c0 && n > 1) {          // keys that some rows do not see: at most the last two blocks of a walk
+                const half8 sees = seen_of(kv0 + 4 * g, 16, lim);
+#pragma unroll
+                for (int db = 0; db < DB; ++db) {
+                    half8 vf = values(db), kind;
+                    const bool any = __builtin_amdgcn_ballot_w64(take_out_not_finite(vf, kind)) != 0;
+                    O[db] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf, O[db], 0, 0, 0);
+                    if (any) {
+                        const f32x4 kinds = __builtin_amdgcn_mfma_f32_16x16x32_f16(kind, sees, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) O[db][e] += sum_not_finite(kinds[e]);
+                    }
+                }
+                return;
+            }
+#pragma unroll
+        for (int db = 0; db < DB; ++db) O[db] = __builtin_amdgcn_mfma_f32_16x16x32_f16(values(db), pf, O[db], 0, 0, 0);
     };
 
     // block j is here, block j + 1 on its way; nothing of a block's work moves up between the loads of the next one, and
@@ -916,7 +962,6 @@ __global__ void __launch_bounds__(ATT_THREADS, narrow_wgs_per_cu(D)) attn_narrow
     // ---- merge of the four waves: each leaves its result in LDS, in the place of the value blocks
     wait_vmcnt<0>();
     __syncthreads();
-    if (PAGED && threadIdx.x < NAR_ROWS) bad[threadIdx.x] = 0;
     auto om = [&](int w, int row) {                          // a row of wave w's result: waves 0, 1 in one half, 2, 3 in the other
         return reinterpret_cast<float*>(w < 2 ? &ring0[0][0] : &ring1[0][0]) + ((w & 1) * NAR_ROWS + row) * SM::OROW;
     };
@@ -945,8 +990,6 @@ __global__ void __launch_bounds__(ATT_THREADS, narrow_wgs_per_cu(D)) attn_narrow
             L += wt * ml[w][row][1];
             if constexpr (LSE) Le += wt * ml[w][row][2];
         }
-        if constexpr (PAGED)
-            if (n > 1 && (acc[0] != acc[0] || acc[1] != acc[1] || acc[2] != acc[2] || acc[3] != acc[3])) bad[row] = 1;
         if (part >= 0) {
             const int64_t prow = a.few_row0 + ((int64_t)part * a.H_kv + kvh) * NAR_ROWS + row;
             if (dv == 0) *reinterpret_cast<f32x2*>(a.part_ml + prow * 2) = f32x2{M, L};
@@ -957,14 +1000,6 @@ __global__ void __launch_bounds__(ATT_THREADS, narrow_wgs_per_cu(D)) attn_narrow
             if constexpr (LSE) if (dv == 0) a.lse[(int64_t)(tok0 + t) * a.H_q + kvh * G + row - t * G] = row_lse(M, Le, c);
             store_out<OT>(a.o, a.gate, ((int64_t)(tok0 + t) * a.H_q + kvh * G + row - t * G) * D + dv, acc * (1.f / L));
         }
-    }
-    if constexpr (PAGED) {                                   // a single token sees every row there is
-        if (n == 1) return;
-        __syncthreads();
-        for (int row = wave; row < rows; row += 4)
-            if (bad[row])
-                redo_row<D, OT, LSE>(a, slot, kvh, tok0 + row / G, kvh * G + row % G, k0, min(k1, c0 + row / G + 1),
-                                     part >= 0 ? a.few_row0 + ((int64_t)part * a.H_kv + kvh) * NAR_ROWS + row : -1);
     }
 }
 

@@ -1056,3 +1056,96 @@ def test_threads_with_streams_of_their_own_keep_their_own_plans():
     for _, _, calls in work:
         for at, _, _, _, _, o, z in calls:
             assert torch.equal(o, want[at]) and torch.equal(z, wz[at])
+
+
+def attend_with_not_finite_values(q, k, v, start, scale):
+    """The definition row by row: what a row does not see adds nothing, a weight above 0 times an infinity is that infinity."""
+    n, H_q, d = q.shape
+    G = H_q // k.shape[1]
+    finite = np.where(np.isfinite(v), v, 0.0)
+    o = ao.attention_suffix(q, k, finite, start, scale)
+    plus, minus, nan = (np.cumsum(x, 0) > 0 for x in (v == np.inf, v == -np.inf, np.isnan(v)))
+    for t in range(n):
+        for x, what in ((plus, np.inf), (minus, -np.inf), (nan, np.nan)):
+            with np.errstate(invalid="ignore"):         # (infinities of both signs)
+                o[t] += np.where(np.repeat(x[start + t], G, 0), what, 0.0)
+    return o
+
+
+NOT_FINITE = [  # H_q, H_kv, d, P, lens, starts
+    (4, 2, 64, 16, [40], [3]), (16, 2, 128, 32, [24, 5], [100, 60]), (6, 2, 64, 64, [200], [63]), (8, 8, 256, 64, [70], [400]), (32, 4, 128, 128, [400], [600]),
+    (1, 1, 128, 16, [129], [0]), (2, 2, 256, 16, [300], [17]),
+    (4, 1, 128, 16, [3], [1300]), (1, 1, 64, 32, [9], [1100]), (8, 8, 256, 64, [14], [1500]), (16, 2, 64, 128, [2, 2, 2], [1024, 1500, 3000]),   # few rows
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H_q,H_kv,d,P,lens,starts", NOT_FINITE)
+@pytest.mark.parametrize("kind", ["cached", "column", "column of the new", "signs"])
+def test_values_that_are_not_finite_reach_the_rows_and_columns_that_see_them(H_q, H_kv, d, P, lens, starts, kind):
+    """cached: one such value in front of the chunk.  column: a column of infinities, seen and unseen.  signs: infinities of both signs and a NaN among the new
+    rows, in three columns of which one has all of them.  Everything else stays finite and right."""
+    import torch
+    c = Paged(64, H_q, H_kv, d, P, lens, starts)
+    for r, (n, s) in enumerate(zip(lens, starts)):
+        v = c.v_rows[r]
+        if kind == "cached":
+            v[s // 2, 0, 7] = np.inf
+            v[(s + n) // 2, -1, 9] = np.nan
+        elif kind == "column":
+            v[:, 0, 33] = np.inf
+        elif kind == "column of the new":
+            v[s:, 0, 33] = -np.inf
+        else:
+            at = s + np.arange(n)
+            v[at[n // 3], :, 1] = np.inf
+            v[at[n // 2], :, 1] = -np.inf
+            v[at[n // 3], :, 40] = -np.inf
+            v[at[-1], :, 1] = v[at[-1], :, 63] = np.nan
+    c.fill()
+    q = c.bf16(c.T, H_q, d, s=0.5)                     # (no weight rounds to 0)
+    o, z = run_attend(c, q, None, "f32")
+    o, z = o.double().cpu().numpy(), z.double().cpu().numpy()
+    le = logit_error(c, q)
+    for r in range(len(lens)):
+        s = slice(c.cu[r], c.cu[r + 1])
+        k, v = f64(c.k_rows[r]), c.v_rows[r].astype(np.float64)
+        ref = attend_with_not_finite_values(f64(q[s]), k, v, starts[r], d ** -0.5)
+        ok = np.isfinite(ref)
+        assert ((o[s] == ref) | (np.isnan(o[s]) & np.isnan(ref)))[~ok].all(), (r, np.argwhere(~ok & (o[s] != ref) & ~np.isnan(ref))[:5])
+        assert (np.abs(o[s] - np.where(ok, ref, 0.0))[ok] <= 2.0 ** -8 * np.abs(v[np.isfinite(v)]).max()).all(), r
+        zr = po.row_lse(f64(q[s]), k, starts[r], d ** -0.5)
+        assert (np.abs(z[s] - zr) <= le + 2.0 ** -20 * (1 + np.abs(zr))).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H_q,H_kv,d,lens,starts", [(16, 2, 128, [400], [6000]), (8, 2, 64, [600, 300], [3000, 2500]), (8, 8, 128, [8] * 32, [4000] * 32)])
+@pytest.mark.parametrize("kind", ["cached", "column"])
+def test_values_that_are_not_finite_cost_no_more_than_a_few_walks(H_q, H_kv, d, lens, starts, kind):
+    """One bad value among the cached rows, or an overflown column of all rows: a call may walk again what it has to, at the speed of a walk."""
+    import torch
+    c = Paged(65, H_q, H_kv, d, 64, lens, starts).fill()
+    q = c.dev(c.bf16(c.T, H_q, d, s=0.5))
+    sh = AT.make_attn_shape(H_q, H_kv, d, "bf16")
+    o, ws = torch.zeros(c.T, H_q, d, dtype=torch.bfloat16, device="cuda"), c.workspace()
+
+    def best():
+        times = []
+        for _ in range(6):
+            a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            a.record()
+            PG.attn_paged_prefill(sh, q, None, c.cu, c.starts, c.k_pool, c.v_pool, c.page_cu, c.page_ids, o, None, ws)
+            b.record()
+            torch.cuda.synchronize()
+            times.append(a.elapsed_time(b))
+        return min(times)
+    clean = best()
+    for r in range(len(lens)):
+        page, row = c.place(r, c.total[r])
+        if kind == "cached":
+            c.v_pool[int(page[5]), :, int(row[5]), 3] = float("nan")
+        else:
+            c.v_pool[torch.from_numpy(page.astype(np.int64)).cuda(), :, torch.from_numpy(row).cuda(), 3] = float("inf")
+    bad = best()
+    assert not bool(torch.isfinite(o[:, :, 3].float()).any()) and bool(torch.isfinite(o[:, :, :3].float()).all())
+    assert bad <= (1.5 if kind == "cached" else 40) * clean, (clean, bad)
