@@ -45,10 +45,33 @@ def _stream_ptr(stream=None):
 _ints = ctypes.c_int32 * 0
 
 
-def _ip(x):
-    """A host sequence as an int32 array that the call may read in place (a fifth of what `_hp` of `_h32` takes)."""
-    a = _h32(x)
+def _ip(a):
+    """An int32 array as an argument that the call reads in place (a fifth of what `_hp` takes)."""
     return _ints.from_buffer(a if a.flags.writeable else a.copy())
+
+
+def _per_request(n, *arrays):
+    """Host sequences of one entry per request (or None), as arguments."""
+    out = []
+    for x in arrays:
+        a = None if x is None else _h32(x)
+        if a is not None and a.size != n:
+            raise ValueError("index arrays have inconsistent lengths")
+        out.append(None if a is None else _ip(a))
+    return out
+
+
+def _offsets(n, cu, ids=None):
+    """Offsets of n requests, as an argument, and where they say into `ids`, that too."""
+    a = _h32(cu)
+    if a.size != n + 1:
+        raise ValueError("index arrays have inconsistent lengths")
+    if ids is None:
+        return _ip(a)
+    b = _h32(ids)
+    if b.size < a[-1]:
+        raise ValueError("index arrays have inconsistent lengths")
+    return _ip(a), _ip(b)
 
 
 _ready = False
@@ -142,19 +165,21 @@ def attn_rope_append(shape: attn_shape, rope: attn_rope, q, k, v, cu_seqlens, po
     """See include/attn_paged.h.  q, k, v are [T][heads][d] tensors whose token stride is passed on (heads and elements packed);
     pos may be None."""
     _packed(q_out)
-    _check(_lib().attn_rope_append(ctypes.byref(shape), ctypes.byref(rope), _dp(q), _ld(q), _dp(k), _ld(k), _dp(v), _ld(v),
-                                   len(start), _ip(cu_seqlens), None if pos is None else _ip(pos), _ip(start), _pages(shape, k_pool, v_pool),
-                                   _dp(k_pool), _dp(v_pool), _ip(page_cu), _ip(page_ids), _dp(q_out), *_ws(workspace), _stream_ptr(stream)),
-           "attn_rope_append")
+    n = len(start)
+    cu, (pos, start), (page_cu, page_ids) = _offsets(n, cu_seqlens), _per_request(n, pos, start), _offsets(n, page_cu, page_ids)
+    _check(_lib().attn_rope_append(ctypes.byref(shape), ctypes.byref(rope), _dp(q), _ld(q), _dp(k), _ld(k), _dp(v), _ld(v), n, cu, pos, start,
+                                   _pages(shape, k_pool, v_pool), _dp(k_pool), _dp(v_pool), page_cu, page_ids, _dp(q_out), *_ws(workspace),
+                                   _stream_ptr(stream)), "attn_rope_append")
 
 
 def attn_paged_prefill(shape: attn_shape, q, out_gate, cu_seqlens, start, k_pool, v_pool, page_cu, page_ids, o, lse, workspace,
                        stream=None) -> None:
     """See include/attn_paged.h.  out_gate and lse may be None."""
     _packed(q, out_gate, o, lse)
-    _check(_lib().attn_paged_prefill(ctypes.byref(shape), _dp(q), _dp(out_gate), len(start), _ip(cu_seqlens), _ip(start), _pages(shape, k_pool, v_pool),
-                                     _dp(k_pool), _dp(v_pool), _ip(page_cu), _ip(page_ids), _dp(o), _dp(lse), *_ws(workspace),
-                                     _stream_ptr(stream)), "attn_paged_prefill")
+    n = len(start)
+    cu, (start,), (page_cu, page_ids) = _offsets(n, cu_seqlens), _per_request(n, start), _offsets(n, page_cu, page_ids)
+    _check(_lib().attn_paged_prefill(ctypes.byref(shape), _dp(q), _dp(out_gate), n, cu, start, _pages(shape, k_pool, v_pool), _dp(k_pool), _dp(v_pool),
+                                     page_cu, page_ids, _dp(o), _dp(lse), *_ws(workspace), _stream_ptr(stream)), "attn_paged_prefill")
 
 
 def attn_key_weights(shape: attn_shape, q, lse, cu_seqlens, start, k_pool, page_cu, page_ids, decay, w_in, w_out, workspace,
@@ -164,15 +189,19 @@ def attn_key_weights(shape: attn_shape, q, lse, cu_seqlens, start, k_pool, page_
     w_stride = _weights_stride(w_out, k_pool)
     if w_in is not None and w_in is not w_out and _weights_stride(w_in, k_pool) != w_stride:
         raise GdnError(-3, "attn_key_weights: w_in and w_out of one geometry")
-    _check(_lib().attn_key_weights(ctypes.byref(shape), _dp(q), _dp(lse), len(start), _ip(cu_seqlens), _ip(start), _pages(shape, k_pool), _dp(k_pool),
-                                   _ip(page_cu), _ip(page_ids), float(decay), _dp(w_in), _dp(w_out), w_stride, *_ws(workspace),
-                                   _stream_ptr(stream)), "attn_key_weights")
+    n = len(start)
+    cu, (start,), (page_cu, page_ids) = _offsets(n, cu_seqlens), _per_request(n, start), _offsets(n, page_cu, page_ids)
+    _check(_lib().attn_key_weights(ctypes.byref(shape), _dp(q), _dp(lse), n, cu, start, _pages(shape, k_pool), _dp(k_pool), page_cu, page_ids, float(decay),
+                                   _dp(w_in), _dp(w_out), w_stride, *_ws(workspace), _stream_ptr(stream)), "attn_key_weights")
 
 
 def attn_evict(shape: attn_shape, rows, keep, first, recent, k_pool, v_pool, w_pool, page_cu, page_ids, new_page_cu, new_page_ids, index,
                workspace, stream=None) -> None:
     """See include/attn_paged.h.  index: int32, H_kv entries per kept row."""
     _packed(index)
-    _check(_lib().attn_evict(ctypes.byref(shape), len(rows), _ip(rows), _ip(keep), _ip(first), _ip(recent), _pages(shape, k_pool, v_pool), _dp(k_pool),
-                             _dp(v_pool), _dp(w_pool), _weights_stride(w_pool, k_pool), _ip(page_cu), _ip(page_ids), _ip(new_page_cu), _ip(new_page_ids),
-                             _dp(index), *_ws(workspace), _stream_ptr(stream)), "attn_evict")
+    n = len(rows)
+    counts, (page_cu, page_ids), (new_page_cu, new_page_ids) = (_per_request(n, rows, keep, first, recent), _offsets(n, page_cu, page_ids),
+                                                                _offsets(n, new_page_cu, new_page_ids))
+    _check(_lib().attn_evict(ctypes.byref(shape), n, *counts, _pages(shape, k_pool, v_pool), _dp(k_pool), _dp(v_pool), _dp(w_pool),
+                             _weights_stride(w_pool, k_pool), page_cu, page_ids, new_page_cu, new_page_ids, _dp(index), *_ws(workspace),
+                             _stream_ptr(stream)), "attn_evict")

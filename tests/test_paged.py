@@ -1149,3 +1149,27 @@ def test_values_that_are_not_finite_cost_no_more_than_a_few_walks(H_q, H_kv, d, 
     bad = best()
     assert not bool(torch.isfinite(o[:, :, 3].float()).any()) and bool(torch.isfinite(o[:, :, :3].float()).all())
     assert bad <= (1.5 if kind == "cached" else 40) * clean, (clean, bad)
+
+
+@pytest.mark.parametrize("over", [dict(cu_seqlens=[0, 5]), dict(cu_seqlens=[0, 5, 9, 9]), dict(page_cu=[0, 1]), dict(page_cu=[0, 1, 3, 3]), dict(page_ids=[7, 3]),
+                                  dict(page_ids=[])])
+def test_index_arrays_shorter_than_the_call_reads_are_refused(no_stream, over):
+    a = dict(CALL, **over)
+    arrays = a["k_pool"], a["page_cu"], a["page_ids"]
+    rope, kv, lse = PG.make_attn_rope(np.ones(32)), FakePool(0x20000, (9, 2, 64)), FakePool(0x30000)
+    for pos in (None, [0, 100], [0], [0, 1, 2]):
+        with pytest.raises(ValueError):
+            PG.attn_rope_append(a["shape"], rope, X, kv, kv, a["cu_seqlens"], pos, a["start"], a["k_pool"], *arrays, X, WS)
+    with pytest.raises(ValueError):
+        PG.attn_rope_append(CALL["shape"], rope, X, kv, kv, CALL["cu_seqlens"], [0], CALL["start"], K_POOL, V_POOL, CALL["page_cu"], CALL["page_ids"], X, WS)
+    with pytest.raises(ValueError):
+        PG.attn_paged_prefill(a["shape"], X, None, a["cu_seqlens"], a["start"], a["k_pool"], *arrays, X, None, WS)
+    with pytest.raises(ValueError):
+        PG.attn_key_weights(a["shape"], X, lse, a["cu_seqlens"], a["start"], *arrays, 1.0, None, W_POOL, WS)
+    evict = dict(rows=[5, 24], keep=[4, 10], first=[2, 2], recent=[2, 3], page_cu=[0, 1, 3], page_ids=[7, 3, 39], new_page_cu=[0, 1, 2], new_page_ids=[1, 2])
+    for over in (dict(rows=[5]), dict(keep=[4]), dict(first=[2, 2, 2]), dict(recent=[]), dict(page_cu=[0, 1]), dict(page_ids=[7, 3]), dict(new_page_cu=[0, 1]),
+                 dict(new_page_ids=[1])):
+        e = dict(evict, **over)
+        with pytest.raises(ValueError):
+            PG.attn_evict(CALL["shape"], e["rows"], e["keep"], e["first"], e["recent"], K_POOL, V_POOL, W_POOL, e["page_cu"], e["page_ids"], e["new_page_cu"],
+                          e["new_page_ids"], FakePool(), WS)
