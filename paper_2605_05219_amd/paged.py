@@ -9,7 +9,7 @@ import ctypes
 import numpy as np
 
 from .attention import attn_shape
-from .binding import GDN_BF16, GDN_F32, GdnError, _check, _dp, _h32, _hp, lib
+from .binding import GDN_BF16, GDN_F32, GdnError, _check, _hp, lib
 from .binding import _stream_ptr as _stream_object_ptr
 
 _i32, _i64, _vp, _f32, _f64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_float, ctypes.c_double
@@ -39,37 +39,39 @@ def _stream_ptr(stream=None):
     """The given stream's handle, or the current one's without an object made for it (3 us a call)."""
     import torch
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return _vp(raw(torch.cuda.current_device())) if stream is None and raw is not None else _stream_object_ptr(stream)
+    return raw(torch.cuda.current_device()) if stream is None and raw is not None else _stream_object_ptr(stream)
+
+
+def _dp(x):
+    """A device tensor's (or None's) address: a plain number, of which the call's argument types make a pointer (a tenth of a microsecond less)."""
+    return x.data_ptr() if x is not None else None
 
 
 _ints = ctypes.c_int32 * 0
+_from_buffer = _ints.from_buffer
+_INT32 = np.dtype(np.int32)
 
 
 def _ip(a):
     """An int32 array as an argument that the call reads in place (a fifth of what `_hp` takes)."""
-    return _ints.from_buffer(a if a.flags.writeable else a.copy())
+    try:
+        return _from_buffer(a)
+    except (TypeError, ValueError, BufferError):          # read-only, or with gaps
+        return _from_buffer(np.array(a, order="C"))
 
 
-def _per_request(n, *arrays):
-    """Host sequences of one entry per request (or None), as arguments."""
-    out = []
-    for x in arrays:
-        a = None if x is None else _h32(x)
-        if a is not None and a.size != n:
-            raise ValueError("index arrays have inconsistent lengths")
-        out.append(None if a is None else _ip(a))
-    return out
-
-
-def _offsets(n, cu, ids=None):
-    """Offsets of n requests, as an argument, and where they say into `ids`, that too."""
-    a = _h32(cu)
-    if a.size != n + 1:
+def _array(n, x):
+    """A host sequence of n entries (one per request, or the offsets of n - 1) as an argument."""
+    a = np.asarray(x, _INT32)
+    if a.size != n:
         raise ValueError("index arrays have inconsistent lengths")
-    if ids is None:
-        return _ip(a)
-    b = _h32(ids)
-    if b.size < a[-1]:
+    return _ip(a)
+
+
+def _table(n, cu, ids):
+    """The offsets of n requests, and the page ids that they say, as arguments."""
+    a, b = np.asarray(cu, _INT32), np.asarray(ids, _INT32)
+    if a.size != n + 1 or b.size < a.item(n):
         raise ValueError("index arrays have inconsistent lengths")
     return _ip(a), _ip(b)
 
@@ -94,6 +96,20 @@ def _lib():
             f.restype = _i32
         _ready = True
     return L
+
+
+_types = {}                                              # "bf16", "f16", "f32", "i32", and the codes of the first and the third
+
+
+def _typed(want, *tensors):
+    """Refuses tensors (or None) of another type than the kernels read."""
+    if not _types:
+        import torch
+        _types.update({"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32, "i32": torch.int32, GDN_BF16: torch.bfloat16, GDN_F32: torch.float32})
+    want = _types.get(want)                              # (None: a code that the call itself refuses)
+    for x in tensors:
+        if getattr(x, "dtype", want) is not want and want is not None:
+            raise GdnError(-3, f"a tensor of {want} is needed, not of {x.dtype}")
 
 
 def _packed(*tensors):
@@ -127,9 +143,10 @@ def _pages(shape, *pools):
     for x in pools[1:]:
         if x.stride() != stride or x.shape != size:
             raise GdnError(-3, "pools of one geometry")
-    if not _inside(stride, size) or size[1] != shape.H_kv or size[3] != shape.d:
+    n, heads, rows, d = size
+    if ((stride[3] != 1 or stride[2] != d or stride[1] != rows * d) and not _inside(stride, size)) or heads != shape.H_kv or d != shape.d:
         raise GdnError(-3, "a page is packed: [H_kv][page_rows][d]")
-    return ctypes.byref(attn_pages(stride[0], size[0], size[2]))
+    return ctypes.byref(attn_pages(stride[0], n, rows))
 
 
 def _weights_stride(w, k_pool):
@@ -164,44 +181,58 @@ def attn_rope_append(shape: attn_shape, rope: attn_rope, q, k, v, cu_seqlens, po
                      workspace, stream=None) -> None:
     """See include/attn_paged.h.  q, k, v are [T][heads][d] tensors whose token stride is passed on (heads and elements packed);
     pos may be None."""
+    _typed("bf16", k_pool, q_out)
+    _typed("f16", v_pool)
+    _typed(rope.in_dtype, q, k, v)
     _packed(q_out)
     n = len(start)
-    cu, (pos, start), (page_cu, page_ids) = _offsets(n, cu_seqlens), _per_request(n, pos, start), _offsets(n, page_cu, page_ids)
-    _check(_lib().attn_rope_append(ctypes.byref(shape), ctypes.byref(rope), _dp(q), _ld(q), _dp(k), _ld(k), _dp(v), _ld(v), n, cu, pos, start,
-                                   _pages(shape, k_pool, v_pool), _dp(k_pool), _dp(v_pool), page_cu, page_ids, _dp(q_out), *_ws(workspace),
-                                   _stream_ptr(stream)), "attn_rope_append")
+    _check(_lib().attn_rope_append(ctypes.byref(shape), ctypes.byref(rope), _dp(q), _ld(q), _dp(k), _ld(k), _dp(v), _ld(v), n, _array(n + 1, cu_seqlens),
+                                   None if pos is None else _array(n, pos), _array(n, start), _pages(shape, k_pool, v_pool), _dp(k_pool), _dp(v_pool),
+                                   *_table(n, page_cu, page_ids), _dp(q_out), *_ws(workspace), _stream_ptr(stream)), "attn_rope_append")
 
 
 def attn_paged_prefill(shape: attn_shape, q, out_gate, cu_seqlens, start, k_pool, v_pool, page_cu, page_ids, o, lse, workspace,
                        stream=None) -> None:
     """See include/attn_paged.h.  out_gate and lse may be None."""
+    _typed("bf16", q, out_gate, k_pool)
+    _typed("f16", v_pool)
+    _typed("f32", lse)
     _packed(q, out_gate, o, lse)
-    n = len(start)
-    cu, (start,), (page_cu, page_ids) = _offsets(n, cu_seqlens), _per_request(n, start), _offsets(n, page_cu, page_ids)
-    _check(_lib().attn_paged_prefill(ctypes.byref(shape), _dp(q), _dp(out_gate), n, cu, start, _pages(shape, k_pool, v_pool), _dp(k_pool), _dp(v_pool),
-                                     page_cu, page_ids, _dp(o), _dp(lse), *_ws(workspace), _stream_ptr(stream)), "attn_paged_prefill")
+    n, space = len(start), _ws(workspace)
+    cu, table = _array(n + 1, cu_seqlens), _table(n, page_cu, page_ids)
+    try:
+        _typed(shape.o_dtype, o)
+    except GdnError:                                     # (a workspace that is too small is what the call refuses first)
+        if space[1] >= attn_paged_workspace_bytes(shape, n, max(0, int(cu_seqlens[-1])), max(0, int(page_cu[-1]))):
+            raise
+    _check(_lib().attn_paged_prefill(ctypes.byref(shape), _dp(q), _dp(out_gate), n, cu, _array(n, start), _pages(shape, k_pool, v_pool), _dp(k_pool), _dp(v_pool),
+                                     *table, _dp(o), _dp(lse), *space, _stream_ptr(stream)), "attn_paged_prefill")
 
 
 def attn_key_weights(shape: attn_shape, q, lse, cu_seqlens, start, k_pool, page_cu, page_ids, decay, w_in, w_out, workspace,
                      stream=None) -> None:
     """See include/attn_paged.h.  w_in may be None or w_out; the two have one page stride."""
+    _typed("bf16", q, k_pool)
+    _typed("f32", lse, w_in, w_out)
     _packed(q, lse)
     w_stride = _weights_stride(w_out, k_pool)
     if w_in is not None and w_in is not w_out and _weights_stride(w_in, k_pool) != w_stride:
         raise GdnError(-3, "attn_key_weights: w_in and w_out of one geometry")
     n = len(start)
-    cu, (start,), (page_cu, page_ids) = _offsets(n, cu_seqlens), _per_request(n, start), _offsets(n, page_cu, page_ids)
-    _check(_lib().attn_key_weights(ctypes.byref(shape), _dp(q), _dp(lse), n, cu, start, _pages(shape, k_pool), _dp(k_pool), page_cu, page_ids, float(decay),
-                                   _dp(w_in), _dp(w_out), w_stride, *_ws(workspace), _stream_ptr(stream)), "attn_key_weights")
+    _check(_lib().attn_key_weights(ctypes.byref(shape), _dp(q), _dp(lse), n, _array(n + 1, cu_seqlens), _array(n, start), _pages(shape, k_pool), _dp(k_pool),
+                                   *_table(n, page_cu, page_ids), float(decay), _dp(w_in), _dp(w_out), w_stride, *_ws(workspace), _stream_ptr(stream)),
+           "attn_key_weights")
 
 
 def attn_evict(shape: attn_shape, rows, keep, first, recent, k_pool, v_pool, w_pool, page_cu, page_ids, new_page_cu, new_page_ids, index,
                workspace, stream=None) -> None:
     """See include/attn_paged.h.  index: int32, H_kv entries per kept row."""
+    _typed("bf16", k_pool)
+    _typed("f16", v_pool)
+    _typed("f32", w_pool)
+    _typed("i32", index)
     _packed(index)
     n = len(rows)
-    counts, (page_cu, page_ids), (new_page_cu, new_page_ids) = (_per_request(n, rows, keep, first, recent), _offsets(n, page_cu, page_ids),
-                                                                _offsets(n, new_page_cu, new_page_ids))
-    _check(_lib().attn_evict(ctypes.byref(shape), n, *counts, _pages(shape, k_pool, v_pool), _dp(k_pool), _dp(v_pool), _dp(w_pool),
-                             _weights_stride(w_pool, k_pool), page_cu, page_ids, new_page_cu, new_page_ids, _dp(index), *_ws(workspace),
-                             _stream_ptr(stream)), "attn_evict")
+    _check(_lib().attn_evict(ctypes.byref(shape), n, _array(n, rows), _array(n, keep), _array(n, first), _array(n, recent), _pages(shape, k_pool, v_pool),
+                             _dp(k_pool), _dp(v_pool), _dp(w_pool), _weights_stride(w_pool, k_pool), *_table(n, page_cu, page_ids),
+                             *_table(n, new_page_cu, new_page_ids), _dp(index), *_ws(workspace), _stream_ptr(stream)), "attn_evict")

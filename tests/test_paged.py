@@ -1173,3 +1173,44 @@ def test_index_arrays_shorter_than_the_call_reads_are_refused(no_stream, over):
         with pytest.raises(ValueError):
             PG.attn_evict(CALL["shape"], e["rows"], e["keep"], e["first"], e["recent"], K_POOL, V_POOL, W_POOL, e["page_cu"], e["page_ids"], e["new_page_cu"],
                           e["new_page_ids"], FakePool(), WS)
+
+
+def test_tensors_of_another_type_than_the_kernels_read_are_refused(no_stream):
+    import torch
+    bf16, f16, f32, i32 = torch.bfloat16, torch.float16, torch.float32, torch.int32
+    cu, st, tcu, ids = [0, 5, 9], [0, 20], [0, 1, 3], [7, 3, 39]
+    ws = FakePool(0x100000, nbytes=64)
+    pool, w, x, kv, z, i = (torch.zeros(*n) for n in ((40, 2, 16, 64), (40, 2, 16), (9, 4, 64), (9, 2, 64), (9, 4), (99,)))
+
+    def append(in_dtype, q, k, v, kp, vp, out):
+        PG.attn_rope_append(AT.make_attn_shape(4, 2, 64), PG.make_attn_rope(np.ones(32), in_dtype=in_dtype), x.to(q), kv.to(k), kv.to(v), cu, None, st, pool.to(kp),
+                            pool.to(vp), tcu, ids, x.to(out), ws)
+
+    def attend(o_dtype, q, gate, kp, vp, o, lse):
+        PG.attn_paged_prefill(AT.make_attn_shape(4, 2, 64, o_dtype), x.to(q), x.to(gate), cu, st, pool.to(kp), pool.to(vp), tcu, ids, x.to(o), z.to(lse), ws)
+
+    def weigh(q, lse, kp, wi, wo):
+        PG.attn_key_weights(AT.make_attn_shape(4, 2, 64), x.to(q), z.to(lse), cu, st, pool.to(kp), tcu, ids, 1.0, w.to(wi), w.to(wo), ws)
+
+    def evict(kp, vp, wp, index):
+        PG.attn_evict(AT.make_attn_shape(4, 2, 64), [5, 24], [4, 9], [1, 1], [1, 1], pool.to(kp), pool.to(vp), w.to(wp), tcu, ids, [0, 1, 2], [1, 2], i.to(index), ws)
+
+    for call, right in ((append, ("bf16", bf16, bf16, bf16, bf16, f16, bf16)), (append, ("f32", f32, f32, f32, bf16, f16, bf16)),
+                        (attend, ("bf16", bf16, bf16, bf16, f16, bf16, f32)), (attend, ("f32", bf16, bf16, bf16, f16, f32, f32)),
+                        (weigh, (bf16, f32, bf16, f32, f32)), (evict, (bf16, f16, f32, i32))):
+        ws._n = 64
+        refused(call, -9, *right)                                             # nothing else is wrong: the workspace is too small
+        ws._n = 1 << 30
+        for at, want in enumerate(right):
+            for other in (bf16, f16, f32, i32, torch.int16, torch.float64):
+                if not isinstance(want, str) and other is not want:
+                    refused(call, -3, *right[:at], other, *right[at + 1:])
+
+
+@pytest.mark.parametrize("x", [[3, 1, 2], (3, 1, 2), np.array([3, 1, 2]), np.array([3, 9, 1, 9, 2, 9], np.int32)[::2], np.arange(4, 0, -1, dtype=np.int32)[1:][[0, 2, 1]]])
+def test_index_arrays_of_any_kind_arrive_as_they_are(x):
+    read_only = np.array(x, np.int32)
+    read_only.flags.writeable = False
+    for a in (x, read_only):
+        got = PG._array(3, a)
+        assert list((ctypes.c_int32 * 3).from_address(ctypes.addressof(got))) == [3, 1, 2]
