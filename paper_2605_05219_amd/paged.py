@@ -61,11 +61,19 @@ def _ip(a):
 
 
 def _array(n, x):
-    """A host sequence of n entries (one per request, or the offsets of n - 1) as an argument."""
+    """A host sequence of n entries as an argument."""
     a = np.asarray(x, _INT32)
     if a.size != n:
         raise ValueError("index arrays have inconsistent lengths")
     return _ip(a)
+
+
+def _tokens(n, cu):
+    """The new tokens of n requests, and their offsets as an argument."""
+    a = np.asarray(cu, _INT32)
+    if a.size != n + 1:
+        raise ValueError("index arrays have inconsistent lengths")
+    return a.item(n), _ip(a)
 
 
 def _table(n, cu, ids):
@@ -74,6 +82,13 @@ def _table(n, cu, ids):
     if a.size != n + 1 or b.size < a.item(n):
         raise ValueError("index arrays have inconsistent lengths")
     return _ip(a), _ip(b)
+
+
+def _holds(count, *tensors):
+    """Refuses tensors (or None) of fewer elements than the call reads or writes."""
+    for x in tensors:
+        if x is not None and x.numel() < count:
+            raise GdnError(-3, f"{count} elements are needed, not {x.numel()}")
 
 
 _ready = False
@@ -186,7 +201,10 @@ def attn_rope_append(shape: attn_shape, rope: attn_rope, q, k, v, cu_seqlens, po
     _typed(rope.in_dtype, q, k, v)
     _packed(q_out)
     n = len(start)
-    _check(_lib().attn_rope_append(ctypes.byref(shape), ctypes.byref(rope), _dp(q), _ld(q), _dp(k), _ld(k), _dp(v), _ld(v), n, _array(n + 1, cu_seqlens),
+    tokens, cu = _tokens(n, cu_seqlens)
+    _holds(tokens * shape.d * shape.H_q, q, q_out)
+    _holds(tokens * shape.d * shape.H_kv, k, v)
+    _check(_lib().attn_rope_append(ctypes.byref(shape), ctypes.byref(rope), _dp(q), _ld(q), _dp(k), _ld(k), _dp(v), _ld(v), n, cu,
                                    None if pos is None else _array(n, pos), _array(n, start), _pages(shape, k_pool, v_pool), _dp(k_pool), _dp(v_pool),
                                    *_table(n, page_cu, page_ids), _dp(q_out), *_ws(workspace), _stream_ptr(stream)), "attn_rope_append")
 
@@ -199,11 +217,14 @@ def attn_paged_prefill(shape: attn_shape, q, out_gate, cu_seqlens, start, k_pool
     _typed("f32", lse)
     _packed(q, out_gate, o, lse)
     n, space = len(start), _ws(workspace)
-    cu, table = _array(n + 1, cu_seqlens), _table(n, page_cu, page_ids)
+    tokens, cu = _tokens(n, cu_seqlens)
+    table = _table(n, page_cu, page_ids)
+    _holds(tokens * shape.H_q * shape.d, q, out_gate, o)
+    _holds(tokens * shape.H_q, lse)
     try:
         _typed(shape.o_dtype, o)
     except GdnError:                                     # (a workspace that is too small is what the call refuses first)
-        if space[1] >= attn_paged_workspace_bytes(shape, n, max(0, int(cu_seqlens[-1])), max(0, int(page_cu[-1]))):
+        if space[1] >= attn_paged_workspace_bytes(shape, n, max(0, tokens), max(0, int(page_cu[-1]))):
             raise
     _check(_lib().attn_paged_prefill(ctypes.byref(shape), _dp(q), _dp(out_gate), n, cu, _array(n, start), _pages(shape, k_pool, v_pool), _dp(k_pool), _dp(v_pool),
                                      *table, _dp(o), _dp(lse), *space, _stream_ptr(stream)), "attn_paged_prefill")
@@ -219,7 +240,10 @@ def attn_key_weights(shape: attn_shape, q, lse, cu_seqlens, start, k_pool, page_
     if w_in is not None and w_in is not w_out and _weights_stride(w_in, k_pool) != w_stride:
         raise GdnError(-3, "attn_key_weights: w_in and w_out of one geometry")
     n = len(start)
-    _check(_lib().attn_key_weights(ctypes.byref(shape), _dp(q), _dp(lse), n, _array(n + 1, cu_seqlens), _array(n, start), _pages(shape, k_pool), _dp(k_pool),
+    tokens, cu = _tokens(n, cu_seqlens)
+    _holds(tokens * shape.H_q * shape.d, q)
+    _holds(tokens * shape.H_q, lse)
+    _check(_lib().attn_key_weights(ctypes.byref(shape), _dp(q), _dp(lse), n, cu, _array(n, start), _pages(shape, k_pool), _dp(k_pool),
                                    *_table(n, page_cu, page_ids), float(decay), _dp(w_in), _dp(w_out), w_stride, *_ws(workspace), _stream_ptr(stream)),
            "attn_key_weights")
 
@@ -232,7 +256,9 @@ def attn_evict(shape: attn_shape, rows, keep, first, recent, k_pool, v_pool, w_p
     _typed("f32", w_pool)
     _typed("i32", index)
     _packed(index)
-    n = len(rows)
+    n, rows, keep = len(rows), np.asarray(rows, _INT32), np.asarray(keep, _INT32)
+    if rows.size == keep.size:
+        _holds(int(np.minimum(rows, keep).sum(dtype=np.int64)) * shape.H_kv, index)
     _check(_lib().attn_evict(ctypes.byref(shape), n, _array(n, rows), _array(n, keep), _array(n, first), _array(n, recent), _pages(shape, k_pool, v_pool),
                              _dp(k_pool), _dp(v_pool), _dp(w_pool), _weights_stride(w_pool, k_pool), *_table(n, page_cu, page_ids),
                              *_table(n, new_page_cu, new_page_ids), _dp(index), *_ws(workspace), _stream_ptr(stream)), "attn_evict")

@@ -931,11 +931,11 @@ def test_rope_append_refuses_an_output_over_its_inputs(no_stream, over):
 def test_rope_append_refuses_too_many_heads_before_anything_is_enqueued(no_stream):
     """More pieces to a token than its kernel numbers, in a call whose plan is long enough for a launch of its own."""
     n, heads = 200, 1 << 26
-    q = FakePool(0x1000000, (n, heads, 64))
+    q = FakePool(0x1000000, (n, heads, 64), nbytes=1 << 50)
     kv = FakePool(0x10000, (n, 1, 64))
     pool = FakePool(0x200000, (n, 1, 16, 64))
     refused(PG.attn_rope_append, -3, AT.make_attn_shape(heads, 1, 64), PG.make_attn_rope(np.ones(32)), q, kv, kv, np.arange(n + 1), None, np.zeros(n, np.int32),
-            pool, pool, np.arange(n + 1), np.arange(n), FakePool(1 << 50, (n, heads, 64)), FakePool(0x100000, nbytes=1 << 45))
+            pool, pool, np.arange(n + 1), np.arange(n), FakePool(1 << 50, (n, heads, 64), nbytes=1 << 50), FakePool(0x100000, nbytes=1 << 45))
 
 
 @pytest.mark.gpu
@@ -1214,3 +1214,26 @@ def test_index_arrays_of_any_kind_arrive_as_they_are(x):
     for a in (x, read_only):
         got = PG._array(3, a)
         assert list((ctypes.c_int32 * 3).from_address(ctypes.addressof(got))) == [3, 1, 2]
+
+
+def test_tensors_shorter_than_the_call_are_refused(no_stream):
+    """Of each of a call's tensors one element or row less than it reads or writes."""
+    import torch
+    bf16 = torch.bfloat16
+    cu, st, tcu, ids = [0, 5, 9], [0, 20], [0, 1, 3], [7, 3, 39]
+    ws = FakePool(0x100000, nbytes=64)
+    k, v, w = torch.zeros(40, 2, 16, 64, dtype=bf16), torch.zeros(40, 2, 16, 64, dtype=torch.float16), torch.zeros(40, 2, 16)
+    x, kv, z, i = torch.zeros(9, 4, 64, dtype=bf16), torch.zeros(9, 2, 64, dtype=bf16), torch.zeros(9, 4), torch.zeros(26, dtype=torch.int32)
+    sh, rope = AT.make_attn_shape(4, 2, 64, "bf16"), PG.make_attn_rope(np.ones(32))
+    calls = [(lambda q, k_, v_, out: PG.attn_rope_append(sh, rope, q, k_, v_, cu, None, st, k, v, tcu, ids, out, ws), (x, kv, kv, x)),
+             (lambda q, gate, o, lse: PG.attn_paged_prefill(sh, q, gate, cu, st, k, v, tcu, ids, o, lse, ws), (x, x, x, z)),
+             (lambda q, lse: PG.attn_key_weights(sh, q, lse, cu, st, k, tcu, ids, 1.0, w, w, ws), (x, z)),
+             (lambda index: PG.attn_evict(sh, [5, 24], [4, 9], [1, 1], [1, 1], k, v, w, tcu, ids, [0, 1, 2], [1, 2], index, ws), (i,))]
+    for call, right in calls:
+        ws._n = 64
+        refused(call, -9, *right)                                             # nothing else is wrong: the workspace is too small
+        ws._n = 1 << 30
+        for at, t in enumerate(right):
+            refused(call, -3, *right[:at], t[:-1], *right[at + 1:])
+    refused(calls[3][0], -3, torch.zeros(0, dtype=torch.int32))
+    refused(lambda: PG.attn_evict(sh, [5, 24], [4, 90], [1, 1], [1, 1], k, v, w, tcu, ids, [0, 1, 3], [1, 2, 4], torch.zeros(55, dtype=torch.int32), ws), -3)
