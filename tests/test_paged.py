@@ -1237,3 +1237,96 @@ def test_tensors_shorter_than_the_call_are_refused(no_stream):
             refused(call, -3, *right[:at], t[:-1], *right[at + 1:])
     refused(calls[3][0], -3, torch.zeros(0, dtype=torch.int32))
     refused(lambda: PG.attn_evict(sh, [5, 24], [4, 90], [1, 1], [1, 1], k, v, w, tcu, ids, [0, 1, 3], [1, 2, 4], torch.zeros(55, dtype=torch.int32), ws), -3)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H_q,H_kv,d,P,lens,starts", [
+    (16, 2, 128, 64, [1, 1, 1], [3000, 1023, 1500]), (4, 4, 64, 16, [1], [9000]), (8, 1, 256, 128, [2, 1], [1100, 2047]), (32, 4, 64, 32, [2] * 9, [1024 + 211 * i for i in range(9)]),
+    (16, 2, 128, 64, [1] * 40, [1100 + 150 * i for i in range(40)]),          # few-rows walks, cut
+    (8, 8, 64, 64, [1] * 66, [1024 + 3 * i for i in range(66)]),              # ... and whole
+    (16, 2, 128, 64, [600] * 8, [500 + 30 * i for i in range(8)]),            # the 128-row kernel's in a call that fills the chip
+    (16, 4, 64, 32, [500, 700, 640, 1] * 4, [40, 900, 0, 1300] * 4),
+])
+def test_walks_that_both_forms_plan_alike_have_the_same_bits(H_q, H_kv, d, P, lens, starts):
+    """Walks cut and whole as the planner likes: requests of few rows behind 1024 and more, and calls that are not cut.  Where a walk has more than 16 parts the
+    forms merge them in different orders: the same values."""
+    import torch
+    R = len(lens)
+    c = Paged(210, H_q, H_kv, d, P, lens, starts)
+    v_new = [wl.f32_to_bf16_bits(v[s:].astype(np.float32)) for v, s in zip(c.v_rows, starts)]
+    cap = max(c.total)
+    kc, vc = np.zeros((R, cap, H_kv, d), np.uint16), np.zeros((R, cap, H_kv, d), np.float16)
+    for r in range(R):
+        c.v_rows[r][starts[r]:] = wl.to_f32(v_new[r]).astype(np.float16)
+        kc[r, :starts[r]], vc[r, :starts[r]] = c.k_rows[r][:starts[r]], c.v_rows[r][:starts[r]]
+    c.fill()
+    q = c.bf16(c.T, H_q, d)
+    o, _ = run_attend(c, q, None, "f32", lse=False)
+    sh = AT.make_attn_shape(H_q, H_kv, d, "f32")
+    os_ = torch.zeros_like(o)
+    ws = torch.empty(AT.attn_workspace_bytes(sh, R, c.T), dtype=torch.uint8, device="cuda")
+    AT.attn_suffix_prefill(sh, c.dev(q), c.dev(np.concatenate([k[s:] for k, s in zip(c.k_rows, starts)])), c.dev(np.concatenate(v_new)), None, c.cu, starts,
+                           c.dev(kc), torch.from_numpy(vc).cuda(), list(range(R)), os_, ws)
+    units, _, _ = AT.attn_plan(sh, c.cu, starts)
+    if np.unique(units[:, :2], axis=0, return_counts=True)[1].max() <= 16:
+        assert torch.equal(o, os_)
+    else:
+        check_attend(c, q, None, "f32", o, None)
+        check_attend(c, q, None, "f32", os_, None)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H_q,H_kv,d,P,R,n,lo,hi,whole", [
+    (16, 8, 64, 64, 100, 1, 1024, 1300, True), (16, 8, 64, 32, 70, 2, 1023, 1200, True), (8, 8, 128, 16, 96, 1, 1030, 1400, True),
+    (16, 2, 256, 128, 260, 1, 1024, 1100, True), (16, 8, 256, 64, 66, 4, 1030, 1100, True), (32, 4, 128, 64, 130, 2, 1024, 1300, True),
+    (16, 2, 128, 64, 16, 1, 9000, 10000, False),                              # as many bytes, walks cut
+])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_large_batches_of_few_rows_whose_walks_stay_whole(H_q, H_kv, d, P, R, n, lo, hi, whole, dtype):
+    """More requests and heads than workgroups to cut them into, and more bytes than the last cache keeps, gated and with log-sum-exps.  Where a request has
+    several tokens, the last brings an infinity and a NaN, which the rows before it do not see."""
+    import torch
+    gen, rng = torch.Generator(device="cuda").manual_seed(3), np.random.default_rng(4)
+    normal = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    starts = rng.integers(lo, hi, R)
+    pages = -(-(starts + n) // P)
+    tcu = np.concatenate([[0], np.cumsum(pages)])
+    ids = rng.permutation(int(tcu[-1])).astype(np.int32)
+    k, v = normal(ids.size, H_kv, P, d).bfloat16(), normal(ids.size, H_kv, P, d).half()
+    q, gate = normal(R * n, H_q, d).bfloat16(), normal(R * n, H_q, d).bfloat16()
+    cu = np.arange(R + 1) * n
+    places = []
+    for r in range(R):
+        j = np.arange(starts[r] + n)
+        places.append((torch.from_numpy(ids[tcu[r] + j // P].astype(np.int64)).cuda(), torch.from_numpy(j % P).cuda()))
+        if n > 1:
+            v[places[r][0][-1], :, places[r][1][-1], 5] = float("inf")
+            v[places[r][0][-1], :, places[r][1][-1], d - 1] = float("nan")
+    sh = AT.make_attn_shape(H_q, H_kv, d, dtype)
+    units, _, _ = AT.attn_plan(sh, cu, starts)
+    assert (units[:, 4] == -1).all() == whole and int((starts + n).sum()) * H_kv * d * 4 > 1 << 27
+    o, z = torch.full((R * n, H_q, d), float("nan"), dtype=torch.float32 if dtype == "f32" else torch.bfloat16, device="cuda"), torch.full((R * n, H_q), float("nan"), device="cuda")
+    ws = torch.full((PG.attn_paged_workspace_bytes(sh, R, R * n, ids.size),), 0xA5, dtype=torch.uint8, device="cuda")
+    PG.attn_paged_prefill(sh, q, gate, cu, starts, k, v, tcu, ids, o, z, ws)
+    o2 = torch.zeros_like(o)
+    PG.attn_paged_prefill(sh, q, gate, cu, starts, k, v, tcu, ids, o2, None, ws)
+    assert torch.equal(o.view(torch.int16), o2.view(torch.int16))
+    G, step = 2.0 ** -8, 2.0 ** -8 if dtype == "bf16" else 0.0
+    for r in range(R):
+        page, row = places[r]
+        kr, vr = k[page, :, row].double(), v[page, :, row].double()           # [rows][H_kv][d]
+        for t in range(n):
+            seen = starts[r] + t + 1
+            qt = q[r * n + t].double().view(H_kv, -1, d)
+            x = torch.stack([qt[g] @ kr[:seen, g].T.contiguous() for g in range(H_kv)]) * d ** -0.5
+            zr = torch.logsumexp(x, -1)
+            p = (x - zr[..., None]).exp()
+            ref = torch.stack([p[g] @ vr[:seen, g] for g in range(H_kv)]).view(H_q, d) * torch.sigmoid(gate[r * n + t].double())
+            got, zt = o[r * n + t].double(), z[r * n + t].double()
+            le = (d + 16) * 2.0 ** -24 * d ** -0.5 * float(kr[:seen].norm(dim=-1).max() * qt.norm(dim=-1).max())
+            assert bool(((zt - zr.view(-1)).abs() <= le + 2.0 ** -20 * (1 + zr.view(-1).abs())).all()), (r, t)
+            if t == n - 1 and n > 1:
+                assert bool((got[:, 5] == float("inf")).all()) and bool(got[:, d - 1].isnan().all())
+                got[:, [5, d - 1]] = ref[:, [5, d - 1]] = 0.0
+            top = float(vr[:seen].nan_to_num(0.0, 0.0, 0.0).abs().max())
+            assert bool(((got - ref).abs() <= G * top + step * ref.abs()).all()), (r, t, float((got - ref).abs().max()))
