@@ -588,7 +588,8 @@ __device__ __forceinline__ int wave_sum_upto(int x) {
 // which the smallest rank kept lies leaves few rows as a rule, one to a thread from there on; the next 11 bits are counted until one row or all bits are
 // left.  The counts of every 64 rows, summed, then say where each one's rows go.
 // Bound: latencies, and the instructions of one compute unit per head (four copies of the counters, because neighbouring weights share their
-// highest bits).  8200 rows 15.7 us, 30000 rows 30 (four rounds of 8 bits over memory 24 and 91).
+// highest bits).  8200 rows 15.7 us, 30000 rows 30 (four rounds of 8 bits over memory 24 and 91).  Behind 32768 rows each pass reads again what is not
+// held: a call that keeps 2000 rows of two heads takes 33 us from 32768, 41 from 40000, 101 from 100000 and 188 from 200000.
 constexpr int SEL_THREADS = 1024;
 constexpr int SEL_OWN = 8;             // rows of a thread in a block
 constexpr int SEL_HELD = 4;

@@ -1330,3 +1330,46 @@ def test_large_batches_of_few_rows_whose_walks_stay_whole(H_q, H_kv, d, P, R, n,
                 got[:, [5, d - 1]] = ref[:, [5, d - 1]] = 0.0
             top = float(vr[:seen].nan_to_num(0.0, 0.0, 0.0).abs().max())
             assert bool(((got - ref).abs() <= G * top + step * ref.abs()).all()), (r, t, float((got - ref).abs().max()))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H_kv,P,rows,keep,first,recent,kind", [
+    (2, 16, [32768, 32769], [3000, 3000], [4, 0], [64, 64], "normal"), (1, 64, [40961, 100], [40000, 7], [0, 1], [0, 1], "ties"),
+    (1, 256, [200003], [1000], [4], [100], "normal"), (2, 128, [70000], [33000], [33], [64], "equal"), (1, 32, [90001], [45000], [8], [8], "tail"),
+    (1, 32, [90001], [89000], [40000], [33000], "ties"),
+])
+def test_evict_from_more_rows_than_registers_hold(H_kv, P, rows, keep, first, recent, kind):
+    """Requests of more than 32768 rows, whose later ranks are read again."""
+    import torch
+    d = 64
+    new_n = [-(-m // P) for m in keep]
+    c = Paged(33, H_kv, H_kv, d, P, [0] * len(rows), rows, extra=sum(new_n)).fill()
+    w_np = np.full(c.k_np.shape[:1] + (H_kv, P), np.nan, np.float32)
+    w_rows = []
+    for r, n in enumerate(rows):
+        w = c.rng.standard_normal((n, H_kv)).astype(np.float32)
+        if kind == "ties":
+            w = np.round(2 * w)
+        if kind == "equal":
+            w[:] = -1.5
+        if kind == "tail":                              # what is kept lies behind the rows held
+            w[:50000] -= 100.0
+            w[60000::3] = np.nan
+        w_rows.append(w)
+        page, row = c.place(r, n)
+        w_np[page, :, row] = w
+    spare = list(c.spare)
+    new_table = [np.array([spare.pop() for _ in range(m)], np.int32) for m in new_n]
+    w_pool = torch.from_numpy(w_np).cuda()
+    index = torch.full((sum(keep) * H_kv,), -7, dtype=torch.int32, device="cuda")
+    PG.attn_evict(c.shape, rows, keep, first, recent, c.k_pool, c.v_pool, w_pool, c.page_cu, c.page_ids, np.concatenate([[0], np.cumsum(new_n)]),
+                  np.concatenate(new_table), index, c.workspace(0, c.page_ids.size + sum(new_n)))
+    idx, k_got, v_got, w_got, at = index.cpu().numpy(), bits_of(c.k_pool), bits_of(c.v_pool), w_pool.cpu().numpy(), 0
+    for r in range(len(rows)):
+        page, row = c.place(r, keep[r], new_table[r])
+        for g in range(H_kv):
+            want = po.rows_kept(w_rows[r][:, g], keep[r], first[r], recent[r])
+            assert np.array_equal(idx[at:at + keep[r]], want), (r, g)
+            at += keep[r]
+            assert np.array_equal(k_got[page, g, row], c.k_rows[r][want, g]) and np.array_equal(v_got[page, g, row], c.v_rows[r][want, g].view(np.uint16))
+            assert np.array_equal(w_got[page, g, row].view(np.uint32), w_rows[r][want, g].view(np.uint32))
