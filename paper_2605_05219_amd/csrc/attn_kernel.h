@@ -40,7 +40,8 @@
 // one of the wave's next 64 tiles, a tile takes its page by a lane read and makes its buffer descriptor of it: one vector load of page ids for every 64
 // tiles, no wait on a dependent load in between.  The descriptor ends with the request's last row in the page, so that rows behind it (which
 // another request may have left, whatever they hold) come as zeros.  64 one-token requests behind 4 to 10 thousand rows in pages of 64: 76 us, 6.0 TB/s;
-// 8192 tokens of 16 heads 286 us a call, 960 TFLOP/s, as in slots.
+// 8192 tokens of 16 heads 285 to 300 us a call by card, back to back, 965 to 915 TFLOP/s, as in slots (the kernel alone, each launch waited for by a profiler, 309
+// to 328).
 //
 // LDS rows are unpadded (a load to LDS writes a wave's 64 x 16 bytes contiguously); bank
 // conflicts are avoided by storing 16-byte chunk c of row r at chunk position c ^ f(r), with f

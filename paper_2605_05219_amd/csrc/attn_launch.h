@@ -49,7 +49,8 @@ constexpr int SPLIT_MAX_WGS = 768;
 // part takes as long as its key tiles, the merge as long as 4 to 8 of them (32 to 128 workgroups) and 0.4 for each part of 128 rows.  (The slot form does not: there a row's bits do not
 // depend on the call around it below 1024 keys.)  Of 120 drawn calls of fewer than 400 workgroups without the cut 27 change by 3 % or more, one of them for the worse: one
 // token of 4 requests behind 469 to 938 rows, 6 heads on 2, d = 256, 35.2 -> 15.9 us; 7 to 14 tokens of two behind 499 to 998, 8 heads, d = 128, 23.0 -> 15.4; one of 4
-// behind 515 to 1030, d = 64, 19.5 -> 14.7; one to 4 tokens of three behind 294 to 588, 16 heads on 4, 16.1 -> 17.6.
+// behind 515 to 1030, d = 64, 19.5 -> 14.7; one to 4 tokens of three behind 294 to 588, 16 heads on 4, 16.1 -> 17.6.  (profiles/paged_kernels_kernel_trace.txt has
+// calls of the first three kinds in both forms.)
 inline int fine_keys(int d) { return d == 256 ? 128 : 256; }
 // The few-rows kernel's walks are cut into at most NARROW_WGS workgroups in all: two per compute unit, one round, at d = 64 and
 // 128 (64 one-token requests behind 4 to 10 thousand keys, d = 128: at most 256 / 384 / 512 / 640 / 768 / 1024 workgroups 104 / 109 /

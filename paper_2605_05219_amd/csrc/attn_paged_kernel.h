@@ -215,7 +215,7 @@ __global__ void __launch_bounds__(ROPE_THREADS) attn_rope_kernel(RopeArgs a, Pla
 // exchange between lanes but one with the other half at the end, and no atomics.  A row's log-sum-exp comes by LDS in units of log2.
 // Bound: matrix and vector units alike (8192 tokens of 16 heads, d = 128: 55 us of products and 70 us of multiply-adds, exponentials and
 // sums at 2.4 GHz), so a wave computes the products of the next 32 rows in between the exponentials of the last (in turn they took 40 % more).  The call takes
-// 157 us (875 TFLOP/s): matrix units busy 0.40, vector units 0.50 of 341 k clocks at a power-limited 2.1 GHz, two waves to a SIMD (registers); a unit's
+// 157 to 163 us by card (875 TFLOP/s): matrix units busy 0.40, vector units 0.50 of 341 k clocks at a power-limited 2.1 GHz, two waves to a SIMD (registers); a unit's
 // start (4 us, three rounds) and the last round cost 25 of them.  500 tokens behind 7700 rows, d = 64: 24 us.
 constexpr int WGT_THREADS = 256;      // of the few-rows kernel
 __host__ __device__ constexpr int wgt_waves(int d) { return d == 64 ? 8 : 4; }
