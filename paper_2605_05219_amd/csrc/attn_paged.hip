@@ -215,14 +215,14 @@ class Plan {
         const size_t bytes = (size_t)ints * sizeof(int32_t);
         if (s.bytes < bytes) {            // (a buffer outgrown is not freed, which would wait for the device: the next one is more than twice as long)
             FetchRing::Slot fresh;
-            fresh.taken = true;
             fresh.bytes = (std::max<size_t>(2 * bytes, 1 << 17) + FETCH_PIECE - 1) / FETCH_PIECE * FETCH_PIECE;
             void* p = nullptr;
             const hipError_t e = hipHostMalloc(&p, fresh.bytes + fresh.words_bytes(), hipHostMallocCoherent | hipHostMallocPortable);
             if (e != hipSuccess) return hip_err(e);
-            fresh.host = static_cast<char*>(p);
             std::memset(p, 0, fresh.words_bytes());
-            s = fresh;
+            s.host = static_cast<char*>(p);      // (`taken` is the lock's)
+            s.bytes = fresh.bytes;
+            s.mark = s.blocks = 0;
         }
         data_ = reinterpret_cast<int32_t*>(s.host + s.words_bytes());
         return GDN_OK;

@@ -73,3 +73,19 @@ def test_an_eviction_to_few_rows_keeps_of_the_first_and_the_last_what_there_is_r
     assert list(call[2]) == [keep] * 2 and list(call[3]) == [want[0]] * 2 and list(call[4]) == [want[1]] * 2
     assert list(layer.rows) == [keep] * 2
     whole(layer, 80)
+
+
+def test_a_step_that_fails_loses_no_page_and_no_row(made, monkeypatch):
+    import torch
+    layer = made([15, 31], 6)                   # 3 pages held, 3 free
+
+    def refuse(*args):
+        raise B.GdnError(-3, "refused")
+    monkeypatch.setattr(PG, "attn_rope_append", refuse)
+    q, k = torch.zeros(80, 4, 64), torch.zeros(80, 2, 64)
+    with pytest.raises(RuntimeError, match="out of pages"):
+        layer.step(q, k, k, [30, 50])
+    with pytest.raises(B.GdnError):
+        layer.step(q[:4], k[:4], k[:4], [2, 2])
+    assert list(layer.rows) == list(layer.pos) == [15, 31]
+    whole(layer, 6)
