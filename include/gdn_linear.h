@@ -74,6 +74,48 @@ int32_t gdn_linear_plan(int64_t T, int32_t N, int32_t K, int32_t *shape, int32_t
  */
 int32_t gdn_linear_tune(int32_t shape);
 
+/*
+ * The map with an epilogue: activation, a second product as the gate's counterpart, a factor and a residual, as the two products of a
+ * feed-forward block want them,
+ *
+ *     z[t][n] = bias[n] + sum_k x[t][k] w[n][k]
+ *     a       = act(z)                                                     without w_up
+ *     a       = act(z) * (bias_up[n] + sum_k x[t][k] w_up[n][k])           with it (w is the gate's weight)
+ *     y[t][n] = scale * a + residual[t][n]
+ *
+ *   w_up      device, bf16, N rows of K at ldw_up elements, or NULL;  bias_up: device, fp32, N, or NULL (also without w_up)
+ *   residual  device, res_dtype, T rows of N elements at ldr elements (alignment as y of that type), or NULL; it may be y itself (the
+ *             same address, ldr = ldy, res_dtype = out_dtype).  Otherwise y shares no byte with x, w, w_up, a bias or the residual
+ * Everything else as gdn_linear.  Arithmetic: fp32 sums of the bf16 products; act, factor and residual in fp32; one rounding to out_dtype.
+ * For at most 64 rows the sum over k may be taken in eight parts that are added in order (which parts: by T, N and K alone), else it is
+ * gdn_linear's.  Errors as gdn_linear, and GDN_ERR_NULL without an epilogue, GDN_ERR_SHAPE for an unknown activation or res_dtype, a bias_up
+ * without w_up, ldr < N or ldw_up < K, GDN_ERR_SLOT_HAZARD where y shares bytes as said.
+ */
+enum { GDN_ACT_NONE = 0, GDN_ACT_SILU = 1, GDN_ACT_GELU = 2, GDN_ACT_GELU_TANH = 3, GDN_ACT_RELU = 4, GDN_ACT_RELU2 = 5, GDN_ACT_SIGMOID = 6 };
+
+typedef struct gdn_linear_epilogue {
+    int32_t act;               /* GDN_ACT_*; GELU by the error function or by tanh; RELU2: the square of RELU */
+    int32_t res_dtype;         /* GDN_BF16 or GDN_F32 (of a residual that is there) */
+    float scale;
+    const void *w_up;
+    int64_t ldw_up;
+    const float *bias_up;
+    const void *residual;
+    int64_t ldr;
+} gdn_linear_epilogue;
+
+int32_t gdn_linear_act(const void *x, int64_t ldx, const void *w, int64_t ldw, const float *bias,
+                       const gdn_linear_epilogue *epilogue, void *y, int64_t ldy, int32_t out_dtype,
+                       int64_t T, int32_t N, int32_t K, void *stream);
+
+/* gdn_linear_plan of gdn_linear_act; gated: 1 with a w_up.  Shape 6: the kernel of few rows, for T <= 64. */
+int32_t gdn_linear_act_plan(int64_t T, int32_t N, int32_t K, int32_t gated, int32_t *shape, int32_t *cols, int32_t *rest_shape);
+
+/*
+ * gdn_linear_tune of gdn_linear_act: 0 .. 5 (1 is 2, and with a w_up 5 is 0), 6: the kernel of few rows where T <= 64, anything else: chosen per call.
+ */
+int32_t gdn_linear_act_tune(int32_t shape);
+
 #ifdef __cplusplus
 }
 #endif

@@ -33,7 +33,10 @@
 #include <cmath>
 #include <cstdint>
 
+#include "gdn_act.h"
+#include "gdn_few_kernel.h"
 #include "gdn_linear.h"
+#include "gdn_rows.h"
 
 namespace gdn {
 namespace linear {
@@ -62,6 +65,21 @@ struct LinearArgs {
     void* seg_y[LIN_MAX_SEG];
     int64_t seg_ld[LIN_MAX_SEG];
 };
+
+// gdn_linear_act: what its epilogue does beside the bias
+struct LinearActArgs : LinearArgs {
+    const void* w_up;                   // null: one product
+    const float* bias_up;
+    const void* residual;
+    int64_t ldw_up, ldr;
+    int32_t act, res_f32;
+    float scale;
+};
+// What a kernel makes of its sums: the bias added; with an activation, a factor and a residual; the same of two products, in the tiles of
+// 16 outputs in turn (a wave's output tile 2 p holds 16 outputs of the gate, 2 p + 1 the same of w_up: one lane has both).
+enum { EPI_BIAS = 0, EPI_ACT = 1, EPI_GATED = 2 };
+template <int EPI> struct EpiArgs { typedef LinearActArgs type; };
+template <> struct EpiArgs<EPI_BIAS> { typedef LinearArgs type; };
 
 inline int32_t hip_err(hipError_t e) { return e == hipSuccess ? GDN_OK : GDN_ERR_HIP - (int32_t)e; }
 
@@ -112,16 +130,104 @@ struct LinLoad {
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (__attribute__((address_space(3))) void*)(ws + ((CFG::BN / CFG::NW) * wave + CFG::ROWS_PER_LOAD * (j - CFG::XL)) * CFG::RB), 16, woff[j - CFG::XL], k0 * 2, 0, 0);
         }
     }
-    static __device__ __forceinline__ void all(char* smem, int stage, int k0, int wave, const char* xb, int x_bytes, const char* wb, int w_bytes,
-                                               const int* xoff, const int* woff) {
-#pragma unroll
-        for (int j = 0; j < CFG::LPS; ++j) one(j, smem, stage, k0, wave, xb, x_bytes, wb, w_bytes, xoff, woff);
-    }
 };
 
-template <typename CFG, bool OUT_BF16>
+// Which of the two weights the wave's load j belongs to, where tiles of 16 rows take turns (a load's rows lie in one of them).
+template <typename CFG>
+__device__ __forceinline__ bool up_load(int j, int wave) {
+    return (((CFG::BN / CFG::NW) * wave + CFG::ROWS_PER_LOAD * j) >> 4) & 1;
+}
+
+// One bias, activation, factor and residual on a wave's outputs, and out through LDS in fp32 (one rounding, behind the residual): as
+// the epilogue below, a row of at most 64 outputs to a pass.
+template <typename CFG, bool OUT_BF16, int EPI>
+__device__ __forceinline__ void act_epilogue(const LinearActArgs& a, f32x4 (&acc)[CFG::TJ][CFG::TI], char* reg, int64_t tok0, int col0, int lane) {
+    constexpr int PAIR = EPI == EPI_GATED ? 2 : 1;                 // accumulator tiles to a tile of outputs
+    constexpr int WN = CFG::WN / PAIR, WM = CFG::WM;
+    constexpr int REGION = CFG::SMEM / CFG::NW;
+    constexpr int PW = WN <= 64 ? WN : 16;                         // outputs per pass (shape 5's 80 go 16 at a time)
+    constexpr int RBY = PW * 4 <= 64 ? 64 : PW * 4 <= 128 ? 128 : 256, PPR = RBY / 16;
+    constexpr int TP = WM * RBY <= REGION ? WM : REGION / RBY >= 64 ? 64 : REGION / RBY >= 32 ? 32 : 16;
+    constexpr int OPL = OUT_BF16 ? 8 : 4;                          // outputs of a lane's store
+    constexpr int LPR = PW / OPL, RPI = 64 / LPR;                  // lanes per row, rows a wave-wide store covers
+    static_assert(TP * RBY <= REGION && TP % RPI == 0 && WM % TP == 0 && WN % PW == 0 && PW % 16 == 0 && CFG::TJ % PAIR == 0, "epilogue region");
+    const int lr = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int c0 = 0; c0 < WN; c0 += PW) {
+#pragma unroll
+        for (int t0 = 0; t0 < WM; t0 += TP) {
+#pragma unroll
+            for (int tj = c0 / 16; tj < (c0 + PW) / 16; ++tj) {
+                const int cl = 16 * tj + 4 * g;
+                f32x4 bv = {0.f, 0.f, 0.f, 0.f}, bu = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (col0 + cl + e < a.N) {
+                        if (a.bias) bv[e] = a.bias[col0 + cl + e];
+                        if (EPI == EPI_GATED && a.bias_up) bu[e] = a.bias_up[col0 + cl + e];
+                    }
+#pragma unroll
+                for (int ti = t0 / 16; ti < (t0 + TP) / 16; ++ti) {
+                    const int row = 16 * ti + lr - t0;
+                    f32x4 v = activate(a.act, acc[PAIR * tj][ti] + bv);
+                    if (EPI == EPI_GATED) v *= acc[PAIR * tj + PAIR - 1][ti] + bu;
+                    const int piece = (cl - c0) / 4;
+                    *reinterpret_cast<f32x4*>(reg + row * RBY + ((piece ^ (row % PPR)) << 4)) = v;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < TP / RPI; ++i) {
+                const int row = RPI * i + lane / LPR, first = lane % LPR * OPL;
+                f32x4 v[OPL / 4];
+#pragma unroll
+                for (int h = 0; h < OPL / 4; ++h)
+                    v[h] = a.scale * *reinterpret_cast<const f32x4*>(reg + row * RBY + (((first / 4 + h) ^ (row % PPR)) << 4));
+                const int64_t tok = tok0 + t0 + row;
+                const int col = col0 + c0 + first;
+                if (tok >= a.T || col >= a.N) continue;
+                const bool whole = col + OPL <= a.N;
+                if (a.residual) {
+                    if (whole && a.res_f32) {
+                        const f32x4* r = reinterpret_cast<const f32x4*>(static_cast<const float*>(a.residual) + tok * a.ldr + col);
+#pragma unroll
+                        for (int h = 0; h < OPL / 4; ++h) v[h] += r[h];
+                    } else if (whole) {
+                        const uint16_t* r = static_cast<const uint16_t*>(a.residual) + tok * a.ldr + col;
+#pragma unroll
+                        for (int h = 0; h < OPL / 4; ++h) v[h] += __builtin_convertvector(*reinterpret_cast<const bf16x4*>(r + 4 * h), f32x4);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < OPL; ++e)
+                            if (col + e < a.N)
+                                v[e / 4][e % 4] += a.res_f32 ? static_cast<const float*>(a.residual)[tok * a.ldr + col + e]
+                                                             : __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.residual)[tok * a.ldr + col + e] << 16);
+                    }
+                }
+                char* const p = static_cast<char*>(a.y) + (tok * a.ldy + col) * (OUT_BF16 ? 2 : 4);
+                if (OUT_BF16) {
+                    bf16x8 o;
+#pragma unroll
+                    for (int e = 0; e < OPL; ++e) o[e] = (__bf16)v[e / 4][e % 4];
+                    if (whole) *reinterpret_cast<bf16x8*>(p) = o;
+                    else
+#pragma unroll
+                        for (int e = 0; e < OPL; ++e)
+                            if (col + e < a.N) reinterpret_cast<__bf16*>(p)[e] = o[e];
+                } else if (whole) {
+                    *reinterpret_cast<f32x4*>(p) = v[0];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < OPL; ++e)
+                        if (col + e < a.N) reinterpret_cast<float*>(p)[e] = v[0][e];
+                }
+            }
+        }
+    }
+}
+
+template <typename CFG, bool OUT_BF16, int EPI>
 __global__ void __launch_bounds__(CFG::THREADS) __attribute__((amdgpu_waves_per_eu(CFG::WGS_PER_CU * CFG::NW / 4, CFG::WGS_PER_CU * CFG::NW / 4)))
-gdn_linear_kernel(LinearArgs a) {
+gdn_linear_kernel(typename EpiArgs<EPI>::type a) {
     constexpr int BM = CFG::BM, BN = CFG::BN, BK = CFG::BK, STAGES = CFG::STAGES, RB = CFG::RB, PP = CFG::PP, RL = CFG::RL;
     constexpr int RPL = CFG::ROWS_PER_LOAD, TI = CFG::TI, TJ = CFG::TJ, XL = CFG::XL, WL = CFG::WL;
     extern __shared__ __align__(16) char smem[];
@@ -146,13 +252,19 @@ gdn_linear_kernel(LinearArgs a) {
     const int grp_rows = min(a.tiles_m - grp * GROUP_M, GROUP_M);
     const int tile_m = grp * GROUP_M + in_grp % grp_rows, tile_n = in_grp / grp_rows;
     const int64_t m0 = (int64_t)tile_m * BM;
-    const int n0 = tile_n * BN;
-
+    constexpr int BNO = EPI == EPI_GATED ? BN / 2 : BN;         // outputs of a tile
+    const int n0 = tile_n * BNO;
     const int64_t rows_x = a.T - m0 < BM ? a.T - m0 : BM;
-    const int rows_w = a.N - n0 < BN ? a.N - n0 : BN;
+    const int rows_w = a.N - n0 < BNO ? a.N - n0 : BNO;
     const char* xb = reinterpret_cast<const char*>(a.x) + m0 * a.ldx * 2;
     const char* wb = reinterpret_cast<const char*>(a.w) + (int64_t)n0 * a.ldw * 2;
     const int x_bytes = (int)((rows_x - 1) * a.ldx * 2 + (int64_t)a.K * 2), w_bytes = (int)((int64_t)(rows_w - 1) * a.ldw * 2 + (int64_t)a.K * 2);
+    const char* ub = wb;                                         // the second weight's rows
+    int u_bytes = w_bytes;
+    if constexpr (EPI == EPI_GATED) {
+        ub = reinterpret_cast<const char*>(a.w_up) + (int64_t)n0 * a.ldw_up * 2;
+        u_bytes = (int)((int64_t)(rows_w - 1) * a.ldw_up * 2 + (int64_t)a.K * 2);
+    }
 
     // a wave-wide load writes RPL rows of RB bytes: lane i lands at row i / PP, position i % PP, and fetches the piece that belongs there
     const int ld_row = lane / PP, ld_pos = lane % PP;
@@ -165,8 +277,16 @@ gdn_linear_kernel(LinearArgs a) {
 #pragma unroll
     for (int j = 0; j < WL; ++j) {
         const int row = (BN / CFG::NW) * wave + RPL * j + ld_row;
-        woff[j] = (int)(row * a.ldw * 2) + ((ld_pos ^ ((row / RL) % PP)) << 4);
+        if constexpr (EPI == EPI_GATED)
+            woff[j] = (int)(((row >> 5) * 16 + (row & 15)) * (up_load<CFG>(j, wave) ? a.ldw_up : a.ldw) * 2) + ((ld_pos ^ ((row / RL) % PP)) << 4);
+        else
+            woff[j] = (int)(row * a.ldw * 2) + ((ld_pos ^ ((row / RL) % PP)) << 4);
     }
+    // one of the wave's loads of a stage; past the last k step (not live) it fetches nothing
+    auto load = [&](int j, int stage, int k0, bool live) {
+        const bool up = EPI == EPI_GATED && j >= XL && up_load<CFG>(j - XL, wave);
+        LinLoad<CFG>::one(j, smem, stage, k0, wave, xb, live ? x_bytes : 0, up ? ub : wb, live ? (up ? u_bytes : w_bytes) : 0, xoff, woff);
+    };
     f32x4 acc[TJ][TI];           // [output tile][token tile]: lane lr = token, register e = output 4 g + e
 #pragma unroll
     for (int i = 0; i < TJ; ++i)
@@ -208,7 +328,8 @@ gdn_linear_kernel(LinearArgs a) {
 #pragma unroll
     for (int p = 0; p < STAGES; ++p) {
         const bool live = p < n_steps;
-        LinLoad<CFG>::all(smem, p, live ? p * BK : 0, wave, xb, live ? x_bytes : 0, wb, live ? w_bytes : 0, xoff, woff);
+#pragma unroll
+        for (int j = 0; j < CFG::LPS; ++j) load(j, p, live ? p * BK : 0, live);
     }
     wait_vm<(STAGES - 1) * CFG::LPS>();
     __syncthreads();
@@ -257,7 +378,7 @@ gdn_linear_kernel(LinearArgs a) {
             // against 47.3, 3000 x 4096 x 4096 90.4 / 85.9, 1000 x 8224 x 2048 50.4 / 48.7; warm 8192 x 8192 x 2048 189 / 191; two loads a slot: 48.0, 87.1, 49.1, 192.)
             // The fragments of the next stage's first k step are read in between as well.
             const bool live = step + STAGES < n_steps;
-            const int xbytes = live ? x_bytes : 0, wbytes = live ? w_bytes : 0, k_ahead = live ? (step + STAGES) * BK : 0;
+            const int k_ahead = live ? (step + STAGES) * BK : 0;
             const char* xs = smem + next_stage * CFG::STAGE_BYTES;
             const char* ws = xs + CFG::X_BYTES;
             const int pos = (g ^ sw) * 16;
@@ -274,7 +395,7 @@ gdn_linear_kernel(LinearArgs a) {
                     if (r < TI) xf[0][r] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(xs + xrow + 16 * r * RB + pos));
                     else wf[0][r - TI] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(ws + wrow + 16 * (r - TI) * RB + pos));
                 }
-                if (i < NL) LinLoad<CFG>::one(i, smem, stage, k_ahead, wave, xb, xbytes, wb, wbytes, xoff, woff);
+                if (i < NL) load(i, stage, k_ahead, live);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -294,6 +415,12 @@ gdn_linear_kernel(LinearArgs a) {
     //      piece) spread over the banks; then 4, 8 or 16 lanes store one row's contiguous bytes.  A wave's LDS operations execute in
     //      order, so no barrier stands between its writes and reads; the one barrier before keeps the other waves' last
     //      fragment reads out of the way.
+    if constexpr (EPI != EPI_BIAS) {
+        wait_vm<0>();
+        __syncthreads();
+        act_epilogue<CFG, OUT_BF16, EPI>(a, acc, smem + wave * (CFG::SMEM / CFG::NW), m0 + CFG::WM * wm, n0 + CFG::WN / (EPI == EPI_GATED ? 2 : 1) * wn, lane);
+        return;
+    } else {
     constexpr int ES = OUT_BF16 ? 2 : 4;
     constexpr int WN = CFG::WN, WM = CFG::WM;                      // the wave's outputs and tokens
     constexpr int REGION = CFG::SMEM / CFG::NW;                    // the wave's part of the ring
@@ -367,22 +494,89 @@ gdn_linear_kernel(LinearArgs a) {
             }
         }
     }
+    }
 }
 
-template <typename CFG, bool OUT_BF16>
-hipError_t launch_linear(LinearArgs a, hipStream_t stream) {
-    static hipError_t attr_err = hipFuncSetAttribute(reinterpret_cast<const void*>(&gdn_linear_kernel<CFG, OUT_BF16>),
+template <typename CFG, bool OUT_BF16, int EPI>
+hipError_t launch_linear(typename EpiArgs<EPI>::type a, hipStream_t stream) {
+    static hipError_t attr_err = hipFuncSetAttribute(reinterpret_cast<const void*>(&gdn_linear_kernel<CFG, OUT_BF16, EPI>),
                                                      hipFuncAttributeMaxDynamicSharedMemorySize, CFG::SMEM);
     if (attr_err != hipSuccess) return attr_err;
     const int64_t tiles_m = (a.T + CFG::BM - 1) / CFG::BM;
-    a.tiles_n = (a.N + CFG::BN - 1) / CFG::BN;
+    constexpr int BNO = EPI == EPI_GATED ? CFG::BN / 2 : CFG::BN;
+    a.tiles_n = (a.N + BNO - 1) / BNO;
     a.tiles_m = (int32_t)tiles_m;
     a.per_xcd = (int32_t)((tiles_m * a.tiles_n + 7) / 8);
-    hipLaunchKernelGGL((gdn_linear_kernel<CFG, OUT_BF16>), dim3((unsigned)(8 * (int64_t)a.per_xcd)), dim3(CFG::THREADS), CFG::SMEM, stream, a);
+    hipLaunchKernelGGL((gdn_linear_kernel<CFG, OUT_BF16, EPI>), dim3((unsigned)(8 * (int64_t)a.per_xcd)), dim3(CFG::THREADS), CFG::SMEM, stream, a);
     return hipGetLastError();
 }
 
-std::atomic<int32_t> g_linear_shape{-1};
+// ---- few rows (gdn_few_kernel.h): a workgroup of eight waves makes 16 outputs (of two products with a second weight) of up to 16 RT rows
+constexpr int FEW_WAVES = 8;
+
+template <int RT, bool OUT_BF16, bool GATED>
+__global__ void __launch_bounds__(64 * FEW_WAVES) gdn_linear_few_kernel(LinearActArgs a) {
+    constexpr int NT = GATED ? 2 : 1, U = RT == 4 ? 2 : 4;
+    __shared__ f32x4 sums[FEW_WAVES * NT * RT * 16 * 4];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lr = lane & 15, g = lane >> 4;
+    const int n0 = (int)blockIdx.x * 16;
+    // rows past the end are read as the last one: their sums are not used
+    const int64_t wrow = min(n0 + lr, a.N - 1);
+    const uint16_t* wp[NT];
+    const uint16_t* xp[RT];
+    wp[0] = static_cast<const uint16_t*>(a.w) + wrow * a.ldw + 8 * g;
+    if (GATED) wp[NT - 1] = static_cast<const uint16_t*>(a.w_up) + wrow * a.ldw_up + 8 * g;
+#pragma unroll
+    for (int j = 0; j < RT; ++j) xp[j] = static_cast<const uint16_t*>(a.x) + (int64_t)min(16 * j + lr, (int)a.T - 1) * a.ldx + 8 * g;
+    f32x4 acc[NT][RT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int j = 0; j < RT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    few::accumulate<NT, RT, FEW_WAVES, U>(acc, wp, xp, a.K / few::STEP, wave);
+    few::put_sums<NT, RT, FEW_WAVES>(acc, sums, wave, lane);
+    __syncthreads();
+    for (int i = threadIdx.x; i < RT * 16 * 4; i += 64 * FEW_WAVES) {      // four outputs of a row each
+        const int row = i >> 2, piece = i & 3, col = n0 + 4 * piece;
+        if (row >= a.T || col >= a.N) continue;
+        f32x4 v = few::get_sum<NT, RT, FEW_WAVES>(sums, 0, row, piece), up = {1.f, 1.f, 1.f, 1.f};
+        if (GATED) up = few::get_sum<NT, RT, FEW_WAVES>(sums, NT - 1, row, piece);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (col + e < a.N) {
+                if (a.bias) v[e] += a.bias[col + e];
+                if (GATED && a.bias_up) up[e] += a.bias_up[col + e];
+            }
+        v = activate(a.act, v);
+        if (GATED) v *= up;
+        v *= a.scale;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (col + e < a.N) {
+                if (a.residual)
+                    v[e] += a.res_f32 ? static_cast<const float*>(a.residual)[row * a.ldr + col + e]
+                                      : __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.residual)[row * a.ldr + col + e] << 16);
+                if (OUT_BF16) static_cast<__bf16*>(a.y)[row * a.ldy + col + e] = (__bf16)v[e];
+                else static_cast<float*>(a.y)[row * a.ldy + col + e] = v[e];
+            }
+    }
+}
+
+template <int RT>
+hipError_t launch_few(const LinearActArgs& a, bool bf, hipStream_t stream) {
+    const dim3 grid((unsigned)((a.N + 15) / 16)), block(64 * FEW_WAVES);
+    if (a.w_up) {
+        if (bf) hipLaunchKernelGGL((gdn_linear_few_kernel<RT, true, true>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((gdn_linear_few_kernel<RT, false, true>), grid, block, 0, stream, a);
+    } else {
+        if (bf) hipLaunchKernelGGL((gdn_linear_few_kernel<RT, true, false>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((gdn_linear_few_kernel<RT, false, false>), grid, block, 0, stream, a);
+    }
+    return hipGetLastError();
+}
+
+std::atomic<int32_t> g_linear_shape{-1}, g_act_shape{-1};
 
 int chip_cus_linear() {
     static const int n = [] {
@@ -427,12 +621,11 @@ double shape_cost(const ShapeCost& c, int64_t T, int64_t N, int32_t K) {
 // into columns that fill whole rounds of 256 x 256 tiles and a rest in a smaller shape, a launch of its own.  Measured, whole / cut: 8192 x
 // 8224 (33 tile columns where 32 fill four rounds) 233 / 211 us, 8192 x 2560 88 / 76, 2048 x 8224 90 / 65, 4096 x 8224 138 / 113.
 struct LinearPlan { int shape, rest_shape; int32_t cols; };   // outputs 0 .. cols - 1 in `shape`, the others in `rest_shape`
-LinearPlan plan_linear(int64_t T, int32_t N, int32_t K) {
-    const int forced = g_linear_shape.load();
-    if (forced >= 0) return {forced, 0, N};
+LinearPlan plan_tiles(int64_t T, int32_t N, int32_t K, bool gated) {      // gated: N rows of both weights together; no shape 5
     auto best_of = [&](int64_t n, int shapes, double* t) {
         int best = 0;
         for (int i = 0; i < shapes; ++i) {
+            if (gated && SHAPES[i].id == 5) continue;
             const double ti = shape_cost(SHAPES[i], T, n, K);
             if (i == 0 || ti < *t) { best = SHAPES[i].id; *t = ti; }
         }
@@ -452,6 +645,22 @@ LinearPlan plan_linear(int64_t T, int32_t N, int32_t K) {
         const double t = shape_cost(SHAPES[4], T, cols, K) + rest + launch;
         if (t < least) { least = t; p = {2, rest_shape, (int32_t)cols}; }
     }
+    return p;
+}
+LinearPlan plan_linear(int64_t T, int32_t N, int32_t K) {
+    const int forced = g_linear_shape.load();
+    return forced >= 0 ? LinearPlan{forced, 0, N} : plan_tiles(T, N, K, false);
+}
+
+constexpr int FEW = 6, FEW_ROWS = 64;
+LinearPlan plan_act(int64_t T, int32_t N, int32_t K, bool gated) {
+    const int forced = g_act_shape.load();
+    if (T <= FEW_ROWS && (forced == FEW || forced < 0)) return {FEW, 0, N};
+    if (forced >= 0 && forced != FEW) return {forced == 1 ? 2 : gated && forced == 5 ? 0 : forced, 0, N};
+    if (!gated) return plan_tiles(T, N, K, false);
+    if (N > INT32_MAX / 2) return {2, 0, N};
+    LinearPlan p = plan_tiles(T, 2 * N, K, true);
+    p.cols /= 2;                                         // (a multiple of 128 where it is cut)
     return p;
 }
 
@@ -479,17 +688,24 @@ int32_t linear_checks(const void* x, int64_t ldx, const void* w, int64_t ldw, co
     return GDN_OK;
 }
 
-int32_t launch_shape(const LinearArgs& a, int shape, bool bf, hipStream_t stream) {
-    hipError_t e;
+template <typename CFG, int EPI>
+hipError_t launch_out(const typename EpiArgs<EPI>::type& a, bool bf, hipStream_t stream) {
+    return bf ? launch_linear<CFG, true, EPI>(a, stream) : launch_linear<CFG, false, EPI>(a, stream);
+}
+template <int EPI>
+int32_t launch_shape(const typename EpiArgs<EPI>::type& a, int shape, bool bf, hipStream_t stream) {
     switch (shape) {
-        case 1: e = bf ? launch_linear<LinBig, true>(a, stream) : launch_linear<LinBig, false>(a, stream); break;
-        case 2: e = bf ? launch_linear<LinBig8, true>(a, stream) : launch_linear<LinBig8, false>(a, stream); break;
-        case 3: e = bf ? launch_linear<LinTiny, true>(a, stream) : launch_linear<LinTiny, false>(a, stream); break;
-        case 4: e = bf ? launch_linear<LinDeep, true>(a, stream) : launch_linear<LinDeep, false>(a, stream); break;
-        case 5: e = bf ? launch_linear<LinWide, true>(a, stream) : launch_linear<LinWide, false>(a, stream); break;
-        default: e = bf ? launch_linear<LinSmall, true>(a, stream) : launch_linear<LinSmall, false>(a, stream); break;
+        case 1:
+            if constexpr (EPI == EPI_BIAS) return hip_err(launch_out<LinBig, EPI>(a, bf, stream));
+            [[fallthrough]];
+        case 2: return hip_err(launch_out<LinBig8, EPI>(a, bf, stream));
+        case 3: return hip_err(launch_out<LinTiny, EPI>(a, bf, stream));
+        case 4: return hip_err(launch_out<LinDeep, EPI>(a, bf, stream));
+        case 5:
+            if constexpr (EPI != EPI_GATED) return hip_err(launch_out<LinWide, EPI>(a, bf, stream));   // (an odd number of tiles to a wave)
+            return GDN_ERR_SHAPE;
+        default: return hip_err(launch_out<LinSmall, EPI>(a, bf, stream));
     }
-    return hip_err(e);
 }
 
 // Columns c0 .. c1 - 1 of a projection as a projection of its own (c0 a multiple of 256: every alignment holds).
@@ -518,10 +734,24 @@ LinearArgs column_range(const LinearArgs& a, int32_t c0, int32_t c1, int es) {
 int32_t linear_launch(const LinearArgs& a, int32_t out_dtype, hipStream_t stream) {
     const bool bf = out_dtype == GDN_BF16;
     const LinearPlan p = plan_linear(a.T, a.N, a.K);
-    if (p.cols == a.N) return launch_shape(a, p.shape, bf, stream);
+    if (p.cols == a.N) return launch_shape<EPI_BIAS>(a, p.shape, bf, stream);
     const int es = bf ? 2 : 4;
-    const int32_t rc = launch_shape(column_range(a, 0, p.cols, es), p.shape, bf, stream);
-    return rc != GDN_OK ? rc : launch_shape(column_range(a, p.cols, a.N, es), p.rest_shape, bf, stream);
+    const int32_t rc = launch_shape<EPI_BIAS>(column_range(a, 0, p.cols, es), p.shape, bf, stream);
+    return rc != GDN_OK ? rc : launch_shape<EPI_BIAS>(column_range(a, p.cols, a.N, es), p.rest_shape, bf, stream);
+}
+
+// Outputs c0 .. c1 - 1 of a projection with an epilogue, as one of its own.
+LinearActArgs act_range(const LinearActArgs& a, int32_t c0, int32_t c1, int es) {
+    LinearActArgs b = a;
+    static_cast<LinearArgs&>(b) = column_range(a, c0, c1, es);
+    if (a.w_up) b.w_up = static_cast<const char*>(a.w_up) + (int64_t)c0 * a.ldw_up * 2;
+    if (a.bias_up) b.bias_up = a.bias_up + c0;
+    if (a.residual) b.residual = static_cast<const char*>(a.residual) + (int64_t)c0 * (a.res_f32 ? 4 : 2);
+    return b;
+}
+int32_t launch_act_shape(const LinearActArgs& a, int shape, bool bf, hipStream_t stream) {
+    if (shape == FEW) return hip_err(a.T <= 16 ? launch_few<1>(a, bf, stream) : a.T <= 32 ? launch_few<2>(a, bf, stream) : launch_few<4>(a, bf, stream));
+    return a.w_up ? launch_shape<EPI_GATED>(a, shape, bf, stream) : launch_shape<EPI_ACT>(a, shape, bf, stream);
 }
 }  // namespace
 
@@ -587,4 +817,56 @@ extern "C" int32_t gdn_linear_plan(int64_t T, int32_t N, int32_t K, int32_t* sha
 
 extern "C" int32_t gdn_linear_tune(int32_t shape) {
     return g_linear_shape.exchange(shape < 0 || shape > 5 ? -1 : shape);
+}
+
+extern "C" int32_t gdn_linear_act(const void* x, int64_t ldx, const void* w, int64_t ldw, const float* bias, const gdn_linear_epilogue* epi, void* y,
+                                  int64_t ldy, int32_t out_dtype, int64_t T, int32_t N, int32_t K, void* stream_) {
+    if (!epi) return GDN_ERR_NULL;
+    int32_t rc = linear_checks(x, ldx, w, ldw, bias, out_dtype, T, N, K);
+    if (rc != GDN_OK) return rc;
+    if (epi->act < GDN_ACT_NONE || epi->act > GDN_ACT_SIGMOID || (epi->bias_up && !epi->w_up) || ldy < N) return GDN_ERR_SHAPE;
+    if (epi->w_up && epi->ldw_up < K) return GDN_ERR_SHAPE;
+    if (epi->residual && (!dtype_known(epi->res_dtype) || epi->ldr < N)) return GDN_ERR_SHAPE;
+    if (T == 0 || N == 0) return GDN_OK;
+    if (!y) return GDN_ERR_NULL;
+    const int es = dtype_bytes(out_dtype), rs = dtype_bytes(epi->res_dtype);
+    if (off_align(y, es == 2 ? 8 : 16) || (ldy & 3)) return GDN_ERR_ALIGN;
+    if (epi->w_up && (off_align(epi->w_up, 16) || (epi->ldw_up & 7))) return GDN_ERR_ALIGN;
+    if (off_align(epi->bias_up, 4)) return GDN_ERR_ALIGN;
+    if (epi->residual && (off_align(epi->residual, rs == 2 ? 8 : 16) || (epi->ldr & 3))) return GDN_ERR_ALIGN;
+    if (epi->w_up && (int64_t)256 * epi->ldw_up * 2 >= ((int64_t)1 << 31)) return GDN_ERR_COUNT;
+    if (T > ((int64_t)1 << 40) || ldy > ((int64_t)1 << 30) || (epi->residual && epi->ldr > ((int64_t)1 << 30))) return GDN_ERR_COUNT;
+    const Rows out(y, T, ldy * es, (int64_t)N * es), res(epi->residual, T, epi->ldr * rs, (int64_t)N * rs);
+    if (share_bytes(out, Rows(x, T, ldx * 2, (int64_t)K * 2)) || share_bytes(out, Rows(w, N, ldw * 2, (int64_t)K * 2)) ||
+        share_bytes(out, Rows(epi->w_up, N, epi->ldw_up * 2, (int64_t)K * 2)) || share_bytes(out, Rows(bias, 1, (int64_t)N * 4, (int64_t)N * 4)) ||
+        share_bytes(out, Rows(epi->bias_up, 1, (int64_t)N * 4, (int64_t)N * 4)) || (share_bytes(out, res) && !same_rows(out, res)))
+        return GDN_ERR_SLOT_HAZARD;
+    LinearActArgs a = {};
+    a.x = x; a.w = w; a.bias = bias; a.y = y;
+    a.ldx = ldx; a.ldw = ldw; a.ldy = ldy;
+    a.T = T; a.N = N; a.K = K;
+    a.w_up = epi->w_up; a.ldw_up = epi->ldw_up; a.bias_up = epi->bias_up;
+    a.residual = epi->residual; a.ldr = epi->ldr; a.res_f32 = epi->res_dtype == GDN_F32;
+    a.act = epi->act; a.scale = epi->scale;
+    hipStream_t stream = (hipStream_t)stream_;
+    const bool bf = out_dtype == GDN_BF16;
+    const LinearPlan p = plan_act(T, N, K, epi->w_up != nullptr);
+    if (p.cols == N) return launch_act_shape(a, p.shape, bf, stream);
+    rc = launch_act_shape(act_range(a, 0, p.cols, es), p.shape, bf, stream);
+    return rc != GDN_OK ? rc : launch_act_shape(act_range(a, p.cols, N, es), p.rest_shape, bf, stream);
+}
+
+extern "C" int32_t gdn_linear_act_plan(int64_t T, int32_t N, int32_t K, int32_t gated, int32_t* shape, int32_t* cols, int32_t* rest_shape) {
+    if (T <= 0 || N <= 0 || K <= 0) return GDN_ERR_COUNT;
+    if (K % 64 != 0 || gated < 0 || gated > 1) return GDN_ERR_SHAPE;
+    if (!shape || !cols || !rest_shape) return GDN_ERR_NULL;
+    const LinearPlan p = plan_act(T, N, K, gated != 0);
+    *shape = p.shape;
+    *cols = p.cols;
+    *rest_shape = p.rest_shape;
+    return GDN_OK;
+}
+
+extern "C" int32_t gdn_linear_act_tune(int32_t shape) {
+    return g_act_shape.exchange(shape < 0 || shape > FEW ? -1 : shape);
 }

@@ -3,11 +3,20 @@ from __future__ import annotations
 
 import ctypes
 
+from . import rows
 from .binding import GDN_BF16, GDN_F32, _check, _dp, _stream_ptr, lib
 
 _i32, _i64, _vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p
 
-EXPORTS = ["gdn_linear", "gdn_linear_split", "gdn_linear_plan", "gdn_linear_tune"]
+EXPORTS = ["gdn_linear", "gdn_linear_split", "gdn_linear_plan", "gdn_linear_tune", "gdn_linear_act", "gdn_linear_act_plan", "gdn_linear_act_tune"]
+
+ACTS = {"none": 0, "silu": 1, "gelu": 2, "gelu_tanh": 3, "relu": 4, "relu2": 5, "sigmoid": 6}
+
+
+class gdn_linear_epilogue(ctypes.Structure):
+    _fields_ = [("act", _i32), ("res_dtype", _i32), ("scale", ctypes.c_float), ("w_up", _vp), ("ldw_up", _i64), ("bias_up", _vp),
+                ("residual", _vp), ("ldr", _i64)]
+
 
 _ready = False
 
@@ -24,6 +33,12 @@ def _lib():
         L.gdn_linear_plan.argtypes = [_i64, _i32, _i32, _vp, _vp, _vp]
         L.gdn_linear_tune.restype = _i32
         L.gdn_linear_tune.argtypes = [_i32]
+        L.gdn_linear_act.restype = _i32
+        L.gdn_linear_act.argtypes = [_vp, _i64, _vp, _i64, _vp, ctypes.POINTER(gdn_linear_epilogue), _vp, _i64, _i32, _i64, _i32, _i32, _vp]
+        L.gdn_linear_act_plan.restype = _i32
+        L.gdn_linear_act_plan.argtypes = [_i64, _i32, _i32, _i32, _vp, _vp, _vp]
+        L.gdn_linear_act_tune.restype = _i32
+        L.gdn_linear_act_tune.argtypes = [_i32]
         _ready = True
     return L
 
@@ -115,3 +130,49 @@ def gdn_linear_split(x, w, bias, ys, stream=None) -> None:
     ldw = int(w.stride(0)) if int(w.shape[0]) > 1 else K
     _check(gdn_linear_split_raw(x.data_ptr(), ldx, w.data_ptr(), ldw, bias.data_ptr() if bias is not None else 0, plan, code, T, K,
                                 _stream_ptr(stream).value or 0), "gdn_linear_split")
+
+
+def gdn_linear_act_raw(x_ptr: int, ldx: int, w_ptr: int, ldw: int, bias_ptr: int, epilogue, y_ptr: int, ldy: int, out_dtype: int, T: int, N: int,
+                       K: int, stream_ptr: int = 0) -> int:
+    """The C entry point with plain integers for the pointers; returns the status code (no exception)."""
+    return int(_lib().gdn_linear_act(x_ptr, ldx, w_ptr, ldw, bias_ptr, ctypes.byref(epilogue) if epilogue is not None else None, y_ptr, ldy, out_dtype,
+                                     T, N, K, stream_ptr))
+
+
+_codes = {}                                              # torch's types and their codes
+
+
+def gdn_linear_act(x, w, bias, y, act="none", w_up=None, bias_up=None, residual=None, scale=1.0, stream=None) -> None:
+    """y = scale * a + residual, a = act(x w^T + bias), or act(x w^T + bias) * (x w_up^T + bias_up) with a w_up; act: one of ACTS.  x [T][K], w and w_up
+    [N][K] are bf16, biases fp32 [N] or None, y and residual [T][N] bf16 or fp32; inner strides are 1, row strides passed on.  residual may be y."""
+    if not _codes:
+        import torch
+        _codes.update({torch.bfloat16: GDN_BF16, torch.float32: GDN_F32})
+    (T, K), N = x.shape, w.shape[0]
+    if (w.shape[1] != K or y.shape != (T, N) or (w_up is not None and w_up.shape != w.shape) or (residual is not None and residual.shape != y.shape)
+            or (bias is not None and bias.shape != (N,)) or (bias_up is not None and bias_up.shape != (N,))):
+        raise ValueError("gdn_linear_act: shapes do not match")
+    code, res_code = _codes.get(y.dtype), _codes.get(residual.dtype) if residual is not None else GDN_BF16
+    if _codes.get(x.dtype) != GDN_BF16 or w.dtype is not x.dtype or (w_up is not None and w_up.dtype is not x.dtype) or code is None or res_code is None:
+        raise ValueError("gdn_linear_act: x and the weights are bf16, y and residual bf16 or fp32")
+    for b in (bias, bias_up):
+        if b is not None and (_codes.get(b.dtype) != GDN_F32 or (N > 1 and b.stride(0) != 1)):
+            raise ValueError("gdn_linear_act: biases are fp32, without gaps")
+    if act not in ACTS:
+        raise ValueError(f"gdn_linear_act: an activation of {sorted(ACTS)}")
+    device = rows._here(x, w, bias, y, w_up, bias_up, residual)
+    epilogue = gdn_linear_epilogue(ACTS[act], res_code, scale, rows._dp(w_up), rows._ld(w_up), rows._dp(bias_up), rows._dp(residual), rows._ld(residual))
+    _check(_lib().gdn_linear_act(x.data_ptr(), rows._ld(x), w.data_ptr(), rows._ld(w), rows._dp(bias), ctypes.byref(epilogue), y.data_ptr(), rows._ld(y),
+                                 code, T, N, K, rows._stream_ptr(stream, device)), "gdn_linear_act")
+
+
+def gdn_linear_act_plan(T: int, N: int, K: int, gated: bool = False):
+    """(tile shape, outputs it covers, tile shape of the other outputs) of a projection with an epilogue, in gdn_linear_act_tune's numbers; host only."""
+    shape, cols, rest = _i32(0), _i32(0), _i32(0)
+    _check(_lib().gdn_linear_act_plan(int(T), int(N), int(K), int(gated), ctypes.byref(shape), ctypes.byref(cols), ctypes.byref(rest)), "gdn_linear_act_plan")
+    return shape.value, cols.value, rest.value
+
+
+def gdn_linear_act_tune(shape: int) -> int:
+    """Fixes the kernel of gdn_linear_act (0 to 6, see include/gdn_linear.h) or returns the choice to the library (-1); returns the previous setting."""
+    return int(_lib().gdn_linear_act_tune(int(shape)))
