@@ -3,7 +3,7 @@ from __future__ import annotations
 
 import ctypes
 
-from .binding import GDN_BF16, GDN_F32, GdnError, _check, lib
+from .binding import GDN_BF16, GDN_F32, _check, lib
 from .rows import _dp, _here, _ld, _stream_ptr
 
 _i32, _i64, _vp, _f32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_float

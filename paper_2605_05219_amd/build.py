@@ -11,7 +11,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libgdn_resume.so")
 LIB_PHASES = os.path.join(PKG, "libgdn_resume_phases.so")   # profiling build: the fused kernel leaves cycle stamps
-SOURCES = ["gdn_resume.hip", "gdn_layer.hip", "gdn_linear.hip", "gdn_block.hip", "attn_resume.hip", "attn_paged.hip", "gdn_plan.cpp", "ckpt_place.cpp"]
+SOURCES = ["gdn_resume.hip", "gdn_layer.hip", "gdn_linear.hip", "gdn_block.hip", "gdn_moe.hip", "attn_resume.hip", "attn_paged.hip", "gdn_plan.cpp", "ckpt_place.cpp"]
 
 
 def build_library(verbose: bool = False, phase_stamps: bool = False) -> str:

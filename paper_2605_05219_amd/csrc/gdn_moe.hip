@@ -1,0 +1,128 @@
+// gdn_moe: host side of a mixture of experts (see include/gdn_moe.h, kernels in gdn_moe_kernel.h).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "gdn_moe.h"
+#include "gdn_moe_kernel.h"
+#include "gdn_rows.h"
+
+namespace gdn {
+namespace moe {
+
+inline int32_t hip_err(hipError_t e) { return e == hipSuccess ? GDN_OK : GDN_ERR_HIP - (int32_t)e; }
+
+int32_t check_shape(const gdn_moe_shape* s, int64_t T) {
+    if (!s) return GDN_ERR_NULL;
+    if (T < 0) return GDN_ERR_COUNT;
+    if (s->E < 1 || s->E > MAX_E || s->k < 1 || s->k > MAX_K || s->k > s->E) return GDN_ERR_SHAPE;
+    if (s->D < 64 || s->D > 32768 || s->D % 64 || s->F < 64 || s->F > 32768 || s->F % 64) return GDN_ERR_SHAPE;
+    if (s->act < GDN_ACT_NONE || s->act > GDN_ACT_SIGMOID || s->score < 0 || s->score > GDN_SCORE_SIGMOID || s->normalise < 0 || s->normalise > 1 ||
+        !dtype_known(s->router_dtype) || !std::isfinite(s->routed_scale))
+        return GDN_ERR_SHAPE;
+    if (T * s->k >= ((int64_t)1 << 24) || T >= ((int64_t)1 << 24)) return GDN_ERR_COUNT;
+    return GDN_OK;
+}
+
+// Byte offsets of the workspace's arrays.
+struct Layout { int64_t logits, ids, weights, counts, active, list, h, part, end; };
+Layout layout(const gdn_moe_shape& s, int64_t T) {
+    Layout w;
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) { const int64_t here = at; at += (bytes + 255) / 256 * 256; return here; };
+    w.logits = take(T * s.E * 4);
+    w.ids = take(T * s.k * 4);
+    w.weights = take(T * s.k * 4);
+    w.counts = take((s.E + 1) * 4);
+    w.active = take(s.E * 4);
+    w.list = take(T * s.E * 4);
+    w.h = take(T * s.k * s.F * 2);
+    w.part = take(T * s.k * s.D * 4);
+    w.end = at;
+    return w;
+}
+
+template <int TT, int TE>
+void launch_logits(const MoeArgs& a, hipStream_t stream) {
+    hipLaunchKernelGGL((moe_logits_kernel<TT, TE>), dim3((unsigned)((a.E + 4 * TE - 1) / (4 * TE)), (unsigned)((a.T + TT - 1) / TT)), dim3(256), 0, stream, a);
+}
+template <int P>
+void launch_route(const MoeArgs& a, hipStream_t stream) {
+    hipLaunchKernelGGL((moe_route_kernel<P>), dim3((unsigned)((a.T + 3) / 4)), dim3(256), 0, stream, a);
+}
+template <int RT>
+void launch_products(const MoeArgs& a, hipStream_t stream) {
+    const unsigned most = (unsigned)std::min<int64_t>(a.E, (int64_t)a.T * a.k);
+    hipLaunchKernelGGL((moe_up_kernel<RT>), dim3((unsigned)(a.F / 16), most), dim3(64 * UP_WAVES), 0, stream, a);
+    hipLaunchKernelGGL((moe_down_kernel<RT>), dim3((unsigned)(a.D / 16), most), dim3(64 * DOWN_WAVES), 0, stream, a);
+}
+
+}  // namespace moe
+}  // namespace gdn
+
+using namespace gdn;
+using namespace gdn::moe;
+
+extern "C" int64_t gdn_moe_workspace_bytes(const gdn_moe_shape* shape, int64_t T) {
+    const int32_t rc = check_shape(shape, T);
+    return rc != GDN_OK ? rc : layout(*shape, T).end;
+}
+
+extern "C" int32_t gdn_moe(const gdn_moe_shape* s, const void* x, int64_t ldx, const void* w_router, const float* choice_bias, const void* w_gate_up,
+                           const void* w_down, const void* add, int64_t ld_add, void* y, int64_t ldy, int32_t* ids, float* weights, int64_t T,
+                           void* workspace, int64_t workspace_bytes, void* stream_) {
+    const int32_t rc = check_shape(s, T);
+    if (rc != GDN_OK || T == 0) return rc;
+    if (!x || !w_router || !w_gate_up || !w_down || !y) return GDN_ERR_NULL;
+    const int64_t D = s->D, F = s->F, E = s->E, most = (int64_t)1 << 30;
+    if (ldx < D || ldy < D || (add && ld_add < D)) return GDN_ERR_SHAPE;
+    for (const void* p : {x, w_router, w_gate_up, w_down, add, (const void*)y})
+        if (off_align(p, 16)) return GDN_ERR_ALIGN;
+    if (off_align(choice_bias, 4) || off_align(ids, 4) || off_align(weights, 4)) return GDN_ERR_ALIGN;
+    if ((ldx & 7) || (ldy & 7) || (add && (ld_add & 7))) return GDN_ERR_ALIGN;
+    if (ldx > most || ldy > most || (add && ld_add > most)) return GDN_ERR_COUNT;
+    const Layout w = layout(*s, T);
+    if (!workspace || off_align(workspace, 16) || workspace_bytes < w.end) return GDN_ERR_WORKSPACE;
+
+    const Rows outs[4] = {Rows(y, T, ldy * 2, D * 2), Rows(ids, 1, T * s->k * 4, T * s->k * 4), Rows(weights, 1, T * s->k * 4, T * s->k * 4),
+                          Rows(workspace, 1, w.end, w.end)};
+    const int64_t rb = dtype_bytes(s->router_dtype);
+    const Rows ins[6] = {Rows(x, T, ldx * 2, D * 2), Rows(w_router, 1, E * D * rb, E * D * rb), Rows(choice_bias, 1, E * 4, E * 4),
+                         Rows(w_gate_up, 1, E * 2 * F * D * 2, E * 2 * F * D * 2), Rows(w_down, 1, E * D * F * 2, E * D * F * 2), Rows(add, T, ld_add * 2, D * 2)};
+    for (int i = 0; i < 4; ++i) {
+        for (int j = i + 1; j < 4; ++j)
+            if (share_bytes(outs[i], outs[j])) return GDN_ERR_SLOT_HAZARD;
+        for (int j = 0; j < 6; ++j)
+            if (share_bytes(outs[i], ins[j]) && !(i == 0 && j == 5 && same_rows(outs[i], ins[j]))) return GDN_ERR_SLOT_HAZARD;
+    }
+
+    MoeArgs a = {};
+    a.x = static_cast<const uint16_t*>(x); a.w_router = w_router; a.choice_bias = choice_bias;
+    a.w_gate_up = static_cast<const uint16_t*>(w_gate_up); a.w_down = static_cast<const uint16_t*>(w_down); a.add = static_cast<const uint16_t*>(add);
+    a.y = static_cast<uint16_t*>(y); a.out_ids = ids; a.out_weights = weights;
+    a.ldx = ldx; a.ld_add = ld_add; a.ldy = ldy;
+    a.T = (int32_t)T; a.E = s->E; a.k = s->k; a.D = s->D; a.F = s->F;
+    a.act = s->act; a.score = s->score; a.normalise = s->normalise; a.router_f32 = s->router_dtype == GDN_F32; a.routed_scale = s->routed_scale;
+    char* const ws = static_cast<char*>(workspace);
+    a.logits = reinterpret_cast<float*>(ws + w.logits); a.ids = reinterpret_cast<int32_t*>(ws + w.ids); a.weights = reinterpret_cast<float*>(ws + w.weights);
+    a.counts = reinterpret_cast<int32_t*>(ws + w.counts); a.active = reinterpret_cast<int32_t*>(ws + w.active); a.list = reinterpret_cast<int32_t*>(ws + w.list);
+    a.h = reinterpret_cast<uint16_t*>(ws + w.h); a.part = reinterpret_cast<float*>(ws + w.part);
+    hipStream_t stream = static_cast<hipStream_t>(stream_);
+
+    if (T == 1) launch_logits<1, 2>(a, stream);
+    else if (T <= 16) launch_logits<2, 2>(a, stream);
+    else launch_logits<4, 4>(a, stream);
+    const int per_lane = (s->E + 63) / 64;
+    if (per_lane <= 1) launch_route<1>(a, stream);
+    else if (per_lane <= 2) launch_route<2>(a, stream);
+    else if (per_lane <= 4) launch_route<4>(a, stream);
+    else if (per_lane <= 8) launch_route<8>(a, stream);
+    else launch_route<16>(a, stream);
+    const double rows = (double)T * s->k / s->E;                 // of an expert, by an even choice
+    if (rows <= 8) launch_products<1>(a, stream);
+    else if (rows <= 24) launch_products<2>(a, stream);
+    else launch_products<4>(a, stream);
+    hipLaunchKernelGGL(moe_sum_kernel, dim3((unsigned)((T * (D / 8) + 255) / 256)), dim3(256), 0, stream, a);
+    return hip_err(hipGetLastError());
+}
