@@ -64,6 +64,12 @@ int32_t gdn_moe(const gdn_moe_shape *shape, const void *x, int64_t ldx, const vo
                 const void *w_gate_up, const void *w_down, const void *add, int64_t ld_add, void *y, int64_t ldy,
                 int32_t *ids, float *weights, int64_t T, void *workspace, int64_t workspace_bytes, void *stream);
 
+/*
+ * Tuning knob, not a method step: fixes the kernels of the experts' products (0, 2, 3: the projections' tiles of 128 x 128, 256 x 256, 64 x 64, where their
+ * 31-bit offsets reach; 6: the kernels of few rows; anything else: chosen per call, the default).  Process-wide; returns the previous setting (-1 = per call).
+ */
+int32_t gdn_moe_tune(int32_t shape);
+
 #ifdef __cplusplus
 }
 #endif

@@ -32,10 +32,12 @@
 #include <atomic>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "gdn_act.h"
 #include "gdn_few_kernel.h"
 #include "gdn_linear.h"
+#include "gdn_linear_tiles.h"
 #include "gdn_rows.h"
 
 namespace gdn {
@@ -77,9 +79,21 @@ struct LinearActArgs : LinearArgs {
 };
 // What a kernel makes of its sums: the bias added; with an activation, a factor and a residual; the same of two products, in the tiles of
 // 16 outputs in turn (a wave's output tile 2 p holds 16 outputs of the gate, 2 p + 1 the same of w_up: one lane has both).
-enum { EPI_BIAS = 0, EPI_ACT = 1, EPI_GATED = 2 };
-template <int EPI> struct EpiArgs { typedef LinearActArgs type; };
+// The experts' products are the second and the third of these on rows that a list names (gdn_linear_tiles.h).
+enum { EPI_BIAS = 0, EPI_ACT = 1, EPI_GATED = 2, EPI_EXPERT = 3, EPI_EXPERT_GATED = 4 };
+constexpr bool epi_gated(int e) { return e == EPI_GATED || e == EPI_EXPERT_GATED; }
+constexpr bool epi_expert(int e) { return e >= EPI_EXPERT; }
+struct ExpertArgs : LinearActArgs {
+    const int32_t* list;
+    const ExpertTile* table;
+    const int32_t* n_tiles;
+    const float* weights;
+    int32_t list_stride, div, x_rows;
+};
+template <int EPI> struct EpiArgs { typedef ExpertArgs type; };
 template <> struct EpiArgs<EPI_BIAS> { typedef LinearArgs type; };
+template <> struct EpiArgs<EPI_ACT> { typedef LinearActArgs type; };
+template <> struct EpiArgs<EPI_GATED> { typedef LinearActArgs type; };
 
 inline int32_t hip_err(hipError_t e) { return e == hipSuccess ? GDN_OK : GDN_ERR_HIP - (int32_t)e; }
 
@@ -141,8 +155,9 @@ __device__ __forceinline__ bool up_load(int j, int wave) {
 // One bias, activation, factor and residual on a wave's outputs, and out through LDS in fp32 (one rounding, behind the residual): as
 // the epilogue below, a row of at most 64 outputs to a pass.
 template <typename CFG, bool OUT_BF16, int EPI>
-__device__ __forceinline__ void act_epilogue(const LinearActArgs& a, f32x4 (&acc)[CFG::TJ][CFG::TI], char* reg, int64_t tok0, int col0, int lane) {
-    constexpr int PAIR = EPI == EPI_GATED ? 2 : 1;                 // accumulator tiles to a tile of outputs
+__device__ __forceinline__ void act_epilogue(const typename EpiArgs<EPI>::type& a, f32x4 (&acc)[CFG::TJ][CFG::TI], char* reg, int64_t tok0, int col0,
+                                             int lane, const int32_t* list, int64_t n_rows) {
+    constexpr int PAIR = epi_gated(EPI) ? 2 : 1;                 // accumulator tiles to a tile of outputs
     constexpr int WN = CFG::WN / PAIR, WM = CFG::WM;
     constexpr int REGION = CFG::SMEM / CFG::NW;
     constexpr int PW = WN <= 64 ? WN : 16;                         // outputs per pass (shape 5's 80 go 16 at a time)
@@ -164,13 +179,13 @@ __device__ __forceinline__ void act_epilogue(const LinearActArgs& a, f32x4 (&acc
                 for (int e = 0; e < 4; ++e)
                     if (col0 + cl + e < a.N) {
                         if (a.bias) bv[e] = a.bias[col0 + cl + e];
-                        if (EPI == EPI_GATED && a.bias_up) bu[e] = a.bias_up[col0 + cl + e];
+                        if (epi_gated(EPI) && a.bias_up) bu[e] = a.bias_up[col0 + cl + e];
                     }
 #pragma unroll
                 for (int ti = t0 / 16; ti < (t0 + TP) / 16; ++ti) {
                     const int row = 16 * ti + lr - t0;
                     f32x4 v = activate(a.act, acc[PAIR * tj][ti] + bv);
-                    if (EPI == EPI_GATED) v *= acc[PAIR * tj + PAIR - 1][ti] + bu;
+                    if (epi_gated(EPI)) v *= acc[PAIR * tj + PAIR - 1][ti] + bu;
                     const int piece = (cl - c0) / 4;
                     *reinterpret_cast<f32x4*>(reg + row * RBY + ((piece ^ (row % PPR)) << 4)) = v;
                 }
@@ -181,12 +196,19 @@ __device__ __forceinline__ void act_epilogue(const LinearActArgs& a, f32x4 (&acc
                 f32x4 v[OPL / 4];
 #pragma unroll
                 for (int h = 0; h < OPL / 4; ++h)
-                    v[h] = a.scale * *reinterpret_cast<const f32x4*>(reg + row * RBY + (((first / 4 + h) ^ (row % PPR)) << 4));
-                const int64_t tok = tok0 + t0 + row;
+                    v[h] = *reinterpret_cast<const f32x4*>(reg + row * RBY + (((first / 4 + h) ^ (row % PPR)) << 4));
+                int64_t tok = tok0 + t0 + row;
                 const int col = col0 + c0 + first;
-                if (tok >= a.T || col >= a.N) continue;
+                if (tok >= n_rows || col >= a.N) continue;
+                float scale = a.scale;
+                if constexpr (epi_expert(EPI)) {
+                    tok = list[tok];
+                    if (EPI == EPI_EXPERT) scale = a.weights[tok];
+                }
+#pragma unroll
+                for (int h = 0; h < OPL / 4; ++h) v[h] *= scale;
                 const bool whole = col + OPL <= a.N;
-                if (a.residual) {
+                if (!epi_expert(EPI) && a.residual) {
                     if (whole && a.res_f32) {
                         const f32x4* r = reinterpret_cast<const f32x4*>(static_cast<const float*>(a.residual) + tok * a.ldr + col);
 #pragma unroll
@@ -225,6 +247,12 @@ __device__ __forceinline__ void act_epilogue(const LinearActArgs& a, f32x4 (&acc
     }
 }
 
+template <typename ARGS>
+__device__ __forceinline__ int64_t x_rows(const ARGS& a) {
+    if constexpr (std::is_same<ARGS, ExpertArgs>::value) return a.x_rows;
+    else return 0;
+}
+
 template <typename CFG, bool OUT_BF16, int EPI>
 __global__ void __launch_bounds__(CFG::THREADS) __attribute__((amdgpu_waves_per_eu(CFG::WGS_PER_CU * CFG::NW / 4, CFG::WGS_PER_CU * CFG::NW / 4)))
 gdn_linear_kernel(typename EpiArgs<EPI>::type a) {
@@ -244,24 +272,43 @@ gdn_linear_kernel(typename EpiArgs<EPI>::type a) {
     // same cold rows of w on every k step; so a row comes from memory for one or two of them and from the memory-side cache for
     // the others (8192 x 8192 x 2048 with cold weights 226 -> 209 us; 197 with warm ones either way).
     const int xcd = (int)blockIdx.x & 7;
+    if constexpr (epi_expert(EPI)) {               // how many tiles there are the device knows: the grid is as many as there can be
+        a.tiles_m = *a.n_tiles;
+        a.per_xcd = (a.tiles_m * a.tiles_n + 7) / 8;
+        if (((int)blockIdx.x >> 3) >= a.per_xcd) return;
+    }
     int in_run = ((int)blockIdx.x >> 3) + xcd * a.per_xcd / 8;
     if (in_run >= a.per_xcd) in_run -= a.per_xcd;
     const int seq = xcd * a.per_xcd + in_run;
     if (seq >= a.tiles_m * a.tiles_n) return;      // (the grid is 8 per_xcd)
     const int grp = seq / (GROUP_M * a.tiles_n), in_grp = seq % (GROUP_M * a.tiles_n);
     const int grp_rows = min(a.tiles_m - grp * GROUP_M, GROUP_M);
-    const int tile_m = grp * GROUP_M + in_grp % grp_rows, tile_n = in_grp / grp_rows;
+    int tile_m = grp * GROUP_M + in_grp % grp_rows, tile_n = in_grp / grp_rows;
+    const int32_t* list = nullptr;
+    int64_t n_rows = a.T;
+    if constexpr (epi_expert(EPI)) {
+        // an expert's tiles are numbered down its rows first, so that those that share rows of w follow each other
+        const ExpertTile& entry = a.table[seq / a.tiles_n];
+        const int in_expert = seq - entry.first * a.tiles_n;
+        tile_m = in_expert % entry.tiles;
+        tile_n = in_expert / entry.tiles;
+        list = a.list + (int64_t)entry.expert * a.list_stride;
+        n_rows = entry.rows;
+        const int64_t skip = (int64_t)entry.expert * a.N * a.ldw * 2 * (epi_gated(EPI) ? 2 : 1);
+        a.w = reinterpret_cast<const char*>(a.w) + skip;
+        if (epi_gated(EPI)) a.w_up = reinterpret_cast<const char*>(a.w_up) + skip;
+    }
     const int64_t m0 = (int64_t)tile_m * BM;
-    constexpr int BNO = EPI == EPI_GATED ? BN / 2 : BN;         // outputs of a tile
+    constexpr int BNO = epi_gated(EPI) ? BN / 2 : BN;            // outputs of a tile
     const int n0 = tile_n * BNO;
-    const int64_t rows_x = a.T - m0 < BM ? a.T - m0 : BM;
+    const int64_t rows_x = n_rows - m0 < BM ? n_rows - m0 : BM;
     const int rows_w = a.N - n0 < BNO ? a.N - n0 : BNO;
-    const char* xb = reinterpret_cast<const char*>(a.x) + m0 * a.ldx * 2;
+    const char* xb = reinterpret_cast<const char*>(a.x) + (epi_expert(EPI) ? 0 : m0 * a.ldx * 2);
     const char* wb = reinterpret_cast<const char*>(a.w) + (int64_t)n0 * a.ldw * 2;
-    const int x_bytes = (int)((rows_x - 1) * a.ldx * 2 + (int64_t)a.K * 2), w_bytes = (int)((int64_t)(rows_w - 1) * a.ldw * 2 + (int64_t)a.K * 2);
+    const int x_bytes = (int)(((epi_expert(EPI) ? x_rows(a) : rows_x) - 1) * a.ldx * 2 + (int64_t)a.K * 2), w_bytes = (int)((int64_t)(rows_w - 1) * a.ldw * 2 + (int64_t)a.K * 2);
     const char* ub = wb;                                         // the second weight's rows
     int u_bytes = w_bytes;
-    if constexpr (EPI == EPI_GATED) {
+    if constexpr (epi_gated(EPI)) {
         ub = reinterpret_cast<const char*>(a.w_up) + (int64_t)n0 * a.ldw_up * 2;
         u_bytes = (int)((int64_t)(rows_w - 1) * a.ldw_up * 2 + (int64_t)a.K * 2);
     }
@@ -272,19 +319,21 @@ gdn_linear_kernel(typename EpiArgs<EPI>::type a) {
 #pragma unroll
     for (int j = 0; j < XL; ++j) {
         const int row = (BM / CFG::NW) * wave + RPL * j + ld_row;
-        xoff[j] = (int)(row * a.ldx * 2) + ((ld_pos ^ ((row / RL) % PP)) << 4);
+        int64_t at = row;
+        if constexpr (epi_expert(EPI)) at = list[min((int64_t)row, rows_x - 1) + m0] / a.div;      // (behind the last row its copies, for outputs that go nowhere)
+        xoff[j] = (int)(at * a.ldx * 2) + ((ld_pos ^ ((row / RL) % PP)) << 4);
     }
 #pragma unroll
     for (int j = 0; j < WL; ++j) {
         const int row = (BN / CFG::NW) * wave + RPL * j + ld_row;
-        if constexpr (EPI == EPI_GATED)
+        if constexpr (epi_gated(EPI))
             woff[j] = (int)(((row >> 5) * 16 + (row & 15)) * (up_load<CFG>(j, wave) ? a.ldw_up : a.ldw) * 2) + ((ld_pos ^ ((row / RL) % PP)) << 4);
         else
             woff[j] = (int)(row * a.ldw * 2) + ((ld_pos ^ ((row / RL) % PP)) << 4);
     }
     // one of the wave's loads of a stage; past the last k step (not live) it fetches nothing
     auto load = [&](int j, int stage, int k0, bool live) {
-        const bool up = EPI == EPI_GATED && j >= XL && up_load<CFG>(j - XL, wave);
+        const bool up = epi_gated(EPI) && j >= XL && up_load<CFG>(j - XL, wave);
         LinLoad<CFG>::one(j, smem, stage, k0, wave, xb, live ? x_bytes : 0, up ? ub : wb, live ? (up ? u_bytes : w_bytes) : 0, xoff, woff);
     };
     f32x4 acc[TJ][TI];           // [output tile][token tile]: lane lr = token, register e = output 4 g + e
@@ -418,7 +467,8 @@ gdn_linear_kernel(typename EpiArgs<EPI>::type a) {
     if constexpr (EPI != EPI_BIAS) {
         wait_vm<0>();
         __syncthreads();
-        act_epilogue<CFG, OUT_BF16, EPI>(a, acc, smem + wave * (CFG::SMEM / CFG::NW), m0 + CFG::WM * wm, n0 + CFG::WN / (EPI == EPI_GATED ? 2 : 1) * wn, lane);
+        act_epilogue<CFG, OUT_BF16, EPI>(a, acc, smem + wave * (CFG::SMEM / CFG::NW), m0 + CFG::WM * wm, n0 + CFG::WN / (epi_gated(EPI) ? 2 : 1) * wn, lane,
+                                         list, n_rows);
         return;
     } else {
     constexpr int ES = OUT_BF16 ? 2 : 4;
@@ -502,8 +552,8 @@ hipError_t launch_linear(typename EpiArgs<EPI>::type a, hipStream_t stream) {
     static hipError_t attr_err = hipFuncSetAttribute(reinterpret_cast<const void*>(&gdn_linear_kernel<CFG, OUT_BF16, EPI>),
                                                      hipFuncAttributeMaxDynamicSharedMemorySize, CFG::SMEM);
     if (attr_err != hipSuccess) return attr_err;
-    const int64_t tiles_m = (a.T + CFG::BM - 1) / CFG::BM;
-    constexpr int BNO = EPI == EPI_GATED ? CFG::BN / 2 : CFG::BN;
+    const int64_t tiles_m = epi_expert(EPI) ? a.T : (a.T + CFG::BM - 1) / CFG::BM;      // (the experts' T: how many tiles there can be)
+    constexpr int BNO = epi_gated(EPI) ? CFG::BN / 2 : CFG::BN;
     a.tiles_n = (a.N + BNO - 1) / BNO;
     a.tiles_m = (int32_t)tiles_m;
     a.per_xcd = (int32_t)((tiles_m * a.tiles_n + 7) / 8);
@@ -574,6 +624,28 @@ hipError_t launch_few(const LinearActArgs& a, bool bf, hipStream_t stream) {
         else hipLaunchKernelGGL((gdn_linear_few_kernel<RT, false, false>), grid, block, 0, stream, a);
     }
     return hipGetLastError();
+}
+
+int expert_tile_rows(int shape) { return shape == 2 ? LinBig8::BM : shape == 3 ? LinTiny::BM : LinSmall::BM; }
+
+template <typename CFG>
+hipError_t launch_expert_shape(const ExpertArgs& a, bool gated, hipStream_t stream) {
+    return gated ? launch_linear<CFG, true, EPI_EXPERT_GATED>(a, stream) : launch_linear<CFG, false, EPI_EXPERT>(a, stream);
+}
+hipError_t launch_expert_product(const ExpertProduct& p, int shape, hipStream_t stream) {
+    ExpertArgs a = {};
+    a.x = p.x; a.w = p.w; a.y = p.y;
+    a.ldx = p.ldx; a.ldw = a.ldw_up = p.K; a.ldy = p.N;
+    a.T = p.most_tiles; a.N = p.N; a.K = p.K;
+    a.w_up = p.gated ? static_cast<const char*>(p.w) + (int64_t)p.N * p.K * 2 : nullptr;
+    a.act = p.act; a.scale = 1.f;
+    a.list = p.list; a.table = p.table; a.n_tiles = p.n_tiles; a.weights = p.weights;
+    a.list_stride = p.list_stride; a.div = p.div; a.x_rows = p.x_rows;
+    switch (shape) {
+        case 2: return launch_expert_shape<LinBig8>(a, p.gated, stream);
+        case 3: return launch_expert_shape<LinTiny>(a, p.gated, stream);
+        default: return launch_expert_shape<LinSmall>(a, p.gated, stream);
+    }
 }
 
 std::atomic<int32_t> g_linear_shape{-1}, g_act_shape{-1};

@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 #include "gdn_moe.h"
@@ -26,7 +27,10 @@ int32_t check_shape(const gdn_moe_shape* s, int64_t T) {
 }
 
 // Byte offsets of the workspace's arrays.
-struct Layout { int64_t logits, ids, weights, counts, active, list, h, part, end; };
+struct Layout { int64_t logits, ids, weights, counts, active, list, table, h, part, end; };
+int64_t most_tiles(const gdn_moe_shape& s, int64_t T) {         // of 64 rows, the smallest: every expert may have one that is not full
+    return T * s.k / 64 + std::min<int64_t>(s.E, T * s.k);
+}
 Layout layout(const gdn_moe_shape& s, int64_t T) {
     Layout w;
     int64_t at = 0;
@@ -37,6 +41,7 @@ Layout layout(const gdn_moe_shape& s, int64_t T) {
     w.counts = take((s.E + 1) * 4);
     w.active = take(s.E * 4);
     w.list = take(T * s.E * 4);
+    w.table = take((most_tiles(s, T) + 1) * (int64_t)sizeof(linear::ExpertTile));
     w.h = take(T * s.k * s.F * 2);
     w.part = take(T * s.k * s.D * 4);
     w.end = at;
@@ -57,6 +62,28 @@ void launch_products(const MoeArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((moe_up_kernel<RT>), dim3((unsigned)(a.F / 16), most), dim3(64 * UP_WAVES), 0, stream, a);
     hipLaunchKernelGGL((moe_down_kernel<RT>), dim3((unsigned)(a.D / 16), most), dim3(64 * DOWN_WAVES), 0, stream, a);
 }
+
+// The products of many rows an expert, in the projections' tiles.
+hipError_t launch_tiles(MoeArgs& a, const gdn_moe_shape& s, int shape, hipStream_t stream) {
+    a.tile_rows = linear::expert_tile_rows(shape);
+    hipLaunchKernelGGL(moe_tiles_kernel, dim3(1), dim3(MAX_E), 0, stream, a);
+    const int64_t pairs = (int64_t)a.T * a.k;
+    linear::ExpertProduct p = {};
+    p.list = a.list; p.list_stride = a.T; p.table = a.table; p.n_tiles = a.n_tiles;
+    p.most_tiles = (int32_t)(pairs / a.tile_rows + std::min<int64_t>(a.E, pairs));
+    p.x = a.x; p.ldx = a.ldx; p.x_rows = a.T; p.div = a.k;
+    p.w = a.w_gate_up; p.gated = true; p.act = a.act;
+    p.y = a.h; p.N = a.F; p.K = a.D;
+    hipError_t e = linear::launch_expert_product(p, shape, stream);
+    if (e != hipSuccess) return e;
+    p.x = a.h; p.ldx = a.F; p.x_rows = (int32_t)pairs; p.div = 1;
+    p.w = a.w_down; p.gated = false; p.act = GDN_ACT_NONE; p.weights = a.weights;
+    p.y = a.part; p.N = a.D; p.K = a.F;
+    return linear::launch_expert_product(p, shape, stream);
+}
+
+constexpr int FEW = 6;
+std::atomic<int32_t> g_moe_shape{-1};
 
 }  // namespace moe
 }  // namespace gdn
@@ -107,6 +134,8 @@ extern "C" int32_t gdn_moe(const gdn_moe_shape* s, const void* x, int64_t ldx, c
     char* const ws = static_cast<char*>(workspace);
     a.logits = reinterpret_cast<float*>(ws + w.logits); a.ids = reinterpret_cast<int32_t*>(ws + w.ids); a.weights = reinterpret_cast<float*>(ws + w.weights);
     a.counts = reinterpret_cast<int32_t*>(ws + w.counts); a.active = reinterpret_cast<int32_t*>(ws + w.active); a.list = reinterpret_cast<int32_t*>(ws + w.list);
+    a.table = reinterpret_cast<linear::ExpertTile*>(ws + w.table) + 1;
+    a.n_tiles = reinterpret_cast<int32_t*>(ws + w.table);
     a.h = reinterpret_cast<uint16_t*>(ws + w.h); a.part = reinterpret_cast<float*>(ws + w.part);
     hipStream_t stream = static_cast<hipStream_t>(stream_);
 
@@ -120,9 +149,19 @@ extern "C" int32_t gdn_moe(const gdn_moe_shape* s, const void* x, int64_t ldx, c
     else if (per_lane <= 8) launch_route<8>(a, stream);
     else launch_route<16>(a, stream);
     const double rows = (double)T * s->k / s->E;                 // of an expert, by an even choice
-    if (rows <= 8) launch_products<1>(a, stream);
+    const bool tiles_fit = (T - 1) * ldx * 2 + D * 2 < INT32_MAX && T * s->k * F * 2 < INT32_MAX;      // the tiles' offsets of rows are 31 bits
+    const int forced = g_moe_shape.load();
+    const int shape = !tiles_fit ? FEW : forced >= 0 ? forced : FEW;
+    if (shape != FEW) {
+        const hipError_t e = launch_tiles(a, *s, shape, stream);
+        if (e != hipSuccess) return hip_err(e);
+    } else if (rows <= 8) launch_products<1>(a, stream);
     else if (rows <= 24) launch_products<2>(a, stream);
     else launch_products<4>(a, stream);
     hipLaunchKernelGGL(moe_sum_kernel, dim3((unsigned)((T * (D / 8) + 255) / 256)), dim3(256), 0, stream, a);
     return hip_err(hipGetLastError());
+}
+
+extern "C" int32_t gdn_moe_tune(int32_t shape) {
+    return g_moe_shape.exchange(shape == 0 || shape == 2 || shape == 3 || shape == FEW ? shape : -1);
 }

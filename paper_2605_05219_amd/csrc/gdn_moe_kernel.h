@@ -6,6 +6,7 @@
 
 #include "gdn_act.h"
 #include "gdn_few_kernel.h"
+#include "gdn_linear_tiles.h"
 #include "gdn_moe.h"
 
 namespace gdn {
@@ -39,6 +40,9 @@ struct MoeArgs {
     int32_t* list;                // [E][T]: an expert's choices (t k + j), in no order: no result depends on it
     uint16_t* h;                  // [T k][F]
     float* part;                  // [T k][D]: weighted outputs
+    linear::ExpertTile* table;    // tiles of tile_rows rows, an expert's one after the other; n_tiles: how many
+    int32_t* n_tiles;
+    int32_t tile_rows;
 };
 
 // ---- the router's sums.  A wave makes TE experts x TT tokens, its lanes along D, 8 elements at a time.  The sums decide a choice, so
@@ -220,6 +224,25 @@ __global__ void __launch_bounds__(256) moe_route_kernel(MoeArgs a) {
         a.list[(int64_t)id * a.T + at] = pair;
         if (at == 0) a.active[atomicAdd(a.counts + a.E, 1)] = id;
     }
+}
+
+// ---- the tile table, one workgroup: thread e has expert e's tiles, and those of the experts before it by a sum over the threads
+__global__ void __launch_bounds__(MAX_E) moe_tiles_kernel(MoeArgs a) {
+    __shared__ int32_t before[MAX_E / 64];
+    const int e = threadIdx.x, lane = e & 63, wave = e >> 6;
+    const int n = e < a.E ? a.counts[e] : 0, tiles = (n + a.tile_rows - 1) / a.tile_rows;
+    int sum = tiles;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const int other = __shfl_up(sum, m);
+        if (lane >= m) sum += other;
+    }
+    if (lane == 63) before[wave] = sum;
+    __syncthreads();
+    int first = sum - tiles;
+    for (int w = 0; w < wave; ++w) first += before[w];
+    for (int i = 0; i < tiles; ++i) a.table[first + i] = linear::ExpertTile{e, first, tiles, n};
+    if (e == MAX_E - 1) *a.n_tiles = first + tiles;
 }
 
 // ---- h = act(gate x) * (up x): a workgroup makes 16 of an expert's F for all of its rows, 16 RT at a time

@@ -9,7 +9,7 @@ from .rows import _dp, _here, _ld, _stream_ptr
 
 _i32, _i64, _vp, _f32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_float
 
-EXPORTS = ["gdn_moe_workspace_bytes", "gdn_moe"]
+EXPORTS = ["gdn_moe_workspace_bytes", "gdn_moe", "gdn_moe_tune"]
 
 _SCORES = {"softmax": 0, "sigmoid": 1}
 
@@ -37,6 +37,8 @@ def _lib():
         L.gdn_moe_workspace_bytes.argtypes = [sh, _i64]
         L.gdn_moe.restype = _i32
         L.gdn_moe.argtypes = [sh, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _vp]
+        L.gdn_moe_tune.restype = _i32
+        L.gdn_moe_tune.argtypes = [_i32]
         _ready = True
     return L
 
@@ -78,3 +80,8 @@ def gdn_moe(shape: gdn_moe_shape, x, w_router, choice_bias, w_gate_up, w_down, a
         raise ValueError("gdn_moe: a workspace without gaps")
     _check(_lib().gdn_moe(ctypes.byref(shape), x.data_ptr(), _ld(x), _dp(w_router), _dp(choice_bias), _dp(w_gate_up), _dp(w_down), _dp(add), _ld(add),
                           y.data_ptr(), _ld(y), _dp(ids), _dp(weights), T, _dp(workspace), room, _stream_ptr(stream, device)), "gdn_moe")
+
+
+def gdn_moe_tune(shape: int) -> int:
+    """Fixes the kernels of the experts' products (see include/gdn_moe.h) or returns the choice to the library (-1); returns the previous setting."""
+    return int(_lib().gdn_moe_tune(int(shape)))

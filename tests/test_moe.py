@@ -325,3 +325,25 @@ def test_another_stream_and_captured_graphs_with_one_workspace(T):
             call.run()
             torch.cuda.synchronize()
             assert torch.equal(got, call.y)
+
+
+@pytest.fixture
+def knob():
+    yield MO.gdn_moe_tune
+    MO.gdn_moe_tune(-1)
+
+
+def test_knob_round_trip(knob):
+    assert [knob(v) for v in (0, 2, 3, 6, 1, 9)] == [-1, 0, 2, 3, 6, -1]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [0, 2, 3, 6])
+@pytest.mark.parametrize("T,E,k,D,F,bias", [(1, 8, 2, 64, 64, None), (40, 60, 4, 320, 192, None), (700, 8, 3, 256, 320, None), (300, 20, 4, 128, 64, "one"), (90, 130, 10, 192, 128, None)])
+def test_every_kernel(knob, shape, T, E, k, D, F, bias):
+    """The tiles on experts of no row, of part of a tile and of several, and where all tokens take the same ones."""
+    if bias:
+        bias = np.zeros(E)
+        bias[[2, E - 1]] = 50
+    knob(shape)
+    Call(T, E, k, D, F, "gelu_tanh", bias=bias, add=True, pad=8, seed=T).run().check()
