@@ -29,7 +29,8 @@
  *   workspace    device, 16-byte aligned, >= gdn_moe_workspace_bytes(shape, T); nothing in it is kept from call to call, and
  *                two calls that may run at once need one each
  *   E is 1 .. 1024, k 1 .. min(E, 16), D and F multiples of 64 up to 32768; pointers 16-byte aligned (choice_bias, ids, weights 4), ld
- *   multiples of 8 and at least D.  T = 0 is legal and does nothing; T k is below 2^24.
+ *   multiples of 8 and at least D.  T = 0 is legal and does nothing.  T k is below 2^24, and x's rows (T ldx) and the experts' inner rows
+ *   (T k F) span less than 2^30 elements: longer batches go in parts.
  * Arithmetic: the router's sums in fp64; bf16 products with fp32 sums in the experts; act(gate) * up is rounded to bf16, as the next
  * product's operand; weighted and added in fp32; one rounding to y.
  * Errors: GDN_ERR_NULL, _ALIGN, _SHAPE (a size out of its range, an unknown type, activation or score, a routed_scale that is not finite, an ld
@@ -65,8 +66,8 @@ int32_t gdn_moe(const gdn_moe_shape *shape, const void *x, int64_t ldx, const vo
                 int32_t *ids, float *weights, int64_t T, void *workspace, int64_t workspace_bytes, void *stream);
 
 /*
- * Tuning knob, not a method step: fixes the kernels of the experts' products (0, 2, 3: the projections' tiles of 128 x 128, 256 x 256, 64 x 64, where their
- * 31-bit offsets reach; 6: the kernels of few rows; anything else: chosen per call, the default).  Process-wide; returns the previous setting (-1 = per call).
+ * Tuning knob, not a method step: fixes the tile of the experts' products (0, 2, 3: 128 x 128, 256 x 256, 64 x 64, as gdn_linear_tune; anything
+ * else: chosen per call, the default).  Every tile gives the same results.  Process-wide; returns the previous setting (-1 = per call).
  */
 int32_t gdn_moe_tune(int32_t shape);
 

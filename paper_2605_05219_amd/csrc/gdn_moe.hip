@@ -27,7 +27,7 @@ int32_t check_shape(const gdn_moe_shape* s, int64_t T) {
 }
 
 // Byte offsets of the workspace's arrays.
-struct Layout { int64_t logits, ids, weights, counts, active, list, table, h, part, end; };
+struct Layout { int64_t logits, ids, weights, counts, list, table, h, part, end; };
 int64_t most_tiles(const gdn_moe_shape& s, int64_t T) {         // of 64 rows, the smallest: every expert may have one that is not full
     return T * s.k / 64 + std::min<int64_t>(s.E, T * s.k);
 }
@@ -38,8 +38,7 @@ Layout layout(const gdn_moe_shape& s, int64_t T) {
     w.logits = take(T * s.E * 4);
     w.ids = take(T * s.k * 4);
     w.weights = take(T * s.k * 4);
-    w.counts = take((s.E + 1) * 4);
-    w.active = take(s.E * 4);
+    w.counts = take(s.E * 4);
     w.list = take(T * s.E * 4);
     w.table = take((most_tiles(s, T) + 1) * (int64_t)sizeof(linear::ExpertTile));
     w.h = take(T * s.k * s.F * 2);
@@ -48,25 +47,25 @@ Layout layout(const gdn_moe_shape& s, int64_t T) {
     return w;
 }
 
-template <int TT, int TE>
+template <int TT, int TE, int U>
 void launch_logits(const MoeArgs& a, hipStream_t stream) {
-    hipLaunchKernelGGL((moe_logits_kernel<TT, TE>), dim3((unsigned)((a.E + 4 * TE - 1) / (4 * TE)), (unsigned)((a.T + TT - 1) / TT)), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((moe_logits_kernel<TT, TE, U>), dim3((unsigned)((a.E + 4 * TE - 1) / (4 * TE)), (unsigned)((a.T + TT - 1) / TT)), dim3(256), 0, stream, a);
 }
 template <int P>
 void launch_route(const MoeArgs& a, hipStream_t stream) {
+    if constexpr (P <= 8) {                                      // (16 keys a lane do not fit the registers of 16 waves)
+        if (a.T <= FEW_TOKENS) {
+            hipLaunchKernelGGL((moe_route_few_kernel<P>), dim3(1), dim3(MAX_E), 0, stream, a);
+            return;
+        }
+    }
     hipLaunchKernelGGL((moe_route_kernel<P>), dim3((unsigned)((a.T + 3) / 4)), dim3(256), 0, stream, a);
-}
-template <int RT>
-void launch_products(const MoeArgs& a, hipStream_t stream) {
-    const unsigned most = (unsigned)std::min<int64_t>(a.E, (int64_t)a.T * a.k);
-    hipLaunchKernelGGL((moe_up_kernel<RT>), dim3((unsigned)(a.F / 16), most), dim3(64 * UP_WAVES), 0, stream, a);
-    hipLaunchKernelGGL((moe_down_kernel<RT>), dim3((unsigned)(a.D / 16), most), dim3(64 * DOWN_WAVES), 0, stream, a);
+    hipLaunchKernelGGL(moe_lists_kernel, dim3((unsigned)a.E), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL(moe_table_kernel, dim3(1), dim3(MAX_E), 0, stream, a);
 }
 
-// The products of many rows an expert, in the projections' tiles.
-hipError_t launch_tiles(MoeArgs& a, const gdn_moe_shape& s, int shape, hipStream_t stream) {
-    a.tile_rows = linear::expert_tile_rows(shape);
-    hipLaunchKernelGGL(moe_tiles_kernel, dim3(1), dim3(MAX_E), 0, stream, a);
+// The experts' products, in the projections' tiles.
+hipError_t launch_products(const MoeArgs& a, int shape, hipStream_t stream) {
     const int64_t pairs = (int64_t)a.T * a.k;
     linear::ExpertProduct p = {};
     p.list = a.list; p.list_stride = a.T; p.table = a.table; p.n_tiles = a.n_tiles;
@@ -82,8 +81,8 @@ hipError_t launch_tiles(MoeArgs& a, const gdn_moe_shape& s, int shape, hipStream
     return linear::launch_expert_product(p, shape, stream);
 }
 
-constexpr int FEW = 6;
 std::atomic<int32_t> g_moe_shape{-1};
+int choose_shape(double rows) { return rows <= 64 ? 3 : rows <= 160 ? 0 : 2; }      // rows of an expert, by an even choice
 
 }  // namespace moe
 }  // namespace gdn
@@ -109,6 +108,7 @@ extern "C" int32_t gdn_moe(const gdn_moe_shape* s, const void* x, int64_t ldx, c
     if (off_align(choice_bias, 4) || off_align(ids, 4) || off_align(weights, 4)) return GDN_ERR_ALIGN;
     if ((ldx & 7) || (ldy & 7) || (add && (ld_add & 7))) return GDN_ERR_ALIGN;
     if (ldx > most || ldy > most || (add && ld_add > most)) return GDN_ERR_COUNT;
+    if ((T - 1) * ldx * 2 + D * 2 > INT32_MAX || T * s->k * F * 2 > INT32_MAX) return GDN_ERR_COUNT;      // the tiles' offsets of rows are 31 bits
     const Layout w = layout(*s, T);
     if (!workspace || off_align(workspace, 16) || workspace_bytes < w.end) return GDN_ERR_WORKSPACE;
 
@@ -133,35 +133,30 @@ extern "C" int32_t gdn_moe(const gdn_moe_shape* s, const void* x, int64_t ldx, c
     a.act = s->act; a.score = s->score; a.normalise = s->normalise; a.router_f32 = s->router_dtype == GDN_F32; a.routed_scale = s->routed_scale;
     char* const ws = static_cast<char*>(workspace);
     a.logits = reinterpret_cast<float*>(ws + w.logits); a.ids = reinterpret_cast<int32_t*>(ws + w.ids); a.weights = reinterpret_cast<float*>(ws + w.weights);
-    a.counts = reinterpret_cast<int32_t*>(ws + w.counts); a.active = reinterpret_cast<int32_t*>(ws + w.active); a.list = reinterpret_cast<int32_t*>(ws + w.list);
+    a.counts = reinterpret_cast<int32_t*>(ws + w.counts); a.list = reinterpret_cast<int32_t*>(ws + w.list);
     a.table = reinterpret_cast<linear::ExpertTile*>(ws + w.table) + 1;
     a.n_tiles = reinterpret_cast<int32_t*>(ws + w.table);
     a.h = reinterpret_cast<uint16_t*>(ws + w.h); a.part = reinterpret_cast<float*>(ws + w.part);
     hipStream_t stream = static_cast<hipStream_t>(stream_);
 
-    if (T == 1) launch_logits<1, 2>(a, stream);
-    else if (T <= 16) launch_logits<2, 2>(a, stream);
-    else launch_logits<4, 4>(a, stream);
+    const int forced = g_moe_shape.load();
+    const int shape = forced >= 0 ? forced : choose_shape((double)T * s->k / s->E);
+    a.tile_rows = linear::expert_tile_rows(shape);
+    if (T == 1) launch_logits<1, 2, 4>(a, stream);
+    else if (T <= 64) launch_logits<2, 2, 2>(a, stream);
+    else launch_logits<4, 4, 1>(a, stream);
     const int per_lane = (s->E + 63) / 64;
     if (per_lane <= 1) launch_route<1>(a, stream);
     else if (per_lane <= 2) launch_route<2>(a, stream);
     else if (per_lane <= 4) launch_route<4>(a, stream);
     else if (per_lane <= 8) launch_route<8>(a, stream);
     else launch_route<16>(a, stream);
-    const double rows = (double)T * s->k / s->E;                 // of an expert, by an even choice
-    const bool tiles_fit = (T - 1) * ldx * 2 + D * 2 < INT32_MAX && T * s->k * F * 2 < INT32_MAX;      // the tiles' offsets of rows are 31 bits
-    const int forced = g_moe_shape.load();
-    const int shape = !tiles_fit ? FEW : forced >= 0 ? forced : FEW;
-    if (shape != FEW) {
-        const hipError_t e = launch_tiles(a, *s, shape, stream);
-        if (e != hipSuccess) return hip_err(e);
-    } else if (rows <= 8) launch_products<1>(a, stream);
-    else if (rows <= 24) launch_products<2>(a, stream);
-    else launch_products<4>(a, stream);
+    const hipError_t e = launch_products(a, shape, stream);
+    if (e != hipSuccess) return hip_err(e);
     hipLaunchKernelGGL(moe_sum_kernel, dim3((unsigned)((T * (D / 8) + 255) / 256)), dim3(256), 0, stream, a);
     return hip_err(hipGetLastError());
 }
 
 extern "C" int32_t gdn_moe_tune(int32_t shape) {
-    return g_moe_shape.exchange(shape == 0 || shape == 2 || shape == 3 || shape == FEW ? shape : -1);
+    return g_moe_shape.exchange(shape == 0 || shape == 2 || shape == 3 ? shape : -1);
 }

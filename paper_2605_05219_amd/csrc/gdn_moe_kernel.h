@@ -4,8 +4,6 @@
 
 #include <cstdint>
 
-#include "gdn_act.h"
-#include "gdn_few_kernel.h"
 #include "gdn_linear_tiles.h"
 #include "gdn_moe.h"
 
@@ -35,9 +33,8 @@ struct MoeArgs {
     float* logits;                // [T][E]
     int32_t* ids;                 // [T][k]: -1 for a choice that is left out
     float* weights;               // [T][k]
-    int32_t* counts;              // [E]: choices of an expert; then the number of experts that have any
-    int32_t* active;              // those experts, in no order
-    int32_t* list;                // [E][T]: an expert's choices (t k + j), in no order: no result depends on it
+    int32_t* counts;              // [E]: choices of an expert
+    int32_t* list;                // [E][T]: an expert's choices (t k + j)
     uint16_t* h;                  // [T k][F]
     float* part;                  // [T k][D]: weighted outputs
     linear::ExpertTile* table;    // tiles of tile_rows rows, an expert's one after the other; n_tiles: how many
@@ -45,14 +42,51 @@ struct MoeArgs {
     int32_t tile_rows;
 };
 
+// Sums and largest values over a wave, by moves within the vector unit (a shuffle goes through LDS: 64 of them are what a choice would wait for).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t moved(uint32_t v, uint32_t none) {
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, CTRL, ROWS, 0xf, false);
+}
+// Lane 63 gets op over all lanes: 1, 2, 4, 8 lanes up within a row of 16, then the last lane of a row to the next row, and of the first half to the second.
+template <typename T, typename OP>
+__device__ __forceinline__ T wave_up(T v, uint32_t none, OP op) {
+    v = op(v, __builtin_bit_cast(T, moved<0x111, 0xf>(__builtin_bit_cast(uint32_t, v), none)));
+    v = op(v, __builtin_bit_cast(T, moved<0x112, 0xf>(__builtin_bit_cast(uint32_t, v), none)));
+    v = op(v, __builtin_bit_cast(T, moved<0x114, 0xf>(__builtin_bit_cast(uint32_t, v), none)));
+    v = op(v, __builtin_bit_cast(T, moved<0x118, 0xf>(__builtin_bit_cast(uint32_t, v), none)));
+    v = op(v, __builtin_bit_cast(T, moved<0x142, 0xa>(__builtin_bit_cast(uint32_t, v), none)));
+    v = op(v, __builtin_bit_cast(T, moved<0x143, 0xc>(__builtin_bit_cast(uint32_t, v), none)));
+    return v;
+}
+template <typename T>
+__device__ __forceinline__ T from_lane(T v, int lane) { return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane)); }
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) { return from_lane(wave_up(v, 0u, [](uint32_t a, uint32_t b) { return max(a, b); }), 63); }
+__device__ __forceinline__ float wave_sum(float v) { return from_lane(wave_up(v, 0u, [](float a, float b) { return a + b; }), 63); }
+__device__ __forceinline__ float wave_fmax(float v) { return from_lane(wave_up(v, 0xff800000u, [](float a, float b) { return fmaxf(a, b); }), 63); }
+// The sum of fp64 values, on lane 63.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved_add(double v) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint64_t m = (uint64_t)moved<CTRL, ROWS>((uint32_t)(b >> 32), 0) << 32 | moved<CTRL, ROWS>((uint32_t)b, 0);
+    return v + __builtin_bit_cast(double, m);
+}
+__device__ __forceinline__ double wave_total(double v) {
+    v = moved_add<0x111, 0xf>(v);
+    v = moved_add<0x112, 0xf>(v);
+    v = moved_add<0x114, 0xf>(v);
+    v = moved_add<0x118, 0xf>(v);
+    v = moved_add<0x142, 0xa>(v);
+    return moved_add<0x143, 0xc>(v);
+}
+
 // ---- the router's sums.  A wave makes TE experts x TT tokens, its lanes along D, 8 elements at a time.  The sums decide a choice, so
 // that one in fp32, whose error changes with the order of its terms, would let the choice hang on how the work is split: in fp64 a sum of products of two bf16
 // numbers is exact but for terms 2^30 times smaller than the largest, whatever the order, and equal rows of w_router give equal keys.
-template <int TT, int TE>
+//
+// U pieces of a row are on their way at once: with one the time of a single token is the latency of D / 512 loads in a row.
+template <int TT, int TE, int U>
 __global__ void __launch_bounds__(256) moe_logits_kernel(MoeArgs a) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if (blockIdx.x == 0 && blockIdx.y == 0)                      // the counts of the launch behind this one
-        for (int e = threadIdx.x; e <= a.E; e += 256) a.counts[e] = 0;
     const int t0 = blockIdx.y * TT, e0 = (blockIdx.x * 4 + wave) * TE;
     if (e0 >= a.E) return;
     double acc[TE][TT];
@@ -60,49 +94,55 @@ __global__ void __launch_bounds__(256) moe_logits_kernel(MoeArgs a) {
     for (int i = 0; i < TE; ++i)
 #pragma unroll
         for (int j = 0; j < TT; ++j) acc[i][j] = 0.0;
-    for (int c = 8 * lane; c < a.D; c += 512) {
-        float xv[TT][8], wv[TE][8];
+    const uint16_t* xp[TT];
+    int64_t wp[TE];                                              // (rows past the end are the last one's: their sums go nowhere)
 #pragma unroll
-        for (int j = 0; j < TT; ++j) {
-            const u32x4 v = *reinterpret_cast<const u32x4*>(a.x + (int64_t)min(t0 + j, a.T - 1) * a.ldx + c);
+    for (int j = 0; j < TT; ++j) xp[j] = a.x + (int64_t)min(t0 + j, a.T - 1) * a.ldx;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) { xv[j][2 * q] = __uint_as_float(v[q] << 16); xv[j][2 * q + 1] = __uint_as_float(v[q] & 0xffff0000u); }
-        }
+    for (int i = 0; i < TE; ++i) wp[i] = (int64_t)min(e0 + i, a.E - 1) * a.D;
+    for (int c0 = 8 * lane; c0 < a.D; c0 += 512 * U) {
+        u32x4 xr[U][TT], wr[U][TE][2];
 #pragma unroll
-        for (int i = 0; i < TE; ++i) {
-            const int64_t at = (int64_t)min(e0 + i, a.E - 1) * a.D + c;
-            if (a.router_f32) {
-                const f32x4* p = reinterpret_cast<const f32x4*>(static_cast<const float*>(a.w_router) + at);
-                const f32x4 lo = p[0], hi = p[1];
+        for (int u = 0; u < U; ++u) {
+            const int c = c0 + 512 * u;
+            const bool in = c < a.D;
 #pragma unroll
-                for (int q = 0; q < 4; ++q) { wv[i][q] = lo[q]; wv[i][q + 4] = hi[q]; }
-            } else {
-                const u32x4 v = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.w_router) + at);
+            for (int j = 0; j < TT; ++j) xr[u][j] = in ? *reinterpret_cast<const u32x4*>(xp[j] + c) : u32x4{0, 0, 0, 0};
 #pragma unroll
-                for (int q = 0; q < 4; ++q) { wv[i][2 * q] = __uint_as_float(v[q] << 16); wv[i][2 * q + 1] = __uint_as_float(v[q] & 0xffff0000u); }
+            for (int i = 0; i < TE; ++i) {
+                wr[u][i][0] = wr[u][i][1] = u32x4{0, 0, 0, 0};
+                if (!in) continue;
+                if (a.router_f32) {
+                    const u32x4* p = reinterpret_cast<const u32x4*>(static_cast<const float*>(a.w_router) + wp[i] + c);
+                    wr[u][i][0] = p[0];
+                    wr[u][i][1] = p[1];
+                } else {
+                    wr[u][i][0] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.w_router) + wp[i] + c);
+                }
             }
         }
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            double xd[TT], wd[TE];
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int j = 0; j < TT; ++j) xd[j] = (double)xv[j][q];
+            for (int q = 0; q < 8; ++q) {
+                double xd[TT], wd[TE];
 #pragma unroll
-            for (int i = 0; i < TE; ++i) wd[i] = (double)wv[i][q];
+                for (int j = 0; j < TT; ++j) xd[j] = (double)__uint_as_float(q & 1 ? xr[u][j][q / 2] & 0xffff0000u : xr[u][j][q / 2] << 16);
 #pragma unroll
-            for (int i = 0; i < TE; ++i)
+                for (int i = 0; i < TE; ++i)
+                    wd[i] = (double)__uint_as_float(a.router_f32 ? wr[u][i][q / 4][q % 4] : q & 1 ? wr[u][i][0][q / 2] & 0xffff0000u : wr[u][i][0][q / 2] << 16);
 #pragma unroll
-                for (int j = 0; j < TT; ++j) acc[i][j] = fma(wd[i], xd[j], acc[i][j]);
-        }
+                for (int i = 0; i < TE; ++i)
+#pragma unroll
+                    for (int j = 0; j < TT; ++j) acc[i][j] = fma(wd[i], xd[j], acc[i][j]);
+            }
     }
 #pragma unroll
     for (int i = 0; i < TE; ++i)
 #pragma unroll
         for (int j = 0; j < TT; ++j) {
-            double v = acc[i][j];
-#pragma unroll
-            for (int m = 32; m > 0; m >>= 1) v += __shfl_xor(v, m);
-            if (lane == 0 && e0 + i < a.E && t0 + j < a.T) a.logits[(int64_t)(t0 + j) * a.E + e0 + i] = (float)v;
+            const double v = wave_total(acc[i][j]);
+            if (lane == 63 && e0 + i < a.E && t0 + j < a.T) a.logits[(int64_t)(t0 + j) * a.E + e0 + i] = (float)v;
         }
 }
 
@@ -114,22 +154,6 @@ __device__ __forceinline__ uint32_t key_order(float key) {
     const uint32_t b = __float_as_uint(key + 0.f);               // (-0 and 0 are equal)
     return (b & 0x80000000u ? ~b : b | 0x80000000u);
 }
-__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
-#pragma unroll
-    for (int m = 32; m > 0; m >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, m));
-    return v;
-}
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int m = 32; m > 0; m >>= 1) v += __shfl_xor(v, m);
-    return v;
-}
-__device__ __forceinline__ float wave_fmax(float v) {
-#pragma unroll
-    for (int m = 32; m > 0; m >>= 1) v = fmaxf(v, __shfl_xor(v, m));
-    return v;
-}
-
 // The choices of one token: lane j < k gets the j-th one's expert (-1 where there is none) and weight.
 template <int P>
 __device__ __forceinline__ void choose(const MoeArgs& a, int t, int lane, int& my_id, float& my_weight) {
@@ -184,8 +208,8 @@ __device__ __forceinline__ void choose(const MoeArgs& a, int t, int lane, int& m
                 at_l = l[i];
                 if (lane == first) key[i] = 0;
             }
-        at = __shfl(at, first);
-        at_l = __shfl(at_l, first);
+        at = from_lane(at, first);
+        at_l = from_lane(at_l, first);
         if (lane == j) { my_id = at; my_l = at_l; }
     }
     float p = 0.f;
@@ -204,11 +228,9 @@ __device__ __forceinline__ void choose(const MoeArgs& a, int t, int lane, int& m
     my_weight = have ? p * a.routed_scale : 0.f;
 }
 
+// The choices of a token to memory; the id that is kept is -1 for a choice of weight zero (a NaN weight is in).
 template <int P>
-__global__ void __launch_bounds__(256) moe_route_kernel(MoeArgs a) {
-    const int lane = threadIdx.x & 63;
-    const int t = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (t >= a.T) return;
+__device__ __forceinline__ void choose_and_keep(const MoeArgs& a, int t, int lane, int32_t* kept) {
     int id;
     float p;
     choose<P>(a, t, lane, id, p);
@@ -216,21 +238,16 @@ __global__ void __launch_bounds__(256) moe_route_kernel(MoeArgs a) {
     const int pair = t * a.k + lane;
     if (a.out_ids) a.out_ids[pair] = id;
     if (a.out_weights) a.out_weights[pair] = p;
-    const bool in = id >= 0 && p != 0.f;                         // (a NaN weight is in)
-    a.ids[pair] = in ? id : -1;
+    const int in = p != 0.f ? id : -1;
+    a.ids[pair] = in;
     a.weights[pair] = p;
-    if (in) {
-        const int at = atomicAdd(a.counts + id, 1);
-        a.list[(int64_t)id * a.T + at] = pair;
-        if (at == 0) a.active[atomicAdd(a.counts + a.E, 1)] = id;
-    }
+    if (kept) kept[pair] = in;
 }
 
-// ---- the tile table, one workgroup: thread e has expert e's tiles, and those of the experts before it by a sum over the threads
-__global__ void __launch_bounds__(MAX_E) moe_tiles_kernel(MoeArgs a) {
-    __shared__ int32_t before[MAX_E / 64];
+// The tile table, by a workgroup of MAX_E threads: thread e has expert e's tiles, and those of the experts before it by a sum over the threads.
+__device__ __forceinline__ void make_table(const MoeArgs& a, int n, int32_t* before) {
     const int e = threadIdx.x, lane = e & 63, wave = e >> 6;
-    const int n = e < a.E ? a.counts[e] : 0, tiles = (n + a.tile_rows - 1) / a.tile_rows;
+    const int tiles = (n + a.tile_rows - 1) / a.tile_rows;
     int sum = tiles;
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) {
@@ -245,79 +262,68 @@ __global__ void __launch_bounds__(MAX_E) moe_tiles_kernel(MoeArgs a) {
     if (e == MAX_E - 1) *a.n_tiles = first + tiles;
 }
 
-// ---- h = act(gate x) * (up x): a workgroup makes 16 of an expert's F for all of its rows, 16 RT at a time
-constexpr int UP_WAVES = 8;
-template <int RT>
-__global__ void __launch_bounds__(64 * UP_WAVES) moe_up_kernel(MoeArgs a) {
-    constexpr int U = RT == 4 ? 2 : 4;
-    __shared__ f32x4 sums[UP_WAVES * 2 * RT * 16 * 4];
-    __shared__ int32_t rows[RT * 16];
-    if ((int)blockIdx.y >= a.counts[a.E]) return;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int lr = lane & 15, g = lane >> 4;
-    const int e = a.active[blockIdx.y], n = a.counts[e], f0 = blockIdx.x * 16;
-    const int32_t* list = a.list + (int64_t)e * a.T;
-    const uint16_t* wp[2];
-    wp[0] = a.w_gate_up + ((int64_t)e * 2 * a.F + f0 + lr) * a.D + 8 * g;
-    wp[1] = wp[0] + (int64_t)a.F * a.D;
-    for (int r0 = 0; r0 < n; r0 += 16 * RT) {
-        if (threadIdx.x < RT * 16) rows[threadIdx.x] = list[min(r0 + (int)threadIdx.x, n - 1)];
-        __syncthreads();
-        const uint16_t* xp[RT];
-        f32x4 acc[2][RT];
-#pragma unroll
-        for (int j = 0; j < RT; ++j) {
-            xp[j] = a.x + (int64_t)(rows[16 * j + lr] / a.k) * a.ldx + 8 * g;
-            acc[0][j] = acc[1][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        }
-        few::accumulate<2, RT, UP_WAVES, U>(acc, wp, xp, a.D / few::STEP, wave);
-        few::put_sums<2, RT, UP_WAVES>(acc, sums, wave, lane);
-        __syncthreads();
-        for (int i = threadIdx.x; i < RT * 16 * 4; i += 64 * UP_WAVES) {
-            const int row = i >> 2, piece = i & 3;
-            if (r0 + row >= n) continue;
-            f32x4 v = activate(a.act, few::get_sum<2, RT, UP_WAVES>(sums, 0, row, piece));
-            v *= few::get_sum<2, RT, UP_WAVES>(sums, 1, row, piece);
-            *reinterpret_cast<bf16x4*>(a.h + (int64_t)rows[row] * a.F + f0 + 4 * piece) = __builtin_convertvector(v, bf16x4);
-        }
-        __syncthreads();
+// Few tokens: choices, lists and tile table in one workgroup, a wave to a token.  An expert's list is in no order there: a row of a product
+// is the same whatever rows stand beside it.
+constexpr int FEW_TOKENS = 64;
+template <int P>
+__global__ void __launch_bounds__(MAX_E) moe_route_few_kernel(MoeArgs a) {
+    __shared__ int32_t kept[FEW_TOKENS * MAX_K], counts[MAX_E], before[MAX_E / 64];
+    const int tid = threadIdx.x;
+    counts[tid] = 0;
+    for (int t = tid >> 6; t < a.T; t += MAX_E / 64) choose_and_keep<P>(a, t, tid & 63, kept);
+    __syncthreads();
+    if (tid < a.T * a.k) {
+        const int e = kept[tid];
+        if (e >= 0) a.list[(int64_t)e * a.T + atomicAdd(counts + e, 1)] = tid;
     }
+    __syncthreads();
+    make_table(a, counts[tid], before);
 }
 
-// ---- part = weight * (w_down h): a workgroup makes 16 of D for all of an expert's rows
-constexpr int DOWN_WAVES = 4;
-template <int RT>
-__global__ void __launch_bounds__(64 * DOWN_WAVES) moe_down_kernel(MoeArgs a) {
-    constexpr int U = RT == 4 ? 2 : 4;
-    __shared__ f32x4 sums[DOWN_WAVES * RT * 16 * 4];
-    __shared__ int32_t rows[RT * 16];
-    if ((int)blockIdx.y >= a.counts[a.E]) return;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int lr = lane & 15, g = lane >> 4;
-    const int e = a.active[blockIdx.y], n = a.counts[e], d0 = blockIdx.x * 16;
-    const int32_t* list = a.list + (int64_t)e * a.T;
-    const uint16_t* wp[1] = {a.w_down + ((int64_t)e * a.D + d0 + lr) * a.F + 8 * g};
-    for (int r0 = 0; r0 < n; r0 += 16 * RT) {
-        if (threadIdx.x < RT * 16) rows[threadIdx.x] = list[min(r0 + (int)threadIdx.x, n - 1)];
-        __syncthreads();
-        const uint16_t* xp[RT];
-        f32x4 acc[1][RT];
+// More: the choices, a wave to a token ...
+template <int P>
+__global__ void __launch_bounds__(256) moe_route_kernel(MoeArgs a) {
+    const int t = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (t < a.T) choose_and_keep<P>(a, t, threadIdx.x & 63, nullptr);
+}
+// ... the lists, a workgroup to an expert, which looks through all choices (a counter that the tokens of all workgroups add to is
+// slower: 12288 choices of 64 experts 37 us) ...
+__global__ void __launch_bounds__(256) moe_lists_kernel(MoeArgs a) {
+    __shared__ int32_t found[4];
+    const int e = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pairs = a.T * a.k;
+    int32_t* list = a.list + (int64_t)e * a.T;
+    int n = 0;
+    for (int p0 = 0; p0 < pairs; p0 += 1024) {                   // four to a thread
+        const int p = p0 + 4 * threadIdx.x;
+        int id[4], mine = 0;
 #pragma unroll
-        for (int j = 0; j < RT; ++j) {
-            xp[j] = a.h + (int64_t)rows[16 * j + lr] * a.F + 8 * g;
-            acc[0][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < 4; ++i) {
+            id[i] = p + i < pairs ? a.ids[p + i] : -1;
+            mine += id[i] == e;
         }
-        few::accumulate<1, RT, DOWN_WAVES, U>(acc, wp, xp, a.F / few::STEP, wave);
-        few::put_sums<1, RT, DOWN_WAVES>(acc, sums, wave, lane);
-        __syncthreads();
-        for (int i = threadIdx.x; i < RT * 16 * 4; i += 64 * DOWN_WAVES) {
-            const int row = i >> 2, piece = i & 3;
-            if (r0 + row >= n) continue;
-            *reinterpret_cast<f32x4*>(a.part + (int64_t)rows[row] * a.D + d0 + 4 * piece) =
-                a.weights[rows[row]] * few::get_sum<1, RT, DOWN_WAVES>(sums, 0, row, piece);
+        int sum = mine;
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) {
+            const int other = __shfl_up(sum, m);
+            if (lane >= m) sum += other;
         }
         __syncthreads();
+        if (lane == 63) found[wave] = sum;
+        __syncthreads();
+        int at = n + sum - mine;
+        for (int w = 0; w < wave; ++w) at += found[w];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (id[i] == e) list[at++] = p + i;
+        n += found[0] + found[1] + found[2] + found[3];
     }
+    if (threadIdx.x == 0) a.counts[e] = n;
+}
+// ... and the tile table.
+__global__ void __launch_bounds__(MAX_E) moe_table_kernel(MoeArgs a) {
+    __shared__ int32_t before[MAX_E / 64];
+    const int e = threadIdx.x;
+    make_table(a, e < a.E ? a.counts[e] : 0, before);
 }
 
 // ---- y = add + the choices' parts, in the order of their keys; a thread owns 8 adjacent channels
@@ -332,13 +338,26 @@ __global__ void __launch_bounds__(256) moe_sum_kernel(MoeArgs a) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) { v[2 * q] = __uint_as_float(r[q] << 16); v[2 * q + 1] = __uint_as_float(r[q] & 0xffff0000u); }
     }
-    for (int j = 0; j < a.k; ++j) {
-        const int64_t pair = (int64_t)t * a.k + j;
-        if (a.ids[pair] < 0) continue;
-        const f32x4* p = reinterpret_cast<const f32x4*>(a.part + pair * a.D + c);
-        const f32x4 lo = p[0], hi = p[1];
+    const int32_t* ids = a.ids + (int64_t)t * a.k;
+    const float* part = a.part + (int64_t)t * a.k * a.D + c;
+    int j = 0;
+    for (; j + 1 < a.k; j += 2) {                                // (two at once; the part of a choice that is left out holds anything)
+        f32x4 p[2][2];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) { v[q] += lo[q]; v[q + 4] += hi[q]; }
+        for (int i = 0; i < 2; ++i) {
+            p[i][0] = reinterpret_cast<const f32x4*>(part + (int64_t)(j + i) * a.D)[0];
+            p[i][1] = reinterpret_cast<const f32x4*>(part + (int64_t)(j + i) * a.D)[1];
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (ids[j + i] >= 0)
+#pragma unroll
+                for (int q = 0; q < 8; ++q) v[q] += p[i][q / 4][q % 4];
+    }
+    if (j < a.k && ids[j] >= 0) {
+        const f32x4* p = reinterpret_cast<const f32x4*>(part + (int64_t)j * a.D);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] += p[q / 4][q % 4];
     }
     bf16x8 o;
 #pragma unroll
