@@ -1,10 +1,10 @@
-// Products of a few rows with a weight matrix: the part that the projections' and the experts' kernels share.
+// A product of a few rows with a weight matrix, for the projections' epilogues.
 //
-// With at most 64 rows such a product does at most 64 flops for every weight element's 2 bytes: it is bound by how fast the
-// weights come from memory, not by the matrix cores.  So nothing is staged: a wave's lanes load weight rows straight into the
-// left operand's registers of v_mfma_f32_16x16x32_bf16 (lane: row lane % 16, k 8 (lane / 16) .. + 7: 16 bytes), x rows, which the
-// caches hold, into the right one's, and the waves of a workgroup share the k range out step by step, a step of 64 (a whole
-// 128-byte line of every row) to a wave, U steps on their way at once.  Their sums meet in LDS, in the order of the waves.
+// With a few rows such a product does few flops for every weight element's 2 bytes: it is bound by how fast the weights come from
+// memory, and with the few workgroups that a narrow output gives, by how much of them each has on its way.  The tiles of gdn_linear.hip
+// walk k one step after the other, with a barrier each (0.13 to 0.2 us a step: 96 steps of a 2048 x 6144 weight take 17 us at best); here the waves of a
+// workgroup share the steps out instead.  A wave has a ring of its own in LDS, which 16-byte loads to LDS fill S steps of 64 ahead, and no other wave
+// reads it: there is no barrier until the waves' sums meet, in LDS, in the order of the waves.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -17,56 +17,106 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int STEP = 64;                          // k of a step
+constexpr int STEP = 64;                          // k of a step: a row of 128 bytes
 
-// acc[i][j] += (weight tile i) x (row tile j) over the wave's share of `steps` k steps.  wp[i], xp[j]: the lane's row of the tile at k = 8 (lane / 16).
-// Result: lane lr = lane % 16 holds row lr of tile j, register e output 4 (lane / 16) + e of tile i.
-template <int NT, int RT, int WAVES, int U>
-__device__ __forceinline__ void accumulate(f32x4 (&acc)[NT][RT], const uint16_t* const (&wp)[NT], const uint16_t* const (&xp)[RT], int steps, int wave) {
-    u32x4 w[U][2][NT], x[U][2][RT];
-    for (int s0 = wave; s0 < steps; s0 += WAVES * U) {
+// Rows of a matrix: where they begin, the bytes up to the last one's end (what lies behind arrives as zeros), the bytes from one to the next.
+struct Part {
+    const char* at;
+    int bytes, pitch;
+};
+
+// RT: tiles of 16 rows of x; WR: weight rows of a workgroup (8, 16 or 32); WAVES waves; S steps of a wave on their way
+template <int RT_, int WR_, int WAVES_, int S_>
+struct Few {
+    static constexpr int RT = RT_, WR = WR_, WAVES = WAVES_, S = S_, ROWS = 16 * RT;
+    static constexpr int CT = (WR + 15) / 16;     // tiles of 16 weight rows (of 8 rows the tile's other half is what lies behind them in LDS, for sums that go nowhere)
+    static constexpr int X_LOADS = ROWS / 8, W_LOADS = WR / 8, LOADS = X_LOADS + W_LOADS;        // of 1 KiB, 8 rows each, per step
+    static constexpr int HALF = (W_LOADS + 1) / 2;                                               // the first part's loads of the weights
+    static constexpr int STAGE = LOADS * 1024, RING = S * STAGE;
+    static constexpr int SUMS = CT * ROWS * 64;   // bytes of a wave's sums: [tile][row][16 outputs]
+    static constexpr int SMEM = WAVES * (RING > SUMS ? RING : SUMS) + (WR == 8 ? 1024 : 0);
+    static constexpr int AHEAD = (S - 1) * LOADS; // loads that may be on their way when a step's have landed
+    static_assert(SMEM <= 160 * 1024 && AHEAD < 64, "ring");
+
+    // One step's loads.  They go out for every step slot, also behind the last one (not live, an empty descriptor: nothing is fetched), so that the
+    // number on their way, and with it the wait, is always the same.
+    static __device__ __forceinline__ void fetch(char* to, int k, const Part& w0, const Part& w1, const Part& x, bool live, const int* xoff, const int* woff) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int s = s0 + u * WAVES;
-            if (s >= steps) break;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                for (int i = 0; i < NT; ++i) w[u][h][i] = *reinterpret_cast<const u32x4*>(wp[i] + s * STEP + 32 * h);
-#pragma unroll
-                for (int j = 0; j < RT; ++j) x[u][h][j] = *reinterpret_cast<const u32x4*>(xp[j] + s * STEP + 32 * h);
-            }
+        for (int j = 0; j < W_LOADS; ++j) {
+            const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(j >= HALF ? w1.at : w0.at), 0, live ? (j >= HALF ? w1.bytes : w0.bytes) : 0, 0x00020000);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(to + (X_LOADS + j) * 1024), 16, woff[j], k, 0, 0);
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (s0 + u * WAVES >= steps) break;
+        for (int j = 0; j < X_LOADS; ++j) {
+            const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(x.at), 0, live ? x.bytes : 0, 0x00020000);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(to + j * 1024), 16, xoff[j], k, 0, 0);
+        }
+    }
+
+    // The sums of a wave's steps over the weight rows, w0's (8 HALF) and then w1's, and rows x.  acc[i RT + j]: lane lr = lane % 16 holds row lr of row tile j,
+    // register e weight row 16 i + 4 (lane / 16) + e.  The steps are walked from `first` on: workgroups that begin at the same k of rows whose pitch is a
+    // power of two ask the same few memory channels (8192 x 8192, 16 rows: 34 us, 26 with 5 steps from one workgroup's beginning to the next's).
+    static __device__ __forceinline__ void sums_of(f32x4* acc, const Part& w0, const Part& w1, const Part& x, int steps, int first, char* ring, int wave, int lane) {
+        auto k_of = [&](int step) { const int s = step + first; return (s >= steps ? s - steps : s) * STEP * 2; };
+        const int row = lane >> 3, pos = lane & 7;    // of a load: lane i lands at row i / 8, piece i % 8
+        int xoff[X_LOADS], woff[W_LOADS];
+        // piece p of row r lies at p ^ (r / 2) % 8: 16 rows' pieces of one k then spread over the banks
+#pragma unroll
+        for (int j = 0; j < X_LOADS; ++j) xoff[j] = (8 * j + row) * x.pitch + ((pos ^ (((8 * j + row) >> 1) & 7)) << 4);
+#pragma unroll
+        for (int j = 0; j < W_LOADS; ++j)
+            woff[j] = (8 * (j >= HALF ? j - HALF : j) + row) * (j >= HALF ? w1.pitch : w0.pitch) + ((pos ^ (((8 * j + row) >> 1) & 7)) << 4);
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            const int step = wave + s * WAVES;
+            fetch(ring + s * STAGE, step < steps ? k_of(step) : 0, w0, w1, x, step < steps, xoff, woff);
+        }
+        const int lr = lane & 15, g = lane >> 4, sw = lr >> 1;
+        int slot = 0;
+        for (int step = wave; step < steps; step += WAVES) {
+            __builtin_amdgcn_s_waitcnt(((AHEAD & 0x30) << 10) | (AHEAD & 0xF) | 0x0F70);      // this step's loads have landed (vmcnt)
+            asm volatile("" ::: "memory");
+            const char* at = ring + slot * STAGE + lr * 128;
+            u32x4 wf[2][CT], xf[2][RT];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int piece = ((4 * h + g) ^ sw) << 4;
+#pragma unroll
+                for (int i = 0; i < CT; ++i) wf[h][i] = *reinterpret_cast<const u32x4*>(at + X_LOADS * 1024 + i * 2048 + piece);
+#pragma unroll
+                for (int j = 0; j < RT; ++j) xf[h][j] = *reinterpret_cast<const u32x4*>(at + j * 2048 + piece);
+            }
+            __builtin_amdgcn_s_waitcnt(0xC07F);       // read (lgkmcnt(0)): the slot is free
+            asm volatile("" ::: "memory");
+            const int next = step + S * WAVES;
+            fetch(ring + slot * STAGE, next < steps ? k_of(next) : 0, w0, w1, x, next < steps, xoff, woff);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int i = 0; i < NT; ++i)
+                for (int i = 0; i < CT; ++i)
 #pragma unroll
                     for (int j = 0; j < RT; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[u][h][i]), __builtin_bit_cast(bf16x8, x[u][h][j]),
-                                                                            acc[i][j], 0, 0, 0);
+                        acc[i * RT + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wf[h][i]), __builtin_bit_cast(bf16x8, xf[h][j]),
+                                                                                  acc[i * RT + j], 0, 0, 0);
+            slot = slot + 1 == S ? 0 : slot + 1;
         }
     }
-}
 
-// The waves' sums to LDS: [wave][tile i][row of all row tiles][16 outputs], 16-byte pieces.
-template <int NT, int RT, int WAVES>
-__device__ __forceinline__ void put_sums(f32x4 (&acc)[NT][RT], f32x4* sums, int wave, int lane) {
+    // The waves' sums to LDS (behind a barrier of the caller's: the rings have been read), and one of them.
+    static __device__ __forceinline__ void put_sums(const f32x4* acc, f32x4* sums, int wave, int lane) {
 #pragma unroll
-    for (int i = 0; i < NT; ++i)
+        for (int i = 0; i < CT; ++i)
 #pragma unroll
-        for (int j = 0; j < RT; ++j) sums[((wave * NT + i) * RT * 16 + j * 16 + (lane & 15)) * 4 + (lane >> 4)] = acc[i][j];
-}
-template <int NT, int RT, int WAVES>
-__device__ __forceinline__ f32x4 get_sum(const f32x4* sums, int tile, int row, int piece) {
-    f32x4 v = sums[(tile * RT * 16 + row) * 4 + piece];
+            for (int j = 0; j < RT; ++j) sums[((wave * CT + i) * ROWS + j * 16 + (lane & 15)) * 4 + (lane >> 4)] = acc[i * RT + j];
+    }
+    static __device__ __forceinline__ f32x4 get_sum(const f32x4* sums, int row, int quad) {      // weight rows 4 quad .. + 3
+        const int at = ((quad >> 2) * ROWS + row) * 4 + (quad & 3);
+        f32x4 v = sums[at];
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) v += sums[((w * NT + tile) * RT * 16 + row) * 4 + piece];
-    return v;
-}
+        for (int w = 1; w < WAVES; ++w) v += sums[w * CT * ROWS * 4 + at];
+        return v;
+    }
+};
 
 }  // namespace few
 }  // namespace gdn

@@ -561,37 +561,40 @@ hipError_t launch_linear(typename EpiArgs<EPI>::type a, hipStream_t stream) {
     return hipGetLastError();
 }
 
-// ---- few rows (gdn_few_kernel.h): a workgroup of eight waves makes 16 outputs (of two products with a second weight) of up to 16 RT rows
-constexpr int FEW_WAVES = 8;
-
-template <int RT, bool OUT_BF16, bool GATED>
-__global__ void __launch_bounds__(64 * FEW_WAVES) gdn_linear_few_kernel(LinearActArgs a) {
-    constexpr int NT = GATED ? 2 : 1, U = RT == 4 ? 2 : 4;
-    __shared__ f32x4 sums[FEW_WAVES * NT * RT * 16 * 4];
+// ---- few rows (gdn_few_kernel.h): a workgroup makes WR outputs of up to 16 RT rows, or WR / 2 of two products
+template <typename C, bool OUT_BF16, bool GATED>
+__global__ void __launch_bounds__(64 * C::WAVES) gdn_linear_few_kernel(LinearActArgs a) {
+    extern __shared__ __align__(16) char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int lr = lane & 15, g = lane >> 4;
-    const int n0 = (int)blockIdx.x * 16;
-    // rows past the end are read as the last one: their sums are not used
-    const int64_t wrow = min(n0 + lr, a.N - 1);
-    const uint16_t* wp[NT];
-    const uint16_t* xp[RT];
-    wp[0] = static_cast<const uint16_t*>(a.w) + wrow * a.ldw + 8 * g;
-    if (GATED) wp[NT - 1] = static_cast<const uint16_t*>(a.w_up) + wrow * a.ldw_up + 8 * g;
+    // workgroups are dealt to the 8 XCDs in turn: the row tiles of the same outputs follow each other on one of them, whose L2 then has the weights
+    const int seq = (int)blockIdx.x / (8 * a.tiles_m), in = (int)blockIdx.x % (8 * a.tiles_m);
+    const int tile_n = seq * 8 + (in & 7), tile_m = in >> 3;
+    if (tile_n >= a.tiles_n) return;                             // (the grid is whole eights)
+    constexpr int OUTS = GATED ? C::WR / 2 : C::WR;
+    const int n0 = tile_n * OUTS, m0 = tile_m * C::ROWS;
+    const int rows_x = min((int)a.T - m0, C::ROWS);
+    auto weights = [&](const void* w, int64_t ld, int first) {
+        const int rows = a.N - first;
+        return few::Part{static_cast<const char*>(w) + (int64_t)min(first, a.N - 1) * ld * 2,
+                         rows > 0 ? (int)((int64_t)(min(rows, C::WR) - 1) * ld * 2 + (int64_t)a.K * 2) : 0, (int)(ld * 2)};
+    };
+    const few::Part x = {static_cast<const char*>(a.x) + (int64_t)m0 * a.ldx * 2, (int)((int64_t)(rows_x - 1) * a.ldx * 2 + (int64_t)a.K * 2), (int)(a.ldx * 2)};
+    f32x4 acc[C::CT * C::RT];
 #pragma unroll
-    for (int j = 0; j < RT; ++j) xp[j] = static_cast<const uint16_t*>(a.x) + (int64_t)min(16 * j + lr, (int)a.T - 1) * a.ldx + 8 * g;
-    f32x4 acc[NT][RT];
-#pragma unroll
-    for (int i = 0; i < NT; ++i)
-#pragma unroll
-        for (int j = 0; j < RT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    few::accumulate<NT, RT, FEW_WAVES, U>(acc, wp, xp, a.K / few::STEP, wave);
-    few::put_sums<NT, RT, FEW_WAVES>(acc, sums, wave, lane);
+    for (int i = 0; i < C::CT * C::RT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    C::sums_of(acc, weights(a.w, a.ldw, n0), GATED ? weights(a.w_up, a.ldw_up, n0) : weights(a.w, a.ldw, n0 + 8 * C::HALF), x, a.K / few::STEP, (int)((uint32_t)tile_n * 5u % (uint32_t)(a.K / few::STEP)), smem + wave * C::RING,
+               wave, lane);
+    wait_vm<0>();                                                // (no load of an empty descriptor writes behind the sums)
     __syncthreads();
-    for (int i = threadIdx.x; i < RT * 16 * 4; i += 64 * FEW_WAVES) {      // four outputs of a row each
-        const int row = i >> 2, piece = i & 3, col = n0 + 4 * piece;
-        if (row >= a.T || col >= a.N) continue;
-        f32x4 v = few::get_sum<NT, RT, FEW_WAVES>(sums, 0, row, piece), up = {1.f, 1.f, 1.f, 1.f};
-        if (GATED) up = few::get_sum<NT, RT, FEW_WAVES>(sums, NT - 1, row, piece);
+    f32x4* const sums = reinterpret_cast<f32x4*>(smem);
+    C::put_sums(acc, sums, wave, lane);
+    __syncthreads();
+    constexpr int PER_ROW = OUTS / 4;
+    for (int i = threadIdx.x; i < C::ROWS * PER_ROW; i += 64 * C::WAVES) {      // four outputs of a row each
+        const int row = i / PER_ROW, piece = i % PER_ROW, col = n0 + 4 * piece;
+        if (row >= rows_x || col >= a.N) continue;
+        f32x4 v = C::get_sum(sums, row, piece), up = {1.f, 1.f, 1.f, 1.f};
+        if (GATED) up = C::get_sum(sums, row, piece + PER_ROW);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             if (col + e < a.N) {
@@ -601,29 +604,35 @@ __global__ void __launch_bounds__(64 * FEW_WAVES) gdn_linear_few_kernel(LinearAc
         v = activate(a.act, v);
         if (GATED) v *= up;
         v *= a.scale;
+        const int64_t t = m0 + row;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             if (col + e < a.N) {
                 if (a.residual)
-                    v[e] += a.res_f32 ? static_cast<const float*>(a.residual)[row * a.ldr + col + e]
-                                      : __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.residual)[row * a.ldr + col + e] << 16);
-                if (OUT_BF16) static_cast<__bf16*>(a.y)[row * a.ldy + col + e] = (__bf16)v[e];
-                else static_cast<float*>(a.y)[row * a.ldy + col + e] = v[e];
+                    v[e] += a.res_f32 ? static_cast<const float*>(a.residual)[t * a.ldr + col + e]
+                                      : __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.residual)[t * a.ldr + col + e] << 16);
+                if (OUT_BF16) static_cast<__bf16*>(a.y)[t * a.ldy + col + e] = (__bf16)v[e];
+                else static_cast<float*>(a.y)[t * a.ldy + col + e] = v[e];
             }
     }
 }
 
-template <int RT>
-hipError_t launch_few(const LinearActArgs& a, bool bf, hipStream_t stream) {
-    const dim3 grid((unsigned)((a.N + 15) / 16)), block(64 * FEW_WAVES);
-    if (a.w_up) {
-        if (bf) hipLaunchKernelGGL((gdn_linear_few_kernel<RT, true, true>), grid, block, 0, stream, a);
-        else hipLaunchKernelGGL((gdn_linear_few_kernel<RT, false, true>), grid, block, 0, stream, a);
-    } else {
-        if (bf) hipLaunchKernelGGL((gdn_linear_few_kernel<RT, true, false>), grid, block, 0, stream, a);
-        else hipLaunchKernelGGL((gdn_linear_few_kernel<RT, false, false>), grid, block, 0, stream, a);
-    }
+template <typename C, bool OUT_BF16, bool GATED>
+hipError_t launch_few_kernel(LinearActArgs a, hipStream_t stream) {
+    static hipError_t attr_err = hipFuncSetAttribute(reinterpret_cast<const void*>(&gdn_linear_few_kernel<C, OUT_BF16, GATED>),
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+    if (attr_err != hipSuccess) return attr_err;
+    constexpr int OUTS = GATED ? C::WR / 2 : C::WR;
+    a.tiles_n = (a.N + OUTS - 1) / OUTS;
+    a.tiles_m = (int32_t)((a.T + C::ROWS - 1) / C::ROWS);
+    hipLaunchKernelGGL((gdn_linear_few_kernel<C, OUT_BF16, GATED>), dim3((unsigned)((a.tiles_n + 7) / 8 * 8 * a.tiles_m)), dim3(64 * C::WAVES), C::SMEM, stream, a);
     return hipGetLastError();
+}
+template <typename C>
+hipError_t launch_few(const LinearActArgs& a, bool bf, hipStream_t stream) {
+    if constexpr (C::WR >= 16)
+        if (a.w_up) return bf ? launch_few_kernel<C, true, true>(a, stream) : launch_few_kernel<C, false, true>(a, stream);
+    return bf ? launch_few_kernel<C, true, false>(a, stream) : launch_few_kernel<C, false, false>(a, stream);
 }
 
 int expert_tile_rows(int shape) { return shape == 2 ? LinBig8::BM : shape == 3 ? LinTiny::BM : LinSmall::BM; }
@@ -724,15 +733,42 @@ LinearPlan plan_linear(int64_t T, int32_t N, int32_t K) {
     return forced >= 0 ? LinearPlan{forced, 0, N} : plan_tiles(T, N, K, false);
 }
 
-constexpr int FEW = 6, FEW_ROWS = 64;
+// ---- the kernels of few rows, shapes 6 .. 11: 16 rows of x with 8, 16, 32 rows of w, then 32 with each.  A compute unit takes what it is sent at 57 KB a us
+// whatever it is (64 workgroups of 8 waves with twice as much on its way: no faster), memory sends 5.5 TB/s, and 3 us go to the beginning and the end.  So a
+// narrow weight wants many workgroups, that is few of its rows each, until x, which each of them reads whole, outweighs them.  us, T x N x K, estimated / measured:
+// 1 x 2048 x 6144 in shapes 6 / 7 / 8: 8.0 / 8.1, 8.9 / 8.6, 11.4 / 12.0; 16 rows 9.9 / 9.3, 11.3 / 10.8, 15.9 / 15.1, 48 rows 6 / 8 / 10: 19.0 / 18.1, 14.2 / 14.0,
+// 13.1 / 11.8; 16 x 8192 x 8192 7 / 8: 29.8 / 26, 28.2 / 26; 64 rows in 11 41.9 / 38.4 (64 x 64 tiles 44); 64 x 2048 x 6144 in 64 x 64 tiles 31, the first form of these kernels,
+// whose waves loaded w and x into registers, 30, and 26 at 48 rows.
+constexpr int FEW = 6, FEW_ROWS = 128;
+struct FewShape { int rt, wr; };
+constexpr FewShape FEW_SHAPES[6] = {{1, 8}, {1, 16}, {1, 32}, {2, 8}, {2, 16}, {2, 32}};
+double bytes_cost(double per_cu, double weights) { return 3.0 + std::sqrt(per_cu * per_cu / (57e3 * 57e3) + weights * weights / (5.5e6 * 5.5e6)); }
+double few_cost(const FewShape& s, int64_t T, int64_t N, int32_t K, bool gated) {
+    const int64_t outs = gated ? s.wr / 2 : s.wr, tiles_n = (N + outs - 1) / outs, tiles_m = (T + 16 * s.rt - 1) / (16 * s.rt);
+    const double one = 2.0 * K * (double)(std::min<int64_t>(T, 16 * s.rt) + s.wr), all = 2.0 * K * (double)tiles_n * (double)(T + tiles_m * s.wr);
+    return bytes_cost(std::max(one, all / chip_cus_linear()), 2.0 * K * (double)N * (gated ? 2 : 1));
+}
+
 LinearPlan plan_act(int64_t T, int32_t N, int32_t K, bool gated) {
     const int forced = g_act_shape.load();
-    if (T <= FEW_ROWS && (forced == FEW || forced < 0)) return {FEW, 0, N};
-    if (forced >= 0 && forced != FEW) return {forced == 1 ? 2 : gated && forced == 5 ? 0 : forced, 0, N};
-    if (!gated) return plan_tiles(T, N, K, false);
-    if (N > INT32_MAX / 2) return {2, 0, N};
-    LinearPlan p = plan_tiles(T, 2 * N, K, true);
-    p.cols /= 2;                                         // (a multiple of 128 where it is cut)
+    if (forced >= FEW && T <= FEW_ROWS) return {gated && FEW_SHAPES[forced - FEW].wr == 8 ? forced + 1 : forced, 0, N};
+    if (forced >= 0 && forced < FEW) return {forced == 1 ? 2 : gated && forced == 5 ? 0 : forced, 0, N};
+    if (gated && N > INT32_MAX / 2) return {2, 0, N};
+    LinearPlan p = plan_tiles(T, gated ? 2 * N : N, K, gated);
+    if (T <= FEW_ROWS) {
+        // (the tiles' estimate knows rounds of them; with so few rows what a tile's compute unit is sent, and the weights, may take longer,
+        // and a tenth more with a barrier at every step)
+        const ShapeCost* c = SHAPES;
+        while (c->id != p.shape) ++c;
+        const int64_t rows_w = gated ? 2 * (int64_t)N : N;
+        double least = std::max(shape_cost(*c, T, rows_w, K), 1.1 * bytes_cost(2.0 * K * (double)(std::min<int64_t>(T, c->bm) + c->bn), 2.0 * K * (double)rows_w));
+        for (int i = 0; i < 6; ++i) {
+            if (gated && FEW_SHAPES[i].wr == 8) continue;
+            const double t = few_cost(FEW_SHAPES[i], T, N, K, gated);
+            if (t < least) { least = t; p = {FEW + i, 0, gated ? 2 * N : N}; }
+        }
+    }
+    if (gated) p.cols /= 2;                              // (a multiple of 128 where it is cut)
     return p;
 }
 
@@ -822,7 +858,15 @@ LinearActArgs act_range(const LinearActArgs& a, int32_t c0, int32_t c1, int es) 
     return b;
 }
 int32_t launch_act_shape(const LinearActArgs& a, int shape, bool bf, hipStream_t stream) {
-    if (shape == FEW) return hip_err(a.T <= 16 ? launch_few<1>(a, bf, stream) : a.T <= 32 ? launch_few<2>(a, bf, stream) : launch_few<4>(a, bf, stream));
+    switch (shape - FEW) {
+        case 0: return hip_err(launch_few<few::Few<1, 8, 4, 6>>(a, bf, stream));
+        case 1: return hip_err(launch_few<few::Few<1, 16, 4, 4>>(a, bf, stream));
+        case 2: return hip_err(launch_few<few::Few<1, 32, 4, 3>>(a, bf, stream));
+        case 3: return hip_err(launch_few<few::Few<2, 8, 4, 4>>(a, bf, stream));
+        case 4: return hip_err(launch_few<few::Few<2, 16, 4, 3>>(a, bf, stream));
+        case 5: return hip_err(launch_few<few::Few<2, 32, 4, 2>>(a, bf, stream));
+        default: break;
+    }
     return a.w_up ? launch_shape<EPI_GATED>(a, shape, bf, stream) : launch_shape<EPI_ACT>(a, shape, bf, stream);
 }
 }  // namespace
@@ -940,5 +984,5 @@ extern "C" int32_t gdn_linear_act_plan(int64_t T, int32_t N, int32_t K, int32_t 
 }
 
 extern "C" int32_t gdn_linear_act_tune(int32_t shape) {
-    return g_act_shape.exchange(shape < 0 || shape > FEW ? -1 : shape);
+    return g_act_shape.exchange(shape < 0 || shape > FEW + 5 ? -1 : shape);
 }

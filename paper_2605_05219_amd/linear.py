@@ -174,5 +174,5 @@ def gdn_linear_act_plan(T: int, N: int, K: int, gated: bool = False):
 
 
 def gdn_linear_act_tune(shape: int) -> int:
-    """Fixes the kernel of gdn_linear_act (0 to 6, see include/gdn_linear.h) or returns the choice to the library (-1); returns the previous setting."""
+    """Fixes the kernel of gdn_linear_act (0 to 11, see include/gdn_linear.h) or returns the choice to the library (-1); returns the previous setting."""
     return int(_lib().gdn_linear_act_tune(int(shape)))
