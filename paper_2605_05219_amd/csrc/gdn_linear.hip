@@ -164,13 +164,34 @@ __device__ __forceinline__ void act_epilogue(const typename EpiArgs<EPI>::type& 
     constexpr int RBY = PW * 4 <= 64 ? 64 : PW * 4 <= 128 ? 128 : 256, PPR = RBY / 16;
     constexpr int TP = WM * RBY <= REGION ? WM : REGION / RBY >= 64 ? 64 : REGION / RBY >= 32 ? 32 : 16;
     constexpr int OPL = OUT_BF16 ? 8 : 4;                          // outputs of a lane's store
-    constexpr int LPR = PW / OPL, RPI = 64 / LPR;                  // lanes per row, rows a wave-wide store covers
+    constexpr int LPR = PW / OPL, RPI = 64 / LPR, IT = TP / RPI;  // lanes per row, rows a wave-wide store covers, stores of a pass
     static_assert(TP * RBY <= REGION && TP % RPI == 0 && WM % TP == 0 && WN % PW == 0 && PW % 16 == 0 && CFG::TJ % PAIR == 0, "epilogue region");
     const int lr = lane & 15, g = lane >> 4;
 #pragma unroll
     for (int c0 = 0; c0 < WN; c0 += PW) {
 #pragma unroll
         for (int t0 = 0; t0 < WM; t0 += TP) {
+            // the pass's residual goes out in front of the activations, whose time covers its latency
+            u32x4 res[IT][2];
+            if (!epi_expert(EPI) && a.residual) {
+#pragma unroll
+                for (int i = 0; i < IT; ++i) {
+                    const int64_t tok = tok0 + t0 + RPI * i + lane / LPR;
+                    const int col = col0 + c0 + lane % LPR * OPL;
+                    if (tok >= n_rows || col + OPL > a.N) continue;      // (the last columns one by one below)
+                    if (a.res_f32) {
+                        const u32x4* r = reinterpret_cast<const u32x4*>(static_cast<const float*>(a.residual) + tok * a.ldr + col);
+                        res[i][0] = r[0];
+                        if (OUT_BF16) res[i][1] = r[1];
+                    } else if (OUT_BF16) {
+                        res[i][0] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.residual) + tok * a.ldr + col);
+                    } else {
+                        const uint2 r = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(a.residual) + tok * a.ldr + col);
+                        res[i][0][0] = r.x;
+                        res[i][0][1] = r.y;
+                    }
+                }
+            }
 #pragma unroll
             for (int tj = c0 / 16; tj < (c0 + PW) / 16; ++tj) {
                 const int cl = 16 * tj + 4 * g;
@@ -191,7 +212,7 @@ __device__ __forceinline__ void act_epilogue(const typename EpiArgs<EPI>::type& 
                 }
             }
 #pragma unroll
-            for (int i = 0; i < TP / RPI; ++i) {
+            for (int i = 0; i < IT; ++i) {
                 const int row = RPI * i + lane / LPR, first = lane % LPR * OPL;
                 f32x4 v[OPL / 4];
 #pragma unroll
@@ -210,13 +231,12 @@ __device__ __forceinline__ void act_epilogue(const typename EpiArgs<EPI>::type& 
                 const bool whole = col + OPL <= a.N;
                 if (!epi_expert(EPI) && a.residual) {
                     if (whole && a.res_f32) {
-                        const f32x4* r = reinterpret_cast<const f32x4*>(static_cast<const float*>(a.residual) + tok * a.ldr + col);
 #pragma unroll
-                        for (int h = 0; h < OPL / 4; ++h) v[h] += r[h];
+                        for (int h = 0; h < OPL / 4; ++h) v[h] += __builtin_bit_cast(f32x4, res[i][h]);
                     } else if (whole) {
-                        const uint16_t* r = static_cast<const uint16_t*>(a.residual) + tok * a.ldr + col;
 #pragma unroll
-                        for (int h = 0; h < OPL / 4; ++h) v[h] += __builtin_convertvector(*reinterpret_cast<const bf16x4*>(r + 4 * h), f32x4);
+                        for (int e = 0; e < OPL; ++e)
+                            v[e / 4][e % 4] += __uint_as_float(e & 1 ? res[i][0][e / 2] & 0xffff0000u : res[i][0][e / 2] << 16);
                     } else {
 #pragma unroll
                         for (int e = 0; e < OPL; ++e)
