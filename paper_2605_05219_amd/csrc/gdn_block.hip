@@ -1,10 +1,11 @@
 // gdn_block_norm: the residual stream between two blocks, with the norms on both sides (see include/gdn_block.h).
 //
 // s = r + scale g N_post(y), x = N_pre(s): a few flops for every element read or written once, so memory traffic is all that
-// bounds it.  A row is held in registers from its loads to its stores, 8 adjacent elements to a piece (16 bytes of bf16), up
-// to four pieces a thread, so that neither the squares of what the mean leaves nor the second norm read it again.  A row is
-// dealt to 1, 4 or 16 waves: the fewest that hold it where there are rows enough to fill the chip (a wave by itself needs no
-// barrier for its sums), more where there are few and a row's own latency is the time.
+// bounds it.  A row is held in registers from its loads to its stores, 8 adjacent elements to a piece (16 bytes of bf16), so that neither the squares of
+// what the mean leaves nor the second norm read it again: one piece to a thread and as many waves as the row has pieces for, up to 16 (rows of up to 8192), then two or
+// four.  A norm costs one barrier.  8192 rows of 2048 in bf16, the norm in front alone, 26 us (134 MB: 5.2 TB/s, a plain copy of 2 GiB 4.9), with
+// one behind the block and a gate per channel 32; 1777 rows of 5120, two layer norms with a gate per element and a stream in fp32, 38 (3.3 TB/s: a row's two norms wait for
+// each other, and with ten waves to a row a compute unit has two rows at once); a single row 2.4, which a call's host time of 8 covers.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -30,34 +31,35 @@ struct BlockArgs {
     int32_t D;
     int32_t post, pre, gate_kind, gate_act;
     int32_t in_f32, s_f32, x_f32;
+    int32_t waves;
     float eps_post, eps_pre, scale, offset, inv_d;
 };
 
-// 8 elements as they lie in memory, so that a row's loads are all on their way before the first is unpacked.
-struct Piece { u32x4 lo, hi; };
-__device__ __forceinline__ Piece fetch(const void* p, int64_t at, int f32) {
-    Piece v = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-    if (f32) {
-        const u32x4* q = reinterpret_cast<const u32x4*>(static_cast<const float*>(p) + at);
-        v.lo = q[0];
-        v.hi = q[1];
-    } else {
-        v.lo = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p) + at);
-    }
+// 8 elements as they lie in memory (fp32 or bf16), so that a row's loads are all on their way before the first is unpacked.
+template <bool F32>
+struct Piece { u32x4 q[F32 ? 2 : 1]; };
+template <bool F32>
+__device__ __forceinline__ Piece<F32> fetch(const void* p, int64_t at) {
+    Piece<F32> v;
+    const u32x4* q = reinterpret_cast<const u32x4*>(static_cast<const char*>(p) + at * (F32 ? 4 : 2));
+    v.q[0] = q[0];
+    if constexpr (F32) v.q[1] = q[1];
     return v;
 }
-__device__ __forceinline__ f32x8 unpack(const Piece& v, int f32) {
+template <bool F32>
+__device__ __forceinline__ Piece<F32> nothing() {
+    Piece<F32> v;
+    v.q[0] = u32x4{0, 0, 0, 0};
+    if constexpr (F32) v.q[1] = v.q[0];
+    return v;
+}
+template <bool F32>
+__device__ __forceinline__ f32x8 unpack(const Piece<F32>& v) {
     f32x8 o;
-    if (f32) {
-        const f32x4 a = __builtin_bit_cast(f32x4, v.lo), b = __builtin_bit_cast(f32x4, v.hi);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { o[i] = a[i]; o[i + 4] = b[i]; }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            o[2 * i] = __uint_as_float(v.lo[i] << 16);
-            o[2 * i + 1] = __uint_as_float(v.lo[i] & 0xffff0000u);
-        }
+    for (int e = 0; e < 8; ++e) {
+        if constexpr (F32) o[e] = __uint_as_float(v.q[e / 4][e % 4]);
+        else o[e] = __uint_as_float(e & 1 ? v.q[0][e / 2] & 0xffff0000u : v.q[0][e / 2] << 16);
     }
     return o;
 }
@@ -75,128 +77,185 @@ __device__ __forceinline__ f32x8 fetch_f32(const float* p) {
     return f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 }
 
-// The sum over a row's waves, the same on every thread and the same whenever it runs: a butterfly over the lanes, then the waves' sums in order.
-// `part`: WAVES floats of this row; `turn` alternates between two sets, so one barrier is enough for each sum.
-template <int WAVES>
-__device__ __forceinline__ float row_sum(float v, float (*part)[WAVES], int& turn, int wave) {
+// The sum over a wave, on every lane: moves within the vector unit.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float moved(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+    v += moved<0x111, 0xf>(v);           // 1, 2, 4, 8 lanes up a row of 16, then the last lane of a row to the next one, and of the first half to the second
+    v += moved<0x112, 0xf>(v);
+    v += moved<0x114, 0xf>(v);
+    v += moved<0x118, 0xf>(v);
+    v += moved<0x142, 0xa>(v);
+    v += moved<0x143, 0xc>(v);
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+constexpr int MAX_WAVES = 16;
+struct Parts { float sum, squares; };
+
+// A norm's weights (with their offset) for a thread's pieces.
+template <int PIECES>
+struct Weights { f32x8 w[PIECES]; };
+template <int PIECES>
+__device__ __forceinline__ void fetch_weights(Weights<PIECES>& q, const float* w, float offset, int first, int stride, int D) {
 #pragma unroll
-    for (int m = 32; m > 0; m >>= 1) v += __shfl_xor(v, m);
-    if (WAVES == 1) return v;
-    float* p = part[turn];
-    turn ^= 1;
-    if ((threadIdx.x & 63) == 0) p[wave] = v;
-    __syncthreads();
-    float total = 0.f;
+    for (int i = 0; i < PIECES; ++i) {
+        const int c = first + i * stride;
+        q.w[i] = f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (c >= D) continue;
+        q.w[i] = fetch_f32(w + c);
 #pragma unroll
-    for (int i = 0; i < WAVES; ++i) total += p[i];
-    return total;
+        for (int e = 0; e < 8; ++e) q.w[i][e] += offset;
+    }
 }
 
-// v <- N(v) over the row; w, b: the row's parameters (b may be null).
-template <int WAVES, int PIECES>
-__device__ __forceinline__ void normalise(f32x8 (&v)[PIECES], int kind, const float* w, const float* b, float offset, float eps, float inv_d, int D,
-                                          int first, float (*part)[WAVES], int& turn, int wave) {
-    if (kind == GDN_NORM_LAYER) {
-        float sum = 0.f;
+// v <- N(v) over the row.  Every wave takes the mean of its own elements and the squares of what that leaves; the waves' meet in LDS behind one barrier, in
+// order, the squares about the row's mean by  sum (v - m)^2 = sum over waves of (sum (v - m_w)^2 + n_w (m_w - m)^2).  `part`: two sets, between which
+// `turn` alternates, so one barrier is enough for each norm.  The same on every thread, and the same whenever it runs.
+template <int PIECES>
+__device__ __forceinline__ void normalise(f32x8 (&v)[PIECES], int kind, const Weights<PIECES>& q, const float* bias, float eps, const BlockArgs& a, int first, int stride,
+                                          Parts (*part)[MAX_WAVES], int& turn, int wave) {
+    const int waves = a.waves;
+    auto count = [&](int w) {                                    // elements of a wave
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) n += min(max(a.D - i * stride - w * 512, 0), 512);
+        return (float)n;
+    };
+    const bool layer = kind == GDN_NORM_LAYER;
+    Parts mine = {0.f, 0.f};
+    float own = 0.f;
+    if (layer) {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum += v[i][e];          // (pieces behind the row's end hold zeros)
-        const float mean = row_sum<WAVES>(sum, part, turn, wave) * inv_d;
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i)
-            if (first + i * WAVES * 512 < D)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[i][e] -= mean;
+            for (int e = 0; e < 8; ++e) mine.sum += v[i][e];     // (pieces behind the row's end hold zeros)
+        mine.sum = wave_sum(mine.sum);
+        own = mine.sum / count(waves == 1 ? 0 : wave);
     }
-    float squares = 0.f;
 #pragma unroll
     for (int i = 0; i < PIECES; ++i)
+        if (first + i * stride < a.D)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) squares = fmaf(v[i][e], v[i][e], squares);
-    const float inv = 1.f / sqrtf(row_sum<WAVES>(squares, part, turn, wave) * inv_d + eps);
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-        const int c = first + i * WAVES * 512;
-        if (c >= D) continue;
-        const f32x8 wv = fetch_f32(w + c);
-        f32x8 bv = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (b) bv = fetch_f32(b + c);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] = fmaf(v[i][e] * inv, wv[e] + offset, bv[e]);
-    }
-}
-
-// WAVES waves to a row, PIECES pieces of 8 elements to a thread; a workgroup of at least four waves.
-template <int WAVES, int PIECES>
-__global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) gdn_block_norm_kernel(BlockArgs a) {
-    __shared__ float part[2][WAVES];
-    constexpr int ROWS = WAVES == 1 ? 4 : 1;                     // rows of a workgroup
-    const int tid = threadIdx.x, wave = tid >> 6;
-    const int64_t t = (int64_t)blockIdx.x * ROWS + (WAVES == 1 ? wave : 0);
-    if (t >= a.T) return;                                        // (whole waves; with more waves to a row the grid is the rows)
-    const int first = 8 * (WAVES == 1 ? tid & 63 : tid);
-    int turn = 0;
-    Piece py[PIECES], pr[PIECES], pg[PIECES];
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-        const int c = first + i * WAVES * 512;
-        py[i] = pr[i] = pg[i] = Piece{{0, 0, 0, 0}, {0, 0, 0, 0}};
-        if (c >= a.D) continue;
-        if (a.y) py[i] = fetch(a.y, t * a.ldy + c, a.in_f32);
-        if (a.r) pr[i] = fetch(a.r, t * a.ldr + c, a.s_f32);
-        if (a.gate_kind == GDN_GATE_ELEMENT) pg[i] = fetch(a.gate, t * a.ldg + c, a.in_f32);
-    }
-    float one_gate = a.scale;
-    if (a.gate_kind == GDN_GATE_TOKEN) {
-        float g = a.in_f32 ? static_cast<const float*>(a.gate)[t * a.ldg]
-                           : __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.gate)[t * a.ldg] << 16);
-        if (a.gate_act) g = 1.f / (1.f + expf(-g));
-        one_gate *= g;
-    }
-    f32x8 v[PIECES];
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) v[i] = unpack(py[i], a.in_f32);
-    if (a.post != GDN_NORM_NONE)
-        normalise<WAVES, PIECES>(v, a.post, a.w_post, a.b_post, a.offset, a.eps_post, a.inv_d, a.D, first, part, turn, wave);
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-        const int c = first + i * WAVES * 512;
-        if (c >= a.D) continue;
-        if (a.gate_kind == GDN_GATE_ELEMENT || a.gate_kind == GDN_GATE_CHANNEL) {
-            f32x8 g = a.gate_kind == GDN_GATE_ELEMENT ? unpack(pg[i], a.in_f32) : fetch_f32(static_cast<const float*>(a.gate) + c);
-            if (a.gate_act)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) g[e] = 1.f / (1.f + __expf(-g[e]));
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[i][e] *= g[e];
+            for (int e = 0; e < 8; ++e) mine.squares = fmaf(v[i][e] - own, v[i][e] - own, mine.squares);
+    mine.squares = wave_sum(mine.squares);
+    float mean = own, squares = mine.squares;
+    if (waves > 1) {
+        Parts* p = part[turn];
+        turn ^= 1;
+        if ((threadIdx.x & 63) == 0) p[wave] = mine;
+        __syncthreads();
+        float sum = 0.f;
+        for (int w = 0; w < waves; ++w) sum += p[w].sum;
+        mean = sum * a.inv_d;
+        squares = 0.f;
+        for (int w = 0; w < waves; ++w) {
+            squares += p[w].squares;
+            if (layer) {
+                const float n = count(w), d = p[w].sum / n - mean;
+                squares = fmaf(n * d, d, squares);
+            }
         }
-        const f32x8 r = unpack(pr[i], a.s_f32);
-        if (a.y)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[i][e] = a.r ? fmaf(one_gate, v[i][e], r[e]) : one_gate * v[i][e];
-        else v[i] = r;
-        if (a.s) put(a.s, t * a.lds + c, a.s_f32, v[i]);
     }
-    if (a.pre == GDN_NORM_NONE) return;
-    normalise<WAVES, PIECES>(v, a.pre, a.w_pre, a.b_pre, a.offset, a.eps_pre, a.inv_d, a.D, first, part, turn, wave);
+    const float inv = 1.f / sqrtf(squares * a.inv_d + eps);
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-        const int c = first + i * WAVES * 512;
-        if (c < a.D) put(a.x, t * a.ldx + c, a.x_f32, v[i]);
+        const int c = first + i * stride;
+        if (c >= a.D) continue;
+        f32x8 b = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (bias) b = fetch_f32(bias + c);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[i][e] = fmaf((v[i][e] - mean) * inv, q.w[i][e], b[e]);
     }
 }
 
-template <int WAVES, int PIECES>
-hipError_t launch(const BlockArgs& a, hipStream_t stream) {
-    const int64_t blocks = WAVES == 1 ? (a.T + 3) / 4 : a.T;
-    hipLaunchKernelGGL((gdn_block_norm_kernel<WAVES, PIECES>), dim3((unsigned)blocks), dim3(WAVES == 1 ? 256 : 64 * WAVES), 0, stream, a);
-    return hipGetLastError();
+// `a.waves` waves to a row, PIECES pieces of 8 elements to a thread; with one wave to a row a workgroup has four rows.  A workgroup goes through
+// every grid-th row and keeps the weights (and a gate per channel) in registers: read anew for each row those arrays of fp32 are more than the row
+// itself, two of bf16 read and two written, and come out of L2.  (Rows wider than 8192 have more than one piece to a thread, and read them each time.)
+template <int PIECES, bool IN_F32, bool S_F32>
+__global__ void __launch_bounds__(64 * MAX_WAVES) gdn_block_norm_kernel(BlockArgs a) {
+    __shared__ Parts part[2][MAX_WAVES];
+    constexpr bool KEEP = PIECES == 1;
+    const int tid = threadIdx.x, wave = tid >> 6, waves = a.waves, stride = waves * 512;
+    const int rows = waves == 1 ? 4 : 1;                         // rows of a workgroup
+    const int first = 8 * (waves == 1 ? tid & 63 : tid);
+    int turn = 0;
+    Weights<PIECES> post, pre, channel;
+    if (KEEP && a.post != GDN_NORM_NONE) fetch_weights(post, a.w_post, a.offset, first, stride, a.D);
+    if (KEEP && a.pre != GDN_NORM_NONE) fetch_weights(pre, a.w_pre, a.offset, first, stride, a.D);
+    if (KEEP && a.gate_kind == GDN_GATE_CHANNEL) fetch_weights(channel, static_cast<const float*>(a.gate), 0.f, first, stride, a.D);
+    // (whole waves leave with one wave to a row; with more the loop's count is the workgroup's)
+    for (int64_t t = (int64_t)blockIdx.x * rows + (waves == 1 ? wave : 0); t < a.T; t += (int64_t)gridDim.x * rows) {
+        Piece<IN_F32> py[PIECES], pg[PIECES];
+        Piece<S_F32> pr[PIECES];
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int c = first + i * stride;
+            py[i] = pg[i] = nothing<IN_F32>();
+            pr[i] = nothing<S_F32>();
+            if (c >= a.D) continue;
+            if (a.y) py[i] = fetch<IN_F32>(a.y, t * a.ldy + c);
+            if (a.r) pr[i] = fetch<S_F32>(a.r, t * a.ldr + c);
+            if (a.gate_kind == GDN_GATE_ELEMENT) pg[i] = fetch<IN_F32>(a.gate, t * a.ldg + c);
+        }
+        float one_gate = a.scale;
+        if (a.gate_kind == GDN_GATE_TOKEN) {
+            float g = IN_F32 ? static_cast<const float*>(a.gate)[t * a.ldg] : __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.gate)[t * a.ldg] << 16);
+            if (a.gate_act) g = 1.f / (1.f + expf(-g));
+            one_gate *= g;
+        }
+        f32x8 v[PIECES];
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) v[i] = unpack(py[i]);
+        if (a.post != GDN_NORM_NONE) {
+            if (!KEEP) fetch_weights(post, a.w_post, a.offset, first, stride, a.D);
+            normalise(v, a.post, post, a.b_post, a.eps_post, a, first, stride, part, turn, wave);
+        }
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int c = first + i * stride;
+            if (c >= a.D) continue;
+            if (a.gate_kind == GDN_GATE_ELEMENT || a.gate_kind == GDN_GATE_CHANNEL) {
+                f32x8 g = unpack(pg[i]);
+                if (a.gate_kind == GDN_GATE_CHANNEL) g = KEEP ? channel.w[i] : fetch_f32(static_cast<const float*>(a.gate) + c);
+                if (a.gate_act)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) g[e] = 1.f / (1.f + __expf(-g[e]));
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[i][e] *= g[e];
+            }
+            const f32x8 r = unpack(pr[i]);
+            if (a.y)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[i][e] = a.r ? fmaf(one_gate, v[i][e], r[e]) : one_gate * v[i][e];
+            else v[i] = r;
+            if (a.s) put(a.s, t * a.lds + c, S_F32, v[i]);
+        }
+        if (a.pre == GDN_NORM_NONE) continue;
+        if (!KEEP) fetch_weights(pre, a.w_pre, a.offset, first, stride, a.D);
+        normalise(v, a.pre, pre, a.b_pre, a.eps_pre, a, first, stride, part, turn, wave);
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int c = first + i * stride;
+            if (c < a.D) put(a.x, t * a.ldx + c, a.x_f32, v[i]);
+        }
+    }
 }
 
-template <int WAVES>
-hipError_t launch_pieces(const BlockArgs& a, int pieces, hipStream_t stream) {
-    return pieces <= 1 ? launch<WAVES, 1>(a, stream) : pieces <= 2 ? launch<WAVES, 2>(a, stream) : launch<WAVES, 4>(a, stream);
+template <int PIECES, bool IN_F32, bool S_F32>
+void launch_kernel(const BlockArgs& a, unsigned blocks, unsigned threads, hipStream_t stream) {
+    hipLaunchKernelGGL((gdn_block_norm_kernel<PIECES, IN_F32, S_F32>), dim3(blocks), dim3(threads), 0, stream, a);
+}
+template <int PIECES>
+hipError_t launch(BlockArgs a, hipStream_t stream) {
+    a.waves = (a.D + 512 * PIECES - 1) / (512 * PIECES);
+    // as many workgroups as are on the chip at once (24 waves to a compute unit, by their registers): 4096 rows of 8192, 16 waves each, 58 us in 256 workgroups, 82 in 320
+    const int per_block = a.waves == 1 ? 4 : a.waves;            // waves
+    const unsigned blocks = (unsigned)std::min<int64_t>(a.waves == 1 ? (a.T + 3) / 4 : a.T, (int64_t)chip_cus() * (24 / per_block)), threads = 64u * per_block;
+    if (a.in_f32) a.s_f32 ? launch_kernel<PIECES, true, true>(a, blocks, threads, stream) : launch_kernel<PIECES, true, false>(a, blocks, threads, stream);
+    else a.s_f32 ? launch_kernel<PIECES, false, true>(a, blocks, threads, stream) : launch_kernel<PIECES, false, false>(a, blocks, threads, stream);
+    return hipGetLastError();
 }
 
 int32_t check(const gdn_block_shape* p, const void* y, int64_t ldy, const void* gate, int64_t ldg, const float* w_post, const float* b_post,
@@ -276,10 +335,6 @@ extern "C" int32_t gdn_block_norm(const gdn_block_shape* p, const void* y, int64
     a.eps_post = p->eps_post; a.eps_pre = p->eps_pre; a.scale = p->scale; a.offset = p->offset;
     a.inv_d = 1.f / (float)p->D;
     hipStream_t stream = static_cast<hipStream_t>(stream_);
-    const int pieces = (p->D / 8 + 63) / 64;                     // of a wave that has the row by itself
-    hipError_t e;
-    if (pieces > 16) e = launch_pieces<16>(a, (pieces + 15) / 16, stream);
-    else if (pieces > 4 || (pieces > 1 && T < 4096)) e = launch_pieces<4>(a, (pieces + 3) / 4, stream);
-    else e = launch_pieces<1>(a, pieces, stream);
+    const hipError_t e = p->D <= 8192 ? launch<1>(a, stream) : p->D <= 16384 ? launch<2>(a, stream) : launch<4>(a, stream);
     return e == hipSuccess ? GDN_OK : GDN_ERR_HIP - (int32_t)e;
 }

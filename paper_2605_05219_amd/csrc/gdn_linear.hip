@@ -679,18 +679,6 @@ hipError_t launch_expert_product(const ExpertProduct& p, int shape, hipStream_t 
 
 std::atomic<int32_t> g_linear_shape{-1}, g_act_shape{-1};
 
-int chip_cus_linear() {
-    static const int n = [] {
-        int dev = 0, cus = 0;
-        if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus <= 0) {
-            (void)hipGetLastError();
-            return 256;
-        }
-        return cus;
-    }();
-    return n;
-}
-
 // The estimated time of a problem in a tile shape, in us: full rounds of workgroups over the chip, and a last one that costs its latency (a
 // workgroup alone walks k no faster) and more the fuller it is, since the compute units share power and memory.  A round has a part that
 // grows with k and a part that does not (first loads, outputs): at K = 64 the second is the larger, and the more so
@@ -712,7 +700,7 @@ constexpr ShapeCost SHAPES[5] = {{3, 64, 64, 2, 10.4, 1.8, 3.9, 2.0, false},
                                  {5, 128, 160, 1, 15.9, 5.0, 12.9, 3.9, false},
                                  {2, 256, 256, 1, 41.9, 6.9, 32.6, 4.0, true}};
 double shape_cost(const ShapeCost& c, int64_t T, int64_t N, int32_t K) {
-    const int64_t tiles = ((T + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn), slots = (int64_t)chip_cus_linear() * c.per_cu;
+    const int64_t tiles = ((T + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn), slots = (int64_t)chip_cus() * c.per_cu;
     const double k = (double)K / 2048.0, f = (double)(tiles % slots) / (double)slots;
     const double full = c.full_k * k + c.full, alone = c.alone_k * k + c.alone;
     return (double)(tiles / slots) * full + (f > 0 ? alone + (full - alone) * (c.square ? f * f : f) : 0.0);
@@ -736,7 +724,7 @@ LinearPlan plan_tiles(int64_t T, int32_t N, int32_t K, bool gated) {      // gat
     LinearPlan p = {best_of(N, 5, &whole), 0, N};
     const double launch = 2.5;                           // a launch beyond its estimate
     double least = 0.97 * whole;                         // (a cut has to be worth it)
-    const int64_t tiles_m = (T + 255) / 256, cus = chip_cus_linear();
+    const int64_t tiles_m = (T + 255) / 256, cus = chip_cus();
     for (int64_t r = 1; r <= 64; ++r) {                  // the most columns that r rounds of 256 x 256 tiles hold
         const int64_t cols = r * cus / tiles_m * 256;
         if (cols >= N) break;
@@ -766,7 +754,7 @@ double bytes_cost(double per_cu, double weights) { return 3.0 + std::sqrt(per_cu
 double few_cost(const FewShape& s, int64_t T, int64_t N, int32_t K, bool gated) {
     const int64_t outs = gated ? s.wr / 2 : s.wr, tiles_n = (N + outs - 1) / outs, tiles_m = (T + 16 * s.rt - 1) / (16 * s.rt);
     const double one = 2.0 * K * (double)(std::min<int64_t>(T, 16 * s.rt) + s.wr), all = 2.0 * K * (double)tiles_n * (double)(T + tiles_m * s.wr);
-    return bytes_cost(std::max(one, all / chip_cus_linear()), 2.0 * K * (double)N * (gated ? 2 : 1));
+    return bytes_cost(std::max(one, all / chip_cus()), 2.0 * K * (double)N * (gated ? 2 : 1));
 }
 
 LinearPlan plan_act(int64_t T, int32_t N, int32_t K, bool gated) {

@@ -1,5 +1,7 @@
-// Host checks of row-strided tensors, shared by the entry points that take them.
+// Host checks of row-strided tensors and the chip's size, shared by entry points.
 #pragma once
+#include <hip/hip_runtime.h>
+
 #include <cstdint>
 
 #include "gdn_resume.h"
@@ -35,6 +37,19 @@ inline bool share_bytes(const Rows& a, const Rows& b) {
 // The same rows, element for element: an output over an input that each thread reads before it writes.
 inline bool same_rows(const Rows& a, const Rows& b) {
     return a.at == b.at && a.width == b.width && a.rows == b.rows && (a.pitch == b.pitch || a.rows <= 1);
+}
+
+// Compute units of the chip (256 where that cannot be asked).
+inline int chip_cus() {
+    static const int n = [] {
+        int dev = 0, cus = 0;
+        if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus <= 0) {
+            (void)hipGetLastError();
+            return 256;
+        }
+        return cus;
+    }();
+    return n;
 }
 
 inline bool dtype_known(int32_t t) { return t == GDN_F32 || t == GDN_BF16; }
