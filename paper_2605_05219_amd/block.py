@@ -4,7 +4,7 @@ from __future__ import annotations
 import ctypes
 
 from .binding import GDN_BF16, GDN_F32, _check, lib
-from .rows import _dp, _here, _ld, _stream_ptr
+from .rows import _device, _packed, _rows, _stream
 
 _i32, _i64, _vp, _f32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_float
 
@@ -48,39 +48,37 @@ def gdn_block_norm_raw(shape, y=0, ldy=0, gate=0, ldg=0, w_post=0, b_post=0, r=0
                                      s, lds, x, ldx, T, stream_ptr))
 
 
-_types = {}
-
-
-def _dtype(code):
-    if not _types:
-        import torch
-        _types.update({GDN_BF16: torch.bfloat16, GDN_F32: torch.float32})
-    return _types.get(code)
+_types = []                                              # torch's fp32 and bf16, in the order of their codes
 
 
 def gdn_block_norm(shape: gdn_block_shape, y, gate, w_post, b_post, r, w_pre, b_pre, s, x, stream=None) -> None:
     """See include/gdn_block.h.  y, r, s, x (and a gate per element) are [T][D] tensors with unit inner stride, whose row stride is passed
     on; a gate per token is [T]; w, b and a gate per channel are fp32 [D].  y or r, and s or x, may be None."""
+    if not _types:
+        import torch
+        _types.extend((torch.float32, torch.bfloat16))
     of = y if y is not None else r
-    if of is None or len(of.shape) != 2:
-        raise ValueError("gdn_block_norm: y or r is needed, [T][D]")
-    D, size = shape.D, of.shape
-    T = size[0]
-    element = shape.gate == 1
-    code = shape.in_dtype
-    for t, c in ((y, code), (r, shape.s_dtype), (s, shape.s_dtype), (x, shape.x_dtype), (gate if element else None, code)):
-        if t is not None and (t.shape != size or size[1] != D or t.dtype is not _dtype(c)):
-            raise ValueError("gdn_block_norm: tensors are [T][D], of the types that the shape says")
-    for t in (w_post, b_post, w_pre, b_pre, gate if shape.gate == 3 else None):
-        if t is not None and (t.numel() != D or t.dtype is not _dtype(GDN_F32) or not t.is_contiguous()):
-            raise ValueError("gdn_block_norm: weights, biases and a gate per channel are fp32 [D]")
-    ldg = 0
-    if shape.gate == 2 and gate is not None:
-        if gate.shape != size[:1] or gate.dtype is not _dtype(code):
-            raise ValueError("gdn_block_norm: a gate per token is [T], of y's type")
-        ldg = gate.stride(0) if T > 1 else 1
-    elif element and gate is not None:
-        ldg = _ld(gate)
-    device = _here(y, gate, w_post, b_post, r, w_pre, b_pre, s, x)
-    _check(_lib().gdn_block_norm(ctypes.byref(shape), _dp(y), _ld(y), _dp(gate), ldg, _dp(w_post), _dp(b_post), _dp(r), _ld(r), _dp(w_pre),
-                                 _dp(b_pre), _dp(s), _ld(s), _dp(x), _ld(x), T, _stream_ptr(stream, device)), "gdn_block_norm")
+    size = of.shape if of is not None else ()
+    D = shape.D
+    if len(size) != 2 or size[1] != D or not (0 <= shape.in_dtype <= 1 and 0 <= shape.s_dtype <= 1 and 0 <= shape.x_dtype <= 1):
+        raise ValueError("gdn_block_norm: y or r is needed, [T][D], and types that there are")
+    name, f32, device, T, vector = "gdn_block_norm", _types[0], _device(), size[0], size[1:]
+    wide, held = _types[shape.in_dtype], _types[shape.s_dtype]
+    kind = shape.gate
+    if kind == 1:
+        at_gate, ldg = _rows(gate, size, wide, device, name)
+    elif kind == 3:
+        at_gate, ldg = _packed(gate, vector, f32, device, name), 0
+    elif kind == 2 and gate is not None:
+        if gate.shape != size[:1] or gate.dtype is not wide or gate.get_device() != device:
+            raise ValueError("gdn_block_norm: a gate per token is [T], of y's type and on its device")
+        at_gate, ldg = gate.data_ptr(), gate.stride(0) if T > 1 else 1
+    else:
+        at_gate, ldg = None, 0
+    at_y, ldy = _rows(y, size, wide, device, name)
+    at_r, ldr = _rows(r, size, held, device, name)
+    at_s, lds = _rows(s, size, held, device, name)
+    at_x, ldx = _rows(x, size, _types[shape.x_dtype], device, name)
+    _check(_lib().gdn_block_norm(ctypes.byref(shape), at_y, ldy, at_gate, ldg, _packed(w_post, vector, f32, device, name),
+                                 _packed(b_post, vector, f32, device, name), at_r, ldr, _packed(w_pre, vector, f32, device, name),
+                                 _packed(b_pre, vector, f32, device, name), at_s, lds, at_x, ldx, T, _stream(stream, device)), name)

@@ -3,8 +3,8 @@ from __future__ import annotations
 
 import ctypes
 
-from . import rows
 from .binding import GDN_BF16, GDN_F32, _check, _dp, _stream_ptr, lib
+from .rows import _device, _packed, _rows, _stream
 
 _i32, _i64, _vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p
 
@@ -148,22 +148,24 @@ def gdn_linear_act(x, w, bias, y, act="none", w_up=None, bias_up=None, residual=
     if not _codes:
         import torch
         _codes.update({torch.bfloat16: GDN_BF16, torch.float32: GDN_F32})
-    (T, K), N = x.shape, w.shape[0]
-    if (w.shape[1] != K or y.shape != (T, N) or (w_up is not None and w_up.shape != w.shape) or (residual is not None and residual.shape != y.shape)
-            or (bias is not None and bias.shape != (N,)) or (bias_up is not None and bias_up.shape != (N,))):
-        raise ValueError("gdn_linear_act: shapes do not match")
-    code, res_code = _codes.get(y.dtype), _codes.get(residual.dtype) if residual is not None else GDN_BF16
-    if _codes.get(x.dtype) != GDN_BF16 or w.dtype is not x.dtype or (w_up is not None and w_up.dtype is not x.dtype) or code is None or res_code is None:
-        raise ValueError("gdn_linear_act: x and the weights are bf16, y and residual bf16 or fp32")
-    for b in (bias, bias_up):
-        if b is not None and (_codes.get(b.dtype) != GDN_F32 or (N > 1 and b.stride(0) != 1)):
-            raise ValueError("gdn_linear_act: biases are fp32, without gaps")
+    bf16, f32 = _codes
+    name, device, size, weight, out = "gdn_linear_act", _device(), x.shape, w.shape, y.shape
+    if len(size) != 2 or len(weight) != 2 or weight[1] != size[1] or out != (size[0], weight[0]):
+        raise ValueError("gdn_linear_act: x is [T][K], w [N][K], y [T][N]")
+    if y.dtype not in _codes or (residual is not None and residual.dtype not in _codes):
+        raise ValueError("gdn_linear_act: y and residual are bf16 or fp32")
     if act not in ACTS:
         raise ValueError(f"gdn_linear_act: an activation of {sorted(ACTS)}")
-    device = rows._here(x, w, bias, y, w_up, bias_up, residual)
-    epilogue = gdn_linear_epilogue(ACTS[act], res_code, scale, rows._dp(w_up), rows._ld(w_up), rows._dp(bias_up), rows._dp(residual), rows._ld(residual))
-    _check(_lib().gdn_linear_act(x.data_ptr(), rows._ld(x), w.data_ptr(), rows._ld(w), rows._dp(bias), ctypes.byref(epilogue), y.data_ptr(), rows._ld(y),
-                                 code, T, N, K, rows._stream_ptr(stream, device)), "gdn_linear_act")
+    (T, K), N = size, weight[0]
+    at_x, ldx = _rows(x, size, bf16, device, name)
+    at_w, ldw = _rows(w, weight, bf16, device, name)
+    at_y, ldy = _rows(y, out, y.dtype, device, name)
+    at_up, ld_up = _rows(w_up, weight, bf16, device, name)
+    at_res, ldr = (None, 0) if residual is None else _rows(residual, out, residual.dtype, device, name)
+    epilogue = gdn_linear_epilogue(ACTS[act], GDN_BF16 if residual is None else _codes[residual.dtype], scale, at_up, ld_up,
+                                   _packed(bias_up, weight[:1], f32, device, name), at_res, ldr)
+    _check(_lib().gdn_linear_act(at_x, ldx, at_w, ldw, _packed(bias, weight[:1], f32, device, name), ctypes.byref(epilogue), at_y, ldy, _codes[y.dtype],
+                                 T, N, K, _stream(stream, device)), name)
 
 
 def gdn_linear_act_plan(T: int, N: int, K: int, gated: bool = False):

@@ -5,7 +5,7 @@ import ctypes
 
 from .binding import GDN_BF16, GDN_F32, _check, lib
 from .linear import ACTS
-from .rows import _dp, _here, _ld, _stream_ptr
+from .rows import _device, _packed, _rows, _stream
 
 _i32, _i64, _vp, _f32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_float
 
@@ -65,21 +65,23 @@ def gdn_moe(shape: gdn_moe_shape, x, w_router, choice_bias, w_gate_up, w_down, a
         import torch
         _types.extend((torch.float32, torch.bfloat16, torch.int32))         # in the order of their codes
     f32, bf16, i32 = _types
-    E, k, D, F, (T, width) = shape.E, shape.k, shape.D, shape.F, x.shape
-    if width != D or y.shape != x.shape or (add is not None and add.shape != x.shape):
-        raise ValueError("gdn_moe: x, add and y are [T][D]")
-    if x.dtype is not bf16 or y.dtype is not bf16 or (add is not None and add.dtype is not bf16):
-        raise ValueError("gdn_moe: x, add and y are bf16")
-    for t, size, dtype in ((w_router, (E, D), f32 if shape.router_dtype == GDN_F32 else bf16), (choice_bias, (E,), f32), (w_gate_up, (E, 2 * F, D), bf16),
-                           (w_down, (E, D, F), bf16), (ids, (T, k), i32), (weights, (T, k), f32)):
-        if t is not None and (t.shape != size or t.dtype is not dtype or not t.is_contiguous()):
-            raise ValueError(f"gdn_moe: a tensor of {dtype} {size} without gaps is needed, not {t.dtype} {tuple(t.shape)}")
-    device = _here(x, w_router, choice_bias, w_gate_up, w_down, add, y, ids, weights, workspace)
-    room = workspace.numel() * workspace.element_size() if workspace is not None else 0
-    if room and not workspace.is_contiguous():
-        raise ValueError("gdn_moe: a workspace without gaps")
-    _check(_lib().gdn_moe(ctypes.byref(shape), x.data_ptr(), _ld(x), _dp(w_router), _dp(choice_bias), _dp(w_gate_up), _dp(w_down), _dp(add), _ld(add),
-                          y.data_ptr(), _ld(y), _dp(ids), _dp(weights), T, _dp(workspace), room, _stream_ptr(stream, device)), "gdn_moe")
+    name, size, device = "gdn_moe", x.shape, _device()
+    E, k, D, F = shape.E, shape.k, shape.D, shape.F
+    if len(size) != 2 or size[1] != D:
+        raise ValueError("gdn_moe: x is [T][D]")
+    T = size[0]
+    at_x, ldx = _rows(x, size, bf16, device, name)
+    at_add, ld_add = _rows(add, size, bf16, device, name)
+    at_y, ldy = _rows(y, size, bf16, device, name)
+    room = 0
+    if workspace is not None:
+        room = workspace.numel() * workspace.element_size()
+        if not workspace.is_contiguous() or workspace.get_device() != device:
+            raise ValueError("gdn_moe: a workspace without gaps on the tensors' device")
+    _check(_lib().gdn_moe(ctypes.byref(shape), at_x, ldx, _packed(w_router, (E, D), f32 if shape.router_dtype == GDN_F32 else bf16, device, name),
+                          _packed(choice_bias, (E,), f32, device, name), _packed(w_gate_up, (E, 2 * F, D), bf16, device, name),
+                          _packed(w_down, (E, D, F), bf16, device, name), at_add, ld_add, at_y, ldy, _packed(ids, (T, k), i32, device, name),
+                          _packed(weights, (T, k), f32, device, name), T, workspace.data_ptr() if room else None, room, _stream(stream, device)), name)
 
 
 def gdn_moe_tune(shape: int) -> int:
