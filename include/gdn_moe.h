@@ -14,7 +14,8 @@
  *     than k may be); a NaN is behind every other key that can be
  *     p[j]   = softmax over all e of l, or sigmoid(l), at the j-th choice; divided by the sum of the k with `normalise` (a
  *              sum of zero leaves zeros); * routed_scale
- *     y[t]   = add[t] + sum_j p[j] * w_down[e_j] (act(gate_(e_j) x[t]) * (up_(e_j) x[t]))
+ *     h[j]   = p[j] * act(gate_(e_j) x[t]) * (up_(e_j) x[t])                   rounded once, to bf16
+ *     y[t]   = add[t] + sum_j w_down[e_j] h[j]
  *
  * A choice whose p[j] is zero is left out of the sum, whatever its expert would give.  A token with a NaN in x has NaN weights and a NaN row y.
  *
@@ -31,8 +32,9 @@
  *   E is 1 .. 1024, k 1 .. min(E, 16), D and F multiples of 64 up to 32768; pointers 16-byte aligned (choice_bias, ids, weights 4), ld
  *   multiples of 8 and at least D.  T = 0 is legal and does nothing.  T k is below 2^24, and x's rows (T ldx) and the experts' inner rows
  *   (T k F) span less than 2^30 elements: longer batches go in parts.
- * Arithmetic: the router's sums in fp64; bf16 products with fp32 sums in the experts; act(gate) * up is rounded to bf16, as the next
- * product's operand; weighted and added in fp32; one rounding to y.
+ * Arithmetic: the router's sums in fp64; bf16 products with fp32 sums in the experts; h is rounded to bf16, as the next product's
+ * operand, behind its weight; the choices are added in fp32; one rounding to y.  (For few tokens a token's choices are summed as one product, for
+ * more each by itself and then in the order of their keys: the same but for the order of fp32 additions.)
  * Errors: GDN_ERR_NULL, _ALIGN, _SHAPE (a size out of its range, an unknown type, activation or score, a routed_scale that is not finite, an ld
  * smaller than D), _COUNT, _WORKSPACE, _SLOT_HAZARD (y, ids, weights or the workspace share a byte with each other or an input, but for y = add).
  */
@@ -66,8 +68,9 @@ int32_t gdn_moe(const gdn_moe_shape *shape, const void *x, int64_t ldx, const vo
                 int32_t *ids, float *weights, int64_t T, void *workspace, int64_t workspace_bytes, void *stream);
 
 /*
- * Tuning knob, not a method step: fixes the tile of the experts' products (0, 2, 3: 128 x 128, 256 x 256, 64 x 64, as gdn_linear_tune; anything
- * else: chosen per call, the default).  Every tile gives the same results.  Process-wide; returns the previous setting (-1 = per call).
+ * Tuning knob, not a method step: fixes the kernels of the experts' products (0, 2, 3: tiles of 128 x 128, 256 x 256, 64 x 64, as gdn_linear_tune; 6: those
+ * of few tokens where T <= 32; anything else: chosen per call, the default).  Every tile gives the same results.  Process-wide; returns the previous
+ * setting (-1 = per call).
  */
 int32_t gdn_moe_tune(int32_t shape);
 

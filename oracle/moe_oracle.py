@@ -2,7 +2,7 @@
 code with the HIP library.
 
 The definition in fp64, token by token and choice by choice, with the three roundings that the definition has (the router's sum and the key to
-fp32, act(gate) * up to bf16), and a bound on what fp32 arithmetic may be off by beside every value.
+fp32, p * act(gate) * up to bf16), and a bound on what fp32 arithmetic may be off by beside every value.
 
 Pins (tests/test_moe.py): a hand-worked case, one expert against the plain gated block, order and ties, keys that are never chosen.
 """
@@ -60,7 +60,7 @@ def route(x, w_router, choice_bias, k, score="softmax", normalise=True, routed_s
 def experts(x, ids, p, ep, w_gate_up, w_down, add, act):
     """(y [T][D], bound of fp32's error) for given choices; a choice of weight zero is left out."""
     T, D = x.shape
-    F = w_down.shape[2]
+    F, K = w_down.shape[2], ids.shape[1]                  # (a sum may go over all choices at once)
     y = np.zeros((T, D)) if add is None else np.array(add, np.float64)
     e = np.zeros((T, D))
     size = np.abs(y)
@@ -72,16 +72,16 @@ def experts(x, ids, p, ep, w_gate_up, w_down, add, act):
         gate, up = (lo.linear(xe, w_gate_up[ex][h]) for h in (slice(0, F), slice(F, 2 * F)))
         eg, eu = ((D + 8) * U23 * (np.abs(xe) @ np.abs(w_gate_up[ex][h]).T) for h in (slice(0, F), slice(F, 2 * F)))
         a, ea = lo.act_with_bound(act, gate, eg)
-        h, eh = a * up, ea * np.abs(up) + np.abs(a) * eu + ea * eu + U23 * np.abs(a * up)
+        w, ew = p[t, j][:, None], ep[t, j][:, None]
+        g, eg = a * up, ea * np.abs(up) + np.abs(a) * eu + ea * eu + U23 * np.abs(a * up)
+        h, eh = w * g, np.abs(w) * eg + ew * (np.abs(g) + eg) + U23 * np.abs(w * g)
         hr = to_bf16(h)
         er = np.maximum(np.abs(to_bf16(h + eh) - hr), np.abs(to_bf16(h - eh) - hr))       # a step where a boundary is within reach
         down = np.abs(w_down[ex])
         o = hr @ w_down[ex].T
-        eo = er @ down.T + (F + 8) * U23 * ((np.abs(hr) + er) @ down.T)
-        w = p[t, j][:, None]
-        y[t] += w * o                                                                      # (a token takes an expert once)
-        e[t] += np.abs(w) * eo + ep[t, j][:, None] * (np.abs(o) + eo) + U23 * np.abs(w * o)
-        size[t] += np.abs(w * o)
+        y[t] += o                                                                          # (a token takes an expert once)
+        e[t] += er @ down.T + (K * F + 8) * U23 * ((np.abs(hr) + er) @ down.T)
+        size[t] += np.abs(o)
     return y, e + 20 * U23 * size
 
 

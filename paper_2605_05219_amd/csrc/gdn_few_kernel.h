@@ -38,8 +38,8 @@ struct Few {
     static constexpr int AHEAD = (S - 1) * LOADS; // loads that may be on their way when a step's have landed
     static_assert(SMEM <= 160 * 1024 && AHEAD < 64, "ring");
 
-    // One step's loads.  They go out for every step slot, also behind the last one (not live, an empty descriptor: nothing is fetched), so that the
-    // number on their way, and with it the wait, is always the same.
+    // One step's loads, k bytes on in the rows.  They go out for every step slot, also behind the last one (not live, an empty descriptor: nothing is fetched), so
+    // that the number on their way, and with it the wait, is always the same.
     static __device__ __forceinline__ void fetch(char* to, int k, const Part& w0, const Part& w1, const Part& x, bool live, const int* xoff, const int* woff) {
 #pragma unroll
         for (int j = 0; j < W_LOADS; ++j) {
@@ -54,10 +54,10 @@ struct Few {
     }
 
     // The sums of a wave's steps over the weight rows, w0's (8 HALF) and then w1's, and rows x.  acc[i RT + j]: lane lr = lane % 16 holds row lr of row tile j,
-    // register e weight row 16 i + 4 (lane / 16) + e.  The steps are walked from `first` on: workgroups that begin at the same k of rows whose pitch is a
-    // power of two ask the same few memory channels (8192 x 8192, 16 rows: 34 us, 26 with 5 steps from one workgroup's beginning to the next's).
-    static __device__ __forceinline__ void sums_of(f32x4* acc, const Part& w0, const Part& w1, const Part& x, int steps, int first, char* ring, int wave, int lane) {
-        auto k_of = [&](int step) { const int s = step + first; return (s >= steps ? s - steps : s) * STEP * 2; };
+    // register e weight row 16 i + 4 (lane / 16) + e.  place(step, w0, w1, x) moves the parts to a step's rows (those of another matrix of the same pitch, for
+    // one) and returns its bytes along k.
+    template <typename PLACE>
+    static __device__ __forceinline__ void sums_of(f32x4* acc, const Part& w0, const Part& w1, const Part& x, int steps, PLACE place, char* ring, int wave, int lane) {
         const int row = lane >> 3, pos = lane & 7;    // of a load: lane i lands at row i / 8, piece i % 8
         int xoff[X_LOADS], woff[W_LOADS];
         // piece p of row r lies at p ^ (r / 2) % 8: 16 rows' pieces of one k then spread over the banks
@@ -66,11 +66,14 @@ struct Few {
 #pragma unroll
         for (int j = 0; j < W_LOADS; ++j)
             woff[j] = (8 * (j >= HALF ? j - HALF : j) + row) * (j >= HALF ? w1.pitch : w0.pitch) + ((pos ^ (((8 * j + row) >> 1) & 7)) << 4);
+        auto load = [&](int slot, int step) {
+            Part v0 = w0, v1 = w1, vx = x;
+            const bool live = step < steps;
+            const int k = live ? place(step, v0, v1, vx) : 0;
+            fetch(ring + slot * STAGE, k, v0, v1, vx, live, xoff, woff);
+        };
 #pragma unroll
-        for (int s = 0; s < S; ++s) {
-            const int step = wave + s * WAVES;
-            fetch(ring + s * STAGE, step < steps ? k_of(step) : 0, w0, w1, x, step < steps, xoff, woff);
-        }
+        for (int s = 0; s < S; ++s) load(s, wave + s * WAVES);
         const int lr = lane & 15, g = lane >> 4, sw = lr >> 1;
         int slot = 0;
         for (int step = wave; step < steps; step += WAVES) {
@@ -88,8 +91,7 @@ struct Few {
             }
             __builtin_amdgcn_s_waitcnt(0xC07F);       // read (lgkmcnt(0)): the slot is free
             asm volatile("" ::: "memory");
-            const int next = step + S * WAVES;
-            fetch(ring + slot * STAGE, next < steps ? k_of(next) : 0, w0, w1, x, next < steps, xoff, woff);
+            load(slot, step + S * WAVES);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll

@@ -224,7 +224,7 @@ __device__ __forceinline__ void act_epilogue(const typename EpiArgs<EPI>::type& 
                 float scale = a.scale;
                 if constexpr (epi_expert(EPI)) {
                     tok = list[tok];
-                    if (EPI == EPI_EXPERT) scale = a.weights[tok];
+                    if (EPI == EPI_EXPERT_GATED) scale = a.weights[tok];
                 }
 #pragma unroll
                 for (int h = 0; h < OPL / 4; ++h) v[h] *= scale;
@@ -602,8 +602,12 @@ __global__ void __launch_bounds__(64 * C::WAVES) gdn_linear_few_kernel(LinearAct
     f32x4 acc[C::CT * C::RT];
 #pragma unroll
     for (int i = 0; i < C::CT * C::RT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    C::sums_of(acc, weights(a.w, a.ldw, n0), GATED ? weights(a.w_up, a.ldw_up, n0) : weights(a.w, a.ldw, n0 + 8 * C::HALF), x, a.K / few::STEP, (int)((uint32_t)tile_n * 5u % (uint32_t)(a.K / few::STEP)), smem + wave * C::RING,
-               wave, lane);
+    // A workgroup begins 5 steps on from the one before it: those that begin at the same k of rows whose pitch is a power of two all ask the same few memory
+    // channels (16 rows, 8192 x 8192: 34 us, 26 so)
+    const int steps = a.K / few::STEP, first = (int)((uint32_t)tile_n * 5u % (uint32_t)steps);
+    C::sums_of(acc, weights(a.w, a.ldw, n0), GATED ? weights(a.w_up, a.ldw_up, n0) : weights(a.w, a.ldw, n0 + 8 * C::HALF), x, steps,
+               [&](int step, few::Part&, few::Part&, few::Part&) { return (step + first >= steps ? step + first - steps : step + first) * few::STEP * 2; },
+               smem + wave * C::RING, wave, lane);
     wait_vm<0>();                                                // (no load of an empty descriptor writes behind the sums)
     __syncthreads();
     f32x4* const sums = reinterpret_cast<f32x4*>(smem);

@@ -18,7 +18,7 @@ struct ExpertProduct {
     const void* w;                 // bf16, per expert [n_w][K]: N rows, or with `gated` N of the gate and N of up
     bool gated;
     int32_t act;
-    const float* weights;          // by listed row: a factor on the outputs (or null)
+    const float* weights;          // by listed row: a factor on the outputs (with `gated`)
     void* y;                       // row v of y for a listed row v, N apart: bf16 with `gated`, else fp32
     const int32_t* list;           // [expert][list_stride]
     int32_t list_stride;

@@ -51,6 +51,30 @@ template <int TT, int TE, int U>
 void launch_logits(const MoeArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((moe_logits_kernel<TT, TE, U>), dim3((unsigned)((a.E + 4 * TE - 1) / (4 * TE)), (unsigned)((a.T + TT - 1) / TT)), dim3(256), 0, stream, a);
 }
+template <typename K>
+hipError_t launch_few_kernel(K kernel, dim3 grid, int threads, int smem, const MoeArgs& a, hipStream_t stream) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, grid, dim3(threads), smem, stream, a);
+    return hipGetLastError();
+}
+hipError_t launch_few(const MoeArgs& a, hipStream_t stream) {
+    const dim3 up((unsigned)(a.F / 16), (unsigned)(a.T * a.k));
+    const int per_lane = (a.E + 63) / 64, threads = 64 * UpFew::WAVES;
+    hipError_t e;
+    if (per_lane <= 1) e = launch_few_kernel(&moe_up_few_kernel<1>, up, threads, UpFew::SMEM, a, stream);
+    else if (per_lane <= 2) e = launch_few_kernel(&moe_up_few_kernel<2>, up, threads, UpFew::SMEM, a, stream);
+    else if (per_lane <= 4) e = launch_few_kernel(&moe_up_few_kernel<4>, up, threads, UpFew::SMEM, a, stream);
+    else if (per_lane <= 8) e = launch_few_kernel(&moe_up_few_kernel<8>, up, threads, UpFew::SMEM, a, stream);
+    else e = launch_few_kernel(&moe_up_few_kernel<16>, up, threads, UpFew::SMEM, a, stream);
+    if (e != hipSuccess) return e;
+    // a narrow output in workgroups of 8 of its rows, so that there is one for every compute unit
+    typedef few::Few<1, 8, 4, 6> D8;
+    typedef few::Few<1, 16, 4, 4> D16;
+    if (a.T * (a.D / 16) < chip_cus()) return launch_few_kernel(&moe_down_few_kernel<D8>, dim3((unsigned)(a.D / 8), (unsigned)a.T), 64 * D8::WAVES, D8::SMEM, a, stream);
+    return launch_few_kernel(&moe_down_few_kernel<D16>, dim3((unsigned)(a.D / 16), (unsigned)a.T), 64 * D16::WAVES, D16::SMEM, a, stream);
+}
+
 template <int P>
 void launch_route(const MoeArgs& a, hipStream_t stream) {
     if constexpr (P <= 8) {                                      // (16 keys a lane do not fit the registers of 16 waves)
@@ -71,16 +95,17 @@ hipError_t launch_products(const MoeArgs& a, int shape, hipStream_t stream) {
     p.list = a.list; p.list_stride = a.T; p.table = a.table; p.n_tiles = a.n_tiles;
     p.most_tiles = (int32_t)(pairs / a.tile_rows + std::min<int64_t>(a.E, pairs));
     p.x = a.x; p.ldx = a.ldx; p.x_rows = a.T; p.div = a.k;
-    p.w = a.w_gate_up; p.gated = true; p.act = a.act;
+    p.w = a.w_gate_up; p.gated = true; p.act = a.act; p.weights = a.weights;
     p.y = a.h; p.N = a.F; p.K = a.D;
     hipError_t e = linear::launch_expert_product(p, shape, stream);
     if (e != hipSuccess) return e;
     p.x = a.h; p.ldx = a.F; p.x_rows = (int32_t)pairs; p.div = 1;
-    p.w = a.w_down; p.gated = false; p.act = GDN_ACT_NONE; p.weights = a.weights;
+    p.w = a.w_down; p.gated = false; p.act = GDN_ACT_NONE; p.weights = nullptr;
     p.y = a.part; p.N = a.D; p.K = a.F;
     return linear::launch_expert_product(p, shape, stream);
 }
 
+constexpr int FEW = 6, FEW_BATCH = 4, MOST_FEW = 32;
 std::atomic<int32_t> g_moe_shape{-1};
 int choose_shape(double rows) { return rows <= 64 ? 3 : rows <= 160 ? 0 : 2; }      // rows of an expert, by an even choice
 
@@ -140,11 +165,12 @@ extern "C" int32_t gdn_moe(const gdn_moe_shape* s, const void* x, int64_t ldx, c
     hipStream_t stream = static_cast<hipStream_t>(stream_);
 
     const int forced = g_moe_shape.load();
-    const int shape = forced >= 0 ? forced : choose_shape((double)T * s->k / s->E);
+    const int shape = forced >= 0 && forced != FEW ? forced : choose_shape((double)T * s->k / s->E);
     a.tile_rows = linear::expert_tile_rows(shape);
     if (T == 1) launch_logits<1, 2, 4>(a, stream);
     else if (T <= 64) launch_logits<2, 2, 2>(a, stream);
     else launch_logits<4, 4, 1>(a, stream);
+    if (forced == FEW ? T <= MOST_FEW : forced < 0 && T <= FEW_BATCH) return hip_err(launch_few(a, stream));
     const int per_lane = (s->E + 63) / 64;
     if (per_lane <= 1) launch_route<1>(a, stream);
     else if (per_lane <= 2) launch_route<2>(a, stream);
@@ -158,5 +184,5 @@ extern "C" int32_t gdn_moe(const gdn_moe_shape* s, const void* x, int64_t ldx, c
 }
 
 extern "C" int32_t gdn_moe_tune(int32_t shape) {
-    return g_moe_shape.exchange(shape == 0 || shape == 2 || shape == 3 ? shape : -1);
+    return g_moe_shape.exchange(shape == 0 || shape == 2 || shape == 3 || shape == FEW ? shape : -1);
 }

@@ -4,6 +4,8 @@
 
 #include <cstdint>
 
+#include "gdn_act.h"
+#include "gdn_few_kernel.h"
 #include "gdn_linear_tiles.h"
 #include "gdn_moe.h"
 
@@ -35,8 +37,8 @@ struct MoeArgs {
     float* weights;               // [T][k]
     int32_t* counts;              // [E]: choices of an expert
     int32_t* list;                // [E][T]: an expert's choices (t k + j)
-    uint16_t* h;                  // [T k][F]
-    float* part;                  // [T k][D]: weighted outputs
+    uint16_t* h;                  // [T k][F]: weighted
+    float* part;                  // [T k][D]: the choices' outputs
     linear::ExpertTile* table;    // tiles of tile_rows rows, an expert's one after the other; n_tiles: how many
     int32_t* n_tiles;
     int32_t tile_rows;
@@ -363,6 +365,102 @@ __global__ void __launch_bounds__(256) moe_sum_kernel(MoeArgs a) {
 #pragma unroll
     for (int q = 0; q < 8; ++q) o[q] = (__bf16)v[q];
     *reinterpret_cast<bf16x8*>(a.y + (int64_t)t * a.ldy + c) = o;
+}
+
+// ---- A few tokens: the choice with the first product, the second one with the sum, in two launches behind the router's sums, by the waves and rings of
+// gdn_few_kernel.h.  A workgroup's time is that of its weights, so that every one of a token's chooses anew (2 us) what a launch of its own would take 4 for.
+typedef few::Few<1, 32, 4, 3> UpFew;
+template <int P>
+__global__ void __launch_bounds__(64 * UpFew::WAVES) moe_up_few_kernel(MoeArgs a) {      // 16 of a choice's F; grid: (F / 16, T k)
+    extern __shared__ __align__(16) char smem[];
+    __shared__ int32_t chosen;
+    __shared__ float weight;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int pair = blockIdx.y, t = pair / a.k, j = pair % a.k, f0 = blockIdx.x * 16;
+    if (wave == 0) {
+        int id;
+        float p;
+        choose<P>(a, t, lane, id, p);
+        if (lane == j) { chosen = p != 0.f ? id : -1; weight = p; }
+        if (lane < a.k && j == 0 && blockIdx.x == 0) {
+            if (a.out_ids) a.out_ids[pair + lane] = id;
+            if (a.out_weights) a.out_weights[pair + lane] = p;
+            a.ids[pair + lane] = p != 0.f ? id : -1;
+        }
+    }
+    __syncthreads();
+    const int e = __builtin_amdgcn_readfirstlane(chosen);
+    if (e < 0) return;
+    const int bytes = 15 * a.D * 2 + a.D * 2;
+    const few::Part gate = {reinterpret_cast<const char*>(a.w_gate_up + ((int64_t)e * 2 * a.F + f0) * a.D), bytes, a.D * 2};
+    const few::Part up = {gate.at + (int64_t)a.F * a.D * 2, bytes, a.D * 2};
+    const few::Part x = {reinterpret_cast<const char*>(a.x + t * a.ldx), a.D * 2, a.D * 2};      // one row: the others of its tile are behind its end, zeros
+    f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    const int steps = a.D / few::STEP, first = (int)((blockIdx.x + 3 * blockIdx.y) * 5u % (uint32_t)steps);
+    UpFew::sums_of(acc, gate, up, x, steps,
+                   [&](int step, few::Part&, few::Part&, few::Part&) { return (step + first >= steps ? step + first - steps : step + first) * few::STEP * 2; },
+                   smem + wave * UpFew::RING, wave, lane);
+    __builtin_amdgcn_s_waitcnt(0x0F70);                          // (no load of an empty descriptor writes behind the sums)
+    __syncthreads();
+    f32x4* const sums = reinterpret_cast<f32x4*>(smem);
+    UpFew::put_sums(acc, sums, wave, lane);
+    __syncthreads();
+    if (threadIdx.x < 4) {
+        const int piece = threadIdx.x;
+        const f32x4 v = weight * (activate(a.act, UpFew::get_sum(sums, 0, piece)) * UpFew::get_sum(sums, 0, piece + 4));
+        *reinterpret_cast<bf16x4*>(a.h + (int64_t)pair * a.F + f0 + 4 * piece) = __builtin_convertvector(v, bf16x4);
+    }
+}
+
+template <typename C>
+__global__ void __launch_bounds__(64 * C::WAVES) moe_down_few_kernel(MoeArgs a) {        // WR of a token's D; grid: (D / WR, T)
+    extern __shared__ __align__(16) char smem[];
+    __shared__ int32_t ids[MAX_K], at[MAX_K];                    // the choices that count, and which they are
+    __shared__ int32_t count;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int t = blockIdx.y, d0 = blockIdx.x * C::WR;
+    if (wave == 0) {
+        const int id = lane < a.k ? a.ids[t * a.k + lane] : -1;
+        const uint64_t in = __ballot(id >= 0);
+        if (id >= 0) {
+            const int n = __popcll(in & ((1ull << lane) - 1));
+            ids[n] = id;
+            at[n] = lane;
+        }
+        if (lane == 0) count = __popcll(in);
+    }
+    __syncthreads();
+    const int per = a.F / few::STEP, n = __builtin_amdgcn_readfirstlane(count), steps = n * per;
+    const int my_id = lane < n ? ids[lane] : 0, my_at = lane < n ? at[lane] : 0;      // (in a lane each: a read of LDS would wait for the loads to LDS)
+    const int64_t expert = (int64_t)a.D * a.F * 2;
+    const few::Part w0 = {reinterpret_cast<const char*>(a.w_down + (int64_t)d0 * a.F), C::WR * a.F * 2, a.F * 2};
+    const few::Part w1 = {w0.at + (int64_t)8 * C::HALF * a.F * 2, w0.bytes - 8 * C::HALF * a.F * 2, a.F * 2};
+    const few::Part x = {reinterpret_cast<const char*>(a.h + (int64_t)t * a.k * a.F), a.F * 2, a.F * 2};
+    f32x4 acc[C::CT];
+#pragma unroll
+    for (int i = 0; i < C::CT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int first = steps ? (int)(blockIdx.x * 5u % (uint32_t)steps) : 0;
+    C::sums_of(acc, w0, w1, x, steps,
+               [&](int step, few::Part& v0, few::Part& v1, few::Part& vx) {
+                   const int s = step + first >= steps ? step + first - steps : step + first, j = s / per;
+                   const int64_t skip = from_lane(my_id, j) * expert;
+                   v0.at += skip;
+                   v1.at += skip;
+                   vx.at += (int64_t)from_lane(my_at, j) * a.F * 2;
+                   return (s - j * per) * few::STEP * 2;
+               },
+               smem + wave * C::RING, wave, lane);
+    __builtin_amdgcn_s_waitcnt(0x0F70);
+    __syncthreads();
+    f32x4* const sums = reinterpret_cast<f32x4*>(smem);
+    C::put_sums(acc, sums, wave, lane);
+    __syncthreads();
+    if (threadIdx.x < C::WR / 4) {
+        const int d = d0 + 4 * threadIdx.x;
+        f32x4 v = C::get_sum(sums, 0, threadIdx.x);
+        if (a.add) v += __builtin_convertvector(*reinterpret_cast<const bf16x4*>(a.add + t * a.ld_add + d), f32x4);
+        *reinterpret_cast<bf16x4*>(a.y + t * a.ldy + d) = __builtin_convertvector(v, bf16x4);
+    }
 }
 
 }  // namespace moe

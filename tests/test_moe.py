@@ -335,16 +335,39 @@ def knob():
 
 
 def test_knob_round_trip(knob):
-    assert [knob(v) for v in (0, 2, 3, 1, 2, 9)] == [-1, 0, 2, 3, -1, 2]
+    assert [knob(v) for v in (0, 2, 3, 6, 1, 2, 9)] == [-1, 0, 2, 3, 6, -1, 2]
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("shape", [0, 2, 3])
-@pytest.mark.parametrize("T,E,k,D,F,bias", [(1, 8, 2, 64, 64, None), (40, 60, 4, 320, 192, None), (700, 8, 3, 256, 320, None), (300, 20, 4, 128, 64, "one"), (90, 130, 10, 192, 128, None)])
+@pytest.mark.parametrize("shape", [0, 2, 3, 6])
+@pytest.mark.parametrize("T,E,k,D,F,bias", [(1, 8, 2, 64, 64, None), (3, 600, 5, 128, 64, None), (30, 60, 4, 320, 192, None), (32, 300, 16, 4160, 64, None), (700, 8, 3, 256, 320, None),
+                                            (300, 20, 4, 128, 64, "one"), (90, 130, 10, 192, 128, None)])
 def test_every_kernel(knob, shape, T, E, k, D, F, bias):
-    """The tiles on experts of no row, of part of a tile and of several, and where all tokens take the same ones."""
+    """The tiles on experts of no row, of part of a tile and of several, and where all tokens take the same ones; the kernels of few tokens up to their most."""
+    if shape == 6 and T > 32:
+        pytest.skip("few tokens are at most 32")
     if bias:
         bias = np.zeros(E)
         bias[[2, E - 1]] = 50
     knob(shape)
     Call(T, E, k, D, F, "gelu_tanh", bias=bias, add=True, pad=8, seed=T).run().check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [3, 6])
+@pytest.mark.parametrize("T", [1, 7])
+def test_masks_and_zero_weights_in_every_path(knob, shape, T):
+    """Fewer than k choices, none, and a weight of zero in front of and between choices that count."""
+    knob(shape)
+    for left in (0, 1, 3):
+        bias = np.full(70, -np.inf)
+        bias[[3, 11, 69][:left]] = 0
+        c = Call(T, 70, 4, 128, 128, "silu", "sigmoid", False, 1.5, bias=bias, add=True, seed=left)
+        c.gu[0] = float("nan")
+        c.run().check()
+    c = Call(T, 12, 4, 64, 64, score="sigmoid", normalise=False, bias=np.array([3.0, 0, 2, 0, 1, 0, 0, 0, 0, 0, 0, 0.5]))
+    c.x[:] = 1
+    c.wr[[0, 4]] = -64                                                # chosen by their bias, weights that underflow
+    c.gu[0] = c.down[4] = float("inf")
+    c.run().check()
+    assert c.ids[0, :3].tolist() == [0, 2, 4] and c.weights[0, 0] == 0 and c.weights[0, 2] == 0
