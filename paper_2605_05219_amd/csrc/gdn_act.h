@@ -18,7 +18,7 @@ __device__ __forceinline__ float gelu(float z) {
     q = fmaf(t, q, -0.284496736f);
     q = fmaf(t, q, 0.254829592f);
     q *= 0.5f * t * __expf(-x * x);
-    return z < 0.f ? z * q : z - z * q;
+    return z < 0.f ? z * q : z < 1e30f ? z - z * q : z;          // (q is zero from 14 on, and an infinity times zero no number)
 }
 
 // f(z) of four values in fp32.  exp and the reciprocal are the hardware's (one part in 2^22 each at most); a NaN stays a NaN.  `act` is the same on

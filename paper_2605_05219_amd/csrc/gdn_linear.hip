@@ -569,8 +569,8 @@ gdn_linear_kernel(typename EpiArgs<EPI>::type a) {
 
 template <typename CFG, bool OUT_BF16, int EPI>
 hipError_t launch_linear(typename EpiArgs<EPI>::type a, hipStream_t stream) {
-    static hipError_t attr_err = hipFuncSetAttribute(reinterpret_cast<const void*>(&gdn_linear_kernel<CFG, OUT_BF16, EPI>),
-                                                     hipFuncAttributeMaxDynamicSharedMemorySize, CFG::SMEM);
+    static std::atomic<uint64_t> done{0};
+    const hipError_t attr_err = allow_lds(reinterpret_cast<const void*>(&gdn_linear_kernel<CFG, OUT_BF16, EPI>), CFG::SMEM, done);
     if (attr_err != hipSuccess) return attr_err;
     const int64_t tiles_m = epi_expert(EPI) ? a.T : (a.T + CFG::BM - 1) / CFG::BM;      // (the experts' T: how many tiles there can be)
     constexpr int BNO = epi_gated(EPI) ? CFG::BN / 2 : CFG::BN;
@@ -643,8 +643,8 @@ __global__ void __launch_bounds__(64 * C::WAVES) gdn_linear_few_kernel(LinearAct
 
 template <typename C, bool OUT_BF16, bool GATED>
 hipError_t launch_few_kernel(LinearActArgs a, hipStream_t stream) {
-    static hipError_t attr_err = hipFuncSetAttribute(reinterpret_cast<const void*>(&gdn_linear_few_kernel<C, OUT_BF16, GATED>),
-                                                     hipFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+    static std::atomic<uint64_t> done{0};
+    const hipError_t attr_err = allow_lds(reinterpret_cast<const void*>(&gdn_linear_few_kernel<C, OUT_BF16, GATED>), C::SMEM, done);
     if (attr_err != hipSuccess) return attr_err;
     constexpr int OUTS = GATED ? C::WR / 2 : C::WR;
     a.tiles_n = (a.N + OUTS - 1) / OUTS;

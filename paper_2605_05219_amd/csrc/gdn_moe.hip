@@ -49,30 +49,34 @@ Layout layout(const gdn_moe_shape& s, int64_t T) {
 
 template <int TT, int TE, int U>
 void launch_logits(const MoeArgs& a, hipStream_t stream) {
-    hipLaunchKernelGGL((moe_logits_kernel<TT, TE, U>), dim3((unsigned)((a.E + 4 * TE - 1) / (4 * TE)), (unsigned)((a.T + TT - 1) / TT)), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((moe_logits_few_kernel<TT, TE, U>), dim3((unsigned)((a.E + 4 * TE - 1) / (4 * TE)), (unsigned)((a.T + TT - 1) / TT)), dim3(256), 0, stream, a);
 }
-template <typename K>
-hipError_t launch_few_kernel(K kernel, dim3 grid, int threads, int smem, const MoeArgs& a, hipStream_t stream) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, smem);
+template <void (*KERNEL)(MoeArgs)>
+hipError_t launch_few_kernel(dim3 grid, int waves, int smem, const MoeArgs& a, hipStream_t stream) {
+    static std::atomic<uint64_t> done{0};
+    const hipError_t e = allow_lds(reinterpret_cast<const void*>(KERNEL), smem, done);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, grid, dim3(threads), smem, stream, a);
+    hipLaunchKernelGGL(KERNEL, grid, dim3(64 * waves), smem, stream, a);
     return hipGetLastError();
 }
+template <int P>
+hipError_t launch_up_few(const MoeArgs& a, hipStream_t stream) {
+    return launch_few_kernel<moe_up_few_kernel<P>>(dim3((unsigned)(a.F / 16), (unsigned)(a.T * a.k)), UpFew::WAVES, UpFew::SMEM, a, stream);
+}
+template <typename C>
+hipError_t launch_down_few(const MoeArgs& a, hipStream_t stream) {
+    return launch_few_kernel<moe_down_few_kernel<C>>(dim3((unsigned)(a.D / C::WR), (unsigned)a.T), C::WAVES, C::SMEM, a, stream);
+}
 hipError_t launch_few(const MoeArgs& a, hipStream_t stream) {
-    const dim3 up((unsigned)(a.F / 16), (unsigned)(a.T * a.k));
-    const int per_lane = (a.E + 63) / 64, threads = 64 * UpFew::WAVES;
-    hipError_t e;
-    if (per_lane <= 1) e = launch_few_kernel(&moe_up_few_kernel<1>, up, threads, UpFew::SMEM, a, stream);
-    else if (per_lane <= 2) e = launch_few_kernel(&moe_up_few_kernel<2>, up, threads, UpFew::SMEM, a, stream);
-    else if (per_lane <= 4) e = launch_few_kernel(&moe_up_few_kernel<4>, up, threads, UpFew::SMEM, a, stream);
-    else if (per_lane <= 8) e = launch_few_kernel(&moe_up_few_kernel<8>, up, threads, UpFew::SMEM, a, stream);
-    else e = launch_few_kernel(&moe_up_few_kernel<16>, up, threads, UpFew::SMEM, a, stream);
+    const int per_lane = (a.E + 63) / 64;
+    const hipError_t e = per_lane <= 1   ? launch_up_few<1>(a, stream)
+                         : per_lane <= 2 ? launch_up_few<2>(a, stream)
+                         : per_lane <= 4 ? launch_up_few<4>(a, stream)
+                         : per_lane <= 8 ? launch_up_few<8>(a, stream)
+                                         : launch_up_few<16>(a, stream);
     if (e != hipSuccess) return e;
     // a narrow output in workgroups of 8 of its rows, so that there is one for every compute unit
-    typedef few::Few<1, 8, 4, 6> D8;
-    typedef few::Few<1, 16, 4, 4> D16;
-    if (a.T * (a.D / 16) < chip_cus()) return launch_few_kernel(&moe_down_few_kernel<D8>, dim3((unsigned)(a.D / 8), (unsigned)a.T), 64 * D8::WAVES, D8::SMEM, a, stream);
-    return launch_few_kernel(&moe_down_few_kernel<D16>, dim3((unsigned)(a.D / 16), (unsigned)a.T), 64 * D16::WAVES, D16::SMEM, a, stream);
+    return a.T * (a.D / 16) < chip_cus() ? launch_down_few<few::Few<1, 8, 4, 6>>(a, stream) : launch_down_few<few::Few<1, 16, 4, 4>>(a, stream);
 }
 
 template <int P>
@@ -84,7 +88,11 @@ void launch_route(const MoeArgs& a, hipStream_t stream) {
         }
     }
     hipLaunchKernelGGL((moe_route_kernel<P>), dim3((unsigned)((a.T + 3) / 4)), dim3(256), 0, stream, a);
-    hipLaunchKernelGGL(moe_lists_kernel, dim3((unsigned)a.E), dim3(256), 0, stream, a);
+    if ((int64_t)a.T * a.k <= FEW_PAIRS) {
+        hipLaunchKernelGGL(moe_lists_few_kernel, dim3(1), dim3(MAX_E), 0, stream, a);
+        return;
+    }
+    hipLaunchKernelGGL(moe_lists_kernel, dim3((unsigned)a.E), dim3(64 * LIST_WAVES), 0, stream, a);
     hipLaunchKernelGGL(moe_table_kernel, dim3(1), dim3(MAX_E), 0, stream, a);
 }
 
@@ -105,7 +113,14 @@ hipError_t launch_products(const MoeArgs& a, int shape, hipStream_t stream) {
     return linear::launch_expert_product(p, shape, stream);
 }
 
-constexpr int FEW = 6, FEW_BATCH = 4, MOST_FEW = 32;
+constexpr int FEW = 6, MOST_FEW = 32;
+// The kernels of few tokens save launches, some 10 us, and read an expert once for every token that chooses it (though not from memory).  us, theirs / tiles of 64 x 64, by tokens:
+// 128 experts, k 8, D 2048, F 768: 1 28 / 38, 4 63 / 74, 6 89 / 94, 8 110 / 112, 12 154 / 141; 16, 2, 4096, 2048: 2 48 / 60, 4 79 / 97, 8 134 / 132.
+bool few_pays(const gdn_moe_shape& s, int64_t T) {
+    const double choices = (double)T * s.k, distinct = s.E * (1.0 - std::pow(1.0 - (double)s.k / s.E, (double)T));
+    return (choices - distinct) * 6.0 * s.D * s.F <= 10.0 * 5.3e6;
+}
+
 std::atomic<int32_t> g_moe_shape{-1};
 int choose_shape(double rows) { return rows <= 64 ? 3 : rows <= 160 ? 0 : 2; }      // rows of an expert, by an even choice
 
@@ -168,9 +183,9 @@ extern "C" int32_t gdn_moe(const gdn_moe_shape* s, const void* x, int64_t ldx, c
     const int shape = forced >= 0 && forced != FEW ? forced : choose_shape((double)T * s->k / s->E);
     a.tile_rows = linear::expert_tile_rows(shape);
     if (T == 1) launch_logits<1, 2, 4>(a, stream);
-    else if (T <= 64) launch_logits<2, 2, 2>(a, stream);
-    else launch_logits<4, 4, 1>(a, stream);
-    if (forced == FEW ? T <= MOST_FEW : forced < 0 && T <= FEW_BATCH) return hip_err(launch_few(a, stream));
+    else if (T * E <= 16384) launch_logits<2, 2, 2>(a, stream);
+    else hipLaunchKernelGGL(moe_logits_kernel<8>, dim3((unsigned)((E + 15) / 16), (unsigned)((T + 15) / 16)), dim3(64 * 8), 0, stream, a);
+    if (forced == FEW ? T <= MOST_FEW : forced < 0 && T <= MOST_FEW && few_pays(*s, T)) return hip_err(launch_few(a, stream));
     const int per_lane = (s->E + 63) / 64;
     if (per_lane <= 1) launch_route<1>(a, stream);
     else if (per_lane <= 2) launch_route<2>(a, stream);

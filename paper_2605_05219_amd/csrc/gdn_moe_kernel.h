@@ -81,13 +81,14 @@ __device__ __forceinline__ double wave_total(double v) {
     return moved_add<0x143, 0xc>(v);
 }
 
-// ---- the router's sums.  A wave makes TE experts x TT tokens, its lanes along D, 8 elements at a time.  The sums decide a choice, so
-// that one in fp32, whose error changes with the order of its terms, would let the choice hang on how the work is split: in fp64 a sum of products of two bf16
-// numbers is exact but for terms 2^30 times smaller than the largest, whatever the order, and equal rows of w_router give equal keys.
+// ---- the router's sums.  The sums decide a choice, so that one in fp32, whose error changes with the order of its terms, would let the choice hang on how the
+// work is split: in fp64 a sum of products of two bf16 numbers is exact but for terms 2^30 times smaller than the largest, whatever the order, and equal rows of
+// w_router give equal keys.
 //
-// U pieces of a row are on their way at once: with one the time of a single token is the latency of D / 512 loads in a row.
+// Few tokens: a wave makes TE experts x TT tokens, its lanes along D, 8 elements at a time, U such pieces of a row on their way at once: the time of a single token is
+// the latency of its loads (128 experts 5 us).
 template <int TT, int TE, int U>
-__global__ void __launch_bounds__(256) moe_logits_kernel(MoeArgs a) {
+__global__ void __launch_bounds__(256) moe_logits_few_kernel(MoeArgs a) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int t0 = blockIdx.y * TT, e0 = (blockIdx.x * 4 + wave) * TE;
     if (e0 >= a.E) return;
@@ -146,6 +147,60 @@ __global__ void __launch_bounds__(256) moe_logits_kernel(MoeArgs a) {
             const double v = wave_total(acc[i][j]);
             if (lane == 63 && e0 + i < a.E && t0 + j < a.T) a.logits[(int64_t)(t0 + j) * a.E + e0 + i] = (float)v;
         }
+}
+
+// More: a workgroup makes 16 experts x 16 tokens on v_mfma_f64_16x16x4_f64 (lane: row lane % 16 of either operand and one k of its group of 16 lanes; of the result
+// token lane % 16, register r expert lane / 16 + 4 r), its waves the blocks of 32 k in turn: a lane loads 8 adjacent elements of each row, and which k a product
+// pairs is the same for both.  Making fp64 of the elements is what the vector units spend most on, and a matrix product takes sixteen uses of each: 200 tokens x 512
+// experts 16 us, 2048 x 64 17 (by 4 x 4 on the vector units 27 and 35; 1 x 128 8.5, 64 x 128 9.6 against 5 and 7.5 of the kernel above).
+template <int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) moe_logits_kernel(MoeArgs a) {
+    typedef double f64x4 __attribute__((ext_vector_type(4)));
+    __shared__ f64x4 sums[WAVES][64];
+    constexpr int U = 4;                                          // blocks on their way
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lr = lane & 15, g = lane >> 4;
+    const int e0 = blockIdx.x * 16, t0 = blockIdx.y * 16;
+    // (rows past the end are the last one's: their sums go nowhere)
+    const uint16_t* const x = a.x + (int64_t)min(t0 + lr, a.T - 1) * a.ldx + 8 * g;
+    const int64_t w = (int64_t)min(e0 + lr, a.E - 1) * a.D + 8 * g;
+    f64x4 acc = {0.0, 0.0, 0.0, 0.0};
+    const int blocks = a.D / 32;
+    for (int b0 = wave; b0 < blocks; b0 += WAVES * U) {
+        u32x4 xr[U], wr[U][2];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int b = b0 + u * WAVES;
+            xr[u] = wr[u][0] = wr[u][1] = u32x4{0, 0, 0, 0};
+            if (b >= blocks) continue;
+            xr[u] = *reinterpret_cast<const u32x4*>(x + 32 * b);
+            if (a.router_f32) {
+                const u32x4* p = reinterpret_cast<const u32x4*>(static_cast<const float*>(a.w_router) + w + 32 * b);
+                wr[u][0] = p[0];
+                wr[u][1] = p[1];
+            } else {
+                wr[u][0] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.w_router) + w + 32 * b);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (b0 + u * WAVES >= blocks) break;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const uint32_t half = q & 1 ? wr[u][0][q / 2] & 0xffff0000u : wr[u][0][q / 2] << 16;
+                const float wv = __uint_as_float(a.router_f32 ? wr[u][q / 4][q % 4] : half);
+                const float xv = __uint_as_float(q & 1 ? xr[u][q / 2] & 0xffff0000u : xr[u][q / 2] << 16);
+                acc = __builtin_amdgcn_mfma_f64_16x16x4f64((double)wv, (double)xv, acc, 0, 0, 0);
+            }
+        }
+    }
+    sums[wave][lane] = acc;
+    __syncthreads();
+    if (threadIdx.x >= 256) return;
+    const int from = threadIdx.x >> 2, r = threadIdx.x & 3;
+    double v = sums[0][from][r];
+    for (int i = 1; i < WAVES; ++i) v += sums[i][from][r];
+    const int t = t0 + (from & 15), e = e0 + (from >> 4) + 4 * r;
+    if (t < a.T && e < a.E) a.logits[(int64_t)t * a.E + e] = (float)v;
 }
 
 // ---- the choice, a wave to a token.  Lane l holds the keys of experts P l .. P l + P - 1 as whole numbers of the same order, so that of the lanes with the
@@ -266,7 +321,7 @@ __device__ __forceinline__ void make_table(const MoeArgs& a, int n, int32_t* bef
 
 // Few tokens: choices, lists and tile table in one workgroup, a wave to a token.  An expert's list is in no order there: a row of a product
 // is the same whatever rows stand beside it.
-constexpr int FEW_TOKENS = 64;
+constexpr int FEW_TOKENS = 16;
 template <int P>
 __global__ void __launch_bounds__(MAX_E) moe_route_few_kernel(MoeArgs a) {
     __shared__ int32_t kept[FEW_TOKENS * MAX_K], counts[MAX_E], before[MAX_E / 64];
@@ -288,14 +343,31 @@ __global__ void __launch_bounds__(256) moe_route_kernel(MoeArgs a) {
     const int t = blockIdx.x * 4 + (threadIdx.x >> 6);
     if (t < a.T) choose_and_keep<P>(a, t, threadIdx.x & 63, nullptr);
 }
-// ... the lists, a workgroup to an expert, which looks through all choices (a counter that the tokens of all workgroups add to is
+// ... the lists and the table of a moderate number of choices, in one workgroup ...
+constexpr int FEW_PAIRS = 4096;
+__global__ void __launch_bounds__(MAX_E) moe_lists_few_kernel(MoeArgs a) {
+    __shared__ int32_t counts[MAX_E], before[MAX_E / 64];
+    const int tid = threadIdx.x, pairs = a.T * a.k;
+    int id[FEW_PAIRS / MAX_E];
+#pragma unroll
+    for (int i = 0; i < FEW_PAIRS / MAX_E; ++i) id[i] = tid + i * MAX_E < pairs ? a.ids[tid + i * MAX_E] : -1;
+    counts[tid] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < FEW_PAIRS / MAX_E; ++i)
+        if (id[i] >= 0) a.list[(int64_t)id[i] * a.T + atomicAdd(counts + id[i], 1)] = tid + i * MAX_E;
+    __syncthreads();
+    make_table(a, counts[tid], before);
+}
+// ... of more the lists, a workgroup to an expert, which looks through all choices (a counter that the tokens of all workgroups add to is
 // slower: 12288 choices of 64 experts 37 us) ...
-__global__ void __launch_bounds__(256) moe_lists_kernel(MoeArgs a) {
-    __shared__ int32_t found[4];
+constexpr int LIST_WAVES = 16;
+__global__ void __launch_bounds__(64 * LIST_WAVES) moe_lists_kernel(MoeArgs a) {
+    __shared__ int32_t found[LIST_WAVES];
     const int e = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pairs = a.T * a.k;
     int32_t* list = a.list + (int64_t)e * a.T;
     int n = 0;
-    for (int p0 = 0; p0 < pairs; p0 += 1024) {                   // four to a thread
+    for (int p0 = 0; p0 < pairs; p0 += 256 * LIST_WAVES) {       // four to a thread
         const int p = p0 + 4 * threadIdx.x;
         int id[4], mine = 0;
 #pragma unroll
@@ -317,7 +389,8 @@ __global__ void __launch_bounds__(256) moe_lists_kernel(MoeArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (id[i] == e) list[at++] = p + i;
-        n += found[0] + found[1] + found[2] + found[3];
+#pragma unroll
+        for (int w = 0; w < LIST_WAVES; ++w) n += found[w];
     }
     if (threadIdx.x == 0) a.counts[e] = n;
 }

@@ -2,6 +2,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 
 #include "gdn_resume.h"
@@ -50,6 +51,18 @@ inline int chip_cus() {
         return cus;
     }();
     return n;
+}
+
+// Lets a kernel have more than 64 KiB of LDS, once for each device that it is launched on; `done`: the kernel's own.
+inline hipError_t allow_lds(const void* kernel, int bytes, std::atomic<uint64_t>& done) {
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (done.load(std::memory_order_acquire) & bit) return hipSuccess;
+    e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == hipSuccess) done.fetch_or(bit, std::memory_order_release);
+    return e;
 }
 
 inline bool dtype_known(int32_t t) { return t == GDN_F32 || t == GDN_BF16; }

@@ -28,6 +28,8 @@ def _stream(stream, device):
             return None
         if _raw_stream is not None:
             return _raw_stream(device)
+    if getattr(stream, "device_index", device) != device:
+        raise ValueError(f"a stream of device {device} is needed, not of {stream.device}")
     return _stream_object_ptr(stream)
 
 

@@ -226,6 +226,28 @@ def test_values_that_are_not_finite_stay_in_their_row(T):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("act", list(LN.ACTS))
+@pytest.mark.parametrize("T", [3, 200])
+def test_activations_at_their_ends(act, T):
+    """Sums of zero, of either sign far out, and infinite: what the formula's limits are (an infinity times zero is NaN)."""
+    import torch
+    K, N = 64, 8                                                      # (rows of y are whole groups of four)
+    x, w = torch.zeros(T, K, device="cuda", dtype=torch.bfloat16), torch.zeros(N, K, device="cuda", dtype=torch.bfloat16)
+    x[:, 0] = 1
+    z = [0.0, 50.0, -50.0, 1e30, -1e30, float("inf"), 1.0, -1.0]
+    w[:, 0] = torch.tensor(z, device="cuda")
+    x[:, 1:], w[:, 1:] = 0, 0
+    y = torch.empty(T, N, device="cuda")
+    LN.gdn_linear_act(x, w, None, y, act)
+    zb = w[:, 0].double()
+    with np.errstate(all="ignore"):
+        want = {"none": zb, "silu": torch.nn.functional.silu(zb), "gelu": torch.nn.functional.gelu(zb), "gelu_tanh": torch.nn.functional.gelu(zb, approximate="tanh"),
+                "relu": torch.relu(zb), "relu2": torch.relu(zb) ** 2, "sigmoid": torch.sigmoid(zb)}[act].float()
+    torch.cuda.synchronize()
+    assert torch.allclose(y, want.expand(T, N), rtol=1e-5, atol=1e-12, equal_nan=True), (y[0], want)
+
+
+@pytest.mark.gpu
 def test_rows_whose_offsets_pass_32_bits():
     import torch
     T, wide = 70000, 32768
