@@ -4,7 +4,7 @@
 // bounds it.  A row is held in registers from its loads to its stores, 8 adjacent elements to a piece (16 bytes of bf16), so that neither the squares of
 // what the mean leaves nor the second norm read it again: one piece to a thread and as many waves as the row has pieces for, up to 16 (rows of up to 8192), then two or
 // four.  A norm costs one barrier.  8192 rows of 2048 in bf16, the norm in front alone, 26 us (134 MB: 5.2 TB/s, a plain copy of 2 GiB 4.9), with
-// one behind the block and a gate per channel 32; 1777 rows of 5120, two layer norms with a gate per element and a stream in fp32, 38 (3.3 TB/s: a row's two norms wait for
+// one behind the block and a gate per channel 30; 1777 rows of 5120, two layer norms with a gate per element and a stream in fp32, 39 (3.3 TB/s: a row's two norms wait for
 // each other, and with ten waves to a row a compute unit has two rows at once); a single row 2.4, which a call's host time of 8 covers.
 #include <hip/hip_runtime.h>
 
@@ -124,6 +124,12 @@ __device__ __forceinline__ void normalise(f32x8 (&v)[PIECES], int kind, const We
         return (float)n;
     };
     const bool layer = kind == GDN_NORM_LAYER;
+    f32x8 b[PIECES];                                             // (asked for in front of the sums, not behind the barrier)
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        b[i] = f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (bias && first + i * stride < a.D) b[i] = fetch_f32(bias + first + i * stride);
+    }
     Parts mine = {0.f, 0.f};
     float own = 0.f;
     if (layer) {
@@ -161,12 +167,9 @@ __device__ __forceinline__ void normalise(f32x8 (&v)[PIECES], int kind, const We
     const float inv = 1.f / sqrtf(squares * a.inv_d + eps);
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-        const int c = first + i * stride;
-        if (c >= a.D) continue;
-        f32x8 b = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (bias) b = fetch_f32(bias + c);
+        if (first + i * stride >= a.D) continue;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] = fmaf((v[i][e] - mean) * inv, q.w[i][e], b[e]);
+        for (int e = 0; e < 8; ++e) v[i][e] = fmaf((v[i][e] - mean) * inv, q.w[i][e], b[i][e]);
     }
 }
 

@@ -122,7 +122,10 @@ bool few_pays(const gdn_moe_shape& s, int64_t T) {
 }
 
 std::atomic<int32_t> g_moe_shape{-1};
-int choose_shape(double rows) { return rows <= 64 ? 3 : rows <= 160 ? 0 : 2; }      // rows of an expert, by an even choice
+// By the rows of an expert, if the choice is even: tiles of 64 x 64 stream the weights through the most loads on their way (64 experts, k 6, D 2048, F 1408: 512 tokens, 48
+// rows, 271 us, 274 of 128 x 128, 331 of 256 x 256), the larger read them for fewer row tiles each (96 rows 365 / 301 / 353, 144 477 / 420 / 380, 768 1826 / 1231 / 1099; 128
+// experts, k 8, F 768 at 128 rows 526 / 453 / 474).
+int choose_shape(double rows) { return rows <= 48 ? 3 : rows <= 130 ? 0 : 2; }
 
 }  // namespace moe
 }  // namespace gdn
