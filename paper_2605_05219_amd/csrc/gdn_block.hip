@@ -3,9 +3,10 @@
 // s = r + scale g N_post(y), x = N_pre(s): a few flops for every element read or written once, so memory traffic is all that
 // bounds it.  A row is held in registers from its loads to its stores, 8 adjacent elements to a piece (16 bytes of bf16), so that neither the squares of
 // what the mean leaves nor the second norm read it again: one piece to a thread and as many waves as the row has pieces for, up to 16 (rows of up to 8192), then two or
-// four.  A norm costs one barrier.  8192 rows of 2048 in bf16, the norm in front alone, 26 us (134 MB: 5.2 TB/s, a plain copy of 2 GiB 4.9), with
-// one behind the block and a gate per channel 30; 1777 rows of 5120, two layer norms with a gate per element and a stream in fp32, 39 (3.3 TB/s: a row's two norms wait for
-// each other, and with ten waves to a row a compute unit has two rows at once); a single row 2.4, which a call's host time of 8 covers.
+// four.  A norm costs one barrier, and few instructions: the vector units, 4 clocks to each instruction of a wave, are not far behind the memory (with the waves' sums added up by every
+// thread, and divisions, 928 instructions for 8 elements of two layer norms kept them busy for three quarters of the time: 1777 rows of 5120 43 us, now 32).  8192 rows of 2048 in
+// bf16, the norm in front alone, 26 us (134 MB: 5.2 TB/s, a plain copy of 2 GiB 4.9), with one behind the block and a gate per channel 28; 1777 rows of 5120 out of wider
+// buffers, two layer norms with a gate per element and a stream in fp32, 32 (127 MB: 3.9 TB/s); 4096 rows of 8192 50; a single row 2.4, which a call's host time of 7 covers.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -92,7 +93,7 @@ __device__ __forceinline__ float wave_sum(float v) {
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
 }
 constexpr int MAX_WAVES = 16;
-struct Parts { float sum, squares; };
+struct alignas(16) Parts { float sum, mean, squares, count; };
 
 // A norm's weights (with their offset) for a thread's pieces.
 template <int PIECES>
@@ -110,66 +111,64 @@ __device__ __forceinline__ void fetch_weights(Weights<PIECES>& q, const float* w
     }
 }
 
-// v <- N(v) over the row.  Every wave takes the mean of its own elements and the squares of what that leaves; the waves' meet in LDS behind one barrier, in
-// order, the squares about the row's mean by  sum (v - m)^2 = sum over waves of (sum (v - m_w)^2 + n_w (m_w - m)^2).  `part`: two sets, between which
+// v <- N(v) over the row.  Every wave takes the mean of its own elements and the squares of what that leaves; the waves' meet in LDS behind one barrier,
+// a wave's to a lane, the squares about the row's mean by  sum (v - m)^2 = sum over waves of (sum (v - m_w)^2 + n_w (m_w - m)^2).  `part`: two sets, between which
 // `turn` alternates, so one barrier is enough for each norm.  The same on every thread, and the same whenever it runs.
 template <int PIECES>
 __device__ __forceinline__ void normalise(f32x8 (&v)[PIECES], int kind, const Weights<PIECES>& q, const float* bias, float eps, const BlockArgs& a, int first, int stride,
                                           Parts (*part)[MAX_WAVES], int& turn, int wave) {
     const int waves = a.waves;
-    auto count = [&](int w) {                                    // elements of a wave
-        int n = 0;
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i) n += min(max(a.D - i * stride - w * 512, 0), 512);
-        return (float)n;
-    };
     const bool layer = kind == GDN_NORM_LAYER;
-    f32x8 b[PIECES];                                             // (asked for in front of the sums, not behind the barrier)
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-        b[i] = f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (bias && first + i * stride < a.D) b[i] = fetch_f32(bias + first + i * stride);
-    }
-    Parts mine = {0.f, 0.f};
-    float own = 0.f;
+    // the biases: asked for in front of the sums, not behind the barrier, where there are registers for them
+    f32x8 early = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (PIECES == 1 && bias && first < a.D) early = fetch_f32(bias + first);
+    Parts mine = {0.f, 0.f, 0.f, 0.f};
     if (layer) {
+        int n = 0;                                               // the wave's elements
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) n += min(max(a.D - i * stride - (waves == 1 ? 0 : wave * 512), 0), 512);
+        mine.count = (float)n;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e) mine.sum += v[i][e];     // (pieces behind the row's end hold zeros)
         mine.sum = wave_sum(mine.sum);
-        own = mine.sum / count(waves == 1 ? 0 : wave);
+        mine.mean = mine.sum * (n == 512 ? 1.f / 512.f : __builtin_amdgcn_rcpf(mine.count));
     }
 #pragma unroll
     for (int i = 0; i < PIECES; ++i)
         if (first + i * stride < a.D)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) mine.squares = fmaf(v[i][e] - own, v[i][e] - own, mine.squares);
+            for (int e = 0; e < 8; ++e) {
+                const float d = v[i][e] - mine.mean;
+                mine.squares = fmaf(d, d, mine.squares);
+            }
     mine.squares = wave_sum(mine.squares);
-    float mean = own, squares = mine.squares;
+    float mean = mine.mean, squares = mine.squares;
     if (waves > 1) {
+        const int lane = threadIdx.x & 63;
         Parts* p = part[turn];
         turn ^= 1;
-        if ((threadIdx.x & 63) == 0) p[wave] = mine;
+        if (lane == 0) p[wave] = mine;
         __syncthreads();
-        float sum = 0.f;
-        for (int w = 0; w < waves; ++w) sum += p[w].sum;
-        mean = sum * a.inv_d;
-        squares = 0.f;
-        for (int w = 0; w < waves; ++w) {
-            squares += p[w].squares;
-            if (layer) {
-                const float n = count(w), d = p[w].sum / n - mean;
-                squares = fmaf(n * d, d, squares);
-            }
+        Parts other = {0.f, 0.f, 0.f, 0.f};                      // a wave's parts to a lane
+        if (lane < waves) other = p[lane];
+        if (layer) {
+            mean = wave_sum(other.sum) * a.inv_d;
+            const float d = other.mean - mean;
+            other.squares = fmaf(other.count * d, d, other.squares);
         }
+        squares = wave_sum(other.squares);
     }
-    const float inv = 1.f / sqrtf(squares * a.inv_d + eps);
+    const float inv = __builtin_amdgcn_rsqf(fmaf(squares, a.inv_d, eps));
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-        if (first + i * stride >= a.D) continue;
+        const int c = first + i * stride;
+        if (c >= a.D) continue;
+        f32x8 b = early;
+        if (PIECES > 1 && bias) b = fetch_f32(bias + c);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] = fmaf((v[i][e] - mean) * inv, q.w[i][e], b[i][e]);
+        for (int e = 0; e < 8; ++e) v[i][e] = fmaf((v[i][e] - mean) * inv, q.w[i][e], b[e]);
     }
 }
 
@@ -180,7 +179,7 @@ template <int PIECES, bool IN_F32, bool S_F32>
 __global__ void __launch_bounds__(64 * MAX_WAVES) gdn_block_norm_kernel(BlockArgs a) {
     __shared__ Parts part[2][MAX_WAVES];
     constexpr bool KEEP = PIECES == 1;
-    const int tid = threadIdx.x, wave = tid >> 6, waves = a.waves, stride = waves * 512;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = a.waves, stride = waves * 512;
     const int rows = waves == 1 ? 4 : 1;                         // rows of a workgroup
     const int first = 8 * (waves == 1 ? tid & 63 : tid);
     int turn = 0;
@@ -224,7 +223,7 @@ __global__ void __launch_bounds__(64 * MAX_WAVES) gdn_block_norm_kernel(BlockArg
                 if (a.gate_kind == GDN_GATE_CHANNEL) g = KEEP ? channel.w[i] : fetch_f32(static_cast<const float*>(a.gate) + c);
                 if (a.gate_act)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) g[e] = 1.f / (1.f + __expf(-g[e]));
+                    for (int e = 0; e < 8; ++e) g[e] = __builtin_amdgcn_rcpf(1.f + __expf(-g[e]));
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[i][e] *= g[e];
             }
