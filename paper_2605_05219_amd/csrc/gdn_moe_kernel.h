@@ -415,24 +415,21 @@ __global__ void __launch_bounds__(256) moe_sum_kernel(MoeArgs a) {
     }
     const int32_t* ids = a.ids + (int64_t)t * a.k;
     const float* part = a.part + (int64_t)t * a.k * a.D + c;
-    int j = 0;
-    for (; j + 1 < a.k; j += 2) {                                // (two at once; the part of a choice that is left out holds anything)
-        f32x4 p[2][2];
+    for (int j0 = 0; j0 < a.k; j0 += 4) {                        // (four at once; the part of a choice that is left out holds anything)
+        f32x4 p[4][2];
+        int id[4];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            p[i][0] = reinterpret_cast<const f32x4*>(part + (int64_t)(j + i) * a.D)[0];
-            p[i][1] = reinterpret_cast<const f32x4*>(part + (int64_t)(j + i) * a.D)[1];
+        for (int i = 0; i < 4; ++i) {
+            const int j = min(j0 + i, a.k - 1);
+            p[i][0] = reinterpret_cast<const f32x4*>(part + (int64_t)j * a.D)[0];
+            p[i][1] = reinterpret_cast<const f32x4*>(part + (int64_t)j * a.D)[1];
+            id[i] = j0 + i < a.k ? ids[j] : -1;
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            if (ids[j + i] >= 0)
+        for (int i = 0; i < 4; ++i)
+            if (id[i] >= 0)
 #pragma unroll
                 for (int q = 0; q < 8; ++q) v[q] += p[i][q / 4][q % 4];
-    }
-    if (j < a.k && ids[j] >= 0) {
-        const f32x4* p = reinterpret_cast<const f32x4*>(part + (int64_t)j * a.D);
-#pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] += p[q / 4][q % 4];
     }
     bf16x8 o;
 #pragma unroll
