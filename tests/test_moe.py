@@ -341,7 +341,7 @@ def test_knob_round_trip(knob):
 @pytest.mark.gpu
 @pytest.mark.parametrize("shape", [0, 2, 3, 6])
 @pytest.mark.parametrize("T,E,k,D,F,bias", [(1, 8, 2, 64, 64, None), (3, 600, 5, 128, 64, None), (30, 60, 4, 320, 192, None), (32, 300, 16, 4160, 64, None), (700, 8, 3, 256, 320, None),
-                                            (300, 20, 4, 128, 64, "one"), (90, 130, 10, 192, 128, None)])
+                                            (300, 20, 4, 128, 64, "one"), (90, 130, 10, 192, 128, None), (80, 12, 3, 1088, 1152, None)])
 def test_every_kernel(knob, shape, T, E, k, D, F, bias):
     """The tiles on experts of no row, of part of a tile and of several, and where all tokens take the same ones; the kernels of few tokens up to their most."""
     if shape == 6 and T > 32:
