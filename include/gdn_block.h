@@ -23,11 +23,13 @@
  *   per token), pointers 16-byte aligned (a gate per token: its element).  D is 8 .. 32768.  The rows of one tensor may lie in
  *   a wider buffer.  T = 0 is legal and does nothing.
  * Arithmetic: fp32 throughout, the mean first and then the squares of what is left; x is made of the s that is held in fp32,
- * so that each output is rounded once.  eps = 0 with a row of zeros gives NaN, as the formula does.
+ * so that each output is rounded once.  A row whose mean square and eps together lie below 2^-126 (eps = 0 with a row of zeros, for
+ * one) has no norm: NaN or infinities.
  * In place: s and x may each be the same rows as y, r or a gate per element (the same address, row stride and element size);
  * s and x may not share a byte, nor any output one with an input in another way.
  * Errors: GDN_ERR_NULL, _ALIGN, _SHAPE (an unknown type, norm or gate, D out of range, a row stride smaller than its row, an eps
- * that is negative or not finite, a norm or gate of a y that is not there), _COUNT (T negative; more than 2^31 workgroups),
+ * that is negative or not finite, a norm or gate of a y that is not there), _COUNT (T negative or not below 2^31; a row stride above 2^40 or a tensor that spans more than 2^60
+ * elements),
  * _SLOT_HAZARD (an output that overlaps an input or the other output).
  */
 #ifndef GDN_BLOCK_H

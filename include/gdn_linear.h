@@ -89,7 +89,8 @@ int32_t gdn_linear_tune(int32_t shape);
  * Everything else as gdn_linear.  Arithmetic: fp32 sums of the bf16 products; act, factor and residual in fp32; one rounding to out_dtype.
  * For at most 128 rows the sum over k may be taken in four parts that are added in order (whether and which: by T, N and K alone), else it is
  * gdn_linear's.  Errors as gdn_linear, and GDN_ERR_NULL without an epilogue, GDN_ERR_SHAPE for an unknown activation or res_dtype, a bias_up
- * without w_up, ldr < N or ldw_up < K, GDN_ERR_SLOT_HAZARD where y shares bytes as said.
+ * without w_up, ldr < N or ldw_up < K, GDN_ERR_COUNT for N from 2^24 on or a y or residual with a row stride above 2^30 or a
+ * span of more than 2^60 elements, GDN_ERR_SLOT_HAZARD where y shares bytes as said.
  */
 enum { GDN_ACT_NONE = 0, GDN_ACT_SILU = 1, GDN_ACT_GELU = 2, GDN_ACT_GELU_TANH = 3, GDN_ACT_RELU = 4, GDN_ACT_RELU2 = 5, GDN_ACT_SIGMOID = 6 };
 

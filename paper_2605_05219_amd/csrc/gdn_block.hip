@@ -295,10 +295,10 @@ int32_t check(const gdn_block_shape* p, const void* y, int64_t ldy, const void* 
     for (const float* q : {p->post != GDN_NORM_NONE ? w_post : nullptr, p->post != GDN_NORM_NONE ? b_post : nullptr,
                            p->pre != GDN_NORM_NONE ? w_pre : nullptr, p->pre != GDN_NORM_NONE ? b_pre : nullptr})
         if (off_align(q, 16)) return GDN_ERR_ALIGN;
-    // every byte offset of a row has to fit 63 bits, and a workgroup's number 31
+    // the tensors' spans have to fit 63 bits, and a workgroup's number 31
     int64_t most = std::max(std::max(y ? ldy : 0, r ? ldr : 0), std::max(s ? lds : 0, x ? ldx : 0));
     if (p->gate == GDN_GATE_ELEMENT || p->gate == GDN_GATE_TOKEN) most = std::max(most, ldg);
-    if (T > INT32_MAX || most > ((int64_t)1 << 40)) return GDN_ERR_COUNT;
+    if (T > INT32_MAX || most > std::min((int64_t)1 << 40, ((int64_t)1 << 60) / T)) return GDN_ERR_COUNT;
 
     const Rows outs[2] = {Rows(s, T, lds * sb, D * sb), Rows(x, T, ldx * xb, D * xb)};
     if (share_bytes(outs[0], outs[1])) return GDN_ERR_SLOT_HAZARD;

@@ -964,8 +964,10 @@ extern "C" int32_t gdn_linear_act(const void* x, int64_t ldx, const void* w, int
     if (epi->w_up && (off_align(epi->w_up, 16) || (epi->ldw_up & 7))) return GDN_ERR_ALIGN;
     if (off_align(epi->bias_up, 4)) return GDN_ERR_ALIGN;
     if (epi->residual && (off_align(epi->residual, rs == 2 ? 8 : 16) || (epi->ldr & 3))) return GDN_ERR_ALIGN;
-    if (epi->w_up && (int64_t)256 * epi->ldw_up * 2 >= ((int64_t)1 << 31)) return GDN_ERR_COUNT;
-    if (T > ((int64_t)1 << 40) || ldy > ((int64_t)1 << 30) || (epi->residual && epi->ldr > ((int64_t)1 << 30))) return GDN_ERR_COUNT;
+    if (epi->w_up && epi->ldw_up >= ((int64_t)1 << 22)) return GDN_ERR_COUNT;
+    // a kernel of few rows has as many threads as that, and the tensors' spans have to fit 63 bits
+    const int64_t most = std::min((int64_t)1 << 30, ((int64_t)1 << 60) / T);
+    if (N >= 1 << 24 || ldy > most || (epi->residual && epi->ldr > most)) return GDN_ERR_COUNT;
     const Rows out(y, T, ldy * es, (int64_t)N * es), res(epi->residual, T, epi->ldr * rs, (int64_t)N * rs);
     if (share_bytes(out, Rows(x, T, ldx * 2, (int64_t)K * 2)) || share_bytes(out, Rows(w, N, ldw * 2, (int64_t)K * 2)) ||
         share_bytes(out, Rows(epi->w_up, N, epi->ldw_up * 2, (int64_t)K * 2)) || share_bytes(out, Rows(bias, 1, (int64_t)N * 4, (int64_t)N * 4)) ||

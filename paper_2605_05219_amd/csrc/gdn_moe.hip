@@ -22,7 +22,7 @@ int32_t check_shape(const gdn_moe_shape* s, int64_t T) {
     if (s->act < GDN_ACT_NONE || s->act > GDN_ACT_SIGMOID || s->score < 0 || s->score > GDN_SCORE_SIGMOID || s->normalise < 0 || s->normalise > 1 ||
         !dtype_known(s->router_dtype) || !std::isfinite(s->routed_scale))
         return GDN_ERR_SHAPE;
-    if (T * s->k >= ((int64_t)1 << 24) || T >= ((int64_t)1 << 24)) return GDN_ERR_COUNT;
+    if (T >= ((int64_t)1 << 24) || T * s->k >= ((int64_t)1 << 24)) return GDN_ERR_COUNT;
     return GDN_OK;
 }
 
@@ -187,7 +187,7 @@ extern "C" int32_t gdn_moe(const gdn_moe_shape* s, const void* x, int64_t ldx, c
     a.tile_rows = linear::expert_tile_rows(shape);
     if (T == 1) launch_logits<1, 2, 4>(a, stream);
     else if (T * E <= 16384) launch_logits<2, 2, 2>(a, stream);
-    else hipLaunchKernelGGL(moe_logits_kernel<8>, dim3((unsigned)((E + 15) / 16), (unsigned)((T + 15) / 16)), dim3(64 * 8), 0, stream, a);
+    else hipLaunchKernelGGL(moe_logits_kernel<8>, dim3((unsigned)((T + 15) / 16), (unsigned)((E + 15) / 16)), dim3(64 * 8), 0, stream, a);
     if (forced == FEW ? T <= MOST_FEW : forced < 0 && T <= MOST_FEW && few_pays(*s, T)) return hip_err(launch_few(a, stream));
     const int per_lane = (s->E + 63) / 64;
     if (per_lane <= 1) launch_route<1>(a, stream);

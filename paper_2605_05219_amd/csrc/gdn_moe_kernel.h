@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(64 * WAVES) moe_logits_kernel(MoeArgs a) {
     __shared__ f64x4 sums[WAVES][64];
     constexpr int U = 4;                                          // blocks on their way
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lr = lane & 15, g = lane >> 4;
-    const int e0 = blockIdx.x * 16, t0 = blockIdx.y * 16;
+    const int t0 = blockIdx.x * 16, e0 = blockIdx.y * 16;      // (the tokens may be more than a grid's y holds)
     // (rows past the end are the last one's: their sums go nowhere)
     const uint16_t* const x = a.x + (int64_t)min(t0 + lr, a.T - 1) * a.ldx + 8 * g;
     const int64_t w = (int64_t)min(e0 + lr, a.E - 1) * a.D + 8 * g;

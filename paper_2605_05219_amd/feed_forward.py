@@ -14,8 +14,8 @@ from . import block, linear, moe
 
 
 class FeedForward:
-    """weights: "norm" (fp32 [D]); dense: "gate", "up" [F][D], "down" [D][F]; experts: "router" [E][D], "gate_up" [E][2 F][D], "down" [E][D][F], and of a
-    shared expert "shared_gate", "shared_up" [F_s][D], "shared_down" [D][F_s] (bf16)."""
+    """weights: "norm" (fp32 [D]); dense: "gate", "up" [F][D], "down" [D][F]; experts: "router" [E][D], "gate_up" [E][2 F][D], "down" [E][D][F], a
+    "choice_bias" (fp32 [E]) where there is one, and of a shared expert "shared_gate", "shared_up" [F_s][D], "shared_down" [D][F_s] (bf16)."""
 
     def __init__(self, weights, experts_per_token=0, act="silu", score="softmax", normalise=True, routed_scale=1.0, stream_dtype="f32", eps=1e-6):
         self.w, self.act = weights, act

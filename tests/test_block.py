@@ -351,3 +351,9 @@ def test_another_stream_and_a_captured_graph():
         c.run()
         torch.cuda.synchronize()
         assert torch.equal(got[0], c.s) and torch.equal(got[1], c.x)
+
+
+def test_spans_past_63_bits_are_refused():
+    assert raw(T=(1 << 31) - 1, ldy=1 << 32) == -11
+    assert raw(T=(1 << 31) - 1, ldx=1 << 30) == -11
+    assert raw(shaped(gate="token"), T=1 << 30, ldg=1 << 32) == -11

@@ -138,3 +138,20 @@ def test_a_capture_that_would_need_new_buffers_is_refused():
     first = ff.held["x"]
     ff.step(y.repeat(9, 1), stream.repeat(9, 1))
     assert any(t is first for t in ff.outgrown)                              # a graph that has it may go on
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("experts", [0, 8])
+def test_a_step_of_no_tokens_and_one_without_a_block_before_it(experts):
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    ff = FF.FeedForward(FF.random_weights(128, 64, experts, 64 if experts else 0, gen), 2)
+    out = ff.step(torch.empty(0, 128, device="cuda", dtype=torch.bfloat16), torch.empty(0, 128, device="cuda"))
+    assert out is None if not experts else out.shape == (0, 128)
+    stream = torch.randn(5, 128, generator=gen, device="cuda")
+    alone, added = stream.clone(), stream.clone()
+    first = ff.step(None, alone)
+    first = None if first is None else first.clone()
+    second = ff.step(torch.zeros(5, 128, device="cuda", dtype=torch.bfloat16), added)
+    torch.cuda.synchronize()
+    assert torch.equal(alone, added) and (first is None or torch.equal(first, second))

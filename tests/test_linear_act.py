@@ -286,3 +286,10 @@ def test_another_stream_and_a_captured_graph(T):
         c.run()
         torch.cuda.synchronize()
         assert torch.equal(got, c.y)
+
+
+def test_spans_past_63_bits_and_more_outputs_than_threads_are_refused():
+    assert raw(T=1 << 37, N=64, ldy=1 << 24) == -11
+    assert raw(dict(ldr=1 << 24), T=1 << 37, N=64) == -11
+    assert raw(dict(ldw_up=1 << 60)) == -11
+    assert raw(dict(ldr=1 << 24), N=1 << 24, ldy=1 << 24) == -11

@@ -371,3 +371,17 @@ def test_masks_and_zero_weights_in_every_path(knob, shape, T):
     c.gu[0] = c.down[4] = float("inf")
     c.run().check()
     assert c.ids[0, :3].tolist() == [0, 2, 4] and c.weights[0, 0] == 0 and c.weights[0, 2] == 0
+
+
+@pytest.mark.gpu
+def test_more_tokens_than_a_grid_has_rows():
+    import torch
+    T = 16 * 65536 + 5
+    c = Call(T, 3, 1, 64, 64, add=True, seed=5).run()
+    torch.cuda.synchronize()
+    some = torch.cat([torch.arange(40), torch.arange(65520, 65560), torch.arange(T - 40, T)]).cuda()
+    ids, (p, ep), (y, ey) = mo.moe(f64(c.x[some]), f64(c.wr), None, f64(c.gu), f64(c.down), f64(c.add[some]), 1, **c.kw)
+    assert np.array_equal(c.ids[some].cpu().numpy(), ids) and (np.abs(f64(c.weights[some]) - p) <= ep).all()
+    worst = np.abs(f64(c.y[some]) - y) - (ey + 2.0 ** -8 * (np.abs(y) + ey) + 2.0 ** -134)
+    assert not np.isnan(worst).any() and worst.max() <= 0, float(worst.max())
+    assert (c.all[T:] == 77).all()
