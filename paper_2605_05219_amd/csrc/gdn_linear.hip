@@ -17,6 +17,11 @@
 //      (384 x 8224 x 2048 23 us against 31 of shape 0)
 //   5: 128 x 160 x 64, 4 stages, four waves, one workgroup per compute unit: the same for problems that shape 4 just does not
 //      fit in one round (512 x 8224: 260 tiles of 128 outputs for 256 compute units, 208 of 160; 27 us against 36 of shape 4, 32 of shape 0)
+// The same tiles make gdn_linear_act's products, with the activation, gate, factor and residual between the sums and the store (act_epilogue), and those of a mixture
+// of experts, on rows that a list names (launch_expert_product).  For at most 128 rows gdn_linear_act has six kernels more, shapes 6 to 11 (gdn_few_kernel.h).
+//   8192 x 2 x 6144 x 2048 with SiLU and gate 305 us (1350 TFLOP/s; a library product of 8192 x 12288 x 2048 alone 361), the activation under 3 % of it;
+//   1401 x 1733 x 1600 with GELU, an fp32 residual and fp32 outputs 22: 10 of them its 25 k steps (what a compute unit is sent, 80 GB/s), 2.5 the GELU, 1.6 the residual,
+//   8 the beginning and the end of one round of 154 tiles (shape 0 35, 3 25.7, 5 36; three workgroups of shape 3 with three stages each 23.8, tiles of 96 x 128 24.7).
 // The products are v_mfma_f32_16x16x32_bf16: half the accumulator traffic per flop of the 32 x 32 x 16 instruction, at the same rate on
 // paper; on a chip held by its power limit 8192 x 2048 x 2048 takes 51 us with it and 56 with the other, 512 x 2048 10.4 and 12.3.
 // A load to LDS writes a wave's 1 KiB contiguously (lane i at 16 i), so rows are unpadded (2 BK bytes) and bank

@@ -152,7 +152,7 @@ __global__ void __launch_bounds__(256) moe_logits_few_kernel(MoeArgs a) {
 // More: a workgroup makes 16 experts x 16 tokens on v_mfma_f64_16x16x4_f64 (lane: row lane % 16 of either operand and one k of its group of 16 lanes; of the result
 // token lane % 16, register r expert lane / 16 + 4 r), its waves the blocks of 32 k in turn: a lane loads 8 adjacent elements of each row, and which k a product
 // pairs is the same for both.  Making fp64 of the elements is what the vector units spend most on, and a matrix product takes sixteen uses of each: 200 tokens x 512
-// experts 16 us, 2048 x 64 17 (by 4 x 4 on the vector units 27 and 35; 1 x 128 8.5, 64 x 128 9.6 against 5 and 7.5 of the kernel above).
+// experts, D 2048, 17 us, 2048 x 64 17.5 (by 4 x 4 on the vector units 27 and 35; 1 x 128 8.5, 64 x 128 9.6 against 5 and 7.5 of the kernel above).
 template <int WAVES>
 __global__ void __launch_bounds__(64 * WAVES) moe_logits_kernel(MoeArgs a) {
     typedef double f64x4 __attribute__((ext_vector_type(4)));
@@ -360,7 +360,7 @@ __global__ void __launch_bounds__(MAX_E) moe_lists_few_kernel(MoeArgs a) {
     make_table(a, counts[tid], before);
 }
 // ... of more the lists, a workgroup to an expert, which looks through all choices (a counter that the tokens of all workgroups add to is
-// slower: 12288 choices of 64 experts 37 us) ...
+// slower: 12288 choices of 64 experts 37 us, 7 so) ...
 constexpr int LIST_WAVES = 16;
 __global__ void __launch_bounds__(64 * LIST_WAVES) moe_lists_kernel(MoeArgs a) {
     __shared__ int32_t found[LIST_WAVES];
@@ -401,7 +401,8 @@ __global__ void __launch_bounds__(MAX_E) moe_table_kernel(MoeArgs a) {
     make_table(a, e < a.E ? a.counts[e] : 0, before);
 }
 
-// ---- y = add + the choices' parts, in the order of their keys; a thread owns 8 adjacent channels
+// ---- y = add + the choices' parts, in the order of their keys; a thread owns 8 adjacent channels.  Bound by memory: 2048 tokens of 6
+// choices, D 2048, 109 MB in 18 us, most of it out of the memory-side cache.
 __global__ void __launch_bounds__(256) moe_sum_kernel(MoeArgs a) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int groups = a.D / 8;
