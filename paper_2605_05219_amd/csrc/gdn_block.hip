@@ -6,7 +6,8 @@
 // four.  A norm costs one barrier, and few instructions: the vector units, 4 clocks to each instruction of a wave, are not far behind the memory (with the waves' sums added up by every
 // thread, and divisions, 928 instructions for 8 elements of two layer norms kept them busy for three quarters of the time: 1777 rows of 5120 43 us, now 32).  8192 rows of 2048 in
 // bf16, the norm in front alone, 26 us (134 MB: 5.2 TB/s, a plain copy of 2 GiB 4.9), with one behind the block and a gate per channel 28; 1777 rows of 5120 out of wider
-// buffers, two layer norms with a gate per element and a stream in fp32, 32 (127 MB: 3.9 TB/s); 4096 rows of 8192 50; a single row 2.4, which a call's host time of 7 covers.
+// buffers, two layer norms with a gate per element and a stream in fp32, 32 (127 MB: 3.9 TB/s); 4096 rows of 8192 50; 1000 of 32768 63 (4.2 TB/s; with
+// all operands and weights asked for at once the registers spill: 89); a single row 2.4, which a call's host time of 7 covers.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -115,7 +116,7 @@ __device__ __forceinline__ void fetch_weights(Weights<PIECES>& q, const float* w
 // a wave's to a lane, the squares about the row's mean by  sum (v - m)^2 = sum over waves of (sum (v - m_w)^2 + n_w (m_w - m)^2).  `part`: two sets, between which
 // `turn` alternates, so one barrier is enough for each norm.  The same on every thread, and the same whenever it runs.
 template <int PIECES>
-__device__ __forceinline__ void normalise(f32x8 (&v)[PIECES], int kind, const Weights<PIECES>& q, const float* bias, float eps, const BlockArgs& a, int first, int stride,
+__device__ __forceinline__ void normalise(f32x8 (&v)[PIECES], int kind, const Weights<PIECES>& kept, const float* w, const float* bias, float eps, const BlockArgs& a, int first, int stride,
                                           Parts (*part)[MAX_WAVES], int& turn, int wave) {
     const int waves = a.waves;
     const bool layer = kind == GDN_NORM_LAYER;
@@ -167,18 +168,22 @@ __device__ __forceinline__ void normalise(f32x8 (&v)[PIECES], int kind, const We
         if (c >= a.D) continue;
         f32x8 b = early;
         if (PIECES > 1 && bias) b = fetch_f32(bias + c);
+        f32x8 g;
+        if constexpr (PIECES == 1) g = kept.w[0];
+        else g = fetch_f32(w + c) + a.offset;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] = fmaf((v[i][e] - mean) * inv, q.w[i][e], b[e]);
+        for (int e = 0; e < 8; ++e) v[i][e] = fmaf((v[i][e] - mean) * inv, g[e], b[e]);
     }
 }
 
 // `a.waves` waves to a row, PIECES pieces of 8 elements to a thread; with one wave to a row a workgroup has four rows.  A workgroup goes through
 // every grid-th row and keeps the weights (and a gate per channel) in registers: read anew for each row those arrays of fp32 are more than the row
-// itself, two of bf16 read and two written, and come out of L2.  (Rows wider than 8192 have more than one piece to a thread, and read them each time.)
+// itself, two of bf16 read and two written, and come out of L2.  (Rows wider than 8192 have more than one piece to a thread, and read them where they are used; with four pieces the stream and
+// the gate too are asked for only behind the first norm.)
 template <int PIECES, bool IN_F32, bool S_F32>
 __global__ void __launch_bounds__(64 * MAX_WAVES) gdn_block_norm_kernel(BlockArgs a) {
     __shared__ Parts part[2][MAX_WAVES];
-    constexpr bool KEEP = PIECES == 1;
+    constexpr bool KEEP = PIECES == 1, LATE = PIECES == 4;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = a.waves, stride = waves * 512;
     const int rows = waves == 1 ? 4 : 1;                         // rows of a workgroup
     const int first = 8 * (waves == 1 ? tid & 63 : tid);
@@ -198,6 +203,7 @@ __global__ void __launch_bounds__(64 * MAX_WAVES) gdn_block_norm_kernel(BlockArg
             pr[i] = nothing<S_F32>();
             if (c >= a.D) continue;
             if (a.y) py[i] = fetch<IN_F32>(a.y, t * a.ldy + c);
+            if (LATE) continue;
             if (a.r) pr[i] = fetch<S_F32>(a.r, t * a.ldr + c);
             if (a.gate_kind == GDN_GATE_ELEMENT) pg[i] = fetch<IN_F32>(a.gate, t * a.ldg + c);
         }
@@ -210,14 +216,13 @@ __global__ void __launch_bounds__(64 * MAX_WAVES) gdn_block_norm_kernel(BlockArg
         f32x8 v[PIECES];
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) v[i] = unpack(py[i]);
-        if (a.post != GDN_NORM_NONE) {
-            if (!KEEP) fetch_weights(post, a.w_post, a.offset, first, stride, a.D);
-            normalise(v, a.post, post, a.b_post, a.eps_post, a, first, stride, part, turn, wave);
-        }
+        if (a.post != GDN_NORM_NONE) normalise(v, a.post, post, a.w_post, a.b_post, a.eps_post, a, first, stride, part, turn, wave);
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             const int c = first + i * stride;
             if (c >= a.D) continue;
+            if (LATE && a.r) pr[i] = fetch<S_F32>(a.r, t * a.ldr + c);
+            if (LATE && a.gate_kind == GDN_GATE_ELEMENT) pg[i] = fetch<IN_F32>(a.gate, t * a.ldg + c);
             if (a.gate_kind == GDN_GATE_ELEMENT || a.gate_kind == GDN_GATE_CHANNEL) {
                 f32x8 g = unpack(pg[i]);
                 if (a.gate_kind == GDN_GATE_CHANNEL) g = KEEP ? channel.w[i] : fetch_f32(static_cast<const float*>(a.gate) + c);
@@ -235,8 +240,7 @@ __global__ void __launch_bounds__(64 * MAX_WAVES) gdn_block_norm_kernel(BlockArg
             if (a.s) put(a.s, t * a.lds + c, S_F32, v[i]);
         }
         if (a.pre == GDN_NORM_NONE) continue;
-        if (!KEEP) fetch_weights(pre, a.w_pre, a.offset, first, stride, a.D);
-        normalise(v, a.pre, pre, a.b_pre, a.eps_pre, a, first, stride, part, turn, wave);
+        normalise(v, a.pre, pre, a.w_pre, a.b_pre, a.eps_pre, a, first, stride, part, turn, wave);
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             const int c = first + i * stride;
