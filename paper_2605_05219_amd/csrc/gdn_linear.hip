@@ -710,11 +710,21 @@ constexpr ShapeCost SHAPES[5] = {{3, 64, 64, 2, 10.4, 1.8, 3.9, 2.0, false},
                                  {4, 128, 128, 1, 14.2, 2.6, 10.4, 2.1, false},
                                  {5, 128, 160, 1, 15.9, 5.0, 12.9, 3.9, false},
                                  {2, 256, 256, 1, 41.9, 6.9, 32.6, 4.0, true}};
-double shape_cost(const ShapeCost& c, int64_t T, int64_t N, int32_t K) {
-    const int64_t tiles = ((T + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn), slots = (int64_t)chip_cus() * c.per_cu;
+double rounds_cost(const ShapeCost& c, int64_t tiles, int32_t K) {
+    const int64_t slots = (int64_t)chip_cus() * c.per_cu;
     const double k = (double)K / 2048.0, f = (double)(tiles % slots) / (double)slots;
     const double full = c.full_k * k + c.full, alone = c.alone_k * k + c.alone;
     return (double)(tiles / slots) * full + (f > 0 ? alone + (full - alone) * (c.square ? f * f : f) : 0.0);
+}
+double shape_cost(const ShapeCost& c, int64_t T, int64_t N, int32_t K) {
+    return rounds_cost(c, ((T + c.bm - 1) / c.bm) * ((N + c.bn - 1) / c.bn), K);
+}
+
+double expert_product_us(int shape, int64_t row_tiles, int64_t rows_w, int32_t K) {
+    // (three workgroups to a compute unit where k is short: a round of half as many more tiles)
+    constexpr ShapeCost three = {3, 64, 64, 3, 15.1, 2.4, 3.9, 2.0, false};
+    const ShapeCost& c = shape == 2 ? SHAPES[4] : shape == 0 ? SHAPES[1] : K <= 1024 ? three : SHAPES[0];
+    return rounds_cost(c, row_tiles * ((rows_w + c.bn - 1) / c.bn), K);
 }
 
 // Which tile shape a problem gets, and how many of its columns: a problem whose tiles leave a last round nearly empty may be cut

@@ -30,6 +30,8 @@ struct ExpertProduct {
 
 // Rows of a tile in tile shape `shape` (as gdn_linear_tune's numbers: 0, 2 or 3).
 int expert_tile_rows(int shape);
+// The estimated time of a product of so many row tiles with weights of so many rows, by the rounds over the chip.
+double expert_product_us(int shape, int64_t row_tiles, int64_t rows_w, int32_t K);
 hipError_t launch_expert_product(const ExpertProduct& p, int shape, hipStream_t stream);
 
 }  // namespace linear
