@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <type_traits>
 
 #include "gdn_moe.h"
 #include "gdn_moe_kernel.h"
@@ -67,27 +68,44 @@ template <typename C>
 hipError_t launch_down_few(const MoeArgs& a, hipStream_t stream) {
     return launch_few_kernel<moe_down_few_kernel<C>>(dim3((unsigned)(a.D / C::WR), (unsigned)a.T), C::WAVES, C::SMEM, a, stream);
 }
+// f(a constant of how many experts a lane looks at)
+template <typename F>
+auto by_experts(int E, F f) {
+    const int per_lane = (E + 63) / 64;
+    return per_lane <= 1   ? f(std::integral_constant<int, 1>())
+           : per_lane <= 2 ? f(std::integral_constant<int, 2>())
+           : per_lane <= 4 ? f(std::integral_constant<int, 4>())
+           : per_lane <= 8 ? f(std::integral_constant<int, 8>())
+                           : f(std::integral_constant<int, 16>());
+}
+void launch_choices(const MoeArgs& a, hipStream_t stream) {
+    by_experts(a.E, [&](auto p) { hipLaunchKernelGGL((moe_route_kernel<decltype(p)::value>), dim3((unsigned)((a.T + 3) / 4)), dim3(256), 0, stream, a); });
+}
 hipError_t launch_few(const MoeArgs& a, hipStream_t stream) {
-    const int per_lane = (a.E + 63) / 64;
-    const hipError_t e = per_lane <= 1   ? launch_up_few<1>(a, stream)
-                         : per_lane <= 2 ? launch_up_few<2>(a, stream)
-                         : per_lane <= 4 ? launch_up_few<4>(a, stream)
-                         : per_lane <= 8 ? launch_up_few<8>(a, stream)
-                                         : launch_up_few<16>(a, stream);
+    // Every workgroup of the first product chooses anew where all of them are on the chip at once, two to a compute unit: a launch less.  In more rounds the choice, 2 us and with
+    // many experts 4, comes once in each.  us, chosen inside / by a launch: 1 token of 128 experts, k 8, F 768 (384 workgroups) 25.2 / 27.0; 2 35 / 35; 4 of 512, F 256 (512) 20.8 / 22.6, 8
+    // 29.7 / 27.3, 32 93 / 65; 16 of 512, k 10, F 512 209 / 172.
+    const bool inside = (int64_t)a.T * a.k * (a.F / 16) <= 2 * chip_cus();
+    hipError_t e;
+    if (inside) {
+        e = by_experts(a.E, [&](auto p) { return launch_up_few<decltype(p)::value>(a, stream); });
+    } else {
+        launch_choices(a, stream);
+        e = launch_up_few<0>(a, stream);
+    }
     if (e != hipSuccess) return e;
     // a narrow output in workgroups of 8 of its rows, so that there is one for every compute unit
     return a.T * (a.D / 16) < chip_cus() ? launch_down_few<few::Few<1, 8, 4, 6>>(a, stream) : launch_down_few<few::Few<1, 16, 4, 4>>(a, stream);
 }
 
-template <int P>
 void launch_route(const MoeArgs& a, hipStream_t stream) {
-    if constexpr (P <= 8) {                                      // (16 keys a lane do not fit the registers of 16 waves)
-        if (a.T <= FEW_TOKENS) {
-            hipLaunchKernelGGL((moe_route_few_kernel<P>), dim3(1), dim3(MAX_E), 0, stream, a);
-            return;
-        }
+    if (a.T <= FEW_TOKENS && a.E <= 512) {                       // (16 keys a lane do not fit the registers of 16 waves)
+        by_experts(a.E, [&](auto p) {
+            if constexpr (decltype(p)::value <= 8) hipLaunchKernelGGL((moe_route_few_kernel<decltype(p)::value>), dim3(1), dim3(MAX_E), 0, stream, a);
+        });
+        return;
     }
-    hipLaunchKernelGGL((moe_route_kernel<P>), dim3((unsigned)((a.T + 3) / 4)), dim3(256), 0, stream, a);
+    launch_choices(a, stream);
     if ((int64_t)a.T * a.k <= FEW_PAIRS) {
         hipLaunchKernelGGL(moe_lists_few_kernel, dim3(1), dim3(MAX_E), 0, stream, a);
         return;
@@ -114,11 +132,12 @@ hipError_t launch_products(const MoeArgs& a, int shape, hipStream_t stream) {
 }
 
 constexpr int FEW = 6, MOST_FEW = 32;
-// The kernels of few tokens save launches, some 10 us, and read an expert once for every token that chooses it (though not from memory).  us, theirs / tiles of 64 x 64, by tokens:
-// 128 experts, k 8, D 2048, F 768: 1 28 / 38, 4 63 / 74, 6 89 / 94, 8 110 / 112, 12 154 / 141; 16, 2, 4096, 2048: 2 48 / 60, 4 79 / 97, 8 134 / 132.
+// The kernels of few tokens save launches, some 10 us, and read an expert once for every token that chooses it, out of the caches after the first (20 MB a us).  us, theirs / tiles, by
+// tokens: 128 experts, k 8, D 2048, F 768: 1 25 / 33, 4 58 / 67, 8 102 / 108, 16 187 / 165; 8, 2, 2048, 2048: 2 26 / 32, 4 42 / 49, 8 66 / 57; 512, 10, 2048, 512: 8 98 / 115, 16 172 / 188, 32
+// 314 / 291; 1024, 8, 1024, 256: 16 54 / 64, 32 91 / 100.
 bool few_pays(const gdn_moe_shape& s, int64_t T) {
     const double choices = (double)T * s.k, distinct = s.E * (1.0 - std::pow(1.0 - (double)s.k / s.E, (double)T));
-    return (choices - distinct) * 6.0 * s.D * s.F <= 10.0 * 5.3e6;
+    return (choices - distinct) * 6.0 * s.D * s.F <= 10.0 * 20e6;
 }
 
 std::atomic<int32_t> g_moe_shape{-1};
@@ -209,12 +228,7 @@ extern "C" int32_t gdn_moe(const gdn_moe_shape* s, const void* x, int64_t ldx, c
     else if (T * E <= 16384) launch_logits<2, 2, 2>(a, stream);
     else hipLaunchKernelGGL(moe_logits_kernel<8>, dim3((unsigned)((T + 15) / 16), (unsigned)((E + 15) / 16)), dim3(64 * 8), 0, stream, a);
     if (forced == FEW ? T <= MOST_FEW : forced < 0 && T <= MOST_FEW && few_pays(*s, T)) return hip_err(launch_few(a, stream));
-    const int per_lane = (s->E + 63) / 64;
-    if (per_lane <= 1) launch_route<1>(a, stream);
-    else if (per_lane <= 2) launch_route<2>(a, stream);
-    else if (per_lane <= 4) launch_route<4>(a, stream);
-    else if (per_lane <= 8) launch_route<8>(a, stream);
-    else launch_route<16>(a, stream);
+    launch_route(a, stream);
     const hipError_t e = launch_products(a, shape, stream);
     if (e != hipSuccess) return hip_err(e);
     hipLaunchKernelGGL(moe_sum_kernel, dim3((unsigned)((T * (D / 8) + 255) / 256)), dim3(256), 0, stream, a);

@@ -217,20 +217,25 @@ __device__ __forceinline__ void choose(const MoeArgs& a, int t, int lane, int& m
     float l[P];
     uint32_t key[P];
     const float* row = a.logits + (int64_t)t * a.E;
+    float bias[P];
+#pragma unroll
+    for (int i = 0; i < P; ++i) {                                // (all asked for before the first is used)
+        const int e = min(lane * P + i, a.E - 1);
+        l[i] = row[e];
+        bias[i] = a.choice_bias ? a.choice_bias[e] : 0.f;
+    }
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-        const int e = lane * P + i;
-        l[i] = -__builtin_inff();
-        key[i] = 0;
-        if (e < a.E) {
-            l[i] = row[e];
-            float s = l[i];
-            if (a.score == GDN_SCORE_SIGMOID || a.choice_bias) {
-                double d = a.score == GDN_SCORE_SIGMOID ? 1.0 / (1.0 + exp(-(double)l[i])) : (double)l[i];
-                if (a.choice_bias) d += (double)a.choice_bias[e];
-                s = (float)d;
-            }
-            key[i] = key_order(s);
+        float s = l[i];
+        if (a.score == GDN_SCORE_SIGMOID || a.choice_bias) {
+            double d = a.score == GDN_SCORE_SIGMOID ? 1.0 / (1.0 + exp(-(double)l[i])) : (double)l[i];
+            if (a.choice_bias) d += (double)bias[i];
+            s = (float)d;
+        }
+        key[i] = key_order(s);
+        if (lane * P + i >= a.E) {
+            l[i] = -__builtin_inff();
+            key[i] = 0;
         }
     }
     float top = 0.f, total = 1.f;
@@ -439,7 +444,7 @@ __global__ void __launch_bounds__(256) moe_sum_kernel(MoeArgs a) {
 }
 
 // ---- A few tokens: the choice with the first product, the second one with the sum, in two launches behind the router's sums, by the waves and rings of
-// gdn_few_kernel.h.  A workgroup's time is that of its weights, so that every one of a token's chooses anew (2 us) what a launch of its own would take 4 for.
+// gdn_few_kernel.h.  P > 0: every workgroup of a token chooses anew; P = 0: the choices have been made.
 typedef few::Few<1, 32, 4, 3> UpFew;
 template <int P>
 __global__ void __launch_bounds__(64 * UpFew::WAVES) moe_up_few_kernel(MoeArgs a) {      // 16 of a choice's F; grid: (F / 16, T k)
@@ -448,19 +453,21 @@ __global__ void __launch_bounds__(64 * UpFew::WAVES) moe_up_few_kernel(MoeArgs a
     __shared__ float weight;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int pair = blockIdx.y, t = pair / a.k, j = pair % a.k, f0 = blockIdx.x * 16;
-    if (wave == 0) {
-        int id;
-        float p;
-        choose<P>(a, t, lane, id, p);
-        if (lane == j) { chosen = p != 0.f ? id : -1; weight = p; }
-        if (lane < a.k && j == 0 && blockIdx.x == 0) {
-            if (a.out_ids) a.out_ids[pair + lane] = id;
-            if (a.out_weights) a.out_weights[pair + lane] = p;
-            a.ids[pair + lane] = p != 0.f ? id : -1;
+    if constexpr (P > 0) {
+        if (wave == 0) {
+            int id;
+            float p;
+            choose<P>(a, t, lane, id, p);
+            if (lane == j) { chosen = p != 0.f ? id : -1; weight = p; }
+            if (lane < a.k && j == 0 && blockIdx.x == 0) {
+                if (a.out_ids) a.out_ids[pair + lane] = id;
+                if (a.out_weights) a.out_weights[pair + lane] = p;
+                a.ids[pair + lane] = p != 0.f ? id : -1;
+            }
         }
+        __syncthreads();
     }
-    __syncthreads();
-    const int e = __builtin_amdgcn_readfirstlane(chosen);
+    const int e = __builtin_amdgcn_readfirstlane(P > 0 ? chosen : a.ids[pair]);
     if (e < 0) return;
     const int bytes = 15 * a.D * 2 + a.D * 2;
     const few::Part gate = {reinterpret_cast<const char*>(a.w_gate_up + ((int64_t)e * 2 * a.F + f0) * a.D), bytes, a.D * 2};
@@ -478,7 +485,7 @@ __global__ void __launch_bounds__(64 * UpFew::WAVES) moe_up_few_kernel(MoeArgs a
     __syncthreads();
     if (threadIdx.x < 4) {
         const int piece = threadIdx.x;
-        const f32x4 v = weight * (activate(a.act, UpFew::get_sum(sums, 0, piece)) * UpFew::get_sum(sums, 0, piece + 4));
+        const f32x4 v = (P > 0 ? weight : a.weights[pair]) * (activate(a.act, UpFew::get_sum(sums, 0, piece)) * UpFew::get_sum(sums, 0, piece + 4));
         *reinterpret_cast<bf16x4*>(a.h + (int64_t)pair * a.F + f0 + 4 * piece) = __builtin_convertvector(v, bf16x4);
     }
 }
