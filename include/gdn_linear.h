@@ -87,7 +87,7 @@ int32_t gdn_linear_tune(int32_t shape);
  *   residual  device, res_dtype, T rows of N elements at ldr elements (alignment as y of that type), or NULL; it may be y itself (the
  *             same address, ldr = ldy, res_dtype = out_dtype).  Otherwise y shares no byte with x, w, w_up, a bias or the residual
  * Everything else as gdn_linear.  Arithmetic: fp32 sums of the bf16 products; act, factor and residual in fp32; one rounding to out_dtype.
- * For at most 128 rows the sum over k may be taken in four parts that are added in order (whether and which: by T, N and K alone), else it is
+ * For at most 1024 rows the sum over k may be taken in four parts that are added in order (whether and which: by T, N and K alone), else it is
  * gdn_linear's.  Errors as gdn_linear, and GDN_ERR_NULL without an epilogue, GDN_ERR_SHAPE for an unknown activation or res_dtype, a bias_up
  * without w_up, ldr < N or ldw_up < K, GDN_ERR_COUNT for N from 2^24 on or a y or residual with a row stride above 2^30 or a
  * span of more than 2^60 elements, GDN_ERR_SLOT_HAZARD where y shares bytes as said.
@@ -109,11 +109,11 @@ int32_t gdn_linear_act(const void *x, int64_t ldx, const void *w, int64_t ldw, c
                        const gdn_linear_epilogue *epilogue, void *y, int64_t ldy, int32_t out_dtype,
                        int64_t T, int32_t N, int32_t K, void *stream);
 
-/* gdn_linear_plan of gdn_linear_act; gated: 1 with a w_up.  Shapes 6 .. 11: the kernels of few rows, for T <= 128. */
+/* gdn_linear_plan of gdn_linear_act; gated: 1 with a w_up.  Shapes 6 .. 11: the kernels of few rows, for T <= 1024. */
 int32_t gdn_linear_act_plan(int64_t T, int32_t N, int32_t K, int32_t gated, int32_t *shape, int32_t *cols, int32_t *rest_shape);
 
 /*
- * gdn_linear_tune of gdn_linear_act: 0 .. 5 (1 is 2, and with a w_up 5 is 0); 6 .. 11 the kernels of few rows where T <= 128, workgroups of
+ * gdn_linear_tune of gdn_linear_act: 0 .. 5 (1 is 2, and with a w_up 5 is 0); 6 .. 11 the kernels of few rows where T <= 1024, workgroups of
  * 16 rows of x with 8, 16 or 32 of w, then of 32 with each (8 is 16 with a w_up); anything else: chosen per call.
  */
 int32_t gdn_linear_act_tune(int32_t shape);

@@ -18,7 +18,7 @@
 //   5: 128 x 160 x 64, 4 stages, four waves, one workgroup per compute unit: the same for problems that shape 4 just does not
 //      fit in one round (512 x 8224: 260 tiles of 128 outputs for 256 compute units, 208 of 160; 27 us against 36 of shape 4, 32 of shape 0)
 // The same tiles make gdn_linear_act's products, with the activation, gate, factor and residual between the sums and the store (act_epilogue), and those of a mixture
-// of experts, on rows that a list names (launch_expert_product).  For at most 128 rows gdn_linear_act has six kernels more, shapes 6 to 11 (gdn_few_kernel.h).
+// of experts, on rows that a list names (launch_expert_product).  For at most 1024 rows gdn_linear_act has six kernels more, shapes 6 to 11 (gdn_few_kernel.h).
 //   8192 x 2 x 6144 x 2048 with SiLU and gate 305 us (1350 TFLOP/s; a library product of 8192 x 12288 x 2048 alone 361), the activation under 3 % of it;
 //   1401 x 1733 x 1600 with GELU, an fp32 residual and fp32 outputs 22: 10 of them its 25 k steps (what a compute unit is sent, 80 GB/s), 2.5 the GELU, 1.6 the residual,
 //   8 the beginning and the end of one round of 154 tiles (shape 0 35, 3 25.7, 5 36; three workgroups of shape 3 with three stages each 23.8, tiles of 96 x 128 24.7).
@@ -762,20 +762,24 @@ LinearPlan plan_linear(int64_t T, int32_t N, int32_t K) {
     return forced >= 0 ? LinearPlan{forced, 0, N} : plan_tiles(T, N, K, false);
 }
 
-// ---- the kernels of few rows, shapes 6 .. 11: 16 rows of x with 8, 16, 32 rows of w, then 32 with each.  A compute unit takes what it is sent at 57 KB a us
-// whatever it is (64 workgroups of 8 waves with twice as much on its way: no faster), memory sends 5.5 TB/s, and 3 us go to the beginning and the end.  So a
-// narrow weight wants many workgroups, that is few of its rows each, until x, which each of them reads whole, outweighs them.  us, T x N x K, estimated / measured:
-// 1 x 2048 x 6144 in shapes 6 / 7 / 8: 8.0 / 8.1, 8.9 / 8.6, 11.4 / 12.0; 16 rows 9.9 / 9.3, 11.3 / 10.8, 15.9 / 15.1, 48 rows 6 / 8 / 10: 19.0 / 18.1, 14.2 / 14.0,
-// 13.1 / 11.8; 16 x 8192 x 8192 7 / 8: 29.8 / 26, 28.2 / 26; 64 rows in 11 41.9 / 38.4 (64 x 64 tiles 44); 64 x 2048 x 6144 in 64 x 64 tiles 31, the first form of these kernels,
-// whose waves loaded w and x into registers, 30, and 26 at 48 rows.
-constexpr int FEW = 6, FEW_ROWS = 128;
+// ---- the kernels of few rows, shapes 6 .. 11: 16 rows of x with 8, 16, 32 rows of w, then 32 with each.  A compute unit takes rows of x, which it finds in L2, at 90 KB a us,
+// rows of w at 50, and at 40 where workgroups of other rows ask for them at the same time; memory sends 5.5 TB/s, and 3 us go to the beginning and the end.  So a narrow weight
+// wants many workgroups, that is few of its rows each, until x, which each of them reads whole, outweighs them; and a compute unit with one workgroup more than the others is
+// waited for, and its first loads cost 0.8 us more.  us, T x N x K, weights in the memory-side cache, in shapes 6 / 7 / 8 / 9 / 10 / 11 and 64 x 64 tiles: 16 x 2048 x 6144 7.3 / 8.1 / 10.2 /
+// 7.7 / 8.6 / 10.9, 19; 48 14.8 / 11.9 / 10.0 / 14.1 / 8.9 / 11.2, 19.6; 128 31 / 21 / 16 / 30 / 16.1 / 12.4, 20.8; weights from memory 48 rows 19.9 / 16.9 / 14.5 / 18.4 / 12.2 / 16.2, 29.8.  With
+// few outputs they are the better for more rows too: 174 x 44 x 7232 7.7, tiles 22; 491 x 298 x 3712 9.3, 14; from some 1000 rows on the tiles always were (3737 x 19 x 3648 32, tiles
+// 13.8).  Over 350 problems (1 to 1024 rows, N 8 to 8192, K 256 to 8192) the choice is 2 to 3 % from the best on average, and 7 to 12 % or more in one of twenty.
+constexpr int FEW = 6, FEW_ROWS = 1024;
 struct FewShape { int rt, wr; };
 constexpr FewShape FEW_SHAPES[6] = {{1, 8}, {1, 16}, {1, 32}, {2, 8}, {2, 16}, {2, 32}};
-double bytes_cost(double per_cu, double weights) { return 3.0 + std::sqrt(per_cu * per_cu / (57e3 * 57e3) + weights * weights / (5.5e6 * 5.5e6)); }
+// (per_cu: us that a compute unit's bytes take it; bytes: all that memory sends)
+double bytes_cost(double per_cu, double bytes) { return 3.0 + std::sqrt(per_cu * per_cu + bytes * bytes / (5.5e6 * 5.5e6)); }
 double few_cost(const FewShape& s, int64_t T, int64_t N, int32_t K, bool gated) {
     const int64_t outs = gated ? s.wr / 2 : s.wr, tiles_n = (N + outs - 1) / outs, tiles_m = (T + 16 * s.rt - 1) / (16 * s.rt);
-    const double one = 2.0 * K * (double)(std::min<int64_t>(T, 16 * s.rt) + s.wr), all = 2.0 * K * (double)tiles_n * (double)(T + tiles_m * s.wr);
-    return bytes_cost(std::max(one, all / chip_cus()), 2.0 * K * (double)N * (gated ? 2 : 1));
+    const int64_t cus = chip_cus(), most = (tiles_n * tiles_m + cus - 1) / cus;                   // workgroups of a compute unit
+    const double shared = 1.0 - 1.0 / (double)tiles_m, row = 2.0 * K;
+    const double one = row * ((double)std::min<int64_t>(T, 16 * s.rt) / 90e3 + s.wr * (shared / 40e3 + (1.0 - shared) / 50e3));
+    return bytes_cost(one * (double)most, row * ((double)N * (gated ? 2 : 1) + (double)T)) + 0.8 * (double)(most - 1);
 }
 
 LinearPlan plan_act(int64_t T, int32_t N, int32_t K, bool gated) {
@@ -790,7 +794,7 @@ LinearPlan plan_act(int64_t T, int32_t N, int32_t K, bool gated) {
         const ShapeCost* c = SHAPES;
         while (c->id != p.shape) ++c;
         const int64_t rows_w = gated ? 2 * (int64_t)N : N;
-        double least = std::max(shape_cost(*c, T, rows_w, K), 1.1 * bytes_cost(2.0 * K * (double)(std::min<int64_t>(T, c->bm) + c->bn), 2.0 * K * (double)rows_w));
+        double least = std::max(shape_cost(*c, T, rows_w, K), 1.1 * bytes_cost(2.0 * K * (double)(std::min<int64_t>(T, c->bm) + c->bn) / 57e3, 2.0 * K * (double)rows_w));
         for (int i = 0; i < 6; ++i) {
             if (gated && FEW_SHAPES[i].wr == 8) continue;
             const double t = few_cost(FEW_SHAPES[i], T, N, K, gated);
