@@ -224,7 +224,8 @@ extern "C" int32_t gdn_moe(const gdn_moe_shape* s, const void* x, int64_t ldx, c
     const int forced = g_moe_shape.load();
     const int shape = forced >= 0 && forced != FEW ? forced : choose_shape(*s, T);
     a.tile_rows = linear::expert_tile_rows(shape);
-    if (T == 1) launch_logits<1, 2, 4>(a, stream);
+    if (T * E <= 4096) launch_logits<1, 1, 4>(a, stream);
+    else if (T * E <= 8192) launch_logits<2, 1, 4>(a, stream);
     else if (T * E <= 16384) launch_logits<2, 2, 2>(a, stream);
     else hipLaunchKernelGGL(moe_logits_kernel<8>, dim3((unsigned)((T + 15) / 16), (unsigned)((E + 15) / 16)), dim3(64 * 8), 0, stream, a);
     if (forced == FEW ? T <= MOST_FEW : forced < 0 && T <= MOST_FEW && few_pays(*s, T)) return hip_err(launch_few(a, stream));

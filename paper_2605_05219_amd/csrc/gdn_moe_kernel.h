@@ -85,8 +85,9 @@ __device__ __forceinline__ double wave_total(double v) {
 // work is split: in fp64 a sum of products of two bf16 numbers is exact but for terms 2^30 times smaller than the largest, whatever the order, and equal rows of
 // w_router give equal keys.
 //
-// Few tokens: a wave makes TE experts x TT tokens, its lanes along D, 8 elements at a time, U such pieces of a row on their way at once: the time of a single token is
-// the latency of its loads (128 experts 5 us).
+// Few tokens: a wave makes TE experts x TT tokens, its lanes along D, 8 elements at a time, U such pieces of a row on their way at once: the time is the latency of
+// its loads and of the conversions behind them, so that few sums are given a wave each (1 token x 128 experts, D 2048: 3.7 us, 5.0 with two experts to a wave;
+// 64 x 128 7.1 with two tokens to a wave, 7.5 with two of each).
 template <int TT, int TE, int U>
 __global__ void __launch_bounds__(256) moe_logits_few_kernel(MoeArgs a) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -152,7 +153,7 @@ __global__ void __launch_bounds__(256) moe_logits_few_kernel(MoeArgs a) {
 // More: a workgroup makes 16 experts x 16 tokens on v_mfma_f64_16x16x4_f64 (lane: row lane % 16 of either operand and one k of its group of 16 lanes; of the result
 // token lane % 16, register r expert lane / 16 + 4 r), its waves the blocks of 32 k in turn: a lane loads 8 adjacent elements of each row, and which k a product
 // pairs is the same for both.  Making fp64 of the elements is what the vector units spend most on, and a matrix product takes sixteen uses of each: 200 tokens x 512
-// experts, D 2048, 17 us, 2048 x 64 17.5 (by 4 x 4 on the vector units 27 and 35; 1 x 128 8.5, 64 x 128 9.6 against 5 and 7.5 of the kernel above).
+// experts, D 2048, 17 us, 2048 x 64 17.5 (by 4 x 4 on the vector units 27 and 35; 1 x 128 8.5, 64 x 128 9.6 against 3.7 and 7.1 of the kernel above).
 template <int WAVES>
 __global__ void __launch_bounds__(64 * WAVES) moe_logits_kernel(MoeArgs a) {
     typedef double f64x4 __attribute__((ext_vector_type(4)));
