@@ -782,9 +782,15 @@ double few_cost(const FewShape& s, int64_t T, int64_t N, int32_t K, bool gated) 
     return bytes_cost(one * (double)most, row * ((double)N * (gated ? 2 : 1) + (double)T)) + 0.8 * (double)(most - 1);
 }
 
+// (a launch has less than 2^32 threads)
+bool few_fits(const FewShape& s, int64_t T, int64_t N, bool gated) {
+    const int64_t outs = gated ? s.wr / 2 : s.wr;
+    return T <= FEW_ROWS && (N / outs + 16) * ((T + 16 * s.rt - 1) / (16 * s.rt)) < (int64_t)1 << 24;
+}
 LinearPlan plan_act(int64_t T, int32_t N, int32_t K, bool gated) {
-    const int forced = g_act_shape.load();
-    if (forced >= FEW && T <= FEW_ROWS) return {gated && FEW_SHAPES[forced - FEW].wr == 8 ? forced + 1 : forced, 0, N};
+    int forced = g_act_shape.load();
+    if (gated && forced >= FEW && FEW_SHAPES[forced - FEW].wr == 8) ++forced;
+    if (forced >= FEW && few_fits(FEW_SHAPES[forced - FEW], T, N, gated)) return {forced, 0, N};
     if (forced >= 0 && forced < FEW) return {forced == 1 ? 2 : gated && forced == 5 ? 0 : forced, 0, N};
     if (gated && N > INT32_MAX / 2) return {2, 0, N};
     LinearPlan p = plan_tiles(T, gated ? 2 * N : N, K, gated);
@@ -796,7 +802,7 @@ LinearPlan plan_act(int64_t T, int32_t N, int32_t K, bool gated) {
         const int64_t rows_w = gated ? 2 * (int64_t)N : N;
         double least = std::max(shape_cost(*c, T, rows_w, K), 1.1 * bytes_cost(2.0 * K * (double)(std::min<int64_t>(T, c->bm) + c->bn) / 57e3, 2.0 * K * (double)rows_w));
         for (int i = 0; i < 6; ++i) {
-            if (gated && FEW_SHAPES[i].wr == 8) continue;
+            if ((gated && FEW_SHAPES[i].wr == 8) || !few_fits(FEW_SHAPES[i], T, N, gated)) continue;
             const double t = few_cost(FEW_SHAPES[i], T, N, K, gated);
             if (t < least) { least = t; p = {FEW + i, 0, gated ? 2 * N : N}; }
         }
@@ -984,7 +990,7 @@ extern "C" int32_t gdn_linear_act(const void* x, int64_t ldx, const void* w, int
     if (off_align(epi->bias_up, 4)) return GDN_ERR_ALIGN;
     if (epi->residual && (off_align(epi->residual, rs == 2 ? 8 : 16) || (epi->ldr & 3))) return GDN_ERR_ALIGN;
     if (epi->w_up && epi->ldw_up >= ((int64_t)1 << 22)) return GDN_ERR_COUNT;
-    // a kernel of few rows has as many threads as that, and the tensors' spans have to fit 63 bits
+    // a kernel of a few rows has some 32 threads to an output, a launch less than 2^32, and the tensors' spans have to fit 63 bits
     const int64_t most = std::min((int64_t)1 << 30, ((int64_t)1 << 60) / T);
     if (N >= 1 << 24 || ldy > most || (epi->residual && epi->ldr > most)) return GDN_ERR_COUNT;
     const Rows out(y, T, ldy * es, (int64_t)N * es), res(epi->residual, T, epi->ldr * rs, (int64_t)N * rs);

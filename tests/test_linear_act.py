@@ -291,3 +291,14 @@ def test_spans_past_63_bits_and_more_outputs_than_threads_are_refused():
     assert raw(dict(ldr=1 << 24), T=1 << 37, N=64) == -11
     assert raw(dict(ldw_up=1 << 60)) == -11
     assert raw(dict(ldr=1 << 24), N=1 << 24, ldy=1 << 24) == -11
+
+
+def test_kernels_of_few_rows_keep_to_the_threads_of_a_launch():
+    for knob in range(6, 12):
+        prev = LN.gdn_linear_act_tune(knob)
+        try:
+            for gated in (False, True):
+                assert LN.gdn_linear_act_plan(1024, (1 << 24) - 1, 64, gated)[0] < 6
+                assert LN.gdn_linear_act_plan(16, 1 << 20, 64, gated)[0] >= 6
+        finally:
+            LN.gdn_linear_act_tune(prev)
