@@ -60,9 +60,9 @@ hipError_t launch_few_kernel(dim3 grid, int waves, int smem, const MoeArgs& a, h
     hipLaunchKernelGGL(KERNEL, grid, dim3(64 * waves), smem, stream, a);
     return hipGetLastError();
 }
-template <int P>
+template <typename C, int P>
 hipError_t launch_up_few(const MoeArgs& a, hipStream_t stream) {
-    return launch_few_kernel<moe_up_few_kernel<P>>(dim3((unsigned)(a.F / 16), (unsigned)(a.T * a.k)), UpFew::WAVES, UpFew::SMEM, a, stream);
+    return launch_few_kernel<moe_up_few_kernel<C, P>>(dim3((unsigned)(2 * a.F / C::WR), (unsigned)(a.T * a.k)), C::WAVES, C::SMEM, a, stream);
 }
 template <typename C>
 hipError_t launch_down_few(const MoeArgs& a, hipStream_t stream) {
@@ -82,16 +82,19 @@ void launch_choices(const MoeArgs& a, hipStream_t stream) {
     by_experts(a.E, [&](auto p) { hipLaunchKernelGGL((moe_route_kernel<decltype(p)::value>), dim3((unsigned)((a.T + 3) / 4)), dim3(256), 0, stream, a); });
 }
 hipError_t launch_few(const MoeArgs& a, hipStream_t stream) {
-    // Every workgroup of the first product chooses anew where all of them are on the chip at once, two to a compute unit: a launch less.  In more rounds the choice, 2 us and with
-    // many experts 4, comes once in each.  us, chosen inside / by a launch: 1 token of 128 experts, k 8, F 768 (384 workgroups) 25.2 / 27.0; 2 35 / 35; 4 of 512, F 256 (512) 20.8 / 22.6, 8
-    // 29.7 / 27.3, 32 93 / 65; 16 of 512, k 10, F 512 209 / 172.
-    const bool inside = (int64_t)a.T * a.k * (a.F / 16) <= 2 * chip_cus();
+    // Every workgroup of the first product chooses anew where all of them are on the chip at once: a launch less.  In more rounds the choice, 2 us and with
+    // many experts 4, comes once in each.  us, chosen inside / by a launch: 1 token of 128 experts, k 8, F 768 25.2 / 27.0; 2 35 / 35; 4 of 512, F 256 20.8 / 22.6, 8 29.7 / 27.3, 32
+    // 93 / 65; 16 of 512, k 10, F 512 209 / 172.  Workgroups of 16 of F, two to a compute unit, or of 8, three: the smaller spread more evenly until there are many.  us, 16 / 8 (and workgroups
+    // of 16): 128 experts, k 8, D 2048, F 768: 23.8 / 22.8 (384), 35.3 / 33.1 (768), 57 / 55 (1536), 98 / 101 (3072); 256, F 512: 25.4 / 28.4 (512, of which those of 8 are more than a round); 64, k 6, F 1408:
+    // 30.9 / 29.8 (528), 73 / 75 (2112).
+    const int64_t wide_ones = (int64_t)a.T * a.k * (a.F / 16), cus = chip_cus();
+    const bool inside = wide_ones <= 2 * cus, wide = inside ? 2 * wide_ones > 3 * cus : wide_ones > 6 * cus;
     hipError_t e;
     if (inside) {
-        e = by_experts(a.E, [&](auto p) { return launch_up_few<decltype(p)::value>(a, stream); });
+        e = by_experts(a.E, [&](auto p) { return wide ? launch_up_few<few::Few<1, 32, 4, 3>, decltype(p)::value>(a, stream) : launch_up_few<few::Few<1, 16, 4, 3>, decltype(p)::value>(a, stream); });
     } else {
         launch_choices(a, stream);
-        e = launch_up_few<0>(a, stream);
+        e = wide ? launch_up_few<few::Few<1, 32, 4, 3>, 0>(a, stream) : launch_up_few<few::Few<1, 16, 4, 3>, 0>(a, stream);
     }
     if (e != hipSuccess) return e;
     // a narrow output in workgroups of 8 of its rows, so that there is one for every compute unit

@@ -446,14 +446,13 @@ __global__ void __launch_bounds__(256) moe_sum_kernel(MoeArgs a) {
 
 // ---- A few tokens: the choice with the first product, the second one with the sum, in two launches behind the router's sums, by the waves and rings of
 // gdn_few_kernel.h.  P > 0: every workgroup of a token chooses anew; P = 0: the choices have been made.
-typedef few::Few<1, 32, 4, 3> UpFew;
-template <int P>
-__global__ void __launch_bounds__(64 * UpFew::WAVES) moe_up_few_kernel(MoeArgs a) {      // 16 of a choice's F; grid: (F / 16, T k)
+template <typename C, int P>
+__global__ void __launch_bounds__(64 * C::WAVES) moe_up_few_kernel(MoeArgs a) {          // WR / 2 of a choice's F; grid: (2 F / WR, T k)
     extern __shared__ __align__(16) char smem[];
     __shared__ int32_t chosen;
     __shared__ float weight;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int pair = blockIdx.y, t = pair / a.k, j = pair % a.k, f0 = blockIdx.x * 16;
+    const int pair = blockIdx.y, t = pair / a.k, j = pair % a.k, f0 = blockIdx.x * (C::WR / 2);
     if constexpr (P > 0) {
         if (wave == 0) {
             int id;
@@ -470,23 +469,25 @@ __global__ void __launch_bounds__(64 * UpFew::WAVES) moe_up_few_kernel(MoeArgs a
     }
     const int e = __builtin_amdgcn_readfirstlane(P > 0 ? chosen : a.ids[pair]);
     if (e < 0) return;
-    const int bytes = 15 * a.D * 2 + a.D * 2;
+    const int bytes = C::WR / 2 * a.D * 2;
     const few::Part gate = {reinterpret_cast<const char*>(a.w_gate_up + ((int64_t)e * 2 * a.F + f0) * a.D), bytes, a.D * 2};
     const few::Part up = {gate.at + (int64_t)a.F * a.D * 2, bytes, a.D * 2};
     const few::Part x = {reinterpret_cast<const char*>(a.x + t * a.ldx), a.D * 2, a.D * 2};      // one row: the others of its tile are behind its end, zeros
-    f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    f32x4 acc[C::CT];
+#pragma unroll
+    for (int i = 0; i < C::CT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int steps = a.D / few::STEP, first = (int)((blockIdx.x + 3 * blockIdx.y) * 5u % (uint32_t)steps);
-    UpFew::sums_of(acc, gate, up, x, steps,
+    C::sums_of(acc, gate, up, x, steps,
                    [&](int step, few::Part&, few::Part&, few::Part&) { return (step + first >= steps ? step + first - steps : step + first) * few::STEP * 2; },
-                   smem + wave * UpFew::RING, wave, lane);
+                   smem + wave * C::RING, wave, lane);
     __builtin_amdgcn_s_waitcnt(0x0F70);                          // (no load of an empty descriptor writes behind the sums)
     __syncthreads();
     f32x4* const sums = reinterpret_cast<f32x4*>(smem);
-    UpFew::put_sums(acc, sums, wave, lane);
+    C::put_sums(acc, sums, wave, lane);
     __syncthreads();
-    if (threadIdx.x < 4) {
+    if (threadIdx.x < C::WR / 8) {
         const int piece = threadIdx.x;
-        const f32x4 v = (P > 0 ? weight : a.weights[pair]) * (activate(a.act, UpFew::get_sum(sums, 0, piece)) * UpFew::get_sum(sums, 0, piece + 4));
+        const f32x4 v = (P > 0 ? weight : a.weights[pair]) * (activate(a.act, C::get_sum(sums, 0, piece)) * C::get_sum(sums, 0, piece + C::WR / 8));
         *reinterpret_cast<bf16x4*>(a.h + (int64_t)pair * a.F + f0 + 4 * piece) = __builtin_convertvector(v, bf16x4);
     }
 }

@@ -385,3 +385,14 @@ def test_more_tokens_than_a_grid_has_rows():
     worst = np.abs(f64(c.y[some]) - y) - (ey + 2.0 ** -8 * (np.abs(y) + ey) + 2.0 ** -134)
     assert not np.isnan(worst).any() and worst.max() <= 0, float(worst.max())
     assert (c.all[T:] == 77).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("E", [60, 100, 200, 400, 1000])
+@pytest.mark.parametrize("T,F", [(9, 64), (25, 64), (25, 192), (32, 320)])
+def test_few_tokens_on_few_and_many_workgroups(knob, E, T, F):
+    """The kernels of few tokens whose first product has fewer workgroups than the chip, about as many, and more, with every number of experts to a lane."""
+    knob(6)
+    bias = np.zeros(E)
+    bias[E // 2] = 20                                                 # one that all tokens take
+    Call(T, E, 4, 192, F, "silu", "sigmoid", True, 2.0, router="f32", bias=bias, add=bool(T % 2), pad=8, seed=E).run().check()
