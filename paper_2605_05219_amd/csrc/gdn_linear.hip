@@ -20,7 +20,7 @@
 // The same tiles make gdn_linear_act's products, with the activation, gate, factor and residual between the sums and the store (act_epilogue), and those of a mixture
 // of experts, on rows that a list names (launch_expert_product).  For at most 1024 rows gdn_linear_act has six kernels more, shapes 6 to 11 (gdn_few_kernel.h).
 //   8192 x 2 x 6144 x 2048 with SiLU and gate 305 us (1350 TFLOP/s; a library product of 8192 x 12288 x 2048 alone 361), the activation under 3 % of it;
-//   1401 x 1733 x 1600 with GELU, an fp32 residual and fp32 outputs 22: 10 of them its 25 k steps (what a compute unit is sent, 80 GB/s), 2.5 the GELU, 1.6 the residual,
+//   1401 x 1733 x 1600 with GELU, an fp32 residual and fp32 outputs 21.6: 10 of them its 25 k steps (what a compute unit is sent, 80 GB/s), 2.5 the GELU, 1.6 the residual,
 //   8 the beginning and the end of one round of 154 tiles (shape 0 35, 3 25.7, 5 36; three workgroups of shape 3 with three stages each 23.8, tiles of 96 x 128 24.7).
 // The products are v_mfma_f32_16x16x32_bf16: half the accumulator traffic per flop of the 32 x 32 x 16 instruction, at the same rate on
 // paper; on a chip held by its power limit 8192 x 2048 x 2048 takes 51 us with it and 56 with the other, 512 x 2048 10.4 and 12.3.
@@ -184,7 +184,7 @@ __device__ __forceinline__ void act_epilogue(const typename EpiArgs<EPI>::type& 
                 for (int i = 0; i < IT; ++i) {
                     const int64_t tok = tok0 + t0 + RPI * i + lane / LPR;
                     const int col = col0 + c0 + lane % LPR * OPL;
-                    if (tok >= n_rows || col + OPL > a.N) continue;      // (the last columns one by one below)
+                    if (tok >= n_rows || col + OPL > a.N) continue;      // (the last columns below)
                     if (a.res_f32) {
                         const u32x4* r = reinterpret_cast<const u32x4*>(static_cast<const float*>(a.residual) + tok * a.ldr + col);
                         res[i][0] = r[0];
@@ -226,7 +226,7 @@ __device__ __forceinline__ void act_epilogue(const typename EpiArgs<EPI>::type& 
                     v[h] = *reinterpret_cast<const f32x4*>(reg + row * RBY + (((first / 4 + h) ^ (row % PPR)) << 4));
                 int64_t tok = tok0 + t0 + row;
                 const int col = col0 + c0 + first;
-                if (tok >= n_rows || col >= a.N) continue;
+                if (tok >= n_rows || col + OPL > a.N) continue;
                 float scale = a.scale;
                 if constexpr (epi_expert(EPI)) {
                     tok = list[tok];
@@ -234,21 +234,14 @@ __device__ __forceinline__ void act_epilogue(const typename EpiArgs<EPI>::type& 
                 }
 #pragma unroll
                 for (int h = 0; h < OPL / 4; ++h) v[h] *= scale;
-                const bool whole = col + OPL <= a.N;
                 if (!epi_expert(EPI) && a.residual) {
-                    if (whole && a.res_f32) {
+                    if (a.res_f32) {
 #pragma unroll
                         for (int h = 0; h < OPL / 4; ++h) v[h] += __builtin_bit_cast(f32x4, res[i][h]);
-                    } else if (whole) {
-#pragma unroll
-                        for (int e = 0; e < OPL; ++e)
-                            v[e / 4][e % 4] += __uint_as_float(e & 1 ? res[i][0][e / 2] & 0xffff0000u : res[i][0][e / 2] << 16);
                     } else {
 #pragma unroll
                         for (int e = 0; e < OPL; ++e)
-                            if (col + e < a.N)
-                                v[e / 4][e % 4] += a.res_f32 ? static_cast<const float*>(a.residual)[tok * a.ldr + col + e]
-                                                             : __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.residual)[tok * a.ldr + col + e] << 16);
+                            v[e / 4][e % 4] += __uint_as_float(e & 1 ? res[i][0][e / 2] & 0xffff0000u : res[i][0][e / 2] << 16);
                     }
                 }
                 char* const p = static_cast<char*>(a.y) + (tok * a.ldy + col) * (OUT_BF16 ? 2 : 4);
@@ -256,17 +249,37 @@ __device__ __forceinline__ void act_epilogue(const typename EpiArgs<EPI>::type& 
                     bf16x8 o;
 #pragma unroll
                     for (int e = 0; e < OPL; ++e) o[e] = (__bf16)v[e / 4][e % 4];
-                    if (whole) *reinterpret_cast<bf16x8*>(p) = o;
-                    else
-#pragma unroll
-                        for (int e = 0; e < OPL; ++e)
-                            if (col + e < a.N) reinterpret_cast<__bf16*>(p)[e] = o[e];
-                } else if (whole) {
-                    *reinterpret_cast<f32x4*>(p) = v[0];
+                    *reinterpret_cast<bf16x8*>(p) = o;
                 } else {
+                    *reinterpret_cast<f32x4*>(p) = v[0];
+                }
+            }
+            if constexpr (!epi_expert(EPI)) {
+                // The last columns, where they are no whole store: an element to a lane, all residuals asked for before the first is used (a lane with its row's
+                // elements one after the other waits for each of its rows: 1313 x 7414 x 128 onto a residual 35 us, 25 so, and 20 with 7416).
+                const int tail = a.N / OPL * OPL, first = tail - (col0 + c0);
+                if (tail < a.N && first >= 0 && first < PW) {
+                    constexpr int ROWS = 64 / OPL, STEPS = TP / ROWS;
+                    const int e = lane % OPL, col = tail + e;
+                    float one[STEPS];
 #pragma unroll
-                    for (int e = 0; e < OPL; ++e)
-                        if (col + e < a.N) reinterpret_cast<float*>(p)[e] = v[0][e];
+                    for (int i = 0; i < STEPS; ++i) {
+                        const int64_t tok = tok0 + t0 + ROWS * i + lane / OPL;
+                        one[i] = 0.f;
+                        if (tok >= n_rows || col >= a.N || !a.residual) continue;
+                        if (a.res_f32) one[i] = static_cast<const float*>(a.residual)[tok * a.ldr + col];
+                        else one[i] = __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.residual)[tok * a.ldr + col] << 16);
+                    }
+#pragma unroll
+                    for (int i = 0; i < STEPS; ++i) {
+                        const int row = ROWS * i + lane / OPL;
+                        const int64_t tok = tok0 + t0 + row;
+                        if (tok >= n_rows || col >= a.N) continue;
+                        float v = *reinterpret_cast<const float*>(reg + row * RBY + ((((first + e) / 4) ^ (row % PPR)) << 4) + (first + e) % 4 * 4) * a.scale;
+                        if (a.residual) v += one[i];
+                        if (OUT_BF16) static_cast<__bf16*>(a.y)[tok * a.ldy + col] = (__bf16)v;
+                        else static_cast<float*>(a.y)[tok * a.ldy + col] = v;
+                    }
                 }
             }
         }
