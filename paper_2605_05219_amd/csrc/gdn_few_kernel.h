@@ -10,20 +10,14 @@
 
 #include <cstdint>
 
+#include "gdn_few_parts.h"
+
 namespace gdn {
 namespace few {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
-constexpr int STEP = 64;                          // k of a step: a row of 128 bytes
-
-// Rows of a matrix: where they begin, the bytes up to the last one's end (what lies behind arrives as zeros), the bytes from one to the next.
-struct Part {
-    const char* at;
-    int bytes, pitch;
-};
 
 // RT: tiles of 16 rows of x; WR: weight rows of a workgroup (8, 16 or 32); WAVES waves; S steps of a wave on their way
 template <int RT_, int WR_, int WAVES_, int S_>
@@ -60,12 +54,10 @@ struct Few {
     static __device__ __forceinline__ void sums_of(f32x4* acc, const Part& w0, const Part& w1, const Part& x, int steps, PLACE place, char* ring, int wave, int lane) {
         const int row = lane >> 3, pos = lane & 7;    // of a load: lane i lands at row i / 8, piece i % 8
         int xoff[X_LOADS], woff[W_LOADS];
-        // piece p of row r lies at p ^ (r / 2) % 8: 16 rows' pieces of one k then spread over the banks
 #pragma unroll
-        for (int j = 0; j < X_LOADS; ++j) xoff[j] = (8 * j + row) * x.pitch + ((pos ^ (((8 * j + row) >> 1) & 7)) << 4);
+        for (int j = 0; j < X_LOADS; ++j) xoff[j] = load_offset(8 * j + row, 8 * j + row, pos, x.pitch);
 #pragma unroll
-        for (int j = 0; j < W_LOADS; ++j)
-            woff[j] = (8 * (j >= HALF ? j - HALF : j) + row) * (j >= HALF ? w1.pitch : w0.pitch) + ((pos ^ (((8 * j + row) >> 1) & 7)) << 4);
+        for (int j = 0; j < W_LOADS; ++j) woff[j] = load_offset(8 * j + row, 8 * (j >= HALF ? j - HALF : j) + row, pos, j >= HALF ? w1.pitch : w0.pitch);
         auto load = [&](int slot, int step) {
             Part v0 = w0, v1 = w1, vx = x;
             const bool live = step < steps;

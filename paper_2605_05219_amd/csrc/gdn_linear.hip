@@ -612,11 +612,7 @@ __global__ void __launch_bounds__(64 * C::WAVES) gdn_linear_few_kernel(LinearAct
     constexpr int OUTS = GATED ? C::WR / 2 : C::WR;
     const int n0 = tile_n * OUTS, m0 = tile_m * C::ROWS;
     const int rows_x = min((int)a.T - m0, C::ROWS);
-    auto weights = [&](const void* w, int64_t ld, int first) {
-        const int rows = a.N - first;
-        return few::Part{static_cast<const char*>(w) + (int64_t)min(first, a.N - 1) * ld * 2,
-                         rows > 0 ? (int)((int64_t)(min(rows, C::WR) - 1) * ld * 2 + (int64_t)a.K * 2) : 0, (int)(ld * 2)};
-    };
+    auto weights = [&](const void* w, int64_t ld, int first) { return few::rows_from(w, ld, a.N, a.K, first, C::WR); };
     const few::Part x = {static_cast<const char*>(a.x) + (int64_t)m0 * a.ldx * 2, (int)((int64_t)(rows_x - 1) * a.ldx * 2 + (int64_t)a.K * 2), (int)(a.ldx * 2)};
     f32x4 acc[C::CT * C::RT];
 #pragma unroll
