@@ -34,7 +34,8 @@
  *   (T k F) span less than 2^30 elements: longer batches go in parts.
  * Arithmetic: the router's sums in fp64; bf16 products with fp32 sums in the experts; h is rounded to bf16, as the next product's
  * operand, behind its weight; the choices are added in fp32; one rounding to y.  (For few tokens a token's choices are summed as one product, for
- * more each by itself and then in the order of their keys: the same but for the order of fp32 additions.)
+ * more each by itself and then in the order of their keys: the same but for the order of fp32 additions.  Which it is depends on the shape and T; within a
+ * call a token's row is the same bits wherever it stands.)
  * Errors: GDN_ERR_NULL, _ALIGN, _SHAPE (a size out of its range, an unknown type, activation or score, a routed_scale that is not finite, an ld
  * smaller than D), _COUNT, _WORKSPACE, _SLOT_HAZARD (y, ids, weights or the workspace share a byte with each other or an input, but for y = add).
  */

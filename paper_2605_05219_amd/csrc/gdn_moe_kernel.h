@@ -476,7 +476,8 @@ __global__ void __launch_bounds__(64 * C::WAVES) moe_up_few_kernel(MoeArgs a) { 
     f32x4 acc[C::CT];
 #pragma unroll
     for (int i = 0; i < C::CT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int steps = a.D / few::STEP, first = (int)((blockIdx.x + 3 * blockIdx.y) * 5u % (uint32_t)steps);
+    // (where k begins, see gdn_linear_few_kernel: by the expert and its rows, not by the choice's place in the batch, so that a row's sums are the same wherever its token stands)
+    const int steps = a.D / few::STEP, first = (int)((blockIdx.x + 3u * (uint32_t)e) * 5u % (uint32_t)steps);
     C::sums_of(acc, gate, up, x, steps,
                    [&](int step, few::Part&, few::Part&, few::Part&) { return (step + first >= steps ? step + first - steps : step + first) * few::STEP * 2; },
                    smem + wave * C::RING, wave, lane);

@@ -396,3 +396,26 @@ def test_few_tokens_on_few_and_many_workgroups(knob, E, T, F):
     bias = np.zeros(E)
     bias[E // 2] = 20                                                 # one that all tokens take
     Call(T, E, 4, 192, F, "silu", "sigmoid", True, 2.0, router="f32", bias=bias, add=bool(T % 2), pad=8, seed=E).run().check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [-1, 0, 2, 3, 6])
+@pytest.mark.parametrize("T,E,k,D,F", [(8, 16, 4, 2048, 128), (24, 8, 3, 1024, 64), (31, 40, 8, 576, 192)])
+def test_a_row_is_the_same_wherever_its_token_stands(knob, shape, T, E, k, D, F):
+    """Equal tokens of one call give equal bits, and so does each token of a batch in another order (T, E, k, D and F choose the kernels; they are the same)."""
+    import torch
+    knob(shape)
+    c = Call(T, E, k, D, F, seed=T)
+    c.x[T // 2:2 * (T // 2)] = c.x[:T // 2]
+    c.run()
+    torch.cuda.synchronize()
+    half = T // 2
+    assert torch.equal(c.ids[:half], c.ids[half:2 * half]) and torch.equal(c.weights[:half], c.weights[half:2 * half])
+    assert torch.equal(c.y[:half], c.y[half:2 * half])
+    want = c.y.clone()
+    order = torch.randperm(T, generator=torch.Generator().manual_seed(T)).cuda()
+    c.x.copy_(c.x[order])
+    c.run()
+    torch.cuda.synchronize()
+    assert torch.equal(c.y, want[order])
+    c.check()
