@@ -13,7 +13,7 @@
  *     the k experts of the largest keys, of equal ones those of the lowest index first.  A key of -infinity is never chosen (fewer
  *     than k may be); a NaN is behind every other key that can be
  *     p[j]   = softmax over all e of l, or sigmoid(l), at the j-th choice; divided by the sum of the k with `normalise` (a
- *              sum of zero leaves zeros); * routed_scale
+ *              sum of zero, which only logits of -infinity give, leaves zeros); * routed_scale
  *     h[j]   = p[j] * act(gate_(e_j) x[t]) * (up_(e_j) x[t])                   rounded once, to bf16
  *     y[t]   = add[t] + sum_j w_down[e_j] h[j]
  *

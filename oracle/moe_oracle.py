@@ -43,7 +43,8 @@ def route(x, w_router, choice_bias, k, score="softmax", normalise=True, routed_s
                 continue
             l = s[t, got]
             if score == "sigmoid":
-                w = 1 / (1 + np.exp(-l))
+                ls = -np.logaddexp(0, -l)    # (by its logarithm: divided by their sum, sigmoids below fp64's range still count)
+                w = np.exp(ls - (ls.max() if normalise and ls.max() != -np.inf else 0))
             else:
                 w = np.exp(l - s[t].max())
                 w = w / np.exp(s[t] - s[t].max()).sum()

@@ -281,8 +281,12 @@ __device__ __forceinline__ void choose(const MoeArgs& a, int t, int lane, int& m
         if (a.normalise) top = wave_fmax(have ? my_l : -__builtin_inff());
         if (have) p = expf(my_l - top);
         if (!a.normalise) p = p / total;
-    } else if (have) {
-        p = 1.f / (1.f + expf(-my_l));
+    } else {
+        // below -64 a sigmoid is e^l to 2^-92: where the largest of the chosen is there and they are divided by their sum, all of them times e^-largest, so that none that
+        // counts is lost to fp32's range (from -88 on 1 / (1 + e^-l) is zero)
+        float from = a.normalise ? wave_fmax(have ? my_l : -__builtin_inff()) : 0.f;
+        if (!(from < -64.f) || from == -__builtin_inff()) from = 0.f;
+        if (have) p = my_l < -64.f ? expf(my_l - from) : 1.f / (1.f + expf(-my_l));
     }
     if (a.normalise) {
         const float sum = wave_sum(p);

@@ -419,3 +419,21 @@ def test_a_row_is_the_same_wherever_its_token_stands(knob, shape, T, E, k, D, F)
     torch.cuda.synchronize()
     assert torch.equal(c.y, want[order])
     c.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [1, 50])
+@pytest.mark.parametrize("normalise", [True, False])
+@pytest.mark.parametrize("logits", [[-95, -90, -96, -103, -91, -94, -89, -92],      # sigmoids between 2^-149 and 2^-126
+                                    [-200, -203, -201, -202, -207, -204, -206, -205],      # keys of zero: the lowest indices
+                                    [-800, -801, -799, -802, -750, -740, -700, -900], [-60, -100, -63.5, -65, -64.5, -88, -200, -300], [-70, 3, -90, -1, -66, -68, -120, -100],
+                                    [float("-inf")] * 8, [-120, float("-inf"), -121, float("-inf"), -122, -123, -124, -125]])
+def test_sigmoids_of_far_logits(T, normalise, logits):
+    """Weights that are divided by their sum are what they are however small the sigmoids, also below the least number of fp32."""
+    import torch
+    c = Call(T, 8, 3, 64, 64, score="sigmoid", normalise=normalise, scale=2.5, add=True, seed=1)
+    c.x[:, 1:], c.x[:, 0] = 0, 1
+    c.wr[:, 1:], c.wr[:, 0] = 0, torch.tensor(logits, device="cuda")
+    c.run().check()
+    if normalise and logits[0] != float("-inf"):
+        assert abs(float(c.weights[0].sum()) - 2.5) < 1e-5
