@@ -302,3 +302,28 @@ def test_kernels_of_few_rows_keep_to_the_threads_of_a_launch():
                 assert LN.gdn_linear_act_plan(16, 1 << 20, 64, gated)[0] >= 6
         finally:
             LN.gdn_linear_act_tune(prev)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh", "sigmoid"])
+@pytest.mark.parametrize("T", [3, 200])
+def test_activations_keep_their_digits_far_out(act, T):
+    """Values that are small because z is far below zero are right to a relative error: of an exponential (its argument + 4) 2^-23, twice that for the roundings of its
+    argument, 8 units for the sums, products, reciprocals and polynomials around it; and what lies below the least normal number may be zero."""
+    import torch
+    from scipy.special import erfc
+    far = {"gelu": 13.0, "gelu_tanh": 9.0}.get(act, 80.0)
+    z = -torch.exp(torch.linspace(np.log(2.0 ** -7), np.log(far), 800, device="cuda", dtype=torch.float64)).bfloat16()
+    K, N = 64, z.numel()
+    x, w = torch.zeros(T, K, device="cuda", dtype=torch.bfloat16), torch.zeros(N, K, device="cuda", dtype=torch.bfloat16)
+    x[:, 0], w[:, 0] = 1, z
+    y = torch.empty(T, N, device="cuda")
+    LN.gdn_linear_act(x, w, None, y, act)
+    z = f64(z)
+    u2 = np.sqrt(8 / np.pi) * (z + 0.044715 * z ** 3)
+    with np.errstate(over="ignore"):                                  # (of the activations that are not looked at)
+        want = {"silu": z / (1 + np.exp(-z)), "gelu": 0.5 * z * erfc(-z / np.sqrt(2)), "gelu_tanh": z / (1 + np.exp(-u2)), "sigmoid": 1 / (1 + np.exp(-z))}[act]
+    arg = {"gelu": z * z / 2, "gelu_tanh": np.abs(u2)}.get(act, np.abs(z))
+    torch.cuda.synchronize()
+    worst = np.abs(f64(y) - want) - ((2 * (arg + 4) + 8) * 2.0 ** -23 * np.abs(want) + 2.0 ** -126 * np.maximum(1, np.abs(z)))
+    assert worst.max() <= 0, [(float(z[n]), float(y[t, n]), float(want[n])) for t, n in [np.unravel_index(int(worst.argmax()), worst.shape)]]
