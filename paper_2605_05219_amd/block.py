@@ -48,15 +48,16 @@ def gdn_block_norm_raw(shape, y=0, ldy=0, gate=0, ldg=0, w_post=0, b_post=0, r=0
                                      s, lds, x, ldx, T, stream_ptr))
 
 
-_types = []                                              # torch's fp32 and bf16, in the order of their codes
+_types = ()                                              # torch's fp32 and bf16, in the order of their codes: assigned at once, since threads' first calls may meet
 
 
 def gdn_block_norm(shape: gdn_block_shape, y, gate, w_post, b_post, r, w_pre, b_pre, s, x, stream=None) -> None:
     """See include/gdn_block.h.  y, r, s, x (and a gate per element) are [T][D] tensors with unit inner stride, whose row stride is passed
     on; a gate per token is [T]; w, b and a gate per channel are fp32 [D].  y or r, and s or x, may be None."""
+    global _types
     if not _types:
         import torch
-        _types.extend((torch.float32, torch.bfloat16))
+        _types = (torch.float32, torch.bfloat16)
     of = y if y is not None else r
     size = of.shape if of is not None else ()
     D = shape.D

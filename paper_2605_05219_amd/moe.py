@@ -54,16 +54,17 @@ def gdn_moe_raw(shape, x=0, ldx=0, w_router=0, choice_bias=0, w_gate_up=0, w_dow
                               ids, weights, T, workspace, workspace_bytes, stream_ptr))
 
 
-_types = []
+_types = ()                                              # torch's fp32, bf16 and int32: assigned at once, since threads' first calls may meet
 
 
 def gdn_moe(shape: gdn_moe_shape, x, w_router, choice_bias, w_gate_up, w_down, add, y, ids, weights, workspace, stream=None) -> None:
     """See include/gdn_moe.h.  x, add, y: bf16 [T][D] with unit inner stride, whose row stride is passed on; w_router [E][D] (bf16 or fp32, as the shape
     says), w_gate_up [E][2 F][D] and w_down [E][D][F] bf16, choice_bias fp32 [E], ids int32 and weights fp32 [T][k], all without gaps.
     choice_bias, add, ids and weights may be None."""
+    global _types
     if not _types:
         import torch
-        _types.extend((torch.float32, torch.bfloat16, torch.int32))         # in the order of their codes
+        _types = (torch.float32, torch.bfloat16, torch.int32)
     f32, bf16, i32 = _types
     name, size, device = "gdn_moe", x.shape, _device()
     E, k, D, F = shape.E, shape.k, shape.D, shape.F
