@@ -327,3 +327,29 @@ def test_activations_keep_their_digits_far_out(act, T):
     torch.cuda.synchronize()
     worst = np.abs(f64(y) - want) - ((2 * (arg + 4) + 8) * 2.0 ** -23 * np.abs(want) + 2.0 ** -126 * np.maximum(1, np.abs(z)))
     assert worst.max() <= 0, [(float(z[n]), float(y[t, n]), float(want[n])) for t, n in [np.unravel_index(int(worst.argmax()), worst.shape)]]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [-1, 0, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11])
+@pytest.mark.parametrize("T,N,K", [(5, 50, 8192), (37, 17, 4160), (70, 73, 4096), (33, 9, 6144)])
+@pytest.mark.parametrize("gated", [False, True])
+def test_every_term_of_a_long_sum_counts(knob, shape, T, N, K, gated):
+    """Small whole numbers, whose products and sums fp32 holds exactly in any order: the outputs are equal, so no term is lost or taken twice."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(K + N)
+    whole = lambda *n: torch.randint(-2, 3, n, generator=gen, device="cuda").bfloat16()  # noqa: E731
+    x, behind = whole(T, K), torch.full((N + 40, K), float("nan"), dtype=torch.bfloat16, device="cuda")
+    w, up = behind.clone()[:N], behind.clone()[:N]                    # (what lies behind a weight's last row counts for nothing)
+    w.copy_(whole(N, K))
+    up.copy_(whole(N, K))
+    res = torch.zeros(T, -(-N // 4) * 4, device="cuda")[:, :N]
+    res.copy_(torch.randint(-1000, 1000, (T, N), generator=gen, device="cuda"))
+    bias = torch.randint(-9, 9, (N,), generator=gen, device="cuda").float()
+    y = torch.full((T, -(-N // 4) * 4), 77.0, device="cuda")[:, :N]
+    knob(shape)
+    LN.gdn_linear_act(x, w, bias, y, "none", up if gated else None, None, res, 0.5)
+    z = f64(x) @ f64(w).T + f64(bias)
+    want = 0.5 * z * (f64(x) @ f64(up).T if gated else 1.0) + f64(res)
+    assert np.abs(f64(x)).sum(1).max() * 2 < 2 ** 24 and np.abs(2 * want).max() + 2000 < 2 ** 24      # exact in fp32, in halves too
+    torch.cuda.synchronize()
+    assert np.array_equal(f64(y), want)

@@ -437,3 +437,37 @@ def test_sigmoids_of_far_logits(T, normalise, logits):
     c.run().check()
     if normalise and logits[0] != float("-inf"):
         assert abs(float(c.weights[0].sum()) - 2.5) < 1e-5
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [-1, 0, 2, 3, 6])
+@pytest.mark.parametrize("T,E,k,D,F", [(1, 8, 4, 2048, 1088), (30, 6, 1, 4096, 576), (30, 5, 4, 1088, 2048), (200, 4, 2, 2048, 1024), (700, 6, 1, 576, 4096)])
+def test_every_term_of_the_sums_counts(knob, shape, T, E, k, D, F):
+    """Small whole numbers: the first products are exact in fp32 in any order, h is rounded where the definition rounds it, and the second products and the sum of the choices, of
+    weights that are powers of two, are exact again.  So y is equal to the last bit, and no term is lost or taken twice."""
+    import torch
+    if shape == 6 and T > 32:
+        pytest.skip("few tokens are at most 32")
+    knob(shape)
+    c = Call(T, E, k, D, F, "none", add=True, seed=D)
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    whole = lambda t: t.copy_(torch.randint(-1, 2, t.shape, generator=gen, device="cuda"))  # noqa: E731
+    for t in (c.x, c.gu, c.down):
+        whole(t)
+    c.add.copy_(torch.randint(-100, 100, c.add.shape, generator=gen, device="cuda"))
+    if k > 1:
+        c.wr.zero_()                                                  # equal keys: the first k, 1 / k each
+    c.run()
+    torch.cuda.synchronize()
+    ids, p, _ = mo.route(f64(c.x), f64(c.wr), None, k)
+    assert np.array_equal(c.ids.cpu().numpy(), ids) and np.array_equal(f64(c.weights), np.full((T, k), 1.0 / k)) and np.allclose(p, 1.0 / k)
+    x, gu, down, want, size = f64(c.x), f64(c.gu), f64(c.down), f64(c.add), np.abs(f64(c.add))
+    for e in range(E):
+        t = np.nonzero((ids == e).any(1))[0]
+        g, u = x[t] @ gu[e, :F].T, x[t] @ gu[e, F:].T
+        assert not t.size or (np.abs(g).max() < 2 ** 12 and np.abs(u).max() < 2 ** 12)
+        h = mo.to_bf16(g * u / k)
+        want[t] += h @ down[e].T
+        size[t] += np.abs(h) @ np.abs(down[e]).T
+    assert size.max() * k < 2 ** 24                                  # (in units of 1 / k)
+    assert np.array_equal(f64(c.y), mo.to_bf16(want))
