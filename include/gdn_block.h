@@ -24,7 +24,7 @@
  *   a wider buffer.  T = 0 is legal and does nothing.
  * Arithmetic: fp32 throughout, the mean first and then the squares of what is left; x is made of the s that is held in fp32,
  * so that each output is rounded once.  A row whose mean square and eps together lie below 2^-126 (eps = 0 with a row of zeros, for
- * one) has no norm: NaN or infinities.
+ * one) or whose squares add up past fp32's range (values of 10^17 and more) has no norm: NaN, infinities or zeros.
  * In place: s and x may each be the same rows as y, r or a gate per element (the same address, row stride and element size);
  * s and x may not share a byte, nor any output one with an input in another way.
  * Errors: GDN_ERR_NULL, _ALIGN, _SHAPE (an unknown type, norm or gate, D out of range, a row stride smaller than its row, an eps

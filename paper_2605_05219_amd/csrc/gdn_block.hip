@@ -1,13 +1,23 @@
 // gdn_block_norm: the residual stream between two blocks, with the norms on both sides (see include/gdn_block.h).
 //
-// s = r + scale g N_post(y), x = N_pre(s): a few flops for every element read or written once, so memory traffic is all that
-// bounds it.  A row is held in registers from its loads to its stores, 8 adjacent elements to a piece (16 bytes of bf16), so that neither the squares of
-// what the mean leaves nor the second norm read it again: one piece to a thread and as many waves as the row has pieces for, up to 16 (rows of up to 8192), then two or
-// four.  A norm costs one barrier, and few instructions: the vector units, 4 clocks to each instruction of a wave, are not far behind the memory (with the waves' sums added up by every
-// thread, and divisions, 928 instructions for 8 elements of two layer norms kept them busy for three quarters of the time: 1777 rows of 5120 43 us, now 32).  8192 rows of 2048 in
-// bf16, the norm in front alone, 26 us (134 MB: 5.2 TB/s, a plain copy of 2 GiB 4.9), with one behind the block and a gate per channel 28; 1777 rows of 5120 out of wider
-// buffers, two layer norms with a gate per element and a stream in fp32, 32 (127 MB: 3.9 TB/s); 4096 rows of 8192 50; 1000 of 32768 63 (4.2 TB/s; with
-// all operands and weights asked for at once the registers spill: 89); a single row 2.4, which a call's host time of 7 covers.
+// s = r + scale g N_post(y), x = N_pre(s): a few flops for every element read or written once, so memory traffic is all that bounds it.
+//
+// A row is held in registers from its loads to its stores, 8 adjacent elements to a piece (16 bytes of bf16), so that neither the squares of
+// what the mean leaves nor the second norm read it again: one piece to a thread and as many waves as the row has pieces for, up to 16
+// (rows of up to 8192), then two or four.  A norm costs one barrier, and few instructions: the vector units, 4 clocks to each instruction
+// of a wave, are not far behind the memory (with the waves' sums added up by every thread, and divisions, 928 instructions for 8 elements of
+// two layer norms kept them busy for three quarters of the time: 1777 rows of 5120 43 us, now 32).
+//
+// us, and read and written (a plain copy of 2 GiB 4.9 TB/s):
+//   8192 rows of 2048, bf16, the norm in front alone                     26   134 MB   5.2 TB/s     (with one behind the block and a gate per channel 28)
+//   8192 of 2048, block and stream fp32, a norm on both sides            46.5 235      5.05
+//   1777 of 5120 out of wider buffers, two layer norms, a gate, fp32 stream   32   127      3.9
+//   4096 of 4096, bf16, both sides                                       23   134      5.75
+//   2048 of 10240, block and stream fp32                                 61.5 294      4.8
+//   1000 of 32768, bf16                                                  62   262      4.2          (fp32 block and stream 128, 459 MB, 3.6)
+//   a single row 2.4, which a call's host time of 7 covers
+// Rows of more than 16384 need more than the 128 registers that 16 waves leave each: 16 to 18 of them, 64 with block and stream in fp32, go to memory and
+// back (all operands and weights asked for at once: more of them, 89 us for 1000 of 32768).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -256,7 +266,9 @@ void launch_kernel(const BlockArgs& a, unsigned blocks, unsigned threads, hipStr
 template <int PIECES>
 hipError_t launch(BlockArgs a, hipStream_t stream) {
     a.waves = (a.D + 512 * PIECES - 1) / (512 * PIECES);
-    // as many workgroups as are on the chip at once (24 waves to a compute unit, by their registers): 4096 rows of 8192, 16 waves each, 58 us in 256 workgroups, 82 in 320
+    // As many workgroups as are on the chip at once, at 24 waves to a compute unit, which is what the registers of the kernels of rows up to 8192 leave (4096 rows of 8192, 16 waves
+    // each, 58 us in 256 workgroups, 82 in 320).  With block and stream in fp32 it is 20, and 16 for wider rows, so that some widths (fp32: up to 2048, 2561 to 4096, 5121 to 6144; any type:
+    // 8193 to 12288, 16385 to 24576) get more workgroups than fit: 8192 rows of 2048 and 4096 of 4096 in fp32 run at 5.05 TB/s all the same, 2048 of 10240 at 4.8.
     const int per_block = a.waves == 1 ? 4 : a.waves;            // waves
     const unsigned blocks = (unsigned)std::min<int64_t>(a.waves == 1 ? (a.T + 3) / 4 : a.T, (int64_t)chip_cus() * (24 / per_block)), threads = 64u * per_block;
     if (a.in_f32) a.s_f32 ? launch_kernel<PIECES, true, true>(a, blocks, threads, stream) : launch_kernel<PIECES, true, false>(a, blocks, threads, stream);

@@ -19,7 +19,8 @@
 //      fit in one round (512 x 8224: 260 tiles of 128 outputs for 256 compute units, 208 of 160; 27 us against 36 of shape 4, 32 of shape 0)
 // The same tiles make gdn_linear_act's products, with the activation, gate, factor and residual between the sums and the store (act_epilogue), and those of a mixture
 // of experts, on rows that a list names (launch_expert_product).  For at most 1024 rows gdn_linear_act has six kernels more, shapes 6 to 11 (gdn_few_kernel.h).
-//   8192 x 2 x 6144 x 2048 with SiLU and gate 305 us (1350 TFLOP/s; a library product of 8192 x 12288 x 2048 alone 361), the activation under 3 % of it;
+//   8192 x 2 x 6144 x 2048 with SiLU and gate 304 to 325 us by card (1270 to 1355 TFLOP/s; a library product of 8192 x 12288 x 2048 alone 361), the activation under 3 % of it;
+//   8192 x 2048 x 6144 onto the stream, the way back, 168 us with it in bf16, 180 in fp32 (1226, 1147 TFLOP/s; a library product alone 141), 2048 rows onto fp32 53 (52);
 //   1401 x 1733 x 1600 with GELU, an fp32 residual and fp32 outputs 21.6: 10 of them its 25 k steps (what a compute unit is sent, 80 GB/s), 2.5 the GELU, 1.6 the residual,
 //   8 the beginning and the end of one round of 154 tiles (shape 0 35, 3 25.7, 5 36; three workgroups of shape 3 with three stages each 23.8, tiles of 96 x 128 24.7).
 // The products are v_mfma_f32_16x16x32_bf16: half the accumulator traffic per flop of the 32 x 32 x 16 instruction, at the same rate on
@@ -229,6 +230,8 @@ __device__ __forceinline__ void act_epilogue(const typename EpiArgs<EPI>::type& 
                 if (tok >= n_rows || col + OPL > a.N) continue;
                 float scale = a.scale;
                 if constexpr (epi_expert(EPI)) {
+                    // (an expert's inner row, weighted, is rounded to bf16 below: the second product's operand on the bf16 matrix cores.  Whole, it would be two operands, twice that
+                    // product's instructions and twice the bytes here; so y is off by 2.3e-3 (norms, against 64 bits), of which its own rounding is 1.7e-3)
                     tok = list[tok];
                     if (EPI == EPI_EXPERT_GATED) scale = a.weights[tok];
                 }
@@ -771,13 +774,18 @@ LinearPlan plan_linear(int64_t T, int32_t N, int32_t K) {
     return forced >= 0 ? LinearPlan{forced, 0, N} : plan_tiles(T, N, K, false);
 }
 
-// ---- the kernels of few rows, shapes 6 .. 11: 16 rows of x with 8, 16, 32 rows of w, then 32 with each.  A compute unit takes rows of x, which it finds in L2, at 90 KB a us,
-// rows of w at 50, and at 40 where workgroups of other rows ask for them at the same time; memory sends 5.5 TB/s, and 3 us go to the beginning and the end.  So a narrow weight
-// wants many workgroups, that is few of its rows each, until x, which each of them reads whole, outweighs them; and a compute unit with one workgroup more than the others is
-// waited for, and its first loads cost 0.8 us more.  us, T x N x K, weights in the memory-side cache, in shapes 6 / 7 / 8 / 9 / 10 / 11 and 64 x 64 tiles: 16 x 2048 x 6144 7.3 / 8.1 / 10.2 /
-// 7.7 / 8.6 / 10.9, 19; 48 14.8 / 11.9 / 10.0 / 14.1 / 8.9 / 11.2, 19.6; 128 31 / 21 / 16 / 30 / 16.1 / 12.4, 20.8; weights from memory 48 rows 19.9 / 16.9 / 14.5 / 18.4 / 12.2 / 16.2, 29.8.  With
-// few outputs they are the better for more rows too: 174 x 44 x 7232 7.7, tiles 22; 491 x 298 x 3712 9.3, 14; from some 1000 rows on the tiles always were (3737 x 19 x 3648 32, tiles
-// 13.8).  Over 350 problems (1 to 1024 rows, N 8 to 8192, K 256 to 8192) the choice is 2 to 3 % from the best on average, and 7 to 12 % or more in one of twenty.
+// ---- the kernels of few rows, shapes 6 .. 11: 16 rows of x with 8, 16, 32 rows of w, then 32 with each.
+// The estimate: a compute unit takes rows of x, which it finds in L2, at 90 KB a us, rows of w at 50, and at 40 where workgroups of other rows ask for them at the
+// same time; memory sends 5.5 TB/s, and 3 us go to the beginning and the end.  So a narrow weight wants many workgroups, that is few of its rows each, until x, which each of
+// them reads whole, outweighs them; and a compute unit with one workgroup more than the others is waited for, and its first loads cost 0.8 us more.
+//   us, N 2048, K 6144, shapes 6 / 7 / 8 / 9 / 10 / 11, and 64 x 64 tiles
+//     weights in the memory-side cache   16 rows   7.3 /  8.1 / 10.2 /  7.7 /  8.6 / 10.9, 19
+//                                        48       14.8 / 11.9 / 10.0 / 14.1 /  8.9 / 11.2, 19.6
+//                                       128       31   / 21   / 16   / 30   / 16.1 / 12.4, 20.8
+//     weights from memory                48       19.9 / 16.9 / 14.5 / 18.4 / 12.2 / 16.2, 29.8
+// With few outputs they are the better for more rows too: 174 x 44 x 7232 7.7, tiles 22; 491 x 298 x 3712 9.3, 14; from some 1000 rows on the tiles always were
+// (3737 x 19 x 3648 32, tiles 13.8).  Over 350 problems (1 to 1024 rows, N 8 to 8192, K 256 to 8192) the choice is 2 to 3 % from the best on average, and 7 to 12 % or more in one
+// of twenty.
 constexpr int FEW = 6, FEW_ROWS = 1024;
 struct FewShape { int rt, wr; };
 constexpr FewShape FEW_SHAPES[6] = {{1, 8}, {1, 16}, {1, 32}, {2, 8}, {2, 16}, {2, 32}};

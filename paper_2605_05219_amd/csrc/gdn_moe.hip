@@ -82,11 +82,13 @@ void launch_choices(const MoeArgs& a, hipStream_t stream) {
     by_experts(a.E, [&](auto p) { hipLaunchKernelGGL((moe_route_kernel<decltype(p)::value>), dim3((unsigned)((a.T + 3) / 4)), dim3(256), 0, stream, a); });
 }
 hipError_t launch_few(const MoeArgs& a, hipStream_t stream) {
-    // Every workgroup of the first product chooses anew where all of them are on the chip at once: a launch less.  In more rounds the choice, 2 us and with
-    // many experts 4, comes once in each.  us, chosen inside / by a launch: 1 token of 128 experts, k 8, F 768 25.2 / 27.0; 2 35 / 35; 4 of 512, F 256 20.8 / 22.6, 8 29.7 / 27.3, 32
-    // 93 / 65; 16 of 512, k 10, F 512 209 / 172.  Workgroups of 16 of F, two to a compute unit, or of 8, three: the smaller spread more evenly until there are many.  us, 16 / 8 (and workgroups
-    // of 16): 128 experts, k 8, D 2048, F 768: 23.8 / 22.8 (384), 35.3 / 33.1 (768), 57 / 55 (1536), 98 / 101 (3072); 256, F 512: 25.4 / 28.4 (512, of which those of 8 are more than a round); 64, k 6, F 1408:
-    // 30.9 / 29.8 (528), 73 / 75 (2112).
+    // Where all workgroups of the first product are on the chip at once, each of them chooses anew: a launch less.  In more rounds the choice, 2 us and
+    // with many experts 4, would come once in each.
+    //   us, chosen inside / by a launch:  128 experts, k 8, F 768: 1 token 25.2 / 27.0, 2 35 / 35;  512 experts, F 256: 4 20.8 / 22.6, 8 29.7 / 27.3, 32 93 / 65;
+    //                                     512, k 10, F 512: 16 209 / 172
+    // Workgroups of 16 of F, two to a compute unit, or of 8, three: the smaller spread more evenly until there are many, or until they are more than a round.
+    //   us, of 16 / of 8, by the workgroups of 16 that there are:  128 experts, k 8, D 2048, F 768: 384 23.8 / 22.8, 768 35.3 / 33.1, 1536 57 / 55, twice that 98 / 101;
+    //                                     256, F 512: 512 25.4 / 28.4;  64, k 6, F 1408: 528 30.9 / 29.8, 2112 73 / 75
     const int64_t wide_ones = (int64_t)a.T * a.k * (a.F / 16), cus = chip_cus();
     const bool inside = wide_ones <= 2 * cus, wide = inside ? 2 * wide_ones > 3 * cus : wide_ones > 6 * cus;
     hipError_t e;
@@ -137,20 +139,22 @@ hipError_t launch_products(const MoeArgs& a, int shape, hipStream_t stream) {
 }
 
 constexpr int FEW = 6, MOST_FEW = 32;
-// The kernels of few tokens save launches, some 10 us, and read an expert once for every token that chooses it, out of the caches after the first (20 MB a us).  us, theirs / tiles, by
-// tokens: 128 experts, k 8, D 2048, F 768: 1 25 / 33, 4 58 / 67, 8 102 / 108, 16 187 / 165; 8, 2, 2048, 2048: 2 26 / 32, 4 42 / 49, 8 66 / 57; 512, 10, 2048, 512: 8 98 / 115, 16 172 / 188, 32
-// 314 / 291; 1024, 8, 1024, 256: 16 54 / 64, 32 91 / 100.
+// The kernels of few tokens save launches, some 10 us, and read an expert once for every token that chooses it, out of the caches after the first (20 MB a us).
+//   us, theirs / tiles, by tokens:  128 experts, k 8, D 2048, F 768: 1 25 / 33, 4 58 / 67, 8 102 / 108, 16 187 / 165
+//                                   8, 2, 2048, 2048: 2 26 / 32, 4 42 / 49, 8 66 / 57
+//                                   512, 10, 2048, 512: 8 98 / 115, 16 172 / 188, 32 314 / 291;  1024, 8, 1024, 256: 16 54 / 64, 32 91 / 100
 bool few_pays(const gdn_moe_shape& s, int64_t T) {
     const double choices = (double)T * s.k, distinct = s.E * (1.0 - std::pow(1.0 - (double)s.k / s.E, (double)T));
     return (choices - distinct) * 6.0 * s.D * s.F <= 10.0 * 20e6;
 }
 
 std::atomic<int32_t> g_moe_shape{-1};
-// By the rounds of tiles over the chip that the two products would take, if the choice is even: larger tiles read the weights for fewer row tiles each, smaller ones are
-// more, which few experts or narrow ones need to occupy the chip, and less of them is empty.  us, tiles of 64 x 64 / 128 x 128 / 256 x 256: 64 experts, k 6, D 2048, F 1408: 512 tokens (48
-// rows an expert) 271 / 274 / 331, 1024 365 / 301 / 353, 1536 477 / 420 / 380, 8192 1826 / 1231 / 1099; 128 experts, k 8, F 768, 2048 tokens 526 / 453 / 474; 8 experts, k 5, D 2112, F 256,
-// 363 tokens (227 rows) 43 / 59 / 93; 8 experts, k 8, D 768, F 576, 791 tokens 65 / 59 / 78.  Over 142 calls (4 to 512 experts, D 256 to 4096, F 128 to 2048, 33 to 8192 tokens) the tiles that are
-// chosen are 0.6 % from the best of the three on average, 13 % at most; chosen by the rows alone up to 140 %.
+// The tile: by the rounds of tiles over the chip that the two products would take, if the choice is even.  Larger tiles read the weights for fewer row tiles each; of smaller
+// ones there are more, which few experts or narrow ones need to occupy the chip, and less of them is empty.
+//   us, tiles of 64 x 64 / 128 x 128 / 256 x 256:  64 experts, k 6, D 2048, F 1408: 512 tokens (48 rows an expert) 271 / 274 / 331, 1024 365 / 301 / 353, 1536 477 / 420 / 380, 8192 1826 / 1231 / 1099
+//                                                  128, 8, 2048, 768: 2048 526 / 453 / 474;  8, 5, 2112, 256: 363 43 / 59 / 93;  8, 8, 768, 576: 791 65 / 59 / 78
+// Over 142 calls (4 to 512 experts, D 256 to 4096, F 128 to 2048, 33 to 8192 tokens) the tiles that are chosen are 0.6 % from the best of the three on average, 13 % at most; chosen
+// by the rows alone up to 140 %.
 //
 // The row tiles that an expert's rows give: their number is near normal, of a variance of its mean, and has a tile more for every whole tile that it passes.
 double row_tiles(double rows, int tile) {

@@ -493,6 +493,7 @@ __global__ void __launch_bounds__(64 * C::WAVES) moe_up_few_kernel(MoeArgs a) { 
     if (threadIdx.x < C::WR / 8) {
         const int piece = threadIdx.x;
         const f32x4 v = (P > 0 ? weight : a.weights[pair]) * (activate(a.act, C::get_sum(sums, 0, piece)) * C::get_sum(sums, 0, piece + C::WR / 8));
+        // (rounded to bf16 as in the tiles, whose second product takes it so: a token's row does not change with how many stand beside it but for the order of fp32 sums)
         *reinterpret_cast<bf16x4*>(a.h + (int64_t)pair * a.F + f0 + 4 * piece) = __builtin_convertvector(v, bf16x4);
     }
 }
