@@ -47,21 +47,23 @@ class FeedForward:
         w, (T, D) = self.w, stream.shape
         like = w["down"]
         rows = lambda cols: lambda n: torch.empty(n, cols, dtype=like.dtype, device=like.device)  # noqa: E731
+        # every buffer before the first launch: what fails here leaves the stream as it was
         x = self._room("x", T, rows(D))
+        inner = w["gate"] if self.experts is None else w.get("shared_gate")
+        h = self._room("h", T, rows(inner.shape[0])) if inner is not None else None
+        if self.experts is not None:
+            out = self._room("out", T, rows(D))
+            ws = self._room("workspace", moe.gdn_moe_workspace_bytes(self.experts, T), lambda n: torch.empty(n, dtype=torch.uint8, device=like.device))
         block.gdn_block_norm(self.norm, y, None, None, None, stream, w["norm"], None, stream if y is not None else None, x)
         if self.experts is None:
-            h = self._room("h", T, rows(w["gate"].shape[0]))
             linear.gdn_linear_act(x, w["gate"], None, h, self.act, w["up"])
             linear.gdn_linear_act(h, w["down"], None, stream, residual=stream)
             return None
-        out = self._room("out", T, rows(D))
         add = None
-        if "shared_gate" in w:
-            h = self._room("h", T, rows(w["shared_gate"].shape[0]))
+        if h is not None:
             linear.gdn_linear_act(x, w["shared_gate"], None, h, self.act, w["shared_up"])
             linear.gdn_linear_act(h, w["shared_down"], None, out)
             add = out
-        ws = self._room("workspace", moe.gdn_moe_workspace_bytes(self.experts, T), lambda n: torch.empty(n, dtype=torch.uint8, device=like.device))
         moe.gdn_moe(self.experts, x, w["router"], w.get("choice_bias"), w["gate_up"], w["down"], add, out, None, None, ws)
         return out
 

@@ -155,3 +155,16 @@ def test_a_step_of_no_tokens_and_one_without_a_block_before_it(experts):
     second = ff.step(torch.zeros(5, 128, device="cuda", dtype=torch.bfloat16), added)
     torch.cuda.synchronize()
     assert torch.equal(alone, added) and (first is None or torch.equal(first, second))
+
+
+@pytest.mark.gpu
+def test_a_step_that_finds_no_buffers_leaves_the_stream_as_it_was():
+    import torch
+    from paper_2605_05219_amd import binding as B
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    stream, y = torch.randn(6, 128, generator=gen, device="cuda"), torch.randn(6, 128, generator=gen, device="cuda").bfloat16()
+    want = stream.clone()
+    with pytest.raises(B.GdnError):                                   # no experts for a token: no workspace has a size
+        FF.FeedForward(FF.random_weights(128, 64, 8, generator=gen), 0).step(y, stream)
+    torch.cuda.synchronize()
+    assert torch.equal(stream, want)
